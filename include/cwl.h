@@ -380,6 +380,63 @@ cwl_status cwl_apply_noalloc(const void* X, int64_t ldx, const void* W, int64_t 
                              cwl_chunk_table table, int32_t window,
                              void* Y, int64_t ldy, int32_t* status_word, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Training a ladder and reporting on answers: what a logit row says about given tokens, the distillation of a teacher's
+ * top logits into a student, and the gradient of the adapter factors.  The paper trains nothing (its ladder is cut from
+ * a trained adapter, Sec. III-C); these calls are what tuning the prefixes of a ladder needs beside the calls above. */
+
+/* Element type of logits and of gradients. */
+typedef enum { CWL_F32 = 0, CWL_BF16 = 1, CWL_F16 = 2 } cwl_dtype;
+#define CWL_MAX_TOP_K 128
+
+/* Log-probabilities of given tokens, with the row's entropy and its top alternatives.  With tau = temperature,
+ *   lse[t] = ln sum_v exp(z_v / tau),  logprob[t] = z_y / tau - lse[t],  entropy[t] = -sum_v q_v ln q_v  (nats),
+ *   q = softmax(z / tau);  top_ids[t, :] are the top_k tokens by (logit descending, index ascending) and
+ *   top_logprobs[t, :] their log-probabilities.
+ * -inf logits contribute nothing (an alternative may be one, with log-probability -inf, when fewer than top_k tokens
+ * are allowed).  A row with NaN or +inf, or of -inf only, gives NaN everywhere and ids of -1.
+ *   logits   DEV [T, V] of `dtype`, row stride ld_logits >= V; rows may start at any element
+ *   targets  DEV int32 [T] or NULL; a negative entry means no token (logprob 0); one >= V gives NaN and flags
+ *            CWL_ERR_INVALID_ARG in *status_word
+ *   logprob  DEV fp32 [T], given exactly when targets is;  lse, entropy  DEV fp32 [T], each may be NULL
+ *   top_ids  DEV int32 [T, top_k], top_logprobs  DEV fp32 [T, top_k]; unused when top_k == 0
+ * The row is read once; fp32 arithmetic.
+ * Errors: INVALID_ARG (NULLs, T < 0, V < 1, top_k outside [0, V], temperature not positive and finite, unknown dtype),
+ * UNSUPPORTED (top_k > CWL_MAX_TOP_K), SHAPE (ld_logits < V, logits not aligned to its type), CUDA.  T == 0 is a no-op. */
+cwl_status cwl_token_logprobs(const void* logits, cwl_dtype dtype, int64_t ld_logits, int32_t T, int32_t V,
+                              const int32_t* targets, float temperature, int32_t top_k,
+                              float* logprob, float* lse, float* entropy, int32_t* top_ids, float* top_logprobs,
+                              int32_t* status_word, void* stream);
+
+/* Distillation from a teacher's top logits: loss and gradient.  Row t has K teacher entries (id_j, u_j); with
+ * q = softmax(z_t / tau) the student's distribution,
+ *   CWL_TEACHER_LOGITS     p = softmax_j(u_j / tau): the teacher renormalised over its entries, p_rest = 0
+ *   CWL_TEACHER_LOGPROBS   p_j = exp(u_j), u_j log-probabilities of the tempered teacher (cwl_token_logprobs gives them);
+ *                          what is left, p_rest = max(0, 1 - sum_j p_j), is one more outcome, matched against
+ *                          q_rest = sum of q outside the entries
+ *   loss[t]      = weight[t] tau^2 ( sum_j p_j ln(p_j / q_{id_j}) + p_rest ln(p_rest / q_rest) )
+ *   dlogits[t,v] = dloss[t] d loss[t] / d z_v
+ *                = dloss[t] weight[t] tau ( q_v (sum_j p_j + p_rest) - p_v - [v not among the entries] p_rest q_v / q_rest )
+ * An entry with a negative id is padding.  Rows of weight 0 give loss 0 and gradient 0 and are not read; so do rows
+ * without entries under CWL_TEACHER_LOGITS.  -inf student logits have q = 0 (loss +inf if the teacher wants one).  A row
+ * with NaN or +inf logits, or of -inf only, gives NaN.  An id that occurs twice counts with the sum of its p.  An id >= V
+ * counts as padding and flags CWL_ERR_INVALID_ARG in *status_word.
+ *   logits          DEV [T, V] of `dtype`, row stride ld_logits >= V; rows may start at any element
+ *   teacher_ids     DEV int32 [T, K], teacher_values DEV fp32 [T, K], both with row stride ld_teacher >= K
+ *   weight          DEV fp32 [T] or NULL (all 1);  dloss  DEV fp32 [T] or NULL (all 1): the upstream gradient of loss[t]
+ *   loss            DEV fp32 [T] or NULL;  dlogits  DEV [T, V] of `dtype`, row stride ld_dlogits >= V, or NULL; not both
+ *                   NULL.  dlogits may be logits itself (same pointer and stride): each row is read before it is written.
+ * One call gives both where the upstream gradient is known (weight carries a mean); a first call with dlogits == NULL and
+ * a second with loss == NULL and dloss are forward and backward.  Logits are read once and dlogits written once.
+ * Errors: INVALID_ARG (NULLs, T < 0, V < 1, K < 1, bad temperature, dtype or mode), UNSUPPORTED (K > CWL_MAX_TOP_K; rows
+ * of more than CWL_MAX_DISTILL_ROW_BYTES bytes), SHAPE (strides, alignment to the type), CUDA.  T == 0 is a no-op. */
+typedef enum { CWL_TEACHER_LOGITS = 0, CWL_TEACHER_LOGPROBS = 1 } cwl_teacher_mode;
+#define CWL_MAX_DISTILL_ROW_BYTES (8 * 208 * 1024)
+cwl_status cwl_distill_topk(const void* logits, cwl_dtype dtype, int64_t ld_logits, int32_t T, int32_t V,
+                            const int32_t* teacher_ids, const float* teacher_values, int64_t ld_teacher, int32_t K,
+                            cwl_teacher_mode mode, float temperature, const float* weight, const float* dloss,
+                            float* loss, void* dlogits, int64_t ld_dlogits, int32_t* status_word, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -26,10 +26,13 @@ EXPORTS = ["cwl_status_string", "cwl_version", "cwl_score_tokens", "cwl_score_to
            "cwl_apply_rows", "cwl_ladder_workspace_bytes", "cwl_ladder_build",
            "cwl_apply_noalloc_scratch_need", "cwl_apply_noalloc", "cwl_prefetch_next", "cwl_apply_mode",
            "cwl_batch_align_workspace_bytes", "cwl_batch_align", "cwl_set_pair_budget",
-           "cwl_apply_batch_workspace_bytes", "cwl_apply_batch"]
+           "cwl_apply_batch_workspace_bytes", "cwl_apply_batch", "cwl_token_logprobs", "cwl_distill_topk"]
 NOALLOC_SCRATCH_BYTES = 8 << 20
 WINDOW_CAUSAL, WINDOW_CENTRED = 0, 1
 MAX_BATCH = 4
+MAX_TOP_K = 128
+TEACHER_MODES = {"logits": 0, "logprobs": 1}
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
 class CwlError(RuntimeError):
@@ -195,6 +198,13 @@ def _declare(L):
         L.cwl_apply_noalloc.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                                         C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                                         CChunkTable, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+        L.cwl_token_logprobs.restype = C.c_int
+        L.cwl_token_logprobs.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_float, C.c_int32,
+                                         C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.cwl_distill_topk.restype = C.c_int
+        L.cwl_distill_topk.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64,
+                                       C.c_int32, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                                       C.c_void_p, C.c_void_p]
     return L
 
 
@@ -567,6 +577,74 @@ def cwl_apply_noalloc(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor
         _p(X), X.stride(0), _p(W), W.stride(0), _p(A), A.stride(0) if R else 0, _p(B), B.stride(0) if R else 0,
         T, d_in, d_out, R, ct, int(window), _p(Y), Y.stride(0), _p(status_word), _stream_ptr(stream)))
     return Y
+
+
+class TokenLogprobs:
+    """What cwl_token_logprobs writes for up to `T` rows, in one device allocation: ``lse``, ``entropy`` and (with
+    targets) ``logprob`` fp32 [T], ``top_ids`` int32 and ``top_logprobs`` fp32 [T, top_k].  A decode loop keeps one."""
+
+    def __init__(self, T: int, top_k: int = 0, with_targets: bool = True, device="cuda"):
+        self.T, self.top_k = int(T), int(top_k)
+        n = self.T
+        buf = torch.empty(3 * n + 2 * n * self.top_k, dtype=torch.float32, device=device)
+        self.lse, self.entropy = buf[:n], buf[n:2 * n]
+        self.logprob = buf[2 * n:3 * n] if with_targets else None
+        self.top_logprobs = buf[3 * n:3 * n + n * self.top_k].view(n, self.top_k)
+        self.top_ids = buf[3 * n + n * self.top_k:].view(torch.int32).view(n, self.top_k)
+        self._ptrs = (_p(self.logprob), _p(self.lse), _p(self.entropy), _p(self.top_ids), _p(self.top_logprobs))
+
+
+def cwl_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top_k: int = 0, temperature: float = 1.0,
+                       out: Optional[TokenLogprobs] = None, status_word: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> TokenLogprobs:
+    """Log-probability of each row's target token (negative: none), log-sum-exp, entropy in nats and the ``top_k`` most
+    likely tokens of softmax(logits / temperature); logits fp32, bf16 or fp16 [T, V] on the device."""
+    assert logits.is_cuda and logits.dtype in _DTYPES and logits.dim() == 2 and logits.stride(1) == 1
+    T, V = logits.shape
+    if out is None:
+        out = TokenLogprobs(T, top_k, targets is not None, logits.device)
+    assert out.T == T and out.top_k == top_k and (out.logprob is not None) == (targets is not None)
+    if targets is not None:
+        assert targets.is_cuda and targets.dtype == torch.int32 and targets.is_contiguous() and targets.numel() == T
+    _check("cwl_token_logprobs", lib().cwl_token_logprobs(
+        _p(logits), _DTYPES[logits.dtype], logits.stride(0) if T > 1 else max(V, logits.stride(0)), T, V, _p(targets),
+        temperature, top_k, *out._ptrs, _p(status_word), _stream_ptr(stream)))
+    return out
+
+
+def cwl_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values: torch.Tensor, teacher: str = "logits",
+                     temperature: float = 1.0, weight: Optional[torch.Tensor] = None, dloss: Optional[torch.Tensor] = None,
+                     want_loss: bool = True, want_grad: bool = True, loss: Optional[torch.Tensor] = None,
+                     dlogits: Optional[torch.Tensor] = None, status_word: Optional[torch.Tensor] = None,
+                     stream: Optional[torch.cuda.Stream] = None):
+    """Distillation of a teacher's top entries (``teacher_ids`` int32 and ``teacher_values`` fp32 [T, K]; negative ids are
+    padding) into the student's logits [T, V] (fp32, bf16 or fp16).  ``teacher`` says what the values are: "logits",
+    renormalised over the entries, or "logprobs" of the tempered teacher, whose remaining mass is one more outcome.
+    Returns (loss fp32 [T] or None, dlogits or None); ``dlogits`` may be ``logits`` itself."""
+    assert logits.is_cuda and logits.dtype in _DTYPES and logits.dim() == 2 and logits.stride(1) == 1
+    T, V = logits.shape
+    K = teacher_ids.shape[1]
+    assert teacher_ids.is_cuda and teacher_ids.dtype == torch.int32 and teacher_ids.shape == (T, K) and teacher_ids.stride(1) == 1
+    assert teacher_values.is_cuda and teacher_values.dtype == torch.float32 and teacher_values.shape == (T, K)
+    assert teacher_values.stride() == teacher_ids.stride()
+    for t in (weight, dloss):
+        assert t is None or (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == T)
+    if want_loss and loss is None:
+        loss = torch.empty(T, dtype=torch.float32, device=logits.device)
+    if want_grad and dlogits is None:
+        dlogits = torch.empty(T, V, dtype=logits.dtype, device=logits.device)
+    if loss is not None:
+        assert loss.is_cuda and loss.dtype == torch.float32 and loss.is_contiguous() and loss.numel() == T
+    if dlogits is not None:
+        assert dlogits.is_cuda and dlogits.dtype == logits.dtype and dlogits.shape == (T, V) and dlogits.stride(1) == 1
+    many = T > 1
+    _check("cwl_distill_topk", lib().cwl_distill_topk(
+        _p(logits), _DTYPES[logits.dtype], logits.stride(0) if many else max(V, logits.stride(0)), T, V, _p(teacher_ids),
+        _p(teacher_values), teacher_ids.stride(0) if many else max(K, teacher_ids.stride(0)), K, TEACHER_MODES[teacher],
+        temperature, _p(weight), _p(dloss), _p(loss), _p(dlogits),
+        0 if dlogits is None else dlogits.stride(0) if many else max(V, dlogits.stride(0)), _p(status_word),
+        _stream_ptr(stream)))
+    return loss, dlogits
 
 
 def bf16_from_bits(bits, device="cuda") -> torch.Tensor:

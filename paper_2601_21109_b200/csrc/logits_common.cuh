@@ -1,0 +1,205 @@
+// Shared pieces of the kernels that walk logit rows of several types (logprobs.cu, distill.cu): 16-byte access to rows
+// that may start at any element, the online softmax triple, clusters of CTAs that share a row.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math_constants.h>
+
+#include "cwl_common.cuh"
+
+namespace cwl {
+
+constexpr float kRowLog2e = 1.4426950408889634f;
+constexpr float kRowLn2 = 0.6931471805599453f;
+constexpr float kMaskedExponent = -1.0e30f;   // stands for -inf where a weight of 0 is multiplied with its exponent
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// maximum that a NaN on either side wins: the maximum of a row then tells a bad row by itself
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+// true for a row maximum that leaves the softmax undefined: NaN, +inf, or nothing but -inf
+__device__ __forceinline__ bool bad_max(float m) { return !(m < CUDART_INF_F) || m == -CUDART_INF_F; }
+
+// Element types of a logit row: how many sit in 16 bytes, how they become fp32 and how a gradient is rounded back.
+template <typename T> struct Elem;
+template <> struct Elem<float> {
+  static constexpr int kVec = 4;
+  static __device__ __forceinline__ float load(const float* p) { return __ldg(p); }
+  static __device__ __forceinline__ float to_float(float v) { return v; }
+  static __device__ __forceinline__ float from_float(float v) { return v; }
+  static __device__ __forceinline__ void unpack(const uint4& q, float (&f)[4]) {
+    f[0] = __uint_as_float(q.x); f[1] = __uint_as_float(q.y); f[2] = __uint_as_float(q.z); f[3] = __uint_as_float(q.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+  static __device__ __forceinline__ uint32_t masked() { return 0xFF800000u; }   // -inf
+};
+template <> struct Elem<__nv_bfloat16> {
+  static constexpr int kVec = 8;
+  static __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat162float(__ldg(p)); }
+  static __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+  static __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
+  static __device__ __forceinline__ void unpack(const uint4& q, float (&f)[8]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ uint32_t masked() { return 0xFF80FF80u; }
+};
+template <> struct Elem<__half> {
+  static constexpr int kVec = 8;
+  static __device__ __forceinline__ float load(const __half* p) { return __half2float(__ldg(p)); }
+  static __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+  static __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
+  static __device__ __forceinline__ void unpack(const uint4& q, float (&f)[8]) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+      f[2 * i] = v.x; f[2 * i + 1] = v.y;
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 v = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ uint32_t masked() { return 0xFC00FC00u; }
+};
+
+// Online softmax statistics of what a thread (then a warp, a CTA, a cluster) has seen:
+//   m = max z,  S = sum 2^t,  U = sum t 2^t,  t = (z - m) c,  c = log2(e) / temperature.
+struct RowStat { float m, S, U; };
+
+// Moves a triple to a new (not smaller) maximum; m == -inf means nothing was seen.  A NaN or +inf maximum is told by m
+// alone, S and U are then of no account.
+__device__ __forceinline__ void rebase(RowStat& a, float m_new, float c) {
+  const float dt = (a.m - m_new) * c;     // <= 0; -inf for an empty triple
+  const float sc = exp2_fast(dt);
+  a.U = sc > 0.f ? (a.U + dt * a.S) * sc : 0.f;
+  a.S = sc > 0.f ? a.S * sc : 0.f;
+  a.m = m_new;
+}
+__device__ __forceinline__ void absorb(RowStat& a, float z, float c) {
+  // z - m first: exact when z == m however large m is, so rows of the type's lowest value keep their uniform softmax
+  const float t = fmaxf((z - a.m) * c, kMaskedExponent);
+  const float e = exp2_fast(t);
+  a.S += e;
+  a.U = fmaf(t, e, a.U);
+}
+__device__ __forceinline__ RowStat merge(RowStat a, RowStat b, float c) {
+  const float m = max_nan(a.m, b.m);
+  if (m == -CUDART_INF_F) return a;       // both empty
+  rebase(a, m, c);
+  rebase(b, m, c);
+  a.S += b.S;
+  a.U += b.U;
+  return a;
+}
+
+// Where the elements of a row sit for one of the `n_cta` CTAs that share it: scalars up to the first 16-byte boundary
+// (CTA 0), whole 16-byte vectors dealt out in contiguous runs, scalars after the last vector (last CTA).
+struct RowSlice {
+  int head;        // elements before the first vector of the row
+  int v0, v1;      // this CTA's vectors
+  int e0, e1;      // this CTA's elements, contiguous
+  int own_head, own_tail, tail_start;
+};
+template <typename T>
+__device__ __forceinline__ RowSlice row_slice(const T* z, int V, int cta, int n_cta) {
+  RowSlice s;
+  const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(z) & 15u);
+  s.head = min((int)(((16u - off) & 15u) / sizeof(T)), V);
+  const int n_vec = (V - s.head) / Elem<T>::kVec;
+  const int per = (n_vec + n_cta - 1) / n_cta;
+  s.v0 = min(cta * per, n_vec);
+  s.v1 = min(s.v0 + per, n_vec);
+  s.tail_start = s.head + n_vec * Elem<T>::kVec;
+  s.own_head = cta == 0 ? s.head : 0;
+  s.own_tail = cta == n_cta - 1 ? V - s.tail_start : 0;
+  s.e0 = cta == 0 ? 0 : s.head + s.v0 * Elem<T>::kVec;
+  s.e1 = cta == n_cta - 1 ? V : s.head + s.v1 * Elem<T>::kVec;
+  return s;
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// address of this shared-memory object in another CTA of the cluster
+__device__ __forceinline__ uint32_t peer_shared(const void* p, uint32_t cta) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(cta));
+  return r;
+}
+__device__ __forceinline__ float ld_peer_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ unsigned long long ld_peer_u64(uint32_t addr) {
+  unsigned long long v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_peer_f32(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+
+// Launch in clusters of `cluster` CTAs, chained to the launch ahead like launch_chained.
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_clusters(bool chained, int cluster, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,
+                                   cudaStream_t stream, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  int n = 0;
+  attr[n].id = cudaLaunchAttributeClusterDimension;
+  attr[n].val.clusterDim.x = cluster; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
+  ++n;
+  if (chained) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n].val.programmaticStreamSerializationAllowed = 1;
+    ++n;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
+inline size_t elem_size(cwl_dtype t) { return t == CWL_F32 ? 4 : 2; }
+inline bool known_dtype(cwl_dtype t) { return t == CWL_F32 || t == CWL_BF16 || t == CWL_F16; }
+
+}  // namespace cwl
