@@ -437,6 +437,27 @@ cwl_status cwl_distill_topk(const void* logits, cwl_dtype dtype, int64_t ld_logi
                             cwl_teacher_mode mode, float temperature, const float* weight, const float* dloss,
                             float* loss, void* dlogits, int64_t ld_dlogits, int32_t* status_word, void* stream);
 
+/* Gradient of the adapter factors of cwl_apply (cwl_apply_mode), dY being the gradient of the loss with respect to Y.
+ * With g_t[j] the gate of row t (rank mask, scale, cross-fade weight) and H' = g o (X A) as the forward pass computes it,
+ *   G = g o (dY B^T),   dA = X^T G,   dB = H'^T dY
+ * (the gradient with respect to X is cwl_apply itself on transposed factors: dX = dY W^T + G A^T, i.e. X := dY,
+ * W := W^T, A := B^T, B := A^T with the same table; W is frozen and has no gradient).
+ * bf16 operands, fp32 accumulation on the tensor cores; H' and G are rounded to bf16 once, as the forward pass rounds H'.
+ *   X DEV bf16 [T, d_in]; dY DEV bf16 [T, d_out]; A DEV bf16 [d_in, R]; B DEV bf16 [R, d_out]; finite
+ *   table, window, window_mode   as for cwl_apply_mode; rows outside every chunk contribute nothing
+ *   dA DEV [d_in, R], dB DEV [R, d_out] of grad_dtype (CWL_F32 or CWL_BF16), overwritten
+ *   workspace   DEV, at least cwl_apply_grads_workspace_bytes(T, d_in, d_out, R) bytes, 256-byte aligned
+ * Supported shapes: d_in, d_out, R multiples of 16, 16 <= R <= CWL_MAX_RANK; all base pointers 16-byte aligned and rows
+ * a multiple of 16 bytes apart.  T == 0 writes zeros.  Results do not depend on timing (fixed order of all sums).
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED, WORKSPACE, CUDA; TIMEOUT through *status_word. */
+size_t     cwl_apply_grads_workspace_bytes(int32_t T, int32_t d_in, int32_t d_out, int32_t R);
+cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY, int64_t lddy,
+                           const void* A, int64_t lda, const void* B, int64_t ldb,
+                           int32_t T, int32_t d_in, int32_t d_out, int32_t R,
+                           cwl_chunk_table table, int32_t window, int32_t window_mode,
+                           void* dA, int64_t ldda, void* dB, int64_t lddb, cwl_dtype grad_dtype,
+                           void* workspace, size_t workspace_bytes, int32_t* status_word, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

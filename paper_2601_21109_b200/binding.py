@@ -26,7 +26,8 @@ EXPORTS = ["cwl_status_string", "cwl_version", "cwl_score_tokens", "cwl_score_to
            "cwl_apply_rows", "cwl_ladder_workspace_bytes", "cwl_ladder_build",
            "cwl_apply_noalloc_scratch_need", "cwl_apply_noalloc", "cwl_prefetch_next", "cwl_apply_mode",
            "cwl_batch_align_workspace_bytes", "cwl_batch_align", "cwl_set_pair_budget",
-           "cwl_apply_batch_workspace_bytes", "cwl_apply_batch", "cwl_token_logprobs", "cwl_distill_topk"]
+           "cwl_apply_batch_workspace_bytes", "cwl_apply_batch", "cwl_token_logprobs", "cwl_distill_topk",
+           "cwl_apply_grads_workspace_bytes", "cwl_apply_grads"]
 NOALLOC_SCRATCH_BYTES = 8 << 20
 WINDOW_CAUSAL, WINDOW_CENTRED = 0, 1
 MAX_BATCH = 4
@@ -205,6 +206,13 @@ def _declare(L):
         L.cwl_distill_topk.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64,
                                        C.c_int32, C.c_int, C.c_float, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
                                        C.c_void_p, C.c_void_p]
+        L.cwl_apply_grads_workspace_bytes.restype = C.c_size_t
+        L.cwl_apply_grads_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+        L.cwl_apply_grads.restype = C.c_int
+        L.cwl_apply_grads.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                      C.c_int32, C.c_int32, C.c_int32, C.c_int32, CChunkTable, C.c_int32, C.c_int32,
+                                      C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_size_t,
+                                      C.c_void_p, C.c_void_p]
     return L
 
 
@@ -645,6 +653,38 @@ def cwl_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_va
         0 if dlogits is None else dlogits.stride(0) if many else max(V, dlogits.stride(0)), _p(status_word),
         _stream_ptr(stream)))
     return loss, dlogits
+
+
+def cwl_apply_grads_workspace_bytes(T: int, d_in: int, d_out: int, R: int) -> int:
+    return int(lib().cwl_apply_grads_workspace_bytes(T, d_in, d_out, R))
+
+
+def cwl_apply_grads(X: torch.Tensor, dY: torch.Tensor, A: torch.Tensor, B: torch.Tensor, table: DeviceChunkTable, window: int,
+                    dA: Optional[torch.Tensor] = None, dB: Optional[torch.Tensor] = None,
+                    grad_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None,
+                    status_word: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None,
+                    centred: bool = False):
+    """Gradients (dA [d_in, R], dB [R, d_out]) of the adapter factors of ``cwl_apply`` under ``table``, from the activations X
+    and the output's gradient dY (bf16); fp32 or bf16, of the type of ``dA`` and ``dB`` where they are given."""
+    for t in (X, dY, A, B):
+        assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 2 and t.stride(1) == 1
+    T, d_in = X.shape
+    d_out, R = dY.shape[1], A.shape[1]
+    assert dY.shape[0] == T and A.shape[0] == d_in and B.shape == (R, d_out)
+    if dA is None:
+        dA = torch.empty(d_in, R, dtype=grad_dtype, device=X.device)
+    if dB is None:
+        dB = torch.empty(R, d_out, dtype=dA.dtype, device=X.device)
+    assert dA.is_cuda and dA.dtype in _DTYPES and dA.shape == (d_in, R) and dA.stride(1) == 1
+    assert dB.is_cuda and dB.dtype == dA.dtype and dB.shape == (R, d_out) and dB.stride(1) == 1
+    if workspace is None:
+        workspace = torch.empty(cwl_apply_grads_workspace_bytes(T, d_in, d_out, R), dtype=torch.uint8, device=X.device)
+    _check("cwl_apply_grads", lib().cwl_apply_grads(
+        _p(X), X.stride(0) if T > 1 else max(d_in, X.stride(0)), _p(dY), dY.stride(0) if T > 1 else max(d_out, dY.stride(0)),
+        _p(A), A.stride(0), _p(B), B.stride(0), T, d_in, d_out, R, table.c_struct(), int(window),
+        WINDOW_CENTRED if centred else WINDOW_CAUSAL, _p(dA), dA.stride(0), _p(dB), dB.stride(0), _DTYPES[dA.dtype],
+        _p(workspace), workspace.numel(), _p(status_word), _stream_ptr(stream)))
+    return dA, dB
 
 
 def bf16_from_bits(bits, device="cuda") -> torch.Tensor:

@@ -49,6 +49,8 @@
 #include <unordered_map>
 
 #include "cwl_common.cuh"
+#include "gate.cuh"
+#include "tcgen05_common.cuh"
 
 namespace cwl {
 namespace {
@@ -75,8 +77,6 @@ constexpr int kGroupM = 16;         // pair rows (256 tokens each) per raster gr
 constexpr int kPairsPlanned = 74;   // most CTA pairs ever launched (148 SMs); plans never use more
 constexpr int kMaxSplits = 16;      // split factor of the shrink along d_in
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;
-
-struct RowGate { float w_in, w_out; int r_in, r_out; };  // g[j] = w_in [j < r_in] + w_out [j < r_out]
 
 // Host-side schedule of one launch.  Everything the device needs to enumerate its items.
 struct Plan {
@@ -129,32 +129,7 @@ struct GroupMaps {
 };
 
 // ------------------------------------------------------------------------------------------ PTX
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ unsigned long long global_timer() {
-  unsigned long long t;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  return t;
-}
-// The CTA's wait limit in ns sits 12 bytes after its abort flag in shared memory (set once at kernel start).
-__device__ __forceinline__ unsigned long long wait_limit(volatile int* abort_flag) {
-  return *reinterpret_cast<volatile unsigned long long*>(abort_flag + 3);
-}
 #ifdef CWL_TEST_HOOKS
 // Test build only (cwl_trace_set): the leader CTA of one chosen pair writes %globaltimer readings of its producer, its
 // MMA issuer and its first epilogue thread into a caller-supplied array; the slots are listed in cwl_test_hooks.h.
@@ -168,19 +143,6 @@ __device__ int g_trace_pair = -1;
 #define CWL_TRACE(i) do {} while (0)
 #define CWL_TRACE_N(base, i) do {} while (0)
 #endif
-
-// Bounded wait.  Returns false when the limit ran out or another role already gave up.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const unsigned long long t0 = global_timer();
-  for (uint32_t spins = 1;; ++spins) {
-    if (mbar_try_wait(bar, parity)) return true;
-    if ((spins & 255u) == 0) {
-      if (*abort_flag) return false;
-      if (global_timer() - t0 > wait_limit(abort_flag)) { *abort_flag = 1; return false; }
-    }
-  }
-}
 
 // TMA load into THIS CTA's shared memory whose bytes are counted on the pair leader's mbarrier
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t leader_bar, int x, int y) {
@@ -230,12 +192,6 @@ __device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
   asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ void prefetch_tmap(const CUtensorMap* map) {
-  asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
-}
-
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
 __device__ __forceinline__ void tmem_alloc(uint32_t dst_smem, uint32_t cols) {
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(cols) : "memory");
@@ -262,42 +218,11 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                ::"r"(bar), "h"(both) : "memory");
 }
-// 32 consecutive fp32 columns of this thread's TMEM lane
-__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
-        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
-        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-      : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-
-// Shared-memory matrix descriptor, 128-byte swizzle (layout code 2), descriptor version 1.
-// lbo / sbo are byte offsets: for the K-major operand sbo = distance between 8-row groups (lbo unused);
-// for the N-major operand lbo = distance between 64-column atoms, sbo = distance between 8-deep K groups.
-__device__ __forceinline__ uint64_t make_smem_desc(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
-  uint64_t d = 0;
-  d |= (uint64_t)((saddr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)((lbo >> 4) & 0x3FFFu) << 16;
-  d |= (uint64_t)((sbo >> 4) & 0x3FFFu) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
-}
 
 // Instruction descriptor of kind::f16: fp32 accumulate, bf16 x bf16, A K-major, B N-major.
 __host__ __device__ constexpr uint32_t make_idesc(int m, int n) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (0u << 15) | (1u << 16) | ((uint32_t)(n >> 3) << 17) |
          ((uint32_t)(m >> 4) << 24);
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-  return *reinterpret_cast<uint32_t*>(&v);
 }
 
 __device__ __forceinline__ void epilogue_barrier() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -415,61 +340,6 @@ __device__ __forceinline__ bool get_item(int i, int b, int sh_begin, const Apply
   it.n_blk1 = (ks == pl.split_k - 1) ? pl.nkb1 : 0;
   set_widths(it);
   return true;
-}
-
-// Per-row gate from the chunk table (Sec. III-C rank mask and scale, Sec. III-D cross-fade weight).
-__device__ __forceinline__ RowGate row_gate(int t, const ApplyParams& p) {
-  RowGate g{0.f, 0.f, 0, 0};
-  if (p.row_gates != nullptr) {
-    if (t < p.T) {
-      const cwl_row_gate d = p.row_gates[t];
-      g.r_in = min(max(d.rank_in, 0), p.R);
-      g.w_in = d.lambda * d.scale_in;
-      if (d.lambda < 1.f) {
-        g.r_out = min(max(d.rank_out, 0), p.R);
-        g.w_out = (1.f - d.lambda) * d.scale_out;
-      }
-    }
-    return g;
-  }
-  const cwl_chunk_table& tb = p.table;
-  const int C = min(*tb.n_chunks, tb.capacity);
-  if (t < p.T && C > 0 && t >= tb.offsets[0] && t < tb.offsets[C]) {
-    int lo = 0, hi = C;                            // offsets[lo] <= t < offsets[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (tb.offsets[mid] <= t) lo = mid; else hi = mid;
-    }
-    const int c = lo, j = t - tb.offsets[c];
-    float lam = 1.f;
-    int c_in = c, c_out = c;                       // configurations carrying lam and 1 - lam
-    if (p.window_mode == CWL_WINDOW_CENTRED) {
-      // the window lies around the join: floor(w/2) rows before it, ceil(w/2) rows after it; where a short chunk's
-      // two windows meet, the rows belong to the join that opened the chunk
-      const int before = p.window >> 1, after = p.window - before;
-      const int len = tb.offsets[c + 1] - tb.offsets[c];
-      if (c > 0 && !(tb.flags[c] & 1) && j < after) {
-        lam = (float)(before + j + 1) / (float)(p.window + 1);
-        c_out = c - 1;
-      } else if (c + 1 < C && !(tb.flags[c + 1] & 1) && len - j <= before) {
-        lam = (float)(before - (len - j) + 1) / (float)(p.window + 1);
-        c_in = c + 1;
-      }
-    } else if (c > 0 && !(tb.flags[c] & 1) && j < p.window) {
-      lam = (float)(j + 1) / (float)(p.window + 1);
-      c_out = c - 1;
-    }
-    g.r_in = min(max(tb.rank[c_in], 0), p.R);
-    g.w_in = lam * tb.scale[c_in];
-    if (lam < 1.f) {
-      g.r_out = min(max(tb.rank[c_out], 0), p.R);
-      g.w_out = (1.f - lam) * tb.scale[c_out];
-    }
-  }
-  return g;
-}
-__device__ __forceinline__ float gate_at(const RowGate& g, int j) {
-  return (j < g.r_in ? g.w_in : 0.f) + (j < g.r_out ? g.w_out : 0.f);
 }
 
 // Bounded acquire-wait until *word >= target.
@@ -1311,67 +1181,6 @@ Plan make_plan(int T, int d_in, int n_proj, const int* d_out, int R, int pairs, 
   next_slot = (next_slot + 1) % 64;
   if (n_entries < 64) ++n_entries;
   return pl;
-}
-
-// ------------------------------------------------------------------------------- host: TMA maps
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiledFn encode_fn() {
-  static EncodeTiledFn fn = []() -> EncodeTiledFn {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-      return nullptr;
-    return reinterpret_cast<EncodeTiledFn>(f);
-  }();
-  return fn;
-}
-
-struct MapKey {
-  const void* ptr; uint64_t inner, outer, ld; uint32_t box_inner, box_outer;
-  bool operator==(const MapKey& o) const {
-    return ptr == o.ptr && inner == o.inner && outer == o.outer && ld == o.ld && box_inner == o.box_inner &&
-           box_outer == o.box_outer;
-  }
-};
-struct MapKeyHash {
-  size_t operator()(const MapKey& k) const {
-    size_t h = reinterpret_cast<size_t>(k.ptr);
-    for (uint64_t v : {k.inner, k.outer, k.ld, (uint64_t)k.box_inner, (uint64_t)k.box_outer})
-      h = h * 0x9E3779B97F4A7C15ull + v;
-    return h;
-  }
-};
-
-// bf16 row-major [outer, inner] with row stride ld (elements), box = box_inner x box_outer, 128B swizzle.
-// Rows and columns outside the tensor read as zero.  Descriptors depend only on the key: cached.
-bool make_map(CUtensorMap* out, const void* ptr, uint64_t inner, uint64_t outer, uint64_t ld,
-              uint32_t box_inner, uint32_t box_outer) {
-  static std::mutex mu;
-  static std::unordered_map<MapKey, CUtensorMap, MapKeyHash> cache;
-  const MapKey key{ptr, inner, outer, ld, box_inner, box_outer};
-  {
-    std::lock_guard<std::mutex> lock(mu);
-    auto it = cache.find(key);
-    if (it != cache.end()) { *out = it->second; return true; }
-  }
-  EncodeTiledFn fn = encode_fn();
-  if (fn == nullptr) return false;
-  cuuint64_t dims[2] = {inner, outer};
-  cuuint64_t strides[1] = {ld * 2};
-  cuuint32_t box[2] = {box_inner, box_outer};
-  cuuint32_t estr[2] = {1, 1};
-  CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return false;
-  std::lock_guard<std::mutex> lock(mu);
-  if (cache.size() > 4096) cache.clear();
-  cache.emplace(key, *out);
-  return true;
 }
 
 // CTA pairs that can be resident at once (clusters of 2 need both SMs in one GPC); 74 when no device answers

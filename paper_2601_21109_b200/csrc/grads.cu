@@ -1,0 +1,450 @@
+// cwl_apply_grads: gradient of the adapter factors under a chunk table.
+//
+//   Y = X W + H' B,  H' = g o (X A)  (g: the per-row gate of cwl_apply)
+//   G = g o (dY B^T),   dA = X^T G,   dB = H'^T dY
+//
+// Two launches of tcgen05 products whose narrow side is the ladder rank R:
+//   SHRINK  one output tile per 128 rows: P = X A and Q = dY B^T (K = d_in and d_out), gated and rounded to bf16 as the
+//           forward pass rounds H', so that dB is the gradient of the projection that was computed;
+//   FOLD    one output tile per 128 columns of X or dY: dA = X^T G and dB^T = dY^T H' (K = T).
+// X and dY are read by both: no output of FOLD can be summed before all of d_in / d_out went through SHRINK for its rows.
+// The K loop of a tile is split over the CTAs of a cluster where the tiles alone do not fill the GPU; the partial
+// accumulators meet in distributed shared memory in a fixed order, so results do not depend on timing.
+//
+// Roles per CTA: warp 0 = TMA producer, warp 1 = tcgen05.mma issuer and owner of the tensor memory, warps 2..5 move the
+// accumulator to shared memory; all warps reduce and store.  SHRINK reads the rows of X / dY K-major; A is N-major and
+// B K-major, as they lie in memory.  FOLD reads X / dY M-major (their columns are the output rows) and G / H' N-major.
+// Every wait is bounded: when one runs out the CTA raises CWL_ERR_TIMEOUT, stores nothing and still meets its cluster.
+#include "cwl_common.cuh"
+#include "gate.cuh"
+#include "tcgen05_common.cuh"
+
+namespace cwl {
+namespace {
+
+constexpr int kGM = 128;                        // rows of an accumulator tile = TMEM lanes
+constexpr int kGK = 64;                         // K elements per stage
+constexpr int kGThreads = 192;
+constexpr int kGLeftBytes = kGM * kGK * 2;      // 16 KB of the wide operand per stage
+constexpr int kGBoxBytes = 64 * kGK * 2;        // one 64-column box
+constexpr int kGMaxStages = 8;
+constexpr int kGMaxCluster = 8;
+constexpr unsigned long long kGWaitLimitNs = 2000000000ull;
+
+enum : int { PHASE_SHRINK = 0, PHASE_FOLD = 1 };
+
+struct GradMaps { CUtensorMap wide[2], narrow[2]; };   // per side: 0 = X with A / G, 1 = dY with B / H'
+
+struct GradParams {
+  int T, R;
+  int d[2];                    // d_in, d_out
+  int window, window_mode;
+  cwl_chunk_table table;
+  const cwl_row_gate* row_gates;
+  int n_tiles[2], first;       // output tiles per side; the side whose tiles come first (the one with the longer K loop)
+  int n_kb[2];                 // 64-deep K blocks per side
+  int split;                   // CTAs of the cluster that share a tile's K loop
+  int stages, stage_bytes, narrow_bytes, tmem_cols, ring_bytes;
+  __nv_bfloat16* gated[2];     // SHRINK: where side s's result goes: H' (side 0) and G (side 1), [T, R]
+  void* out[2]; int64_t ld[2]; // FOLD: dA, dB
+  int out_f32;
+  unsigned long long wait_limit_ns;
+  int32_t* status_word;
+};
+
+__device__ __forceinline__ void tmem_alloc1(uint32_t dst_smem, uint32_t cols) {
+  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tmem_relinquish1() {
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc1(uint32_t taddr, uint32_t cols) {
+  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void umma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+// kind::f16, fp32 accumulate, bf16 x bf16; a_mn / b_mn: that operand lies with its M / N dimension contiguous
+__device__ __forceinline__ uint32_t grad_idesc(int n, int a_mn, int b_mn) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(kGM >> 4) << 24);
+}
+__device__ __forceinline__ uint32_t grad_cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void grad_cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t grad_peer(uint32_t addr, uint32_t cta) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
+  return r;
+}
+__device__ __forceinline__ float4 ld_peer_v4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float ld_peer1(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+template <int kPhase>
+__global__ void __launch_bounds__(kGThreads)
+grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradParams p) {
+  pdl_launch_dependents();
+  extern __shared__ uint8_t grad_raw[];
+  const uint32_t raw = smem_u32(grad_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;         // swizzled boxes need 1024-byte alignment
+  uint8_t* base_ptr = grad_raw + (base - raw);
+  const uint32_t bars = base + (uint32_t)p.ring_bytes;
+  auto full_bar = [&](int s) { return bars + 8u * s; };
+  auto empty_bar = [&](int s) { return bars + 8u * (kGMaxStages + s); };
+  const uint32_t acc_bar = bars + 8u * (2 * kGMaxStages);
+  uint8_t* misc = base_ptr + p.ring_bytes + 8 * (2 * kGMaxStages + 1) + 8;
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 4);     // its wait limit sits at misc + 16
+  RowGate* gates = reinterpret_cast<RowGate*>(misc + 32);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  // which tile, which share of its K loop
+  const int split = p.split;
+  const int cta = split > 1 ? (int)grad_cluster_rank() : 0;
+  int tile = blockIdx.x / split;
+  int side = p.first;
+  if (tile >= p.n_tiles[side]) { tile -= p.n_tiles[side]; side ^= 1; }
+  const int per = (p.n_kb[side] + split - 1) / split;
+  const int kb0 = min(cta * per, p.n_kb[side]);
+  const int n_blk = min(kb0 + per, p.n_kb[side]) - kb0;
+  const int m0 = tile * kGM;
+  const CUtensorMap* wide = &maps.wide[side];
+  const CUtensorMap* narrow = &maps.narrow[side];
+
+  if (tid == 0) {
+    for (int s = 0; s < kGMaxStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    mbar_init(acc_bar, 1);
+    *abort_flag = 0;
+    *reinterpret_cast<volatile unsigned long long*>(misc + 16) = p.wait_limit_ns;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    prefetch_tmap(wide);
+    prefetch_tmap(narrow);
+  }
+  if (warp == 1) {
+    tmem_alloc1(smem_u32(const_cast<uint32_t*>(tmem_slot)), (uint32_t)p.tmem_cols);
+    tmem_relinquish1();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  pdl_wait();                                            // nothing above reads or writes global memory
+
+  const bool narrow_k_major = kPhase == PHASE_SHRINK && side == 1;      // B [R, d_out]: its K dimension is contiguous
+  if (warp == 0) {
+    if (lane == 0) {
+      const int n_boxes = narrow_k_major ? 1 : (p.R + 63) / 64;
+      const uint32_t tx = (uint32_t)(kGLeftBytes + (narrow_k_major ? p.R * kGK * 2 : n_boxes * kGBoxBytes));
+      int s = 0;
+      uint32_t ph = 0;
+      int issued = 0;
+      bool ok = true;
+      for (int b = 0; b < n_blk; ++b) {
+        if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) { ok = false; break; }
+        const int k = (kb0 + b) * kGK;
+        const uint32_t sa = base + (uint32_t)(s * p.stage_bytes), sb = sa + kGLeftBytes;
+        mbar_expect_tx(full_bar(s), tx);
+        if (kPhase == PHASE_SHRINK) {
+          tma_load_2d(sa, wide, full_bar(s), k, m0);
+        } else {
+          tma_load_2d(sa, wide, full_bar(s), m0, k);
+          tma_load_2d(sa + kGBoxBytes, wide, full_bar(s), m0 + 64, k);
+        }
+        if (narrow_k_major) {
+          tma_load_2d(sb, narrow, full_bar(s), k, 0);
+        } else {
+          for (int j = 0; j < n_boxes; ++j) tma_load_2d(sb + j * kGBoxBytes, narrow, full_bar(s), j * 64, k);
+        }
+        ++issued;
+        if (++s == p.stages) { s = 0; ph ^= 1u; }
+      }
+      if (!ok) {
+        // copies already issued get a bounded chance to land before the CTA goes on
+        for (int back = 1; back <= p.stages && back <= issued; ++back) {
+          const int j = issued - back;
+          const unsigned long long t0 = global_timer();
+          while (!mbar_try_wait(full_bar(j % p.stages), (uint32_t)(j / p.stages) & 1u) && global_timer() - t0 < p.wait_limit_ns) {}
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && n_blk > 0) {
+      const uint32_t idesc = grad_idesc(p.R, kPhase == PHASE_FOLD, !narrow_k_major);
+      // one K step of 16 further on: 32 bytes in a K-major tile, 16 rows of 128 bytes in a box with the other order
+      const uint64_t step_a = kPhase == PHASE_SHRINK ? (16 * 2) >> 4 : (16 * 128) >> 4;
+      const uint64_t step_b = narrow_k_major ? (16 * 2) >> 4 : (16 * 128) >> 4;
+      int s = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int b = 0; b < n_blk; ++b) {
+        if (!mbar_wait(full_bar(s), ph, abort_flag)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t sa = base + (uint32_t)(s * p.stage_bytes), sb = sa + kGLeftBytes;
+        const uint64_t da = kPhase == PHASE_SHRINK ? make_smem_desc(sa, 16, 1024) : make_smem_desc(sa, kGBoxBytes, 1024);
+        const uint64_t db = narrow_k_major ? make_smem_desc(sb, 16, 1024) : make_smem_desc(sb, kGBoxBytes, 1024);
+#pragma unroll
+        for (int kk = 0; kk < kGK / 16; ++kk)
+          umma_bf16(tmem, da + kk * step_a, db + kk * step_b, idesc, (b | kk) ? 1u : 0u);
+        umma_commit(empty_bar(s));
+        if (++s == p.stages) { s = 0; ph ^= 1u; }
+      }
+      if (ok) {
+        umma_commit(acc_bar);
+      } else {
+        // MMAs in flight get a bounded time to retire before the tensor memory is released
+        const unsigned long long t0 = global_timer();
+        while (global_timer() - t0 < 1000000ull) {}
+      }
+    }
+  } else if (kPhase == PHASE_SHRINK) {
+    gates[tid - 64] = row_gate(m0 + tid - 64, p);        // while the main loop runs (a chain of dependent loads)
+  }
+
+  // accumulator -> shared memory, [128][R + 4] fp32 over the ring, which is idle once every MMA has finished
+  const int pitch = p.R + 4;
+  float* dump = reinterpret_cast<float*>(base_ptr);
+  if (warp >= 2) {
+    const int quad = warp & 3, row = quad * 32 + lane;
+    const bool have = n_blk > 0 && mbar_wait(acc_bar, 0, abort_flag);
+    __syncwarp();
+    tc_fence_after();
+    for (int c = 0; c < p.R; c += 32) {
+      uint32_t v[32];
+      if (n_blk > 0) {
+        tmem_ld32(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
+        tmem_ld_wait();
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (c + q * 4 < p.R && (have || n_blk == 0))
+          *reinterpret_cast<float4*>(dump + row * pitch + c + q * 4) =
+              n_blk > 0 ? make_float4(__uint_as_float(v[q * 4]), __uint_as_float(v[q * 4 + 1]), __uint_as_float(v[q * 4 + 2]),
+                                      __uint_as_float(v[q * 4 + 3]))
+                        : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    tc_fence_before();
+  }
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc1(tmem, (uint32_t)p.tmem_cols);
+  }
+  const bool failed = *abort_flag != 0;
+  if (failed && tid == 0) flag_status(p.status_word, CWL_ERR_TIMEOUT);
+  if (split > 1) grad_cluster_barrier();                 // every CTA's partial accumulator lies in its shared memory
+
+  uint32_t peer[kGMaxCluster];
+  const uint32_t dump_addr = base;
+#pragma unroll
+  for (int r = 0; r < kGMaxCluster; ++r) peer[r] = r < split ? (split > 1 ? grad_peer(dump_addr, r) : dump_addr) : 0;
+  auto sum4 = [&](int row, int col) {                    // in the order of the CTAs
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int r = 0; r < kGMaxCluster; ++r) {
+      if (r < split) {
+        const float4 v = ld_peer_v4(peer[r] + (uint32_t)(row * pitch + col) * 4u);
+        a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+      }
+    }
+    return a;
+  };
+  if (!failed) {
+    if (kPhase == PHASE_SHRINK || side == 0) {
+      // rows of the tile are rows of the output: this CTA's share of them, eight columns a thread
+      const int rows = kGM / split, groups = p.R / 8;
+      for (int i = tid; i < rows * groups; i += kGThreads) {
+        const int row = cta * rows + i / groups, col = (i % groups) * 8;
+        const float4 a = sum4(row, col), b = sum4(row, col + 4);
+        if (kPhase == PHASE_SHRINK) {
+          if (m0 + row < p.T) {
+            const RowGate g = gates[row];
+            uint4 q;
+            q.x = pack_bf16(a.x * gate_at(g, col + 0), a.y * gate_at(g, col + 1));
+            q.y = pack_bf16(a.z * gate_at(g, col + 2), a.w * gate_at(g, col + 3));
+            q.z = pack_bf16(b.x * gate_at(g, col + 4), b.y * gate_at(g, col + 5));
+            q.w = pack_bf16(b.z * gate_at(g, col + 6), b.w * gate_at(g, col + 7));
+            *reinterpret_cast<uint4*>(p.gated[side] + (int64_t)(m0 + row) * p.R + col) = q;
+          }
+        } else if (m0 + row < p.d[0]) {
+          if (p.out_f32) {
+            float* o = reinterpret_cast<float*>(p.out[0]) + (int64_t)(m0 + row) * p.ld[0] + col;
+            *reinterpret_cast<float4*>(o) = a;
+            *reinterpret_cast<float4*>(o + 4) = b;
+          } else {
+            __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.out[0]) + (int64_t)(m0 + row) * p.ld[0] + col;
+            *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+          }
+        }
+      }
+    } else {
+      // dB: rows of the tile are columns of the output.  This CTA's share of the R output rows; a warp stores 32
+      // neighbouring columns of one of them.
+      const int cols = p.R / split;
+      for (int i = tid; i < cols * kGM; i += kGThreads) {
+        const int n = cta * cols + i / kGM, m = i % kGM;
+        float a = 0.f;
+#pragma unroll
+        for (int r = 0; r < kGMaxCluster; ++r)
+          if (r < split) a += ld_peer1(peer[r] + (uint32_t)(m * pitch + n) * 4u);
+        if (m0 + m < p.d[1]) {
+          const int64_t at = (int64_t)n * p.ld[1] + m0 + m;
+          if (p.out_f32) reinterpret_cast<float*>(p.out[1])[at] = a;
+          else reinterpret_cast<__nv_bfloat16*>(p.out[1])[at] = __float2bfloat16_rn(a);
+        }
+      }
+    }
+  }
+  if (split > 1) grad_cluster_barrier();                 // nobody leaves while its shared memory is being read
+}
+
+struct GradLaunch {
+  int split, stages, stage_bytes, narrow_bytes, tmem_cols, ring_bytes;
+  size_t smem;
+};
+
+// CTAs a tile's K loop is split over: doubled while all CTAs still fit the GPU at two per SM and each keeps four K blocks.
+int grad_split(int tiles, int min_kb) {
+  int s = 1;
+  while (s < kGMaxCluster && tiles * s * 2 <= 296 && min_kb / (s * 2) >= 4) s *= 2;
+  return s;
+}
+
+GradLaunch grad_launch(int R, int tiles, int min_kb) {
+  GradLaunch l;
+  l.split = grad_split(tiles, min_kb);
+  l.narrow_bytes = ((R + 63) / 64) * kGBoxBytes;
+  l.stage_bytes = kGLeftBytes + l.narrow_bytes;
+  // up to R = 128 a ring of 96 KB lets two CTAs share an SM; above, one CTA takes what the SM has
+  const int budget = R <= 128 ? 96 * 1024 : 192 * 1024;
+  l.stages = budget / l.stage_bytes;
+  if (l.stages > kGMaxStages) l.stages = kGMaxStages;
+  const int dump = (kGM * (R + 4) * 4 + 1023) / 1024 * 1024;
+  l.ring_bytes = l.stages * l.stage_bytes > dump ? l.stages * l.stage_bytes : dump;
+  l.tmem_cols = 32;
+  while (l.tmem_cols < R) l.tmem_cols *= 2;
+  l.smem = (size_t)l.ring_bytes + 1024 + 8 * (2 * kGMaxStages + 1) + 8 + 32 + kGM * sizeof(RowGate);
+  return l;
+}
+
+template <int kPhase>
+cudaError_t launch_phase(const GradMaps& maps, const GradParams& p, const GradLaunch& l, cudaStream_t st) {
+  const cudaError_t e = cudaFuncSetAttribute(grad_kernel<kPhase>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)l.smem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((p.n_tiles[0] + p.n_tiles[1]) * l.split));
+  cfg.blockDim = dim3(kGThreads);
+  cfg.dynamicSmemBytes = l.smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = l.split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = stream_is_capturing(st) ? 1 : 2;
+  return cudaLaunchKernelEx(&cfg, grad_kernel<kPhase>, maps, p);
+}
+
+size_t gated_bytes(int T, int R) { return ((size_t)T * R * 2 + 255) / 256 * 256; }
+
+bool bad_matrix(const void* ptr, int64_t ld, int64_t cols, int elem) {
+  return !aligned16(ptr) || ld < cols || (ld * elem) % 16 != 0;
+}
+
+}  // namespace
+}  // namespace cwl
+
+extern "C" size_t cwl_apply_grads_workspace_bytes(int32_t T, int32_t d_in, int32_t d_out, int32_t R) {
+  if (T <= 0 || d_in <= 0 || d_out <= 0 || R <= 0) return 0;
+  return 2 * cwl::gated_bytes(T, R);
+}
+
+extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY, int64_t lddy,
+                                      const void* A, int64_t lda, const void* B, int64_t ldb,
+                                      int32_t T, int32_t d_in, int32_t d_out, int32_t R,
+                                      cwl_chunk_table table, int32_t window, int32_t window_mode,
+                                      void* dA, int64_t ldda, void* dB, int64_t lddb, cwl_dtype grad_dtype,
+                                      void* workspace, size_t workspace_bytes, int32_t* status_word, void* stream) {
+  using namespace cwl;
+  if (T < 0 || d_in <= 0 || d_out <= 0 || R <= 0 || window < 0) return CWL_ERR_INVALID_ARG;
+  if (window_mode != CWL_WINDOW_CAUSAL && window_mode != CWL_WINDOW_CENTRED) return CWL_ERR_INVALID_ARG;
+  if (grad_dtype != CWL_F32 && grad_dtype != CWL_BF16) return CWL_ERR_INVALID_ARG;
+  if (dA == nullptr || dB == nullptr) return CWL_ERR_INVALID_ARG;
+  if (d_in % 16 != 0 || d_out % 16 != 0 || R % 16 != 0 || R > CWL_MAX_RANK) return CWL_ERR_UNSUPPORTED;
+  const int es = grad_dtype == CWL_F32 ? 4 : 2;
+  if (bad_matrix(dA, ldda, R, es) || bad_matrix(dB, lddb, d_out, es)) return CWL_ERR_SHAPE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (T == 0) {                                          // a sum over no rows
+    CWL_CUDA_TRY(cudaMemset2DAsync(dA, (size_t)ldda * es, 0, (size_t)R * es, d_in, st));
+    CWL_CUDA_TRY(cudaMemset2DAsync(dB, (size_t)lddb * es, 0, (size_t)d_out * es, R, st));
+    return CWL_OK;
+  }
+  if (X == nullptr || dY == nullptr || A == nullptr || B == nullptr) return CWL_ERR_INVALID_ARG;
+  if (table.offsets == nullptr || table.rank == nullptr || table.scale == nullptr || table.flags == nullptr ||
+      table.n_chunks == nullptr || table.capacity < 0)
+    return CWL_ERR_INVALID_ARG;
+  if (bad_matrix(X, ldx, d_in, 2) || bad_matrix(dY, lddy, d_out, 2) || bad_matrix(A, lda, R, 2) || bad_matrix(B, ldb, d_out, 2))
+    return CWL_ERR_SHAPE;
+  if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
+      workspace_bytes < cwl_apply_grads_workspace_bytes(T, d_in, d_out, R))
+    return CWL_ERR_WORKSPACE;
+
+  __nv_bfloat16* H = static_cast<__nv_bfloat16*>(workspace);
+  __nv_bfloat16* G = reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(workspace) + gated_bytes(T, R));
+  GradParams p = {};
+  p.T = T; p.R = R; p.d[0] = d_in; p.d[1] = d_out;
+  p.window = window; p.window_mode = window_mode; p.table = table; p.row_gates = nullptr;
+  p.gated[0] = H; p.gated[1] = G;
+  p.out[0] = dA; p.out[1] = dB; p.ld[0] = ldda; p.ld[1] = lddb; p.out_f32 = grad_dtype == CWL_F32;
+  p.wait_limit_ns = kGWaitLimitNs;
+  p.status_word = status_word;
+
+  GradMaps shrink, fold;
+  const bool maps_ok =
+      make_map(&shrink.wide[0], X, d_in, T, ldx, kGK, kGM) && make_map(&shrink.narrow[0], A, R, d_in, lda, 64, kGK) &&
+      make_map(&shrink.wide[1], dY, d_out, T, lddy, kGK, kGM) && make_map(&shrink.narrow[1], B, d_out, R, ldb, kGK, R) &&
+      make_map(&fold.wide[0], X, d_in, T, ldx, 64, kGK) && make_map(&fold.narrow[0], G, R, T, R, 64, kGK) &&
+      make_map(&fold.wide[1], dY, d_out, T, lddy, 64, kGK) && make_map(&fold.narrow[1], H, R, T, R, 64, kGK);
+  if (!maps_ok) return CWL_ERR_CUDA;
+
+  auto fill = [&](int tiles0, int tiles1, int kb0, int kb1) {
+    p.n_tiles[0] = tiles0; p.n_tiles[1] = tiles1;
+    p.n_kb[0] = kb0; p.n_kb[1] = kb1;
+    p.first = kb1 > kb0 ? 1 : 0;                         // the longer loops start first
+    const GradLaunch l = grad_launch(R, tiles0 + tiles1, kb0 < kb1 ? kb0 : kb1);
+    p.split = l.split; p.stages = l.stages; p.stage_bytes = l.stage_bytes; p.narrow_bytes = l.narrow_bytes;
+    p.tmem_cols = l.tmem_cols; p.ring_bytes = l.ring_bytes;
+    return l;
+  };
+  const int row_tiles = ceil_div(T, kGM), t_blocks = ceil_div(T, kGK);
+  GradLaunch l = fill(row_tiles, row_tiles, ceil_div(d_in, kGK), ceil_div(d_out, kGK));
+  CWL_CUDA_TRY(launch_phase<PHASE_SHRINK>(shrink, p, l, st));
+  l = fill(ceil_div(d_in, kGM), ceil_div(d_out, kGM), t_blocks, t_blocks);
+  CWL_CUDA_TRY(launch_phase<PHASE_FOLD>(fold, p, l, st));
+  return CWL_OK;
+}
