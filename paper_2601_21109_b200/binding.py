@@ -217,8 +217,9 @@ def _declare(L):
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return int(s.cuda_stream)
+    if stream is None:      # the current stream's handle without a stream object around it (3 us less per call)
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return int(stream.cuda_stream)
 
 
 def _p(t: Optional[torch.Tensor]) -> Optional[int]:

@@ -12,6 +12,7 @@ namespace cwl {
 
 constexpr float kRowLog2e = 1.4426950408889634f;
 constexpr float kRowLn2 = 0.6931471805599453f;
+constexpr float kMaskedLogit = -1.0e30f;
 constexpr float kMaskedExponent = -1.0e30f;   // stands for -inf where a weight of 0 is multiplied with its exponent
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -32,6 +33,7 @@ __device__ __forceinline__ bool bad_max(float m) { return !(m < CUDART_INF_F) ||
 template <typename T> struct Elem;
 template <> struct Elem<float> {
   static constexpr int kVec = 4;
+  static constexpr int kZeroBits = 0;     // low bits that are 0 in every value's fp32 form
   static __device__ __forceinline__ float load(const float* p) { return __ldg(p); }
   static __device__ __forceinline__ float to_float(float v) { return v; }
   static __device__ __forceinline__ float from_float(float v) { return v; }
@@ -42,9 +44,20 @@ template <> struct Elem<float> {
     return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
   }
   static __device__ __forceinline__ uint32_t masked() { return 0xFF800000u; }   // -inf
+  // maximum of the elements of n words, NaN wins
+  template <int n> static __device__ __forceinline__ float max_of(const uint32_t (&w)[n]) {
+    float m = __uint_as_float(w[0]);
+#pragma unroll
+    for (int i = 1; i < n; ++i) m = max_nan(m, __uint_as_float(w[i]));
+    return m;
+  }
+  // a word whose -inf (and whatever lies below) became kMaskedLogit: finite, and of weight 0 beside an ordinary maximum
+  static __device__ __forceinline__ uint32_t floor_word(uint32_t w) { return __float_as_uint(fmaxf(__uint_as_float(w), kMaskedLogit)); }
+  static __device__ __forceinline__ void unpack_word(uint32_t w, float (&f)[1]) { f[0] = __uint_as_float(w); }
 };
 template <> struct Elem<__nv_bfloat16> {
   static constexpr int kVec = 8;
+  static constexpr int kZeroBits = 16;
   static __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat162float(__ldg(p)); }
   static __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
   static __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
@@ -66,9 +79,25 @@ template <> struct Elem<__nv_bfloat16> {
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
   static __device__ __forceinline__ uint32_t masked() { return 0xFF80FF80u; }
+  template <int n> static __device__ __forceinline__ float max_of(const uint32_t (&w)[n]) {
+    uint32_t m = w[0];
+#pragma unroll
+    for (int i = 1; i < n; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i]));
+    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ uint32_t floor_word(uint32_t w) {
+    uint32_t y;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(w), "r"(0xF149F149u));     // kMaskedLogit in bf16, twice
+    return y;
+  }
+  static __device__ __forceinline__ void unpack_word(uint32_t w, float (&f)[2]) {
+    f[0] = __uint_as_float(w << 16);
+    f[1] = __uint_as_float(w & 0xFFFF0000u);
+  }
 };
 template <> struct Elem<__half> {
   static constexpr int kVec = 8;
+  static constexpr int kZeroBits = 13;
   static __device__ __forceinline__ float load(const __half* p) { return __half2float(__ldg(p)); }
   static __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
   static __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
@@ -90,6 +119,22 @@ template <> struct Elem<__half> {
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
   static __device__ __forceinline__ uint32_t masked() { return 0xFC00FC00u; }
+  template <int n> static __device__ __forceinline__ float max_of(const uint32_t (&w)[n]) {
+    uint32_t m = w[0];
+#pragma unroll
+    for (int i = 1; i < n; ++i) asm("max.NaN.f16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i]));
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&m));
+    return max_nan(v.x, v.y);
+  }
+  static __device__ __forceinline__ uint32_t floor_word(uint32_t w) {
+    uint32_t y;
+    asm("max.f16x2 %0, %1, %2;" : "=r"(y) : "r"(w), "r"(0xFBFFFBFFu));      // the type's lowest value, twice
+    return y;
+  }
+  static __device__ __forceinline__ void unpack_word(uint32_t w, float (&f)[2]) {
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    f[0] = v.x; f[1] = v.y;
+  }
 };
 
 // Online softmax statistics of what a thread (then a warp, a CTA, a cluster) has seen:
@@ -120,6 +165,104 @@ __device__ __forceinline__ RowStat merge(RowStat a, RowStat b, float c) {
   a.S += b.S;
   a.U += b.U;
   return a;
+}
+
+// A thread's running statistic over batches of 16-byte vectors.  While the maximum is an ordinary number (|m| up to
+// kOrdinaryLogit, and a temperature between 1/100 and 100) an exponent is one multiply-add, t = z c - M with M = m c
+// rounded once, and -inf is replaced beforehand by a finite value of weight 0: for 16-bit types that is one instruction
+// for two elements, and so is the maximum.  6 instructions an element instead of 8, which is what a row of 16-bit logits
+// is bound by.  Beyond, or for other temperatures, t = (z - m) c with the exponent clamped; a thread that has met an
+// extraordinary maximum stays there.
+constexpr float kOrdinaryLogit = 16384.f;
+struct RunningStat {
+  float m, M, S, U;
+  bool ordinary;
+  __device__ __forceinline__ void start(bool temperature_ok) {
+    m = -CUDART_INF_F; M = 0.f; S = 0.f; U = 0.f; ordinary = temperature_ok;
+  }
+  // S and U relative to m itself instead of the rounded M
+  __device__ __forceinline__ void leave_ordinary(float c) {
+    if (ordinary && m != -CUDART_INF_F) {
+      const float d = fmaf(m, c, -M), sc = exp2_fast(-d);
+      U = (U - d * S) * sc;
+      S *= sc;
+    }
+    ordinary = false;
+  }
+  template <typename T, int n>
+  __device__ __forceinline__ void take(const uint4 (&q)[n], float c) {
+    uint32_t w[4 * n];
+#pragma unroll
+    for (int i = 0; i < n; ++i) { w[4 * i] = q[i].x; w[4 * i + 1] = q[i].y; w[4 * i + 2] = q[i].z; w[4 * i + 3] = q[i].w; }
+    take_words<T, 4 * n>(w, Elem<T>::max_of(w), c);
+  }
+  template <typename T, int n>
+  __device__ __forceinline__ void take_words(const uint32_t (&w)[n], float batch_max, float c) {
+    constexpr int kPer = Elem<T>::kVec / 4;
+    const float m_new = max_nan(m, batch_max);
+    if (m_new == -CUDART_INF_F) return;                 // nothing but -inf so far
+    if (ordinary && !(fabsf(m_new) <= kOrdinaryLogit)) leave_ordinary(c);
+    if (ordinary) {
+      if (m_new != m) {
+        const float M_new = m_new * c;
+        const float dt = M - M_new;                     // S == 0 when nothing was seen
+        const float sc = m == -CUDART_INF_F ? 0.f : exp2_fast(dt);
+        U = (U + dt * S) * sc;
+        S *= sc;
+        m = m_new; M = M_new;
+      }
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        float f[kPer];
+        Elem<T>::unpack_word(Elem<T>::floor_word(w[i]), f);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+          const float t = fmaf(f[e], c, -M), x = exp2_fast(t);
+          S += x;
+          U = fmaf(t, x, U);
+        }
+      }
+    } else {
+      RowStat a{m, S, U};
+      if (m_new != m) rebase(a, m_new, c);
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        float f[kPer];
+        Elem<T>::unpack_word(w[i], f);
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) absorb(a, f[e], c);
+      }
+      m = a.m; S = a.S; U = a.U;
+    }
+  }
+  __device__ __forceinline__ void take_scalar(float v, float c) {
+    leave_ordinary(c);
+    const float m_new = max_nan(m, v);
+    if (m_new == -CUDART_INF_F) return;
+    RowStat a{m, S, U};
+    if (m_new != m) rebase(a, m_new, c);
+    absorb(a, v, c);
+    m = a.m; S = a.S; U = a.U;
+  }
+  __device__ __forceinline__ RowStat done(float c) {
+    leave_ordinary(c);
+    return RowStat{m, S, U};
+  }
+};
+inline bool ordinary_temperature(float t) { return t >= 0.01f && t <= 100.f; }
+
+// order-preserving map of a float to 32 bits; -0 and +0 are equal, a NaN (as max_nan makes them) comes above +inf
+__device__ __forceinline__ uint32_t order_key(float v) {
+  const uint32_t b = __float_as_uint(v + 0.0f);
+  return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float key_value(uint32_t k) {
+  return __uint_as_float((k & 0x80000000u) ? (k & 0x7FFFFFFFu) : ~k);
+}
+// a triple rescaled to a maximum that is not smaller; empty triples stay empty
+__device__ __forceinline__ void rescale(RowStat& a, float m_new, float c) {
+  if (m_new == a.m || m_new == -CUDART_INF_F) return;
+  rebase(a, m_new, c);
 }
 
 // Where the elements of a row sit for one of the `n_cta` CTAs that share it: scalars up to the first 16-byte boundary

@@ -27,31 +27,24 @@ struct LogprobParams {
   const void* logits; int64_t ld; int T, V;
   const int32_t* targets;
   float c, inv_temp;          // log2(e) / temperature, 1 / temperature
+  int ordinary;               // temperature within what the short form of the exponent takes
   int top_k;
   float *logprob, *lse, *entropy;
   int32_t* top_ids; float* top_logprobs;
   int32_t* status_word;
 };
 
-// order-preserving map of a float (no NaN) to 32 bits; -0 and +0 are equal
-__device__ __forceinline__ uint32_t order_key(float v) {
-  const uint32_t b = __float_as_uint(v + 0.0f);
-  return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-}
-__device__ __forceinline__ float key_value(uint32_t k) {
-  return __uint_as_float((k & 0x80000000u) ? (k & 0x7FFFFFFFu) : ~k);
-}
 // larger logit first, lower index first among equals: a larger 64-bit number comes first
 __device__ __forceinline__ unsigned long long rank_key(uint32_t key, int idx) {
   return ((unsigned long long)key << 32) | (0xFFFFFFFFu - (uint32_t)idx);
 }
 
 struct LpShared {
-  unsigned long long cand[kMaxCand];           // candidates; then the lists of the whole cluster
-  unsigned long long top[CWL_MAX_TOP_K];       // this CTA's sorted list; in the leader at the end the row's
+  alignas(16) unsigned long long cand[kMaxCand + 2];   // candidates; then the lists of the whole cluster
+  alignas(16) uint32_t cell[kLpThreads];               // order key of every cell's maximum, 0 for an empty cell
+  unsigned long long top[CWL_MAX_TOP_K];               // this CTA's sorted list; in the leader at the end the row's
   RowStat part[kLpWarps];
-  RowStat stat;                                // this CTA's triple, read by the leader
-  alignas(16) uint32_t cell[kLpThreads];       // order key of every cell's maximum, 0 for an empty cell
+  RowStat stat;                                        // this CTA's triple, read by the leader
   uint32_t hist[256];
   int ties[kMaxTies];
   int warp_count[kLpWarps];
@@ -84,56 +77,112 @@ __device__ void append_ties_in_order(LpShared& sh, const T* z, const RowSlice& r
   }
 }
 
+constexpr uint32_t kKeyOfMinusInf = 0x007FFFFFu;
+
+// The want-th largest of the cells' keys, rounded down to its first bits (all that a 16-bit type has, 20 of fp32: a
+// bound that is a little lower admits a few logits more).  One warp: a bit per step, from the first in which the keys differ.
+template <typename T>
+__device__ __forceinline__ uint32_t cell_bound(const uint32_t* cell, int want) {
+  constexpr int kLastBit = Elem<T>::kZeroBits > 0 ? Elem<T>::kZeroBits : 12;
+  const int lane = threadIdx.x & 31;
+  uint32_t k[kLpThreads / 32], hi = 0, lo = 0xFFFFFFFFu;
+#pragma unroll
+  for (int i = 0; i < kLpThreads / 32; ++i) {
+    k[i] = cell[i * 32 + lane];
+    hi = max(hi, k[i]);
+    lo = min(lo, k[i]);
+  }
+  hi = __reduce_max_sync(0xffffffffu, hi);
+  lo = __reduce_min_sync(0xffffffffu, lo);
+  const int first = 31 - __clz((int)(hi ^ lo));          // -1 when all keys are equal
+  uint32_t prefix = first >= 31 ? 0u : hi & ~((2u << first) - 1u);
+  if (first < 0) prefix = hi;
+  for (int bit = first; bit >= kLastBit; --bit) {
+    const uint32_t trial = prefix | (1u << bit);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kLpThreads / 32; ++i) n += k[i] >= trial;
+    if (__reduce_add_sync(0xffffffffu, n) >= want) prefix = trial;
+  }
+  // exact where it can be: a negative 16-bit value has ones below its bits, and -inf is alone in its range of keys
+  if (Elem<T>::kZeroBits > 0) return prefix | ((prefix >> 31) != 0 ? 0u : (1u << kLastBit) - 1u);
+  return prefix >= (kKeyOfMinusInf & ~0xFFFu) && prefix < kKeyOfMinusInf ? kKeyOfMinusInf : prefix;
+}
+
 // The `k` largest rank keys of this CTA's elements, sorted, into sh.top (padded with 0).  sh.cell holds the cell maxima.
 template <typename T>
 __device__ void local_top(LpShared& sh, const T* z, const RowSlice& rs, int k) {
   constexpr int kVec = Elem<T>::kVec;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31;
   const int n = rs.e1 - rs.e0;
   const int want = min(k, n);
-  if (tid == 0) { sh.n_hits = 0; sh.n_cand = 0; sh.n_ties = 0; sh.thr = 0; }
-  if (tid < k) sh.top[tid] = 0ull;
-  __syncthreads();
-  // bound: the want-th largest of the cell maxima (0, below every element's key, when fewer cells hold anything)
-  const uint32_t mine = sh.cell[tid];
-  int above = 0;
-  const uint4* cells = reinterpret_cast<const uint4*>(sh.cell);
-#pragma unroll 8
-  for (int j = 0; j < kLpThreads / 4; ++j) {
-    const uint4 q = cells[j];
-    above += (q.x > mine || (q.x == mine && 4 * j + 0 < tid)) + (q.y > mine || (q.y == mine && 4 * j + 1 < tid)) +
-             (q.z > mine || (q.z == mine && 4 * j + 2 < tid)) + (q.w > mine || (q.w == mine && 4 * j + 3 < tid));
+  if (tid < 32) {
+    const uint32_t bound = cell_bound<T>(sh.cell, want);
+    if (lane == 0) { sh.n_hits = 0; sh.n_cand = 0; sh.n_ties = 0; sh.thr = bound; }
+  } else if (tid - 32 < k) {
+    sh.top[tid - 32] = 0ull;
   }
-  if (above == want - 1) sh.thr = mine;
   __syncthreads();
+  const uint32_t mine = sh.cell[tid];
   uint32_t thr = sh.thr;
-  if (mine >= thr && mine != 0) sh.hits[atomicAdd(&sh.n_hits, 1)] = (uint16_t)tid;
+  const bool hit = mine >= thr && mine != 0;
+  {
+    const unsigned bal = __ballot_sync(0xffffffffu, hit);
+    int at = 0;
+    if (lane == 0 && bal != 0) at = atomicAdd(&sh.n_hits, __popc(bal));
+    at = __shfl_sync(0xffffffffu, at, 0);
+    if (hit) sh.hits[at + __popc(bal & ((1u << lane) - 1u))] = (uint16_t)tid;
+  }
   __syncthreads();
 
+  // a bound below every element's key (fewer nonempty cells than wanted): everything is above it, -inf too
+  const bool all = thr < kKeyOfMinusInf;
+  float bound = all ? -CUDART_INF_F : key_value(thr);
   auto take = [&](float v, int i) {
-    const uint32_t key = order_key(v);
-    if (key > thr) {
+    if (v > bound || all) {
       const int at = atomicAdd(&sh.n_cand, 1);
-      if (at < kMaxCand) sh.cand[at] = rank_key(key, i);
-    } else if (key == thr) {
+      if (at < kMaxCand) sh.cand[at] = rank_key(order_key(v), i);
+    } else if (v == bound) {
       const int at = atomicAdd(&sh.n_ties, 1);
       if (at < kMaxTies) sh.ties[at] = i;
     }
   };
   const int per_cell = (rs.v1 - rs.v0 + kLpThreads - 1) / kLpThreads;
-  const int n_hits = sh.n_hits;
+  const int n_work = sh.n_hits * per_cell;
+  const float inv_per_cell = 1.f / (float)per_cell;
   const uint4* zv = reinterpret_cast<const uint4*>(z + rs.head);
-  for (int w = tid; w < n_hits * per_cell; w += kLpThreads) {
-    const int h = w / per_cell, j = w - h * per_cell;
-    const int i = rs.v0 + sh.hits[h] + j * kLpThreads;
-    if (i < rs.v1) {
-      float f[kVec];
-      Elem<T>::unpack(__ldg(zv + i), f);
+  const uint4 pad = make_uint4(Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked());
+  constexpr int kAhead = 4;                      // second reads in flight per thread
+  for (int w0 = tid; w0 < n_work; w0 += kLpThreads * kAhead) {
+    uint4 q[kAhead];
+    int at[kAhead];
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) take(f[e], rs.head + i * kVec + e);
+    for (int u = 0; u < kAhead; ++u) {
+      const int w = w0 + u * kLpThreads;
+      // w / per_cell: w stays below 2^24 (256 cells of fewer than 2^16 vectors), the quotient is off by at most one
+      int h = (int)((float)w * inv_per_cell);
+      int j = w - h * per_cell;
+      if (j < 0) { --h; j += per_cell; }
+      if (j >= per_cell) { ++h; j -= per_cell; }
+      at[u] = -1;
+      q[u] = pad;
+      if (w < n_work) {
+        const int i = rs.v0 + sh.hits[h] + j * kLpThreads;
+        if (i < rs.v1) { at[u] = i; q[u] = __ldg(zv + i); }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+      if (at[u] >= 0 && Elem<T>::max_of(w) >= bound) {
+        float f[kVec];
+        Elem<T>::unpack(q[u], f);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) take(f[e], rs.head + at[u] * kVec + e);
+      }
     }
   }
-  if (mine >= thr && mine != 0) {
+  if (hit) {
     if (tid < rs.own_head) take(Elem<T>::load(z + tid), tid);
     if (tid < rs.own_tail) take(Elem<T>::load(z + rs.tail_start + tid), rs.tail_start + tid);
   }
@@ -164,11 +213,11 @@ __device__ void local_top(LpShared& sh, const T* z, const RowSlice& rs, int k) {
       __syncthreads();
     }
     thr = prefix;
+    bound = key_value(thr);                       // an element's own key here, and fewer than `want` lie above it
     if (tid == 0) { sh.n_cand = 0; sh.n_ties = 0; }
     __syncthreads();
     for (int i = rs.e0 + tid; i < rs.e1; i += kLpThreads) {
-      const float v = Elem<T>::load(z + i);
-      if (order_key(v) >= thr) take(v, i);
+      take(Elem<T>::load(z + i), i);
     }
     __syncthreads();
     n_cand = sh.n_cand;               // fewer than want
@@ -185,10 +234,18 @@ __device__ void local_top(LpShared& sh, const T* z, const RowSlice& rs, int k) {
     }
     __syncthreads();
   }
+  // place of each candidate = how many come before it, two keys a read
+  if (tid == 0) sh.cand[n_cand] = 0ull;
+  __syncthreads();
+  const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(sh.cand);
   for (int i = tid; i < n_cand; i += kLpThreads) {
     const unsigned long long key = sh.cand[i];
     int before = 0;
-    for (int j = 0; j < n_cand; ++j) before += sh.cand[j] > key;
+#pragma unroll 4
+    for (int j = 0; j < (n_cand + 1) / 2; ++j) {
+      const ulonglong2 o = pairs[j];
+      before += (o.x > key) + (o.y > key);
+    }
     if (before < k) sh.top[before] = key;
   }
 }
@@ -207,26 +264,17 @@ token_logprobs_kernel(const LogprobParams p, const int n_cta) {
   for (int row = blockIdx.x / n_cta; row < p.T; row += n_rows_at_once) {
     const T* z = reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.ld;
     const RowSlice rs = row_slice<T>(z, p.V, cta, n_cta);
-    RowStat acc{-CUDART_INF_F, 0.f, 0.f};
-    bool any = false;
+    RunningStat run;
+    run.start(p.ordinary != 0);
+    bool any = rs.v0 + tid < rs.v1 || tid < rs.own_head || tid < rs.own_tail;
     float z_target = 0.f;
     int target = -1;
     if (cta == 0 && tid == 0 && p.targets != nullptr) {
       target = p.targets[row];
       if (target >= 0 && target < p.V) z_target = Elem<T>::load(z + target);
     }
-    auto take_scalar = [&](float v) {
-      any = true;
-      const float m_new = max_nan(acc.m, v);
-      if (m_new == -CUDART_INF_F) return;
-      if (m_new != acc.m) rebase(acc, m_new, p.c);
-      absorb(acc, v, p.c);
-    };
-    if (tid < rs.own_head) take_scalar(Elem<T>::load(z + tid));
-    if (tid < rs.own_tail) take_scalar(Elem<T>::load(z + rs.tail_start + tid));
     const uint4* zv = reinterpret_cast<const uint4*>(z + rs.head);
     const uint4 pad = make_uint4(Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked());
-    if (rs.v0 + tid < rs.v1) any = true;
     for (int i = rs.v0 + tid; i < rs.v1; i += kLpThreads * kLpBatch) {
       uint4 q[kLpBatch];
 #pragma unroll
@@ -234,32 +282,29 @@ token_logprobs_kernel(const LogprobParams p, const int n_cta) {
         const int at = i + u * kLpThreads;
         q[u] = at < rs.v1 ? __ldg(zv + at) : pad;      // a padding vector (-inf) contributes nothing
       }
-#pragma unroll
-      for (int u = 0; u < kLpBatch; ++u) {
-        float f[kVec];
-        Elem<T>::unpack(q[u], f);
-        float m_new = acc.m;
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) m_new = max_nan(m_new, f[e]);
-        if (m_new == -CUDART_INF_F) continue;
-        if (m_new != acc.m) rebase(acc, m_new, p.c);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) absorb(acc, f[e], p.c);
-      }
+      run.template take<T, kLpBatch>(q, p.c);
     }
-    if (p.top_k > 0) sh.cell[tid] = any ? order_key(acc.m) : 0u;
+    if (tid < rs.own_head) run.take_scalar(Elem<T>::load(z + tid), p.c);
+    if (tid < rs.own_tail) run.take_scalar(Elem<T>::load(z + rs.tail_start + tid), p.c);
+    RowStat acc = run.done(p.c);
+    const uint32_t my_key = order_key(acc.m);
+    if (p.top_k > 0) sh.cell[tid] = any ? my_key : 0u;
+    // the warp's maximum first, one rescaling each, then plain sums
+    rescale(acc, key_value(__reduce_max_sync(0xffffffffu, my_key)), p.c);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
-      RowStat o;
-      o.m = __shfl_xor_sync(0xffffffffu, acc.m, off);
-      o.S = __shfl_xor_sync(0xffffffffu, acc.S, off);
-      o.U = __shfl_xor_sync(0xffffffffu, acc.U, off);
-      acc = merge(acc, o, p.c);
+      acc.S += __shfl_xor_sync(0xffffffffu, acc.S, off);
+      acc.U += __shfl_xor_sync(0xffffffffu, acc.U, off);
     }
     if (lane == 0) sh.part[wid] = acc;
     __syncthreads();
-    RowStat a = sh.part[0];
-    for (int w = 1; w < kLpWarps; ++w) a = merge(a, sh.part[w], p.c);
+    RowStat a = sh.part[lane & (kLpWarps - 1)];        // every warp sums the eight parts in the same order
+    rescale(a, key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), p.c);
+#pragma unroll
+    for (int off = kLpWarps / 2; off > 0; off >>= 1) {
+      a.S += __shfl_xor_sync(0xffffffffu, a.S, off);
+      a.U += __shfl_xor_sync(0xffffffffu, a.U, off);
+    }
     // A NaN cell maximum would order wrongly: a bad row (its maximum says so) lists nothing.  With several CTAs the others
     // may not know yet; what they list is not used then.
     const bool list = p.top_k > 0 && !(a.m != a.m);
@@ -361,7 +406,7 @@ extern "C" cwl_status cwl_token_logprobs(const void* logits, cwl_dtype dtype, in
   if (ld_logits < V) return CWL_ERR_SHAPE;
   if (reinterpret_cast<uintptr_t>(logits) % cwl::elem_size(dtype) != 0) return CWL_ERR_SHAPE;
   cwl::LogprobParams p{logits, ld_logits, T, V, targets, (float)(1.4426950408889634074 / (double)temperature),
-                       (float)(1.0 / (double)temperature), top_k, logprob, lse, entropy, top_ids, top_logprobs, status_word};
+                       (float)(1.0 / (double)temperature), cwl::ordinary_temperature(temperature) ? 1 : 0, top_k, logprob, lse, entropy, top_ids, top_logprobs, status_word};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   switch (dtype) {
     case CWL_F32: CWL_CUDA_TRY(cwl::launch_logprobs<float>(p, st)); break;

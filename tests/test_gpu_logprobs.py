@@ -219,7 +219,7 @@ def test_rows_past_two_to_the_31_elements():
     z = buf.view(T, 1024)[:, :V]
     z.copy_(torch.randn(T, V, device="cuda"))
     o = cwl.cwl_token_logprobs(z, top_k=2)
-    last = z[-4:].float().contiguous()
+    last = z[-4:].contiguous()
     w = cwl.cwl_token_logprobs(last, top_k=2)
     assert torch.equal(o.top_ids[-4:], w.top_ids) and torch.equal(o.lse[-4:], w.lse)
 
