@@ -85,21 +85,22 @@ __device__ __forceinline__ void store_slice(T* d, bool same_phase, const RowSlic
 
 template <typename T>
 __global__ void __launch_bounds__(kDsThreads)
-distill_kernel(const DistillParams p, const int n_cta) {
+distill_kernel(const DistillParams p, const int log2_cta) {
   constexpr int kVec = Elem<T>::kVec;
+  const int n_cta = 1 << log2_cta;
   pdl_launch_dependents();
   extern __shared__ __align__(16) uint8_t ds_raw[];
   __shared__ DsShared sh;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int cta = n_cta > 1 ? (int)cluster_rank() : 0;
-  const int n_rows_at_once = gridDim.x / n_cta;
+  const int n_rows_at_once = gridDim.x >> log2_cta;
   if (n_cta > 1) cluster_barrier();                // the peers run before anything is written to their shared memory
   pdl_wait();
 
-  for (int row = blockIdx.x / n_cta; row < p.T; row += n_rows_at_once) {
+  for (int row = blockIdx.x >> log2_cta; row < p.T; row += n_rows_at_once) {
     const T* z = reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.ld;
     T* d = p.dlogits != nullptr ? reinterpret_cast<T*>(p.dlogits) + (int64_t)row * p.ld_d : nullptr;
-    const RowSlice rs = row_slice<T>(z, p.V, cta, n_cta);
+    const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
     const bool same_phase = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(d)) & 15u) == 0;
     const float w = p.weight != nullptr ? p.weight[row] : 1.f;
     if (w == 0.f) {                                // a row that is not trained on: not read (the whole cluster agrees)
@@ -291,6 +292,8 @@ template <typename T>
 cudaError_t launch_distill(const DistillParams& p, cudaStream_t st) {
   const int64_t row_bytes = (int64_t)p.V * sizeof(T);
   const int c = distill_cluster(p.T, row_bytes);
+  int log2_cta = 0;
+  while ((1 << log2_cta) < c) ++log2_cta;
   // one slice: its vectors, and head and tail scalars in a vector of their own each
   const size_t smem = (size_t)((row_bytes / 16 + c - 1) / c) * 16 + 32;
   if (smem > 40 * 1024) {                          // beyond what a kernel may use without asking
@@ -298,7 +301,7 @@ cudaError_t launch_distill(const DistillParams& p, cudaStream_t st) {
     if (e != cudaSuccess) return e;
   }
   const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
-  return launch_clusters(!stream_is_capturing(st), c, distill_kernel<T>, dim3(rows * c), dim3(kDsThreads), smem, st, p, c);
+  return launch_clusters(!stream_is_capturing(st), c, distill_kernel<T>, dim3(rows * c), dim3(kDsThreads), smem, st, p, log2_cta);
 }
 
 }  // namespace

@@ -265,7 +265,7 @@ __device__ __forceinline__ void rescale(RowStat& a, float m_new, float c) {
   rebase(a, m_new, c);
 }
 
-// Where the elements of a row sit for one of the `n_cta` CTAs that share it: scalars up to the first 16-byte boundary
+// Where the elements of a row sit for one of the 2^log2_cta CTAs that share it: scalars up to the first 16-byte boundary
 // (CTA 0), whole 16-byte vectors dealt out in contiguous runs, scalars after the last vector (last CTA).
 struct RowSlice {
   int head;        // elements before the first vector of the row
@@ -274,12 +274,13 @@ struct RowSlice {
   int own_head, own_tail, tail_start;
 };
 template <typename T>
-__device__ __forceinline__ RowSlice row_slice(const T* z, int V, int cta, int n_cta) {
+__device__ __forceinline__ RowSlice row_slice(const T* z, int V, int cta, int log2_cta) {
+  const int n_cta = 1 << log2_cta;
   RowSlice s;
   const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(z) & 15u);
   s.head = min((int)(((16u - off) & 15u) / sizeof(T)), V);
   const int n_vec = (V - s.head) / Elem<T>::kVec;
-  const int per = (n_vec + n_cta - 1) / n_cta;
+  const int per = (n_vec + n_cta - 1) >> log2_cta;
   s.v0 = min(cta * per, n_vec);
   s.v1 = min(s.v0 + per, n_vec);
   s.tail_start = s.head + n_vec * Elem<T>::kVec;
@@ -307,6 +308,11 @@ __device__ __forceinline__ uint32_t peer_shared(const void* p, uint32_t cta) {
 __device__ __forceinline__ float ld_peer_f32(uint32_t addr) {
   float v;
   asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t ld_peer_u32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
   return v;
 }
 __device__ __forceinline__ unsigned long long ld_peer_u64(uint32_t addr) {

@@ -4,10 +4,10 @@
 //   m = max z,  S = sum e^((z-m)/tau):   lse = m/tau + ln S,   H = ln S - (1/S) sum (z-m)/tau e^((z-m)/tau),
 //   logprob(y) = (z_y - m)/tau - ln S,   top K by (z descending, index ascending)
 //
-// The row is read once.  Every thread keeps the online triple of its own elements (its cell: every 256th 16-byte vector),
-// and the maximum of the triple is at the same time the cell's maximum.  The K-th largest of the cell maxima is a lower
-// bound of the row's K-th largest logit, and only cells whose maximum reaches it can hold one of the top K: about K of
-// 256 cells are read a second time (from L2), and what reaches the bound is sorted in shared memory.
+// The row is read once.  Every thread keeps the online triple of its own elements and the maximum of each of up to eight
+// runs of them (its cells; the batch maxima that the triple needs anyway).  The K-th largest of the half-way maxima of the
+// threads is a lower bound of the row's K-th largest logit, and only cells whose maximum reaches it can hold one of the
+// top K: a few per cent of the row are read a second time (from L2), and what reaches the bound is sorted in shared memory.
 #include <cmath>
 
 #include "logits_common.cuh"
@@ -15,13 +15,16 @@
 namespace cwl {
 namespace {
 
-constexpr int kLpThreads = 256;       // also the number of cells a CTA's elements are dealt to
+constexpr int kLpThreads = 128;       // small blocks, eight to an SM: while one row selects, others stream
 constexpr int kLpWarps = kLpThreads / 32;
 constexpr int kLpBatch = 4;           // 16-byte loads in flight per thread
-constexpr int kMaxCand = 1152;        // logits above the bound kept for sorting; fewer than K nonempty cells hold at most
-                                      // (CWL_MAX_TOP_K - 1) * 8 + 14 elements, which fit
+constexpr int kLpBatchVecs = kLpThreads * kLpBatch;
+constexpr int kSegs = 8;              // cells per thread
+constexpr int kMaxCand = 1152;        // logits above the bound kept for sorting; with fewer than K threads that hold
+                                      // anything a slice has at most (CWL_MAX_TOP_K - 1) * 8 + 14 elements, which fit
 constexpr int kMaxTies = 256;         // logits equal to the bound kept for sorting
 constexpr int kMaxLpCluster = 8;
+constexpr uint32_t kKeyOfMinusInf = 0x007FFFFFu;
 
 struct LogprobParams {
   const void* logits; int64_t ld; int T, V;
@@ -41,16 +44,17 @@ __device__ __forceinline__ unsigned long long rank_key(uint32_t key, int idx) {
 
 struct LpShared {
   alignas(16) unsigned long long cand[kMaxCand + 2];   // candidates; then the lists of the whole cluster
-  alignas(16) uint32_t cell[kLpThreads];               // order key of every cell's maximum, 0 for an empty cell
-  unsigned long long top[CWL_MAX_TOP_K];               // this CTA's sorted list; in the leader at the end the row's
+  uint32_t cell[kSegs * kLpThreads];                   // order key of every cell's maximum, 0 for an empty cell
+  uint32_t half[2 * kLpThreads];                       // the larger of a thread's first four cells, of its last four
+  unsigned long long top[CWL_MAX_TOP_K];               // a CTA's sorted list, read by the leader of its cluster
   RowStat part[kLpWarps];
   RowStat stat;                                        // this CTA's triple, read by the leader
   uint32_t hist[256];
   int ties[kMaxTies];
   int warp_count[kLpWarps];
-  uint16_t hits[kLpThreads];
+  uint16_t hits[kSegs * kLpThreads];
   uint32_t thr;
-  int n_hits, n_cand, n_ties, rest;
+  int n_hits, n_cand, n_ties, rest, n_list;
 };
 static_assert(kMaxLpCluster * CWL_MAX_TOP_K <= kMaxCand, "the cluster's lists are gathered in the candidate buffer");
 
@@ -77,18 +81,18 @@ __device__ void append_ties_in_order(LpShared& sh, const T* z, const RowSlice& r
   }
 }
 
-constexpr uint32_t kKeyOfMinusInf = 0x007FFFFFu;
-
-// The want-th largest of the cells' keys, rounded down to its first bits (all that a 16-bit type has, 20 of fp32: a
-// bound that is a little lower admits a few logits more).  One warp: a bit per step, from the first in which the keys differ.
+// The want-th largest of the threads' half-way maxima, rounded down to its first bits (all that a 16-bit type has, 20 of
+// fp32: a bound that is a little lower admits a few logits more).  One warp: a bit per step, from the first in which the
+// keys differ.
 template <typename T>
-__device__ __forceinline__ uint32_t cell_bound(const uint32_t* cell, int want) {
+__device__ __forceinline__ uint32_t cell_bound(const uint32_t* half, int want) {
   constexpr int kLastBit = Elem<T>::kZeroBits > 0 ? Elem<T>::kZeroBits : 12;
+  constexpr int n = 2 * kLpThreads / 32;
   const int lane = threadIdx.x & 31;
-  uint32_t k[kLpThreads / 32], hi = 0, lo = 0xFFFFFFFFu;
+  uint32_t k[n], hi = 0, lo = 0xFFFFFFFFu;
 #pragma unroll
-  for (int i = 0; i < kLpThreads / 32; ++i) {
-    k[i] = cell[i * 32 + lane];
+  for (int i = 0; i < n; ++i) {
+    k[i] = half[i * 32 + lane];
     hi = max(hi, k[i]);
     lo = min(lo, k[i]);
   }
@@ -99,39 +103,35 @@ __device__ __forceinline__ uint32_t cell_bound(const uint32_t* cell, int want) {
   if (first < 0) prefix = hi;
   for (int bit = first; bit >= kLastBit; --bit) {
     const uint32_t trial = prefix | (1u << bit);
-    int n = 0;
+    int count = 0;
 #pragma unroll
-    for (int i = 0; i < kLpThreads / 32; ++i) n += k[i] >= trial;
-    if (__reduce_add_sync(0xffffffffu, n) >= want) prefix = trial;
+    for (int i = 0; i < n; ++i) count += k[i] >= trial;
+    if (__reduce_add_sync(0xffffffffu, count) >= want) prefix = trial;
   }
   // exact where it can be: a negative 16-bit value has ones below its bits, and -inf is alone in its range of keys
   if (Elem<T>::kZeroBits > 0) return prefix | ((prefix >> 31) != 0 ? 0u : (1u << kLastBit) - 1u);
   return prefix >= (kKeyOfMinusInf & ~0xFFFu) && prefix < kKeyOfMinusInf ? kKeyOfMinusInf : prefix;
 }
 
-// The `k` largest rank keys of this CTA's elements, sorted, into sh.top (padded with 0).  sh.cell holds the cell maxima.
+// Leaves in sh.cand a set that holds the `want` largest rank keys of this CTA's elements; returns its size (at least
+// `want`).  sh.cell and sh.half hold the maxima.
 template <typename T>
-__device__ void local_top(LpShared& sh, const T* z, const RowSlice& rs, int k) {
+__device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const RowSlice& rs, int want) {
   constexpr int kVec = Elem<T>::kVec;
   const int tid = threadIdx.x, lane = tid & 31;
-  const int n = rs.e1 - rs.e0;
-  const int want = min(k, n);
   if (tid < 32) {
-    const uint32_t bound = cell_bound<T>(sh.cell, want);
+    const uint32_t bound = cell_bound<T>(sh.half, want);
     if (lane == 0) { sh.n_hits = 0; sh.n_cand = 0; sh.n_ties = 0; sh.thr = bound; }
-  } else if (tid - 32 < k) {
-    sh.top[tid - 32] = 0ull;
   }
   __syncthreads();
-  const uint32_t mine = sh.cell[tid];
   uint32_t thr = sh.thr;
-  const bool hit = mine >= thr && mine != 0;
-  {
-    const unsigned bal = __ballot_sync(0xffffffffu, hit);
-    int at = 0;
-    if (lane == 0 && bal != 0) at = atomicAdd(&sh.n_hits, __popc(bal));
-    at = __shfl_sync(0xffffffffu, at, 0);
-    if (hit) sh.hits[at + __popc(bal & ((1u << lane) - 1u))] = (uint16_t)tid;
+  const uint32_t best = max(sh.half[tid], sh.half[kLpThreads + tid]);
+  if (best >= thr && best != 0) {
+#pragma unroll
+    for (int s = 0; s < kSegs; ++s) {
+      const uint32_t key = sh.cell[s * kLpThreads + tid];
+      if (key >= thr && key != 0) sh.hits[atomicAdd(&sh.n_hits, 1)] = (uint16_t)(s * kLpThreads + tid);
+    }
   }
   __syncthreads();
 
@@ -147,28 +147,31 @@ __device__ void local_top(LpShared& sh, const T* z, const RowSlice& rs, int k) {
       if (at < kMaxTies) sh.ties[at] = i;
     }
   };
-  const int per_cell = (rs.v1 - rs.v0 + kLpThreads - 1) / kLpThreads;
-  const int n_work = sh.n_hits * per_cell;
+  // cell (s, t) holds the vectors t, t + 128, ... of the batches s * per_seg .. (s + 1) * per_seg - 1
+  const int nv = rs.v1 - rs.v0;
+  const int per_seg = max(1, ((nv + kLpBatchVecs - 1) / kLpBatchVecs + kSegs - 1) / kSegs);
+  const int per_cell = per_seg * kLpBatch;
+  const int n_work = sh.n_hits * per_cell;               // at most 1024 cells times nv / 1024 + 4 vectors each: below 2^24
   const float inv_per_cell = 1.f / (float)per_cell;
-  const uint4* zv = reinterpret_cast<const uint4*>(z + rs.head);
+  const uint4* zv = reinterpret_cast<const uint4*>(z + rs.head) + rs.v0;
   const uint4 pad = make_uint4(Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked());
-  constexpr int kAhead = 4;                      // second reads in flight per thread
+  constexpr int kAhead = 4;                              // second reads in flight per thread
   for (int w0 = tid; w0 < n_work; w0 += kLpThreads * kAhead) {
     uint4 q[kAhead];
     int at[kAhead];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int w = w0 + u * kLpThreads;
-      // w / per_cell: w stays below 2^24 (256 cells of fewer than 2^16 vectors), the quotient is off by at most one
-      int h = (int)((float)w * inv_per_cell);
+      int h = (int)((float)w * inv_per_cell);            // w / per_cell, off by at most one
       int j = w - h * per_cell;
       if (j < 0) { --h; j += per_cell; }
       if (j >= per_cell) { ++h; j -= per_cell; }
       at[u] = -1;
       q[u] = pad;
       if (w < n_work) {
-        const int i = rs.v0 + sh.hits[h] + j * kLpThreads;
-        if (i < rs.v1) { at[u] = i; q[u] = __ldg(zv + i); }
+        const int cell = sh.hits[h];
+        const int i = (cell / kLpThreads) * per_seg * kLpBatchVecs + j * kLpThreads + cell % kLpThreads;
+        if (i < nv) { at[u] = i; q[u] = __ldg(zv + i); }
       }
     }
 #pragma unroll
@@ -178,14 +181,12 @@ __device__ void local_top(LpShared& sh, const T* z, const RowSlice& rs, int k) {
         float f[kVec];
         Elem<T>::unpack(q[u], f);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) take(f[e], rs.head + at[u] * kVec + e);
+        for (int e = 0; e < kVec; ++e) take(f[e], rs.head + (rs.v0 + at[u]) * kVec + e);
       }
     }
   }
-  if (hit) {
-    if (tid < rs.own_head) take(Elem<T>::load(z + tid), tid);
-    if (tid < rs.own_tail) take(Elem<T>::load(z + rs.tail_start + tid), rs.tail_start + tid);
-  }
+  if (tid < rs.own_head) take(Elem<T>::load(z + tid), tid);
+  if (tid < rs.own_tail) take(Elem<T>::load(z + rs.tail_start + tid), rs.tail_start + tid);
   __syncthreads();
   int n_cand = sh.n_cand, n_ties = sh.n_ties;
   if (n_cand > kMaxCand) {
@@ -193,7 +194,7 @@ __device__ void local_top(LpShared& sh, const T* z, const RowSlice& rs, int k) {
     uint32_t prefix = 0, mask = 0;
     int rest = want;
     for (int shift = 24; shift >= 0; shift -= 8) {
-      sh.hist[tid] = 0;
+      for (int i = tid; i < 256; i += kLpThreads) sh.hist[i] = 0;
       __syncthreads();
       for (int i = rs.e0 + tid; i < rs.e1; i += kLpThreads) {
         const uint32_t key = order_key(Elem<T>::load(z + i));
@@ -213,92 +214,126 @@ __device__ void local_top(LpShared& sh, const T* z, const RowSlice& rs, int k) {
       __syncthreads();
     }
     thr = prefix;
-    bound = key_value(thr);                       // an element's own key here, and fewer than `want` lie above it
+    bound = key_value(thr);                              // an element's own key here, and fewer than `want` lie above it
     if (tid == 0) { sh.n_cand = 0; sh.n_ties = 0; }
     __syncthreads();
     for (int i = rs.e0 + tid; i < rs.e1; i += kLpThreads) {
-      take(Elem<T>::load(z + i), i);
+      const float v = Elem<T>::load(z + i);
+      const uint32_t key = order_key(v);
+      if (key > thr) sh.cand[atomicAdd(&sh.n_cand, 1)] = rank_key(key, i);
+      else if (key == thr) {
+        const int at = atomicAdd(&sh.n_ties, 1);
+        if (at < kMaxTies) sh.ties[at] = i;
+      }
     }
     __syncthreads();
-    n_cand = sh.n_cand;               // fewer than want
+    n_cand = sh.n_cand;
     n_ties = sh.n_ties;
   }
   if (n_cand < want) {
-    const int need = want - n_cand;
     if (n_ties <= kMaxTies) {
-      for (int i = tid; i < n_ties && n_cand + i < kMaxCand; i += kLpThreads) sh.cand[n_cand + i] = rank_key(thr, sh.ties[i]);
-      n_cand = min(n_cand + n_ties, kMaxCand);
+      for (int i = tid; i < n_ties; i += kLpThreads) sh.cand[n_cand + i] = rank_key(thr, sh.ties[i]);
+      n_cand += n_ties;                                  // at most 127 + 256
     } else {
-      append_ties_in_order(sh, z, rs, thr, n_cand, need);
+      append_ties_in_order(sh, z, rs, thr, n_cand, want - n_cand);
       n_cand = want;
     }
     __syncthreads();
   }
-  // place of each candidate = how many come before it, two keys a read
-  if (tid == 0) sh.cand[n_cand] = 0ull;
-  __syncthreads();
-  const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(sh.cand);
-  for (int i = tid; i < n_cand; i += kLpThreads) {
-    const unsigned long long key = sh.cand[i];
-    int before = 0;
-#pragma unroll 4
-    for (int j = 0; j < (n_cand + 1) / 2; ++j) {
-      const ulonglong2 o = pairs[j];
-      before += (o.x > key) + (o.y > key);
-    }
-    if (before < k) sh.top[before] = key;
+  if ((n_cand & 1) != 0) {                               // the sort reads pairs
+    if (tid == 0) sh.cand[n_cand] = 0ull;
+    __syncthreads();
   }
+  return n_cand;
+}
+
+// how many of the `n` candidates come before `key`
+__device__ __forceinline__ int place_among(const LpShared& sh, unsigned long long key, int n) {
+  const ulonglong2* pairs = reinterpret_cast<const ulonglong2*>(sh.cand);
+  int before = 0;
+#pragma unroll 4
+  for (int j = 0; j < (n + 1) / 2; ++j) {
+    const ulonglong2 o = pairs[j];
+    before += (o.x > key) + (o.y > key);
+  }
+  return before;
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kLpThreads)
-token_logprobs_kernel(const LogprobParams p, const int n_cta) {
-  constexpr int kVec = Elem<T>::kVec;
+__global__ void __launch_bounds__(kLpThreads, 8)
+token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
   pdl_launch_dependents();
   __shared__ LpShared sh;
+  const int n_cta = 1 << log2_cta;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int cta = n_cta > 1 ? (int)cluster_rank() : 0;
-  const int n_rows_at_once = gridDim.x / n_cta;
+  const int cta = log2_cta > 0 ? (int)cluster_rank() : 0;
+  const int n_rows_at_once = gridDim.x >> log2_cta;
   pdl_wait();
 
-  for (int row = blockIdx.x / n_cta; row < p.T; row += n_rows_at_once) {
+  for (int row = blockIdx.x >> log2_cta; row < p.T; row += n_rows_at_once) {
     const T* z = reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.ld;
-    const RowSlice rs = row_slice<T>(z, p.V, cta, n_cta);
-    RunningStat run;
-    run.start(p.ordinary != 0);
-    bool any = rs.v0 + tid < rs.v1 || tid < rs.own_head || tid < rs.own_tail;
+    const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
     float z_target = 0.f;
     int target = -1;
     if (cta == 0 && tid == 0 && p.targets != nullptr) {
       target = p.targets[row];
       if (target >= 0 && target < p.V) z_target = Elem<T>::load(z + target);
     }
-    const uint4* zv = reinterpret_cast<const uint4*>(z + rs.head);
+    RunningStat run;
+    run.start(p.ordinary != 0);
+    const int nv = rs.v1 - rs.v0;
+    const int n_batch = (nv + kLpBatchVecs - 1) / kLpBatchVecs;
+    const int per_seg = max(1, (n_batch + kSegs - 1) / kSegs);
+    const uint4* src = reinterpret_cast<const uint4*>(z + rs.head) + rs.v0 + tid;
     const uint4 pad = make_uint4(Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked());
-    for (int i = rs.v0 + tid; i < rs.v1; i += kLpThreads * kLpBatch) {
+    float seg_max = -CUDART_INF_F;
+    uint32_t half_key[2] = {0u, 0u};
+    int seg = 0, left = per_seg;
+    for (int b = 0; b < n_batch; ++b, src += kLpBatchVecs) {
       uint4 q[kLpBatch];
+      if ((b + 1) * kLpBatchVecs <= nv) {
 #pragma unroll
-      for (int u = 0; u < kLpBatch; ++u) {
-        const int at = i + u * kLpThreads;
-        q[u] = at < rs.v1 ? __ldg(zv + at) : pad;      // a padding vector (-inf) contributes nothing
+        for (int u = 0; u < kLpBatch; ++u) q[u] = __ldg(src + u * kLpThreads);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kLpBatch; ++u)               // a padding vector (-inf) contributes nothing
+          q[u] = b * kLpBatchVecs + u * kLpThreads + tid < nv ? __ldg(src + u * kLpThreads) : pad;
       }
-      run.template take<T, kLpBatch>(q, p.c);
+      uint32_t w[4 * kLpBatch];
+#pragma unroll
+      for (int u = 0; u < kLpBatch; ++u) { w[4 * u] = q[u].x; w[4 * u + 1] = q[u].y; w[4 * u + 2] = q[u].z; w[4 * u + 3] = q[u].w; }
+      const float batch_max = Elem<T>::max_of(w);
+      run.template take_words<T, 4 * kLpBatch>(w, batch_max, p.c);
+      if (p.top_k > 0) {
+        seg_max = max_nan(seg_max, batch_max);
+        if (--left == 0 || b == n_batch - 1) {
+          const uint32_t key = seg * per_seg * kLpBatchVecs + tid < nv ? order_key(seg_max) : 0u;
+          sh.cell[seg * kLpThreads + tid] = key;
+          if (seg < kSegs / 2) half_key[0] = max(half_key[0], key); else half_key[1] = max(half_key[1], key);
+          ++seg;
+          seg_max = -CUDART_INF_F;
+          left = per_seg;
+        }
+      }
     }
     if (tid < rs.own_head) run.take_scalar(Elem<T>::load(z + tid), p.c);
     if (tid < rs.own_tail) run.take_scalar(Elem<T>::load(z + rs.tail_start + tid), p.c);
-    RowStat acc = run.done(p.c);
-    const uint32_t my_key = order_key(acc.m);
-    if (p.top_k > 0) sh.cell[tid] = any ? my_key : 0u;
-    // the warp's maximum first, one rescaling each, then plain sums
-    rescale(acc, key_value(__reduce_max_sync(0xffffffffu, my_key)), p.c);
+    if (p.top_k > 0) {
+      for (; seg < kSegs; ++seg) sh.cell[seg * kLpThreads + tid] = 0u;
+      sh.half[tid] = half_key[0];
+      sh.half[kLpThreads + tid] = half_key[1];
+    }
+    // the warp's maximum first, one rescaling each, then plain sums; the same across the warps
+    RowStat a = run.done(p.c);
+    rescale(a, key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), p.c);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
-      acc.S += __shfl_xor_sync(0xffffffffu, acc.S, off);
-      acc.U += __shfl_xor_sync(0xffffffffu, acc.U, off);
+      a.S += __shfl_xor_sync(0xffffffffu, a.S, off);
+      a.U += __shfl_xor_sync(0xffffffffu, a.U, off);
     }
-    if (lane == 0) sh.part[wid] = acc;
+    if (lane == 0) sh.part[wid] = a;
     __syncthreads();
-    RowStat a = sh.part[lane & (kLpWarps - 1)];        // every warp sums the eight parts in the same order
+    a = sh.part[lane & (kLpWarps - 1)];                  // every warp sums the parts, in the same order
     rescale(a, key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), p.c);
 #pragma unroll
     for (int off = kLpWarps / 2; off > 0; off >>= 1) {
@@ -308,44 +343,36 @@ token_logprobs_kernel(const LogprobParams p, const int n_cta) {
     // A NaN cell maximum would order wrongly: a bad row (its maximum says so) lists nothing.  With several CTAs the others
     // may not know yet; what they list is not used then.
     const bool list = p.top_k > 0 && !(a.m != a.m);
-    if (list) local_top<T>(sh, z, rs, p.top_k);
-    if (n_cta > 1) {
-      if (tid == 0) sh.stat = a;
-      __syncthreads();
-      cluster_barrier();                          // every CTA's triple and list are in its shared memory
+    const int want = min(p.top_k, rs.e1 - rs.e0);
+    const int n_cand = list ? select_candidates<T>(sh, z, rs, want) : 0;
+    if (log2_cta > 0) {
+      for (int i = tid; i < n_cand; i += kLpThreads) {
+        const int before = place_among(sh, sh.cand[i], n_cand);
+        if (before < want) sh.top[before] = sh.cand[i];
+      }
+      if (tid == 0) { sh.stat = a; sh.n_list = list ? want : 0; }
+      cluster_barrier();                                 // every CTA's triple and list are in its shared memory
       if (cta == 0) {
-        for (int r = 1; r < n_cta; ++r) {
-          const uint32_t at = peer_shared(&sh.stat, r);
-          RowStat o{ld_peer_f32(at), ld_peer_f32(at + 4), ld_peer_f32(at + 8)};
-          a = merge(a, o, p.c);
+        {
+          const uint32_t at = peer_shared(&sh.stat, lane & (n_cta - 1));
+          a = RowStat{ld_peer_f32(at), ld_peer_f32(at + 4), ld_peer_f32(at + 8)};
+          rescale(a, key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), p.c);
+          for (int off = n_cta / 2; off > 0; off >>= 1) {
+            a.S += __shfl_xor_sync(0xffffffffu, a.S, off);
+            a.U += __shfl_xor_sync(0xffffffffu, a.U, off);
+          }
         }
         if (p.top_k > 0) {
-          const int all = n_cta * p.top_k;
-          for (int i = tid; i < all; i += kLpThreads) {
-            const int r = i / p.top_k;
-            sh.cand[i] = ld_peer_u64(peer_shared(&sh.top[i - r * p.top_k], r));
-          }
-          __syncthreads();
-          for (int i = tid; i < all; i += kLpThreads) {
-            const unsigned long long key = sh.cand[i];
-            const int r = i / p.top_k;
-            int rank = i - r * p.top_k;           // keys before it in its own list, then in the others
-            for (int o = 0; o < n_cta && rank < p.top_k; ++o) {
-              if (o == r) continue;
-              const unsigned long long* l = sh.cand + o * p.top_k;
-              int lo = 0, hi = p.top_k;
-              while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (l[mid] > key) lo = mid + 1; else hi = mid;
-              }
-              rank += lo;
-            }
-            if (rank < p.top_k) sh.top[rank] = key;
+          // the lists side by side, top_k places each; a list that is shorter ends in zeros
+          for (int r = wid; r < n_cta; r += kLpWarps) {
+            const int n = (int)ld_peer_u32(peer_shared(&sh.n_list, r));
+            for (int j = lane; j < p.top_k; j += 32)
+              sh.cand[r * p.top_k + j] = j < n ? ld_peer_u64(peer_shared(&sh.top[j], r)) : 0ull;
           }
         }
       }
+      __syncthreads();
     }
-    __syncthreads();
     if (cta == 0) {
       const bool bad = bad_max(a.m);
       const float ln_s = logf(a.S);
@@ -361,32 +388,60 @@ token_logprobs_kernel(const LogprobParams p, const int n_cta) {
           p.logprob[row] = v;
         }
       }
-      if (tid < p.top_k) {
-        const unsigned long long key = sh.top[tid];
-        const int64_t at = (int64_t)row * p.top_k + tid;
-        const float v = key_value((uint32_t)(key >> 32));
-        p.top_ids[at] = bad ? -1 : (int32_t)(0xFFFFFFFFu - (uint32_t)key);
-        p.top_logprobs[at] = bad ? CUDART_NAN_F : (v - a.m) * p.inv_temp - ln_s;
+      if (p.top_k > 0) {
+        const int64_t out = (int64_t)row * p.top_k;
+        if (bad) {
+          for (int j = tid; j < p.top_k; j += kLpThreads) {
+            p.top_ids[out + j] = -1;
+            p.top_logprobs[out + j] = CUDART_NAN_F;
+          }
+        } else {
+          const int n = log2_cta > 0 ? p.top_k << log2_cta : n_cand;
+          for (int i = tid; i < n; i += kLpThreads) {
+            const unsigned long long key = sh.cand[i];
+            int place;
+            if (log2_cta == 0) {
+              place = place_among(sh, key, n);
+            } else {
+              const int r = i / p.top_k;
+              place = i - r * p.top_k;                   // keys before it in its own list, then in the others
+              for (int o = 0; o < n_cta && place < p.top_k; ++o) {
+                if (o == r) continue;
+                const unsigned long long* l = sh.cand + o * p.top_k;
+                int lo = 0, hi = p.top_k;
+                while (lo < hi) {
+                  const int mid = (lo + hi) >> 1;
+                  if (l[mid] > key) lo = mid + 1; else hi = mid;
+                }
+                place += lo;
+              }
+            }
+            if (place < p.top_k) {
+              p.top_ids[out + place] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
+              p.top_logprobs[out + place] = (key_value((uint32_t)(key >> 32)) - a.m) * p.inv_temp - ln_s;
+            }
+          }
+        }
       }
     }
-    if (n_cta > 1) cluster_barrier();             // the leader has read the others' shared memory
+    if (log2_cta > 0) cluster_barrier();                 // the leader has read the others' shared memory
     else __syncthreads();
   }
 }
 
-// CTAs that share a row.  One per row once the rows fill the GPU; with fewer rows the row is cut so that more SMs pull
-// on it, down to slices of 2048 elements.
+// CTAs that share a row (as a power of two).  One per row once the rows fill the GPU; with fewer rows the row is cut so
+// that more SMs pull on it, down to slices of 2048 elements.
 int logprob_cluster(int T, int V) {
-  int c = 1;
-  while (c < kMaxLpCluster && (int64_t)T * c * 2 <= 296 && V / (c * 2) >= 2048) c *= 2;
-  return c;
+  int l = 0;
+  while ((1 << l) < kMaxLpCluster && ((int64_t)T << (l + 1)) <= 592 && (V >> (l + 1)) >= 2048) ++l;
+  return l;
 }
 
 template <typename T>
 cudaError_t launch_logprobs(const LogprobParams& p, cudaStream_t st) {
-  const int c = logprob_cluster(p.T, p.V);
+  const int l = logprob_cluster(p.T, p.V);
   const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
-  return launch_clusters(!stream_is_capturing(st), c, token_logprobs_kernel<T>, dim3(rows * c), dim3(kLpThreads), 0, st, p, c);
+  return launch_clusters(!stream_is_capturing(st), 1 << l, token_logprobs_kernel<T>, dim3(rows << l), dim3(kLpThreads), 0, st, p, l);
 }
 
 }  // namespace
