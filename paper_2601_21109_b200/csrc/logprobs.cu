@@ -5,8 +5,8 @@
 //   logprob(y) = (z_y - m)/tau - ln S,   top K by (z descending, index ascending)
 //
 // The row is read once.  Every thread keeps the online triple of its own elements and the maximum of each of up to eight
-// runs of them (its cells; the batch maxima that the triple needs anyway).  The K-th largest of the half-way maxima of the
-// threads is a lower bound of the row's K-th largest logit, and only cells whose maximum reaches it can hold one of the
+// runs of them (its cells; the batch maxima that the triple needs anyway).  The K-th largest of the maxima of the threads'
+// even and odd cells is a lower bound of the row's K-th largest logit, and only cells whose maximum reaches it can hold one of the
 // top K: a few per cent of the row are read a second time (from L2), and what reaches the bound is sorted in shared memory.
 #include <cmath>
 
@@ -43,20 +43,22 @@ __device__ __forceinline__ unsigned long long rank_key(uint32_t key, int idx) {
 }
 
 struct LpShared {
-  alignas(16) unsigned long long cand[kMaxCand + 2];   // candidates; then the lists of the whole cluster
+  alignas(16) unsigned long long cand[kMaxCand + 2];   // candidates
   uint32_t cell[kSegs * kLpThreads];                   // order key of every cell's maximum, 0 for an empty cell
-  uint32_t half[2 * kLpThreads];                       // the larger of a thread's first four cells, of its last four
-  unsigned long long top[CWL_MAX_TOP_K];               // a CTA's sorted list, read by the leader of its cluster
+  uint32_t half[2 * kLpThreads];                       // the largest of a thread's even cells, of its odd ones
   RowStat part[kLpWarps];
-  RowStat stat;                                        // this CTA's triple, read by the leader
   uint32_t hist[256];
   int ties[kMaxTies];
   int warp_count[kLpWarps];
   uint16_t hits[kSegs * kLpThreads];
   uint32_t thr;
-  int n_hits, n_cand, n_ties, rest, n_list;
+  int n_hits, n_cand, n_ties, rest;
 };
-static_assert(kMaxLpCluster * CWL_MAX_TOP_K <= kMaxCand, "the cluster's lists are gathered in the candidate buffer");
+// Shared memory of the leader of a cluster that the others write: every CTA's sorted list (top_k places each, a shorter
+// one ends in zeros), then every CTA's triple.
+static_assert(kMaxLpCluster * CWL_MAX_TOP_K <= kMaxCand, "all lists fit the candidate buffer");
+extern __shared__ __align__(16) unsigned long long lp_lists[];
+inline size_t lp_lists_bytes(int n_cta, int top_k) { return (size_t)n_cta * (top_k * sizeof(unsigned long long) + 16); }
 
 // Appends the lowest-index elements whose key equals `key` to the candidates until `need` are found.
 template <typename T>
@@ -81,12 +83,12 @@ __device__ void append_ties_in_order(LpShared& sh, const T* z, const RowSlice& r
   }
 }
 
-// The want-th largest of the threads' half-way maxima, rounded down to its first bits (all that a 16-bit type has, 20 of
-// fp32: a bound that is a little lower admits a few logits more).  One warp: a bit per step, from the first in which the
+// The want-th largest of the threads' half maxima, rounded down to its first bits (all that a 16-bit type has, 16 of
+// fp32: a bound that is up to 1/128 lower admits a few logits more).  One warp: a bit per step, from the first in which the
 // keys differ.
 template <typename T>
 __device__ __forceinline__ uint32_t cell_bound(const uint32_t* half, int want) {
-  constexpr int kLastBit = Elem<T>::kZeroBits > 0 ? Elem<T>::kZeroBits : 12;
+  constexpr int kLastBit = Elem<T>::kZeroBits > 0 ? Elem<T>::kZeroBits : 16;
   constexpr int n = 2 * kLpThreads / 32;
   const int lane = threadIdx.x & 31;
   uint32_t k[n], hi = 0, lo = 0xFFFFFFFFu;
@@ -110,7 +112,7 @@ __device__ __forceinline__ uint32_t cell_bound(const uint32_t* half, int want) {
   }
   // exact where it can be: a negative 16-bit value has ones below its bits, and -inf is alone in its range of keys
   if (Elem<T>::kZeroBits > 0) return prefix | ((prefix >> 31) != 0 ? 0u : (1u << kLastBit) - 1u);
-  return prefix >= (kKeyOfMinusInf & ~0xFFFu) && prefix < kKeyOfMinusInf ? kKeyOfMinusInf : prefix;
+  return prefix >= (kKeyOfMinusInf & ~0xFFFFu) && prefix < kKeyOfMinusInf ? kKeyOfMinusInf : prefix;
 }
 
 // Leaves in sh.cand a set that holds the `want` largest rank keys of this CTA's elements; returns its size (at least
@@ -268,6 +270,7 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int cta = log2_cta > 0 ? (int)cluster_rank() : 0;
   const int n_rows_at_once = gridDim.x >> log2_cta;
+  if (log2_cta > 0) cluster_barrier_arrive();          // waited for before the leader's shared memory is written
   pdl_wait();
 
   for (int row = blockIdx.x >> log2_cta; row < p.T; row += n_rows_at_once) {
@@ -309,7 +312,7 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
         if (--left == 0 || b == n_batch - 1) {
           const uint32_t key = seg * per_seg * kLpBatchVecs + tid < nv ? order_key(seg_max) : 0u;
           sh.cell[seg * kLpThreads + tid] = key;
-          if (seg < kSegs / 2) half_key[0] = max(half_key[0], key); else half_key[1] = max(half_key[1], key);
+          if ((seg & 1) == 0) half_key[0] = max(half_key[0], key); else half_key[1] = max(half_key[1], key);
           ++seg;
           seg_max = -CUDART_INF_F;
           left = per_seg;
@@ -346,32 +349,25 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
     const int want = min(p.top_k, rs.e1 - rs.e0);
     const int n_cand = list ? select_candidates<T>(sh, z, rs, want) : 0;
     if (log2_cta > 0) {
-      for (int i = tid; i < n_cand; i += kLpThreads) {
-        const int before = place_among(sh, sh.cand[i], n_cand);
-        if (before < want) sh.top[before] = sh.cand[i];
+      // this CTA's sorted list and triple go to the leader, which then finds everything in its own shared memory
+      cluster_barrier_wait();
+      float* stats = reinterpret_cast<float*>(lp_lists + p.top_k * n_cta);
+      for (int i = tid; i < max(n_cand, p.top_k); i += kLpThreads) {
+        const unsigned long long key = i < n_cand ? sh.cand[i] : 0ull;
+        const int before = i < n_cand ? place_among(sh, key, n_cand) : i;
+        if (before < want && i < n_cand) st_peer_u64(peer_shared(&lp_lists[cta * p.top_k + before], 0), key);
+        if (i >= (list ? want : 0) && i < p.top_k) st_peer_u64(peer_shared(&lp_lists[cta * p.top_k + i], 0), 0ull);
       }
-      if (tid == 0) { sh.stat = a; sh.n_list = list ? want : 0; }
-      cluster_barrier();                                 // every CTA's triple and list are in its shared memory
-      if (cta == 0) {
-        {
-          const uint32_t at = peer_shared(&sh.stat, lane & (n_cta - 1));
-          a = RowStat{ld_peer_f32(at), ld_peer_f32(at + 4), ld_peer_f32(at + 8)};
-          rescale(a, key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), p.c);
-          for (int off = n_cta / 2; off > 0; off >>= 1) {
-            a.S += __shfl_xor_sync(0xffffffffu, a.S, off);
-            a.U += __shfl_xor_sync(0xffffffffu, a.U, off);
-          }
-        }
-        if (p.top_k > 0) {
-          // the lists side by side, top_k places each; a list that is shorter ends in zeros
-          for (int r = wid; r < n_cta; r += kLpWarps) {
-            const int n = (int)ld_peer_u32(peer_shared(&sh.n_list, r));
-            for (int j = lane; j < p.top_k; j += 32)
-              sh.cand[r * p.top_k + j] = j < n ? ld_peer_u64(peer_shared(&sh.top[j], r)) : 0ull;
-          }
-        }
+      if (tid < 3) st_peer_f32(peer_shared(&stats[cta * 4 + tid], 0), tid == 0 ? a.m : tid == 1 ? a.S : a.U);
+      cluster_barrier();
+      if (cta != 0) return;                              // a cluster has one row (the host launches as many as there are rows)
+      const float* mine = stats + (lane & (n_cta - 1)) * 4;
+      a = RowStat{mine[0], mine[1], mine[2]};
+      rescale(a, key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), p.c);
+      for (int off = n_cta / 2; off > 0; off >>= 1) {
+        a.S += __shfl_xor_sync(0xffffffffu, a.S, off);
+        a.U += __shfl_xor_sync(0xffffffffu, a.U, off);
       }
-      __syncthreads();
     }
     if (cta == 0) {
       const bool bad = bad_max(a.m);
@@ -396,26 +392,27 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
             p.top_logprobs[out + j] = CUDART_NAN_F;
           }
         } else {
-          const int n = log2_cta > 0 ? p.top_k << log2_cta : n_cand;
+          int n = n_cand;
+          if (log2_cta > 0) {
+            // every list has at least q entries that reach the smallest of the lists' q-th ones: with q = top_k / n_cta
+            // rounded up that is a bound of the row's top_k-th; what reaches it is sorted
+            const int q = (p.top_k + n_cta - 1) >> log2_cta;
+            unsigned long long bound = lp_lists[(lane & (n_cta - 1)) * p.top_k + q - 1];
+            for (int off = n_cta / 2; off > 0; off >>= 1) bound = min(bound, __shfl_xor_sync(0xffffffffu, bound, off));
+            if (tid == 0) sh.n_cand = 0;
+            __syncthreads();
+            for (int i = tid; i < p.top_k << log2_cta; i += kLpThreads) {
+              const unsigned long long key = lp_lists[i];
+              if (key >= bound && key != 0) sh.cand[atomicAdd(&sh.n_cand, 1)] = key;
+            }
+            __syncthreads();
+            n = sh.n_cand;
+            if (tid == 0) sh.cand[n] = 0ull;
+            __syncthreads();
+          }
           for (int i = tid; i < n; i += kLpThreads) {
             const unsigned long long key = sh.cand[i];
-            int place;
-            if (log2_cta == 0) {
-              place = place_among(sh, key, n);
-            } else {
-              const int r = i / p.top_k;
-              place = i - r * p.top_k;                   // keys before it in its own list, then in the others
-              for (int o = 0; o < n_cta && place < p.top_k; ++o) {
-                if (o == r) continue;
-                const unsigned long long* l = sh.cand + o * p.top_k;
-                int lo = 0, hi = p.top_k;
-                while (lo < hi) {
-                  const int mid = (lo + hi) >> 1;
-                  if (l[mid] > key) lo = mid + 1; else hi = mid;
-                }
-                place += lo;
-              }
-            }
+            const int place = place_among(sh, key, n);
             if (place < p.top_k) {
               p.top_ids[out + place] = (int32_t)(0xFFFFFFFFu - (uint32_t)key);
               p.top_logprobs[out + place] = (key_value((uint32_t)(key >> 32)) - a.m) * p.inv_temp - ln_s;
@@ -424,8 +421,8 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
         }
       }
     }
-    if (log2_cta > 0) cluster_barrier();                 // the leader has read the others' shared memory
-    else __syncthreads();
+    if (log2_cta > 0) return;
+    __syncthreads();
   }
 }
 
@@ -441,7 +438,8 @@ template <typename T>
 cudaError_t launch_logprobs(const LogprobParams& p, cudaStream_t st) {
   const int l = logprob_cluster(p.T, p.V);
   const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
-  return launch_clusters(!stream_is_capturing(st), 1 << l, token_logprobs_kernel<T>, dim3(rows << l), dim3(kLpThreads), 0, st, p, l);
+  return launch_clusters(!stream_is_capturing(st), 1 << l, token_logprobs_kernel<T>, dim3(rows << l), dim3(kLpThreads),
+                         l > 0 ? lp_lists_bytes(1 << l, p.top_k) : 0, st, p, l);
 }
 
 }  // namespace
