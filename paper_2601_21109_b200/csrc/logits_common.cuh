@@ -43,6 +43,12 @@ template <> struct Elem<float> {
   static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
     return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
   }
+  // the first element of a vector, which moves up by one
+  static __device__ __forceinline__ float shift_out(uint4& q) {
+    const float f = __uint_as_float(q.x);
+    q.x = q.y; q.y = q.z; q.z = q.w;
+    return f;
+  }
   static __device__ __forceinline__ uint32_t masked() { return 0xFF800000u; }   // -inf
   // maximum of the elements of n words, NaN wins
   template <int n> static __device__ __forceinline__ float max_of(const uint32_t (&w)[n]) {
@@ -77,6 +83,11 @@ template <> struct Elem<__nv_bfloat16> {
       w[i] = *reinterpret_cast<const uint32_t*>(&v);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ float shift_out(uint4& q) {
+    const float f = __uint_as_float(q.x << 16);
+    q.x = __funnelshift_r(q.x, q.y, 16); q.y = __funnelshift_r(q.y, q.z, 16); q.z = __funnelshift_r(q.z, q.w, 16); q.w >>= 16;
+    return f;
   }
   static __device__ __forceinline__ uint32_t masked() { return 0xFF80FF80u; }
   template <int n> static __device__ __forceinline__ float max_of(const uint32_t (&w)[n]) {
@@ -117,6 +128,11 @@ template <> struct Elem<__half> {
       w[i] = *reinterpret_cast<const uint32_t*>(&v);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ float shift_out(uint4& q) {
+    const float f = __half2float(__ushort_as_half((unsigned short)(q.x & 0xFFFFu)));
+    q.x = __funnelshift_r(q.x, q.y, 16); q.y = __funnelshift_r(q.y, q.z, 16); q.z = __funnelshift_r(q.z, q.w, 16); q.w >>= 16;
+    return f;
   }
   static __device__ __forceinline__ uint32_t masked() { return 0xFC00FC00u; }
   template <int n> static __device__ __forceinline__ float max_of(const uint32_t (&w)[n]) {
@@ -167,88 +183,71 @@ __device__ __forceinline__ RowStat merge(RowStat a, RowStat b, float c) {
   return a;
 }
 
-// A thread's running statistic over batches of 16-byte vectors.  While the maximum is an ordinary number (|m| up to
-// kOrdinaryLogit, and a temperature between 1/100 and 100) an exponent is one multiply-add, t = z c - M with M = m c
+__device__ __forceinline__ void absorb_scalar(RowStat& a, float v, float c) {
+  const float m_new = max_nan(a.m, v);
+  if (m_new == -CUDART_INF_F) return;
+  if (m_new != a.m) rebase(a, m_new, c);
+  absorb(a, v, c);
+}
+
+// A thread's running statistic over batches of 16-byte vectors, for rows whose maximum is an ordinary number (|m| up to
+// kOrdinaryLogit, and a temperature between 1/100 and 100): an exponent is one multiply-add, t = z c - M with M = m c
 // rounded once, and -inf is replaced beforehand by a finite value of weight 0: for 16-bit types that is one instruction
 // for two elements, and so is the maximum.  6 instructions an element instead of 8, which is what a row of 16-bit logits
-// is bound by.  Beyond, or for other temperatures, t = (z - m) c with the exponent clamped; a thread that has met an
-// extraordinary maximum stays there.
+// is bound by.  A thread that met an extraordinary maximum says so in the end (`exact_needed`), and its elements are
+// taken again in the form t = (z - m) c with the exponent clamped.
 constexpr float kOrdinaryLogit = 16384.f;
 struct RunningStat {
   float m, M, S, U;
-  bool ordinary;
-  __device__ __forceinline__ void start(bool temperature_ok) {
-    m = -CUDART_INF_F; M = 0.f; S = 0.f; U = 0.f; ordinary = temperature_ok;
-  }
-  // S and U relative to m itself instead of the rounded M
-  __device__ __forceinline__ void leave_ordinary(float c) {
-    if (ordinary && m != -CUDART_INF_F) {
-      const float d = fmaf(m, c, -M), sc = exp2_fast(-d);
-      U = (U - d * S) * sc;
-      S *= sc;
-    }
-    ordinary = false;
-  }
-  template <typename T, int n>
-  __device__ __forceinline__ void take(const uint4 (&q)[n], float c) {
-    uint32_t w[4 * n];
-#pragma unroll
-    for (int i = 0; i < n; ++i) { w[4 * i] = q[i].x; w[4 * i + 1] = q[i].y; w[4 * i + 2] = q[i].z; w[4 * i + 3] = q[i].w; }
-    take_words<T, 4 * n>(w, Elem<T>::max_of(w), c);
+  bool exact_needed;
+  __device__ __forceinline__ void start(bool ordinary_temperature) {
+    m = -CUDART_INF_F; M = 0.f; S = 0.f; U = 0.f; exact_needed = !ordinary_temperature;
   }
   template <typename T, int n>
   __device__ __forceinline__ void take_words(const uint32_t (&w)[n], float batch_max, float c) {
     constexpr int kPer = Elem<T>::kVec / 4;
-    const float m_new = max_nan(m, batch_max);
-    if (m_new == -CUDART_INF_F) return;                 // nothing but -inf so far
-    if (ordinary && !(fabsf(m_new) <= kOrdinaryLogit)) leave_ordinary(c);
-    if (ordinary) {
-      if (m_new != m) {
-        const float M_new = m_new * c;
-        const float dt = M - M_new;                     // S == 0 when nothing was seen
-        const float sc = m == -CUDART_INF_F ? 0.f : exp2_fast(dt);
-        U = (U + dt * S) * sc;
-        S *= sc;
-        m = m_new; M = M_new;
+    if (!(batch_max <= m)) {                            // a new maximum, or a NaN
+      const float m_new = max_nan(m, batch_max);
+      exact_needed = exact_needed || !(fabsf(m_new) <= kOrdinaryLogit);
+      const float M_new = m_new * c;
+      const float dt = M - M_new;
+      const float sc = m == -CUDART_INF_F ? 0.f : exp2_fast(dt);
+      U = (U + dt * S) * sc;
+      S *= sc;
+      m = m_new; M = M_new;
+    }
+    if (m == -CUDART_INF_F) return;                     // nothing but -inf so far
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      float f[kPer];
+      Elem<T>::unpack_word(Elem<T>::floor_word(w[i]), f);
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) {
+        const float t = fmaf(f[e], c, -M), x = exp2_fast(t);
+        S += x;
+        U = fmaf(t, x, U);
       }
-#pragma unroll
-      for (int i = 0; i < n; ++i) {
-        float f[kPer];
-        Elem<T>::unpack_word(Elem<T>::floor_word(w[i]), f);
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-          const float t = fmaf(f[e], c, -M), x = exp2_fast(t);
-          S += x;
-          U = fmaf(t, x, U);
-        }
-      }
-    } else {
-      RowStat a{m, S, U};
-      if (m_new != m) rebase(a, m_new, c);
-#pragma unroll
-      for (int i = 0; i < n; ++i) {
-        float f[kPer];
-        Elem<T>::unpack_word(w[i], f);
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) absorb(a, f[e], c);
-      }
-      m = a.m; S = a.S; U = a.U;
     }
   }
-  __device__ __forceinline__ void take_scalar(float v, float c) {
-    leave_ordinary(c);
-    const float m_new = max_nan(m, v);
-    if (m_new == -CUDART_INF_F) return;
-    RowStat a{m, S, U};
-    if (m_new != m) rebase(a, m_new, c);
-    absorb(a, v, c);
-    m = a.m; S = a.S; U = a.U;
-  }
-  __device__ __forceinline__ RowStat done(float c) {
-    leave_ordinary(c);
-    return RowStat{m, S, U};
+  // the triple relative to m itself instead of the rounded M; of no account where exact_needed is set
+  __device__ __forceinline__ RowStat done(float c) const {
+    if (m == -CUDART_INF_F) return RowStat{m, 0.f, 0.f};
+    const float d = fmaf(m, c, -M), sc = exp2_fast(-d);
+    return RowStat{m, S * sc, (U - d * S) * sc};
   }
 };
+// The exact form over the vectors first, first + stride, ... below n.
+template <typename T>
+__device__ __noinline__ RowStat exact_stat(const uint4* v, int first, int stride, int n, float c) {
+  RowStat a{-CUDART_INF_F, 0.f, 0.f};
+  for (int i = first; i < n; i += stride) {
+    float f[Elem<T>::kVec];
+    Elem<T>::unpack(v[i], f);
+#pragma unroll
+    for (int e = 0; e < Elem<T>::kVec; ++e) absorb_scalar(a, f[e], c);
+  }
+  return a;
+}
 inline bool ordinary_temperature(float t) { return t >= 0.01f && t <= 100.f; }
 
 // order-preserving map of a float to 32 bits; -0 and +0 are equal, a NaN (as max_nan makes them) comes above +inf

@@ -62,12 +62,12 @@ inline size_t lp_lists_bytes(int n_cta, int top_k) { return (size_t)n_cta * (top
 
 // Appends the lowest-index elements whose key equals `key` to the candidates until `need` are found.
 template <typename T>
-__device__ void append_ties_in_order(LpShared& sh, const T* z, const RowSlice& rs, uint32_t key, int have, int need) {
+__device__ __noinline__ void append_ties_in_order(LpShared& sh, const T* z, int e0, int e1, uint32_t key, int have, int need) {
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   int found = 0;
-  for (int base = rs.e0; base < rs.e1 && found < need; base += kLpThreads) {
+  for (int base = e0; base < e1 && found < need; base += kLpThreads) {
     const int i = base + tid;
-    const bool is = i < rs.e1 && order_key(Elem<T>::load(z + i)) == key;
+    const bool is = i < e1 && order_key(Elem<T>::load(z + i)) == key;
     const unsigned bal = __ballot_sync(0xffffffffu, is);
     if (lane == 0) sh.warp_count[wid] = __popc(bal);
     __syncthreads();
@@ -115,6 +115,60 @@ __device__ __forceinline__ uint32_t cell_bound(const uint32_t* half, int want) {
   return prefix >= (kKeyOfMinusInf & ~0xFFFFu) && prefix < kKeyOfMinusInf ? kKeyOfMinusInf : prefix;
 }
 
+// Rows built so that few cells hold everything large: the want-th largest key exactly, eight bits at a time, then the
+// candidates above it and the ties with it.
+template <typename T>
+__device__ __noinline__ uint32_t exact_bound_and_candidates(LpShared& sh, const T* z, int e0, int e1, int want) {
+  const int tid = threadIdx.x;
+  uint32_t prefix = 0, mask = 0;
+  int rest = want;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int i = tid; i < 256; i += kLpThreads) sh.hist[i] = 0;
+    __syncthreads();
+    for (int i = e0 + tid; i < e1; i += kLpThreads) {
+      const uint32_t key = order_key(Elem<T>::load(z + i));
+      if ((key & mask) == prefix) atomicAdd(&sh.hist[(key >> shift) & 255u], 1u);
+    }
+    __syncthreads();
+    if (tid == 0) {
+      int d = 255;
+      while (d > 0 && (int)sh.hist[d] < rest) { rest -= sh.hist[d]; --d; }
+      sh.thr = (uint32_t)d;
+      sh.rest = rest;
+    }
+    __syncthreads();
+    prefix |= sh.thr << shift;
+    mask |= 255u << shift;
+    rest = sh.rest;
+    __syncthreads();
+  }
+  const uint32_t thr = prefix;                         // an element's own key, and fewer than `want` lie above it
+  if (tid == 0) { sh.n_cand = 0; sh.n_ties = 0; }
+  __syncthreads();
+  for (int i = e0 + tid; i < e1; i += kLpThreads) {
+    const float v = Elem<T>::load(z + i);
+    const uint32_t key = order_key(v);
+    if (key > thr) sh.cand[atomicAdd(&sh.n_cand, 1)] = rank_key(key, i);
+    else if (key == thr) {
+      const int at = atomicAdd(&sh.n_ties, 1);
+      if (at < kMaxTies) sh.ties[at] = i;
+    }
+  }
+  __syncthreads();
+  return thr;
+}
+
+// What reaches the bound goes to the candidates, what equals it to the ties.
+__device__ __forceinline__ void take_candidate(LpShared& sh, float v, int i, float bound, bool all) {
+  if (v > bound || all) {
+    const int at = atomicAdd(&sh.n_cand, 1);
+    if (at < kMaxCand) sh.cand[at] = rank_key(order_key(v), i);
+  } else if (v == bound) {
+    const int at = atomicAdd(&sh.n_ties, 1);
+    if (at < kMaxTies) sh.ties[at] = i;
+  }
+}
+
 // Leaves in sh.cand a set that holds the `want` largest rank keys of this CTA's elements; returns its size (at least
 // `want`).  sh.cell and sh.half hold the maxima.
 template <typename T>
@@ -140,15 +194,6 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
   // a bound below every element's key (fewer nonempty cells than wanted): everything is above it, -inf too
   const bool all = thr < kKeyOfMinusInf;
   float bound = all ? -CUDART_INF_F : key_value(thr);
-  auto take = [&](float v, int i) {
-    if (v > bound || all) {
-      const int at = atomicAdd(&sh.n_cand, 1);
-      if (at < kMaxCand) sh.cand[at] = rank_key(order_key(v), i);
-    } else if (v == bound) {
-      const int at = atomicAdd(&sh.n_ties, 1);
-      if (at < kMaxTies) sh.ties[at] = i;
-    }
-  };
   // cell (s, t) holds the vectors t, t + 128, ... of the batches s * per_seg .. (s + 1) * per_seg - 1
   const int nv = rs.v1 - rs.v0;
   const int per_seg = max(1, ((nv + kLpBatchVecs - 1) / kLpBatchVecs + kSegs - 1) / kSegs);
@@ -180,55 +225,20 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
     for (int u = 0; u < kAhead; ++u) {
       const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
       if (at[u] >= 0 && Elem<T>::max_of(w) >= bound) {
-        float f[kVec];
-        Elem<T>::unpack(q[u], f);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) take(f[e], rs.head + (rs.v0 + at[u]) * kVec + e);
+        // few vectors come here: one copy of the code, the elements shifted through
+        uint4 v = q[u];
+        const int first = rs.head + (rs.v0 + at[u]) * kVec;
+#pragma unroll 1
+        for (int e = 0; e < kVec; ++e) take_candidate(sh, Elem<T>::shift_out(v), first + e, bound, all);
       }
     }
   }
-  if (tid < rs.own_head) take(Elem<T>::load(z + tid), tid);
-  if (tid < rs.own_tail) take(Elem<T>::load(z + rs.tail_start + tid), rs.tail_start + tid);
+  if (tid < rs.own_head) take_candidate(sh, Elem<T>::load(z + tid), tid, bound, all);
+  if (tid < rs.own_tail) take_candidate(sh, Elem<T>::load(z + rs.tail_start + tid), rs.tail_start + tid, bound, all);
   __syncthreads();
   int n_cand = sh.n_cand, n_ties = sh.n_ties;
   if (n_cand > kMaxCand) {
-    // Rows built so that few cells hold everything large: the want-th largest key exactly, eight bits at a time.
-    uint32_t prefix = 0, mask = 0;
-    int rest = want;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += kLpThreads) sh.hist[i] = 0;
-      __syncthreads();
-      for (int i = rs.e0 + tid; i < rs.e1; i += kLpThreads) {
-        const uint32_t key = order_key(Elem<T>::load(z + i));
-        if ((key & mask) == prefix) atomicAdd(&sh.hist[(key >> shift) & 255u], 1u);
-      }
-      __syncthreads();
-      if (tid == 0) {
-        int d = 255;
-        while (d > 0 && (int)sh.hist[d] < rest) { rest -= sh.hist[d]; --d; }
-        sh.thr = (uint32_t)d;
-        sh.rest = rest;
-      }
-      __syncthreads();
-      prefix |= sh.thr << shift;
-      mask |= 255u << shift;
-      rest = sh.rest;
-      __syncthreads();
-    }
-    thr = prefix;
-    bound = key_value(thr);                              // an element's own key here, and fewer than `want` lie above it
-    if (tid == 0) { sh.n_cand = 0; sh.n_ties = 0; }
-    __syncthreads();
-    for (int i = rs.e0 + tid; i < rs.e1; i += kLpThreads) {
-      const float v = Elem<T>::load(z + i);
-      const uint32_t key = order_key(v);
-      if (key > thr) sh.cand[atomicAdd(&sh.n_cand, 1)] = rank_key(key, i);
-      else if (key == thr) {
-        const int at = atomicAdd(&sh.n_ties, 1);
-        if (at < kMaxTies) sh.ties[at] = i;
-      }
-    }
-    __syncthreads();
+    thr = exact_bound_and_candidates<T>(sh, z, rs.e0, rs.e1, want);
     n_cand = sh.n_cand;
     n_ties = sh.n_ties;
   }
@@ -237,7 +247,7 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
       for (int i = tid; i < n_ties; i += kLpThreads) sh.cand[n_cand + i] = rank_key(thr, sh.ties[i]);
       n_cand += n_ties;                                  // at most 127 + 256
     } else {
-      append_ties_in_order(sh, z, rs, thr, n_cand, want - n_cand);
+      append_ties_in_order(sh, z, rs.e0, rs.e1, thr, n_cand, want - n_cand);
       n_cand = want;
     }
     __syncthreads();
@@ -319,8 +329,6 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
         }
       }
     }
-    if (tid < rs.own_head) run.take_scalar(Elem<T>::load(z + tid), p.c);
-    if (tid < rs.own_tail) run.take_scalar(Elem<T>::load(z + rs.tail_start + tid), p.c);
     if (p.top_k > 0) {
       for (; seg < kSegs; ++seg) sh.cell[seg * kLpThreads + tid] = 0u;
       sh.half[tid] = half_key[0];
@@ -328,6 +336,12 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
     }
     // the warp's maximum first, one rescaling each, then plain sums; the same across the warps
     RowStat a = run.done(p.c);
+    if (run.exact_needed) a = exact_stat<T>(reinterpret_cast<const uint4*>(z + rs.head) + rs.v0, tid, kLpThreads, nv, p.c);
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {                        // scalars before the first vector and after the last
+      const int i = k == 0 ? tid : rs.tail_start + tid;
+      if (tid < (k == 0 ? rs.own_head : rs.own_tail)) absorb_scalar(a, Elem<T>::load(z + i), p.c);
+    }
     rescale(a, key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), p.c);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) {
