@@ -29,6 +29,24 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 // true for a row maximum that leaves the softmax undefined: NaN, +inf, or nothing but -inf
 __device__ __forceinline__ bool bad_max(float m) { return !(m < CUDART_INF_F) || m == -CUDART_INF_F; }
 
+// Two fp32 numbers in one 64-bit register: one instruction slot does both.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+  return p;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
 // Element types of a logit row: how many sit in 16 bytes, how they become fp32 and how a gradient is rounded back.
 template <typename T> struct Elem;
 template <> struct Elem<float> {
@@ -57,9 +75,11 @@ template <> struct Elem<float> {
     for (int i = 1; i < n; ++i) m = max_nan(m, __uint_as_float(w[i]));
     return m;
   }
-  // a word whose -inf (and whatever lies below) became kMaskedLogit: finite, and of weight 0 beside an ordinary maximum
-  static __device__ __forceinline__ uint32_t floor_word(uint32_t w) { return __float_as_uint(fmaxf(__uint_as_float(w), kMaskedLogit)); }
-  static __device__ __forceinline__ void unpack_word(uint32_t w, float (&f)[1]) { f[0] = __uint_as_float(w); }
+  // two elements, -inf (and whatever lies below kMaskedLogit) made finite: of weight 0 beside an ordinary maximum
+  static constexpr int kPairWords = 2;
+  static __device__ __forceinline__ uint64_t unpack_pair(const uint32_t* w) {
+    return pair(fmaxf(__uint_as_float(w[0]), kMaskedLogit), fmaxf(__uint_as_float(w[1]), kMaskedLogit));
+  }
 };
 template <> struct Elem<__nv_bfloat16> {
   static constexpr int kVec = 8;
@@ -96,14 +116,11 @@ template <> struct Elem<__nv_bfloat16> {
     for (int i = 1; i < n; ++i) asm("max.NaN.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(w[i]));
     return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
   }
-  static __device__ __forceinline__ uint32_t floor_word(uint32_t w) {
+  static constexpr int kPairWords = 1;
+  static __device__ __forceinline__ uint64_t unpack_pair(const uint32_t* w) {
     uint32_t y;
-    asm("max.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(w), "r"(0xF149F149u));     // kMaskedLogit in bf16, twice
-    return y;
-  }
-  static __device__ __forceinline__ void unpack_word(uint32_t w, float (&f)[2]) {
-    f[0] = __uint_as_float(w << 16);
-    f[1] = __uint_as_float(w & 0xFFFF0000u);
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(w[0]), "r"(0xF149F149u));     // kMaskedLogit in bf16, twice
+    return pair(__uint_as_float(y << 16), __uint_as_float(y & 0xFFFF0000u));
   }
 };
 template <> struct Elem<__half> {
@@ -142,14 +159,12 @@ template <> struct Elem<__half> {
     const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&m));
     return max_nan(v.x, v.y);
   }
-  static __device__ __forceinline__ uint32_t floor_word(uint32_t w) {
+  static constexpr int kPairWords = 1;
+  static __device__ __forceinline__ uint64_t unpack_pair(const uint32_t* w) {
     uint32_t y;
-    asm("max.f16x2 %0, %1, %2;" : "=r"(y) : "r"(w), "r"(0xFBFFFBFFu));      // the type's lowest value, twice
-    return y;
-  }
-  static __device__ __forceinline__ void unpack_word(uint32_t w, float (&f)[2]) {
-    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&w));
-    f[0] = v.x; f[1] = v.y;
+    asm("max.f16x2 %0, %1, %2;" : "=r"(y) : "r"(w[0]), "r"(0xFBFFFBFFu));      // the type's lowest value, twice
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&y));
+    return pair(v.x, v.y);
   }
 };
 
@@ -191,47 +206,55 @@ __device__ __forceinline__ void absorb_scalar(RowStat& a, float v, float c) {
 }
 
 // A thread's running statistic over batches of 16-byte vectors, for rows whose maximum is an ordinary number (|m| up to
-// kOrdinaryLogit, and a temperature between 1/100 and 100): an exponent is one multiply-add, t = z c - M with M = m c
-// rounded once, and -inf is replaced beforehand by a finite value of weight 0: for 16-bit types that is one instruction
-// for two elements, and so is the maximum.  6 instructions an element instead of 8, which is what a row of 16-bit logits
-// is bound by.  A thread that met an extraordinary maximum says so in the end (`exact_needed`), and its elements are
-// taken again in the form t = (z - m) c with the exponent clamped.
+// kOrdinaryLogit, and a temperature between 1/100 and 100).  Two elements a step: t = z c - M, M = m c rounded once, and
+// -inf is replaced beforehand by a finite value of weight 0 (for 16-bit types one instruction for two elements, and so
+// is the maximum): 4.5 instruction slots an element, the exponential among them, where the plain form takes 8; a row of
+// 16-bit logits is bound by them.  The reference m follows the maximum only when that runs ahead by kLead powers of two,
+// which leaves the sums far below fp32's range and saves the rescaling of nearly every batch.  A thread that met an
+// extraordinary maximum says so in the end (`exact_needed`), and its elements are taken again in the form t = (z - m) c
+// with the exponent clamped.
 constexpr float kOrdinaryLogit = 16384.f;
+constexpr float kLead = 8.f;
 struct RunningStat {
-  float m, M, S, U;
+  float m, M, limit;           // reference; m c rounded; the batch maximum up to which the reference stays
+  uint64_t S2, U2;             // sums over even and odd elements
   bool exact_needed;
   __device__ __forceinline__ void start(bool ordinary_temperature) {
-    m = -CUDART_INF_F; M = 0.f; S = 0.f; U = 0.f; exact_needed = !ordinary_temperature;
+    m = -CUDART_INF_F; M = 0.f; limit = -CUDART_INF_F; S2 = 0; U2 = 0; exact_needed = !ordinary_temperature;
   }
   template <typename T, int n>
   __device__ __forceinline__ void take_words(const uint32_t (&w)[n], float batch_max, float c) {
-    constexpr int kPer = Elem<T>::kVec / 4;
-    if (!(batch_max <= m)) {                            // a new maximum, or a NaN
+    if (!(batch_max <= limit)) {                        // well above the reference, or a NaN
       const float m_new = max_nan(m, batch_max);
       exact_needed = exact_needed || !(fabsf(m_new) <= kOrdinaryLogit);
       const float M_new = m_new * c;
       const float dt = M - M_new;
       const float sc = m == -CUDART_INF_F ? 0.f : exp2_fast(dt);
-      U = (U + dt * S) * sc;
-      S *= sc;
+      const uint64_t sc2 = pair(sc, sc), zero = pair(0.f, 0.f);
+      U2 = fma_pair(fma_pair(pair(dt, dt), S2, U2), sc2, zero);
+      S2 = fma_pair(S2, sc2, zero);
       m = m_new; M = M_new;
+      limit = m_new + kLead / c;
     }
     if (m == -CUDART_INF_F) return;                     // nothing but -inf so far
+    const uint64_t c2 = pair(c, c), minus_m = pair(-M, -M);
 #pragma unroll
-    for (int i = 0; i < n; ++i) {
-      float f[kPer];
-      Elem<T>::unpack_word(Elem<T>::floor_word(w[i]), f);
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        const float t = fmaf(f[e], c, -M), x = exp2_fast(t);
-        S += x;
-        U = fmaf(t, x, U);
-      }
+    for (int i = 0; i < n; i += Elem<T>::kPairWords) {
+      const uint64_t t = fma_pair(Elem<T>::unpack_pair(w + i), c2, minus_m);
+      float t0, t1;
+      unpair(t, t0, t1);
+      const uint64_t x = pair(exp2_fast(t0), exp2_fast(t1));
+      S2 = add_pair(S2, x);
+      U2 = fma_pair(t, x, U2);
     }
   }
   // the triple relative to m itself instead of the rounded M; of no account where exact_needed is set
   __device__ __forceinline__ RowStat done(float c) const {
     if (m == -CUDART_INF_F) return RowStat{m, 0.f, 0.f};
+    float s0, s1, u0, u1;
+    unpair(S2, s0, s1);
+    unpair(U2, u0, u1);
+    const float S = s0 + s1, U = u0 + u1;
     const float d = fmaf(m, c, -M), sc = exp2_fast(-d);
     return RowStat{m, S * sc, (U - d * S) * sc};
   }

@@ -15,13 +15,14 @@
 namespace cwl {
 namespace {
 
-constexpr int kLpThreads = 128;       // small blocks, eight to an SM: while one row selects, others stream
+constexpr int kLpThreads = 128;       // small blocks, seven to an SM: while one row selects, others stream
 constexpr int kLpWarps = kLpThreads / 32;
 constexpr int kLpBatch = 4;           // 16-byte loads in flight per thread
 constexpr int kLpBatchVecs = kLpThreads * kLpBatch;
 constexpr int kSegs = 8;              // cells per thread
 constexpr int kMaxCand = 1152;        // logits above the bound kept for sorting; with fewer than K threads that hold
                                       // anything a slice has at most (CWL_MAX_TOP_K - 1) * 8 + 14 elements, which fit
+constexpr int kMaxVecs = 256;         // vectors that reach the bound, gathered in the place of the cells (4 KB) and maxima (1 KB)
 constexpr int kMaxTies = 256;         // logits equal to the bound kept for sorting
 constexpr int kMaxLpCluster = 8;
 constexpr uint32_t kKeyOfMinusInf = 0x007FFFFFu;
@@ -44,7 +45,7 @@ __device__ __forceinline__ unsigned long long rank_key(uint32_t key, int idx) {
 
 struct LpShared {
   alignas(16) unsigned long long cand[kMaxCand + 2];   // candidates
-  uint32_t cell[kSegs * kLpThreads];                   // order key of every cell's maximum, 0 for an empty cell
+  alignas(16) uint32_t cell[kSegs * kLpThreads];       // order key of every cell's maximum, 0 for an empty cell
   uint32_t half[2 * kLpThreads];                       // the largest of a thread's even cells, of its odd ones
   RowStat part[kLpWarps];
   uint32_t hist[256];
@@ -52,7 +53,7 @@ struct LpShared {
   int warp_count[kLpWarps];
   uint16_t hits[kSegs * kLpThreads];
   uint32_t thr;
-  int n_hits, n_cand, n_ties, rest;
+  int n_hits, n_cand, n_ties, n_vecs, rest;
 };
 // Shared memory of the leader of a cluster that the others write: every CTA's sorted list (top_k places each, a shorter
 // one ends in zeros), then every CTA's triple.
@@ -177,7 +178,7 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
   const int tid = threadIdx.x, lane = tid & 31;
   if (tid < 32) {
     const uint32_t bound = cell_bound<T>(sh.half, want);
-    if (lane == 0) { sh.n_hits = 0; sh.n_cand = 0; sh.n_ties = 0; sh.thr = bound; }
+    if (lane == 0) { sh.n_hits = 0; sh.n_cand = 0; sh.n_ties = 0; sh.n_vecs = 0; sh.thr = bound; }
   }
   __syncthreads();
   uint32_t thr = sh.thr;
@@ -202,6 +203,10 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
   const float inv_per_cell = 1.f / (float)per_cell;
   const uint4* zv = reinterpret_cast<const uint4*>(z + rs.head) + rs.v0;
   const uint4 pad = make_uint4(Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked());
+  // The few vectors that hold anything are gathered (where the cells and their maxima were, which have served) and their
+  // elements dealt to all threads: taken in place, every warp would walk all elements of its vectors for a lane or two.
+  uint4* vecs = reinterpret_cast<uint4*>(sh.cell);
+  int* vec_at = reinterpret_cast<int*>(sh.half);
   constexpr int kAhead = 4;                              // second reads in flight per thread
   for (int w0 = tid; w0 < n_work; w0 += kLpThreads * kAhead) {
     uint4 q[kAhead];
@@ -225,14 +230,23 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
     for (int u = 0; u < kAhead; ++u) {
       const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
       if (at[u] >= 0 && Elem<T>::max_of(w) >= bound) {
-        // few vectors come here: one copy of the code, the elements shifted through
-        uint4 v = q[u];
-        const int first = rs.head + (rs.v0 + at[u]) * kVec;
+        const int slot = atomicAdd(&sh.n_vecs, 1);
+        if (slot < kMaxVecs) {
+          vecs[slot] = q[u];
+          vec_at[slot] = at[u];
+        } else {                                         // many vectors reach the bound: element by element, here
+          uint4 v = q[u];
+          const int first = rs.head + (rs.v0 + at[u]) * kVec;
 #pragma unroll 1
-        for (int e = 0; e < kVec; ++e) take_candidate(sh, Elem<T>::shift_out(v), first + e, bound, all);
+          for (int e = 0; e < kVec; ++e) take_candidate(sh, Elem<T>::shift_out(v), first + e, bound, all);
+        }
       }
     }
   }
+  __syncthreads();
+  for (int i = tid; i < min(sh.n_vecs, kMaxVecs) * kVec; i += kLpThreads)
+    take_candidate(sh, Elem<T>::to_float(reinterpret_cast<const T*>(vecs)[i]), rs.head + (rs.v0 + vec_at[i / kVec]) * kVec + i % kVec,
+                   bound, all);
   if (tid < rs.own_head) take_candidate(sh, Elem<T>::load(z + tid), tid, bound, all);
   if (tid < rs.own_tail) take_candidate(sh, Elem<T>::load(z + rs.tail_start + tid), rs.tail_start + tid, bound, all);
   __syncthreads();
@@ -272,7 +286,7 @@ __device__ __forceinline__ int place_among(const LpShared& sh, unsigned long lon
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kLpThreads, 8)
+__global__ void __launch_bounds__(kLpThreads, 7)
 token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
   pdl_launch_dependents();
   __shared__ LpShared sh;
@@ -302,16 +316,18 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
     float seg_max = -CUDART_INF_F;
     uint32_t half_key[2] = {0u, 0u};
     int seg = 0, left = per_seg;
-    for (int b = 0; b < n_batch; ++b, src += kLpBatchVecs) {
-      uint4 q[kLpBatch];
+    auto load = [&](int b, uint4 (&q)[kLpBatch]) {
+      const uint4* at = src + b * kLpBatchVecs;
       if ((b + 1) * kLpBatchVecs <= nv) {
 #pragma unroll
-        for (int u = 0; u < kLpBatch; ++u) q[u] = __ldg(src + u * kLpThreads);
+        for (int u = 0; u < kLpBatch; ++u) q[u] = __ldg(at + u * kLpThreads);
       } else {
 #pragma unroll
         for (int u = 0; u < kLpBatch; ++u)               // a padding vector (-inf) contributes nothing
-          q[u] = b * kLpBatchVecs + u * kLpThreads + tid < nv ? __ldg(src + u * kLpThreads) : pad;
+          q[u] = b * kLpBatchVecs + u * kLpThreads + tid < nv ? __ldg(at + u * kLpThreads) : pad;
       }
+    };
+    auto process = [&](int b, const uint4 (&q)[kLpBatch]) {
       uint32_t w[4 * kLpBatch];
 #pragma unroll
       for (int u = 0; u < kLpBatch; ++u) { w[4 * u] = q[u].x; w[4 * u + 1] = q[u].y; w[4 * u + 2] = q[u].z; w[4 * u + 3] = q[u].w; }
@@ -328,6 +344,13 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
           left = per_seg;
         }
       }
+    };
+    for (int b = 0; b < n_batch; b += 2) {
+      uint4 q[kLpBatch], r[kLpBatch];
+      load(b, q);
+      if (b + 1 < n_batch) load(b + 1, r);
+      process(b, q);
+      if (b + 1 < n_batch) process(b + 1, r);
     }
     if (p.top_k > 0) {
       for (; seg < kSegs; ++seg) sh.cell[seg * kLpThreads + tid] = 0u;
