@@ -4,27 +4,35 @@
 //   dz_v = dloss w tau ( q_v (sum p + p_rest) - p_v - [v outside the entries] p_rest q_v / q_rest )
 //
 // The statistics of a row must be known before its first gradient can be written, so the row stays in shared memory in
-// between: one CTA holds it, or a cluster of up to eight CTAs holds a contiguous slice each and exchanges (m, S) through
-// distributed shared memory.  Logits cross HBM once and the gradient once.  The entries' logits are lifted out of the
-// row (their places become -inf) before the sums run: what is summed is then the mass outside the entries itself, not a
-// difference of two nearly equal sums, and the elementwise gradient leaves those places 0 for the entries' own values.
+// between.  Logits cross HBM once and the gradient once.  The entries' logits are lifted out of the row (their places
+// become -inf) before the sums run: what is summed is then the mass outside the entries itself, not a difference of two
+// nearly equal sums, and the elementwise gradient leaves those places 0 for the entries' own values.
+//
+// Two kernels.  Rows of up to kSmallRowBytes: one block of 128 threads a row, many blocks to an SM, which overlap one
+// another's phases.  Longer rows, and few rows: one persistent block an SM that pipelines rows through up to three
+// buffers, alone or in a cluster of up to eight blocks that hold a contiguous slice of each row and exchange (m, S)
+// through distributed shared memory.
+#include <atomic>
 #include <cmath>
 
 #include "logits_common.cuh"
+#include "tcgen05_common.cuh"
 
 namespace cwl {
 namespace {
 
-constexpr int kDsThreads = 256;
+constexpr int kDsThreads = 128;           // of the kernel for short rows; at least CWL_MAX_TOP_K
 constexpr int kDsWarps = kDsThreads / 32;
 constexpr int kMaxDsCluster = 8;
-constexpr int kDsSliceMax = 208 * 1024;      // bytes of a row one CTA can hold
+constexpr int kSmallRowBytes = 16 * 1024;
 
 struct DistillParams {
   const void* logits; int64_t ld; int T, V;
   const int32_t* ids; const float* values; int64_t ld_teacher; int K;
   int mode;
   float temperature, c, inv_temp;
+  double inv_temp_d;
+  int ordinary;               // temperature within what the short form of the exponent takes
   const float *weight, *dloss;
   float* loss;
   void* dlogits; int64_t ld_d;
@@ -32,10 +40,8 @@ struct DistillParams {
 };
 
 struct DsShared {
-  float m_all[kMaxDsCluster], s_all[kMaxDsCluster], in_all[kMaxDsCluster];   // every CTA's max, outside sum, entries' sum
   int id[CWL_MAX_TOP_K];          // -1 for padding
   float p[CWL_MAX_TOP_K];         // teacher probability
-  float z[CWL_MAX_TOP_K];         // student logits of the entries (in the leader: of all CTAs)
   float red[kDsWarps], red2[kDsWarps];
   double red_d[kDsWarps];
 };
@@ -64,11 +70,10 @@ __device__ __forceinline__ float warp_max_nan(float v) {
 
 // Writes one row slice of gradients: whole 16-byte vectors where the output row starts at the same offset from a 16-byte
 // boundary as the input row, element by element otherwise.  value(i, f) fills f with the gradients of vector i.
-template <typename T, typename F, typename G>
-__device__ __forceinline__ void store_slice(T* d, bool same_phase, const RowSlice& rs, F vec_value, G scalar_value) {
+template <typename T, int kThreads, typename F, typename G>
+__device__ __forceinline__ void store_slice(int tid, T* d, bool same_phase, const RowSlice& rs, F vec_value, G scalar_value) {
   constexpr int kVec = Elem<T>::kVec;
-  const int tid = threadIdx.x;
-  for (int i = rs.v0 + tid; i < rs.v1; i += kDsThreads) {
+  for (int i = rs.v0 + tid; i < rs.v1; i += kThreads) {
     float f[kVec];
     vec_value(i, f);
     T* out = d + rs.head + (int64_t)i * kVec;
@@ -83,173 +88,199 @@ __device__ __forceinline__ void store_slice(T* d, bool same_phase, const RowSlic
   if (tid < rs.own_tail) d[rs.tail_start + tid] = Elem<T>::from_float(scalar_value(rs.tail_start + tid));
 }
 
+template <typename T, int kThreads>
+__device__ __forceinline__ void zero_slice(int tid, T* d, bool same_phase, const RowSlice& rs) {
+  store_slice<T, kThreads>(tid, d, same_phase, rs, [](int, float (&f)[Elem<T>::kVec]) {
+#pragma unroll
+    for (int e = 0; e < Elem<T>::kVec; ++e) f[e] = 0.f;
+  }, [](int) { return 0.f; });
+}
+
+// One entry of the teacher, and what all entries of its row share.
+struct Entry {
+  int id;               // -1: padding
+  float value;
+  float p;              // probability
+  double lp;            // its logarithm
+  float p_id;           // probability of the id over all its occurrences, at the first of them; -1 elsewhere
+  float z;              // the student's logit
+  float p_in, p_rest;   // sum of the entries' probabilities; what is left to the rest
+};
+struct EntryRest { double lp; int id; float p, p_id, z; };   // what the loss and the entry's own gradient take of it
+__device__ __forceinline__ void load_entry(const DistillParams& p, int row, int j, Entry& en) {
+  en.id = -1; en.value = 0.f; en.p = 0.f; en.lp = 0.0; en.p_id = -1.f; en.z = 0.f; en.p_in = 0.f; en.p_rest = 0.f;
+  if (j < p.K) {
+    en.id = __ldg(p.ids + (int64_t)row * p.ld_teacher + j);
+    const float v = __ldg(p.values + (int64_t)row * p.ld_teacher + j);
+    if (en.id >= p.V) { flag_status(p.status_word, CWL_ERR_INVALID_ARG); en.id = -1; }
+    if (en.id >= 0) en.value = v;
+  }
+}
+// the entry's weight before normalisation (also left in en.p); v_max: the largest value of the row, for CWL_TEACHER_LOGITS
+__device__ __forceinline__ double entry_weight(const DistillParams& p, float v_max, Entry& en) {
+  if (en.id >= 0) en.p = expf(p.mode == CWL_TEACHER_LOGITS ? (en.value - v_max) * p.inv_temp : en.value);
+  return (double)en.p;
+}
+__device__ __forceinline__ void finish_entry(const DistillParams& p, float v_max, double p_sum, Entry& en) {
+  if (p.mode == CWL_TEACHER_LOGITS) {
+    // no entries at all: nothing to learn from this row
+    en.lp = ((double)en.value - (double)v_max) * p.inv_temp_d - log(p_sum);
+    en.p *= p_sum == 0.0 ? 0.f : (float)(1.0 / p_sum);
+    en.p_in = p_sum == 0.0 ? 0.f : p_sum == p_sum ? 1.f : CUDART_NAN_F;
+    en.p_rest = 0.f;
+  } else {
+    en.lp = (double)en.value;
+    en.p_in = (float)p_sum;
+    en.p_rest = p_sum == p_sum ? (float)fmax(0.0, 1.0 - p_sum) : CUDART_NAN_F;
+  }
+}
+__device__ __forceinline__ float merged_probability(const int* ids, const float* probs, int K, int j) {
+  const int id = ids[j];
+  float sum = 0.f;
+  bool seen = false;
+  for (int k = 0; k < K; ++k) {
+    if (ids[k] == id) {
+      seen = seen || k < j;
+      sum += probs[k];
+    }
+  }
+  return seen ? -1.f : sum;
+}
+// m, the mass outside the entries and all of it from the slices' statistics; a bad row gives m = 0 and NaN masses
+__device__ __forceinline__ void row_statistics(const float (*slot)[4], int n_cta, float c, float& m, float& s, float& s_row) {
+  m = slot[0][0];
+  for (int r = 1; r < n_cta; ++r) m = max_nan(m, slot[r][0]);
+  s = 0.f;
+  float s_in = 0.f;
+  for (int r = 0; r < n_cta; ++r) {
+    if (slot[r][0] == -CUDART_INF_F) continue;
+    const float scale = exp2_fast((slot[r][0] - m) * c);
+    s += slot[r][1] * scale;
+    s_in += slot[r][2] * scale;
+  }
+  if (bad_max(m)) { m = 0.f; s = CUDART_NAN_F; }
+  s_row = s + s_in;
+}
+// This entry's share of the loss (thread 0 adds the rest's), in fp64: the terms nearly cancel where the student is close
+// to the teacher.
+__device__ __forceinline__ double loss_term(const DistillParams& p, int id, float prob, double lp, float z, float p_rest, float m, float s,
+                                            float s_row, int tid) {
+  double term = 0.0;
+  const double ln_s = log((double)s_row);
+  if (id >= 0 && !(prob == 0.f)) term = (double)prob * (lp - (((double)z - (double)m) * p.inv_temp_d - ln_s));
+  if (tid == 0 && !(p_rest == 0.f)) term += (double)p_rest * (log((double)p_rest) - (log((double)s) - ln_s));
+  if (tid == 0 && !(s_row == s_row)) term = (double)CUDART_NAN_F;
+  return term;
+}
+// outside the entries the gradient is 2^t times this: (total - p_rest / q_rest) / S; with no mass outside there is nothing
+// to scale
+__device__ __forceinline__ float outside_factor(float total, float p_rest, float s, float s_row) {
+  return (s > 0.f ? total - p_rest * (s_row / s) : (s == s ? 0.f : s)) * (1.f / s_row);
+}
+__device__ __forceinline__ float entry_gradient(const DistillParams& p, float z, float p_id, float total, float m, float s_row) {
+  return exp2_fast((z - m) * p.c) * (1.f / s_row) * total - p_id;
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kDsThreads)
-distill_kernel(const DistillParams p, const int log2_cta) {
+distill_small_kernel(const DistillParams p) {
   constexpr int kVec = Elem<T>::kVec;
-  const int n_cta = 1 << log2_cta;
   pdl_launch_dependents();
   extern __shared__ __align__(16) uint8_t ds_raw[];
   __shared__ DsShared sh;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int cta = n_cta > 1 ? (int)cluster_rank() : 0;
-  const int n_rows_at_once = gridDim.x >> log2_cta;
-  if (n_cta > 1) cluster_barrier();                // the peers run before anything is written to their shared memory
   pdl_wait();
 
-  for (int row = blockIdx.x >> log2_cta; row < p.T; row += n_rows_at_once) {
+  for (int row = blockIdx.x; row < p.T; row += gridDim.x) {
     const T* z = reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.ld;
     T* d = p.dlogits != nullptr ? reinterpret_cast<T*>(p.dlogits) + (int64_t)row * p.ld_d : nullptr;
-    const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
+    const RowSlice rs = row_slice<T>(z, p.V, 0, 0);
     const bool same_phase = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(d)) & 15u) == 0;
     const float w = p.weight != nullptr ? p.weight[row] : 1.f;
-    if (w == 0.f) {                                // a row that is not trained on: not read (the whole cluster agrees)
-      if (d != nullptr)
-        store_slice<T>(d, same_phase, rs, [](int, float (&f)[kVec]) {
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) f[e] = 0.f;
-        }, [](int) { return 0.f; });
-      if (p.loss != nullptr && cta == 0 && tid == 0) p.loss[row] = 0.f;
+    if (w == 0.f) {                                // a row that is not trained on: not read
+      if (d != nullptr) zero_slice<T, kDsThreads>(tid, d, same_phase, rs);
+      if (p.loss != nullptr && tid == 0) p.loss[row] = 0.f;
       continue;
     }
-    // shared-memory image of the slice: element i of the row at smem[i - e0 + lead], vectors on 16-byte boundaries
-    const int lead = (kVec - rs.own_head % kVec) % kVec;
+    // shared-memory image of the row: element i at sm[i + lead], vectors on 16-byte boundaries
+    const int lead = (kVec - rs.head % kVec) % kVec;
     T* sm = reinterpret_cast<T*>(ds_raw);
-    const uint32_t sm_addr = (uint32_t)__cvta_generic_to_shared(sm);
-    auto at = [&](int i) { return i - rs.e0 + lead; };
     const uint4* zv = reinterpret_cast<const uint4*>(z + rs.head);
-    const uint32_t vec_base = sm_addr + (uint32_t)(rs.v1 > rs.v0 ? at(rs.head + rs.v0 * kVec) : 0) * (uint32_t)sizeof(T);
-    for (int i = rs.v0 + tid; i < rs.v1; i += kDsThreads) cp_async16(vec_base + (uint32_t)(i - rs.v0) * 16u, zv + i);
-    if (tid < rs.own_head) sm[at(tid)] = z[tid];
-    if (tid < rs.own_tail) sm[at(rs.tail_start + tid)] = z[rs.tail_start + tid];
+    const uint32_t vec_base = (uint32_t)__cvta_generic_to_shared(sm + rs.head + lead);
+    for (int i = tid; i < rs.v1; i += kDsThreads) cp_async16(vec_base + (uint32_t)i * 16u, zv + i);
+    if (tid < rs.own_head) sm[lead + tid] = z[tid];
+    if (tid < rs.own_tail) sm[lead + rs.tail_start + tid] = z[rs.tail_start + tid];
 
-    // teacher entries, while the row is on its way (K <= 128: the first four warps, one entry a thread)
-    const bool renorm = p.mode == CWL_TEACHER_LOGITS;
-    int id = -1;
-    float u = -CUDART_INF_F;       // the entry's value
-    double lp;                     // ln p of the entry
-    if (tid < p.K) {
-      id = p.ids[(int64_t)row * p.ld_teacher + tid];
-      if (id >= p.V) { flag_status(p.status_word, CWL_ERR_INVALID_ARG); id = -1; }
-      if (id >= 0) u = p.values[(int64_t)row * p.ld_teacher + tid];
-      sh.id[tid] = id;
-    }
-    float u_max = 0.f;
-    if (renorm) {
-      const float mx = warp_max_nan(u);
+    // teacher entries, one a thread, while the row is on its way
+    Entry en;
+    load_entry(p, row, tid, en);
+    if (tid < p.K) sh.id[tid] = en.id;
+    float v_max = 0.f;
+    if (p.mode == CWL_TEACHER_LOGITS) {
+      const float mx = warp_max_nan(en.id >= 0 ? en.value : -CUDART_INF_F);
       if (lane == 0) sh.red[wid] = mx;
       __syncthreads();
-      u_max = sh.red[0];
-      for (int i = 1; i < kDsWarps; ++i) u_max = max_nan(u_max, sh.red[i]);
+      v_max = sh.red[0];
+      for (int i = 1; i < kDsWarps; ++i) v_max = max_nan(v_max, sh.red[i]);
     }
-    float pj = id >= 0 ? expf(renorm ? (u - u_max) * p.inv_temp : u) : 0.f;
-    double p_sum = warp_sum((double)pj);
+    double p_sum = warp_sum(entry_weight(p, v_max, en));
     if (lane == 0) sh.red_d[wid] = p_sum;
     __syncthreads();
     p_sum = 0.0;
     for (int i = 0; i < kDsWarps; ++i) p_sum += sh.red_d[i];
-    float p_in = (float)p_sum, p_rest = 0.f;
-    if (renorm) {
-      lp = ((double)u - (double)u_max) / (double)p.temperature - log(p_sum);
-      pj *= p_sum == 0.0 ? 0.f : (float)(1.0 / p_sum);           // no entries at all: nothing to learn from this row
-      p_in = p_sum == 0.0 ? 0.f : p_sum == p_sum ? 1.f : CUDART_NAN_F;
-    } else {
-      lp = (double)u;
-      p_rest = p_sum == p_sum ? (float)fmax(0.0, 1.0 - p_sum) : CUDART_NAN_F;
-    }
-    if (tid < p.K) sh.p[tid] = pj;
+    finish_entry(p, v_max, p_sum, en);
+    if (tid < p.K) sh.p[tid] = en.p;
     cp_async_wait_all();
-    __syncthreads();                               // slice and entries are in shared memory
+    __syncthreads();                               // row and entries are in shared memory
 
-    // lift the entries out of the slice
-    float z_id = 0.f;
-    float p_id = -1.f;             // probability of the entry's id: over all its occurrences, at the first of them; else -1
-    bool mine = false;
-    if (id >= 0) {
-      mine = id >= rs.e0 && id < rs.e1;
-      if (mine) z_id = Elem<T>::to_float(sm[at(id)]);
-      p_id = 0.f;
-      for (int j = 0; j < p.K; ++j) {
-        if (sh.id[j] == id) {
-          if (j < tid) { p_id = -1.f; break; }
-          p_id += sh.p[j];
-        }
-      }
+    // lift the entries out of the row
+    if (en.id >= 0) {
+      en.z = Elem<T>::to_float(sm[lead + en.id]);
+      en.p_id = merged_probability(sh.id, sh.p, p.K, tid);
     }
     __syncthreads();
-    if (mine) sm[at(id)] = Elem<T>::from_float(-CUDART_INF_F);
+    if (en.id >= 0) sm[lead + en.id] = Elem<T>::from_float(-CUDART_INF_F);
     __syncthreads();
 
-    // maximum over the slice and its entries, then the sums relative to it
-    float m = mine ? z_id : -CUDART_INF_F;
-    const uint4* sv = reinterpret_cast<const uint4*>(ds_raw + (vec_base - sm_addr));
-    const int n_vec = rs.v1 - rs.v0;
-    for (int i = tid; i < n_vec; i += kDsThreads) {
-      float f[kVec];
-      Elem<T>::unpack(sv[i], f);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) m = max_nan(m, f[e]);
+    // maximum over the row and its entries, then the sums relative to it
+    float m = en.id >= 0 ? en.z : -CUDART_INF_F;
+    const uint4* sv = reinterpret_cast<const uint4*>(sm + rs.head + lead);
+    for (int i = tid; i < rs.v1; i += kDsThreads) {
+      const uint4 q = sv[i];
+      const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+      m = max_nan(m, Elem<T>::max_of(words));
     }
-    if (tid < rs.own_head) m = max_nan(m, Elem<T>::to_float(sm[at(tid)]));
-    if (tid < rs.own_tail) m = max_nan(m, Elem<T>::to_float(sm[at(rs.tail_start + tid)]));
-    m = warp_max_nan(m);
+    if (tid < rs.own_head) m = max_nan(m, Elem<T>::to_float(sm[lead + tid]));
+    if (tid < rs.own_tail) m = max_nan(m, Elem<T>::to_float(sm[lead + rs.tail_start + tid]));
+    m = key_value(__reduce_max_sync(0xffffffffu, order_key(m)));
     if (lane == 0) sh.red[wid] = m;
     __syncthreads();
     m = sh.red[0];
     for (int i = 1; i < kDsWarps; ++i) m = max_nan(m, sh.red[i]);
     __syncthreads();
-    const float m0 = bad_max(m) ? 0.f : m;         // a slice of -inf only sums to 0; NaN and +inf are told by m
+    const bool bad = bad_max(m);
+    if (bad) m = 0.f;
     float s = 0.f;
-    for (int i = tid; i < n_vec; i += kDsThreads) {
+    for (int i = tid; i < rs.v1; i += kDsThreads) {
       float f[kVec];
       Elem<T>::unpack(sv[i], f);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) s += exp2_fast((f[e] - m0) * p.c);
+      for (int e = 0; e < kVec; ++e) s += exp2_fast((f[e] - m) * p.c);
     }
-    if (tid < rs.own_head) s += exp2_fast((Elem<T>::to_float(sm[at(tid)]) - m0) * p.c);
-    if (tid < rs.own_tail) s += exp2_fast((Elem<T>::to_float(sm[at(rs.tail_start + tid)]) - m0) * p.c);
-    float s_in = mine && p_id >= 0.f ? exp2_fast((z_id - m0) * p.c) : 0.f;   // once per distinct id (p_id is -1 at repeats)
+    if (tid < rs.own_head) s += exp2_fast((Elem<T>::to_float(sm[lead + tid]) - m) * p.c);
+    if (tid < rs.own_tail) s += exp2_fast((Elem<T>::to_float(sm[lead + rs.tail_start + tid]) - m) * p.c);
     s = warp_sum(s);
-    s_in = warp_sum(s_in);
-    if (lane == 0) { sh.red[wid] = s; sh.red2[wid] = s_in; }
+    const float s_in_warp = warp_sum(en.p_id >= 0.f ? exp2_fast((en.z - m) * p.c) : 0.f);   // once per distinct id
+    if (lane == 0) { sh.red[wid] = s; sh.red2[wid] = s_in_warp; }
     __syncthreads();
-    s = 0.f; s_in = 0.f;
+    s = 0.f;
+    float s_in = 0.f;
     for (int i = 0; i < kDsWarps; ++i) { s += sh.red[i]; s_in += sh.red2[i]; }
-    if (n_cta > 1) {
-      if (tid < n_cta) {
-        st_peer_f32(peer_shared(&sh.m_all[cta], tid), m);
-        st_peer_f32(peer_shared(&sh.s_all[cta], tid), s);
-        st_peer_f32(peer_shared(&sh.in_all[cta], tid), s_in);
-      }
-      if (mine) st_peer_f32(peer_shared(&sh.z[tid], 0), z_id);
-      cluster_barrier();
-      float m_row = sh.m_all[0];
-      for (int r = 1; r < n_cta; ++r) m_row = max_nan(m_row, sh.m_all[r]);
-      s = 0.f; s_in = 0.f;
-      for (int r = 0; r < n_cta; ++r) {
-        const float mr = sh.m_all[r];
-        if (mr == -CUDART_INF_F) continue;
-        const float scale = exp2_fast((mr - m_row) * p.c);
-        s += sh.s_all[r] * scale;
-        s_in += sh.in_all[r] * scale;
-      }
-      m = m_row;
-    } else if (mine) {
-      sh.z[tid] = z_id;
-    }
-    if (bad_max(m)) { m = 0.f; s = CUDART_NAN_F; }
+    if (bad) s = CUDART_NAN_F;
     const float s_row = s + s_in;
 
-    if (p.loss != nullptr && cta == 0) {
-      // the few terms of the loss in fp64: they nearly cancel where the student is close to the teacher
-      const double ln_s = log((double)s_row);
-      double term = 0.0;
-      if (n_cta == 1) __syncthreads();
-      if (id >= 0 && !(pj == 0.f)) term = (double)pj * (lp - (((double)sh.z[tid] - (double)m) / (double)p.temperature - ln_s));
-      if (tid == 0 && !(p_rest == 0.f)) term += (double)p_rest * (log((double)p_rest) - (log((double)s) - ln_s));
-      if (tid == 0 && !(s_row == s_row)) term = (double)CUDART_NAN_F;
-      term = warp_sum(term);
-      __syncthreads();
+    if (p.loss != nullptr) {
+      const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_rest, m, s, s_row, tid));
       if (lane == 0) sh.red_d[wid] = term;
       __syncthreads();
       if (tid == 0) {
@@ -260,48 +291,429 @@ distill_kernel(const DistillParams p, const int log2_cta) {
     }
     if (d != nullptr) {
       const float up = w * p.temperature * (p.dloss != nullptr ? p.dloss[row] : 1.f);
-      const float total = p_in + p_rest;
-      const float inv_s = 1.f / s_row;
-      // outside the entries: q_v (total - p_rest / q_rest); with no mass outside there is nothing to scale
-      const float outside = s > 0.f ? total - p_rest * (s_row / s) : (s == s ? 0.f : s);
-      const float k_out = outside * up * inv_s;
-      store_slice<T>(d, same_phase, rs, [&](int i, float (&f)[kVec]) {
-        Elem<T>::unpack(sv[i - rs.v0], f);
+      const float k_out = outside_factor(en.p_in + en.p_rest, en.p_rest, s, s_row) * up;
+      store_slice<T, kDsThreads>(tid, d, same_phase, rs, [&](int i, float (&f)[kVec]) {
+        Elem<T>::unpack(sv[i], f);
 #pragma unroll
         for (int e = 0; e < kVec; ++e) f[e] = exp2_fast((f[e] - m) * p.c) * k_out;
-      }, [&](int i) { return exp2_fast((Elem<T>::to_float(sm[at(i)]) - m) * p.c) * k_out; });
+      }, [&](int i) { return exp2_fast((Elem<T>::to_float(sm[lead + i]) - m) * p.c) * k_out; });
       __syncthreads();                             // the entries' places now hold 0: put their own values there
-      if (mine && p_id >= 0.f) d[id] = Elem<T>::from_float((exp2_fast((z_id - m) * p.c) * inv_s * total - p_id) * up);
+      if (en.p_id >= 0.f) d[en.id] = Elem<T>::from_float(entry_gradient(p, en.z, en.p_id, en.p_in + en.p_rest, m, s_row) * up);
     }
-    // the next row overwrites the shared arrays; the peers must have read this CTA's
-    if (n_cta > 1) cluster_barrier(); else __syncthreads();
+    __syncthreads();                               // the next row overwrites the shared arrays
   }
 }
 
-// CTAs that share a row: as few as hold it in slices of kSliceWanted bytes (three CTAs fit an SM, so that one loads while
-// another sums and a third writes), more while the rows do not fill the GPU.
+// ------------------------------------------------------------------------------------------------ long rows, few rows
+constexpr int kEntryThreads = 128;             // warps 0..3 (prepare) and 4..7 (finish): one teacher entry a thread
+constexpr int kSumThreads = 512;               // warps 8..23: sums and gradients
+constexpr int kSumWarps = kSumThreads / 32;
+constexpr int kPipeThreads = 2 * kEntryThreads + kSumThreads;
+constexpr int kMaxBuffers = 3;
+constexpr int kSlots = 4;                      // rows under way between the roles of a block, and statistics between blocks
+constexpr int kLogitSlots = 8;                 // entries' logits on their way to the first block of a cluster
+constexpr int kCopyBytes = 16 * 1024;          // piece of a slice that one bulk copy brings
+constexpr unsigned long long kDsWaitLimitNs = 2000000000ull;
+
+struct DsPipe {
+  alignas(8) unsigned long long full[kMaxBuffers], ready[kMaxBuffers], xchg[kSlots];
+  alignas(16) int misc[8];                     // [1] gave up, [4..5] wait limit in ns (the layout mbar_wait expects)
+  float slot[kSlots][kMaxDsCluster][4];        // (m, S outside the entries, S of the entries) of every block's slice
+  float z[kLogitSlots][CWL_MAX_TOP_K];         // student logits of the entries (in the first block: of all slices)
+  EntryRest entry[kSlots][CWL_MAX_TOP_K];      // from prepare to finish
+  float entry_stat[kSlots][2];                 // (m, S) of this slice's entries
+  float mass[kSlots][2];                       // sum of the teacher's probabilities, and what they leave to the rest
+  int id[CWL_MAX_TOP_K];
+  float p[CWL_MAX_TOP_K];
+  float red[kEntryThreads / 32], red2[kEntryThreads / 32];
+  double red_d[kEntryThreads / 32], red_loss[kEntryThreads / 32];
+  float sum_m[kSumWarps], sum_s[kSumWarps];
+  int repeated;                                // some id occurs twice
+};
+
+struct PipePlan {
+  int log2_cta, n_buffers, buffer_bytes;
+};
+
+__device__ __forceinline__ void prepare_barrier() { __syncwarp(); asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void sum_barrier() { __syncwarp(); asm volatile("bar.sync 2, 512;" ::: "memory"); }
+__device__ __forceinline__ void finish_barrier() { __syncwarp(); asm volatile("bar.sync 3, 128;" ::: "memory"); }
+// the gradients of row n's slice are stored: the sum warps say so and go on, the finish warps wait for it
+__device__ __forceinline__ void stored_arrive(int n) { __syncwarp(); asm volatile("bar.arrive %0, 640;" ::"r"(4 + n % kSlots) : "memory"); }
+__device__ __forceinline__ void stored_wait(int n) { __syncwarp(); asm volatile("bar.sync %0, 640;" ::"r"(4 + n % kSlots) : "memory"); }
+static_assert(kEntryThreads == 128 && kSumThreads == 512, "the barriers' counts");
+
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_peer(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// the bounded wait of mbar_wait, ordered with the arrivals of the whole cluster
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (!mbar_wait(bar, parity, abort_flag)) return false;
+  asm volatile("fence.acq_rel.cluster;" ::: "memory");
+  return true;
+}
+__device__ __forceinline__ void bulk_copy_in(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+// The rows first, first + stride, ... that are trained on; the next one's weight is fetched a row ahead.
+struct RowCursor {
+  const float* weight;
+  int T, stride, row;
+  float ahead;
+  __device__ __forceinline__ float weight_of(int r) const { return weight != nullptr && r < T ? __ldg(weight + r) : 1.f; }
+  __device__ __forceinline__ void start(const float* w, int rows, int first, int step) {
+    weight = w; T = rows; stride = step; row = first - step;
+    ahead = weight_of(first);
+  }
+  __device__ __forceinline__ bool next(float& w) {
+    do {
+      row += stride;
+      w = ahead;
+      ahead = weight_of(row + stride);
+    } while (row < T && w == 0.f);
+    return row < T;
+  }
+};
+
+// One block: rows first, first + stride, ...; rows of weight 0 take no part in the numbering below.  Row number n goes
+// through buffer n % n_buffers:
+//   a finish thread  copies the slice in (full), as soon as row n - n_buffers has left the buffer
+//   prepare warps    entries of the teacher; once the slice is there, lift the entries out of it (ready)
+//   sum warps        sum what is left; their (m, S) with the entries' goes to every block of the cluster (xchg), and once
+//                    all have arrived the gradient of the slice is stored (stored)
+//   finish warps     loss (in the first block of the cluster); gradient of the entries; the next copy
+// How far they drift apart: row k needs its copy, so finish is past row k - n_buffers wherever prepare or the sums are at
+// row k, and four slots and `stored` barriers serve a block.  A block's sums are at most one row ahead of another's, whose
+// finish is at most two rows behind its sums: four slots of statistics.  A block's prepare is at most three rows ahead of
+// another's sums, five ahead of its finish: eight slots of logits.
+// Every wait on a barrier in memory is bounded; one that runs out raises CWL_ERR_TIMEOUT, after which nothing is stored
+// any more, but the loops run to their end so that no other warp or block is left waiting.
+template <typename T>
+__global__ void __launch_bounds__(kPipeThreads, 1)
+distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
+  constexpr int kVec = Elem<T>::kVec;
+  pdl_launch_dependents();
+  extern __shared__ __align__(128) uint8_t ds_raw[];
+  DsPipe& sh = *reinterpret_cast<DsPipe*>(ds_raw + plan.n_buffers * plan.buffer_bytes);
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  const int log2_cta = plan.log2_cta, n_cta = 1 << log2_cta;
+  const int cta = log2_cta > 0 ? (int)cluster_rank() : 0;
+  const int first = blockIdx.x >> log2_cta, stride = gridDim.x >> log2_cta;
+  volatile int* abort_flag = sh.misc + 1;
+  auto full_bar = [&](int b) { return smem_u32(&sh.full[b]); };
+  auto ready_bar = [&](int b) { return smem_u32(&sh.ready[b]); };
+  auto xchg_bar = [&](int k) { return smem_u32(&sh.xchg[k]); };
+  if (tid == 0) {
+    for (int b = 0; b < kMaxBuffers; ++b) { mbar_init(full_bar(b), 1); mbar_init(ready_bar(b), 1); }
+    for (int k = 0; k < kSlots; ++k) mbar_init(xchg_bar(k), n_cta);
+    sh.misc[1] = 0;
+    *reinterpret_cast<volatile unsigned long long*>(sh.misc + 4) = kDsWaitLimitNs;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncthreads();
+  if (log2_cta > 0) cluster_barrier();             // the peers' barriers exist before anything arrives on them
+  pdl_wait();
+
+  auto row_of = [&](int row) { return reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.ld; };
+  auto lead_of = [&](const RowSlice& rs) { return (kVec - rs.own_head % kVec) % kVec; };
+  // element i of the row sits at image[i - e0 + lead]; its vectors begin after own_head + lead elements
+  auto image_of = [&](int n) { return reinterpret_cast<T*>(ds_raw + (n % plan.n_buffers) * plan.buffer_bytes); };
+
+  if (wid < kEntryThreads / 32) {
+    // ---------------------------------------------------------------------------------------------- prepare warps
+    RowCursor at;
+    at.start(p.weight, p.T, first, stride);
+    float w, w_after;
+    bool more = at.next(w);
+    Entry en;
+    if (more) load_entry(p, at.row, tid, en);
+    for (int n = 0; more; ++n) {
+      const int row = at.row;
+      more = at.next(w_after);
+      Entry after;
+      if (more) load_entry(p, at.row, tid, after);       // a row ahead
+      const T* z = row_of(row);
+      const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
+      T* sm = image_of(n) + lead_of(rs) - rs.e0;         // element i of the row at sm[i]
+      float v_max = 0.f;
+      if (p.mode == CWL_TEACHER_LOGITS) {
+        const float mx = warp_max_nan(en.id >= 0 ? en.value : -CUDART_INF_F);
+        if (lane == 0) sh.red[wid] = mx;
+        prepare_barrier();
+        v_max = max_nan(max_nan(sh.red[0], sh.red[1]), max_nan(sh.red[2], sh.red[3]));
+      }
+      const double part = warp_sum(entry_weight(p, v_max, en));
+      if (lane == 0) sh.red_d[wid] = part;
+      prepare_barrier();
+      finish_entry(p, v_max, (sh.red_d[0] + sh.red_d[1]) + (sh.red_d[2] + sh.red_d[3]), en);
+      if (tid < p.K) { sh.id[tid] = en.id; sh.p[tid] = en.p; }
+      if (tid == 0) sh.repeated = 0;
+      const bool mine = en.id >= rs.e0 && en.id < rs.e1;
+      mbar_wait(full_bar(n % plan.n_buffers), (uint32_t)(n / plan.n_buffers) & 1u, abort_flag);
+      __syncwarp();
+      if (tid < rs.own_head) sm[tid] = z[tid];
+      if (tid < rs.own_tail) sm[rs.tail_start + tid] = z[rs.tail_start + tid];
+      prepare_barrier();                                 // head and tail scalars are there too
+      if (mine) en.z = Elem<T>::to_float(sm[en.id]);
+      prepare_barrier();                                 // every entry was read: each leaves its number in its place
+      if (mine) Elem<T>::put_number(sm + en.id, tid);
+      prepare_barrier();
+      if (mine && Elem<T>::number_at(sm + en.id) != tid) sh.repeated = 1;
+      const float mw = key_value(__reduce_max_sync(0xffffffffu, order_key(mine ? en.z : -CUDART_INF_F)));
+      if (lane == 0) sh.red[wid] = mw;
+      prepare_barrier();
+      en.p_id = mine ? en.p : -1.f;
+      if (sh.repeated && mine) en.p_id = merged_probability(sh.id, sh.p, p.K, tid);
+      if (mine) {
+        sm[en.id] = Elem<T>::from_float(-CUDART_INF_F);
+        if (p.loss != nullptr) {
+          float* slot = &sh.z[n % kLogitSlots][tid];
+          st_peer_f32(log2_cta > 0 ? peer_shared(slot, 0) : smem_u32(slot), en.z);
+        }
+      }
+      // (m, S) of this slice's entries, every distinct id once
+      const float me = max_nan(max_nan(sh.red[0], sh.red[1]), max_nan(sh.red[2], sh.red[3]));
+      const float sw = warp_sum(en.p_id >= 0.f && !bad_max(me) ? exp2_fast((en.z - me) * p.c) : 0.f);
+      if (lane == 0) sh.red2[wid] = sw;
+      if (tid < p.K) sh.entry[n % kSlots][tid] = EntryRest{en.lp, en.id, en.p, en.p_id, en.z};
+      prepare_barrier();
+      if (tid == 0) {
+        sh.entry_stat[n % kSlots][0] = me;
+        sh.entry_stat[n % kSlots][1] = (sh.red2[0] + sh.red2[1]) + (sh.red2[2] + sh.red2[3]);
+        sh.mass[n % kSlots][0] = en.p_in;
+        sh.mass[n % kSlots][1] = en.p_rest;
+        mbar_arrive(ready_bar(n % plan.n_buffers));
+      }
+      en = after;
+    }
+  } else if (wid < 2 * kEntryThreads / 32) {
+    // ----------------------------------------------------------------------------------------------- finish warps
+    const int ft = tid - kEntryThreads, fw = wid - kEntryThreads / 32;
+    RowCursor loads;                                     // of thread 0: the slices to copy
+    int loaded = 0;
+    bool more_loads = true;
+    auto copy_next = [&]() {
+      float w;
+      more_loads = more_loads && loads.next(w);
+      if (!more_loads) return;
+      const T* z = row_of(loads.row);
+      const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
+      const int b = loaded % plan.n_buffers;
+      const uint32_t bytes = (uint32_t)(rs.v1 - rs.v0) * 16u;
+      const uint8_t* src = reinterpret_cast<const uint8_t*>(z + rs.head) + (int64_t)rs.v0 * 16;
+      const uint32_t dst = smem_u32(image_of(loaded) + rs.own_head + lead_of(rs));
+      mbar_expect_tx(full_bar(b), bytes);                // an arrival that expects no bytes completes at once
+      for (uint32_t off = 0; off < bytes; off += kCopyBytes)
+        bulk_copy_in(dst + off, src + off, min(bytes - off, (uint32_t)kCopyBytes), full_bar(b));
+      ++loaded;
+    };
+    if (ft == 0) {
+      loads.start(p.weight, p.T, first, stride);
+      for (int b = 0; b < plan.n_buffers; ++b) copy_next();
+    }
+    RowCursor at;
+    at.start(p.weight, p.T, first, stride);
+    float w;
+    for (int n = 0; at.next(w); ++n) {
+      const int row = at.row;
+      const float dl = p.dloss != nullptr ? __ldg(p.dloss + row) : 1.f;
+      const bool ok = mbar_wait_cluster(xchg_bar(n % kSlots), (uint32_t)(n / kSlots) & 1u, abort_flag);
+      __syncwarp();
+      float m, s, s_row;
+      row_statistics(sh.slot[n % kSlots], n_cta, p.c, m, s, s_row);
+      EntryRest e{0.0, -1, 0.f, -1.f, 0.f};
+      if (ft < p.K) e = sh.entry[n % kSlots][ft];
+      const float p_in = sh.mass[n % kSlots][0], p_rest = sh.mass[n % kSlots][1];
+      if (p.loss != nullptr && cta == 0) {
+        const double term = warp_sum(loss_term(p, e.id, e.p, e.lp, ft < p.K ? sh.z[n % kLogitSlots][ft] : 0.f, p_rest, m, s, s_row, ft));
+        if (lane == 0) sh.red_loss[fw] = term;
+        finish_barrier();
+        if (ft == 0 && ok) {
+          const double kl = (sh.red_loss[0] + sh.red_loss[1]) + (sh.red_loss[2] + sh.red_loss[3]);
+          p.loss[row] = (float)((double)w * p.temperature * p.temperature * kl);
+        }
+      }
+      stored_wait(n);
+      if (ft == 0) {
+        asm volatile("fence.proxy.async;" ::: "memory"); // the buffer was read and written with ordinary accesses
+        copy_next();
+      }
+      if (p.dlogits != nullptr && e.p_id >= 0.f && ok && *abort_flag == 0) {
+        T* d = reinterpret_cast<T*>(p.dlogits) + (int64_t)row * p.ld_d;
+        d[e.id] = Elem<T>::from_float(entry_gradient(p, e.z, e.p_id, p_in + p_rest, m, s_row) * (w * p.temperature * dl));
+      }
+    }
+  } else {
+    // -------------------------------------------------------------------------------------------------- sum warps
+    const int st = tid - 2 * kEntryThreads, sw = wid - 2 * kEntryThreads / 32;
+    int n = 0;
+    auto weight_of = [&](int row) { return p.weight != nullptr && row < p.T ? __ldg(p.weight + row) : 1.f; };
+    float w = weight_of(first);
+    for (int row = first; row < p.T; row += stride) {
+      const float w_next = weight_of(row + stride);
+      const T* z = row_of(row);
+      T* d = p.dlogits != nullptr ? reinterpret_cast<T*>(p.dlogits) + (int64_t)row * p.ld_d : nullptr;
+      const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
+      const bool same_phase = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(d)) & 15u) == 0;
+      if (w == 0.f) {                              // a row that is not trained on: not read
+        if (d != nullptr) zero_slice<T, kSumThreads>(st, d, same_phase, rs);
+        if (p.loss != nullptr && cta == 0 && st == 0) p.loss[row] = 0.f;
+        w = w_next;
+        continue;
+      }
+      const float up = w * p.temperature * (p.dloss != nullptr ? __ldg(p.dloss + row) : 1.f);
+      const T* sm = image_of(n) + lead_of(rs) - rs.e0;
+      const uint4* sv = reinterpret_cast<const uint4*>(image_of(n) + rs.own_head + lead_of(rs));
+      const int nv = rs.v1 - rs.v0;
+      mbar_wait(ready_bar(n % plan.n_buffers), (uint32_t)(n / plan.n_buffers) & 1u, abort_flag);
+      __syncwarp();
+
+      RunningSum run;
+      run.start(p.ordinary != 0);
+      int i = st;
+      for (; i + kSumThreads < nv; i += 2 * kSumThreads) {
+        const uint4 q = sv[i], r = sv[i + kSumThreads];
+        const uint32_t words[8] = {q.x, q.y, q.z, q.w, r.x, r.y, r.z, r.w};
+        run.template take_words<T, 8>(words, Elem<T>::max_of(words), p.c);
+      }
+      if (i < nv) {
+        const uint4 q = sv[i];
+        const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+        run.template take_words<T, 4>(words, Elem<T>::max_of(words), p.c);
+      }
+      RowStat a = run.done(p.c);
+      if (run.exact_needed) a = exact_stat<T>(sv, st, kSumThreads, nv, p.c);
+      if (st < rs.own_head) absorb_scalar(a, Elem<T>::to_float(sm[st]), p.c);
+      if (st < rs.own_tail) absorb_scalar(a, Elem<T>::to_float(sm[rs.tail_start + st]), p.c);
+      rescale(a, key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), p.c);
+      a.S = warp_sum(a.S);
+      if (lane == 0) { sh.sum_m[sw] = a.m; sh.sum_s[sw] = a.S; }
+      sum_barrier();
+      if (sw == 0) {
+        // the warps' parts and the entries'; lane r sends the result to block r
+        a = RowStat{sh.sum_m[lane & (kSumWarps - 1)], sh.sum_s[lane & (kSumWarps - 1)], 0.f};
+        const float me = sh.entry_stat[n % kSlots][0];
+        const float m_all = max_nan(key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), me);
+        rescale(a, m_all, p.c);
+        for (int off = kSumWarps / 2; off > 0; off >>= 1) a.S += __shfl_xor_sync(0xffffffffu, a.S, off);
+        RowStat e{me, sh.entry_stat[n % kSlots][1], 0.f};
+        rescale(e, m_all, p.c);
+        if (lane < n_cta) {
+          float* at = sh.slot[n % kSlots][cta];
+          const uint32_t to = log2_cta > 0 ? peer_shared(at, lane) : smem_u32(at);
+          st_peer_f32(to, m_all);
+          st_peer_f32(to + 4, a.S);
+          st_peer_f32(to + 8, e.S);
+          mbar_arrive_peer(log2_cta > 0 ? peer_shared(&sh.xchg[n % kSlots], lane) : xchg_bar(n % kSlots));
+        }
+        __syncwarp();
+      }
+      const bool ok = mbar_wait_cluster(xchg_bar(n % kSlots), (uint32_t)(n / kSlots) & 1u, abort_flag);
+      __syncwarp();
+      if (d != nullptr && ok && *abort_flag == 0) {
+        float m, s, s_row;
+        row_statistics(sh.slot[n % kSlots], n_cta, p.c, m, s, s_row);
+        const float rest = sh.mass[n % kSlots][1];
+        const float k_out = outside_factor(sh.mass[n % kSlots][0] + rest, rest, s, s_row) * up;
+        if (fabsf(m) <= kOrdinaryLogit && p.ordinary != 0) {
+          const float M = m * p.c;
+          const float k = k_out * exp2_fast(-fmaf(m, p.c, -M));
+          const uint64_t c2 = pair(p.c, p.c), minus_m = pair(-M, -M), k2 = pair(k, k), zero = pair(0.f, 0.f);
+          auto grad2 = [&](uint64_t zz) {
+            float t0, t1;
+            unpair(fma_pair(zz, c2, minus_m), t0, t1);
+            return fma_pair(pair(exp2_fast(t0), exp2_fast(t1)), k2, zero);
+          };
+          store_slice<T, kSumThreads>(st, d, same_phase, rs, [&](int v, float (&f)[kVec]) {
+            Elem<T>::unpack(sv[v - rs.v0], f);
+#pragma unroll
+            for (int e = 0; e < kVec; e += 2) {
+              const uint64_t g = grad2(pair(f[e], f[e + 1]));
+              unpair(g, f[e], f[e + 1]);
+            }
+          }, [&](int x) { return exp2_fast((Elem<T>::to_float(sm[x]) - m) * p.c) * k_out; });
+        } else {
+          store_slice<T, kSumThreads>(st, d, same_phase, rs, [&](int v, float (&f)[kVec]) {
+            Elem<T>::unpack(sv[v - rs.v0], f);
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) f[e] = exp2_fast((f[e] - m) * p.c) * k_out;
+          }, [&](int x) { return exp2_fast((Elem<T>::to_float(sm[x]) - m) * p.c) * k_out; });
+        }
+      }
+      stored_arrive(n);
+      w = w_next;
+      ++n;
+    }
+  }
+  __syncthreads();
+  if (tid == 0 && *abort_flag != 0) flag_status(p.status_word, CWL_ERR_TIMEOUT);
+  if (log2_cta > 0) cluster_barrier();             // nobody leaves while a peer may still write to it
+}
+
+static_assert(sizeof(DsPipe) + CWL_MAX_DISTILL_ROW_BYTES / kMaxDsCluster + 160 <= 227 * 1024, "the longest row fits a cluster");
+// How the long-row kernel runs: as few blocks a row as hold it in slices of kSliceWanted bytes (three buffers fit), more
+// while the rows do not fill the GPU, down to slices of 8 KB.
 constexpr int kSliceWanted = 66 * 1024;
-int distill_cluster(int T, int64_t row_bytes) {
-  int c = 1;
-  while (c < kMaxDsCluster && row_bytes / c > kSliceWanted) c *= 2;
-  while (c < kMaxDsCluster && (int64_t)T * c * 2 <= 296 && row_bytes / (c * 2) >= 8192) c *= 2;
-  return c;
+PipePlan pipe_plan(int T, int64_t row_bytes) {
+  PipePlan plan;
+  plan.log2_cta = 0;
+  while ((1 << plan.log2_cta) < kMaxDsCluster && (row_bytes >> plan.log2_cta) > kSliceWanted) ++plan.log2_cta;
+  while ((1 << plan.log2_cta) < kMaxDsCluster && ((int64_t)T << (plan.log2_cta + 1)) <= 148 && (row_bytes >> (plan.log2_cta + 1)) >= 8192)
+    ++plan.log2_cta;
+  const int c = 1 << plan.log2_cta;
+  // one slice: its vectors, and head and tail scalars in a vector of their own each
+  plan.buffer_bytes = ((int)((row_bytes / 16 + c - 1) / c) * 16 + 32 + 127) / 128 * 128;
+  plan.n_buffers = (227 * 1024 - (int)sizeof(DsPipe)) / plan.buffer_bytes;
+  if (plan.n_buffers > kMaxBuffers) plan.n_buffers = kMaxBuffers;
+  return plan;
+}
+
+// Clusters of long-row blocks (one block an SM) that fit the GPU at once; the rows are dealt to that many.
+template <typename T>
+int resident_clusters(int log2_cta, size_t smem) {
+  static std::atomic<int> known[4];                // by log2_cta; every size of shared memory here takes a whole SM
+  const int seen = known[log2_cta].load(std::memory_order_relaxed);
+  if (seen > 0) return seen;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(148u >> log2_cta << log2_cta);
+  cfg.blockDim = dim3(kPipeThreads);
+  cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = 1u << log2_cta; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, distill_pipe_kernel<T>, &cfg) != cudaSuccess || n <= 0) {
+    cudaGetLastError();
+    return 148 >> log2_cta;
+  }
+  known[log2_cta].store(n, std::memory_order_relaxed);
+  return n;
 }
 
 template <typename T>
 cudaError_t launch_distill(const DistillParams& p, cudaStream_t st) {
   const int64_t row_bytes = (int64_t)p.V * sizeof(T);
-  const int c = distill_cluster(p.T, row_bytes);
-  int log2_cta = 0;
-  while ((1 << log2_cta) < c) ++log2_cta;
-  // one slice: its vectors, and head and tail scalars in a vector of their own each
-  const size_t smem = (size_t)((row_bytes / 16 + c - 1) / c) * 16 + 32;
-  if (smem > 40 * 1024) {                          // beyond what a kernel may use without asking
-    const cudaError_t e = cudaFuncSetAttribute(distill_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDsSliceMax + 64);
-    if (e != cudaSuccess) return e;
+  const bool chained = !stream_is_capturing(st);
+  if (row_bytes <= kSmallRowBytes) {
+    const size_t smem = (size_t)(row_bytes / 16) * 16 + 32;
+    const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
+    return launch_clusters(chained, 1, distill_small_kernel<T>, dim3(rows), dim3(kDsThreads), smem, st, p);
   }
-  const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
-  return launch_clusters(!stream_is_capturing(st), c, distill_kernel<T>, dim3(rows * c), dim3(kDsThreads), smem, st, p, log2_cta);
+  const PipePlan plan = pipe_plan(p.T, row_bytes);
+  const size_t smem = (size_t)plan.n_buffers * plan.buffer_bytes + sizeof(DsPipe);
+  const cudaError_t e = cudaFuncSetAttribute(distill_pipe_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  const int clusters = resident_clusters<T>(plan.log2_cta, smem);
+  const int rows = p.T < clusters ? p.T : clusters;
+  return launch_clusters(chained, 1 << plan.log2_cta, distill_pipe_kernel<T>, dim3(rows << plan.log2_cta), dim3(kPipeThreads), smem, st,
+                         p, plan);
 }
 
 }  // namespace
@@ -324,7 +736,7 @@ extern "C" cwl_status cwl_distill_topk(const void* logits, cwl_dtype dtype, int6
   if (reinterpret_cast<uintptr_t>(logits) % es != 0 || reinterpret_cast<uintptr_t>(dlogits) % es != 0) return CWL_ERR_SHAPE;
   if (dlogits == logits && ld_dlogits != ld_logits) return CWL_ERR_SHAPE;
   cwl::DistillParams p{logits, ld_logits, T, V, teacher_ids, teacher_values, ld_teacher, K, (int)mode, temperature,
-                       (float)(1.4426950408889634074 / (double)temperature), (float)(1.0 / (double)temperature), weight, dloss,
+                       (float)(1.4426950408889634074 / (double)temperature), (float)(1.0 / (double)temperature), 1.0 / (double)temperature, cwl::ordinary_temperature(temperature) ? 1 : 0, weight, dloss,
                        loss, dlogits, ld_dlogits, status_word};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   switch (dtype) {

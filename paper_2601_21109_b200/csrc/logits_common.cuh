@@ -55,6 +55,9 @@ template <> struct Elem<float> {
   static __device__ __forceinline__ float load(const float* p) { return __ldg(p); }
   static __device__ __forceinline__ float to_float(float v) { return v; }
   static __device__ __forceinline__ float from_float(float v) { return v; }
+  // a small whole number in the place of an element
+  static __device__ __forceinline__ void put_number(float* p, int n) { *reinterpret_cast<volatile int*>(p) = n; }
+  static __device__ __forceinline__ int number_at(const float* p) { return *reinterpret_cast<const volatile int*>(p); }
   static __device__ __forceinline__ void unpack(const uint4& q, float (&f)[4]) {
     f[0] = __uint_as_float(q.x); f[1] = __uint_as_float(q.y); f[2] = __uint_as_float(q.z); f[3] = __uint_as_float(q.w);
   }
@@ -77,7 +80,8 @@ template <> struct Elem<float> {
   }
   // two elements, -inf (and whatever lies below kMaskedLogit) made finite: of weight 0 beside an ordinary maximum
   static constexpr int kPairWords = 2;
-  static __device__ __forceinline__ uint64_t unpack_pair(const uint32_t* w) {
+  static __device__ __forceinline__ uint64_t unpack_pair(const uint32_t* w) { return pair(__uint_as_float(w[0]), __uint_as_float(w[1])); }
+  static __device__ __forceinline__ uint64_t unpack_pair_floored(const uint32_t* w) {
     return pair(fmaxf(__uint_as_float(w[0]), kMaskedLogit), fmaxf(__uint_as_float(w[1]), kMaskedLogit));
   }
 };
@@ -87,6 +91,8 @@ template <> struct Elem<__nv_bfloat16> {
   static __device__ __forceinline__ float load(const __nv_bfloat16* p) { return __bfloat162float(__ldg(p)); }
   static __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
   static __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
+  static __device__ __forceinline__ void put_number(__nv_bfloat16* p, int n) { *reinterpret_cast<volatile unsigned short*>(p) = (unsigned short)n; }
+  static __device__ __forceinline__ int number_at(const __nv_bfloat16* p) { return *reinterpret_cast<const volatile unsigned short*>(p); }
   static __device__ __forceinline__ void unpack(const uint4& q, float (&f)[8]) {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -118,6 +124,9 @@ template <> struct Elem<__nv_bfloat16> {
   }
   static constexpr int kPairWords = 1;
   static __device__ __forceinline__ uint64_t unpack_pair(const uint32_t* w) {
+    return pair(__uint_as_float(w[0] << 16), __uint_as_float(w[0] & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ uint64_t unpack_pair_floored(const uint32_t* w) {
     uint32_t y;
     asm("max.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(w[0]), "r"(0xF149F149u));     // kMaskedLogit in bf16, twice
     return pair(__uint_as_float(y << 16), __uint_as_float(y & 0xFFFF0000u));
@@ -129,6 +138,8 @@ template <> struct Elem<__half> {
   static __device__ __forceinline__ float load(const __half* p) { return __half2float(__ldg(p)); }
   static __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
   static __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
+  static __device__ __forceinline__ void put_number(__half* p, int n) { *reinterpret_cast<volatile unsigned short*>(p) = (unsigned short)n; }
+  static __device__ __forceinline__ int number_at(const __half* p) { return *reinterpret_cast<const volatile unsigned short*>(p); }
   static __device__ __forceinline__ void unpack(const uint4& q, float (&f)[8]) {
     const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
@@ -161,6 +172,10 @@ template <> struct Elem<__half> {
   }
   static constexpr int kPairWords = 1;
   static __device__ __forceinline__ uint64_t unpack_pair(const uint32_t* w) {
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(w));
+    return pair(v.x, v.y);
+  }
+  static __device__ __forceinline__ uint64_t unpack_pair_floored(const uint32_t* w) {
     uint32_t y;
     asm("max.f16x2 %0, %1, %2;" : "=r"(y) : "r"(w[0]), "r"(0xFBFFFBFFu));      // the type's lowest value, twice
     const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&y));
@@ -215,7 +230,8 @@ __device__ __forceinline__ void absorb_scalar(RowStat& a, float v, float c) {
 // with the exponent clamped.
 constexpr float kOrdinaryLogit = 16384.f;
 constexpr float kLead = 8.f;
-struct RunningStat {
+template <bool kWithU>
+struct Running {
   float m, M, limit;           // reference; m c rounded; the batch maximum up to which the reference stays
   uint64_t S2, U2;             // sums over even and odd elements
   bool exact_needed;
@@ -231,7 +247,7 @@ struct RunningStat {
       const float dt = M - M_new;
       const float sc = m == -CUDART_INF_F ? 0.f : exp2_fast(dt);
       const uint64_t sc2 = pair(sc, sc), zero = pair(0.f, 0.f);
-      U2 = fma_pair(fma_pair(pair(dt, dt), S2, U2), sc2, zero);
+      if (kWithU) U2 = fma_pair(fma_pair(pair(dt, dt), S2, U2), sc2, zero);
       S2 = fma_pair(S2, sc2, zero);
       m = m_new; M = M_new;
       limit = m_new + kLead / c;
@@ -240,12 +256,13 @@ struct RunningStat {
     const uint64_t c2 = pair(c, c), minus_m = pair(-M, -M);
 #pragma unroll
     for (int i = 0; i < n; i += Elem<T>::kPairWords) {
-      const uint64_t t = fma_pair(Elem<T>::unpack_pair(w + i), c2, minus_m);
+      // without U no exponent is multiplied by its weight of 0, and -inf may stay
+      const uint64_t t = fma_pair(kWithU ? Elem<T>::unpack_pair_floored(w + i) : Elem<T>::unpack_pair(w + i), c2, minus_m);
       float t0, t1;
       unpair(t, t0, t1);
       const uint64_t x = pair(exp2_fast(t0), exp2_fast(t1));
       S2 = add_pair(S2, x);
-      U2 = fma_pair(t, x, U2);
+      if (kWithU) U2 = fma_pair(t, x, U2);
     }
   }
   // the triple relative to m itself instead of the rounded M; of no account where exact_needed is set
@@ -259,6 +276,8 @@ struct RunningStat {
     return RowStat{m, S * sc, (U - d * S) * sc};
   }
 };
+using RunningStat = Running<true>;
+using RunningSum = Running<false>;
 // The exact form over the vectors first, first + stride, ... below n.
 template <typename T>
 __device__ __noinline__ RowStat exact_stat(const uint4* v, int first, int stride, int n, float c) {
