@@ -146,18 +146,22 @@ __device__ __forceinline__ float merged_probability(const int* ids, const float*
   }
   return seen ? -1.f : sum;
 }
-// m, the mass outside the entries and all of it from the slices' statistics; a bad row gives m = 0 and NaN masses
-__device__ __forceinline__ void row_statistics(const float (*slot)[4], int n_cta, float c, float& m, float& s, float& s_row) {
-  m = slot[0][0];
-  for (int r = 1; r < n_cta; ++r) m = max_nan(m, slot[r][0]);
+// m, the mass outside the entries and all of it from the parts of a row (a warp together); a bad row gives m = 0 and NaN
+// masses.  `entries_every`: each that many-th part is a slice's entries.
+__device__ __forceinline__ void row_statistics(const float2* part, int n, int entries_every, float c, float& m, float& s, float& s_row) {
+  const int lane = threadIdx.x & 31;
+  m = -CUDART_INF_F;
+  for (int i = lane; i < n; i += 32) m = max_nan(m, part[i].x);
+  m = key_value(__reduce_max_sync(0xffffffffu, order_key(m)));
   s = 0.f;
   float s_in = 0.f;
-  for (int r = 0; r < n_cta; ++r) {
-    if (slot[r][0] == -CUDART_INF_F) continue;
-    const float scale = exp2_fast((slot[r][0] - m) * c);
-    s += slot[r][1] * scale;
-    s_in += slot[r][2] * scale;
+  for (int i = lane; i < n; i += 32) {
+    const float2 q = part[i];
+    const float v = q.x == -CUDART_INF_F ? 0.f : q.y * exp2_fast((q.x - m) * c);
+    if (i % entries_every == entries_every - 1) s_in += v; else s += v;
   }
+  s = warp_sum(s);
+  s_in = warp_sum(s_in);
   if (bad_max(m)) { m = 0.f; s = CUDART_NAN_F; }
   s_row = s + s_in;
 }
@@ -186,7 +190,7 @@ __global__ void __launch_bounds__(kDsThreads)
 distill_small_kernel(const DistillParams p) {
   constexpr int kVec = Elem<T>::kVec;
   pdl_launch_dependents();
-  extern __shared__ __align__(16) uint8_t ds_raw[];
+  extern __shared__ __align__(128) uint8_t ds_raw[];
   __shared__ DsShared sh;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   pdl_wait();
@@ -306,28 +310,28 @@ distill_small_kernel(const DistillParams p) {
 
 // ------------------------------------------------------------------------------------------------ long rows, few rows
 constexpr int kEntryThreads = 128;             // warps 0..3 (prepare) and 4..7 (finish): one teacher entry a thread
-constexpr int kSumThreads = 512;               // warps 8..23: sums and gradients
+constexpr int kSumThreads = 256;               // warps 8..15 and 16..23: sums and gradients of every other row
+constexpr int kSumGroups = 2;
 constexpr int kSumWarps = kSumThreads / 32;
-constexpr int kPipeThreads = 2 * kEntryThreads + kSumThreads;
+constexpr int kPipeThreads = 2 * kEntryThreads + kSumGroups * kSumThreads;
 constexpr int kMaxBuffers = 3;
-constexpr int kSlots = 4;                      // rows under way between the roles of a block, and statistics between blocks
-constexpr int kLogitSlots = 8;                 // entries' logits on their way to the first block of a cluster
+constexpr int kSlots = 3;                      // rows under way between the roles of a block
+constexpr int kClusterSlots = 6;               // rows under way between the blocks of a cluster
+constexpr int kParts = kSumWarps + 1;          // parts of a slice's statistics: its sum warps', its entries'
 constexpr int kCopyBytes = 16 * 1024;          // piece of a slice that one bulk copy brings
 constexpr unsigned long long kDsWaitLimitNs = 2000000000ull;
 
 struct DsPipe {
-  alignas(8) unsigned long long full[kMaxBuffers], ready[kMaxBuffers], xchg[kSlots];
+  alignas(8) unsigned long long full[kMaxBuffers], ready[kMaxBuffers], xchg[kClusterSlots];
   alignas(16) int misc[8];                     // [1] gave up, [4..5] wait limit in ns (the layout mbar_wait expects)
-  float slot[kSlots][kMaxDsCluster][4];        // (m, S outside the entries, S of the entries) of every block's slice
-  float z[kLogitSlots][CWL_MAX_TOP_K];         // student logits of the entries (in the first block: of all slices)
+  float2 slot[kClusterSlots][kMaxDsCluster * kParts];   // (m, S) of every part of the row
+  float z[kClusterSlots][CWL_MAX_TOP_K];       // student logits of the entries (in the first block: of all slices)
   EntryRest entry[kSlots][CWL_MAX_TOP_K];      // from prepare to finish
-  float entry_stat[kSlots][2];                 // (m, S) of this slice's entries
   float mass[kSlots][2];                       // sum of the teacher's probabilities, and what they leave to the rest
   int id[CWL_MAX_TOP_K];
   float p[CWL_MAX_TOP_K];
   float red[kEntryThreads / 32], red2[kEntryThreads / 32];
   double red_d[kEntryThreads / 32], red_loss[kEntryThreads / 32];
-  float sum_m[kSumWarps], sum_s[kSumWarps];
   int repeated;                                // some id occurs twice
 };
 
@@ -336,12 +340,11 @@ struct PipePlan {
 };
 
 __device__ __forceinline__ void prepare_barrier() { __syncwarp(); asm volatile("bar.sync 1, 128;" ::: "memory"); }
-__device__ __forceinline__ void sum_barrier() { __syncwarp(); asm volatile("bar.sync 2, 512;" ::: "memory"); }
-__device__ __forceinline__ void finish_barrier() { __syncwarp(); asm volatile("bar.sync 3, 128;" ::: "memory"); }
+__device__ __forceinline__ void finish_barrier() { __syncwarp(); asm volatile("bar.sync 2, 128;" ::: "memory"); }
 // the gradients of row n's slice are stored: the sum warps say so and go on, the finish warps wait for it
-__device__ __forceinline__ void stored_arrive(int n) { __syncwarp(); asm volatile("bar.arrive %0, 640;" ::"r"(4 + n % kSlots) : "memory"); }
-__device__ __forceinline__ void stored_wait(int n) { __syncwarp(); asm volatile("bar.sync %0, 640;" ::"r"(4 + n % kSlots) : "memory"); }
-static_assert(kEntryThreads == 128 && kSumThreads == 512, "the barriers' counts");
+__device__ __forceinline__ void stored_arrive(int n) { __syncwarp(); asm volatile("bar.arrive %0, 384;" ::"r"(3 + n % kSlots) : "memory"); }
+__device__ __forceinline__ void stored_wait(int n) { __syncwarp(); asm volatile("bar.sync %0, 384;" ::"r"(3 + n % kSlots) : "memory"); }
+static_assert(kEntryThreads == 128 && kSumThreads == 256, "the barriers' counts");
 
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -384,13 +387,13 @@ struct RowCursor {
 // through buffer n % n_buffers:
 //   a finish thread  copies the slice in (full), as soon as row n - n_buffers has left the buffer
 //   prepare warps    entries of the teacher; once the slice is there, lift the entries out of it (ready)
-//   sum warps        sum what is left; their (m, S) with the entries' goes to every block of the cluster (xchg), and once
-//                    all have arrived the gradient of the slice is stored (stored)
+//   sum warps        two groups for every other row, so that one sums while the other waits or stores: sum what is left;
+//                    each warp's (m, S), and the entries', go to every block of the cluster (xchg), and once all have
+//                    arrived the gradient of the slice is stored (stored)
 //   finish warps     loss (in the first block of the cluster); gradient of the entries; the next copy
-// How far they drift apart: row k needs its copy, so finish is past row k - n_buffers wherever prepare or the sums are at
-// row k, and four slots and `stored` barriers serve a block.  A block's sums are at most one row ahead of another's, whose
-// finish is at most two rows behind its sums: four slots of statistics.  A block's prepare is at most three rows ahead of
-// another's sums, five ahead of its finish: eight slots of logits.
+// How far they drift apart: row k needs its copy, so its block's finish is past row k - n_buffers wherever prepare or the
+// sums are at row k: three slots and `stored` barriers serve a block.  Past row k - 3 also means that every block has sent
+// its statistics of row k - 3, so its finish is past row k - 6: six slots serve a cluster.
 // Every wait on a barrier in memory is bounded; one that runs out raises CWL_ERR_TIMEOUT, after which nothing is stored
 // any more, but the loops run to their end so that no other warp or block is left waiting.
 template <typename T>
@@ -410,7 +413,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
   auto xchg_bar = [&](int k) { return smem_u32(&sh.xchg[k]); };
   if (tid == 0) {
     for (int b = 0; b < kMaxBuffers; ++b) { mbar_init(full_bar(b), 1); mbar_init(ready_bar(b), 1); }
-    for (int k = 0; k < kSlots; ++k) mbar_init(xchg_bar(k), n_cta);
+    for (int k = 0; k < kClusterSlots; ++k) mbar_init(xchg_bar(k), n_cta * kParts);
     sh.misc[1] = 0;
     *reinterpret_cast<volatile unsigned long long*>(sh.misc + 4) = kDsWaitLimitNs;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -421,6 +424,17 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
 
   auto row_of = [&](int row) { return reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.ld; };
   auto lead_of = [&](const RowSlice& rs) { return (kVec - rs.own_head % kVec) % kVec; };
+  // one part of row n's statistics to every block of the cluster, from the first lanes of a warp
+  auto send_part = [&](int n, int part, float m, float s) {
+    if (lane < n_cta) {
+      const float2* slot = &sh.slot[n % kClusterSlots][cta * kParts + part];
+      const uint32_t to = log2_cta > 0 ? peer_shared(slot, lane) : smem_u32(slot);
+      st_peer_f32(to, m);
+      st_peer_f32(to + 4, s);
+      mbar_arrive_peer(log2_cta > 0 ? peer_shared(&sh.xchg[n % kClusterSlots], lane) : xchg_bar(n % kClusterSlots));
+    }
+    __syncwarp();
+  };
   // element i of the row sits at image[i - e0 + lead]; its vectors begin after own_head + lead elements
   auto image_of = [&](int n) { return reinterpret_cast<T*>(ds_raw + (n % plan.n_buffers) * plan.buffer_bytes); };
 
@@ -472,7 +486,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       if (mine) {
         sm[en.id] = Elem<T>::from_float(-CUDART_INF_F);
         if (p.loss != nullptr) {
-          float* slot = &sh.z[n % kLogitSlots][tid];
+          float* slot = &sh.z[n % kClusterSlots][tid];
           st_peer_f32(log2_cta > 0 ? peer_shared(slot, 0) : smem_u32(slot), en.z);
         }
       }
@@ -483,12 +497,11 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       if (tid < p.K) sh.entry[n % kSlots][tid] = EntryRest{en.lp, en.id, en.p, en.p_id, en.z};
       prepare_barrier();
       if (tid == 0) {
-        sh.entry_stat[n % kSlots][0] = me;
-        sh.entry_stat[n % kSlots][1] = (sh.red2[0] + sh.red2[1]) + (sh.red2[2] + sh.red2[3]);
         sh.mass[n % kSlots][0] = en.p_in;
         sh.mass[n % kSlots][1] = en.p_rest;
         mbar_arrive(ready_bar(n % plan.n_buffers));
       }
+      if (wid == 0) send_part(n, kSumWarps, me, (sh.red2[0] + sh.red2[1]) + (sh.red2[2] + sh.red2[3]));
       en = after;
     }
   } else if (wid < 2 * kEntryThreads / 32) {
@@ -522,15 +535,15 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
     for (int n = 0; at.next(w); ++n) {
       const int row = at.row;
       const float dl = p.dloss != nullptr ? __ldg(p.dloss + row) : 1.f;
-      const bool ok = mbar_wait_cluster(xchg_bar(n % kSlots), (uint32_t)(n / kSlots) & 1u, abort_flag);
+      const bool ok = mbar_wait_cluster(xchg_bar(n % kClusterSlots), (uint32_t)(n / kClusterSlots) & 1u, abort_flag);
       __syncwarp();
       float m, s, s_row;
-      row_statistics(sh.slot[n % kSlots], n_cta, p.c, m, s, s_row);
+      row_statistics(sh.slot[n % kClusterSlots], n_cta * kParts, kParts, p.c, m, s, s_row);
       EntryRest e{0.0, -1, 0.f, -1.f, 0.f};
       if (ft < p.K) e = sh.entry[n % kSlots][ft];
       const float p_in = sh.mass[n % kSlots][0], p_rest = sh.mass[n % kSlots][1];
       if (p.loss != nullptr && cta == 0) {
-        const double term = warp_sum(loss_term(p, e.id, e.p, e.lp, ft < p.K ? sh.z[n % kLogitSlots][ft] : 0.f, p_rest, m, s, s_row, ft));
+        const double term = warp_sum(loss_term(p, e.id, e.p, e.lp, ft < p.K ? sh.z[n % kClusterSlots][ft] : 0.f, p_rest, m, s, s_row, ft));
         if (lane == 0) sh.red_loss[fw] = term;
         finish_barrier();
         if (ft == 0 && ok) {
@@ -550,8 +563,9 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
     }
   } else {
     // -------------------------------------------------------------------------------------------------- sum warps
-    const int st = tid - 2 * kEntryThreads, sw = wid - 2 * kEntryThreads / 32;
-    int n = 0;
+    const int group = (tid - 2 * kEntryThreads) / kSumThreads;
+    const int st = (tid - 2 * kEntryThreads) % kSumThreads, sw = st >> 5;
+    int n = 0, skipped = 0;
     auto weight_of = [&](int row) { return p.weight != nullptr && row < p.T ? __ldg(p.weight + row) : 1.f; };
     float w = weight_of(first);
     for (int row = first; row < p.T; row += stride) {
@@ -561,9 +575,16 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
       const bool same_phase = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(d)) & 15u) == 0;
       if (w == 0.f) {                              // a row that is not trained on: not read
-        if (d != nullptr) zero_slice<T, kSumThreads>(st, d, same_phase, rs);
-        if (p.loss != nullptr && cta == 0 && st == 0) p.loss[row] = 0.f;
+        if (skipped++ % kSumGroups == group) {
+          if (d != nullptr) zero_slice<T, kSumThreads>(st, d, same_phase, rs);
+          if (p.loss != nullptr && cta == 0 && st == 0) p.loss[row] = 0.f;
+        }
         w = w_next;
+        continue;
+      }
+      if (n % kSumGroups != group) {
+        w = w_next;
+        ++n;
         continue;
       }
       const float up = w * p.temperature * (p.dloss != nullptr ? __ldg(p.dloss + row) : 1.f);
@@ -591,33 +612,12 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       if (st < rs.own_head) absorb_scalar(a, Elem<T>::to_float(sm[st]), p.c);
       if (st < rs.own_tail) absorb_scalar(a, Elem<T>::to_float(sm[rs.tail_start + st]), p.c);
       rescale(a, key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), p.c);
-      a.S = warp_sum(a.S);
-      if (lane == 0) { sh.sum_m[sw] = a.m; sh.sum_s[sw] = a.S; }
-      sum_barrier();
-      if (sw == 0) {
-        // the warps' parts and the entries'; lane r sends the result to block r
-        a = RowStat{sh.sum_m[lane & (kSumWarps - 1)], sh.sum_s[lane & (kSumWarps - 1)], 0.f};
-        const float me = sh.entry_stat[n % kSlots][0];
-        const float m_all = max_nan(key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), me);
-        rescale(a, m_all, p.c);
-        for (int off = kSumWarps / 2; off > 0; off >>= 1) a.S += __shfl_xor_sync(0xffffffffu, a.S, off);
-        RowStat e{me, sh.entry_stat[n % kSlots][1], 0.f};
-        rescale(e, m_all, p.c);
-        if (lane < n_cta) {
-          float* at = sh.slot[n % kSlots][cta];
-          const uint32_t to = log2_cta > 0 ? peer_shared(at, lane) : smem_u32(at);
-          st_peer_f32(to, m_all);
-          st_peer_f32(to + 4, a.S);
-          st_peer_f32(to + 8, e.S);
-          mbar_arrive_peer(log2_cta > 0 ? peer_shared(&sh.xchg[n % kSlots], lane) : xchg_bar(n % kSlots));
-        }
-        __syncwarp();
-      }
-      const bool ok = mbar_wait_cluster(xchg_bar(n % kSlots), (uint32_t)(n / kSlots) & 1u, abort_flag);
+      send_part(n, sw, a.m, warp_sum(a.S));
+      const bool ok = mbar_wait_cluster(xchg_bar(n % kClusterSlots), (uint32_t)(n / kClusterSlots) & 1u, abort_flag);
       __syncwarp();
       if (d != nullptr && ok && *abort_flag == 0) {
         float m, s, s_row;
-        row_statistics(sh.slot[n % kSlots], n_cta, p.c, m, s, s_row);
+        row_statistics(sh.slot[n % kClusterSlots], n_cta * kParts, kParts, p.c, m, s, s_row);
         const float rest = sh.mass[n % kSlots][1];
         const float k_out = outside_factor(sh.mass[n % kSlots][0] + rest, rest, s, s_row) * up;
         if (fabsf(m) <= kOrdinaryLogit && p.ordinary != 0) {
