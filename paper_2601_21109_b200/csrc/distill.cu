@@ -111,10 +111,13 @@ __device__ __forceinline__ void load_entry(const DistillParams& p, int row, int 
   en.id = -1; en.value = 0.f; en.p = 0.f; en.lp = 0.0; en.p_id = -1.f; en.z = 0.f; en.p_in = 0.f; en.p_rest = 0.f;
   if (j < p.K) {
     en.id = __ldg(p.ids + (int64_t)row * p.ld_teacher + j);
-    const float v = __ldg(p.values + (int64_t)row * p.ld_teacher + j);
-    if (en.id >= p.V) { flag_status(p.status_word, CWL_ERR_INVALID_ARG); en.id = -1; }
-    if (en.id >= 0) en.value = v;
+    en.value = __ldg(p.values + (int64_t)row * p.ld_teacher + j);
   }
+}
+// apart from the loads, so that they can be under way while another row is worked on
+__device__ __forceinline__ void check_entry(const DistillParams& p, Entry& en) {
+  if (en.id >= p.V) { flag_status(p.status_word, CWL_ERR_INVALID_ARG); en.id = -1; }
+  if (en.id < 0) { en.id = -1; en.value = 0.f; }
 }
 // the entry's weight before normalisation (also left in en.p); v_max: the largest value of the row, for CWL_TEACHER_LOGITS
 __device__ __forceinline__ double entry_weight(const DistillParams& p, float v_max, Entry& en) {
@@ -218,6 +221,7 @@ distill_small_kernel(const DistillParams p) {
     // teacher entries, one a thread, while the row is on its way
     Entry en;
     load_entry(p, row, tid, en);
+    check_entry(p, en);
     if (tid < p.K) sh.id[tid] = en.id;
     float v_max = 0.f;
     if (p.mode == CWL_TEACHER_LOGITS) {
@@ -332,6 +336,7 @@ struct DsPipe {
   float p[CWL_MAX_TOP_K];
   float red[kEntryThreads / 32], red2[kEntryThreads / 32];
   double red_d[kEntryThreads / 32], red_loss[kEntryThreads / 32];
+  int red_n[kEntryThreads / 32];
   int repeated;                                // some id occurs twice
 };
 
@@ -349,14 +354,36 @@ static_assert(kEntryThreads == 128 && kSumThreads == 256, "the barriers' counts"
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void mbar_arrive_peer(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+// Stores to the shared memory of a block of the cluster that count their bytes on an mbarrier there: no fence, and so no
+// wait for the gradients that the same thread has stored before.
+__device__ __forceinline__ void st_async_f32(uint32_t cluster_addr, float v, uint32_t cluster_bar) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];"
+               ::"r"(cluster_addr), "r"(__float_as_uint(v)), "r"(cluster_bar) : "memory");
 }
-// the bounded wait of mbar_wait, ordered with the arrivals of the whole cluster
+__device__ __forceinline__ void st_async_2f32(uint32_t cluster_addr, float a, float b, uint32_t cluster_bar) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];"
+               ::"r"(cluster_addr), "r"(__float_as_uint(a)), "r"(__float_as_uint(b)), "r"(cluster_bar) : "memory");
+}
+// The bounded wait of mbar_wait, ordered after what the whole cluster did before its arrivals.
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  if (!mbar_wait(bar, parity, abort_flag)) return false;
-  asm volatile("fence.acq_rel.cluster;" ::: "memory");
-  return true;
+  if (mbar_try_wait_cluster(bar, parity)) return true;
+  const unsigned long long t0 = global_timer();
+  for (uint32_t spins = 1;; ++spins) {
+    if (mbar_try_wait_cluster(bar, parity)) return true;
+    if ((spins & 255u) == 0) {
+      if (*abort_flag) return false;
+      if (global_timer() - t0 > wait_limit(abort_flag)) { *abort_flag = 1; return false; }
+    }
+  }
 }
 __device__ __forceinline__ void bulk_copy_in(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -413,7 +440,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
   auto xchg_bar = [&](int k) { return smem_u32(&sh.xchg[k]); };
   if (tid == 0) {
     for (int b = 0; b < kMaxBuffers; ++b) { mbar_init(full_bar(b), 1); mbar_init(ready_bar(b), 1); }
-    for (int k = 0; k < kClusterSlots; ++k) mbar_init(xchg_bar(k), n_cta * kParts);
+    for (int k = 0; k < kClusterSlots; ++k) mbar_init(xchg_bar(k), 1);
     sh.misc[1] = 0;
     *reinterpret_cast<volatile unsigned long long*>(sh.misc + 4) = kDsWaitLimitNs;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -424,15 +451,12 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
 
   auto row_of = [&](int row) { return reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.ld; };
   auto lead_of = [&](const RowSlice& rs) { return (kVec - rs.own_head % kVec) % kVec; };
+  auto cluster_addr = [&](const void* ptr, uint32_t block) { return log2_cta > 0 ? peer_shared(ptr, block) : smem_u32(ptr); };
   // one part of row n's statistics to every block of the cluster, from the first lanes of a warp
   auto send_part = [&](int n, int part, float m, float s) {
-    if (lane < n_cta) {
-      const float2* slot = &sh.slot[n % kClusterSlots][cta * kParts + part];
-      const uint32_t to = log2_cta > 0 ? peer_shared(slot, lane) : smem_u32(slot);
-      st_peer_f32(to, m);
-      st_peer_f32(to + 4, s);
-      mbar_arrive_peer(log2_cta > 0 ? peer_shared(&sh.xchg[n % kClusterSlots], lane) : xchg_bar(n % kClusterSlots));
-    }
+    if (lane < n_cta)
+      st_async_2f32(cluster_addr(&sh.slot[n % kClusterSlots][cta * kParts + part], lane), m, s,
+                    cluster_addr(&sh.xchg[n % kClusterSlots], lane));
     __syncwarp();
   };
   // element i of the row sits at image[i - e0 + lead]; its vectors begin after own_head + lead elements
@@ -451,6 +475,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       more = at.next(w_after);
       Entry after;
       if (more) load_entry(p, at.row, tid, after);       // a row ahead
+      check_entry(p, en);
       const T* z = row_of(row);
       const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
       T* sm = image_of(n) + lead_of(rs) - rs.e0;         // element i of the row at sm[i]
@@ -462,8 +487,10 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
         v_max = max_nan(max_nan(sh.red[0], sh.red[1]), max_nan(sh.red[2], sh.red[3]));
       }
       const double part = warp_sum(entry_weight(p, v_max, en));
-      if (lane == 0) sh.red_d[wid] = part;
+      const int valid = __popc(__ballot_sync(0xffffffffu, en.id >= 0));
+      if (lane == 0) { sh.red_d[wid] = part; sh.red_n[wid] = valid; }
       prepare_barrier();
+      const int n_valid = (sh.red_n[0] + sh.red_n[1]) + (sh.red_n[2] + sh.red_n[3]);
       finish_entry(p, v_max, (sh.red_d[0] + sh.red_d[1]) + (sh.red_d[2] + sh.red_d[3]), en);
       if (tid < p.K) { sh.id[tid] = en.id; sh.p[tid] = en.p; }
       if (tid == 0) sh.repeated = 0;
@@ -485,10 +512,8 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       if (sh.repeated && mine) en.p_id = merged_probability(sh.id, sh.p, p.K, tid);
       if (mine) {
         sm[en.id] = Elem<T>::from_float(-CUDART_INF_F);
-        if (p.loss != nullptr) {
-          float* slot = &sh.z[n % kClusterSlots][tid];
-          st_peer_f32(log2_cta > 0 ? peer_shared(slot, 0) : smem_u32(slot), en.z);
-        }
+        if (p.loss != nullptr)
+          st_async_f32(cluster_addr(&sh.z[n % kClusterSlots][tid], 0), en.z, cluster_addr(&sh.xchg[n % kClusterSlots], 0));
       }
       // (m, S) of this slice's entries, every distinct id once
       const float me = max_nan(max_nan(sh.red[0], sh.red[1]), max_nan(sh.red[2], sh.red[3]));
@@ -499,6 +524,9 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       if (tid == 0) {
         sh.mass[n % kSlots][0] = en.p_in;
         sh.mass[n % kSlots][1] = en.p_rest;
+        // what will arrive for this row: every part of its statistics and, in the first block, every entry's logit
+        mbar_expect_tx(xchg_bar(n % kClusterSlots),
+                       (uint32_t)(n_cta * kParts * sizeof(float2)) + (p.loss != nullptr && cta == 0 ? (uint32_t)n_valid * 4u : 0u));
         mbar_arrive(ready_bar(n % plan.n_buffers));
       }
       if (wid == 0) send_part(n, kSumWarps, me, (sh.red2[0] + sh.red2[1]) + (sh.red2[2] + sh.red2[3]));
