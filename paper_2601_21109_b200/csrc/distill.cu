@@ -317,7 +317,7 @@ constexpr int kEntryThreads = 128;             // warps 0..3 (prepare) and 4..7 
 constexpr int kSumThreads = 256;               // warps 8..15 and 16..23: sums and gradients of every other row
 constexpr int kSumGroups = 2;
 constexpr int kSumWarps = kSumThreads / 32;
-constexpr int kPipeThreads = 2 * kEntryThreads + kSumGroups * kSumThreads;
+constexpr int kPipeThreads = 2 * kEntryThreads + kSumGroups * kSumThreads + 32;   // the last warp copies slices in
 constexpr int kMaxBuffers = 3;
 constexpr int kSlots = 3;                      // rows under way between the roles of a block
 constexpr int kClusterSlots = 6;               // rows under way between the blocks of a cluster
@@ -347,8 +347,8 @@ struct PipePlan {
 __device__ __forceinline__ void prepare_barrier() { __syncwarp(); asm volatile("bar.sync 1, 128;" ::: "memory"); }
 __device__ __forceinline__ void finish_barrier() { __syncwarp(); asm volatile("bar.sync 2, 128;" ::: "memory"); }
 // the gradients of row n's slice are stored: the sum warps say so and go on, the finish warps wait for it
-__device__ __forceinline__ void stored_arrive(int n) { __syncwarp(); asm volatile("bar.arrive %0, 384;" ::"r"(3 + n % kSlots) : "memory"); }
-__device__ __forceinline__ void stored_wait(int n) { __syncwarp(); asm volatile("bar.sync %0, 384;" ::"r"(3 + n % kSlots) : "memory"); }
+__device__ __forceinline__ void stored_arrive(int n) { __syncwarp(); asm volatile("bar.arrive %0, 416;" ::"r"(3 + n % kSlots) : "memory"); }
+__device__ __forceinline__ void stored_wait(int n) { __syncwarp(); asm volatile("bar.sync %0, 416;" ::"r"(3 + n % kSlots) : "memory"); }
 static_assert(kEntryThreads == 128 && kSumThreads == 256, "the barriers' counts");
 
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
@@ -412,12 +412,12 @@ struct RowCursor {
 
 // One block: rows first, first + stride, ...; rows of weight 0 take no part in the numbering below.  Row number n goes
 // through buffer n % n_buffers:
-//   a finish thread  copies the slice in (full), as soon as row n - n_buffers has left the buffer
+//   copy warp        brings the slice in (full), as soon as row n - n_buffers has left the buffer
 //   prepare warps    entries of the teacher; once the slice is there, lift the entries out of it (ready)
 //   sum warps        two groups for every other row, so that one sums while the other waits or stores: sum what is left;
 //                    each warp's (m, S), and the entries', go to every block of the cluster (xchg), and once all have
 //                    arrived the gradient of the slice is stored (stored)
-//   finish warps     loss (in the first block of the cluster); gradient of the entries; the next copy
+//   finish warps     loss (in the first block of the cluster); gradient of the entries
 // How far they drift apart: row k needs its copy, so its block's finish is past row k - n_buffers wherever prepare or the
 // sums are at row k: three slots and `stored` barriers serve a block.  Past row k - 3 also means that every block has sent
 // its statistics of row k - 3, so its finish is past row k - 6: six slots serve a cluster.
@@ -535,28 +535,6 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
   } else if (wid < 2 * kEntryThreads / 32) {
     // ----------------------------------------------------------------------------------------------- finish warps
     const int ft = tid - kEntryThreads, fw = wid - kEntryThreads / 32;
-    RowCursor loads;                                     // of thread 0: the slices to copy
-    int loaded = 0;
-    bool more_loads = true;
-    auto copy_next = [&]() {
-      float w;
-      more_loads = more_loads && loads.next(w);
-      if (!more_loads) return;
-      const T* z = row_of(loads.row);
-      const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
-      const int b = loaded % plan.n_buffers;
-      const uint32_t bytes = (uint32_t)(rs.v1 - rs.v0) * 16u;
-      const uint8_t* src = reinterpret_cast<const uint8_t*>(z + rs.head) + (int64_t)rs.v0 * 16;
-      const uint32_t dst = smem_u32(image_of(loaded) + rs.own_head + lead_of(rs));
-      mbar_expect_tx(full_bar(b), bytes);                // an arrival that expects no bytes completes at once
-      for (uint32_t off = 0; off < bytes; off += kCopyBytes)
-        bulk_copy_in(dst + off, src + off, min(bytes - off, (uint32_t)kCopyBytes), full_bar(b));
-      ++loaded;
-    };
-    if (ft == 0) {
-      loads.start(p.weight, p.T, first, stride);
-      for (int b = 0; b < plan.n_buffers; ++b) copy_next();
-    }
     RowCursor at;
     at.start(p.weight, p.T, first, stride);
     float w;
@@ -580,15 +558,35 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
         }
       }
       stored_wait(n);
-      if (ft == 0) {
-        asm volatile("fence.proxy.async;" ::: "memory"); // the buffer was read and written with ordinary accesses
-        copy_next();
-      }
       if (p.dlogits != nullptr && e.p_id >= 0.f && ok && *abort_flag == 0) {
         T* d = reinterpret_cast<T*>(p.dlogits) + (int64_t)row * p.ld_d;
         d[e.id] = Elem<T>::from_float(entry_gradient(p, e.z, e.p_id, p_in + p_rest, m, s_row) * (w * p.temperature * dl));
       }
     }
+  } else if (wid == kPipeThreads / 32 - 1) {
+    // -------------------------------------------------------------------------------------------------- copy warp
+    RowCursor loads;
+    loads.start(p.weight, p.T, first, stride);
+    int loaded = 0;
+    float w;
+    while (loads.next(w)) {
+      if (loaded >= plan.n_buffers) stored_wait(loaded - plan.n_buffers);
+      if (lane == 0) {
+        asm volatile("fence.proxy.async;" ::: "memory");   // the buffer was read and written with ordinary accesses
+        const T* z = row_of(loads.row);
+        const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
+        const int b = loaded % plan.n_buffers;
+        const uint32_t bytes = (uint32_t)(rs.v1 - rs.v0) * 16u;
+        const uint8_t* src = reinterpret_cast<const uint8_t*>(z + rs.head) + (int64_t)rs.v0 * 16;
+        const uint32_t dst = smem_u32(image_of(loaded) + rs.own_head + lead_of(rs));
+        mbar_expect_tx(full_bar(b), bytes);                // an arrival that expects no bytes completes at once
+        for (uint32_t off = 0; off < bytes; off += kCopyBytes)
+          bulk_copy_in(dst + off, src + off, min(bytes - off, (uint32_t)kCopyBytes), full_bar(b));
+      }
+      __syncwarp();
+      ++loaded;
+    }
+    for (int n = max(0, loaded - plan.n_buffers); n < loaded; ++n) stored_wait(n);   // the barriers count this warp for every row
   } else {
     // -------------------------------------------------------------------------------------------------- sum warps
     const int group = (tid - 2 * kEntryThreads) / kSumThreads;
