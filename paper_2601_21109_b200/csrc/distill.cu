@@ -347,8 +347,8 @@ struct PipePlan {
 __device__ __forceinline__ void prepare_barrier() { __syncwarp(); asm volatile("bar.sync 1, 128;" ::: "memory"); }
 __device__ __forceinline__ void finish_barrier() { __syncwarp(); asm volatile("bar.sync 2, 128;" ::: "memory"); }
 // the gradients of row n's slice are stored: the sum warps say so and go on, the finish warps wait for it
-__device__ __forceinline__ void stored_arrive(int n) { __syncwarp(); asm volatile("bar.arrive %0, 416;" ::"r"(3 + n % kSlots) : "memory"); }
-__device__ __forceinline__ void stored_wait(int n) { __syncwarp(); asm volatile("bar.sync %0, 416;" ::"r"(3 + n % kSlots) : "memory"); }
+__device__ __forceinline__ void stored_arrive(int slot) { __syncwarp(); asm volatile("bar.arrive %0, 416;" ::"r"(3 + slot) : "memory"); }
+__device__ __forceinline__ void stored_wait(int slot) { __syncwarp(); asm volatile("bar.sync %0, 416;" ::"r"(3 + slot) : "memory"); }
 static_assert(kEntryThreads == 128 && kSumThreads == 256, "the barriers' counts");
 
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
@@ -390,23 +390,44 @@ __device__ __forceinline__ void bulk_copy_in(uint32_t dst, const void* src, uint
                ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// The rows first, first + stride, ... that are trained on; the next one's weight is fetched a row ahead.
+// The rows first, first + stride, ... in groups of 32, a row a lane of the warp: their weights come with one load a group,
+// a group ahead, and rows of weight 0 cost nothing.
 struct RowCursor {
   const float* weight;
-  int T, stride, row;
-  float ahead;
-  __device__ __forceinline__ float weight_of(int r) const { return weight != nullptr && r < T ? __ldg(weight + r) : 1.f; }
+  int T, stride, base, row;      // first row of the group; the row at hand
+  unsigned live;                 // rows of the group that are still to come
+  float mine, ahead;             // this lane's weight in the group, in the next one
+  __device__ __forceinline__ float weight_of(int64_t r) const { return r < T ? (weight != nullptr ? __ldg(weight + r) : 1.f) : 0.f; }
+  __device__ __forceinline__ void enter(int64_t first) {
+    base = (int)min(first, (int64_t)T);
+    mine = ahead;
+    ahead = weight_of(first + (int64_t)(32 + (threadIdx.x & 31)) * stride);
+    live = __ballot_sync(0xffffffffu, mine != 0.f);           // a NaN is trained on, and 0 past the end
+  }
   __device__ __forceinline__ void start(const float* w, int rows, int first, int step) {
-    weight = w; T = rows; stride = step; row = first - step;
-    ahead = weight_of(first);
+    weight = w; T = rows; stride = step; row = first;
+    ahead = weight_of(first + (int64_t)(threadIdx.x & 31) * stride);
+    enter(first);
   }
   __device__ __forceinline__ bool next(float& w) {
-    do {
-      row += stride;
-      w = ahead;
-      ahead = weight_of(row + stride);
-    } while (row < T && w == 0.f);
-    return row < T;
+    while (live == 0) {
+      const int64_t after = (int64_t)base + 32ll * stride;
+      if (after >= T) return false;
+      enter(after);
+    }
+    const int k = __ffs((int)live) - 1;
+    live &= live - 1;
+    row = base + k * stride;
+    w = __shfl_sync(0xffffffffu, mine, k);
+    return true;
+  }
+};
+// position in a ring of `size` places, and how often it went round (mod 2)
+struct Ring {
+  int at = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void step(int size) {
+    if (++at == size) { at = 0; phase ^= 1u; }
   }
 };
 
@@ -452,15 +473,15 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
   auto row_of = [&](int row) { return reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.ld; };
   auto lead_of = [&](const RowSlice& rs) { return (kVec - rs.own_head % kVec) % kVec; };
   auto cluster_addr = [&](const void* ptr, uint32_t block) { return log2_cta > 0 ? peer_shared(ptr, block) : smem_u32(ptr); };
-  // one part of row n's statistics to every block of the cluster, from the first lanes of a warp
-  auto send_part = [&](int n, int part, float m, float s) {
+  // one part of a row's statistics to every block of the cluster, from the first lanes of a warp
+  auto send_part = [&](int slot, int part, float m, float s) {
     if (lane < n_cta)
-      st_async_2f32(cluster_addr(&sh.slot[n % kClusterSlots][cta * kParts + part], lane), m, s,
-                    cluster_addr(&sh.xchg[n % kClusterSlots], lane));
+      st_async_2f32(cluster_addr(&sh.slot[slot][cta * kParts + part], lane), m, s,
+                    cluster_addr(&sh.xchg[slot], lane));
     __syncwarp();
   };
   // element i of the row sits at image[i - e0 + lead]; its vectors begin after own_head + lead elements
-  auto image_of = [&](int n) { return reinterpret_cast<T*>(ds_raw + (n % plan.n_buffers) * plan.buffer_bytes); };
+  auto image_of = [&](int buffer) { return reinterpret_cast<T*>(ds_raw + buffer * plan.buffer_bytes); };
 
   if (wid < kEntryThreads / 32) {
     // ---------------------------------------------------------------------------------------------- prepare warps
@@ -470,7 +491,8 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
     bool more = at.next(w);
     Entry en;
     if (more) load_entry(p, at.row, tid, en);
-    for (int n = 0; more; ++n) {
+    Ring buf, slot, cslot;
+    for (; more; buf.step(plan.n_buffers), slot.step(kSlots), cslot.step(kClusterSlots)) {
       const int row = at.row;
       more = at.next(w_after);
       Entry after;
@@ -478,7 +500,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       check_entry(p, en);
       const T* z = row_of(row);
       const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
-      T* sm = image_of(n) + lead_of(rs) - rs.e0;         // element i of the row at sm[i]
+      T* sm = image_of(buf.at) + lead_of(rs) - rs.e0;         // element i of the row at sm[i]
       float v_max = 0.f;
       if (p.mode == CWL_TEACHER_LOGITS) {
         const float mx = warp_max_nan(en.id >= 0 ? en.value : -CUDART_INF_F);
@@ -495,7 +517,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       if (tid < p.K) { sh.id[tid] = en.id; sh.p[tid] = en.p; }
       if (tid == 0) sh.repeated = 0;
       const bool mine = en.id >= rs.e0 && en.id < rs.e1;
-      mbar_wait(full_bar(n % plan.n_buffers), (uint32_t)(n / plan.n_buffers) & 1u, abort_flag);
+      mbar_wait(full_bar(buf.at), buf.phase, abort_flag);
       __syncwarp();
       if (tid < rs.own_head) sm[tid] = z[tid];
       if (tid < rs.own_tail) sm[rs.tail_start + tid] = z[rs.tail_start + tid];
@@ -513,23 +535,23 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       if (mine) {
         sm[en.id] = Elem<T>::from_float(-CUDART_INF_F);
         if (p.loss != nullptr)
-          st_async_f32(cluster_addr(&sh.z[n % kClusterSlots][tid], 0), en.z, cluster_addr(&sh.xchg[n % kClusterSlots], 0));
+          st_async_f32(cluster_addr(&sh.z[cslot.at][tid], 0), en.z, cluster_addr(&sh.xchg[cslot.at], 0));
       }
       // (m, S) of this slice's entries, every distinct id once
       const float me = max_nan(max_nan(sh.red[0], sh.red[1]), max_nan(sh.red[2], sh.red[3]));
       const float sw = warp_sum(en.p_id >= 0.f && !bad_max(me) ? exp2_fast((en.z - me) * p.c) : 0.f);
       if (lane == 0) sh.red2[wid] = sw;
-      if (tid < p.K) sh.entry[n % kSlots][tid] = EntryRest{en.lp, en.id, en.p, en.p_id, en.z};
+      if (tid < p.K) sh.entry[slot.at][tid] = EntryRest{en.lp, en.id, en.p, en.p_id, en.z};
       prepare_barrier();
       if (tid == 0) {
-        sh.mass[n % kSlots][0] = en.p_in;
-        sh.mass[n % kSlots][1] = en.p_rest;
+        sh.mass[slot.at][0] = en.p_in;
+        sh.mass[slot.at][1] = en.p_rest;
         // what will arrive for this row: every part of its statistics and, in the first block, every entry's logit
-        mbar_expect_tx(xchg_bar(n % kClusterSlots),
+        mbar_expect_tx(xchg_bar(cslot.at),
                        (uint32_t)(n_cta * kParts * sizeof(float2)) + (p.loss != nullptr && cta == 0 ? (uint32_t)n_valid * 4u : 0u));
-        mbar_arrive(ready_bar(n % plan.n_buffers));
+        mbar_arrive(ready_bar(buf.at));
       }
-      if (wid == 0) send_part(n, kSumWarps, me, (sh.red2[0] + sh.red2[1]) + (sh.red2[2] + sh.red2[3]));
+      if (wid == 0) send_part(cslot.at, kSumWarps, me, (sh.red2[0] + sh.red2[1]) + (sh.red2[2] + sh.red2[3]));
       en = after;
     }
   } else if (wid < 2 * kEntryThreads / 32) {
@@ -538,18 +560,19 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
     RowCursor at;
     at.start(p.weight, p.T, first, stride);
     float w;
-    for (int n = 0; at.next(w); ++n) {
+    Ring slot, cslot;
+    for (; at.next(w); slot.step(kSlots), cslot.step(kClusterSlots)) {
       const int row = at.row;
       const float dl = p.dloss != nullptr ? __ldg(p.dloss + row) : 1.f;
-      const bool ok = mbar_wait_cluster(xchg_bar(n % kClusterSlots), (uint32_t)(n / kClusterSlots) & 1u, abort_flag);
+      const bool ok = mbar_wait_cluster(xchg_bar(cslot.at), cslot.phase, abort_flag);
       __syncwarp();
       float m, s, s_row;
-      row_statistics(sh.slot[n % kClusterSlots], n_cta * kParts, kParts, p.c, m, s, s_row);
+      row_statistics(sh.slot[cslot.at], n_cta * kParts, kParts, p.c, m, s, s_row);
       EntryRest e{0.0, -1, 0.f, -1.f, 0.f};
-      if (ft < p.K) e = sh.entry[n % kSlots][ft];
-      const float p_in = sh.mass[n % kSlots][0], p_rest = sh.mass[n % kSlots][1];
+      if (ft < p.K) e = sh.entry[slot.at][ft];
+      const float p_in = sh.mass[slot.at][0], p_rest = sh.mass[slot.at][1];
       if (p.loss != nullptr && cta == 0) {
-        const double term = warp_sum(loss_term(p, e.id, e.p, e.lp, ft < p.K ? sh.z[n % kClusterSlots][ft] : 0.f, p_rest, m, s, s_row, ft));
+        const double term = warp_sum(loss_term(p, e.id, e.p, e.lp, ft < p.K ? sh.z[cslot.at][ft] : 0.f, p_rest, m, s, s_row, ft));
         if (lane == 0) sh.red_loss[fw] = term;
         finish_barrier();
         if (ft == 0 && ok) {
@@ -557,7 +580,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
           p.loss[row] = (float)((double)w * p.temperature * p.temperature * kl);
         }
       }
-      stored_wait(n);
+      stored_wait(slot.at);
       if (p.dlogits != nullptr && e.p_id >= 0.f && ok && *abort_flag == 0) {
         T* d = reinterpret_cast<T*>(p.dlogits) + (int64_t)row * p.ld_d;
         d[e.id] = Elem<T>::from_float(entry_gradient(p, e.z, e.p_id, p_in + p_rest, m, s_row) * (w * p.temperature * dl));
@@ -568,56 +591,66 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
     RowCursor loads;
     loads.start(p.weight, p.T, first, stride);
     int loaded = 0;
+    Ring buf, past;                                          // `past`: slot of the row whose buffer comes free next
     float w;
     while (loads.next(w)) {
-      if (loaded >= plan.n_buffers) stored_wait(loaded - plan.n_buffers);
+      if (loaded >= plan.n_buffers) { stored_wait(past.at); past.step(kSlots); }
       if (lane == 0) {
         asm volatile("fence.proxy.async;" ::: "memory");   // the buffer was read and written with ordinary accesses
         const T* z = row_of(loads.row);
         const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
-        const int b = loaded % plan.n_buffers;
         const uint32_t bytes = (uint32_t)(rs.v1 - rs.v0) * 16u;
         const uint8_t* src = reinterpret_cast<const uint8_t*>(z + rs.head) + (int64_t)rs.v0 * 16;
-        const uint32_t dst = smem_u32(image_of(loaded) + rs.own_head + lead_of(rs));
-        mbar_expect_tx(full_bar(b), bytes);                // an arrival that expects no bytes completes at once
+        const uint32_t dst = smem_u32(image_of(buf.at) + rs.own_head + lead_of(rs));
+        mbar_expect_tx(full_bar(buf.at), bytes);                // an arrival that expects no bytes completes at once
         for (uint32_t off = 0; off < bytes; off += kCopyBytes)
-          bulk_copy_in(dst + off, src + off, min(bytes - off, (uint32_t)kCopyBytes), full_bar(b));
+          bulk_copy_in(dst + off, src + off, min(bytes - off, (uint32_t)kCopyBytes), full_bar(buf.at));
       }
       __syncwarp();
+      buf.step(plan.n_buffers);
       ++loaded;
     }
-    for (int n = max(0, loaded - plan.n_buffers); n < loaded; ++n) stored_wait(n);   // the barriers count this warp for every row
+    for (int n = min(loaded, plan.n_buffers); n > 0; --n) { stored_wait(past.at); past.step(kSlots); }   // every row counts this warp
   } else {
     // -------------------------------------------------------------------------------------------------- sum warps
     const int group = (tid - 2 * kEntryThreads) / kSumThreads;
     const int st = (tid - 2 * kEntryThreads) % kSumThreads, sw = st >> 5;
-    int n = 0, skipped = 0;
-    auto weight_of = [&](int row) { return p.weight != nullptr && row < p.T ? __ldg(p.weight + row) : 1.f; };
-    float w = weight_of(first);
-    for (int row = first; row < p.T; row += stride) {
-      const float w_next = weight_of(row + stride);
+    // rows of weight 0 are not read; their zeros go out first, while the first slices come in
+    if (p.weight != nullptr) {
+      int turn = 0;
+      for (int64_t row0 = first; row0 < p.T; row0 += 32ll * stride) {
+        const int64_t mine = row0 + (int64_t)lane * stride;
+        unsigned dead = __ballot_sync(0xffffffffu, mine < p.T && __ldg(p.weight + min(mine, (int64_t)p.T - 1)) == 0.f);
+        for (; dead != 0; dead &= dead - 1) {
+          if ((turn++ & (kSumGroups - 1)) != group) continue;
+          const int64_t row = row0 + (int64_t)(__ffs((int)dead) - 1) * stride;
+          if (p.dlogits != nullptr) {
+            const T* z = row_of((int)row);
+            T* d = reinterpret_cast<T*>(p.dlogits) + row * p.ld_d;
+            zero_slice<T, kSumThreads>(st, d, ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(d)) & 15u) == 0,
+                                       row_slice<T>(z, p.V, cta, log2_cta));
+          }
+          if (p.loss != nullptr && cta == 0 && st == 0) p.loss[row] = 0.f;
+        }
+      }
+    }
+    RowCursor at;
+    at.start(p.weight, p.T, first, stride);
+    Ring buf, slot, cslot;
+    float w;
+    int turn = 0;
+    for (; at.next(w); buf.step(plan.n_buffers), slot.step(kSlots), cslot.step(kClusterSlots)) {
+      if ((turn++ & (kSumGroups - 1)) != group) continue;
+      const int row = at.row;
       const T* z = row_of(row);
       T* d = p.dlogits != nullptr ? reinterpret_cast<T*>(p.dlogits) + (int64_t)row * p.ld_d : nullptr;
       const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
       const bool same_phase = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(d)) & 15u) == 0;
-      if (w == 0.f) {                              // a row that is not trained on: not read
-        if (skipped++ % kSumGroups == group) {
-          if (d != nullptr) zero_slice<T, kSumThreads>(st, d, same_phase, rs);
-          if (p.loss != nullptr && cta == 0 && st == 0) p.loss[row] = 0.f;
-        }
-        w = w_next;
-        continue;
-      }
-      if (n % kSumGroups != group) {
-        w = w_next;
-        ++n;
-        continue;
-      }
       const float up = w * p.temperature * (p.dloss != nullptr ? __ldg(p.dloss + row) : 1.f);
-      const T* sm = image_of(n) + lead_of(rs) - rs.e0;
-      const uint4* sv = reinterpret_cast<const uint4*>(image_of(n) + rs.own_head + lead_of(rs));
+      const T* sm = image_of(buf.at) + lead_of(rs) - rs.e0;
+      const uint4* sv = reinterpret_cast<const uint4*>(image_of(buf.at) + rs.own_head + lead_of(rs));
       const int nv = rs.v1 - rs.v0;
-      mbar_wait(ready_bar(n % plan.n_buffers), (uint32_t)(n / plan.n_buffers) & 1u, abort_flag);
+      mbar_wait(ready_bar(buf.at), buf.phase, abort_flag);
       __syncwarp();
 
       RunningSum run;
@@ -638,14 +671,14 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       if (st < rs.own_head) absorb_scalar(a, Elem<T>::to_float(sm[st]), p.c);
       if (st < rs.own_tail) absorb_scalar(a, Elem<T>::to_float(sm[rs.tail_start + st]), p.c);
       rescale(a, key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), p.c);
-      send_part(n, sw, a.m, warp_sum(a.S));
-      const bool ok = mbar_wait_cluster(xchg_bar(n % kClusterSlots), (uint32_t)(n / kClusterSlots) & 1u, abort_flag);
+      send_part(cslot.at, sw, a.m, warp_sum(a.S));
+      const bool ok = mbar_wait_cluster(xchg_bar(cslot.at), cslot.phase, abort_flag);
       __syncwarp();
       if (d != nullptr && ok && *abort_flag == 0) {
         float m, s, s_row;
-        row_statistics(sh.slot[n % kClusterSlots], n_cta * kParts, kParts, p.c, m, s, s_row);
-        const float rest = sh.mass[n % kSlots][1];
-        const float k_out = outside_factor(sh.mass[n % kSlots][0] + rest, rest, s, s_row) * up;
+        row_statistics(sh.slot[cslot.at], n_cta * kParts, kParts, p.c, m, s, s_row);
+        const float rest = sh.mass[slot.at][1];
+        const float k_out = outside_factor(sh.mass[slot.at][0] + rest, rest, s, s_row) * up;
         if (fabsf(m) <= kOrdinaryLogit && p.ordinary != 0) {
           const float M = m * p.c;
           const float k = k_out * exp2_fast(-fmaf(m, p.c, -M));
@@ -671,9 +704,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
           }, [&](int x) { return exp2_fast((Elem<T>::to_float(sm[x]) - m) * p.c) * k_out; });
         }
       }
-      stored_arrive(n);
-      w = w_next;
-      ++n;
+      stored_arrive(slot.at);
     }
   }
   __syncthreads();
