@@ -322,6 +322,7 @@ constexpr int kMaxBuffers = 3;
 constexpr int kSlots = 3;                      // rows under way between the roles of a block
 constexpr int kClusterSlots = 6;               // rows under way between the blocks of a cluster
 constexpr int kParts = kSumWarps + 1;          // parts of a slice's statistics: its sum warps', its entries'
+constexpr int kAtOnce = 4;                       // vectors of a sum thread in the works at once
 constexpr int kCopyBytes = 16 * 1024;          // piece of a slice that one bulk copy brings
 constexpr unsigned long long kDsWaitLimitNs = 2000000000ull;
 
@@ -656,12 +657,16 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       RunningSum run;
       run.start(p.ordinary != 0);
       int i = st;
-      for (; i + kSumThreads < nv; i += 2 * kSumThreads) {
-        const uint4 q = sv[i], r = sv[i + kSumThreads];
-        const uint32_t words[8] = {q.x, q.y, q.z, q.w, r.x, r.y, r.z, r.w};
-        run.template take_words<T, 8>(words, Elem<T>::max_of(words), p.c);
+      for (; i + (kAtOnce - 1) * kSumThreads < nv; i += kAtOnce * kSumThreads) {
+        uint32_t words[4 * kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+          const uint4 q = sv[i + u * kSumThreads];
+          words[4 * u] = q.x; words[4 * u + 1] = q.y; words[4 * u + 2] = q.z; words[4 * u + 3] = q.w;
+        }
+        run.template take_words<T, 4 * kAtOnce>(words, Elem<T>::max_of(words), p.c);
       }
-      if (i < nv) {
+      for (; i < nv; i += kSumThreads) {
         const uint4 q = sv[i];
         const uint32_t words[4] = {q.x, q.y, q.z, q.w};
         run.template take_words<T, 4>(words, Elem<T>::max_of(words), p.c);
@@ -683,19 +688,49 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
           const float M = m * p.c;
           const float k = k_out * exp2_fast(-fmaf(m, p.c, -M));
           const uint64_t c2 = pair(p.c, p.c), minus_m = pair(-M, -M), k2 = pair(k, k), zero = pair(0.f, 0.f);
-          auto grad2 = [&](uint64_t zz) {
-            float t0, t1;
-            unpair(fma_pair(zz, c2, minus_m), t0, t1);
-            return fma_pair(pair(exp2_fast(t0), exp2_fast(t1)), k2, zero);
-          };
-          store_slice<T, kSumThreads>(st, d, same_phase, rs, [&](int v, float (&f)[kVec]) {
-            Elem<T>::unpack(sv[v - rs.v0], f);
+          auto grad_vec = [&](const uint4& q, float (&f)[kVec]) {
+            const uint32_t words[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-            for (int e = 0; e < kVec; e += 2) {
-              const uint64_t g = grad2(pair(f[e], f[e + 1]));
-              unpair(g, f[e], f[e + 1]);
+            for (int e = 0; e < kVec / 2; ++e) {
+              float t0, t1;
+              unpair(fma_pair(Elem<T>::unpack_pair(words + e * Elem<T>::kPairWords), c2, minus_m), t0, t1);
+              unpair(fma_pair(pair(exp2_fast(t0), exp2_fast(t1)), k2, zero), f[2 * e], f[2 * e + 1]);
             }
-          }, [&](int x) { return exp2_fast((Elem<T>::to_float(sm[x]) - m) * p.c) * k_out; });
+          };
+          if (same_phase) {
+            const uint4* in = sv + st;
+            uint4* out = reinterpret_cast<uint4*>(d + rs.head) + rs.v0 + st;
+            int left = nv - st;
+            for (; left > (kAtOnce - 1) * kSumThreads; left -= kAtOnce * kSumThreads, in += kAtOnce * kSumThreads, out += kAtOnce * kSumThreads) {
+              uint4 q[kAtOnce];
+#pragma unroll
+              for (int u = 0; u < kAtOnce; ++u) q[u] = in[u * kSumThreads];
+#pragma unroll
+              for (int u = 0; u < kAtOnce; ++u) {
+                float f[kVec];
+                grad_vec(q[u], f);
+                out[u * kSumThreads] = Elem<T>::pack(f);
+              }
+            }
+            for (; left > 0; left -= kSumThreads, in += kSumThreads, out += kSumThreads) {
+              float f[kVec];
+              grad_vec(*in, f);
+              *out = Elem<T>::pack(f);
+            }
+          } else {
+            for (int v = st; v < nv; v += kSumThreads) {
+              float f[kVec];
+              grad_vec(sv[v], f);
+              T* out = d + rs.head + (int64_t)(rs.v0 + v) * kVec;
+#pragma unroll
+              for (int e = 0; e < kVec; ++e) out[e] = Elem<T>::from_float(f[e]);
+            }
+          }
+          if (st < rs.own_head) d[st] = Elem<T>::from_float(exp2_fast((Elem<T>::to_float(sm[st]) - m) * p.c) * k_out);
+          if (st < rs.own_tail) {
+            const int x = rs.tail_start + st;
+            d[x] = Elem<T>::from_float(exp2_fast((Elem<T>::to_float(sm[x]) - m) * p.c) * k_out);
+          }
         } else {
           store_slice<T, kSumThreads>(st, d, same_phase, rs, [&](int v, float (&f)[kVec]) {
             Elem<T>::unpack(sv[v - rs.v0], f);
