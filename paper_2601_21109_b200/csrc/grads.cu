@@ -94,15 +94,33 @@ __device__ __forceinline__ uint32_t grad_peer(uint32_t addr, uint32_t cta) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
   return r;
 }
-__device__ __forceinline__ float4 ld_peer_v4(uint32_t addr) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void st_peer_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-__device__ __forceinline__ float ld_peer1(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-  return v;
+__device__ __forceinline__ void st_peer_b32(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ void store8(void* out, int64_t at, int f32, const float4& a, const float4& b) {
+  if (f32) {
+    float4* o = reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + at);
+    o[0] = a;
+    o[1] = b;
+  } else {
+    *reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(out) + at) =
+        make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
+  }
+}
+// eight columns of one row of the tile, where rows of the tile are rows of the output: gated H' or G, or dA
+template <int kPhase>
+__device__ __forceinline__ void store_row8(const GradParams& p, int side, int at, int col, const RowGate& g, const float4& a, const float4& b) {
+  if (kPhase == PHASE_SHRINK) {
+    if (at < p.T)
+      *reinterpret_cast<uint4*>(p.gated[side] + (int64_t)at * p.R + col) =
+          make_uint4(pack_bf16(a.x * gate_at(g, col + 0), a.y * gate_at(g, col + 1)), pack_bf16(a.z * gate_at(g, col + 2), a.w * gate_at(g, col + 3)),
+                     pack_bf16(b.x * gate_at(g, col + 4), b.y * gate_at(g, col + 5)), pack_bf16(b.z * gate_at(g, col + 6), b.w * gate_at(g, col + 7)));
+  } else if (at < p.d[0]) {
+    store8(p.out[0], (int64_t)at * p.ld[0] + col, p.out_f32, a, b);
+  }
 }
 
 template <int kPhase>
@@ -222,104 +240,127 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
       }
     }
   } else if (kPhase == PHASE_SHRINK) {
-    gates[tid - 64] = row_gate(m0 + tid - 64, p);        // while the main loop runs (a chain of dependent loads)
+    const int mine = (warp & 3) * 32 + lane;             // the row this thread drains
+    gates[mine] = row_gate(m0 + mine, p);                // while the main loop runs (a chain of dependent loads)
   }
 
-  // accumulator -> shared memory, [128][R + 4] fp32 over the ring, which is idle once every MMA has finished
-  const int pitch = p.R + 4;
-  float* dump = reinterpret_cast<float*>(base_ptr);
-  if (warp >= 2) {
-    const int quad = warp & 3, row = quad * 32 + lane;
-    const bool have = n_blk > 0 && mbar_wait(acc_bar, 0, abort_flag);
+  // Wait for the accumulator.  A CTA without K blocks (short loops on many CTAs) contributes zeros.
+  const int quad = warp & 3, row = quad * 32 + lane;     // of warps 2..5: the TMEM lanes a warp may read, one tile row a lane
+  const bool drain = warp >= 2;
+  if (drain && n_blk > 0) {
+    mbar_wait(acc_bar, 0, abort_flag);
     __syncwarp();
     tc_fence_after();
-    for (int c = 0; c < p.R; c += 32) {
-      uint32_t v[32];
-      if (n_blk > 0) {
-        tmem_ld32(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
-        tmem_ld_wait();
-      }
+  }
+  auto columns = [&](int c, uint32_t (&v)[32]) {         // 32 columns of this lane's row
+    if (n_blk > 0) {
+      tmem_ld32(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
+      tmem_ld_wait();
+    } else {
 #pragma unroll
-      for (int q = 0; q < 8; ++q)
-        if (c + q * 4 < p.R && (have || n_blk == 0))
-          *reinterpret_cast<float4*>(dump + row * pitch + c + q * 4) =
-              n_blk > 0 ? make_float4(__uint_as_float(v[q * 4]), __uint_as_float(v[q * 4 + 1]), __uint_as_float(v[q * 4 + 2]),
-                                      __uint_as_float(v[q * 4 + 3]))
-                        : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int j = 0; j < 32; ++j) v[j] = 0;
+    }
+  };
+  const bool by_rows = kPhase == PHASE_SHRINK || side == 0;      // rows of the tile are rows of the output (else its columns)
+  if (split == 1) {
+    // straight from the accumulator
+    if (drain && *abort_flag == 0) {
+      for (int c = 0; c < p.R; c += 32) {
+        uint32_t v[32];
+        columns(c, v);
+        if (by_rows) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (c + q * 8 < p.R)
+              store_row8<kPhase>(p, side, m0 + row, c + q * 8, kPhase == PHASE_SHRINK ? gates[row] : RowGate{},
+                                 make_float4(__uint_as_float(v[q * 8]), __uint_as_float(v[q * 8 + 1]), __uint_as_float(v[q * 8 + 2]), __uint_as_float(v[q * 8 + 3])),
+                                 make_float4(__uint_as_float(v[q * 8 + 4]), __uint_as_float(v[q * 8 + 5]), __uint_as_float(v[q * 8 + 6]), __uint_as_float(v[q * 8 + 7])));
+        } else if (m0 + row < p.d[1]) {                  // a warp stores 32 neighbours of an output row at a time
+          const int n = min(32, p.R - c);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            if (j < n) {
+              const int64_t at = (int64_t)(c + j) * p.ld[1] + m0 + row;
+              if (p.out_f32) reinterpret_cast<float*>(p.out[1])[at] = __uint_as_float(v[j]);
+              else reinterpret_cast<__nv_bfloat16*>(p.out[1])[at] = __float2bfloat16_rn(__uint_as_float(v[j]));
+            }
+          }
+        }
+      }
     }
     tc_fence_before();
+    __syncthreads();
+  } else {
+    // Every CTA owns a share of the output: 128 / split rows of the tile, or R / split columns of it where those are the
+    // rows of the output.  The others' accumulators are pushed into its shared memory (over the ring, which is idle in
+    // the whole cluster past the first barrier) and added up there, in the order of the CTAs.
+    tc_fence_before();
+    grad_cluster_barrier();
+    tc_fence_after();
+    const int share = (by_rows ? kGM : p.R) / split;
+    const int pitch = by_rows ? p.R + 4 : kGM + 4;
+    if (drain) {
+      if (by_rows) {
+        const int owner = row / share;
+        const uint32_t to = grad_peer(base, owner) + (uint32_t)((cta * share + row - owner * share) * pitch) * 4u;
+        for (int c = 0; c < p.R; c += 32) {
+          uint32_t v[32];
+          columns(c, v);
+#pragma unroll
+          for (int q = 0; q < 8; ++q)
+            if (c + q * 4 < p.R) st_peer_v4(to + (uint32_t)(c + q * 4) * 4u, v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
+        }
+      } else {
+        for (int c = 0; c < p.R; c += 32) {
+          uint32_t v[32];
+          columns(c, v);
+          const int n = min(32, p.R - c);
+          int owner = c / share, left = share - (c - owner * share);
+          uint32_t to = grad_peer(base, owner) + (uint32_t)((cta * share + share - left) * pitch + row) * 4u;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) {
+            if (j < n) {
+              if (left == 0) {
+                left = share;
+                to = grad_peer(base, ++owner) + (uint32_t)(cta * share * pitch + row) * 4u;
+              }
+              st_peer_b32(to, v[j]);
+              to += (uint32_t)pitch * 4u;
+              --left;
+            }
+          }
+        }
+      }
+      tc_fence_before();
+    }
+    grad_cluster_barrier();                              // this CTA's shares have arrived, and it may leave when it is done
+    if (*abort_flag == 0) {
+      const float* in = reinterpret_cast<const float*>(base_ptr);
+      const int groups = (by_rows ? p.R : kGM) / 8;      // eight numbers a thread
+      for (int i = tid; i < share * groups; i += kGThreads) {
+        const int line = i / groups, col = (i - line * groups) * 8;
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+        for (int r = 0; r < split; ++r) {
+          const float4* q = reinterpret_cast<const float4*>(in + (r * share + line) * pitch + col);
+          const float4 x = q[0], y = q[1];
+          a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
+          b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
+        }
+        const int at = cta * share + line;
+        if (by_rows) {
+          store_row8<kPhase>(p, side, m0 + at, col, kPhase == PHASE_SHRINK ? gates[at] : RowGate{}, a, b);
+        } else if (m0 + col < p.d[1]) {                  // d_out is a multiple of 16
+          store8(p.out[1], (int64_t)at * p.ld[1] + m0 + col, p.out_f32, a, b);
+        }
+      }
+    }
+    __syncthreads();
   }
-  __syncthreads();
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc1(tmem, (uint32_t)p.tmem_cols);
   }
-  const bool failed = *abort_flag != 0;
-  if (failed && tid == 0) flag_status(p.status_word, CWL_ERR_TIMEOUT);
-  if (split > 1) grad_cluster_barrier();                 // every CTA's partial accumulator lies in its shared memory
-
-  uint32_t peer[kGMaxCluster];
-  const uint32_t dump_addr = base;
-#pragma unroll
-  for (int r = 0; r < kGMaxCluster; ++r) peer[r] = r < split ? (split > 1 ? grad_peer(dump_addr, r) : dump_addr) : 0;
-  auto sum4 = [&](int row, int col) {                    // in the order of the CTAs
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int r = 0; r < kGMaxCluster; ++r) {
-      if (r < split) {
-        const float4 v = ld_peer_v4(peer[r] + (uint32_t)(row * pitch + col) * 4u);
-        a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
-      }
-    }
-    return a;
-  };
-  if (!failed) {
-    if (kPhase == PHASE_SHRINK || side == 0) {
-      // rows of the tile are rows of the output: this CTA's share of them, eight columns a thread
-      const int rows = kGM / split, groups = p.R / 8;
-      for (int i = tid; i < rows * groups; i += kGThreads) {
-        const int row = cta * rows + i / groups, col = (i % groups) * 8;
-        const float4 a = sum4(row, col), b = sum4(row, col + 4);
-        if (kPhase == PHASE_SHRINK) {
-          if (m0 + row < p.T) {
-            const RowGate g = gates[row];
-            uint4 q;
-            q.x = pack_bf16(a.x * gate_at(g, col + 0), a.y * gate_at(g, col + 1));
-            q.y = pack_bf16(a.z * gate_at(g, col + 2), a.w * gate_at(g, col + 3));
-            q.z = pack_bf16(b.x * gate_at(g, col + 4), b.y * gate_at(g, col + 5));
-            q.w = pack_bf16(b.z * gate_at(g, col + 6), b.w * gate_at(g, col + 7));
-            *reinterpret_cast<uint4*>(p.gated[side] + (int64_t)(m0 + row) * p.R + col) = q;
-          }
-        } else if (m0 + row < p.d[0]) {
-          if (p.out_f32) {
-            float* o = reinterpret_cast<float*>(p.out[0]) + (int64_t)(m0 + row) * p.ld[0] + col;
-            *reinterpret_cast<float4*>(o) = a;
-            *reinterpret_cast<float4*>(o + 4) = b;
-          } else {
-            __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.out[0]) + (int64_t)(m0 + row) * p.ld[0] + col;
-            *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16(a.x, a.y), pack_bf16(a.z, a.w), pack_bf16(b.x, b.y), pack_bf16(b.z, b.w));
-          }
-        }
-      }
-    } else {
-      // dB: rows of the tile are columns of the output.  This CTA's share of the R output rows; a warp stores 32
-      // neighbouring columns of one of them.
-      const int cols = p.R / split;
-      for (int i = tid; i < cols * kGM; i += kGThreads) {
-        const int n = cta * cols + i / kGM, m = i % kGM;
-        float a = 0.f;
-#pragma unroll
-        for (int r = 0; r < kGMaxCluster; ++r)
-          if (r < split) a += ld_peer1(peer[r] + (uint32_t)(m * pitch + n) * 4u);
-        if (m0 + m < p.d[1]) {
-          const int64_t at = (int64_t)n * p.ld[1] + m0 + m;
-          if (p.out_f32) reinterpret_cast<float*>(p.out[1])[at] = a;
-          else reinterpret_cast<__nv_bfloat16*>(p.out[1])[at] = __float2bfloat16_rn(a);
-        }
-      }
-    }
-  }
-  if (split > 1) grad_cluster_barrier();                 // nobody leaves while its shared memory is being read
+  if (tid == 0 && *abort_flag != 0) flag_status(p.status_word, CWL_ERR_TIMEOUT);
 }
 
 struct GradLaunch {
@@ -327,10 +368,10 @@ struct GradLaunch {
   size_t smem;
 };
 
-// CTAs a tile's K loop is split over: doubled while all CTAs still fit the GPU at two per SM and each keeps four K blocks.
+// CTAs a tile's K loop is split over: doubled while there is an SM for each and each keeps four K blocks.
 int grad_split(int tiles, int min_kb) {
   int s = 1;
-  while (s < kGMaxCluster && tiles * s * 2 <= 296 && min_kb / (s * 2) >= 4) s *= 2;
+  while (s < kGMaxCluster && tiles * s * 2 <= 148 && min_kb / (s * 2) >= 4) s *= 2;
   return s;
 }
 
@@ -343,7 +384,8 @@ GradLaunch grad_launch(int R, int tiles, int min_kb) {
   const int budget = R <= 128 ? 96 * 1024 : 192 * 1024;
   l.stages = budget / l.stage_bytes;
   if (l.stages > kGMaxStages) l.stages = kGMaxStages;
-  const int dump = (kGM * (R + 4) * 4 + 1023) / 1024 * 1024;
+  const int by_rows = kGM * (R + 4), by_columns = R * (kGM + 4);      // where a cluster's partial sums meet
+  const int dump = l.split == 1 ? 0 : ((by_rows > by_columns ? by_rows : by_columns) * 4 + 1023) / 1024 * 1024;
   l.ring_bytes = l.stages * l.stage_bytes > dump ? l.stages * l.stage_bytes : dump;
   l.tmem_cols = 32;
   while (l.tmem_cols < R) l.tmem_cols *= 2;
