@@ -45,6 +45,7 @@ struct GradParams {
   int n_kb[2];                 // 64-deep K blocks per side
   int split;                   // CTAs of the cluster that share a tile's K loop
   int stages, stage_bytes, narrow_bytes, tmem_cols, ring_bytes;
+  int meet_in_ring, meet_off;  // where a cluster's partial sums meet: over the idle ring, or beside it
   __nv_bfloat16* gated[2];     // SHRINK: where side s's result goes: H' (side 0) and G (side 1), [T, R]
   void* out[2]; int64_t ld[2]; // FOLD: dA, dB
   int out_f32;
@@ -89,6 +90,8 @@ __device__ __forceinline__ uint32_t grad_cluster_rank() {
 __device__ __forceinline__ void grad_cluster_barrier() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void grad_cluster_barrier_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void grad_cluster_barrier_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ uint32_t grad_peer(uint32_t addr, uint32_t cta) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
@@ -126,7 +129,6 @@ __device__ __forceinline__ void store_row8(const GradParams& p, int side, int at
 template <int kPhase>
 __global__ void __launch_bounds__(kGThreads)
 grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradParams p) {
-  pdl_launch_dependents();
   extern __shared__ uint8_t grad_raw[];
   const uint32_t raw = smem_u32(grad_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;         // swizzled boxes need 1024-byte alignment
@@ -171,33 +173,50 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  pdl_wait();                                            // nothing above reads or writes global memory
+  if (split > 1 && !p.meet_in_ring) grad_cluster_barrier_arrive();
+  // SHRINK waits here for the launch ahead, and only then lets FOLD be placed: a FOLD that runs therefore knows that what
+  // came before SHRINK is complete.  It reads X and dY at once; all that SHRINK writes, and its own outputs, wait below.
+  if (kPhase == PHASE_SHRINK) {
+    pdl_wait();
+    pdl_launch_dependents();
+  } else {
+    pdl_launch_dependents();
+  }
 
   const bool narrow_k_major = kPhase == PHASE_SHRINK && side == 1;      // B [R, d_out]: its K dimension is contiguous
   if (warp == 0) {
     if (lane == 0) {
       const int n_boxes = narrow_k_major ? 1 : (p.R + 63) / 64;
       const uint32_t tx = (uint32_t)(kGLeftBytes + (narrow_k_major ? p.R * kGK * 2 : n_boxes * kGBoxBytes));
-      int s = 0;
-      uint32_t ph = 0;
-      int issued = 0;
-      bool ok = true;
-      for (int b = 0; b < n_blk; ++b) {
-        if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) { ok = false; break; }
-        const int k = (kb0 + b) * kGK;
-        const uint32_t sa = base + (uint32_t)(s * p.stage_bytes), sb = sa + kGLeftBytes;
-        mbar_expect_tx(full_bar(s), tx);
+      auto load_wide = [&](int st, int k) {
+        const uint32_t sa = base + (uint32_t)(st * p.stage_bytes);
+        mbar_expect_tx(full_bar(st), tx);
         if (kPhase == PHASE_SHRINK) {
-          tma_load_2d(sa, wide, full_bar(s), k, m0);
+          tma_load_2d(sa, wide, full_bar(st), k, m0);
         } else {
-          tma_load_2d(sa, wide, full_bar(s), m0, k);
-          tma_load_2d(sa + kGBoxBytes, wide, full_bar(s), m0 + 64, k);
+          tma_load_2d(sa, wide, full_bar(st), m0, k);
+          tma_load_2d(sa + kGBoxBytes, wide, full_bar(st), m0 + 64, k);
         }
+      };
+      auto load_narrow = [&](int st, int k) {
+        const uint32_t sb = base + (uint32_t)(st * p.stage_bytes) + kGLeftBytes;
         if (narrow_k_major) {
-          tma_load_2d(sb, narrow, full_bar(s), k, 0);
+          tma_load_2d(sb, narrow, full_bar(st), k, 0);
         } else {
-          for (int j = 0; j < n_boxes; ++j) tma_load_2d(sb + j * kGBoxBytes, narrow, full_bar(s), j * 64, k);
+          for (int j = 0; j < n_boxes; ++j) tma_load_2d(sb + j * kGBoxBytes, narrow, full_bar(st), j * 64, k);
         }
+      };
+      const int ahead = min(n_blk, p.stages);            // the ring starts empty
+      for (int b = 0; b < ahead; ++b) load_wide(b, (kb0 + b) * kGK);
+      if (kPhase == PHASE_FOLD) pdl_wait();
+      for (int b = 0; b < ahead; ++b) load_narrow(b, (kb0 + b) * kGK);
+      int issued = ahead, s = 0;
+      uint32_t ph = 1;
+      bool ok = true;
+      for (int b = ahead; b < n_blk; ++b) {
+        if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) { ok = false; break; }
+        load_wide(s, (kb0 + b) * kGK);
+        load_narrow(s, (kb0 + b) * kGK);
         ++issued;
         if (++s == p.stages) { s = 0; ph ^= 1u; }
       }
@@ -244,6 +263,7 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
     gates[mine] = row_gate(m0 + mine, p);                // while the main loop runs (a chain of dependent loads)
   }
 
+  if (kPhase == PHASE_FOLD) pdl_wait();                  // every thread, before it writes an output
   // Wait for the accumulator.  A CTA without K blocks (short loops on many CTAs) contributes zeros.
   const int quad = warp & 3, row = quad * 32 + lane;     // of warps 2..5: the TMEM lanes a warp may read, one tile row a lane
   const bool drain = warp >= 2;
@@ -292,23 +312,29 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
     __syncthreads();
   } else {
     // Every CTA owns a share of the output: 128 / split rows of the tile, or R / split columns of it where those are the
-    // rows of the output.  The others' accumulators are pushed into its shared memory (over the ring, which is idle in
-    // the whole cluster past the first barrier) and added up there, in the order of the CTAs.
-    tc_fence_before();
-    grad_cluster_barrier();
-    tc_fence_after();
+    // rows of the output.  The others' accumulators are pushed into its shared memory and added up there, in the order of
+    // the CTAs.  Layouts are such that a warp's stores are contiguous: [column group of 4][rows][4] and [column][128 rows].
+    if (p.meet_in_ring) {                                // over the ring, once it is idle in the whole cluster
+      tc_fence_before();
+      grad_cluster_barrier();
+      tc_fence_after();
+    } else {
+      grad_cluster_barrier_wait();                       // the peers run (they arrived at their start)
+    }
     const int share = (by_rows ? kGM : p.R) / split;
-    const int pitch = by_rows ? p.R + 4 : kGM + 4;
+    const uint32_t meet = base + (uint32_t)p.meet_off;
+    const int part = by_rows ? share * p.R : share * kGM;            // numbers that one CTA contributes to a share
     if (drain) {
       if (by_rows) {
         const int owner = row / share;
-        const uint32_t to = grad_peer(base, owner) + (uint32_t)((cta * share + row - owner * share) * pitch) * 4u;
+        const uint32_t to = grad_peer(meet, owner) + (uint32_t)(cta * part + (row - owner * share) * 4) * 4u;
         for (int c = 0; c < p.R; c += 32) {
           uint32_t v[32];
           columns(c, v);
 #pragma unroll
           for (int q = 0; q < 8; ++q)
-            if (c + q * 4 < p.R) st_peer_v4(to + (uint32_t)(c + q * 4) * 4u, v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
+            if (c + q * 4 < p.R)
+              st_peer_v4(to + (uint32_t)((c + q * 4) * share) * 4u, v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
         }
       } else {
         for (int c = 0; c < p.R; c += 32) {
@@ -316,16 +342,16 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
           columns(c, v);
           const int n = min(32, p.R - c);
           int owner = c / share, left = share - (c - owner * share);
-          uint32_t to = grad_peer(base, owner) + (uint32_t)((cta * share + share - left) * pitch + row) * 4u;
+          uint32_t to = grad_peer(meet, owner) + (uint32_t)(cta * part + (share - left) * kGM + row) * 4u;
 #pragma unroll
           for (int j = 0; j < 32; ++j) {
             if (j < n) {
               if (left == 0) {
                 left = share;
-                to = grad_peer(base, ++owner) + (uint32_t)(cta * share * pitch + row) * 4u;
+                to = grad_peer(meet, ++owner) + (uint32_t)(cta * part + row) * 4u;
               }
               st_peer_b32(to, v[j]);
-              to += (uint32_t)pitch * 4u;
+              to += kGM * 4u;
               --left;
             }
           }
@@ -335,14 +361,16 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
     }
     grad_cluster_barrier();                              // this CTA's shares have arrived, and it may leave when it is done
     if (*abort_flag == 0) {
-      const float* in = reinterpret_cast<const float*>(base_ptr);
-      const int groups = (by_rows ? p.R : kGM) / 8;      // eight numbers a thread
-      for (int i = tid; i < share * groups; i += kGThreads) {
-        const int line = i / groups, col = (i - line * groups) * 8;
+      const float* in = reinterpret_cast<const float*>(base_ptr + p.meet_off);
+      // eight numbers of an output row a thread
+      for (int i = tid; i < part / 8; i += kGThreads) {
         float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-        for (int r = 0; r < split; ++r) {
-          const float4* q = reinterpret_cast<const float4*>(in + (r * share + line) * pitch + col);
-          const float4 x = q[0], y = q[1];
+        const int line = by_rows ? i % share : i / (kGM / 8);        // row of the tile in the share, or column of it
+        const int col = by_rows ? (i / share) * 8 : (i % (kGM / 8)) * 8;
+        const float* q = in + (by_rows ? col * share + line * 4 : line * kGM + col);
+        const int second = by_rows ? share * 4 : 4;
+        for (int r = 0; r < split; ++r, q += part) {
+          const float4 x = *reinterpret_cast<const float4*>(q), y = *reinterpret_cast<const float4*>(q + second);
           a.x += x.x; a.y += x.y; a.z += x.z; a.w += x.w;
           b.x += y.x; b.y += y.y; b.z += y.z; b.w += y.w;
         }
@@ -364,14 +392,15 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
 }
 
 struct GradLaunch {
-  int split, stages, stage_bytes, narrow_bytes, tmem_cols, ring_bytes;
+  int split, stages, stage_bytes, narrow_bytes, tmem_cols, ring_bytes, meet_in_ring, meet_off;
   size_t smem;
 };
 
-// CTAs a tile's K loop is split over: doubled while there is an SM for each and each keeps four K blocks.
+// CTAs a tile's K loop is split over: doubled while there is an SM for each and each keeps four K blocks; up to two CTAs
+// an SM where each keeps 64 blocks, which is what the meeting of the partial sums (4 us) asks for.
 int grad_split(int tiles, int min_kb) {
   int s = 1;
-  while (s < kGMaxCluster && tiles * s * 2 <= 148 && min_kb / (s * 2) >= 4) s *= 2;
+  while (s < kGMaxCluster && ((tiles * s * 2 <= 148 && min_kb / (s * 2) >= 4) || (tiles * s * 2 <= 296 && min_kb / (s * 2) >= 64))) s *= 2;
   return s;
 }
 
@@ -380,13 +409,31 @@ GradLaunch grad_launch(int R, int tiles, int min_kb) {
   l.split = grad_split(tiles, min_kb);
   l.narrow_bytes = ((R + 63) / 64) * kGBoxBytes;
   l.stage_bytes = kGLeftBytes + l.narrow_bytes;
-  // up to R = 128 a ring of 96 KB lets two CTAs share an SM; above, one CTA takes what the SM has
+  // up to R = 128 a ring of 96 KB lets two CTAs share an SM (FOLD's set-up then runs beside SHRINK's end); above, one CTA
+  // takes what the SM has
   const int budget = R <= 128 ? 96 * 1024 : 192 * 1024;
   l.stages = budget / l.stage_bytes;
   if (l.stages > kGMaxStages) l.stages = kGMaxStages;
-  const int by_rows = kGM * (R + 4), by_columns = R * (kGM + 4);      // where a cluster's partial sums meet
-  const int dump = l.split == 1 ? 0 : ((by_rows > by_columns ? by_rows : by_columns) * 4 + 1023) / 1024 * 1024;
-  l.ring_bytes = l.stages * l.stage_bytes > dump ? l.stages * l.stage_bytes : dump;
+  // a cluster's partial sums, [128][R] fp32: beside a ring of at least three stages where both fit 109 KB (no need to wait
+  // for the whole cluster's MMAs before they are sent), else over the ring
+  const int meet = l.split == 1 ? 0 : kGM * R * 4;
+  l.meet_in_ring = 0;
+  l.ring_bytes = l.stages * l.stage_bytes;
+  if (l.split > 1) {
+    int beside = (109 * 1024 - meet) / l.stage_bytes;
+    if (beside > l.stages) beside = l.stages;
+    if (beside >= 3) {
+      l.stages = beside;
+      l.meet_off = l.stages * l.stage_bytes;
+      l.ring_bytes = l.meet_off + meet;
+    } else {
+      l.meet_in_ring = 1;
+      l.meet_off = 0;
+      if (l.ring_bytes < meet) l.ring_bytes = meet;
+    }
+  } else {
+    l.meet_off = 0;
+  }
   l.tmem_cols = 32;
   while (l.tmem_cols < R) l.tmem_cols *= 2;
   l.smem = (size_t)l.ring_bytes + 1024 + 8 * (2 * kGMaxStages + 1) + 8 + 32 + kGM * sizeof(RowGate);
@@ -480,7 +527,7 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
     p.first = kb1 > kb0 ? 1 : 0;                         // the longer loops start first
     const GradLaunch l = grad_launch(R, tiles0 + tiles1, kb0 < kb1 ? kb0 : kb1);
     p.split = l.split; p.stages = l.stages; p.stage_bytes = l.stage_bytes; p.narrow_bytes = l.narrow_bytes;
-    p.tmem_cols = l.tmem_cols; p.ring_bytes = l.ring_bytes;
+    p.tmem_cols = l.tmem_cols; p.ring_bytes = l.ring_bytes; p.meet_in_ring = l.meet_in_ring; p.meet_off = l.meet_off;
     return l;
   };
   const int row_tiles = ceil_div(T, kGM), t_blocks = ceil_div(T, kGK);
