@@ -396,17 +396,20 @@ struct GradLaunch {
   size_t smem;
 };
 
-// CTAs a tile's K loop is split over: doubled while there is an SM for each and each keeps four K blocks; up to two CTAs
-// an SM where each keeps 64 blocks, which is what the meeting of the partial sums (4 us) asks for.
-int grad_split(int tiles, int min_kb) {
+// CTAs a tile's K loop is split over: doubled while there is an SM for each and each keeps four K blocks; up to `resident`
+// CTAs (two an SM where their shared memory allows it) while each keeps kDeepBlocks, which is what the meeting of the
+// partial sums asks for.
+constexpr int kDeepBlocks = 8;
+int grad_split(int tiles, int min_kb, int resident) {
   int s = 1;
-  while (s < kGMaxCluster && ((tiles * s * 2 <= 148 && min_kb / (s * 2) >= 4) || (tiles * s * 2 <= 296 && min_kb / (s * 2) >= 64))) s *= 2;
+  while (s < kGMaxCluster && ((tiles * s * 2 <= 148 && min_kb / (s * 2) >= 4) || (tiles * s * 2 <= resident && min_kb / (s * 2) >= kDeepBlocks)))
+    s *= 2;
   return s;
 }
 
 GradLaunch grad_launch(int R, int tiles, int min_kb) {
   GradLaunch l;
-  l.split = grad_split(tiles, min_kb);
+  l.split = grad_split(tiles, min_kb, R <= 128 ? 296 : 148);
   l.narrow_bytes = ((R + 63) / 64) * kGBoxBytes;
   l.stage_bytes = kGLeftBytes + l.narrow_bytes;
   // up to R = 128 a ring of 96 KB lets two CTAs share an SM (FOLD's set-up then runs beside SHRINK's end); above, one CTA
