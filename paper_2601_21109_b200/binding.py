@@ -608,16 +608,19 @@ def cwl_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = N
                        stream: Optional[torch.cuda.Stream] = None) -> TokenLogprobs:
     """Log-probability of each row's target token (negative: none), log-sum-exp, entropy in nats and the ``top_k`` most
     likely tokens of softmax(logits / temperature); logits fp32, bf16 or fp16 [T, V] on the device."""
-    assert logits.is_cuda and logits.dtype in _DTYPES and logits.dim() == 2 and logits.stride(1) == 1
+    assert logits.dtype in _DTYPES
     T, V = logits.shape
+    ld, unit = logits.stride()
+    assert logits.is_cuda and unit == 1
     if out is None:
         out = TokenLogprobs(T, top_k, targets is not None, logits.device)
-    assert out.T == T and out.top_k == top_k and (out.logprob is not None) == (targets is not None)
+    else:
+        assert out.T == T and out.top_k == top_k and (out.logprob is None) == (targets is None)
     if targets is not None:
         assert targets.is_cuda and targets.dtype == torch.int32 and targets.is_contiguous() and targets.numel() == T
     _check("cwl_token_logprobs", lib().cwl_token_logprobs(
-        _p(logits), _DTYPES[logits.dtype], logits.stride(0) if T > 1 else max(V, logits.stride(0)), T, V, _p(targets),
-        temperature, top_k, *out._ptrs, _p(status_word), _stream_ptr(stream)))
+        logits.data_ptr(), _DTYPES[logits.dtype], ld if T > 1 else max(V, ld), T, V, _p(targets), temperature, top_k, *out._ptrs,
+        _p(status_word), _stream_ptr(stream)))
     return out
 
 
@@ -630,28 +633,32 @@ def cwl_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_va
     padding) into the student's logits [T, V] (fp32, bf16 or fp16).  ``teacher`` says what the values are: "logits",
     renormalised over the entries, or "logprobs" of the tempered teacher, whose remaining mass is one more outcome.
     Returns (loss fp32 [T] or None, dlogits or None); ``dlogits`` may be ``logits`` itself."""
-    assert logits.is_cuda and logits.dtype in _DTYPES and logits.dim() == 2 and logits.stride(1) == 1
+    assert logits.dtype in _DTYPES
     T, V = logits.shape
     K = teacher_ids.shape[1]
-    assert teacher_ids.is_cuda and teacher_ids.dtype == torch.int32 and teacher_ids.shape == (T, K) and teacher_ids.stride(1) == 1
-    assert teacher_values.is_cuda and teacher_values.dtype == torch.float32 and teacher_values.shape == (T, K)
-    assert teacher_values.stride() == teacher_ids.stride()
-    for t in (weight, dloss):
-        assert t is None or (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.numel() == T)
-    if want_loss and loss is None:
-        loss = torch.empty(T, dtype=torch.float32, device=logits.device)
-    if want_grad and dlogits is None:
-        dlogits = torch.empty(T, V, dtype=logits.dtype, device=logits.device)
+    ld, unit = logits.stride()
+    ld_teacher, t_unit = teacher_ids.stride()
+    assert logits.is_cuda and unit == 1
+    assert teacher_ids.is_cuda and teacher_ids.dtype == torch.int32 and teacher_ids.shape[0] == T and t_unit == 1
+    assert teacher_values.is_cuda and teacher_values.dtype == torch.float32 and teacher_values.shape == teacher_ids.shape
+    assert teacher_values.stride() == (ld_teacher, t_unit)
+    assert weight is None or (weight.is_cuda and weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == T)
+    assert dloss is None or (dloss.is_cuda and dloss.dtype == torch.float32 and dloss.is_contiguous() and dloss.numel() == T)
     if loss is not None:
         assert loss.is_cuda and loss.dtype == torch.float32 and loss.is_contiguous() and loss.numel() == T
+    elif want_loss:
+        loss = teacher_values.new_empty(T)
+    ld_d = 0
     if dlogits is not None:
-        assert dlogits.is_cuda and dlogits.dtype == logits.dtype and dlogits.shape == (T, V) and dlogits.stride(1) == 1
-    many = T > 1
+        ld_d, d_unit = dlogits.stride()
+        assert dlogits.is_cuda and dlogits.dtype == logits.dtype and dlogits.shape == (T, V) and d_unit == 1
+    elif want_grad:
+        dlogits, ld_d = logits.new_empty((T, V)), V
+    if T == 1:                                   # a single row's stride says nothing
+        ld, ld_teacher, ld_d = max(V, ld), max(K, ld_teacher), max(V, ld_d)
     _check("cwl_distill_topk", lib().cwl_distill_topk(
-        _p(logits), _DTYPES[logits.dtype], logits.stride(0) if many else max(V, logits.stride(0)), T, V, _p(teacher_ids),
-        _p(teacher_values), teacher_ids.stride(0) if many else max(K, teacher_ids.stride(0)), K, TEACHER_MODES[teacher],
-        temperature, _p(weight), _p(dloss), _p(loss), _p(dlogits),
-        0 if dlogits is None else dlogits.stride(0) if many else max(V, dlogits.stride(0)), _p(status_word),
+        logits.data_ptr(), _DTYPES[logits.dtype], ld, T, V, teacher_ids.data_ptr(), teacher_values.data_ptr(), ld_teacher, K,
+        TEACHER_MODES[teacher], temperature, _p(weight), _p(dloss), _p(loss), _p(dlogits), ld_d, _p(status_word),
         _stream_ptr(stream)))
     return loss, dlogits
 
@@ -667,24 +674,29 @@ def cwl_apply_grads(X: torch.Tensor, dY: torch.Tensor, A: torch.Tensor, B: torch
                     centred: bool = False):
     """Gradients (dA [d_in, R], dB [R, d_out]) of the adapter factors of ``cwl_apply`` under ``table``, from the activations X
     and the output's gradient dY (bf16); fp32 or bf16, of the type of ``dA`` and ``dB`` where they are given."""
-    for t in (X, dY, A, B):
-        assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 2 and t.stride(1) == 1
-    T, d_in = X.shape
-    d_out, R = dY.shape[1], A.shape[1]
-    assert dY.shape[0] == T and A.shape[0] == d_in and B.shape == (R, d_out)
+    (T, d_in), (rows, d_out), (a_rows, R) = X.shape, dY.shape, A.shape
+    assert rows == T and a_rows == d_in and B.shape == (R, d_out)
+    (ldx, ux), (lddy, uy), (lda, ua), (ldb, ub) = X.stride(), dY.stride(), A.stride(), B.stride()
+    assert ux == uy == ua == ub == 1 and X.is_cuda and dY.is_cuda and A.is_cuda and B.is_cuda
+    assert X.dtype == dY.dtype == A.dtype == B.dtype == torch.bfloat16
     if dA is None:
-        dA = torch.empty(d_in, R, dtype=grad_dtype, device=X.device)
+        dA, ldda = X.new_empty((d_in, R), dtype=grad_dtype if dB is None else dB.dtype), R
+    else:
+        ldda, u = dA.stride()
+        assert dA.is_cuda and dA.dtype in _DTYPES and dA.shape == (d_in, R) and u == 1
     if dB is None:
-        dB = torch.empty(R, d_out, dtype=dA.dtype, device=X.device)
-    assert dA.is_cuda and dA.dtype in _DTYPES and dA.shape == (d_in, R) and dA.stride(1) == 1
-    assert dB.is_cuda and dB.dtype == dA.dtype and dB.shape == (R, d_out) and dB.stride(1) == 1
+        dB, lddb = X.new_empty((R, d_out), dtype=dA.dtype), d_out
+    else:
+        lddb, u = dB.stride()
+        assert dB.is_cuda and dB.dtype == dA.dtype and dB.shape == (R, d_out) and u == 1
     if workspace is None:
         workspace = torch.empty(cwl_apply_grads_workspace_bytes(T, d_in, d_out, R), dtype=torch.uint8, device=X.device)
+    if T == 1:                                   # a single row's stride says nothing
+        ldx, lddy = max(d_in, ldx), max(d_out, lddy)
     _check("cwl_apply_grads", lib().cwl_apply_grads(
-        _p(X), X.stride(0) if T > 1 else max(d_in, X.stride(0)), _p(dY), dY.stride(0) if T > 1 else max(d_out, dY.stride(0)),
-        _p(A), A.stride(0), _p(B), B.stride(0), T, d_in, d_out, R, table.c_struct(), int(window),
-        WINDOW_CENTRED if centred else WINDOW_CAUSAL, _p(dA), dA.stride(0), _p(dB), dB.stride(0), _DTYPES[dA.dtype],
-        _p(workspace), workspace.numel(), _p(status_word), _stream_ptr(stream)))
+        X.data_ptr(), ldx, dY.data_ptr(), lddy, A.data_ptr(), lda, B.data_ptr(), ldb, T, d_in, d_out, R, table.c_struct(),
+        int(window), WINDOW_CENTRED if centred else WINDOW_CAUSAL, dA.data_ptr(), ldda, dB.data_ptr(), lddb, _DTYPES[dA.dtype],
+        workspace.data_ptr(), workspace.numel(), _p(status_word), _stream_ptr(stream)))
     return dA, dB
 
 

@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "cwl.h"
 
 #define CWL_CUDA_TRY(expr)                        \
@@ -55,5 +57,23 @@ inline cudaError_t launch_chained(bool chained, void (*kernel)(KArgs...), dim3 g
   cfg.numAttrs = chained ? 1 : 0;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
+
+// Lets a kernel without static shared memory take all that a block may have (227 KB), once per device.
+class SharedMemoryGrant {
+ public:
+  template <typename Kernel>
+  cudaError_t operator()(Kernel* kernel) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess || (dev < kDevices && done_[dev].load(std::memory_order_acquire))) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024);
+    if (e == cudaSuccess && dev < kDevices) done_[dev].store(true, std::memory_order_release);
+    return e;
+  }
+
+ private:
+  static constexpr int kDevices = 32;
+  std::atomic<bool> done_[kDevices] = {};
+};
 
 }  // namespace cwl

@@ -800,7 +800,8 @@ cudaError_t launch_distill(const DistillParams& p, cudaStream_t st) {
   }
   const PipePlan plan = pipe_plan(p.T, row_bytes);
   const size_t smem = (size_t)plan.n_buffers * plan.buffer_bytes + sizeof(DsPipe);
-  const cudaError_t e = cudaFuncSetAttribute(distill_pipe_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static SharedMemoryGrant grant;
+  const cudaError_t e = grant(distill_pipe_kernel<T>);
   if (e != cudaSuccess) return e;
   const int clusters = resident_clusters<T>(plan.log2_cta, smem);
   const int rows = p.T < clusters ? p.T : clusters;

@@ -445,7 +445,8 @@ GradLaunch grad_launch(int R, int tiles, int min_kb) {
 
 template <int kPhase>
 cudaError_t launch_phase(const GradMaps& maps, const GradParams& p, const GradLaunch& l, cudaStream_t st) {
-  const cudaError_t e = cudaFuncSetAttribute(grad_kernel<kPhase>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)l.smem);
+  static SharedMemoryGrant grant;
+  const cudaError_t e = grant(grad_kernel<kPhase>);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((p.n_tiles[0] + p.n_tiles[1]) * l.split));
