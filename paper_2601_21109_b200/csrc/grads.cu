@@ -4,9 +4,11 @@
 //   G = g o (dY B^T),   dA = X^T G,   dB = H'^T dY
 //
 // Two launches of tcgen05 products whose narrow side is the ladder rank R:
-//   SHRINK  one output tile per 128 rows: P = X A and Q = dY B^T (K = d_in and d_out), gated and rounded to bf16 as the
-//           forward pass rounds H', so that dB is the gradient of the projection that was computed;
-//   FOLD    one output tile per 128 columns of X or dY: dA = X^T G and dB^T = dY^T H' (K = T).
+//   SHRINK  one output tile per 128 rows: P = X A and Q = dY B^T (K = d_in and d_out), gated, and kept as the sum of two
+//           bf16 numbers (16 significant bits: rounded once to 8, the gradients' error would grow by 40 % over that of
+//           their own rounding to bf16, and fp32 gradients would not be worth their name);
+//   FOLD    one output tile per 128 columns of X or dY: dA = X^T G and dB^T = dY^T H' (K = T), both halves in one pass
+//           over X and dY: [G_hi G_lo] is one operand of 2 R columns, and the halves of the product meet in the epilogue.
 // X and dY are read by both: no output of FOLD can be summed before all of d_in / d_out went through SHRINK for its rows.
 // The K loop of a tile is split over the CTAs of a cluster where the tiles alone do not fill the GPU; the partial
 // accumulators meet in distributed shared memory in a fixed order, so results do not depend on timing.
@@ -46,7 +48,8 @@ struct GradParams {
   int split;                   // CTAs of the cluster that share a tile's K loop
   int stages, stage_bytes, narrow_bytes, tmem_cols, ring_bytes;
   int meet_in_ring, meet_off;  // where a cluster's partial sums meet: over the idle ring, or beside it
-  __nv_bfloat16* gated[2];     // SHRINK: where side s's result goes: H' (side 0) and G (side 1), [T, R]
+  __nv_bfloat16* gated[2];     // SHRINK: where side s's result goes: H' (side 0) and G (side 1), [T, gated_ld]
+  int gated_ld, lo_col;        // a row: R columns of high halves, then (from column lo_col) R of low halves
   void* out[2]; int64_t ld[2]; // FOLD: dA, dB
   int out_f32;
   unsigned long long wait_limit_ns;
@@ -117,10 +120,19 @@ __device__ __forceinline__ void store8(void* out, int64_t at, int f32, const flo
 template <int kPhase>
 __device__ __forceinline__ void store_row8(const GradParams& p, int side, int at, int col, const RowGate& g, const float4& a, const float4& b) {
   if (kPhase == PHASE_SHRINK) {
-    if (at < p.T)
-      *reinterpret_cast<uint4*>(p.gated[side] + (int64_t)at * p.R + col) =
-          make_uint4(pack_bf16(a.x * gate_at(g, col + 0), a.y * gate_at(g, col + 1)), pack_bf16(a.z * gate_at(g, col + 2), a.w * gate_at(g, col + 3)),
-                     pack_bf16(b.x * gate_at(g, col + 4), b.y * gate_at(g, col + 5)), pack_bf16(b.z * gate_at(g, col + 6), b.w * gate_at(g, col + 7)));
+    if (at < p.T) {
+      const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float x = v[2 * k] * gate_at(g, col + 2 * k), y = v[2 * k + 1] * gate_at(g, col + 2 * k + 1);
+        hi[k] = pack_bf16(x, y);
+        lo[k] = pack_bf16(x - __uint_as_float(hi[k] << 16), y - __uint_as_float(hi[k] & 0xFFFF0000u));
+      }
+      __nv_bfloat16* o = p.gated[side] + (int64_t)at * p.gated_ld + col;
+      *reinterpret_cast<uint4*>(o) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(o + p.lo_col) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
   } else if (at < p.d[0]) {
     store8(p.out[0], (int64_t)at * p.ld[0] + col, p.out_f32, a, b);
   }
@@ -186,7 +198,7 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
   const bool narrow_k_major = kPhase == PHASE_SHRINK && side == 1;      // B [R, d_out]: its K dimension is contiguous
   if (warp == 0) {
     if (lane == 0) {
-      const int n_boxes = narrow_k_major ? 1 : (p.R + 63) / 64;
+      const int n_boxes = narrow_k_major ? 1 : p.narrow_bytes / kGBoxBytes;
       const uint32_t tx = (uint32_t)(kGLeftBytes + (narrow_k_major ? p.R * kGK * 2 : n_boxes * kGBoxBytes));
       auto load_wide = [&](int st, int k) {
         const uint32_t sa = base + (uint32_t)(st * p.stage_bytes);
@@ -231,7 +243,10 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
     }
   } else if (warp == 1) {
     if (lane == 0 && n_blk > 0) {
-      const uint32_t idesc = grad_idesc(p.R, kPhase == PHASE_FOLD, !narrow_k_major);
+      // FOLD: both halves as one product of 2 R columns where that is at most 256, else one after the other
+      const bool halves = kPhase == PHASE_FOLD && 2 * p.R > 256;
+      const uint32_t idesc = grad_idesc(kPhase == PHASE_FOLD && !halves ? 2 * p.R : p.R, kPhase == PHASE_FOLD, !narrow_k_major);
+      const uint64_t lo_half = (uint64_t)((p.lo_col / 64) * kGBoxBytes) >> 4;
       // one K step of 16 further on: 32 bytes in a K-major tile, 16 rows of 128 bytes in a box with the other order
       const uint64_t step_a = kPhase == PHASE_SHRINK ? (16 * 2) >> 4 : (16 * 128) >> 4;
       const uint64_t step_b = narrow_k_major ? (16 * 2) >> 4 : (16 * 128) >> 4;
@@ -245,8 +260,10 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
         const uint64_t da = kPhase == PHASE_SHRINK ? make_smem_desc(sa, 16, 1024) : make_smem_desc(sa, kGBoxBytes, 1024);
         const uint64_t db = narrow_k_major ? make_smem_desc(sb, 16, 1024) : make_smem_desc(sb, kGBoxBytes, 1024);
 #pragma unroll
-        for (int kk = 0; kk < kGK / 16; ++kk)
+        for (int kk = 0; kk < kGK / 16; ++kk) {
           umma_bf16(tmem, da + kk * step_a, db + kk * step_b, idesc, (b | kk) ? 1u : 0u);
+          if (halves) umma_bf16(tmem + p.lo_col, da + kk * step_a, db + lo_half + kk * step_b, idesc, (b | kk) ? 1u : 0u);
+        }
         umma_commit(empty_bar(s));
         if (++s == p.stages) { s = 0; ph ^= 1u; }
       }
@@ -275,7 +292,15 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
   auto columns = [&](int c, uint32_t (&v)[32]) {         // 32 columns of this lane's row
     if (n_blk > 0) {
       tmem_ld32(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
-      tmem_ld_wait();
+      if (kPhase == PHASE_FOLD) {
+        uint32_t lo[32];
+        tmem_ld32(tmem + ((uint32_t)(quad * 32) << 16) + p.lo_col + c, lo);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(lo[j]));
+      } else {
+        tmem_ld_wait();
+      }
     } else {
 #pragma unroll
       for (int j = 0; j < 32; ++j) v[j] = 0;
@@ -407,14 +432,16 @@ int grad_split(int tiles, int min_kb, int resident) {
   return s;
 }
 
-GradLaunch grad_launch(int R, int tiles, int min_kb) {
+// `columns` of the narrow operand: R, or what both halves of G / H' take
+GradLaunch grad_launch(int R, int columns, int tiles, int min_kb) {
   GradLaunch l;
-  l.split = grad_split(tiles, min_kb, R <= 128 ? 296 : 148);
-  l.narrow_bytes = ((R + 63) / 64) * kGBoxBytes;
+  l.narrow_bytes = ((columns + 63) / 64) * kGBoxBytes;
   l.stage_bytes = kGLeftBytes + l.narrow_bytes;
-  // up to R = 128 a ring of 96 KB lets two CTAs share an SM (FOLD's set-up then runs beside SHRINK's end); above, one CTA
+  // three stages or more in 96 KB let two CTAs share an SM (FOLD's set-up then runs beside SHRINK's end); a deeper stage
   // takes what the SM has
-  const int budget = R <= 128 ? 96 * 1024 : 192 * 1024;
+  const bool pair = 3 * l.stage_bytes <= 96 * 1024;
+  l.split = grad_split(tiles, min_kb, pair ? 296 : 148);
+  const int budget = pair ? 96 * 1024 : 192 * 1024;
   l.stages = budget / l.stage_bytes;
   if (l.stages > kGMaxStages) l.stages = kGMaxStages;
   // a cluster's partial sums, [128][R] fp32: beside a ring of at least three stages where both fit 109 KB (no need to wait
@@ -437,8 +464,10 @@ GradLaunch grad_launch(int R, int tiles, int min_kb) {
   } else {
     l.meet_off = 0;
   }
+  // the epilogue reads 32 columns at a time, from 0 and (low halves) from columns - R on
+  const int read = columns - R + (R + 31) / 32 * 32;
   l.tmem_cols = 32;
-  while (l.tmem_cols < R) l.tmem_cols *= 2;
+  while (l.tmem_cols < read) l.tmem_cols *= 2;
   l.smem = (size_t)l.ring_bytes + 1024 + 8 * (2 * kGMaxStages + 1) + 8 + 32 + kGM * sizeof(RowGate);
   return l;
 }
@@ -463,7 +492,10 @@ cudaError_t launch_phase(const GradMaps& maps, const GradParams& p, const GradLa
   return cudaLaunchKernelEx(&cfg, grad_kernel<kPhase>, maps, p);
 }
 
-size_t gated_bytes(int T, int R) { return ((size_t)T * R * 2 + 255) / 256 * 256; }
+// G and H' hold two halves a row: side by side where one product takes both, else the low half from a multiple of 64 on
+// (a box's edge), where a product of its own can start
+int lo_column(int R) { return 2 * R <= 256 ? R : (R + 63) / 64 * 64; }
+size_t gated_bytes(int T, int R) { return ((size_t)T * (lo_column(R) + R) * 2 + 255) / 256 * 256; }
 
 bool bad_matrix(const void* ptr, int64_t ld, int64_t cols, int elem) {
   return !aligned16(ptr) || ld < cols || (ld * elem) % 16 != 0;
@@ -513,6 +545,8 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
   p.T = T; p.R = R; p.d[0] = d_in; p.d[1] = d_out;
   p.window = window; p.window_mode = window_mode; p.table = table; p.row_gates = nullptr;
   p.gated[0] = H; p.gated[1] = G;
+  p.lo_col = lo_column(R);
+  p.gated_ld = p.lo_col + R;
   p.out[0] = dA; p.out[1] = dB; p.ld[0] = ldda; p.ld[1] = lddb; p.out_f32 = grad_dtype == CWL_F32;
   p.wait_limit_ns = kGWaitLimitNs;
   p.status_word = status_word;
@@ -521,23 +555,23 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
   const bool maps_ok =
       make_map(&shrink.wide[0], X, d_in, T, ldx, kGK, kGM) && make_map(&shrink.narrow[0], A, R, d_in, lda, 64, kGK) &&
       make_map(&shrink.wide[1], dY, d_out, T, lddy, kGK, kGM) && make_map(&shrink.narrow[1], B, d_out, R, ldb, kGK, R) &&
-      make_map(&fold.wide[0], X, d_in, T, ldx, 64, kGK) && make_map(&fold.narrow[0], G, R, T, R, 64, kGK) &&
-      make_map(&fold.wide[1], dY, d_out, T, lddy, 64, kGK) && make_map(&fold.narrow[1], H, R, T, R, 64, kGK);
+      make_map(&fold.wide[0], X, d_in, T, ldx, 64, kGK) && make_map(&fold.narrow[0], G, p.gated_ld, T, p.gated_ld, 64, kGK) &&
+      make_map(&fold.wide[1], dY, d_out, T, lddy, 64, kGK) && make_map(&fold.narrow[1], H, p.gated_ld, T, p.gated_ld, 64, kGK);
   if (!maps_ok) return CWL_ERR_CUDA;
 
-  auto fill = [&](int tiles0, int tiles1, int kb0, int kb1) {
+  auto fill = [&](int columns, int tiles0, int tiles1, int kb0, int kb1) {
     p.n_tiles[0] = tiles0; p.n_tiles[1] = tiles1;
     p.n_kb[0] = kb0; p.n_kb[1] = kb1;
     p.first = kb1 > kb0 ? 1 : 0;                         // the longer loops start first
-    const GradLaunch l = grad_launch(R, tiles0 + tiles1, kb0 < kb1 ? kb0 : kb1);
+    const GradLaunch l = grad_launch(R, columns, tiles0 + tiles1, kb0 < kb1 ? kb0 : kb1);
     p.split = l.split; p.stages = l.stages; p.stage_bytes = l.stage_bytes; p.narrow_bytes = l.narrow_bytes;
     p.tmem_cols = l.tmem_cols; p.ring_bytes = l.ring_bytes; p.meet_in_ring = l.meet_in_ring; p.meet_off = l.meet_off;
     return l;
   };
   const int row_tiles = ceil_div(T, kGM), t_blocks = ceil_div(T, kGK);
-  GradLaunch l = fill(row_tiles, row_tiles, ceil_div(d_in, kGK), ceil_div(d_out, kGK));
+  GradLaunch l = fill(R, row_tiles, row_tiles, ceil_div(d_in, kGK), ceil_div(d_out, kGK));
   CWL_CUDA_TRY(launch_phase<PHASE_SHRINK>(shrink, p, l, st));
-  l = fill(ceil_div(d_in, kGM), ceil_div(d_out, kGM), t_blocks, t_blocks);
+  l = fill(p.gated_ld, ceil_div(d_in, kGM), ceil_div(d_out, kGM), t_blocks, t_blocks);
   CWL_CUDA_TRY(launch_phase<PHASE_FOLD>(fold, p, l, st));
   return CWL_OK;
 }

@@ -94,6 +94,22 @@ def test_sizes(T, d_in, d_out, R, chunk, window):
     check(X, dY, A, B, tab, window, grad_dtype=torch.float32)
 
 
+@pytest.mark.parametrize("T,d_in,d_out,R", [(300, 512, 320, 64), (777, 256, 1040, 144), (129, 1024, 640, 16), (2000, 272, 512, 256)])
+def test_fp32_gradients_carry_more_than_bf16(T, d_in, d_out, R):
+    """H' and G are kept as two bf16 numbers: what they lose is 2^-17 of a number (half of the low one's spacing), so an fp32
+    gradient is within 2^-16 of the magnitudes that it sums, beside the fp32 sums themselves."""
+    X, dY, A, B = operands(T, T, d_in, d_out, R)
+    tab = table(T, T, R, 40)
+    dA, dB = cwl.cwl_apply_grads(X, dY, A, B, dev_table(tab), 4, grad_dtype=torch.float32)
+    g = torch.from_numpy(gate_of(tab, T, R, 4)).cuda()
+    x, dy, a, b = (t.double() for t in (X, dY, A, B))
+    H, G = g * (x @ a), g * (dy @ b.T)
+    u = 2.0 ** -23
+    for got, ref, tol in ((dA, x.T @ G, x.abs().T @ (G.abs() * (2.0 ** -16 + T * u) + g * d_out * u * (dy.abs() @ b.abs().T))),
+                          (dB, H.T @ dy, (H.abs() * (2.0 ** -16 + T * u) + g * d_in * u * (x.abs() @ a.abs())).T @ dy.abs())):
+        assert float(((got.double() - ref).abs() - tol - ref.abs() * 2.0 ** -23).max()) <= 0
+
+
 @pytest.mark.parametrize("window", [0, 1, 7, 8])
 def test_centred_windows(window):
     X, dY, A, B = operands(3, 400, 256, 320, 64)
