@@ -8,8 +8,9 @@
 // become -inf) before the sums run: what is summed is then the mass outside the entries itself, not a difference of two
 // nearly equal sums, and the elementwise gradient leaves those places 0 for the entries' own values.
 //
-// Two kernels.  Rows of up to kSmallRowBytes: one block of 128 threads a row, many blocks to an SM, which overlap one
-// another's phases.  Longer rows, and few rows: one persistent block an SM that pipelines rows through up to three
+// Three kernels.  The loss alone of many rows: a stream over them.  Short rows: one block of 128 threads a row, many
+// blocks to an SM, which overlap
+// one another's phases.  Longer rows, and few rows: one persistent block an SM that pipelines rows through up to three
 // buffers, alone or in a cluster of up to eight blocks that hold a contiguous slice of each row and exchange (m, S)
 // through distributed shared memory.
 #include <atomic>
@@ -24,7 +25,11 @@ namespace {
 constexpr int kDsThreads = 128;           // of the kernel for short rows; at least CWL_MAX_TOP_K
 constexpr int kDsWarps = kDsThreads / 32;
 constexpr int kMaxDsCluster = 8;
+// Rows for one small block each: up to 16 KB always, up to 44 KB when there are four blocks an SM of them (16384 rows of
+// 32 KB: 181 us against 247 us of the pipelined kernel; 48 KB: 279 against 286; 400 rows of 32 KB: 13 against 12).
 constexpr int kSmallRowBytes = 16 * 1024;
+constexpr int kSmallManyRowBytes = 44 * 1024;
+constexpr int kSmallManyRows = 592;
 
 struct DistillParams {
   const void* logits; int64_t ld; int T, V;
@@ -309,6 +314,151 @@ distill_small_kernel(const DistillParams p) {
       if (en.p_id >= 0.f) d[en.id] = Elem<T>::from_float(entry_gradient(p, en.z, en.p_id, en.p_in + en.p_rest, m, s_row) * up);
     }
     __syncthreads();                               // the next row overwrites the shared arrays
+  }
+}
+
+// --------------------------------------------------------------------------------------------- the loss alone, many rows
+// Nothing has to stay for a gradient: rows stream through registers as in logprobs.cu, one block of 128 threads a row,
+// seven blocks an SM.  A bit per element in shared memory marks the entries; a vector that holds one (64 of 4000, say) has
+// it replaced by -inf before it is summed, so that the mass outside the entries is again a sum of its own.
+constexpr int kLossThreads = 128;
+constexpr int kLossWarps = kLossThreads / 32;
+constexpr int kLossBatch = 4;
+constexpr int kLossMinRows = 740;              // five blocks an SM; with fewer the pipelined kernel, which cuts rows up, is faster
+                                               // (256 KB rows: 23 us against 50 us at 200 rows, 76 against 52 us at 1000)
+
+struct LossShared {
+  double red_d[kLossWarps];
+  float red[kLossWarps];
+  float2 part[kLossWarps];                     // (m, S) of every warp's elements outside the entries
+  float m_in[kLossWarps], s_in[kLossWarps];    // and of its entries
+};
+
+template <typename T>
+__device__ __noinline__ RowStat exact_masked_stat(const uint4* v, const uint32_t* marks, int first, int stride, int n, float c) {
+  constexpr int kVec = Elem<T>::kVec;
+  RowStat a{-CUDART_INF_F, 0.f, 0.f};
+  for (int i = first; i < n; i += stride) {
+    uint4 q = v[i];
+    const int pos = (i + 1) * kVec;
+    Elem<T>::mask_out(q, (marks[pos >> 5] >> (pos & 31)) & ((1u << kVec) - 1u));
+    float f[kVec];
+    Elem<T>::unpack(q, f);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) absorb_scalar(a, f[e], c);
+  }
+  return a;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kLossThreads, 7)
+distill_loss_kernel(const DistillParams p, const int mark_words) {
+  constexpr int kVec = Elem<T>::kVec;
+  pdl_launch_dependents();
+  extern __shared__ __align__(128) uint8_t ds_raw[];
+  LossShared& sh = *reinterpret_cast<LossShared*>(ds_raw);
+  uint32_t* marks = reinterpret_cast<uint32_t*>(ds_raw + sizeof(LossShared));   // element i of a row: bit i - head + kVec
+  const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+  for (int i = tid; i < mark_words; i += kLossThreads) marks[i] = 0;
+  pdl_wait();
+  __syncthreads();
+
+  for (int row = blockIdx.x; row < p.T; row += gridDim.x) {
+    const float w = p.weight != nullptr ? __ldg(p.weight + row) : 1.f;
+    if (w == 0.f) {
+      if (tid == 0) p.loss[row] = 0.f;
+      continue;
+    }
+    const T* z = reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.ld;
+    const RowSlice rs = row_slice<T>(z, p.V, 0, 0);
+    Entry en;
+    load_entry(p, row, tid, en);
+    check_entry(p, en);
+    bool counts = false;                       // first to mark its id
+    const int pos = en.id - rs.head + kVec;
+    if (en.id >= 0) {
+      en.z = Elem<T>::load(z + en.id);
+      const uint32_t bit = 1u << (pos & 31);
+      counts = (atomicOr(marks + (pos >> 5), bit) & bit) == 0;
+    }
+    __syncthreads();                           // all marks are set
+
+    RunningSum run;
+    run.start(p.ordinary != 0);
+    const int nv = rs.v1;
+    const uint4* src = reinterpret_cast<const uint4*>(z + rs.head) + tid;
+    const uint4 pad = make_uint4(Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked());
+    auto load = [&](int first, uint4 (&q)[kLossBatch]) {
+#pragma unroll
+      for (int u = 0; u < kLossBatch; ++u) q[u] = first + u * kLossThreads < nv ? __ldg(src + (first - tid) + u * kLossThreads) : pad;
+    };
+    auto process = [&](int first, uint4 (&q)[kLossBatch]) {
+      uint32_t words[4 * kLossBatch];
+#pragma unroll
+      for (int u = 0; u < kLossBatch; ++u) {
+        const int v = min(first + u * kLossThreads, nv - 1);
+        const int at = (v + 1) * kVec;
+        const uint32_t bits = (marks[at >> 5] >> (at & 31)) & ((1u << kVec) - 1u);
+        if (bits != 0) Elem<T>::mask_out(q[u], bits);
+        words[4 * u] = q[u].x; words[4 * u + 1] = q[u].y; words[4 * u + 2] = q[u].z; words[4 * u + 3] = q[u].w;
+      }
+      run.template take_words<T, 4 * kLossBatch>(words, Elem<T>::max_of(words), p.c);
+    };
+    constexpr int kStep = kLossBatch * kLossThreads;
+    for (int i = tid; i - tid < nv; i += 2 * kStep) {
+      uint4 q[kLossBatch], r[kLossBatch];
+      load(i, q);
+      const bool two = i - tid + kStep < nv;
+      if (two) load(i + kStep, r);
+      process(i, q);
+      if (two) process(i + kStep, r);
+    }
+    RowStat a = run.done(p.c);
+    if (run.exact_needed) a = exact_masked_stat<T>(src - tid, marks, tid, kLossThreads, nv, p.c);
+#pragma unroll 1
+    for (int k = 0; k < 2; ++k) {              // scalars before the first vector and after the last
+      const int i = k == 0 ? tid : rs.tail_start + tid;
+      if (tid < (k == 0 ? rs.own_head : rs.own_tail)) {
+        const int at = i - rs.head + kVec;
+        if (((marks[at >> 5] >> (at & 31)) & 1u) == 0) absorb_scalar(a, Elem<T>::load(z + i), p.c);
+      }
+    }
+    rescale(a, key_value(__reduce_max_sync(0xffffffffu, order_key(a.m))), p.c);
+    a.S = warp_sum(a.S);
+    if (lane == 0) sh.part[wid] = make_float2(a.m, a.S);
+
+    // the teacher's side
+    float v_max = 0.f;
+    if (p.mode == CWL_TEACHER_LOGITS) {
+      const float mx = warp_max_nan(en.id >= 0 ? en.value : -CUDART_INF_F);
+      if (lane == 0) sh.red[wid] = mx;
+      __syncthreads();
+      v_max = max_nan(max_nan(sh.red[0], sh.red[1]), max_nan(sh.red[2], sh.red[3]));
+    }
+    const double weight = warp_sum(entry_weight(p, v_max, en));
+    const float mw = key_value(__reduce_max_sync(0xffffffffu, order_key(counts ? en.z : -CUDART_INF_F)));
+    const float sw = warp_sum(counts && !bad_max(mw) ? exp2_fast((en.z - mw) * p.c) : 0.f);
+    if (lane == 0) { sh.red_d[wid] = weight; sh.m_in[wid] = mw; sh.s_in[wid] = sw; }
+    __syncthreads();                           // every thread is done with the marks
+    if (en.id >= 0) marks[pos >> 5] = 0;
+    finish_entry(p, v_max, (sh.red_d[0] + sh.red_d[1]) + (sh.red_d[2] + sh.red_d[3]), en);
+    // all parts together: lanes 0..3 outside the entries, 4..7 the entries
+    const int k = lane & (2 * kLossWarps - 1);
+    RowStat part{k < kLossWarps ? sh.part[k].x : sh.m_in[k - kLossWarps], k < kLossWarps ? sh.part[k].y : sh.s_in[k - kLossWarps], 0.f};
+    float m = key_value(__reduce_max_sync(0xffffffffu, order_key(part.m)));
+    rescale(part, m, p.c);
+    const float rest = warp_sum(lane < kLossWarps ? part.S : 0.f);
+    float s = rest, s_row = rest + warp_sum(lane >= kLossWarps && lane < 2 * kLossWarps ? part.S : 0.f);
+    if (bad_max(m)) { m = 0.f; s = CUDART_NAN_F; s_row = CUDART_NAN_F; }
+    const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_rest, m, s, s_row, tid));
+    __syncthreads();                           // red_d was read
+    if (lane == 0) sh.red_d[wid] = term;
+    __syncthreads();
+    if (tid == 0) {
+      const double kl = (sh.red_d[0] + sh.red_d[1]) + (sh.red_d[2] + sh.red_d[3]);
+      p.loss[row] = (float)((double)w * p.temperature * p.temperature * kl);
+    }
+    __syncthreads();
   }
 }
 
@@ -793,10 +943,19 @@ template <typename T>
 cudaError_t launch_distill(const DistillParams& p, cudaStream_t st) {
   const int64_t row_bytes = (int64_t)p.V * sizeof(T);
   const bool chained = !stream_is_capturing(st);
-  if (row_bytes <= kSmallRowBytes) {
+  if (row_bytes <= kSmallRowBytes || (row_bytes <= kSmallManyRowBytes && p.T >= kSmallManyRows && p.dlogits != nullptr)) {
     const size_t smem = (size_t)(row_bytes / 16) * 16 + 32;
     const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
     return launch_clusters(chained, 1, distill_small_kernel<T>, dim3(rows), dim3(kDsThreads), smem, st, p);
+  }
+  if (p.dlogits == nullptr && p.T >= kLossMinRows) {
+    const int words = (p.V + 2 * Elem<T>::kVec + 31) / 32;
+    static SharedMemoryGrant loss_grant;
+    const cudaError_t e = loss_grant(distill_loss_kernel<T>);
+    if (e != cudaSuccess) return e;
+    const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
+    return launch_clusters(chained, 1, distill_loss_kernel<T>, dim3(rows), dim3(kLossThreads), sizeof(LossShared) + words * sizeof(uint32_t),
+                           st, p, words);
   }
   const PipePlan plan = pipe_plan(p.T, row_bytes);
   const size_t smem = (size_t)plan.n_buffers * plan.buffer_bytes + sizeof(DsPipe);

@@ -71,6 +71,13 @@ template <> struct Elem<float> {
     return f;
   }
   static __device__ __forceinline__ uint32_t masked() { return 0xFF800000u; }   // -inf
+  // the elements of a vector whose bits are set become -inf
+  static __device__ __forceinline__ void mask_out(uint4& q, uint32_t bits) {
+    if (bits & 1u) q.x = 0xFF800000u;
+    if (bits & 2u) q.y = 0xFF800000u;
+    if (bits & 4u) q.z = 0xFF800000u;
+    if (bits & 8u) q.w = 0xFF800000u;
+  }
   // maximum of the elements of n words, NaN wins
   template <int n> static __device__ __forceinline__ float max_of(const uint32_t (&w)[n]) {
     float m = __uint_as_float(w[0]);
@@ -116,6 +123,14 @@ template <> struct Elem<__nv_bfloat16> {
     return f;
   }
   static __device__ __forceinline__ uint32_t masked() { return 0xFF80FF80u; }
+  static __device__ __forceinline__ void mask_out(uint4& q, uint32_t bits) {
+    auto word = [](uint32_t w, uint32_t two) {
+      if (two & 1u) w = (w & 0xFFFF0000u) | 0xFF80u;
+      if (two & 2u) w = (w & 0x0000FFFFu) | (0xFF80u << 16);
+      return w;
+    };
+    q.x = word(q.x, bits); q.y = word(q.y, bits >> 2); q.z = word(q.z, bits >> 4); q.w = word(q.w, bits >> 6);
+  }
   template <int n> static __device__ __forceinline__ float max_of(const uint32_t (&w)[n]) {
     uint32_t m = w[0];
 #pragma unroll
@@ -163,6 +178,14 @@ template <> struct Elem<__half> {
     return f;
   }
   static __device__ __forceinline__ uint32_t masked() { return 0xFC00FC00u; }
+  static __device__ __forceinline__ void mask_out(uint4& q, uint32_t bits) {
+    auto word = [](uint32_t w, uint32_t two) {
+      if (two & 1u) w = (w & 0xFFFF0000u) | 0xFC00u;
+      if (two & 2u) w = (w & 0x0000FFFFu) | (0xFC00u << 16);
+      return w;
+    };
+    q.x = word(q.x, bits); q.y = word(q.y, bits >> 2); q.z = word(q.z, bits >> 4); q.w = word(q.w, bits >> 6);
+  }
   template <int n> static __device__ __forceinline__ float max_of(const uint32_t (&w)[n]) {
     uint32_t m = w[0];
 #pragma unroll

@@ -92,18 +92,18 @@ def device(z, dtype, pad=0, offset=0):
     return v
 
 
-def check(zt, ids, vals, mode, tau=1.0, w=None, dloss=None, dtype="f32", dlogits=None, status=None):
+def check(zt, ids, vals, mode, tau=1.0, w=None, dloss=None, dtype="f32", dlogits=None, status=None, grad_too=True):
     T, V = zt.shape
     dev = lambda a: None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()   # noqa: E731
     z64 = zt.double().cpu().numpy()
     loss, grad = cwl.cwl_distill_topk(zt, dev(ids), dev(vals), teacher=mode, temperature=tau, weight=dev(w), dloss=dev(dloss),
-                                      dlogits=dlogits, status_word=status)
+                                      dlogits=dlogits, status_word=status, want_grad=grad_too)
     tau64 = float(np.float32(tau))
     w64 = np.ones(T) if w is None else w.astype(np.float64)
     d64 = np.ones(T) if dloss is None else dloss.astype(np.float64)
     ids_ok = np.where(ids >= V, -1, ids)
     rl, rg, info = definition(z64, ids_ok, vals.astype(np.float64), mode, tau64, w64, d64)
-    gl, gg = loss.double().cpu().numpy(), grad.double().cpu().numpy()
+    gl, gg = loss.double().cpu().numpy(), grad.double().cpu().numpy() if grad_too else rg
     eps = U * (4 + 3 * np.log2(V + 1) + V / 256 + 40)
     assert np.array_equal(np.isnan(gl), np.isnan(rl)) and np.array_equal(np.isinf(gl), np.isinf(rl))
     assert np.array_equal(np.isnan(gg), np.isnan(rg))
@@ -159,6 +159,15 @@ def test_sizes_and_types(dtype, mode, T, V, K, tau, pad):
     check(zt, ids, vals, mode, tau, w, rng.uniform(-1.5, 1.5, T).astype(np.float32), dtype)
 
 
+@pytest.mark.parametrize("T,V,dtype", [(592, 20003, "bf16"), (600, 11000, "f32"), (591, 20003, "bf16"), (640, 22528, "f16"), (592, 22529, "bf16")])
+def test_rows_on_both_sides_of_the_small_blocks(T, V, dtype):
+    zt = device(rows(V, T, V), dtype, 1)
+    ids, vals = teacher_of(zt.double().cpu().numpy(), 33, "logprobs", 1.0, V)
+    w = np.ones(T, np.float32)
+    w[::7] = 0.0
+    check(zt, ids, vals, "logprobs", 1.0, w, None, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("offset,out_offset", [(1, 1), (3, 0), (0, 5), (6, 7)])
 def test_rows_that_start_anywhere(dtype, offset, out_offset):
@@ -170,6 +179,43 @@ def test_rows_that_start_anywhere(dtype, offset, out_offset):
         check(zt, ids, vals, "logprobs", dtype=dtype, dlogits=guard[:T, out_offset:out_offset + V])
         assert bool(torch.isnan(guard[T]).all()) and bool(torch.isnan(guard[:, :out_offset]).all())
         assert bool(torch.isnan(guard[:, out_offset + V:]).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("mode", ["logits", "logprobs"])
+@pytest.mark.parametrize("T,V,K,tau,pad", [(740, 16411, 128, 1.0, 0), (760, 9001, 20, 2.0, 3), (800, 8200, 1, 0.7, 1), (741, 50021, 64, 1.0, 0)])
+def test_the_loss_alone_of_many_rows(dtype, mode, T, V, K, tau, pad):
+    zt = device(rows(T + V, T, V), dtype, pad)
+    ids, vals = teacher_of(zt.double().cpu().numpy(), K, mode, tau, V)
+    w = np.random.default_rng(T).uniform(0.5, 2.0, T).astype(np.float32)
+    w[1::4] = 0.0
+    check(zt, ids, vals, mode, tau, w, None, dtype, grad_too=False)
+
+
+def test_the_loss_alone_of_special_rows():
+    T, V, K = 745, 12007, 10
+    z = rows(4, T, V)
+    ids, vals = teacher_of(z.astype(np.float64), K, "logprobs", 1.0, 9, short=False)
+    z[0, 100], z[1, 200], z[2, :] = np.nan, np.inf, -np.inf
+    z[3, ~np.isin(np.arange(V), ids[3])] = -np.inf
+    z[4, ids[4, 0]] = -np.inf
+    ids[5] = -1
+    z[6, :] = np.finfo(np.float32).min
+    z[7, ~np.isin(np.arange(V), ids[7])] = np.finfo(np.float32).min
+    z[8, :] += 50000.0                                     # far from 0: the exact form of the exponent
+    ids[9, 1:] = ids[9, 0]
+    z[10, ids[10, 2]] = np.nan
+    zt = device(z, "f32")
+    dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()   # noqa: E731
+    for mode in ("logits", "logprobs"):
+        alone, _ = cwl.cwl_distill_topk(zt, dev(ids), dev(vals), teacher=mode, want_grad=False)
+        both, _ = cwl.cwl_distill_topk(zt, dev(ids), dev(vals), teacher=mode)
+        rl, _, _ = definition(zt.double().cpu().numpy(), ids, vals.astype(np.float64), mode, 1.0, np.ones(T), np.ones(T))
+        for got in (alone, both):
+            g = got.double().cpu().numpy()
+            assert np.array_equal(np.isnan(g), np.isnan(rl)) and np.array_equal(np.isinf(g), np.isinf(rl))
+            fine = np.isfinite(rl)
+            assert np.allclose(g[fine], rl[fine], rtol=2e-4, atol=2e-4)
 
 
 def test_wide_rows_take_a_cluster():
