@@ -116,6 +116,63 @@ __device__ __forceinline__ uint32_t cell_bound(const uint32_t* half, int want) {
   return prefix >= (kKeyOfMinusInf & ~0xFFFFu) && prefix < kKeyOfMinusInf ? kKeyOfMinusInf : prefix;
 }
 
+// The digit whose bin of sh.hist holds the rest-th element from the top, into sh.thr, and its rank inside the bin, into
+// sh.rest.  One warp: eight bins a lane, the highest in lane 0.
+__device__ __forceinline__ void digit_of_rank(LpShared& sh, int rest) {
+  const int lane = threadIdx.x & 31, top = 255 - 8 * lane;
+  int mine = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) mine += sh.hist[top - i];
+  int upto = mine;                                       // elements in this lane's bins and all above
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    const int o = __shfl_up_sync(0xffffffffu, upto, off);
+    if (lane >= off) upto += o;
+  }
+  const int owner = __ffs((int)__ballot_sync(0xffffffffu, upto >= rest)) - 1;
+  if (lane == owner) {
+    int left = rest - (upto - mine), d = top;
+    while (d > top - 7 && (int)sh.hist[d] < left) { left -= sh.hist[d]; --d; }
+    sh.thr = (uint32_t)d;
+    sh.rest = left;
+  }
+}
+
+// Many candidates (short rows of which a good part is wanted): only those from the want-th largest on stay, ties with it
+// included, before the sort, whose work is quadratic.
+constexpr int kSortable = 256;
+__device__ __noinline__ int tighten_candidates(LpShared& sh, int n, int want) {
+  const int tid = threadIdx.x;
+  constexpr int kEach = (kMaxCand + kLpThreads - 1) / kLpThreads;
+  unsigned long long mine[kEach];
+#pragma unroll
+  for (int j = 0; j < kEach; ++j) mine[j] = tid + j * kLpThreads < n ? sh.cand[tid + j * kLpThreads] : 0ull;   // no element has key 0
+  uint32_t prefix = 0, mask = 0;
+  int rest = want;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    for (int i = tid; i < 256; i += kLpThreads) sh.hist[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kEach; ++j) {
+      const uint32_t key = (uint32_t)(mine[j] >> 32);
+      if (mine[j] != 0 && (key & mask) == prefix) atomicAdd(&sh.hist[(key >> shift) & 255u], 1u);
+    }
+    __syncthreads();
+    if (tid < 32) digit_of_rank(sh, rest);
+    __syncthreads();
+    prefix |= sh.thr << shift;
+    mask |= 255u << shift;
+    rest = sh.rest;
+    if (tid == 0) sh.n_cand = 0;
+    __syncthreads();
+  }
+#pragma unroll
+  for (int j = 0; j < kEach; ++j)
+    if ((uint32_t)(mine[j] >> 32) >= prefix) sh.cand[atomicAdd(&sh.n_cand, 1)] = mine[j];
+  __syncthreads();
+  return sh.n_cand;
+}
+
 // Rows built so that few cells hold everything large: the want-th largest key exactly, eight bits at a time, then the
 // candidates above it and the ties with it.
 template <typename T>
@@ -131,12 +188,7 @@ __device__ __noinline__ uint32_t exact_bound_and_candidates(LpShared& sh, const 
       if ((key & mask) == prefix) atomicAdd(&sh.hist[(key >> shift) & 255u], 1u);
     }
     __syncthreads();
-    if (tid == 0) {
-      int d = 255;
-      while (d > 0 && (int)sh.hist[d] < rest) { rest -= sh.hist[d]; --d; }
-      sh.thr = (uint32_t)d;
-      sh.rest = rest;
-    }
+    if (tid < 32) digit_of_rank(sh, rest);
     __syncthreads();
     prefix |= sh.thr << shift;
     mask |= 255u << shift;
@@ -266,6 +318,7 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
     }
     __syncthreads();
   }
+  if (n_cand > kSortable) n_cand = tighten_candidates(sh, n_cand, want);
   if ((n_cand & 1) != 0) {                               // the sort reads pairs
     if (tid == 0) sh.cand[n_cand] = 0ull;
     __syncthreads();
