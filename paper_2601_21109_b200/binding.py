@@ -119,12 +119,15 @@ def test_hooks():
         _hooks_lib = _declare(C.CDLL(HOOKS_LIB_PATH))
         _hooks_lib.cwl_debug_set.restype = None
         _hooks_lib.cwl_debug_set.argtypes = [C.c_int64, C.c_int32]
+        _hooks_lib.cwl_debug_training_set.restype = None
+        _hooks_lib.cwl_debug_training_set.argtypes = [C.c_int64, C.c_int32]
     saved = lib()
     _lib = _hooks_lib
     try:
         yield _hooks_lib
     finally:
         _hooks_lib.cwl_debug_set(0, 0)
+        _hooks_lib.cwl_debug_training_set(0, 0)
         _lib = saved
 
 
@@ -569,6 +572,14 @@ def cwl_debug_set(wait_limit_ns: int = 0, withhold_publish: bool = False) -> Non
     if _lib is not _hooks_lib or _hooks_lib is None:
         raise RuntimeError("cwl_debug_set exists in the test build only: call it inside `with binding.test_hooks():`")
     _hooks_lib.cwl_debug_set(int(wait_limit_ns), 1 if withhold_publish else 0)
+
+
+def cwl_debug_training_set(wait_limit_ns: int = 0, withhold: bool = False) -> None:
+    """Test hook, inside ``with test_hooks():`` only: wait limit of the distillation and gradient kernels, and whether they
+    leave out a copy that they wait for (timeout path)."""
+    if _lib is not _hooks_lib or _hooks_lib is None:
+        raise RuntimeError("cwl_debug_training_set exists in the test build only: call it inside `with binding.test_hooks():`")
+    _hooks_lib.cwl_debug_training_set(int(wait_limit_ns), 1 if withhold else 0)
 
 
 def cwl_apply_noalloc(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor], B: Optional[torch.Tensor],

@@ -12,6 +12,7 @@ LIB = os.path.join(HERE, "libcwl.so")
 LIB_HOOKS = os.path.join(HERE, "libcwl_hooks.so")
 SOURCES = ["api.cu", "score.cu", "partition.cu", "align.cu", "stream.cu", "ladder.cu", "apply.cu", "logprobs.cu", "distill.cu",
            "grads.cu"]
+HOOKED = ["apply.cu", "distill.cu", "grads.cu"]     # sources whose test build differs
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v", "--expt-relaxed-constexpr"]
 
@@ -22,8 +23,9 @@ def _newest_source() -> float:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Builds libcwl.so and, from the same sources plus -DCWL_TEST_HOOKS for apply.cu, the test build
-    libcwl_hooks.so (it adds cwl_debug_set, which shortens the device-side wait limit and withholds H')."""
+    """Builds libcwl.so and, from the same sources plus -DCWL_TEST_HOOKS for HOOKED, the test build
+    libcwl_hooks.so (it adds cwl_debug_set and cwl_debug_training_set, which shorten the device-side wait limits and
+    withhold what is waited for)."""
     if not force and os.path.exists(LIB) and os.path.exists(LIB_HOOKS) and \
             min(os.path.getmtime(LIB), os.path.getmtime(LIB_HOOKS)) >= _newest_source():
         return LIB
@@ -31,7 +33,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     extra = os.environ.get("CWL_NVCC_EXTRA", "").split()   # e.g. -DCWL_STAGES=5 for tuning experiments
     os.makedirs(os.path.join(HERE, "_build"), exist_ok=True)
     jobs = [(src, src.replace(".cu", ".o"), []) for src in SOURCES] + \
-        [("apply.cu", "apply_hooks.o", ["-DCWL_TEST_HOOKS"]), ("probe.cu", "probe_hooks.o", ["-DCWL_TEST_HOOKS"])]
+        [(src, src.replace(".cu", "_hooks.o"), ["-DCWL_TEST_HOOKS"]) for src in HOOKED + ["probe.cu"]]
     procs = []
     for src, obj, defs in jobs:
         cmd = [nvcc, *NVCC_FLAGS, *extra, *defs, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c",
@@ -45,7 +47,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
             sys.stderr.write("\n".join(log))
             raise RuntimeError(f"nvcc failed on {obj}")
     plain = [os.path.join(HERE, "_build", s.replace(".cu", ".o")) for s in SOURCES]
-    hooks = [o if not o.endswith("/apply.o") else o.replace("apply.o", "apply_hooks.o") for o in plain] + \
+    hooks = [o.replace(".o", "_hooks.o") if s in HOOKED else o for s, o in zip(SOURCES, plain)] + \
         [os.path.join(HERE, "_build", "probe_hooks.o")]
     for lib, objs in ((LIB, plain), (LIB_HOOKS, hooks)):
         tmp = lib + f".tmp{os.getpid()}"

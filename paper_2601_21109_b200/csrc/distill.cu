@@ -42,6 +42,8 @@ struct DistillParams {
   float* loss;
   void* dlogits; int64_t ld_d;
   int32_t* status_word;
+  unsigned long long wait_limit_ns;
+  int withhold;               // test build: the slice of row number 1 is never copied
 };
 
 struct DsShared {
@@ -474,7 +476,6 @@ constexpr int kClusterSlots = 6;               // rows under way between the blo
 constexpr int kParts = kSumWarps + 1;          // parts of a slice's statistics: its sum warps', its entries'
 constexpr int kAtOnce = 4;                       // vectors of a sum thread in the works at once
 constexpr int kCopyBytes = 16 * 1024;          // piece of a slice that one bulk copy brings
-constexpr unsigned long long kDsWaitLimitNs = 2000000000ull;
 
 struct DsPipe {
   alignas(8) unsigned long long full[kMaxBuffers], ready[kMaxBuffers], xchg[kClusterSlots];
@@ -614,7 +615,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
     for (int b = 0; b < kMaxBuffers; ++b) { mbar_init(full_bar(b), 1); mbar_init(ready_bar(b), 1); }
     for (int k = 0; k < kClusterSlots; ++k) mbar_init(xchg_bar(k), 1);
     sh.misc[1] = 0;
-    *reinterpret_cast<volatile unsigned long long*>(sh.misc + 4) = kDsWaitLimitNs;
+    *reinterpret_cast<volatile unsigned long long*>(sh.misc + 4) = p.wait_limit_ns;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
@@ -742,11 +743,14 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
     RowCursor loads;
     loads.start(p.weight, p.T, first, stride);
     int loaded = 0;
+    uint32_t copied = 0, odd = 0;                            // buffers that were filled at all; filled an odd number of times
     Ring buf, past;                                          // `past`: slot of the row whose buffer comes free next
     float w;
     while (loads.next(w)) {
       if (loaded >= plan.n_buffers) { stored_wait(past.at); past.step(kSlots); }
-      if (lane == 0) {
+      if (lane == 0 && !(CWL_WITHHELD(p) && loaded == 1)) {
+        copied |= 1u << buf.at;
+        odd ^= 1u << buf.at;
         asm volatile("fence.proxy.async;" ::: "memory");   // the buffer was read and written with ordinary accesses
         const T* z = row_of(loads.row);
         const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
@@ -762,6 +766,13 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       ++loaded;
     }
     for (int n = min(loaded, plan.n_buffers); n > 0; --n) { stored_wait(past.at); past.step(kSlots); }   // every row counts this warp
+    // Where a wait ran out, copies may still be on their way: they get a bounded chance to land.
+    for (int b = 0; b < kMaxBuffers; ++b) {
+      if (lane != 0 || ((copied >> b) & 1u) == 0) continue;
+      const unsigned long long t0 = global_timer();
+      while (!mbar_try_wait(full_bar(b), ((odd >> b) & 1u) ^ 1u) && global_timer() - t0 < p.wait_limit_ns) {}
+    }
+    __syncwarp();
   } else {
     // -------------------------------------------------------------------------------------------------- sum warps
     const int group = (tid - 2 * kEntryThreads) / kSumThreads;
@@ -894,7 +905,13 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
   }
   __syncthreads();
   if (tid == 0 && *abort_flag != 0) flag_status(p.status_word, CWL_ERR_TIMEOUT);
-  if (log2_cta > 0) cluster_barrier();             // nobody leaves while a peer may still write to it
+  if (log2_cta > 0) {
+    cluster_barrier();                             // nobody leaves while a peer may still write to it
+    if (*abort_flag != 0) {                        // a block that gave up has not waited for all that is sent to it
+      const unsigned long long t0 = global_timer();
+      while (global_timer() - t0 < 1000000ull) {}
+    }
+  }
 }
 
 static_assert(sizeof(DsPipe) + CWL_MAX_DISTILL_ROW_BYTES / kMaxDsCluster + 160 <= 227 * 1024, "the longest row fits a cluster");
@@ -989,7 +1006,7 @@ extern "C" cwl_status cwl_distill_topk(const void* logits, cwl_dtype dtype, int6
   if (dlogits == logits && ld_dlogits != ld_logits) return CWL_ERR_SHAPE;
   cwl::DistillParams p{logits, ld_logits, T, V, teacher_ids, teacher_values, ld_teacher, K, (int)mode, temperature,
                        (float)(1.4426950408889634074 / (double)temperature), (float)(1.0 / (double)temperature), 1.0 / (double)temperature, cwl::ordinary_temperature(temperature) ? 1 : 0, weight, dloss,
-                       loss, dlogits, ld_dlogits, status_word};
+                       loss, dlogits, ld_dlogits, status_word, cwl::training_wait_limit(), cwl::training_withhold()};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   switch (dtype) {
     case CWL_F32: CWL_CUDA_TRY(cwl::launch_distill<float>(p, st)); break;
@@ -998,3 +1015,14 @@ extern "C" cwl_status cwl_distill_topk(const void* logits, cwl_dtype dtype, int6
   }
   return CWL_OK;
 }
+
+#ifdef CWL_TEST_HOOKS
+namespace cwl {
+std::atomic<unsigned long long> g_training_wait_limit_ns{kTrainingWaitLimitNs};
+std::atomic<int> g_training_withhold{0};
+}  // namespace cwl
+extern "C" void cwl_debug_training_set(int64_t wait_limit_ns, int32_t withhold) {
+  cwl::g_training_wait_limit_ns.store(wait_limit_ns > 0 ? (unsigned long long)wait_limit_ns : cwl::kTrainingWaitLimitNs);
+  cwl::g_training_withhold.store(withhold != 0 ? 1 : 0);
+}
+#endif

@@ -16,7 +16,8 @@
 // Roles per CTA: warp 0 = TMA producer, warp 1 = tcgen05.mma issuer and owner of the tensor memory, warps 2..5 move the
 // accumulator to shared memory; all warps reduce and store.  SHRINK reads the rows of X / dY K-major; A is N-major and
 // B K-major, as they lie in memory.  FOLD reads X / dY M-major (their columns are the output rows) and G / H' N-major.
-// Every wait is bounded: when one runs out the CTA raises CWL_ERR_TIMEOUT, stores nothing and still meets its cluster.
+// Every wait is bounded: when one runs out the CTA raises CWL_ERR_TIMEOUT, stores nothing and still meets its cluster (whose
+// other CTAs may store what lacks its part).
 #include "cwl_common.cuh"
 #include "gate.cuh"
 #include "tcgen05_common.cuh"
@@ -31,7 +32,6 @@ constexpr int kGLeftBytes = kGM * kGK * 2;      // 16 KB of the wide operand per
 constexpr int kGBoxBytes = 64 * kGK * 2;        // one 64-column box
 constexpr int kGMaxStages = 8;
 constexpr int kGMaxCluster = 8;
-constexpr unsigned long long kGWaitLimitNs = 2000000000ull;
 
 enum : int { PHASE_SHRINK = 0, PHASE_FOLD = 1 };
 
@@ -53,6 +53,7 @@ struct GradParams {
   void* out[2]; int64_t ld[2]; // FOLD: dA, dB
   int out_f32;
   unsigned long long wait_limit_ns;
+  int withhold;                // test build: SHRINK's last K block is never loaded
   int32_t* status_word;
 };
 
@@ -196,6 +197,7 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
   }
 
   const bool narrow_k_major = kPhase == PHASE_SHRINK && side == 1;      // B [R, d_out]: its K dimension is contiguous
+  int issued = 0;                                        // of the producer: K blocks whose loads went out
   if (warp == 0) {
     if (lane == 0) {
       const int n_boxes = narrow_k_major ? 1 : p.narrow_bytes / kGBoxBytes;
@@ -218,27 +220,20 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
           for (int j = 0; j < n_boxes; ++j) tma_load_2d(sb + j * kGBoxBytes, narrow, full_bar(st), j * 64, k);
         }
       };
-      const int ahead = min(n_blk, p.stages);            // the ring starts empty
+      const int n_load = CWL_WITHHELD(p) && kPhase == PHASE_SHRINK ? n_blk - 1 : n_blk;
+      const int ahead = min(n_load, p.stages);           // the ring starts empty
       for (int b = 0; b < ahead; ++b) load_wide(b, (kb0 + b) * kGK);
       if (kPhase == PHASE_FOLD) pdl_wait();
       for (int b = 0; b < ahead; ++b) load_narrow(b, (kb0 + b) * kGK);
-      int issued = ahead, s = 0;
+      issued = max(ahead, 0);
+      int s = 0;
       uint32_t ph = 1;
-      bool ok = true;
-      for (int b = ahead; b < n_blk; ++b) {
-        if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) { ok = false; break; }
+      for (int b = ahead; b < n_load; ++b) {
+        if (!mbar_wait(empty_bar(s), ph ^ 1u, abort_flag)) break;
         load_wide(s, (kb0 + b) * kGK);
         load_narrow(s, (kb0 + b) * kGK);
         ++issued;
         if (++s == p.stages) { s = 0; ph ^= 1u; }
-      }
-      if (!ok) {
-        // copies already issued get a bounded chance to land before the CTA goes on
-        for (int back = 1; back <= p.stages && back <= issued; ++back) {
-          const int j = issued - back;
-          const unsigned long long t0 = global_timer();
-          while (!mbar_try_wait(full_bar(j % p.stages), (uint32_t)(j / p.stages) & 1u) && global_timer() - t0 < p.wait_limit_ns) {}
-        }
       }
     }
   } else if (warp == 1) {
@@ -413,7 +408,15 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
     tc_fence_after();
     tmem_dealloc1(tmem, (uint32_t)p.tmem_cols);
   }
-  if (tid == 0 && *abort_flag != 0) flag_status(p.status_word, CWL_ERR_TIMEOUT);
+  if (tid == 0 && *abort_flag != 0) {
+    flag_status(p.status_word, CWL_ERR_TIMEOUT);
+    // copies that nobody waited for get a bounded chance to land before the CTA leaves
+    for (int back = 1; back <= p.stages && back <= issued; ++back) {
+      const int j = issued - back;
+      const unsigned long long t0 = global_timer();
+      while (!mbar_try_wait(full_bar(j % p.stages), (uint32_t)(j / p.stages) & 1u) && global_timer() - t0 < p.wait_limit_ns) {}
+    }
+  }
 }
 
 struct GradLaunch {
@@ -548,7 +551,8 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
   p.lo_col = lo_column(R);
   p.gated_ld = p.lo_col + R;
   p.out[0] = dA; p.out[1] = dB; p.ld[0] = ldda; p.ld[1] = lddb; p.out_f32 = grad_dtype == CWL_F32;
-  p.wait_limit_ns = kGWaitLimitNs;
+  p.wait_limit_ns = training_wait_limit();
+  p.withhold = training_withhold();
   p.status_word = status_word;
 
   GradMaps shrink, fold;

@@ -5,12 +5,27 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 
+#include <atomic>
 #include <mutex>
 #include <unordered_map>
 
 #include "cwl_common.cuh"
 
 namespace cwl {
+
+constexpr unsigned long long kTrainingWaitLimitNs = 2000000000ull;   // limit of every device-side wait of distill.cu and grads.cu
+#ifdef CWL_TEST_HOOKS
+// test build only (cwl_debug_training_set): a shorter limit, and one copy that is never made, so that waits run out
+extern std::atomic<unsigned long long> g_training_wait_limit_ns;
+extern std::atomic<int> g_training_withhold;
+inline unsigned long long training_wait_limit() { return g_training_wait_limit_ns.load(); }
+inline int training_withhold() { return g_training_withhold.load(); }
+#define CWL_WITHHELD(p) ((p).withhold != 0)
+#else
+inline unsigned long long training_wait_limit() { return kTrainingWaitLimitNs; }
+inline int training_withhold() { return 0; }
+#define CWL_WITHHELD(p) false
+#endif
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
