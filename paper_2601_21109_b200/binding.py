@@ -269,9 +269,16 @@ class DeviceChunkTable:
         t.n_chunks.fill_(n)
         return t
 
+    def __setattr__(self, name, value):
+        self.__dict__[name] = value
+        self.__dict__["_c"] = None               # the marshalled struct follows the arrays
+
     def c_struct(self) -> CChunkTable:
-        return CChunkTable(_p(self.offsets), _p(self.rank), _p(self.scale), _p(self.rung), _p(self.flags),
-                           _p(self.n_chunks), self.capacity)
+        c = self._c
+        if c is None:
+            c = self.__dict__["_c"] = CChunkTable(_p(self.offsets), _p(self.rank), _p(self.scale), _p(self.rung), _p(self.flags),
+                                                  _p(self.n_chunks), self.capacity)
+        return c
 
     def to_host(self) -> dict:
         n = int(self.n_chunks.item())

@@ -476,7 +476,7 @@ GradLaunch grad_launch(int R, int columns, int tiles, int min_kb) {
 }
 
 template <int kPhase>
-cudaError_t launch_phase(const GradMaps& maps, const GradParams& p, const GradLaunch& l, cudaStream_t st) {
+cudaError_t launch_phase(const GradMaps& maps, const GradParams& p, const GradLaunch& l, bool chained, cudaStream_t st) {
   static SharedMemoryGrant grant;
   const cudaError_t e = grant(grad_kernel<kPhase>);
   if (e != cudaSuccess) return e;
@@ -486,12 +486,18 @@ cudaError_t launch_phase(const GradMaps& maps, const GradParams& p, const GradLa
   cfg.dynamicSmemBytes = l.smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = l.split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  int n = 0;
+  if (chained) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (l.split > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
+    attr[n++].val.clusterDim.x = l.split;
+  }
   cfg.attrs = attr;
-  cfg.numAttrs = stream_is_capturing(st) ? 1 : 2;
+  cfg.numAttrs = n;
   return cudaLaunchKernelEx(&cfg, grad_kernel<kPhase>, maps, p);
 }
 
@@ -572,10 +578,11 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
     p.tmem_cols = l.tmem_cols; p.ring_bytes = l.ring_bytes; p.meet_in_ring = l.meet_in_ring; p.meet_off = l.meet_off;
     return l;
   };
+  const bool chained = !stream_is_capturing(st);
   const int row_tiles = ceil_div(T, kGM), t_blocks = ceil_div(T, kGK);
   GradLaunch l = fill(R, row_tiles, row_tiles, ceil_div(d_in, kGK), ceil_div(d_out, kGK));
-  CWL_CUDA_TRY(launch_phase<PHASE_SHRINK>(shrink, p, l, st));
+  CWL_CUDA_TRY(launch_phase<PHASE_SHRINK>(shrink, p, l, chained, st));
   l = fill(p.gated_ld, ceil_div(d_in, kGM), ceil_div(d_out, kGM), t_blocks, t_blocks);
-  CWL_CUDA_TRY(launch_phase<PHASE_FOLD>(fold, p, l, st));
+  CWL_CUDA_TRY(launch_phase<PHASE_FOLD>(fold, p, l, chained, st));
   return CWL_OK;
 }
