@@ -164,6 +164,37 @@ def test_sorted_rows():
     check(on_device(np.repeat(z, 100, 0), "f32"), None, 128)
 
 
+@pytest.mark.parametrize("dtype,V", [("bf16", 9001), ("f32", 5003), ("f16", 16384)])
+@pytest.mark.parametrize("top_k", [1, 64, 128])
+def test_a_row_answers_the_same_among_many(dtype, V, top_k):
+    """Rows of every kind, thousands at once, against calls on parts of them: a row's answer does not depend on the others."""
+    T = 7200
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(V + top_k)
+    z = torch.randn(T, V, device="cuda", generator=gen) / (0.3 + 2.7 * torch.rand(T, 1, device="cuda", generator=gen))
+    z[0::16] = torch.randint(0, 40, (T // 16, V), device="cuda", generator=gen).float()          # ties
+    z[1::16] = 2.5
+    few = torch.rand(T // 16, V, device="cuda", generator=gen) < 10.0 / V                        # fewer allowed than listed
+    z[2::16] = torch.where(few, z[2::16], float("-inf"))
+    z[2::16, 7] = 1.0
+    v = torch.arange(V, device="cuda")
+    z[3::16] += 30.0 * ((v % 512) < 8)                                                           # large logits in few cells
+    z[4::16] -= 30.0 * v / V
+    z[5::16] = z[5::16].sort(dim=1).values
+    z[6::160, 11], z[22::160, V - 1] = float("nan"), float("inf")
+    z[38::160] = float("-inf")
+    z[54::160] = -60000.0
+    z = z.to(DT[dtype])
+    t = torch.randint(-1, V, (T,), dtype=torch.int32, device="cuda", generator=gen)
+    o = cwl.cwl_token_logprobs(z, t, top_k=top_k, temperature=0.8)
+    for a in range(0, T, 2400):
+        b = slice(a, a + 2400)
+        w = cwl.cwl_token_logprobs(z[b], t[b].contiguous(), top_k=top_k, temperature=0.8)
+        assert torch.equal(o.top_ids[b], w.top_ids)
+        for x, y in ((o.lse[b], w.lse), (o.logprob[b], w.logprob), (o.top_logprobs[b], w.top_logprobs), (o.entropy[b], w.entropy)):
+            assert torch.equal(torch.nan_to_num(x, nan=7.0), torch.nan_to_num(y, nan=7.0))
+
+
 def test_bad_targets_are_flagged_and_good_ones_are_not():
     z = on_device(rows(1, 6, 300), "f32")
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
