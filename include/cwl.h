@@ -21,8 +21,9 @@
  *     whose contents never have to be initialised or cleared by the caller.
  *   - Kernels are launched so that their set-up may overlap the end of the kernel ahead of them
  *     in the stream; each waits for that kernel to complete before it reads or writes global
- *     memory, so stream order holds for every buffer.  Launches recorded by a stream capture use
- *     plain stream order.
+ *     memory, so stream order holds for every buffer.  (The second kernel of cwl_apply_grads reads
+ *     X and dY, which the first does not write, while the first ends.)  Launches recorded by a
+ *     stream capture use plain stream order.
  */
 #ifndef CWL_H
 #define CWL_H
@@ -438,11 +439,12 @@ cwl_status cwl_distill_topk(const void* logits, cwl_dtype dtype, int64_t ld_logi
                             float* loss, void* dlogits, int64_t ld_dlogits, int32_t* status_word, void* stream);
 
 /* Gradient of the adapter factors of cwl_apply (cwl_apply_mode), dY being the gradient of the loss with respect to Y.
- * With g_t[j] the gate of row t (rank mask, scale, cross-fade weight) and H' = g o (X A) as the forward pass computes it,
+ * With g_t[j] the gate of row t (rank mask, scale, cross-fade weight) and H' = g o (X A),
  *   G = g o (dY B^T),   dA = X^T G,   dB = H'^T dY
  * (the gradient with respect to X is cwl_apply itself on transposed factors: dX = dY W^T + G A^T, i.e. X := dY,
  * W := W^T, A := B^T, B := A^T with the same table; W is frozen and has no gradient).
- * bf16 operands, fp32 accumulation on the tensor cores; H' and G are rounded to bf16 once, as the forward pass rounds H'.
+ * bf16 operands, fp32 accumulation on the tensor cores; H' and G are kept as the sum of two bf16 numbers (16 significant
+ * bits), so that what a gradient loses is its own rounding to grad_dtype and little more.
  *   X DEV bf16 [T, d_in]; dY DEV bf16 [T, d_out]; A DEV bf16 [d_in, R]; B DEV bf16 [R, d_out]; finite
  *   table, window, window_mode   as for cwl_apply_mode; rows outside every chunk contribute nothing
  *   dA DEV [d_in, R], dB DEV [R, d_out] of grad_dtype (CWL_F32 or CWL_BF16), overwritten

@@ -963,7 +963,7 @@ cudaError_t launch_distill(const DistillParams& p, cudaStream_t st) {
   if (row_bytes <= kSmallRowBytes || (row_bytes <= kSmallManyRowBytes && p.T >= kSmallManyRows && p.dlogits != nullptr)) {
     const size_t smem = (size_t)(row_bytes / 16) * 16 + 32;
     const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
-    return launch_clusters(chained, 1, distill_small_kernel<T>, dim3(rows), dim3(kDsThreads), smem, st, p);
+    return launch_chained(chained, distill_small_kernel<T>, dim3(rows), dim3(kDsThreads), smem, st, p);
   }
   if (p.dlogits == nullptr && p.T >= kLossMinRows) {
     const int words = (p.V + 2 * Elem<T>::kVec + 31) / 32;
@@ -971,8 +971,8 @@ cudaError_t launch_distill(const DistillParams& p, cudaStream_t st) {
     const cudaError_t e = loss_grant(distill_loss_kernel<T>);
     if (e != cudaSuccess) return e;
     const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
-    return launch_clusters(chained, 1, distill_loss_kernel<T>, dim3(rows), dim3(kLossThreads), sizeof(LossShared) + words * sizeof(uint32_t),
-                           st, p, words);
+    return launch_chained(chained, distill_loss_kernel<T>, dim3(rows), dim3(kLossThreads), sizeof(LossShared) + words * sizeof(uint32_t),
+                          st, p, words);
   }
   const PipePlan plan = pipe_plan(p.T, row_bytes);
   const size_t smem = (size_t)plan.n_buffers * plan.buffer_bytes + sizeof(DsPipe);

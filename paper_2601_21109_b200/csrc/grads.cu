@@ -486,18 +486,12 @@ cudaError_t launch_phase(const GradMaps& maps, const GradParams& p, const GradLa
   cfg.dynamicSmemBytes = l.smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
-  int n = 0;
-  if (chained) {
-    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[n++].val.programmaticStreamSerializationAllowed = 1;
-  }
-  if (l.split > 1) {
-    attr[n].id = cudaLaunchAttributeClusterDimension;
-    attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
-    attr[n++].val.clusterDim.x = l.split;
-  }
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = l.split; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = n;
+  cfg.numAttrs = chained ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, grad_kernel<kPhase>, maps, p);
 }
 
@@ -523,7 +517,7 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
                                       int32_t T, int32_t d_in, int32_t d_out, int32_t R,
                                       cwl_chunk_table table, int32_t window, int32_t window_mode,
                                       void* dA, int64_t ldda, void* dB, int64_t lddb, cwl_dtype grad_dtype,
-                                      void* workspace, size_t workspace_bytes, int32_t* status_word, void* stream) {
+                                      void* workspace, size_t workspace_bytes, int32_t* status_word, void* stream) try {
   using namespace cwl;
   if (T < 0 || d_in <= 0 || d_out <= 0 || R <= 0 || window < 0) return CWL_ERR_INVALID_ARG;
   if (window_mode != CWL_WINDOW_CAUSAL && window_mode != CWL_WINDOW_CENTRED) return CWL_ERR_INVALID_ARG;
@@ -585,4 +579,6 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
   l = fill(p.gated_ld, ceil_div(d_in, kGM), ceil_div(d_out, kGM), t_blocks, t_blocks);
   CWL_CUDA_TRY(launch_phase<PHASE_FOLD>(fold, p, l, chained, st));
   return CWL_OK;
+} catch (...) {
+  return CWL_ERR_CUDA;                                   // the cache of tensor maps allocates; nothing may leave a C entry
 }

@@ -378,7 +378,9 @@ __device__ __forceinline__ void st_peer_f32(uint32_t addr, float v) {
   asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
-// Launch in clusters of `cluster` CTAs, chained to the launch ahead like launch_chained.
+// Launch in clusters of `cluster` CTAs, chained to the launch ahead like launch_chained.  A kernel that executes cluster
+// instructions (asynchronous stores among them) needs this launch for clusters of one CTA too: started without the
+// attribute such a kernel ended in an illegal instruction.
 template <typename... KArgs, typename... Args>
 inline cudaError_t launch_clusters(bool chained, int cluster, void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem,
                                    cudaStream_t stream, Args... args) {
@@ -389,11 +391,9 @@ inline cudaError_t launch_clusters(bool chained, int cluster, void (*kernel)(KAr
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   int n = 0;
-  if (cluster > 1) {
-    attr[n].id = cudaLaunchAttributeClusterDimension;
-    attr[n].val.clusterDim.x = cluster; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
-    ++n;
-  }
+  attr[n].id = cudaLaunchAttributeClusterDimension;
+  attr[n].val.clusterDim.x = cluster; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
+  ++n;
   if (chained) {
     attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[n].val.programmaticStreamSerializationAllowed = 1;

@@ -528,8 +528,10 @@ template <typename T>
 cudaError_t launch_logprobs(const LogprobParams& p, cudaStream_t st) {
   const int l = logprob_cluster(p.T, p.V);
   const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
-  return launch_clusters(!stream_is_capturing(st), 1 << l, token_logprobs_kernel<T>, dim3(rows << l), dim3(kLpThreads),
-                         l > 0 ? lp_lists_bytes(1 << l, p.top_k) : 0, st, p, l);
+  const bool chained = !stream_is_capturing(st);
+  if (l == 0) return launch_chained(chained, token_logprobs_kernel<T>, dim3(rows), dim3(kLpThreads), 0, st, p, 0);
+  return launch_clusters(chained, 1 << l, token_logprobs_kernel<T>, dim3(rows << l), dim3(kLpThreads), lp_lists_bytes(1 << l, p.top_k),
+                         st, p, l);
 }
 
 }  // namespace
