@@ -650,7 +650,8 @@ def cwl_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_va
     """Distillation of a teacher's top entries (``teacher_ids`` int32 and ``teacher_values`` fp32 [T, K]; negative ids are
     padding) into the student's logits [T, V] (fp32, bf16 or fp16).  ``teacher`` says what the values are: "logits",
     renormalised over the entries, or "logprobs" of the tempered teacher, whose remaining mass is one more outcome.
-    Returns (loss fp32 [T] or None, dlogits or None); ``dlogits`` may be ``logits`` itself."""
+    Returns (loss fp32 [T] or None, dlogits or None, by default with the logits' row stride); ``dlogits`` may be ``logits``
+    itself."""
     assert logits.dtype in _DTYPES
     T, V = logits.shape
     K = teacher_ids.shape[1]
@@ -671,7 +672,8 @@ def cwl_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_va
         ld_d, d_unit = dlogits.stride()
         assert dlogits.is_cuda and dlogits.dtype == logits.dtype and dlogits.shape == (T, V) and d_unit == 1
     elif want_grad:
-        dlogits, ld_d = logits.new_empty((T, V)), V
+        # rows as far apart as the logits': they then start at the same offset from a 16-byte boundary
+        dlogits, ld_d = (logits.new_empty((T, V)), V) if ld == V else (logits.new_empty_strided((T, V), (ld, 1)), ld)
     if T == 1:                                   # a single row's stride says nothing
         ld, ld_teacher, ld_d = max(V, ld), max(K, ld_teacher), max(V, ld_d)
     _check("cwl_distill_topk", lib().cwl_distill_topk(

@@ -75,26 +75,35 @@ __device__ __forceinline__ float warp_max_nan(float v) {
   return v;
 }
 
-// Writes one row slice of gradients: whole 16-byte vectors where the output row starts at the same offset from a 16-byte
-// boundary as the input row, element by element otherwise.  value(i, f) fills f with the gradients of vector i.
+// Writes one row slice of gradients in 16-byte vectors.  Where the output row starts at the same offset from a 16-byte
+// boundary as the input row, the vectors are those of the input: vec_value(i, f) fills f with the gradients of vector i.
+// Otherwise they lie across the input's, and are put together element by element (scalar_value); the elements before the
+// first and after the last whole vector go out one by one.
 template <typename T, int kThreads, typename F, typename G>
 __device__ __forceinline__ void store_slice(int tid, T* d, bool same_phase, const RowSlice& rs, F vec_value, G scalar_value) {
   constexpr int kVec = Elem<T>::kVec;
-  for (int i = rs.v0 + tid; i < rs.v1; i += kThreads) {
-    float f[kVec];
-    vec_value(i, f);
-    T* out = d + rs.head + (int64_t)i * kVec;
-    if (same_phase) {
-      *reinterpret_cast<uint4*>(out) = Elem<T>::pack(f);
-    } else {
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) out[e] = Elem<T>::from_float(f[e]);
+  if (same_phase) {
+    for (int i = rs.v0 + tid; i < rs.v1; i += kThreads) {
+      float f[kVec];
+      vec_value(i, f);
+      *reinterpret_cast<uint4*>(d + rs.head + (int64_t)i * kVec) = Elem<T>::pack(f);
     }
+    if (tid < rs.own_head) d[tid] = Elem<T>::from_float(scalar_value(tid));
+    if (tid < rs.own_tail) d[rs.tail_start + tid] = Elem<T>::from_float(scalar_value(rs.tail_start + tid));
+  } else {
+    const unsigned off = (unsigned)(reinterpret_cast<uintptr_t>(d + rs.e0) & 15u);
+    const int first = min(rs.e0 + (int)(((16u - off) & 15u) / sizeof(T)), rs.e1);
+    const int n = (rs.e1 - first) / kVec, last = first + n * kVec;
+    for (int i = tid; i < n; i += kThreads) {
+      float f[kVec];
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) f[e] = scalar_value(first + i * kVec + e);
+      *reinterpret_cast<uint4*>(d + first + (int64_t)i * kVec) = Elem<T>::pack(f);
+    }
+    if (tid < first - rs.e0) d[rs.e0 + tid] = Elem<T>::from_float(scalar_value(rs.e0 + tid));
+    if (tid < rs.e1 - last) d[last + tid] = Elem<T>::from_float(scalar_value(last + tid));
   }
-  if (tid < rs.own_head) d[tid] = Elem<T>::from_float(scalar_value(tid));
-  if (tid < rs.own_tail) d[rs.tail_start + tid] = Elem<T>::from_float(scalar_value(rs.tail_start + tid));
 }
-
 template <typename T, int kThreads>
 __device__ __forceinline__ void zero_slice(int tid, T* d, bool same_phase, const RowSlice& rs) {
   store_slice<T, kThreads>(tid, d, same_phase, rs, [](int, float (&f)[Elem<T>::kVec]) {
@@ -878,19 +887,14 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
               grad_vec(*in, f);
               *out = Elem<T>::pack(f);
             }
-          } else {
-            for (int v = st; v < nv; v += kSumThreads) {
-              float f[kVec];
-              grad_vec(sv[v], f);
-              T* out = d + rs.head + (int64_t)(rs.v0 + v) * kVec;
-#pragma unroll
-              for (int e = 0; e < kVec; ++e) out[e] = Elem<T>::from_float(f[e]);
+            if (st < rs.own_head) d[st] = Elem<T>::from_float(exp2_fast((Elem<T>::to_float(sm[st]) - m) * p.c) * k_out);
+            if (st < rs.own_tail) {
+              const int x = rs.tail_start + st;
+              d[x] = Elem<T>::from_float(exp2_fast((Elem<T>::to_float(sm[x]) - m) * p.c) * k_out);
             }
-          }
-          if (st < rs.own_head) d[st] = Elem<T>::from_float(exp2_fast((Elem<T>::to_float(sm[st]) - m) * p.c) * k_out);
-          if (st < rs.own_tail) {
-            const int x = rs.tail_start + st;
-            d[x] = Elem<T>::from_float(exp2_fast((Elem<T>::to_float(sm[x]) - m) * p.c) * k_out);
+          } else {
+            store_slice<T, kSumThreads>(st, d, false, rs, [](int, float (&)[kVec]) {},
+                                        [&](int x) { return exp2_fast(fmaf(Elem<T>::to_float(sm[x]), p.c, -M)) * k; });
           }
         } else {
           store_slice<T, kSumThreads>(st, d, same_phase, rs, [&](int v, float (&f)[kVec]) {

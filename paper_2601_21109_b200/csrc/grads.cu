@@ -424,26 +424,27 @@ struct GradLaunch {
   size_t smem;
 };
 
-// CTAs a tile's K loop is split over: doubled while there is an SM for each and each keeps four K blocks; up to `resident`
+// CTAs a tile's K loop (the longer side's, n_kb blocks) is split over: doubled while there is an SM for each and each keeps
+// four K blocks; up to `resident`
 // CTAs (two an SM where their shared memory allows it) while each keeps kDeepBlocks, which is what the meeting of the
 // partial sums asks for.
 constexpr int kDeepBlocks = 8;
-int grad_split(int tiles, int min_kb, int resident) {
+int grad_split(int tiles, int n_kb, int resident) {
   int s = 1;
-  while (s < kGMaxCluster && ((tiles * s * 2 <= 148 && min_kb / (s * 2) >= 4) || (tiles * s * 2 <= resident && min_kb / (s * 2) >= kDeepBlocks)))
+  while (s < kGMaxCluster && ((tiles * s * 2 <= 148 && n_kb / (s * 2) >= 4) || (tiles * s * 2 <= resident && n_kb / (s * 2) >= kDeepBlocks)))
     s *= 2;
   return s;
 }
 
 // `columns` of the narrow operand: R, or what both halves of G / H' take
-GradLaunch grad_launch(int R, int columns, int tiles, int min_kb) {
+GradLaunch grad_launch(int R, int columns, int tiles, int n_kb) {
   GradLaunch l;
   l.narrow_bytes = ((columns + 63) / 64) * kGBoxBytes;
   l.stage_bytes = kGLeftBytes + l.narrow_bytes;
   // three stages or more in 96 KB let two CTAs share an SM (FOLD's set-up then runs beside SHRINK's end); a deeper stage
   // takes what the SM has
   const bool pair = 3 * l.stage_bytes <= 96 * 1024;
-  l.split = grad_split(tiles, min_kb, pair ? 296 : 148);
+  l.split = grad_split(tiles, n_kb, pair ? 296 : 148);
   const int budget = pair ? 96 * 1024 : 192 * 1024;
   l.stages = budget / l.stage_bytes;
   if (l.stages > kGMaxStages) l.stages = kGMaxStages;
@@ -567,7 +568,7 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
     p.n_tiles[0] = tiles0; p.n_tiles[1] = tiles1;
     p.n_kb[0] = kb0; p.n_kb[1] = kb1;
     p.first = kb1 > kb0 ? 1 : 0;                         // the longer loops start first
-    const GradLaunch l = grad_launch(R, columns, tiles0 + tiles1, kb0 < kb1 ? kb0 : kb1);
+    const GradLaunch l = grad_launch(R, columns, tiles0 + tiles1, kb0 > kb1 ? kb0 : kb1);
     p.split = l.split; p.stages = l.stages; p.stage_bytes = l.stage_bytes; p.narrow_bytes = l.narrow_bytes;
     p.tmem_cols = l.tmem_cols; p.ring_bytes = l.ring_bytes; p.meet_in_ring = l.meet_in_ring; p.meet_off = l.meet_off;
     return l;
