@@ -46,7 +46,8 @@ struct GradParams {
   int n_tiles[2], first;       // output tiles per side; the side whose tiles come first (the one with the longer K loop)
   int n_kb[2];                 // 64-deep K blocks per side
   int split;                   // CTAs of the cluster that share a tile's K loop
-  int stages, stage_bytes, narrow_bytes, tmem_cols, ring_bytes;
+  int tile_m, acc_cols;        // FOLD: 128 or 256 columns of X / dY per CTA (one or two accumulators), TMEM columns of one
+  int stages, stage_bytes, wide_bytes, narrow_bytes, tmem_cols, ring_bytes;
   int meet_in_ring, meet_off;  // where a cluster's partial sums meet: over the idle ring, or beside it
   __nv_bfloat16* gated[2];     // SHRINK: where side s's result goes: H' (side 0) and G (side 1), [T, gated_ld]
   int gated_ld, lo_col;        // a row: R columns of high halves, then (from column lo_col) R of low halves
@@ -165,7 +166,8 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
   const int per = (p.n_kb[side] + split - 1) / split;
   const int kb0 = min(cta * per, p.n_kb[side]);
   const int n_blk = min(kb0 + per, p.n_kb[side]) - kb0;
-  const int m0 = tile * kGM;
+  const int n_acc = kPhase == PHASE_FOLD ? p.tile_m / kGM : 1;
+  const int m0 = tile * kGM * n_acc;
   const CUtensorMap* wide = &maps.wide[side];
   const CUtensorMap* narrow = &maps.narrow[side];
 
@@ -201,19 +203,18 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
   if (warp == 0) {
     if (lane == 0) {
       const int n_boxes = narrow_k_major ? 1 : p.narrow_bytes / kGBoxBytes;
-      const uint32_t tx = (uint32_t)(kGLeftBytes + (narrow_k_major ? p.R * kGK * 2 : n_boxes * kGBoxBytes));
+      const uint32_t tx = (uint32_t)(p.wide_bytes + (narrow_k_major ? p.R * kGK * 2 : n_boxes * kGBoxBytes));
       auto load_wide = [&](int st, int k) {
         const uint32_t sa = base + (uint32_t)(st * p.stage_bytes);
         mbar_expect_tx(full_bar(st), tx);
         if (kPhase == PHASE_SHRINK) {
           tma_load_2d(sa, wide, full_bar(st), k, m0);
         } else {
-          tma_load_2d(sa, wide, full_bar(st), m0, k);
-          tma_load_2d(sa + kGBoxBytes, wide, full_bar(st), m0 + 64, k);
+          for (int j = 0; j < 2 * n_acc; ++j) tma_load_2d(sa + j * kGBoxBytes, wide, full_bar(st), m0 + 64 * j, k);
         }
       };
       auto load_narrow = [&](int st, int k) {
-        const uint32_t sb = base + (uint32_t)(st * p.stage_bytes) + kGLeftBytes;
+        const uint32_t sb = base + (uint32_t)(st * p.stage_bytes + p.wide_bytes);
         if (narrow_k_major) {
           tma_load_2d(sb, narrow, full_bar(st), k, 0);
         } else {
@@ -251,12 +252,14 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
       for (int b = 0; b < n_blk; ++b) {
         if (!mbar_wait(full_bar(s), ph, abort_flag)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t sa = base + (uint32_t)(s * p.stage_bytes), sb = sa + kGLeftBytes;
+        const uint32_t sa = base + (uint32_t)(s * p.stage_bytes), sb = sa + p.wide_bytes;
         const uint64_t da = kPhase == PHASE_SHRINK ? make_smem_desc(sa, 16, 1024) : make_smem_desc(sa, kGBoxBytes, 1024);
         const uint64_t db = narrow_k_major ? make_smem_desc(sb, 16, 1024) : make_smem_desc(sb, kGBoxBytes, 1024);
 #pragma unroll
         for (int kk = 0; kk < kGK / 16; ++kk) {
           umma_bf16(tmem, da + kk * step_a, db + kk * step_b, idesc, (b | kk) ? 1u : 0u);
+          if (kPhase == PHASE_FOLD && n_acc > 1)
+            umma_bf16(tmem + p.acc_cols, da + (kGLeftBytes >> 4) + kk * step_a, db + kk * step_b, idesc, (b | kk) ? 1u : 0u);
           if (halves) umma_bf16(tmem + p.lo_col, da + kk * step_a, db + lo_half + kk * step_b, idesc, (b | kk) ? 1u : 0u);
         }
         umma_commit(empty_bar(s));
@@ -284,12 +287,13 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
     __syncwarp();
     tc_fence_after();
   }
-  auto columns = [&](int c, uint32_t (&v)[32]) {         // 32 columns of this lane's row
+  auto columns = [&](int acc, int c, uint32_t (&v)[32]) {   // 32 columns of this lane's row of an accumulator
     if (n_blk > 0) {
-      tmem_ld32(tmem + ((uint32_t)(quad * 32) << 16) + c, v);
+      const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + acc * p.acc_cols + c;
+      tmem_ld32(at, v);
       if (kPhase == PHASE_FOLD) {
         uint32_t lo[32];
-        tmem_ld32(tmem + ((uint32_t)(quad * 32) << 16) + p.lo_col + c, lo);
+        tmem_ld32(at + p.lo_col, lo);
         tmem_ld_wait();
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(lo[j]));
@@ -305,24 +309,27 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
   if (split == 1) {
     // straight from the accumulator
     if (drain && *abort_flag == 0) {
-      for (int c = 0; c < p.R; c += 32) {
-        uint32_t v[32];
-        columns(c, v);
-        if (by_rows) {
+      for (int acc = 0; acc < n_acc; ++acc) {
+        const int at_row = acc * kGM + row;
+        for (int c = 0; c < p.R; c += 32) {
+          uint32_t v[32];
+          columns(acc, c, v);
+          if (by_rows) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q)
-            if (c + q * 8 < p.R)
-              store_row8<kPhase>(p, side, m0 + row, c + q * 8, kPhase == PHASE_SHRINK ? gates[row] : RowGate{},
-                                 make_float4(__uint_as_float(v[q * 8]), __uint_as_float(v[q * 8 + 1]), __uint_as_float(v[q * 8 + 2]), __uint_as_float(v[q * 8 + 3])),
-                                 make_float4(__uint_as_float(v[q * 8 + 4]), __uint_as_float(v[q * 8 + 5]), __uint_as_float(v[q * 8 + 6]), __uint_as_float(v[q * 8 + 7])));
-        } else if (m0 + row < p.d[1]) {                  // a warp stores 32 neighbours of an output row at a time
-          const int n = min(32, p.R - c);
+            for (int q = 0; q < 4; ++q)
+              if (c + q * 8 < p.R)
+                store_row8<kPhase>(p, side, m0 + at_row, c + q * 8, kPhase == PHASE_SHRINK ? gates[row] : RowGate{},
+                                   make_float4(__uint_as_float(v[q * 8]), __uint_as_float(v[q * 8 + 1]), __uint_as_float(v[q * 8 + 2]), __uint_as_float(v[q * 8 + 3])),
+                                   make_float4(__uint_as_float(v[q * 8 + 4]), __uint_as_float(v[q * 8 + 5]), __uint_as_float(v[q * 8 + 6]), __uint_as_float(v[q * 8 + 7])));
+          } else if (m0 + at_row < p.d[1]) {             // a warp stores 32 neighbours of an output row at a time
+            const int n = min(32, p.R - c);
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            if (j < n) {
-              const int64_t at = (int64_t)(c + j) * p.ld[1] + m0 + row;
-              if (p.out_f32) reinterpret_cast<float*>(p.out[1])[at] = __uint_as_float(v[j]);
-              else reinterpret_cast<__nv_bfloat16*>(p.out[1])[at] = __float2bfloat16_rn(__uint_as_float(v[j]));
+            for (int j = 0; j < 32; ++j) {
+              if (j < n) {
+                const int64_t at = (int64_t)(c + j) * p.ld[1] + m0 + at_row;
+                if (p.out_f32) reinterpret_cast<float*>(p.out[1])[at] = __uint_as_float(v[j]);
+                else reinterpret_cast<__nv_bfloat16*>(p.out[1])[at] = __float2bfloat16_rn(__uint_as_float(v[j]));
+              }
             }
           }
         }
@@ -331,7 +338,7 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
     tc_fence_before();
     __syncthreads();
   } else {
-    // Every CTA owns a share of the output: 128 / split rows of the tile, or R / split columns of it where those are the
+    // Every CTA owns a share of the output: tile_m / split rows of the tile, or R / split columns of it where those are the
     // rows of the output.  The others' accumulators are pushed into its shared memory and added up there, in the order of
     // the CTAs.  Layouts are such that a warp's stores are contiguous: [column group of 4][rows][4] and [column][128 rows].
     if (p.meet_in_ring) {                                // over the ring, once it is idle in the whole cluster
@@ -341,38 +348,42 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
     } else {
       grad_cluster_barrier_wait();                       // the peers run (they arrived at their start)
     }
-    const int share = (by_rows ? kGM : p.R) / split;
+    const int tile_m = kGM * n_acc;
+    const int share = (by_rows ? tile_m : p.R) / split;
     const uint32_t meet = base + (uint32_t)p.meet_off;
-    const int part = by_rows ? share * p.R : share * kGM;            // numbers that one CTA contributes to a share
+    const int part = by_rows ? share * p.R : share * tile_m;         // numbers that one CTA contributes to a share
     if (drain) {
-      if (by_rows) {
-        const int owner = row / share;
-        const uint32_t to = grad_peer(meet, owner) + (uint32_t)(cta * part + (row - owner * share) * 4) * 4u;
-        for (int c = 0; c < p.R; c += 32) {
-          uint32_t v[32];
-          columns(c, v);
+      for (int acc = 0; acc < n_acc; ++acc) {
+        const int at_row = acc * kGM + row;
+        if (by_rows) {
+          const int owner = at_row / share;
+          const uint32_t to = grad_peer(meet, owner) + (uint32_t)(cta * part + (at_row - owner * share) * 4) * 4u;
+          for (int c = 0; c < p.R; c += 32) {
+            uint32_t v[32];
+            columns(acc, c, v);
 #pragma unroll
-          for (int q = 0; q < 8; ++q)
-            if (c + q * 4 < p.R)
-              st_peer_v4(to + (uint32_t)((c + q * 4) * share) * 4u, v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
-        }
-      } else {
-        for (int c = 0; c < p.R; c += 32) {
-          uint32_t v[32];
-          columns(c, v);
-          const int n = min(32, p.R - c);
-          int owner = c / share, left = share - (c - owner * share);
-          uint32_t to = grad_peer(meet, owner) + (uint32_t)(cta * part + (share - left) * kGM + row) * 4u;
+            for (int q = 0; q < 8; ++q)
+              if (c + q * 4 < p.R)
+                st_peer_v4(to + (uint32_t)((c + q * 4) * share) * 4u, v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
+          }
+        } else {
+          for (int c = 0; c < p.R; c += 32) {
+            uint32_t v[32];
+            columns(acc, c, v);
+            const int n = min(32, p.R - c);
+            int owner = c / share, left = share - (c - owner * share);
+            uint32_t to = grad_peer(meet, owner) + (uint32_t)(cta * part + (share - left) * tile_m + at_row) * 4u;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) {
-            if (j < n) {
-              if (left == 0) {
-                left = share;
-                to = grad_peer(meet, ++owner) + (uint32_t)(cta * part + row) * 4u;
+            for (int j = 0; j < 32; ++j) {
+              if (j < n) {
+                if (left == 0) {
+                  left = share;
+                  to = grad_peer(meet, ++owner) + (uint32_t)(cta * part + at_row) * 4u;
+                }
+                st_peer_b32(to, v[j]);
+                to += (uint32_t)tile_m * 4u;
+                --left;
               }
-              st_peer_b32(to, v[j]);
-              to += kGM * 4u;
-              --left;
             }
           }
         }
@@ -385,9 +396,9 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
       // eight numbers of an output row a thread
       for (int i = tid; i < part / 8; i += kGThreads) {
         float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
-        const int line = by_rows ? i % share : i / (kGM / 8);        // row of the tile in the share, or column of it
-        const int col = by_rows ? (i / share) * 8 : (i % (kGM / 8)) * 8;
-        const float* q = in + (by_rows ? col * share + line * 4 : line * kGM + col);
+        const int line = by_rows ? i % share : i / (tile_m / 8);     // row of the tile in the share, or column of it
+        const int col = by_rows ? (i / share) * 8 : (i % (tile_m / 8)) * 8;
+        const float* q = in + (by_rows ? col * share + line * 4 : line * tile_m + col);
         const int second = by_rows ? share * 4 : 4;
         for (int r = 0; r < split; ++r, q += part) {
           const float4 x = *reinterpret_cast<const float4*>(q), y = *reinterpret_cast<const float4*>(q + second);
@@ -420,14 +431,13 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
 }
 
 struct GradLaunch {
-  int split, stages, stage_bytes, narrow_bytes, tmem_cols, ring_bytes, meet_in_ring, meet_off;
+  int split, tile_m, acc_cols, stages, stage_bytes, wide_bytes, narrow_bytes, tmem_cols, ring_bytes, meet_in_ring, meet_off;
   size_t smem;
 };
 
 // CTAs a tile's K loop (the longer side's, n_kb blocks) is split over: doubled while there is an SM for each and each keeps
-// four K blocks; up to `resident`
-// CTAs (two an SM where their shared memory allows it) while each keeps kDeepBlocks, which is what the meeting of the
-// partial sums asks for.
+// four K blocks; up to `resident` CTAs (two an SM where their shared memory allows it) while each keeps kDeepBlocks, which
+// is what the meeting of the partial sums asks for.
 constexpr int kDeepBlocks = 8;
 int grad_split(int tiles, int n_kb, int resident) {
   int s = 1;
@@ -436,11 +446,13 @@ int grad_split(int tiles, int n_kb, int resident) {
   return s;
 }
 
-// `columns` of the narrow operand: R, or what both halves of G / H' take
-GradLaunch grad_launch(int R, int columns, int tiles, int n_kb) {
+// `columns` of the narrow operand: R, or what both halves of G / H' take; tile_m: 128, or 256 (FOLD)
+GradLaunch grad_launch(int R, int columns, int tile_m, int tiles, int n_kb) {
   GradLaunch l;
+  l.tile_m = tile_m;
+  l.wide_bytes = kGLeftBytes * (tile_m / kGM);
   l.narrow_bytes = ((columns + 63) / 64) * kGBoxBytes;
-  l.stage_bytes = kGLeftBytes + l.narrow_bytes;
+  l.stage_bytes = l.wide_bytes + l.narrow_bytes;
   // three stages or more in 96 KB let two CTAs share an SM (FOLD's set-up then runs beside SHRINK's end); a deeper stage
   // takes what the SM has
   const bool pair = 3 * l.stage_bytes <= 96 * 1024;
@@ -448,9 +460,9 @@ GradLaunch grad_launch(int R, int columns, int tiles, int n_kb) {
   const int budget = pair ? 96 * 1024 : 192 * 1024;
   l.stages = budget / l.stage_bytes;
   if (l.stages > kGMaxStages) l.stages = kGMaxStages;
-  // a cluster's partial sums, [128][R] fp32: beside a ring of at least three stages where both fit 109 KB (no need to wait
+  // a cluster's partial sums, [tile_m][R] fp32: beside a ring of at least three stages where both fit 109 KB (no need to wait
   // for the whole cluster's MMAs before they are sent), else over the ring
-  const int meet = l.split == 1 ? 0 : kGM * R * 4;
+  const int meet = l.split == 1 ? 0 : tile_m * R * 4;
   l.meet_in_ring = 0;
   l.ring_bytes = l.stages * l.stage_bytes;
   if (l.split > 1) {
@@ -470,8 +482,9 @@ GradLaunch grad_launch(int R, int columns, int tiles, int n_kb) {
   }
   // the epilogue reads 32 columns at a time, from 0 and (low halves) from columns - R on
   const int read = columns - R + (R + 31) / 32 * 32;
-  l.tmem_cols = 32;
-  while (l.tmem_cols < read) l.tmem_cols *= 2;
+  l.acc_cols = 32;
+  while (l.acc_cols < read) l.acc_cols *= 2;
+  l.tmem_cols = l.acc_cols * (tile_m / kGM);
   l.smem = (size_t)l.ring_bytes + 1024 + 8 * (2 * kGMaxStages + 1) + 8 + 32 + kGM * sizeof(RowGate);
   return l;
 }
@@ -499,6 +512,18 @@ cudaError_t launch_phase(const GradMaps& maps, const GradParams& p, const GradLa
 // G and H' hold two halves a row: side by side where one product takes both, else the low half from a multiple of 64 on
 // (a box's edge), where a product of its own can start
 int lo_column(int R) { return 2 * R <= 256 ? R : (R + 63) / 64 * 64; }
+// Columns of X / dY per CTA of FOLD: 128, or 256 where both halves of G / H' are wider than 128 columns and would come in
+// more often than X and dY themselves (us, 128 -> 256: R = 80 at T = 16384, 4096 -> 11008: 230 -> 188; R = 80 at
+// T = 4096, 4096 -> 4096: 44.9 -> 40.8; R = 128 at T = 8192, 4096 -> 4096: 75.8 -> 71.5; but R = 64 at T = 8192: 57.6 ->
+// 58.2).  Two accumulators must fit the tensor memory, and the CTAs must still take most SMs for loops of kFoldMinBlocks
+// (R = 128 at T = 2048, 4096 -> 4096, loops of 8: 35.0 -> 37.2).
+constexpr int kFoldMinCtas = 96, kFoldMinBlocks = 16;
+int fold_tile(int R, int d_in, int d_out, int t_blocks) {
+  if (R <= 64 || R > 128) return kGM;
+  const int tiles = ceil_div(d_in, 2 * kGM) + ceil_div(d_out, 2 * kGM);
+  const int split = grad_split(tiles, t_blocks, 148);
+  return tiles * split >= kFoldMinCtas && t_blocks / split >= kFoldMinBlocks ? 2 * kGM : kGM;
+}
 size_t gated_bytes(int T, int R) { return ((size_t)T * (lo_column(R) + R) * 2 + 255) / 256 * 256; }
 
 bool bad_matrix(const void* ptr, int64_t ld, int64_t cols, int elem) {
@@ -564,20 +589,22 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
       make_map(&fold.wide[1], dY, d_out, T, lddy, 64, kGK) && make_map(&fold.narrow[1], H, p.gated_ld, T, p.gated_ld, 64, kGK);
   if (!maps_ok) return CWL_ERR_CUDA;
 
-  auto fill = [&](int columns, int tiles0, int tiles1, int kb0, int kb1) {
+  auto fill = [&](int columns, int tile_m, int rows0, int rows1, int kb0, int kb1) {
+    const int tiles0 = ceil_div(rows0, tile_m), tiles1 = ceil_div(rows1, tile_m);
     p.n_tiles[0] = tiles0; p.n_tiles[1] = tiles1;
     p.n_kb[0] = kb0; p.n_kb[1] = kb1;
     p.first = kb1 > kb0 ? 1 : 0;                         // the longer loops start first
-    const GradLaunch l = grad_launch(R, columns, tiles0 + tiles1, kb0 > kb1 ? kb0 : kb1);
-    p.split = l.split; p.stages = l.stages; p.stage_bytes = l.stage_bytes; p.narrow_bytes = l.narrow_bytes;
+    const GradLaunch l = grad_launch(R, columns, tile_m, tiles0 + tiles1, kb0 > kb1 ? kb0 : kb1);
+    p.split = l.split; p.stages = l.stages; p.stage_bytes = l.stage_bytes; p.wide_bytes = l.wide_bytes; p.narrow_bytes = l.narrow_bytes;
+    p.tile_m = l.tile_m; p.acc_cols = l.acc_cols;
     p.tmem_cols = l.tmem_cols; p.ring_bytes = l.ring_bytes; p.meet_in_ring = l.meet_in_ring; p.meet_off = l.meet_off;
     return l;
   };
   const bool chained = !stream_is_capturing(st);
-  const int row_tiles = ceil_div(T, kGM), t_blocks = ceil_div(T, kGK);
-  GradLaunch l = fill(R, row_tiles, row_tiles, ceil_div(d_in, kGK), ceil_div(d_out, kGK));
+  const int t_blocks = ceil_div(T, kGK);
+  GradLaunch l = fill(R, kGM, T, T, ceil_div(d_in, kGK), ceil_div(d_out, kGK));
   CWL_CUDA_TRY(launch_phase<PHASE_SHRINK>(shrink, p, l, chained, st));
-  l = fill(p.gated_ld, ceil_div(d_in, kGM), ceil_div(d_out, kGM), t_blocks, t_blocks);
+  l = fill(p.gated_ld, fold_tile(R, d_in, d_out, t_blocks), d_in, d_out, t_blocks, t_blocks);
   CWL_CUDA_TRY(launch_phase<PHASE_FOLD>(fold, p, l, chained, st));
   return CWL_OK;
 } catch (...) {

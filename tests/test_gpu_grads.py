@@ -94,6 +94,16 @@ def test_sizes(T, d_in, d_out, R, chunk, window):
     check(X, dY, A, B, tab, window, grad_dtype=torch.float32)
 
 
+@pytest.mark.parametrize("T,d_in,d_out,R,chunk,window", [
+    (8256, 3600, 4112, 48, 300, 8), (2050, 12304, 13328, 16, 100, 4), (8200, 4096, 3856, 128, 200, 8), (4133, 10128, 4240, 80, 64, 8),
+    (16384, 2064, 2048, 32, 500, 6)])
+def test_many_rows(T, d_in, d_out, R, chunk, window):
+    X, dY, A, B = operands(T + R, T, d_in, d_out, R)
+    tab = table(T, T, R, chunk, seqs=3)
+    check(X, dY, A, B, tab, window)
+    check(X, dY, A, B, tab, window, grad_dtype=torch.float32)
+
+
 @pytest.mark.parametrize("T,d_in,d_out,R", [(300, 512, 320, 64), (777, 256, 1040, 144), (129, 1024, 640, 16), (2000, 272, 512, 256)])
 def test_fp32_gradients_carry_more_than_bf16(T, d_in, d_out, R):
     """H' and G are kept as two bf16 numbers: what they lose is 2^-17 of a number (half of the low one's spacing), so an fp32
