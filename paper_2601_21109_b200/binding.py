@@ -673,7 +673,7 @@ def cwl_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_va
         assert dlogits.is_cuda and dlogits.dtype == logits.dtype and dlogits.shape == (T, V) and d_unit == 1
     elif want_grad:
         # rows as far apart as the logits': they then start at the same offset from a 16-byte boundary
-        dlogits, ld_d = (logits.new_empty((T, V)), V) if ld == V else (logits.new_empty_strided((T, V), (ld, 1)), ld)
+        dlogits, ld_d = torch.empty_like(logits) if ld == V else logits.new_empty_strided((T, V), (ld, 1)), ld
     if T == 1:                                   # a single row's stride says nothing
         ld, ld_teacher, ld_d = max(V, ld), max(K, ld_teacher), max(V, ld_d)
     _check("cwl_distill_topk", lib().cwl_distill_topk(
@@ -700,12 +700,13 @@ def cwl_apply_grads(X: torch.Tensor, dY: torch.Tensor, A: torch.Tensor, B: torch
     assert ux == uy == ua == ub == 1 and X.is_cuda and dY.is_cuda and A.is_cuda and B.is_cuda
     assert X.dtype == dY.dtype == A.dtype == B.dtype == torch.bfloat16
     if dA is None:
-        dA, ldda = X.new_empty((d_in, R), dtype=grad_dtype if dB is None else dB.dtype), R
+        dtype = grad_dtype if dB is None else dB.dtype
+        dA, ldda = torch.empty_like(A, dtype=dtype) if lda == R else A.new_empty((d_in, R), dtype=dtype), R
     else:
         ldda, u = dA.stride()
         assert dA.is_cuda and dA.dtype in _DTYPES and dA.shape == (d_in, R) and u == 1
     if dB is None:
-        dB, lddb = X.new_empty((R, d_out), dtype=dA.dtype), d_out
+        dB, lddb = torch.empty_like(B, dtype=dA.dtype) if ldb == d_out else B.new_empty((R, d_out), dtype=dA.dtype), d_out
     else:
         lddb, u = dB.stride()
         assert dB.is_cuda and dB.dtype == dA.dtype and dB.shape == (R, d_out) and u == 1

@@ -94,7 +94,8 @@ __device__ __noinline__ void append_ties_in_order(LpShared& sh, const T* z, int 
 
 // The want-th largest of the threads' half maxima, rounded down to its first bits (all that a 16-bit type has, 16 of
 // fp32: a bound that is up to 1/128 lower admits a few logits more).  One warp: a bit per step, from the first in which the
-// keys differ.
+// keys differ.  Where that is the lowest value of all, which the row is then full of (most logits masked with one value), the
+// bound is the number above it: fewer may reach it than are wanted, and the rest are ties, the lowest indices of the row.
 template <typename T>
 __device__ __forceinline__ uint32_t cell_bound(const uint32_t* half, int want) {
   constexpr int kLastBit = Elem<T>::kZeroBits > 0 ? Elem<T>::kZeroBits : 16;
@@ -110,6 +111,12 @@ __device__ __forceinline__ uint32_t cell_bound(const uint32_t* half, int want) {
   hi = __reduce_max_sync(0xffffffffu, hi);
   lo = __reduce_min_sync(0xffffffffu, lo);
   const int first = 31 - __clz((int)(hi ^ lo));          // -1 when all keys are equal
+  if (lo >= kKeyOfMinusInf && __popc(__ballot_sync(0xffffffffu, k[0] == lo)) >= 8) {
+    int above = 0;
+#pragma unroll
+    for (int i = 0; i < n; ++i) above += k[i] > lo;
+    if ((int)__reduce_add_sync(0xffffffffu, above) < want) return lo + 1;
+  }
   uint32_t prefix = first >= 31 ? 0u : hi & ~((2u << first) - 1u);
   if (first < 0) prefix = hi;
   for (int bit = first; bit >= kLastBit; --bit) {
@@ -219,7 +226,7 @@ __device__ __noinline__ uint32_t exact_bound_and_candidates(LpShared& sh, const 
   return thr;
 }
 
-// What reaches the bound goes to the candidates, what equals it to the ties.
+// What lies above the bound goes to the candidates, what equals it to the ties.
 __device__ __forceinline__ void take_candidate(LpShared& sh, float v, int i, float bound, bool all) {
   if (v > bound || all) {
     const int at = atomicAdd(&sh.n_cand, 1);
@@ -230,12 +237,45 @@ __device__ __forceinline__ void take_candidate(LpShared& sh, float v, int i, flo
   }
 }
 
+// Cells of a short row again, of one vector each: a single batch makes one cell a thread, and where nearly as many
+// alternatives are wanted the bound would sink until most of the row lies above it (four rows of 29879 bf16, K = 128, eight
+// blocks a row: 23.2 -> 16.1 us; half as many wanted, or two batches, and the second look at the row costs more than it gives:
+// K = 64 7.8 -> 8.1, 7248 rows of 8250 fp16 with K = 128 129 -> 141).
+constexpr int kFineWant = 96;
+template <typename T>
+__device__ __noinline__ void fine_cells(LpShared& sh, const uint4* zv, int nv) {
+  const int tid = threadIdx.x;
+  const uint4 pad = make_uint4(Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked());
+  uint4 q[kLpBatch];
+  uint32_t half_key[2] = {0u, 0u};
+#pragma unroll
+  for (int s = 0; s < kLpBatch; ++s) q[s] = s * kLpThreads + tid < nv ? __ldg(zv + s * kLpThreads + tid) : pad;
+#pragma unroll
+  for (int s = 0; s < kLpBatch; ++s) {
+    const uint32_t w[4] = {q[s].x, q[s].y, q[s].z, q[s].w};
+    const uint32_t key = s * kLpThreads + tid < nv ? order_key(Elem<T>::max_of(w)) : 0u;
+    sh.cell[s * kLpThreads + tid] = key;                 // the cells above stay empty
+    half_key[s & 1] = max(half_key[s & 1], key);
+  }
+  sh.half[tid] = half_key[0];
+  sh.half[kLpThreads + tid] = half_key[1];
+  __syncthreads();
+}
+
 // Leaves in sh.cand a set that holds the `want` largest rank keys of this CTA's elements; returns its size (at least
 // `want`).  sh.cell and sh.half hold the maxima.
 template <typename T>
 __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const RowSlice& rs, int want) {
   constexpr int kVec = Elem<T>::kVec;
   const int tid = threadIdx.x, lane = tid & 31;
+  const int nv = rs.v1 - rs.v0;
+  const uint4* zv = reinterpret_cast<const uint4*>(z + rs.head) + rs.v0;
+  // cell (s, t) holds the vectors (s * per_cell + j) * 128 + t, j < per_cell
+  int per_cell = kLpBatch * max(1, ((nv + kLpBatchVecs - 1) / kLpBatchVecs + kSegs - 1) / kSegs);
+  if (nv <= kLpBatchVecs && want > kFineWant) {
+    fine_cells<T>(sh, zv, nv);
+    per_cell = 1;
+  }
   if (tid < 32) {
     const uint32_t bound = cell_bound<T>(sh.half, want);
     if (lane == 0) { sh.n_hits = 0; sh.n_cand = 0; sh.n_ties = 0; sh.n_vecs = 0; sh.thr = bound; }
@@ -255,13 +295,8 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
   // a bound below every element's key (fewer nonempty cells than wanted): everything is above it, -inf too
   const bool all = thr < kKeyOfMinusInf;
   float bound = all ? -CUDART_INF_F : key_value(thr);
-  // cell (s, t) holds the vectors t, t + 128, ... of the batches s * per_seg .. (s + 1) * per_seg - 1
-  const int nv = rs.v1 - rs.v0;
-  const int per_seg = max(1, ((nv + kLpBatchVecs - 1) / kLpBatchVecs + kSegs - 1) / kSegs);
-  const int per_cell = per_seg * kLpBatch;
   const int n_work = sh.n_hits * per_cell;               // at most 1024 cells times nv / 1024 + 4 vectors each: below 2^24
   const float inv_per_cell = 1.f / (float)per_cell;
-  const uint4* zv = reinterpret_cast<const uint4*>(z + rs.head) + rs.v0;
   const uint4 pad = make_uint4(Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked());
   // The few vectors that hold anything are gathered (where the cells and their maxima were, which have served) and their
   // elements dealt to all threads: taken in place, every warp would walk all elements of its vectors for a lane or two.
@@ -282,7 +317,7 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
       q[u] = pad;
       if (w < n_work) {
         const int cell = sh.hits[h];
-        const int i = (cell / kLpThreads) * per_seg * kLpBatchVecs + j * kLpThreads + cell % kLpThreads;
+        const int i = ((cell / kLpThreads) * per_cell + j) * kLpThreads + cell % kLpThreads;
         if (i < nv) { at[u] = i; q[u] = __ldg(zv + i); }
       }
     }
@@ -322,6 +357,10 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
       n_cand += n_ties;                                  // at most 127 + 256
     } else {
       append_ties_in_order(sh, z, rs.e0, rs.e1, thr, n_cand, want - n_cand);
+      n_cand = want;
+    }
+    if (n_cand < want) {                                 // the bound was the number above the row's lowest
+      append_ties_in_order(sh, z, rs.e0, rs.e1, thr - 1, n_cand, want - n_cand);
       n_cand = want;
     }
     __syncthreads();

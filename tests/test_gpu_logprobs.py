@@ -141,6 +141,28 @@ def test_rows_with_few_allowed_tokens(allowed):
         check(on_device(z, "bf16"), z.argmax(1), K)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("mask", [-np.inf, "lowest", -1.0e4, 0.0])
+@pytest.mark.parametrize("V,top_k", [(32000, 20), (13363, 128), (900, 64), (70001, 128)])
+def test_rows_full_of_one_value(dtype, mask, V, top_k):
+    """Most logits hold one value (a mask, a floor), which a good part of the listed ones then is, lowest index first."""
+    lowest = {"f32": np.finfo(np.float32).min, "f16": -65504.0, "bf16": -3.3895313892515355e38}[dtype]
+    fill = lowest if mask == "lowest" else mask
+    for T, allowed in ((3, 5), (3, 100), (160, 40), (640, 250)):
+        rng = np.random.default_rng(allowed)
+        z = np.full((T, V), fill, np.float32)
+        for t in range(T):
+            z[t, rng.choice(V, allowed, replace=False)] = rng.standard_normal(allowed) + (t % 2) * 2
+        check(on_device(z, dtype), None, top_k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,V", [(1, 3909), (4, 29879), (21, 13363), (30, 57744), (500, 6000), (700, 12345), (9, 1024)])
+def test_many_alternatives_of_short_slices(dtype, T, V):
+    check(on_device(rows(T + V, T, V), dtype), None, 128)
+    check(on_device(np.round(rows(T + V, T, V) * 3), dtype), None, 100)          # few different values
+
+
 @pytest.mark.parametrize("dtype,stride", [("f32", 1024), ("bf16", 2048), ("f16", 2048)])
 def test_large_logits_gathered_in_few_cells(dtype, stride):
     """Elements `stride` apart belong to the same thread: everything large sits in five threads' elements, so that the
