@@ -924,9 +924,11 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
 }
 
 static_assert(sizeof(DsPipe) + CWL_MAX_DISTILL_ROW_BYTES / kMaxDsCluster + 160 <= 227 * 1024, "the longest row fits a cluster");
-// How the long-row kernel runs: as few blocks a row as hold it in slices of kSliceWanted bytes (three buffers fit), more
-// while the rows do not fill the GPU, down to slices of 8 KB.
-constexpr int kSliceWanted = 66 * 1024;
+// How the long-row kernel runs: as few blocks a row as hold it in slices of kSliceWanted bytes (two buffers fit), more
+// while the rows do not fill the GPU, down to slices of 8 KB.  Half the slice with a third buffer costs more in exchanges than
+// the buffer gives (us, slices up to 66 KB -> up to 104 KB: 2587 rows of 142736 bf16 417 -> 286; 4096 rows of 50000 fp32 298
+// -> 258, of 100000 fp32 635 -> 551, of 25000 fp32 154 -> 133).
+constexpr int kSliceWanted = 104 * 1024;
 PipePlan pipe_plan(int T, int64_t row_bytes) {
   PipePlan plan;
   plan.log2_cta = 0;
