@@ -335,8 +335,9 @@ distill_small_kernel(const DistillParams p) {
 
 // --------------------------------------------------------------------------------------------- the loss alone, many rows
 // Nothing has to stay for a gradient: rows stream through registers as in logprobs.cu, one block of 128 threads a row,
-// seven blocks an SM.  A bit per element in shared memory marks the entries; a vector that holds one (64 of 4000, say) has
+// eight blocks an SM.  A bit per element in shared memory marks the entries; a vector that holds one (64 of 4000, say) has
 // it replaced by -inf before it is summed, so that the mass outside the entries is again a sum of its own.
+// Eight blocks against seven: 16384 rows of 32000 fp16 213 -> 200 us, 1000 rows of 131072 the same 52.
 constexpr int kLossThreads = 128;
 constexpr int kLossWarps = kLossThreads / 32;
 constexpr int kLossBatch = 4;
@@ -367,7 +368,7 @@ __device__ __noinline__ RowStat exact_masked_stat(const uint4* v, const uint32_t
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kLossThreads, 7)
+__global__ void __launch_bounds__(kLossThreads, 8)
 distill_loss_kernel(const DistillParams p, const int mark_words) {
   constexpr int kVec = Elem<T>::kVec;
   pdl_launch_dependents();
