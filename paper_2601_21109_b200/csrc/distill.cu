@@ -335,9 +335,10 @@ distill_small_kernel(const DistillParams p) {
 
 // --------------------------------------------------------------------------------------------- the loss alone, many rows
 // Nothing has to stay for a gradient: rows stream through registers as in logprobs.cu, one block of 128 threads a row,
-// eight blocks an SM.  A bit per element in shared memory marks the entries; a vector that holds one (64 of 4000, say) has
+// seven or eight blocks an SM.  A bit per element in shared memory marks the entries; a vector that holds one (64 of 4000, say) has
 // it replaced by -inf before it is summed, so that the mass outside the entries is again a sum of its own.
-// Eight blocks against seven: 16384 rows of 32000 fp16 213 -> 200 us, 1000 rows of 131072 the same 52.
+// Eight blocks against seven: 16384 rows of 32000 fp16 213 -> 200 us, 4000 rows 61 -> 59; but rows that seven an SM hold at
+// once are spread more evenly that way: 1000 rows of 131072 fp16, back to back, 55 us, with eight 58.
 constexpr int kLossThreads = 128;
 constexpr int kLossWarps = kLossThreads / 32;
 constexpr int kLossBatch = 4;
@@ -367,8 +368,8 @@ __device__ __noinline__ RowStat exact_masked_stat(const uint4* v, const uint32_t
   return a;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kLossThreads, 8)
+template <typename T, int kBlocks>
+__global__ void __launch_bounds__(kLossThreads, kBlocks)
 distill_loss_kernel(const DistillParams p, const int mark_words) {
   constexpr int kVec = Elem<T>::kVec;
   pdl_launch_dependents();
@@ -968,6 +969,17 @@ int resident_clusters(int log2_cta, size_t smem) {
   return n;
 }
 
+template <typename T, int kBlocks>
+cudaError_t launch_loss(const DistillParams& p, bool chained, cudaStream_t st) {
+  const int words = (p.V + 2 * Elem<T>::kVec + 31) / 32;
+  static SharedMemoryGrant grant;
+  const cudaError_t e = grant(distill_loss_kernel<T, kBlocks>);
+  if (e != cudaSuccess) return e;
+  const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
+  return launch_chained(chained, distill_loss_kernel<T, kBlocks>, dim3(rows), dim3(kLossThreads),
+                        sizeof(LossShared) + words * sizeof(uint32_t), st, p, words);
+}
+
 template <typename T>
 cudaError_t launch_distill(const DistillParams& p, cudaStream_t st) {
   const int64_t row_bytes = (int64_t)p.V * sizeof(T);
@@ -978,13 +990,7 @@ cudaError_t launch_distill(const DistillParams& p, cudaStream_t st) {
     return launch_chained(chained, distill_small_kernel<T>, dim3(rows), dim3(kDsThreads), smem, st, p);
   }
   if (p.dlogits == nullptr && p.T >= kLossMinRows) {
-    const int words = (p.V + 2 * Elem<T>::kVec + 31) / 32;
-    static SharedMemoryGrant loss_grant;
-    const cudaError_t e = loss_grant(distill_loss_kernel<T>);
-    if (e != cudaSuccess) return e;
-    const int rows = p.T < (1 << 20) ? p.T : (1 << 20);
-    return launch_chained(chained, distill_loss_kernel<T>, dim3(rows), dim3(kLossThreads), sizeof(LossShared) + words * sizeof(uint32_t),
-                          st, p, words);
+    return p.T <= 7 * 148 ? launch_loss<T, 7>(p, chained, st) : launch_loss<T, 8>(p, chained, st);
   }
   const PipePlan plan = pipe_plan(p.T, row_bytes);
   const size_t smem = (size_t)plan.n_buffers * plan.buffer_bytes + sizeof(DsPipe);

@@ -12,8 +12,8 @@
 // X and dY are read by both: no output of FOLD can be summed before all of d_in / d_out went through SHRINK for its rows.
 //
 // What bounds it: those two passes (R = 64: T = 16384, 4096 -> 11008: 170 us for twice 495 MB, 5.8 TB/s; T = 4096, 57 us).
-// Short ones are bound by the two launches, each with its ramp and its meeting of partial sums (T = 2048, 4096 -> 4096: 23 us;
-// T = 256, 1024 -> 1024, R = 16: 9.8 us), the tensor pipe never (14 % and 30 % of its cycles).  Reading the rows that SHRINK
+// Short ones are bound by the two launches, each with its ramp and its meeting of partial sums (T = 2048, 4096 -> 4096: 24.6
+// us; T = 256, 1024 -> 1024, R = 16: 10 to 12 us on the device), the tensor pipe never (14 % and 30 % of its cycles).  Reading the rows that SHRINK
 // read last first, or SHRINK in waves of rows so that they could still be in L2: 169 -> 169 to 189 us.
 // The K loop of a tile is split over the CTAs of a cluster where the tiles alone do not fill the GPU; the partial
 // accumulators meet in distributed shared memory in a fixed order, so results do not depend on timing.

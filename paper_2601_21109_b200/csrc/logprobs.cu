@@ -10,12 +10,13 @@
 // top K: a few per cent of the row are read a second time (from L2), and what reaches the bound is sorted in shared memory.
 //
 // What bounds it: without alternatives the one pass over the logits (2048 rows of 32000 fp32: 43 us, 6.1 TB/s; 16384 rows
-// of 32000 bf16: 162 us, 6.5 TB/s); with K = 64 the issue slots (16384 rows of 32000 bf16: 263 us, 4.0 TB/s; 12300 warp
+// of 32000 bf16: 162 us, 6.5 TB/s); with K = 64 the issue slots (16384 rows of 32000 bf16: 266 us, 4.0 TB/s; 12300 warp
 // instructions a row, of which 6950 are the pass itself, 2100 the cells and the fixed part of the selection and 3200 the
 // second reads, the 64 places and their sort).  Rows of 500 elements with K = 64: 16384 of them in 193 us.  Few rows are
 // cut up over a cluster: one row of 32000 fp32 with K = 20 in 7.1 us (launch, one pass of 16 KB a block, selection, the
 // leader's merge), 64 bf16 rows in 10 us.
-// A warp a row instead of four (24 rows an SM): 263 -> 350 us; the serial parts of a row then take four times as long.
+// A warp a row instead of four (24 rows an SM): 263 -> 350 us; the serial parts of a row then take four times as long.  Eight
+// blocks an SM instead of seven: 266 -> 271.  Rows cut in two where they do not fill the GPU (777 of 50021 fp32): 32 -> 40.
 #include <cmath>
 
 #include "logits_common.cuh"
