@@ -168,6 +168,15 @@ def test_rows_on_both_sides_of_the_small_blocks(T, V, dtype):
     check(zt, ids, vals, "logprobs", 1.0, w, None, dtype)
 
 
+@pytest.mark.parametrize("T,V,dtype", [(310, 53240, "bf16"), (310, 53257, "f16"), (301, 26619, "f32"), (160, 150001, "bf16"), (165, 100003, "f32")])
+def test_rows_in_the_longest_slices(T, V, dtype):
+    zt = device(rows(V, T, V), dtype, 1)
+    ids, vals = teacher_of(zt.double().cpu().numpy(), 33, "logprobs", 1.0, V)
+    w = np.ones(T, np.float32)
+    w[::7] = 0.0
+    check(zt, ids, vals, "logprobs", 1.0, w, None, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("offset,out_offset", [(1, 1), (3, 0), (0, 5), (6, 7)])
 def test_rows_that_start_anywhere(dtype, offset, out_offset):
