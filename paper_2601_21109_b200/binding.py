@@ -269,16 +269,18 @@ class DeviceChunkTable:
         t.n_chunks.fill_(n)
         return t
 
-    def __setattr__(self, name, value):
-        self.__dict__[name] = value
-        self.__dict__["_c"] = None               # the marshalled struct follows the arrays
+    _c = None                                    # (addresses, marshalled struct) of the last call; not part of the state
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_c"}
 
     def c_struct(self) -> CChunkTable:
+        at = (self.offsets.data_ptr(), self.rank.data_ptr(), self.scale.data_ptr(), self.rung.data_ptr(), self.flags.data_ptr(),
+              self.n_chunks.data_ptr(), self.capacity)
         c = self._c
-        if c is None:
-            c = self.__dict__["_c"] = CChunkTable(_p(self.offsets), _p(self.rank), _p(self.scale), _p(self.rung), _p(self.flags),
-                                                  _p(self.n_chunks), self.capacity)
-        return c
+        if c is None or c[0] != at:              # arrays may be replaced, resized or given other storage at any time
+            c = self._c = (at, CChunkTable(*at))
+        return c[1]
 
     def to_host(self) -> dict:
         n = int(self.n_chunks.item())
