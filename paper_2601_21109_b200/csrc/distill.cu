@@ -170,43 +170,56 @@ __device__ __forceinline__ float merged_probability(const int* ids, const float*
   }
   return seen ? -1.f : sum;
 }
-// m, the mass outside the entries and all of it from the parts of a row (a warp together); a bad row gives m = 0 and NaN
-// masses.  `entries_every`: each that many-th part is a slice's entries.
-__device__ __forceinline__ void row_statistics(const float2* part, int n, int entries_every, float c, float& m, float& s, float& s_row) {
-  const int lane = threadIdx.x & 31;
-  m = -CUDART_INF_F;
-  for (int i = lane; i < n; i += 32) m = max_nan(m, part[i].x);
-  m = key_value(__reduce_max_sync(0xffffffffu, order_key(m)));
-  s = 0.f;
-  float s_in = 0.f;
-  for (int i = lane; i < n; i += 32) {
-    const float2 q = part[i];
-    const float v = q.x == -CUDART_INF_F ? 0.f : q.y * exp2_fast((q.x - m) * c);
-    if (i % entries_every == entries_every - 1) s_in += v; else s += v;
-  }
-  s = warp_sum(s);
-  s_in = warp_sum(s_in);
-  if (bad_max(m)) { m = 0.f; s = CUDART_NAN_F; }
-  s_row = s + s_in;
+// 1 / x within 2^-23, of sums between 1 and 2^30
+__device__ __forceinline__ float inverse(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// What a row's logits come to: its maximum m and S = sum 2^((z - m) c) over all of it, and the same of what lies outside the
+// entries, relative to the largest logit there: however far that lies below the row's maximum, the mass outside has its logarithm
+// and its elements their shares of it.
+struct RowMass {
+  float m, s_row;
+  float m_out, s_out;     // m and 0 where nothing lies outside
+  float scale;            // 2^((m_out - m) c)
+};
+// From the parts outside the entries and of the entries, each relative to its own maximum; a bad row gives m = 0 and NaN masses.
+// An outside that lies below the maximum by more than kMaskedExponent is masked (with the type's lowest value), like -inf.
+__device__ __forceinline__ RowMass row_mass(float m_out, float s_out, float m_in, float s_in, float c) {
+  RowMass r;
+  r.m = max_nan(m_out, m_in);
+  if (bad_max(r.m)) return RowMass{0.f, CUDART_NAN_F, 0.f, CUDART_NAN_F, 1.f};
+  const float below = (m_out - r.m) * c;
+  const bool none = !(below > kMaskedExponent);
+  r.m_out = none ? r.m : m_out;
+  r.s_out = none ? 0.f : s_out;
+  r.scale = none ? 0.f : exp2_fast(below);
+  r.s_row = r.s_out * r.scale + (m_in == -CUDART_INF_F ? 0.f : s_in * exp2_fast((m_in - r.m) * c));
+  return r;
 }
 // This entry's share of the loss (thread 0 adds the rest's), in fp64: the terms nearly cancel where the student is close
 // to the teacher.
-__device__ __forceinline__ double loss_term(const DistillParams& p, int id, float prob, double lp, float z, float p_rest, float m, float s,
-                                            float s_row, int tid) {
+__device__ __forceinline__ double loss_term(const DistillParams& p, int id, float prob, double lp, float z, float p_rest, const RowMass& r,
+                                            int tid) {
   double term = 0.0;
-  const double ln_s = log((double)s_row);
-  if (id >= 0 && !(prob == 0.f)) term = (double)prob * (lp - (((double)z - (double)m) * p.inv_temp_d - ln_s));
-  if (tid == 0 && !(p_rest == 0.f)) term += (double)p_rest * (log((double)p_rest) - (log((double)s) - ln_s));
-  if (tid == 0 && !(s_row == s_row)) term = (double)CUDART_NAN_F;
+  const double ln_s = log((double)r.s_row);
+  if (id >= 0 && !(prob == 0.f)) term = (double)prob * (lp - (((double)z - (double)r.m) * p.inv_temp_d - ln_s));
+  if (tid == 0 && !(p_rest == 0.f)) {
+    const double ln_q_rest = log((double)r.s_out) + ((double)r.m_out - (double)r.m) * p.inv_temp_d - ln_s;
+    term += (double)p_rest * (log((double)p_rest) - ln_q_rest);
+  }
+  if (tid == 0 && !(r.s_row == r.s_row)) term = (double)CUDART_NAN_F;
   return term;
 }
-// outside the entries the gradient is 2^t times this: (total - p_rest / q_rest) / S; with no mass outside there is nothing
-// to scale
-__device__ __forceinline__ float outside_factor(float total, float p_rest, float s, float s_row) {
-  return (s > 0.f ? total - p_rest * (s_row / s) : (s == s ? 0.f : s)) * (1.f / s_row);
+// outside the entries the gradient is 2^((z - m_out) c) times this: total q_v - p_rest q_v / q_rest; with no mass outside
+// there is nothing to scale
+__device__ __forceinline__ float outside_factor(float total, float p_rest, const RowMass& r) {
+  const float k = total * r.scale * inverse(r.s_row) - p_rest * inverse(r.s_out);
+  return r.s_out == 0.f ? 0.f : k;
 }
 __device__ __forceinline__ float entry_gradient(const DistillParams& p, float z, float p_id, float total, float m, float s_row) {
-  return exp2_fast((z - m) * p.c) * (1.f / s_row) * total - p_id;
+  return exp2_fast((z - m) * p.c) * inverse(s_row) * total - p_id;
 }
 
 template <typename T>
@@ -271,45 +284,48 @@ distill_small_kernel(const DistillParams p) {
     if (en.id >= 0) sm[lead + en.id] = Elem<T>::from_float(-CUDART_INF_F);
     __syncthreads();
 
-    // maximum over the row and its entries, then the sums relative to it
-    float m = en.id >= 0 ? en.z : -CUDART_INF_F;
+    // maximum outside the entries and of the entries, then the sums relative to each
+    float m_out = -CUDART_INF_F;
     const uint4* sv = reinterpret_cast<const uint4*>(sm + rs.head + lead);
     for (int i = tid; i < rs.v1; i += kDsThreads) {
       const uint4 q = sv[i];
       const uint32_t words[4] = {q.x, q.y, q.z, q.w};
-      m = max_nan(m, Elem<T>::max_of(words));
+      m_out = max_nan(m_out, Elem<T>::max_of(words));
     }
-    if (tid < rs.own_head) m = max_nan(m, Elem<T>::to_float(sm[lead + tid]));
-    if (tid < rs.own_tail) m = max_nan(m, Elem<T>::to_float(sm[lead + rs.tail_start + tid]));
-    m = key_value(__reduce_max_sync(0xffffffffu, order_key(m)));
-    if (lane == 0) sh.red[wid] = m;
+    if (tid < rs.own_head) m_out = max_nan(m_out, Elem<T>::to_float(sm[lead + tid]));
+    if (tid < rs.own_tail) m_out = max_nan(m_out, Elem<T>::to_float(sm[lead + rs.tail_start + tid]));
+    m_out = key_value(__reduce_max_sync(0xffffffffu, order_key(m_out)));
+    float m_in = key_value(__reduce_max_sync(0xffffffffu, order_key(en.id >= 0 ? en.z : -CUDART_INF_F)));
+    if (lane == 0) { sh.red[wid] = m_out; sh.red2[wid] = m_in; }
     __syncthreads();
-    m = sh.red[0];
-    for (int i = 1; i < kDsWarps; ++i) m = max_nan(m, sh.red[i]);
+    m_out = sh.red[0];
+    m_in = sh.red2[0];
+    for (int i = 1; i < kDsWarps; ++i) {
+      m_out = max_nan(m_out, sh.red[i]);
+      m_in = max_nan(m_in, sh.red2[i]);
+    }
     __syncthreads();
-    const bool bad = bad_max(m);
-    if (bad) m = 0.f;
-    float s = 0.f;
+    const float from = bad_max(m_out) ? 0.f : m_out;
+    float s_out = 0.f;
     for (int i = tid; i < rs.v1; i += kDsThreads) {
       float f[kVec];
       Elem<T>::unpack(sv[i], f);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) s += exp2_fast((f[e] - m) * p.c);
+      for (int e = 0; e < kVec; ++e) s_out += exp2_fast((f[e] - from) * p.c);
     }
-    if (tid < rs.own_head) s += exp2_fast((Elem<T>::to_float(sm[lead + tid]) - m) * p.c);
-    if (tid < rs.own_tail) s += exp2_fast((Elem<T>::to_float(sm[lead + rs.tail_start + tid]) - m) * p.c);
-    s = warp_sum(s);
-    const float s_in_warp = warp_sum(en.p_id >= 0.f ? exp2_fast((en.z - m) * p.c) : 0.f);   // once per distinct id
-    if (lane == 0) { sh.red[wid] = s; sh.red2[wid] = s_in_warp; }
+    if (tid < rs.own_head) s_out += exp2_fast((Elem<T>::to_float(sm[lead + tid]) - from) * p.c);
+    if (tid < rs.own_tail) s_out += exp2_fast((Elem<T>::to_float(sm[lead + rs.tail_start + tid]) - from) * p.c);
+    s_out = warp_sum(s_out);
+    float s_in = warp_sum(en.p_id >= 0.f && !bad_max(m_in) ? exp2_fast((en.z - m_in) * p.c) : 0.f);   // once per distinct id
+    if (lane == 0) { sh.red[wid] = s_out; sh.red2[wid] = s_in; }
     __syncthreads();
-    s = 0.f;
-    float s_in = 0.f;
-    for (int i = 0; i < kDsWarps; ++i) { s += sh.red[i]; s_in += sh.red2[i]; }
-    if (bad) s = CUDART_NAN_F;
-    const float s_row = s + s_in;
+    s_out = 0.f;
+    s_in = 0.f;
+    for (int i = 0; i < kDsWarps; ++i) { s_out += sh.red[i]; s_in += sh.red2[i]; }
+    const RowMass r = row_mass(m_out, s_out, m_in, s_in, p.c);
 
     if (p.loss != nullptr) {
-      const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_rest, m, s, s_row, tid));
+      const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_rest, r, tid));
       if (lane == 0) sh.red_d[wid] = term;
       __syncthreads();
       if (tid == 0) {
@@ -320,14 +336,14 @@ distill_small_kernel(const DistillParams p) {
     }
     if (d != nullptr) {
       const float up = w * p.temperature * (p.dloss != nullptr ? p.dloss[row] : 1.f);
-      const float k_out = outside_factor(en.p_in + en.p_rest, en.p_rest, s, s_row) * up;
+      const float k_out = outside_factor(en.p_in + en.p_rest, en.p_rest, r) * up;
       store_slice<T, kDsThreads>(tid, d, same_phase, rs, [&](int i, float (&f)[kVec]) {
         Elem<T>::unpack(sv[i], f);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) f[e] = exp2_fast((f[e] - m) * p.c) * k_out;
-      }, [&](int i) { return exp2_fast((Elem<T>::to_float(sm[lead + i]) - m) * p.c) * k_out; });
+        for (int e = 0; e < kVec; ++e) f[e] = exp2_fast((f[e] - r.m_out) * p.c) * k_out;
+      }, [&](int i) { return exp2_fast((Elem<T>::to_float(sm[lead + i]) - r.m_out) * p.c) * k_out; });
       __syncthreads();                             // the entries' places now hold 0: put their own values there
-      if (en.p_id >= 0.f) d[en.id] = Elem<T>::from_float(entry_gradient(p, en.z, en.p_id, en.p_in + en.p_rest, m, s_row) * up);
+      if (en.p_id >= 0.f) d[en.id] = Elem<T>::from_float(entry_gradient(p, en.z, en.p_id, en.p_in + en.p_rest, r.m, r.s_row) * up);
     }
     __syncthreads();                               // the next row overwrites the shared arrays
   }
@@ -462,13 +478,15 @@ distill_loss_kernel(const DistillParams p, const int mark_words) {
     finish_entry(p, v_max, (sh.red_d[0] + sh.red_d[1]) + (sh.red_d[2] + sh.red_d[3]), en);
     // all parts together: lanes 0..3 outside the entries, 4..7 the entries
     const int k = lane & (2 * kLossWarps - 1);
-    RowStat part{k < kLossWarps ? sh.part[k].x : sh.m_in[k - kLossWarps], k < kLossWarps ? sh.part[k].y : sh.s_in[k - kLossWarps], 0.f};
-    float m = key_value(__reduce_max_sync(0xffffffffu, order_key(part.m)));
-    rescale(part, m, p.c);
-    const float rest = warp_sum(lane < kLossWarps ? part.S : 0.f);
-    float s = rest, s_row = rest + warp_sum(lane >= kLossWarps && lane < 2 * kLossWarps ? part.S : 0.f);
-    if (bad_max(m)) { m = 0.f; s = CUDART_NAN_F; s_row = CUDART_NAN_F; }
-    const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_rest, m, s, s_row, tid));
+    const bool outside = k < kLossWarps;
+    RowStat part{outside ? sh.part[k].x : sh.m_in[k - kLossWarps], outside ? sh.part[k].y : sh.s_in[k - kLossWarps], 0.f};
+    const float m_out = key_value(__reduce_max_sync(0xffffffffu, order_key(outside ? part.m : -CUDART_INF_F)));
+    const float m_in = key_value(__reduce_max_sync(0xffffffffu, order_key(outside ? -CUDART_INF_F : part.m)));
+    rescale(part, outside ? m_out : m_in, p.c);
+    const float s_out = warp_sum(lane < kLossWarps ? part.S : 0.f);
+    const float s_in = warp_sum(lane >= kLossWarps && lane < 2 * kLossWarps ? part.S : 0.f);
+    const RowMass r = row_mass(m_out, s_out, m_in, s_in, p.c);
+    const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_rest, r, tid));
     __syncthreads();                           // red_d was read
     if (lane == 0) sh.red_d[wid] = term;
     __syncthreads();
@@ -511,6 +529,35 @@ struct DsPipe {
 struct PipePlan {
   int log2_cta, n_buffers, buffer_bytes;
 };
+
+// A row's masses from the parts of its slices, a part a lane of the warp (of eight slices, up to three).  Every sum warp waits
+// for it: a block that has the row to itself reads its entries' part as it stands (2048 rows of 32000 bf16: 48.3 -> 46.4 us).
+__device__ __forceinline__ RowMass row_statistics(const float2* part, int n_cta, float c) {
+  const int lane = threadIdx.x & 31;
+  if (n_cta == 1) {
+    const float2 q = part[lane % kSumWarps], e = part[kSumWarps];
+    const float m_out = key_value(__reduce_max_sync(0xffffffffu, order_key(q.x)));
+    float s = q.x == -CUDART_INF_F ? 0.f : q.y * exp2_fast((q.x - m_out) * c);
+#pragma unroll
+    for (int off = kSumWarps / 2; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+    return row_mass(m_out, s, e.x, e.y, c);
+  }
+  float m_out = -CUDART_INF_F, m_in = -CUDART_INF_F;
+  for (int i = lane; i < n_cta * kParts; i += 32) {
+    const float x = part[i].x;
+    if (i % kParts == kSumWarps) m_in = max_nan(m_in, x); else m_out = max_nan(m_out, x);
+  }
+  m_out = key_value(__reduce_max_sync(0xffffffffu, order_key(m_out)));
+  m_in = key_value(__reduce_max_sync(0xffffffffu, order_key(m_in)));
+  float s_out = 0.f, s_in = 0.f;
+  for (int i = lane; i < n_cta * kParts; i += 32) {
+    const bool entries = i % kParts == kSumWarps;
+    const float2 q = part[i];
+    const float v = q.x == -CUDART_INF_F ? 0.f : q.y * exp2_fast((q.x - (entries ? m_in : m_out)) * c);
+    if (entries) s_in += v; else s_out += v;
+  }
+  return row_mass(m_out, warp_sum(s_out), m_in, warp_sum(s_in), c);
+}
 
 __device__ __forceinline__ void prepare_barrier() { __syncwarp(); asm volatile("bar.sync 1, 128;" ::: "memory"); }
 __device__ __forceinline__ void finish_barrier() { __syncwarp(); asm volatile("bar.sync 2, 128;" ::: "memory"); }
@@ -734,13 +781,12 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       const float dl = p.dloss != nullptr ? __ldg(p.dloss + row) : 1.f;
       const bool ok = mbar_wait_cluster(xchg_bar(cslot.at), cslot.phase, abort_flag);
       __syncwarp();
-      float m, s, s_row;
-      row_statistics(sh.slot[cslot.at], n_cta * kParts, kParts, p.c, m, s, s_row);
+      const RowMass r = row_statistics(sh.slot[cslot.at], n_cta, p.c);
       EntryRest e{0.0, -1, 0.f, -1.f, 0.f};
       if (ft < p.K) e = sh.entry[slot.at][ft];
       const float p_in = sh.mass[slot.at][0], p_rest = sh.mass[slot.at][1];
       if (p.loss != nullptr && cta == 0) {
-        const double term = warp_sum(loss_term(p, e.id, e.p, e.lp, ft < p.K ? sh.z[cslot.at][ft] : 0.f, p_rest, m, s, s_row, ft));
+        const double term = warp_sum(loss_term(p, e.id, e.p, e.lp, ft < p.K ? sh.z[cslot.at][ft] : 0.f, p_rest, r, ft));
         if (lane == 0) sh.red_loss[fw] = term;
         finish_barrier();
         if (ft == 0 && ok) {
@@ -751,7 +797,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       stored_wait(slot.at);
       if (p.dlogits != nullptr && e.p_id >= 0.f && ok && *abort_flag == 0) {
         T* d = reinterpret_cast<T*>(p.dlogits) + (int64_t)row * p.ld_d;
-        d[e.id] = Elem<T>::from_float(entry_gradient(p, e.z, e.p_id, p_in + p_rest, m, s_row) * (w * p.temperature * dl));
+        d[e.id] = Elem<T>::from_float(entry_gradient(p, e.z, e.p_id, p_in + p_rest, r.m, r.s_row) * (w * p.temperature * dl));
       }
     }
   } else if (wid == kPipeThreads / 32 - 1) {
@@ -857,10 +903,10 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       const bool ok = mbar_wait_cluster(xchg_bar(cslot.at), cslot.phase, abort_flag);
       __syncwarp();
       if (d != nullptr && ok && *abort_flag == 0) {
-        float m, s, s_row;
-        row_statistics(sh.slot[cslot.at], n_cta * kParts, kParts, p.c, m, s, s_row);
+        const RowMass r = row_statistics(sh.slot[cslot.at], n_cta, p.c);
+        const float m = r.m_out;                                   // what the elements outside are relative to
         const float rest = sh.mass[slot.at][1];
-        const float k_out = outside_factor(sh.mass[slot.at][0] + rest, rest, s, s_row) * up;
+        const float k_out = outside_factor(sh.mass[slot.at][0] + rest, rest, r) * up;
         if (fabsf(m) <= kOrdinaryLogit && p.ordinary != 0) {
           const float M = m * p.c;
           const float k = k_out * exp2_fast(-fmaf(m, p.c, -M));

@@ -1,0 +1,88 @@
+"""cwl_distill_topk where the student leaves next to nothing, or nothing, outside the teacher's entries: against the
+definition in 64 bits, in logarithms.
+
+Tolerances (u = 2^-24) are those of the sums: S within eps = u (4 + 3 log2 V + V/256 + 40) relative.  ln q_rest is ln S_out
+- ln S_row and an exact distance of two maxima, so the rest's share of the loss is within p_rest 2 eps and what p_rest
+itself is off, 20 u, times its logarithm.  An outside gradient is p_rest 2^t / S_out: relative 2 eps + u (30 + 3 |t|), t its
+distance from the largest logit outside in powers of two, and 20 u / p_rest from p_rest."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2601_21109_b200 import binding as cwl
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HALF_ULP = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+TINY = {"f32": 2.0 ** -126, "bf16": 2.0 ** -126, "f16": 2.0 ** -24}
+# one small block a row; a pipelined block a row; pairs and eights of blocks a row; (without gradients) the stream of many rows
+FORMS = [(40, 1003), (300, 12007), (3, 32003), (165, 60007), (745, 12007)]
+
+
+def definition(zt, ids, vals, mode, tau):
+    """loss [T], gradient [T, V] for weight 1, the masses outside, and their logarithm for the student; fp64"""
+    z, i, u = zt.double() / tau, ids.long(), vals.double()
+    logq = torch.log_softmax(z, 1)
+    p = torch.softmax(u / tau, 1) if mode == "logits" else u.exp()
+    lp = torch.log_softmax(u / tau, 1) if mode == "logits" else u
+    rest = (1.0 - p.sum(1)).clamp(min=0.0) if mode == "logprobs" else torch.zeros_like(p[:, 0])
+    held = torch.zeros(z.shape, dtype=torch.bool, device=z.device).scatter_(1, i, True)
+    out = logq.masked_fill(held, float("-inf"))
+    lq_rest = torch.logsumexp(out, 1)
+    loss = tau * tau * (torch.where(p > 0, p * (lp - logq.gather(1, i)), 0.0).sum(1)
+                        + torch.where(rest > 0, rest * (rest.log() - lq_rest), 0.0))
+    grad = logq.exp() * (p.sum(1) + rest)[:, None]
+    share = torch.where(held, 0.0, (out - lq_rest[:, None]).exp())
+    grad = tau * (grad.scatter_add(1, i, -p) - share * rest[:, None])
+    return loss, grad, rest, lq_rest, share
+
+
+def eps_of(V):
+    return U * (4 + 3 * np.log2(V + 1) + V / 256 + 40)
+
+
+@pytest.mark.parametrize("mode", ["logits", "logprobs"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("gap,tau", [(60.0, 1.0), (87.0, 1.0), (88.5, 1.0), (104.0, 1.0), (130.0, 2.0), (700.0, 1.0), (10000.0, 1.0), (12.0, 0.1)])
+def test_outside_mass_far_below_the_entries(gap, tau, dtype, mode):
+    K = 8
+    tau = float(np.float32(tau))
+    for T, V in FORMS:
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(V + int(gap))
+        z = torch.randn(T, V, device="cuda", generator=gen) * tau - gap
+        ids = torch.rand(T, V, device="cuda", generator=gen).topk(K, dim=1).indices.to(torch.int32)
+        z.scatter_(1, ids.long(), torch.rand(T, K, device="cuda", generator=gen) * 3 * tau)
+        zt = z.to(DT[dtype])
+        vals = torch.randn(T, K, device="cuda", generator=gen)
+        if mode == "logprobs":
+            vals = torch.log_softmax(vals, 1) + np.log(0.8)            # a fifth of the teacher's mass is outside
+        loss, grad = cwl.cwl_distill_topk(zt, ids, vals, teacher=mode, temperature=tau)
+        alone, _ = cwl.cwl_distill_topk(zt, ids, vals, teacher=mode, temperature=tau, want_grad=False)
+        rl, rg, rest, lq_rest, share = definition(zt, ids, vals, mode, tau)
+        eps = eps_of(V)
+        mag = 12.0 + vals.double().abs().amax(1)                       # of the entries' logarithms
+        tol = tau * tau * (2 * eps + 12 * U * mag + torch.where(rest > 0, 20 * U * (1 + (rest.log() - lq_rest).abs()), 0.0)) + 4 * U * rl.abs()
+        for got in (loss, alone):
+            assert bool(torch.isfinite(got).all())
+            assert float(((got.double() - rl).abs() - tol).max()) <= 0
+        held = share == 0
+        top = zt.double().masked_fill(torch.zeros_like(held).scatter_(1, ids.long(), True), float("-inf")).amax(1, keepdim=True)
+        far = ((zt.double() - top).abs() / tau * 1.4427).clamp(max=200.0)
+        tol = rg.abs() * (2 * eps + U * (30 + 3 * far) + torch.where(rest > 0, 20 * U / rest, 0.0)[:, None])
+        tol += rg.abs() * HALF_ULP[dtype] * 1.01 + TINY[dtype] * 1.01
+        tol.scatter_add_(1, ids.long(), tau * (U * (14 + 4 * (vals.double().abs() + np.log(K + 1))) + 6 * eps))
+        assert bool(torch.isfinite(grad).all())
+        assert float(((grad.double() - rg).abs() - tol).max()) <= 0
+
+
+def test_one_outcome_outside_at_the_edge_of_fp32():
+    """Eight entries at 0 and one logit at -87 or below: with a teacher that leaves nothing to it its gradient is q itself."""
+    ids = torch.arange(8, dtype=torch.int32, device="cuda")[None]
+    for at in (-80.0, -87.0, -88.0, -95.0, -103.0, -200.0):
+        z = torch.zeros(1, 9, device="cuda")
+        z[0, 8] = at
+        loss, grad = cwl.cwl_distill_topk(z, ids, torch.zeros(1, 8, device="cuda"), teacher="logits")
+        assert abs(float(loss)) <= 1e-6 and float(grad[0, :8].abs().max()) <= 1e-6
+        assert abs(float(grad[0, 8]) - np.exp(at) / 8) <= 1e-5 * np.exp(at) / 8 + 2.0 ** -126
