@@ -415,6 +415,8 @@ cwl_status cwl_token_logprobs(const void* logits, cwl_dtype dtype, int64_t ld_lo
  *   CWL_TEACHER_LOGPROBS   p_j = exp(u_j), u_j log-probabilities of the tempered teacher (cwl_token_logprobs gives them);
  *                          what is left, p_rest = max(0, 1 - sum_j p_j), is one more outcome, matched against
  *                          q_rest = sum of q outside the entries
+ *                          (the two count as 0 where neither exceeds 2^-20: a record of every token that the row allows
+ *                          leaves the rounding of its log-probabilities, not a rest)
  *   loss[t]      = weight[t] tau^2 ( sum_j p_j ln(p_j / q_{id_j}) + p_rest ln(p_rest / q_rest) )
  *   dlogits[t,v] = dloss[t] d loss[t] / d z_v
  *                = dloss[t] weight[t] tau ( q_v (sum_j p_j + p_rest) - p_v - [v not among the entries] p_rest q_v / q_rest )

@@ -198,6 +198,14 @@ __device__ __forceinline__ RowMass row_mass(float m_out, float s_out, float m_in
   r.s_row = r.s_out * r.scale + (m_in == -CUDART_INF_F ? 0.f : s_in * exp2_fast((m_in - r.m) * c));
   return r;
 }
+// What the teacher leaves to the rest.  1 - sum p of a record that holds everything is not 0 but its rounding: an fp32 log-
+// probability u of a few operations is off by a few 2^-24 (1 + |u|), and sum p (1 + |u|) is at most 1 + ln 128 < 6.  A remainder
+// that small is taken for none where the student has no more than that outside the entries either; its logarithm there may be
+// -inf or that of a mask, and would make an infinite loss, or any, of the rounding.
+constexpr float kRecordRounding = 1.f / (1 << 20);
+__device__ __forceinline__ float rest_of(float p_rest, const RowMass& r) {
+  return p_rest <= kRecordRounding && r.s_out * r.scale <= kRecordRounding * r.s_row ? 0.f : p_rest;
+}
 // This entry's share of the loss (thread 0 adds the rest's), in fp64: the terms nearly cancel where the student is close
 // to the teacher.
 __device__ __forceinline__ double loss_term(const DistillParams& p, int id, float prob, double lp, float z, float p_rest, const RowMass& r,
@@ -323,9 +331,10 @@ distill_small_kernel(const DistillParams p) {
     s_in = 0.f;
     for (int i = 0; i < kDsWarps; ++i) { s_out += sh.red[i]; s_in += sh.red2[i]; }
     const RowMass r = row_mass(m_out, s_out, m_in, s_in, p.c);
+    const float rest = rest_of(en.p_rest, r);
 
     if (p.loss != nullptr) {
-      const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_rest, r, tid));
+      const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, rest, r, tid));
       if (lane == 0) sh.red_d[wid] = term;
       __syncthreads();
       if (tid == 0) {
@@ -336,14 +345,14 @@ distill_small_kernel(const DistillParams p) {
     }
     if (d != nullptr) {
       const float up = w * p.temperature * (p.dloss != nullptr ? p.dloss[row] : 1.f);
-      const float k_out = outside_factor(en.p_in + en.p_rest, en.p_rest, r) * up;
+      const float k_out = outside_factor(en.p_in + rest, rest, r) * up;
       store_slice<T, kDsThreads>(tid, d, same_phase, rs, [&](int i, float (&f)[kVec]) {
         Elem<T>::unpack(sv[i], f);
 #pragma unroll
         for (int e = 0; e < kVec; ++e) f[e] = exp2_fast((f[e] - r.m_out) * p.c) * k_out;
       }, [&](int i) { return exp2_fast((Elem<T>::to_float(sm[lead + i]) - r.m_out) * p.c) * k_out; });
       __syncthreads();                             // the entries' places now hold 0: put their own values there
-      if (en.p_id >= 0.f) d[en.id] = Elem<T>::from_float(entry_gradient(p, en.z, en.p_id, en.p_in + en.p_rest, r.m, r.s_row) * up);
+      if (en.p_id >= 0.f) d[en.id] = Elem<T>::from_float(entry_gradient(p, en.z, en.p_id, en.p_in + rest, r.m, r.s_row) * up);
     }
     __syncthreads();                               // the next row overwrites the shared arrays
   }
@@ -486,7 +495,7 @@ distill_loss_kernel(const DistillParams p, const int mark_words) {
     const float s_out = warp_sum(lane < kLossWarps ? part.S : 0.f);
     const float s_in = warp_sum(lane >= kLossWarps && lane < 2 * kLossWarps ? part.S : 0.f);
     const RowMass r = row_mass(m_out, s_out, m_in, s_in, p.c);
-    const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_rest, r, tid));
+    const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, rest_of(en.p_rest, r), r, tid));
     __syncthreads();                           // red_d was read
     if (lane == 0) sh.red_d[wid] = term;
     __syncthreads();
@@ -784,7 +793,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       const RowMass r = row_statistics(sh.slot[cslot.at], n_cta, p.c);
       EntryRest e{0.0, -1, 0.f, -1.f, 0.f};
       if (ft < p.K) e = sh.entry[slot.at][ft];
-      const float p_in = sh.mass[slot.at][0], p_rest = sh.mass[slot.at][1];
+      const float p_in = sh.mass[slot.at][0], p_rest = rest_of(sh.mass[slot.at][1], r);
       if (p.loss != nullptr && cta == 0) {
         const double term = warp_sum(loss_term(p, e.id, e.p, e.lp, ft < p.K ? sh.z[cslot.at][ft] : 0.f, p_rest, r, ft));
         if (lane == 0) sh.red_loss[fw] = term;
@@ -905,7 +914,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       if (d != nullptr && ok && *abort_flag == 0) {
         const RowMass r = row_statistics(sh.slot[cslot.at], n_cta, p.c);
         const float m = r.m_out;                                   // what the elements outside are relative to
-        const float rest = sh.mass[slot.at][1];
+        const float rest = rest_of(sh.mass[slot.at][1], r);
         const float k_out = outside_factor(sh.mass[slot.at][0] + rest, rest, r) * up;
         if (fabsf(m) <= kOrdinaryLogit && p.ordinary != 0) {
           const float M = m * p.c;

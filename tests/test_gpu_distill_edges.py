@@ -86,3 +86,44 @@ def test_one_outcome_outside_at_the_edge_of_fp32():
         loss, grad = cwl.cwl_distill_topk(z, ids, torch.zeros(1, 8, device="cuda"), teacher="logits")
         assert abs(float(loss)) <= 1e-6 and float(grad[0, :8].abs().max()) <= 1e-6
         assert abs(float(grad[0, 8]) - np.exp(at) / 8) <= 1e-5 * np.exp(at) / 8 + 2.0 ** -126
+
+
+RECORDS = [(64, 100, 100, None), (200, 128, 128, None), (64, 40, 40, None), (300, 12007, 64, 64), (300, 12007, 100, 20), (3, 32003, 128, 128),
+           (165, 60007, 64, 33), (760, 12007, 64, 50), (800, 8200, 128, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mask", [float("-inf"), -1.0e4, "lowest"])
+@pytest.mark.parametrize("T,V,K,allowed", RECORDS)
+def test_a_record_of_every_allowed_token_has_no_rest(T, V, K, allowed, mask, dtype):
+    """The entries hold every token that the row allows: what 1 - sum p shows of a rest is the rounding of the record, and the
+    student, which equals its teacher, has no loss.  Tolerance: the log-probabilities of the record and of the student are each
+    within eps_S + 6 u (|ln p| + ln K), weighted by p."""
+    for tau in (1.0, 0.7, 2.0):
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(T + V)
+        z = torch.randn(T, V, device="cuda", generator=gen) * torch.rand(T, 1, device="cuda", generator=gen) * 3
+        if allowed is not None:
+            keep = torch.rand(T, V, device="cuda", generator=gen).topk(allowed, dim=1).indices
+            held = torch.zeros(T, V, dtype=torch.bool, device="cuda").scatter_(1, keep, True)
+            z.masked_fill_(~held, torch.finfo(DT[dtype]).min if mask == "lowest" else mask)
+        zt = z.to(DT[dtype])
+        o = cwl.cwl_token_logprobs(zt, top_k=K, temperature=tau)
+        loss, grad = cwl.cwl_distill_topk(zt, o.top_ids, o.top_logprobs, teacher="logprobs", temperature=tau)
+        alone, _ = cwl.cwl_distill_topk(zt, o.top_ids, o.top_logprobs, teacher="logprobs", temperature=tau, want_grad=False)
+        tol = tau * tau * (2 * eps_of(V) + 12 * U * (1 + 2 * np.log(K)))
+        for got in (loss, alone):
+            assert bool(torch.isfinite(got).all()) and float(got.abs().max()) <= tol
+        assert bool(torch.isfinite(grad).all()) and float(grad.abs().max()) <= tol / tau + HALF_ULP[dtype] * tol / tau
+
+
+def test_a_rest_that_the_record_can_tell_from_none_is_kept():
+    """A teacher that leaves 1e-5 outside, to a student that allows nothing there: the divergence is infinite."""
+    for T, V in FORMS:
+        z = torch.full((T, V), float("-inf"), device="cuda")
+        z[:, :4] = torch.randn(T, 4, device="cuda")
+        ids = torch.arange(4, dtype=torch.int32, device="cuda").repeat(T, 1)
+        vals = torch.log_softmax(z[:, :4], 1) + np.log1p(-1e-5)
+        loss, grad = cwl.cwl_distill_topk(z, ids, vals, teacher="logprobs")
+        alone, _ = cwl.cwl_distill_topk(z, ids, vals, teacher="logprobs", want_grad=False)
+        assert bool(torch.isinf(loss).all()) and bool(torch.isinf(alone).all()) and bool((grad[:, 4:] == 0).all())
