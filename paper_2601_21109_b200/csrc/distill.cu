@@ -214,8 +214,10 @@ __device__ __forceinline__ double loss_term(const DistillParams& p, int id, floa
   const double ln_s = log((double)r.s_row);
   if (id >= 0 && !(prob == 0.f)) term = (double)prob * (lp - (((double)z - (double)r.m) * p.inv_temp_d - ln_s));
   if (tid == 0 && !(p_rest == 0.f)) {
-    const double ln_q_rest = log((double)r.s_out) + ((double)r.m_out - (double)r.m) * p.inv_temp_d - ln_s;
-    term += (double)p_rest * (log((double)p_rest) - ln_q_rest);
+    // the scale as S_row has it while it counts there: its rounding then falls out between the entries' terms and this one
+    const double ln_out = r.scale > 0x1p-60f ? log((double)r.s_out * (double)r.scale)
+                                             : log((double)r.s_out) + ((double)r.m_out - (double)r.m) * p.inv_temp_d;
+    term += (double)p_rest * (log((double)p_rest) - (ln_out - ln_s));
   }
   if (tid == 0 && !(r.s_row == r.s_row)) term = (double)CUDART_NAN_F;
   return term;
