@@ -434,8 +434,8 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
       for (int u = 0; u < kLpBatch; ++u) { w[4 * u] = q[u].x; w[4 * u + 1] = q[u].y; w[4 * u + 2] = q[u].z; w[4 * u + 3] = q[u].w; }
       const float batch_max = Elem<T>::max_of(w);
       run.template take_words<T, 4 * kLpBatch>(w, batch_max, p.c);
+      seg_max = max_nan(seg_max, batch_max);
       if (p.top_k > 0) {
-        seg_max = max_nan(seg_max, batch_max);
         if (--left == 0 || b == n_batch - 1) {
           const uint32_t key = seg * per_seg * kLpBatchVecs + tid < nv ? order_key(seg_max) : 0u;
           sh.cell[seg * kLpThreads + tid] = key;
@@ -459,7 +459,7 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
       sh.half[kLpThreads + tid] = half_key[1];
     }
     // the warp's maximum first, one rescaling each, then plain sums; the same across the warps
-    RowStat a = run.done(p.c);
+    RowStat a = run.done_at_maximum(p.top_k > 0 ? key_value(max(half_key[0], half_key[1])) : seg_max, p.c);
     if (run.exact_needed) a = exact_stat<T>(reinterpret_cast<const uint4*>(z + rs.head) + rs.v0, tid, kLpThreads, nv, p.c);
 #pragma unroll 1
     for (int k = 0; k < 2; ++k) {                        // scalars before the first vector and after the last

@@ -1,0 +1,33 @@
+"""cwl_token_logprobs at the ends of its range: near-certain tokens, the smallest temperatures, numbers next to zero."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2601_21109_b200 import binding as cwl
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,V", [(2000, 32000), (3000, 4099), (40, 32000), (1, 50021)])
+def test_no_log_probability_is_positive(dtype, T, V):
+    """m is the row's maximum and the largest term of S is 1 itself, so S >= 1 and no log-probability exceeds 0; a near-certain
+    token's is ln S of an S of 1 and little more: what it loses are the terms' roundings beside the 1 (as many as a thread has,
+    each half a spacing at most) and 2 u of its own."""
+    for tau in (1.0, 0.6):
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(T + V)
+        z = torch.randn(T, V, device="cuda", generator=gen) * 0.7
+        at = torch.randint(0, V, (T, 1), device="cuda", generator=gen)
+        z.scatter_(1, at, 12.0 + 14.0 * torch.rand(T, 1, device="cuda", generator=gen))
+        zt = z.to(DT[dtype])
+        t = zt.float().argmax(1).to(torch.int32)
+        o = cwl.cwl_token_logprobs(zt, t, top_k=3, temperature=tau)
+        assert float(o.logprob.max()) <= 0 and float(o.top_logprobs.max()) <= 0
+        d = (zt.double() - zt.double().amax(1, keepdim=True)) / float(np.float32(tau))
+        ref = -torch.log(torch.exp(d).sum(1))
+        # the row's small terms as a whole are off by their own relative error (dist up to 40 powers of two)
+        tol = (V / 256 + 40) * U + ref.abs() * U * (8 + 3 * 60)
+        assert float(((o.logprob.double() - ref).abs() - tol).max()) <= 0
