@@ -377,6 +377,8 @@ struct LossShared {
   float red[kLossWarps];
   float2 part[kLossWarps];                     // (m, S) of every warp's elements outside the entries
   float m_in[kLossWarps], s_in[kLossWarps];    // and of its entries
+  int id[CWL_MAX_TOP_K];
+  int repeated;                                // some id occurs twice
 };
 
 template <typename T>
@@ -405,6 +407,7 @@ distill_loss_kernel(const DistillParams p, const int mark_words) {
   uint32_t* marks = reinterpret_cast<uint32_t*>(ds_raw + sizeof(LossShared));   // element i of a row: bit i - head + kVec
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   for (int i = tid; i < mark_words; i += kLossThreads) marks[i] = 0;
+  if (tid == 0) sh.repeated = 0;
   pdl_wait();
   __syncthreads();
 
@@ -419,14 +422,20 @@ distill_loss_kernel(const DistillParams p, const int mark_words) {
     Entry en;
     load_entry(p, row, tid, en);
     check_entry(p, en);
-    bool counts = false;                       // first to mark its id
+    bool counts = false;                       // the first entry of its id
     const int pos = en.id - rs.head + kVec;
+    if (tid < p.K) sh.id[tid] = en.id;
     if (en.id >= 0) {
       en.z = Elem<T>::load(z + en.id);
       const uint32_t bit = 1u << (pos & 31);
       counts = (atomicOr(marks + (pos >> 5), bit) & bit) == 0;
+      if (!counts) sh.repeated = 1;
     }
     __syncthreads();                           // all marks are set
+    if (sh.repeated != 0) {                    // which of two marked it depends on timing, and so would the order of the sums
+      counts = en.id >= 0;
+      for (int k = 0; k < tid && counts; ++k) counts = sh.id[k] != en.id;
+    }
 
     RunningSum run;
     run.start(p.ordinary != 0);
@@ -486,6 +495,7 @@ distill_loss_kernel(const DistillParams p, const int mark_words) {
     if (lane == 0) { sh.red_d[wid] = weight; sh.m_in[wid] = mw; sh.s_in[wid] = sw; }
     __syncthreads();                           // every thread is done with the marks
     if (en.id >= 0) marks[pos >> 5] = 0;
+    if (tid == 0) sh.repeated = 0;
     finish_entry(p, v_max, (sh.red_d[0] + sh.red_d[1]) + (sh.red_d[2] + sh.red_d[3]), en);
     // all parts together: lanes 0..3 outside the entries, 4..7 the entries
     const int k = lane & (2 * kLossWarps - 1);

@@ -127,3 +127,19 @@ def test_a_rest_that_the_record_can_tell_from_none_is_kept():
         loss, grad = cwl.cwl_distill_topk(z, ids, vals, teacher="logprobs")
         alone, _ = cwl.cwl_distill_topk(z, ids, vals, teacher="logprobs", want_grad=False)
         assert bool(torch.isinf(loss).all()) and bool(torch.isinf(alone).all()) and bool((grad[:, 4:] == 0).all())
+
+
+def test_repeated_ids_give_the_same_bits_every_time():
+    """Many entries name the same few tokens, from different warps: which of them counts the token must not depend on timing."""
+    for T, V in ((745, 12007), (2000, 8200), (300, 12007), (40, 1003)):
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(V)
+        z = torch.randn(T, V, device="cuda", generator=gen)
+        ids = torch.randint(0, V, (T, 40), device="cuda", generator=gen, dtype=torch.int32).repeat(1, 4)[:, :128].contiguous()
+        ids = ids.gather(1, torch.rand(T, 128, device="cuda", generator=gen).argsort(1))
+        z.scatter_(1, ids.long(), torch.rand(T, 128, device="cuda", generator=gen) * 6)
+        vals = torch.randn(T, 128, device="cuda", generator=gen)
+        first, _ = cwl.cwl_distill_topk(z, ids, vals, want_grad=False)
+        for _ in range(60):
+            again, _ = cwl.cwl_distill_topk(z, ids, vals, want_grad=False)
+            assert torch.equal(first, again)
