@@ -1012,16 +1012,22 @@ PipePlan pipe_plan(int T, int64_t row_bytes) {
   return plan;
 }
 
-// Clusters of long-row blocks (one block an SM) that fit the GPU at once; the rows are dealt to that many.
+// Clusters of long-row blocks that fit the GPU at once, one block an SM; the rows are dealt to that many.  Asked with all of an
+// SM's shared memory: the plans' own shares go down to a fifth of it, but 800 threads of 72 registers leave no room for a second.
 template <typename T>
-int resident_clusters(int log2_cta, size_t smem) {
-  static std::atomic<int> known[4];                // by log2_cta; every size of shared memory here takes a whole SM
-  const int seen = known[log2_cta].load(std::memory_order_relaxed);
-  if (seen > 0) return seen;
+int resident_clusters(int log2_cta) {
+  constexpr int kDevices = 32;
+  static std::atomic<int> known[kDevices][4];      // by device and log2_cta
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) dev = kDevices;
+  if (dev < kDevices) {
+    const int seen = known[dev][log2_cta].load(std::memory_order_relaxed);
+    if (seen > 0) return seen;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(148u >> log2_cta << log2_cta);
   cfg.blockDim = dim3(kPipeThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = 227 * 1024;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
   attr.val.clusterDim.x = 1u << log2_cta; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
@@ -1032,7 +1038,7 @@ int resident_clusters(int log2_cta, size_t smem) {
     cudaGetLastError();
     return 148 >> log2_cta;
   }
-  known[log2_cta].store(n, std::memory_order_relaxed);
+  if (dev < kDevices) known[dev][log2_cta].store(n, std::memory_order_relaxed);
   return n;
 }
 
@@ -1064,7 +1070,7 @@ cudaError_t launch_distill(const DistillParams& p, cudaStream_t st) {
   static SharedMemoryGrant grant;
   const cudaError_t e = grant(distill_pipe_kernel<T>);
   if (e != cudaSuccess) return e;
-  const int clusters = resident_clusters<T>(plan.log2_cta, smem);
+  const int clusters = resident_clusters<T>(plan.log2_cta);
   const int rows = p.T < clusters ? p.T : clusters;
   return launch_clusters(chained, 1 << plan.log2_cta, distill_pipe_kernel<T>, dim3(rows << plan.log2_cta), dim3(kPipeThreads), smem, st,
                          p, plan);
