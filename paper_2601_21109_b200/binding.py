@@ -608,6 +608,17 @@ def cwl_apply_noalloc(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor
     return Y
 
 
+def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
+    """Launches go to the current device: every tensor that a kernel is given has to be there."""
+    here = torch._C._cuda_getDevice()
+    for t in tensors:
+        assert t is None or t.get_device() == here, f"a tensor on {t.device}, the current device is cuda:{here}"
+
+
+def _check_status_word(status_word: Optional[torch.Tensor]) -> None:
+    assert status_word is None or (status_word.dtype == torch.int32 and status_word.numel() >= 1)
+
+
 class TokenLogprobs:
     """What cwl_token_logprobs writes for up to `T` rows, in one device allocation: ``lse``, ``entropy`` and (with
     targets) ``logprob`` fp32 [T], ``top_ids`` int32 and ``top_logprobs`` fp32 [T, top_k].  A decode loop keeps one."""
@@ -638,6 +649,8 @@ def cwl_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = N
         assert out.T == T and out.top_k == top_k and (out.logprob is None) == (targets is None)
     if targets is not None:
         assert targets.is_cuda and targets.dtype == torch.int32 and targets.is_contiguous() and targets.numel() == T
+    _check_status_word(status_word)
+    _on_current_device(logits, targets, out.lse, status_word)
     _check("cwl_token_logprobs", lib().cwl_token_logprobs(
         logits.data_ptr(), _DTYPES[logits.dtype], ld if T > 1 else max(V, ld), T, V, _p(targets), temperature, top_k, *out._ptrs,
         _p(status_word), _stream_ptr(stream)))
@@ -678,6 +691,8 @@ def cwl_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_va
         dlogits, ld_d = torch.empty_like(logits) if ld == V else logits.new_empty_strided((T, V), (ld, 1)), ld
     if T == 1:                                   # a single row's stride says nothing
         ld, ld_teacher, ld_d = max(V, ld), max(K, ld_teacher), max(V, ld_d)
+    _check_status_word(status_word)
+    _on_current_device(logits, teacher_ids, teacher_values, weight, dloss, loss, dlogits, status_word)
     _check("cwl_distill_topk", lib().cwl_distill_topk(
         logits.data_ptr(), _DTYPES[logits.dtype], ld, T, V, teacher_ids.data_ptr(), teacher_values.data_ptr(), ld_teacher, K,
         TEACHER_MODES[teacher], temperature, _p(weight), _p(dloss), _p(loss), _p(dlogits), ld_d, _p(status_word),
@@ -714,6 +729,10 @@ def cwl_apply_grads(X: torch.Tensor, dY: torch.Tensor, A: torch.Tensor, B: torch
         assert dB.is_cuda and dB.dtype == dA.dtype and dB.shape == (R, d_out) and u == 1
     if workspace is None:
         workspace = torch.empty(cwl_apply_grads_workspace_bytes(T, d_in, d_out, R), dtype=torch.uint8, device=X.device)
+    else:
+        assert workspace.dtype == torch.uint8 and workspace.is_contiguous()
+    _check_status_word(status_word)
+    _on_current_device(X, dY, A, B, dA, dB, workspace, status_word, table.offsets, table.rank, table.scale, table.flags, table.n_chunks)
     if T == 1:                                   # a single row's stride says nothing
         ldx, lddy = max(d_in, ldx), max(d_out, lddy)
     _check("cwl_apply_grads", lib().cwl_apply_grads(
