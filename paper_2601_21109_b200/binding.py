@@ -619,6 +619,13 @@ def _check_status_word(status_word: Optional[torch.Tensor]) -> None:
     assert status_word is None or (status_word.dtype == torch.int32 and status_word.numel() >= 1)
 
 
+def _row_stride(t: torch.Tensor) -> int:
+    """Distance of the rows of a matrix whose rows are contiguous; the stride of a dimension of one element says nothing."""
+    (rows, cols), (ld, unit) = t.shape, t.stride()
+    assert unit == 1 or cols == 1
+    return ld if rows > 1 else cols
+
+
 class TokenLogprobs:
     """What cwl_token_logprobs writes for up to `T` rows, in one device allocation: ``lse``, ``entropy`` and (with
     targets) ``logprob`` fp32 [T], ``top_ids`` int32 and ``top_logprobs`` fp32 [T, top_k].  A decode loop keeps one."""
@@ -641,8 +648,8 @@ def cwl_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = N
     likely tokens of softmax(logits / temperature); logits fp32, bf16 or fp16 [T, V] on the device."""
     assert logits.dtype in _DTYPES
     T, V = logits.shape
-    ld, unit = logits.stride()
-    assert logits.is_cuda and unit == 1
+    ld = _row_stride(logits)
+    assert logits.is_cuda
     if out is None:
         out = TokenLogprobs(T, top_k, targets is not None, logits.device)
     else:
@@ -652,7 +659,7 @@ def cwl_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = N
     _check_status_word(status_word)
     _on_current_device(logits, targets, out.lse, status_word)
     _check("cwl_token_logprobs", lib().cwl_token_logprobs(
-        logits.data_ptr(), _DTYPES[logits.dtype], ld if T > 1 else max(V, ld), T, V, _p(targets), temperature, top_k, *out._ptrs,
+        logits.data_ptr(), _DTYPES[logits.dtype], ld, T, V, _p(targets), temperature, top_k, *out._ptrs,
         _p(status_word), _stream_ptr(stream)))
     return out
 
@@ -670,12 +677,11 @@ def cwl_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_va
     assert logits.dtype in _DTYPES
     T, V = logits.shape
     K = teacher_ids.shape[1]
-    ld, unit = logits.stride()
-    ld_teacher, t_unit = teacher_ids.stride()
-    assert logits.is_cuda and unit == 1
-    assert teacher_ids.is_cuda and teacher_ids.dtype == torch.int32 and teacher_ids.shape[0] == T and t_unit == 1
+    ld, ld_teacher = _row_stride(logits), _row_stride(teacher_ids)
+    assert logits.is_cuda
+    assert teacher_ids.is_cuda and teacher_ids.dtype == torch.int32 and teacher_ids.shape[0] == T
     assert teacher_values.is_cuda and teacher_values.dtype == torch.float32 and teacher_values.shape == teacher_ids.shape
-    assert teacher_values.stride() == (ld_teacher, t_unit)
+    assert _row_stride(teacher_values) == ld_teacher
     assert weight is None or (weight.is_cuda and weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == T)
     assert dloss is None or (dloss.is_cuda and dloss.dtype == torch.float32 and dloss.is_contiguous() and dloss.numel() == T)
     if loss is not None:
@@ -684,13 +690,11 @@ def cwl_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_va
         loss = teacher_values.new_empty(T)
     ld_d = 0
     if dlogits is not None:
-        ld_d, d_unit = dlogits.stride()
-        assert dlogits.is_cuda and dlogits.dtype == logits.dtype and dlogits.shape == (T, V) and d_unit == 1
+        ld_d = _row_stride(dlogits)
+        assert dlogits.is_cuda and dlogits.dtype == logits.dtype and dlogits.shape == (T, V)
     elif want_grad:
         # rows as far apart as the logits': they then start at the same offset from a 16-byte boundary
         dlogits, ld_d = torch.empty_like(logits) if ld == V else logits.new_empty_strided((T, V), (ld, 1)), ld
-    if T == 1:                                   # a single row's stride says nothing
-        ld, ld_teacher, ld_d = max(V, ld), max(K, ld_teacher), max(V, ld_d)
     _check_status_word(status_word)
     _on_current_device(logits, teacher_ids, teacher_values, weight, dloss, loss, dlogits, status_word)
     _check("cwl_distill_topk", lib().cwl_distill_topk(
@@ -713,28 +717,26 @@ def cwl_apply_grads(X: torch.Tensor, dY: torch.Tensor, A: torch.Tensor, B: torch
     and the output's gradient dY (bf16); fp32 or bf16, of the type of ``dA`` and ``dB`` where they are given."""
     (T, d_in), (rows, d_out), (a_rows, R) = X.shape, dY.shape, A.shape
     assert rows == T and a_rows == d_in and B.shape == (R, d_out)
-    (ldx, ux), (lddy, uy), (lda, ua), (ldb, ub) = X.stride(), dY.stride(), A.stride(), B.stride()
-    assert ux == uy == ua == ub == 1 and X.is_cuda and dY.is_cuda and A.is_cuda and B.is_cuda
+    ldx, lddy, lda, ldb = _row_stride(X), _row_stride(dY), _row_stride(A), _row_stride(B)
+    assert X.is_cuda and dY.is_cuda and A.is_cuda and B.is_cuda
     assert X.dtype == dY.dtype == A.dtype == B.dtype == torch.bfloat16
     if dA is None:
         dtype = grad_dtype if dB is None else dB.dtype
         dA, ldda = torch.empty_like(A, dtype=dtype) if lda == R else A.new_empty((d_in, R), dtype=dtype), R
     else:
-        ldda, u = dA.stride()
-        assert dA.is_cuda and dA.dtype in _DTYPES and dA.shape == (d_in, R) and u == 1
+        ldda = _row_stride(dA)
+        assert dA.is_cuda and dA.dtype in _DTYPES and dA.shape == (d_in, R)
     if dB is None:
         dB, lddb = torch.empty_like(B, dtype=dA.dtype) if ldb == d_out else B.new_empty((R, d_out), dtype=dA.dtype), d_out
     else:
-        lddb, u = dB.stride()
-        assert dB.is_cuda and dB.dtype == dA.dtype and dB.shape == (R, d_out) and u == 1
+        lddb = _row_stride(dB)
+        assert dB.is_cuda and dB.dtype == dA.dtype and dB.shape == (R, d_out)
     if workspace is None:
         workspace = torch.empty(cwl_apply_grads_workspace_bytes(T, d_in, d_out, R), dtype=torch.uint8, device=X.device)
     else:
         assert workspace.dtype == torch.uint8 and workspace.is_contiguous()
     _check_status_word(status_word)
     _on_current_device(X, dY, A, B, dA, dB, workspace, status_word, table.offsets, table.rank, table.scale, table.flags, table.n_chunks)
-    if T == 1:                                   # a single row's stride says nothing
-        ldx, lddy = max(d_in, ldx), max(d_out, lddy)
     _check("cwl_apply_grads", lib().cwl_apply_grads(
         X.data_ptr(), ldx, dY.data_ptr(), lddy, A.data_ptr(), lda, B.data_ptr(), ldb, T, d_in, d_out, R, table.c_struct(),
         int(window), WINDOW_CENTRED if centred else WINDOW_CAUSAL, dA.data_ptr(), ldda, dB.data_ptr(), lddb, _DTYPES[dA.dtype],
