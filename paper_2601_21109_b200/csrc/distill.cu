@@ -242,7 +242,7 @@ distill_small_kernel(const DistillParams p) {
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   pdl_wait();
 
-  for (int row = blockIdx.x; row < p.T; row += gridDim.x) {
+  for (uint32_t row = blockIdx.x; row < (uint32_t)p.T; row += gridDim.x) {     // unsigned: T may be 2^31 - 1
     const T* z = reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.ld;
     T* d = p.dlogits != nullptr ? reinterpret_cast<T*>(p.dlogits) + (int64_t)row * p.ld_d : nullptr;
     const RowSlice rs = row_slice<T>(z, p.V, 0, 0);

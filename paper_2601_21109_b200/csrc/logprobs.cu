@@ -75,9 +75,9 @@ template <typename T>
 __device__ __noinline__ void append_ties_in_order(LpShared& sh, const T* z, int e0, int e1, uint32_t key, int have, int need) {
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   int found = 0;
-  for (int base = e0; base < e1 && found < need; base += kLpThreads) {
-    const int i = base + tid;
-    const bool is = i < e1 && order_key(Elem<T>::load(z + i)) == key;
+  for (uint32_t base = e0; base < (uint32_t)e1 && found < need; base += kLpThreads) {    // unsigned: e1 may be 2^31 - 1
+    const uint32_t i = base + tid;
+    const bool is = i < (uint32_t)e1 && order_key(Elem<T>::load(z + i)) == key;
     const unsigned bal = __ballot_sync(0xffffffffu, is);
     if (lane == 0) sh.warp_count[wid] = __popc(bal);
     __syncthreads();
@@ -199,7 +199,7 @@ __device__ __noinline__ uint32_t exact_bound_and_candidates(LpShared& sh, const 
   for (int shift = 24; shift >= 0; shift -= 8) {
     for (int i = tid; i < 256; i += kLpThreads) sh.hist[i] = 0;
     __syncthreads();
-    for (int i = e0 + tid; i < e1; i += kLpThreads) {
+    for (uint32_t i = e0 + tid; i < (uint32_t)e1; i += kLpThreads) {
       const uint32_t key = order_key(Elem<T>::load(z + i));
       if ((key & mask) == prefix) atomicAdd(&sh.hist[(key >> shift) & 255u], 1u);
     }
@@ -214,7 +214,7 @@ __device__ __noinline__ uint32_t exact_bound_and_candidates(LpShared& sh, const 
   const uint32_t thr = prefix;                         // an element's own key, and fewer than `want` lie above it
   if (tid == 0) { sh.n_cand = 0; sh.n_ties = 0; }
   __syncthreads();
-  for (int i = e0 + tid; i < e1; i += kLpThreads) {
+  for (uint32_t i = e0 + tid; i < (uint32_t)e1; i += kLpThreads) {
     const float v = Elem<T>::load(z + i);
     const uint32_t key = order_key(v);
     if (key > thr) sh.cand[atomicAdd(&sh.n_cand, 1)] = rank_key(key, i);
@@ -296,7 +296,7 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
   // a bound below every element's key (fewer nonempty cells than wanted): everything is above it, -inf too
   const bool all = thr < kKeyOfMinusInf;
   float bound = all ? -CUDART_INF_F : key_value(thr);
-  const int n_work = sh.n_hits * per_cell;               // at most 1024 cells times nv / 1024 + 4 vectors each: below 2^24
+  const int n_work = sh.n_hits * per_cell;               // at most 1024 cells of nv / 1024 + 4 vectors each: below 2^29
   const float inv_per_cell = 1.f / (float)per_cell;
   const uint4 pad = make_uint4(Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked(), Elem<T>::masked());
   // The few vectors that hold anything are gathered (where the cells and their maxima were, which have served) and their
@@ -310,7 +310,7 @@ __device__ __forceinline__ int select_candidates(LpShared& sh, const T* z, const
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
       const int w = w0 + u * kLpThreads;
-      int h = (int)((float)w * inv_per_cell);            // w / per_cell, off by at most one
+      int h = (int)((float)w * inv_per_cell);            // w / per_cell, below 1024: off by at most one
       int j = w - h * per_cell;
       if (j < 0) { --h; j += per_cell; }
       if (j >= per_cell) { ++h; j -= per_cell; }
@@ -394,11 +394,11 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
   const int n_cta = 1 << log2_cta;
   const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int cta = log2_cta > 0 ? (int)cluster_rank() : 0;
-  const int n_rows_at_once = gridDim.x >> log2_cta;
+  const uint32_t n_rows_at_once = gridDim.x >> log2_cta;
   if (log2_cta > 0) cluster_barrier_arrive();          // waited for before the leader's shared memory is written
   pdl_wait();
 
-  for (int row = blockIdx.x >> log2_cta; row < p.T; row += n_rows_at_once) {
+  for (uint32_t row = blockIdx.x >> log2_cta; row < (uint32_t)p.T; row += n_rows_at_once) {   // unsigned: T may be 2^31 - 1
     const T* z = reinterpret_cast<const T*>(p.logits) + (int64_t)row * p.ld;
     const RowSlice rs = row_slice<T>(z, p.V, cta, log2_cta);
     float z_target = 0.f;
