@@ -396,6 +396,7 @@ typedef enum { CWL_F32 = 0, CWL_BF16 = 1, CWL_F16 = 2 } cwl_dtype;
  *   top_logprobs[t, :] their log-probabilities.
  * -inf logits contribute nothing (an alternative may be one, with log-probability -inf, when fewer than top_k tokens
  * are allowed).  A row with NaN or +inf, or of -inf only, gives NaN everywhere and ids of -1.
+ * A temperature below 2^-127 counts as 2^-127.
  *   logits   DEV [T, V] of `dtype`, row stride ld_logits >= V; rows may start at any element
  *   targets  DEV int32 [T] or NULL; a negative entry means no token (logprob 0); one >= V gives NaN and flags
  *            CWL_ERR_INVALID_ARG in *status_word
@@ -425,7 +426,7 @@ cwl_status cwl_token_logprobs(const void* logits, cwl_dtype dtype, int64_t ld_lo
  * is kept by its logarithm, however small; it is 0 where every logit outside the entries is -inf, or lies 1e30 tau ln 2 or more
  * below the row's maximum (masks of the type's lowest value): +inf loss then, if p_rest is not 0, and no gradient there.  A row
  * with NaN or +inf logits, or of -inf only, gives NaN.  An id that occurs twice counts with the sum of its p.  An id >= V
- * counts as padding and flags CWL_ERR_INVALID_ARG in *status_word.
+ * counts as padding and flags CWL_ERR_INVALID_ARG in *status_word.  A temperature below 2^-127 counts as 2^-127.
  *   logits          DEV [T, V] of `dtype`, row stride ld_logits >= V; rows may start at any element
  *   teacher_ids     DEV int32 [T, K], teacher_values DEV fp32 [T, K], both with row stride ld_teacher >= K
  *   weight          DEV fp32 [T] or NULL (all 1);  dloss  DEV fp32 [T] or NULL (all 1): the upstream gradient of loss[t]

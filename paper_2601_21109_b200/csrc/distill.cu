@@ -1095,8 +1095,10 @@ extern "C" cwl_status cwl_distill_topk(const void* logits, cwl_dtype dtype, int6
   if (ld_logits < V || ld_teacher < K || (dlogits != nullptr && ld_dlogits < V)) return CWL_ERR_SHAPE;
   if (reinterpret_cast<uintptr_t>(logits) % es != 0 || reinterpret_cast<uintptr_t>(dlogits) % es != 0) return CWL_ERR_SHAPE;
   if (dlogits == logits && ld_dlogits != ld_logits) return CWL_ERR_SHAPE;
-  cwl::DistillParams p{logits, ld_logits, T, V, teacher_ids, teacher_values, ld_teacher, K, (int)mode, temperature,
-                       (float)(1.4426950408889634074 / (double)temperature), (float)(1.0 / (double)temperature), 1.0 / (double)temperature, cwl::ordinary_temperature(temperature) ? 1 : 0, weight, dloss,
+  const float tau = cwl::usable_temperature(temperature);
+  cwl::DistillParams p{logits, ld_logits, T, V, teacher_ids, teacher_values, ld_teacher, K, (int)mode, tau,
+                       (float)(1.4426950408889634074 / (double)tau), (float)(1.0 / (double)tau), 1.0 / (double)tau,
+                       cwl::ordinary_temperature(tau) ? 1 : 0, weight, dloss,
                        loss, dlogits, ld_dlogits, status_word, cwl::training_wait_limit(), cwl::training_withhold()};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   switch (dtype) {

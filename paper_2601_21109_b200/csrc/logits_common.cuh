@@ -328,6 +328,8 @@ __device__ __noinline__ RowStat exact_stat(const uint4* v, int first, int stride
   }
   return a;
 }
+// the temperature that is calculated with: its reciprocal has to be an fp32 number, times log2 e too
+inline float usable_temperature(float t) { return t < 0x1p-127f ? 0x1p-127f : t; }
 inline bool ordinary_temperature(float t) { return t >= 0.01f && t <= 100.f; }
 
 // order-preserving map of a float to 32 bits; -0 and +0 are equal, a NaN (as max_nan makes them) comes above +inf

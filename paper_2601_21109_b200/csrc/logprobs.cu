@@ -598,8 +598,9 @@ extern "C" cwl_status cwl_token_logprobs(const void* logits, cwl_dtype dtype, in
   if ((targets == nullptr) != (logprob == nullptr)) return CWL_ERR_INVALID_ARG;
   if (ld_logits < V) return CWL_ERR_SHAPE;
   if (reinterpret_cast<uintptr_t>(logits) % cwl::elem_size(dtype) != 0) return CWL_ERR_SHAPE;
-  cwl::LogprobParams p{logits, ld_logits, T, V, targets, (float)(1.4426950408889634074 / (double)temperature),
-                       (float)(1.0 / (double)temperature), cwl::ordinary_temperature(temperature) ? 1 : 0, top_k, logprob, lse, entropy, top_ids, top_logprobs, status_word};
+  const float tau = cwl::usable_temperature(temperature);
+  cwl::LogprobParams p{logits, ld_logits, T, V, targets, (float)(1.4426950408889634074 / (double)tau), (float)(1.0 / (double)tau),
+                       cwl::ordinary_temperature(tau) ? 1 : 0, top_k, logprob, lse, entropy, top_ids, top_logprobs, status_word};
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   switch (dtype) {
     case CWL_F32: CWL_CUDA_TRY(cwl::launch_logprobs<float>(p, st)); break;

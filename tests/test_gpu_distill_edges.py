@@ -143,3 +143,17 @@ def test_repeated_ids_give_the_same_bits_every_time():
         for _ in range(60):
             again, _ = cwl.cwl_distill_topk(z, ids, vals, want_grad=False)
             assert torch.equal(first, again)
+
+
+@pytest.mark.parametrize("temperature", [1.2e-38, 1e-39, 1e-42])
+@pytest.mark.parametrize("mode", ["logits", "logprobs"])
+def test_the_smallest_temperatures(mode, temperature):
+    """Student and teacher put all mass on the same token: nothing to learn; gradients scale with the temperature."""
+    for T, V in FORMS:
+        z = torch.randn(T, V, device="cuda")
+        z[:, 9] = 8.0
+        ids = torch.tensor([[9, 4, 6]], dtype=torch.int32, device="cuda").repeat(T, 1)
+        vals = torch.tensor([[8.0, 1.0, 0.0]] if mode == "logits" else [[0.0, -1e30, -2e30]], device="cuda").repeat(T, 1)
+        loss, grad = cwl.cwl_distill_topk(z, ids, vals, teacher=mode, temperature=temperature)
+        alone, _ = cwl.cwl_distill_topk(z, ids, vals, teacher=mode, temperature=temperature, want_grad=False)
+        assert bool((loss == 0).all()) and bool((alone == 0).all()) and bool((grad == 0).all())

@@ -31,3 +31,23 @@ def test_no_log_probability_is_positive(dtype, T, V):
         # the row's small terms as a whole are off by their own relative error (dist up to 40 powers of two)
         tol = (V / 256 + 40) * U + ref.abs() * U * (8 + 3 * 60)
         assert float(((o.logprob.double() - ref).abs() - tol).max()) <= 0
+
+
+@pytest.mark.parametrize("temperature", [1.2e-38, 1e-39, 1e-42, 1.5e-45, 3.0e38])
+@pytest.mark.parametrize("T,V", [(3, 20011), (400, 20011), (5, 200)])
+def test_the_smallest_and_largest_temperatures(temperature, T, V):
+    """All mass on the largest logits, dealt evenly to those that are equal; or on every allowed token alike."""
+    z = torch.randn(T, V, device="cuda")
+    z[:, 3], z[:, 150], z[:, 7] = 9.0, 9.0, float("-inf")
+    t = torch.tensor([3, 150, 8] * T, dtype=torch.int32, device="cuda")[:T]
+    o = cwl.cwl_token_logprobs(z, t, top_k=3, temperature=temperature)
+    if temperature < 1:
+        want = torch.where(t == 8, float("-inf"), -float(np.log(2.0)))
+        assert torch.allclose(o.entropy, torch.full_like(o.entropy, float(np.log(2.0))), rtol=1e-6)
+        assert bool((o.top_ids[:, :2] == torch.tensor([3, 150], dtype=torch.int32, device="cuda")).all())
+        assert bool((o.top_logprobs[:, 2] < -1e30).all())
+        at = t != 8
+        assert torch.allclose(o.logprob[at], want[at].float(), rtol=1e-6) and bool((o.logprob[~at] < -1e30).all())
+    else:
+        assert torch.allclose(o.logprob, torch.full_like(o.logprob, -float(np.log(V - 1))), rtol=1e-5)
+        assert torch.allclose(o.entropy, torch.full_like(o.entropy, float(np.log(V - 1))), rtol=1e-5)
