@@ -35,6 +35,7 @@ constexpr int kMaxVecs = 256;         // vectors that reach the bound, gathered 
 constexpr int kMaxTies = 256;         // logits equal to the bound kept for sorting
 constexpr int kMaxLpCluster = 8;
 constexpr uint32_t kKeyOfMinusInf = 0x007FFFFFu;
+constexpr uint32_t kKeyOfMinusZero = 0x7FFFFFFFu;      // no element's: -0 and 0 share the next one
 
 struct LogprobParams {
   const void* logits; int64_t ld; int T, V;
@@ -112,7 +113,8 @@ __device__ __forceinline__ uint32_t cell_bound(const uint32_t* half, int want) {
   hi = __reduce_max_sync(0xffffffffu, hi);
   lo = __reduce_min_sync(0xffffffffu, lo);
   const int first = 31 - __clz((int)(hi ^ lo));          // -1 when all keys are equal
-  if (lo >= kKeyOfMinusInf && __popc(__ballot_sync(0xffffffffu, k[0] == lo)) >= 8) {
+  // (above -2^-149 that is 0, whose key is not the next one: the search below finds its bound)
+  if (lo >= kKeyOfMinusInf && lo + 1 != kKeyOfMinusZero && __popc(__ballot_sync(0xffffffffu, k[0] == lo)) >= 8) {
     int above = 0;
 #pragma unroll
     for (int i = 0; i < n; ++i) above += k[i] > lo;

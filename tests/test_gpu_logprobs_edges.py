@@ -51,3 +51,15 @@ def test_the_smallest_and_largest_temperatures(temperature, T, V):
     else:
         assert torch.allclose(o.logprob, torch.full_like(o.logprob, -float(np.log(V - 1))), rtol=1e-5)
         assert torch.allclose(o.entropy, torch.full_like(o.entropy, float(np.log(V - 1))), rtol=1e-5)
+
+
+def test_zeros_above_a_row_of_the_smallest_negative_number():
+    """More zeros than are wanted, all in a few threads' elements, in a row otherwise full of -2^-149: the zeros come first, the
+    lowest indices of them."""
+    for T in (3, 400):
+        V, K = 8192, 64
+        z = torch.full((T, V), -(2.0 ** -149), device="cuda")
+        zeros = torch.cat([torch.arange(c * 512, c * 512 + 20) for c in range(16)])        # five vectors of each batch
+        z[:, zeros.cuda()] = 0.0
+        o = cwl.cwl_token_logprobs(z, top_k=K)
+        assert bool((o.top_ids == zeros[:K].to(torch.int32).cuda()).all())
