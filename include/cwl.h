@@ -421,8 +421,8 @@ cwl_status cwl_token_logprobs(const void* logits, cwl_dtype dtype, int64_t ld_lo
  *   loss[t]      = weight[t] tau^2 ( sum_j p_j ln(p_j / q_{id_j}) + p_rest ln(p_rest / q_rest) )
  *   dlogits[t,v] = dloss[t] d loss[t] / d z_v
  *                = dloss[t] weight[t] tau ( q_v (sum_j p_j + p_rest) - p_v - [v not among the entries] p_rest q_v / q_rest )
- * An entry with a negative id is padding.  Rows of weight 0 give loss 0 and gradient 0 and are not read; so do rows
- * without entries under CWL_TEACHER_LOGITS.  -inf student logits have q = 0 (loss +inf if the teacher wants one).  q_rest
+ * An entry with a negative id is padding.  Rows of weight 0 give loss 0 and gradient 0 and are not read; rows without
+ * entries under CWL_TEACHER_LOGITS give the same, whatever their logits are.  -inf student logits have q = 0 (loss +inf if the teacher wants one).  q_rest
  * is kept by its logarithm, however small; it is 0 where every logit outside the entries is -inf, or lies 1e30 tau ln 2 or more
  * below the row's maximum (masks of the type's lowest value): +inf loss then, if p_rest is not 0, and no gradient there.  A row
  * with NaN or +inf logits, or of -inf only, gives NaN.  An id that occurs twice counts with the sum of its p.  An id >= V

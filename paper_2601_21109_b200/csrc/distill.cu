@@ -206,10 +206,12 @@ constexpr float kRecordRounding = 1.f / (1 << 20);
 __device__ __forceinline__ float rest_of(float p_rest, const RowMass& r) {
   return p_rest <= kRecordRounding && r.s_out * r.scale <= kRecordRounding * r.s_row ? 0.f : p_rest;
 }
+// No entries, and no rest: the row's loss and gradient are 0 whatever its logits are.
+__device__ __forceinline__ bool nothing_taught(float p_in, float p_rest) { return p_in + p_rest == 0.f; }
 // This entry's share of the loss (thread 0 adds the rest's), in fp64: the terms nearly cancel where the student is close
 // to the teacher.
-__device__ __forceinline__ double loss_term(const DistillParams& p, int id, float prob, double lp, float z, float p_rest, const RowMass& r,
-                                            int tid) {
+__device__ __forceinline__ double loss_term(const DistillParams& p, int id, float prob, double lp, float z, float p_in, float p_rest,
+                                            const RowMass& r, int tid) {
   double term = 0.0;
   const double ln_s = log((double)r.s_row);
   if (id >= 0 && !(prob == 0.f)) term = (double)prob * (lp - (((double)z - (double)r.m) * p.inv_temp_d - ln_s));
@@ -219,7 +221,7 @@ __device__ __forceinline__ double loss_term(const DistillParams& p, int id, floa
                                              : log((double)r.s_out) + ((double)r.m_out - (double)r.m) * p.inv_temp_d;
     term += (double)p_rest * (log((double)p_rest) - (ln_out - ln_s));
   }
-  if (tid == 0 && !(r.s_row == r.s_row)) term = (double)CUDART_NAN_F;
+  if (tid == 0 && !(r.s_row == r.s_row) && !nothing_taught(p_in, p_rest)) term = (double)CUDART_NAN_F;
   return term;
 }
 // outside the entries the gradient is 2^((z - m_out) c) times this: total q_v - p_rest q_v / q_rest; with no mass outside
@@ -284,6 +286,11 @@ distill_small_kernel(const DistillParams p) {
     if (tid < p.K) sh.p[tid] = en.p;
     cp_async_wait_all();
     __syncthreads();                               // row and entries are in shared memory
+    if (nothing_taught(en.p_in, en.p_rest)) {
+      if (d != nullptr) zero_slice<T, kDsThreads>(tid, d, same_phase, rs);
+      if (p.loss != nullptr && tid == 0) p.loss[row] = 0.f;
+      continue;
+    }
 
     // lift the entries out of the row
     if (en.id >= 0) {
@@ -336,7 +343,7 @@ distill_small_kernel(const DistillParams p) {
     const float rest = rest_of(en.p_rest, r);
 
     if (p.loss != nullptr) {
-      const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, rest, r, tid));
+      const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_in, rest, r, tid));
       if (lane == 0) sh.red_d[wid] = term;
       __syncthreads();
       if (tid == 0) {
@@ -507,7 +514,7 @@ distill_loss_kernel(const DistillParams p, const int mark_words) {
     const float s_out = warp_sum(lane < kLossWarps ? part.S : 0.f);
     const float s_in = warp_sum(lane >= kLossWarps && lane < 2 * kLossWarps ? part.S : 0.f);
     const RowMass r = row_mass(m_out, s_out, m_in, s_in, p.c);
-    const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, rest_of(en.p_rest, r), r, tid));
+    const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_in, rest_of(en.p_rest, r), r, tid));
     __syncthreads();                           // red_d was read
     if (lane == 0) sh.red_d[wid] = term;
     __syncthreads();
@@ -807,7 +814,7 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       if (ft < p.K) e = sh.entry[slot.at][ft];
       const float p_in = sh.mass[slot.at][0], p_rest = rest_of(sh.mass[slot.at][1], r);
       if (p.loss != nullptr && cta == 0) {
-        const double term = warp_sum(loss_term(p, e.id, e.p, e.lp, ft < p.K ? sh.z[cslot.at][ft] : 0.f, p_rest, r, ft));
+        const double term = warp_sum(loss_term(p, e.id, e.p, e.lp, ft < p.K ? sh.z[cslot.at][ft] : 0.f, p_in, p_rest, r, ft));
         if (lane == 0) sh.red_loss[fw] = term;
         finish_barrier();
         if (ft == 0 && ok) {
@@ -926,9 +933,11 @@ distill_pipe_kernel(const DistillParams p, const PipePlan plan) {
       if (d != nullptr && ok && *abort_flag == 0) {
         const RowMass r = row_statistics(sh.slot[cslot.at], n_cta, p.c);
         const float m = r.m_out;                                   // what the elements outside are relative to
-        const float rest = rest_of(sh.mass[slot.at][1], r);
-        const float k_out = outside_factor(sh.mass[slot.at][0] + rest, rest, r) * up;
-        if (fabsf(m) <= kOrdinaryLogit && p.ordinary != 0) {
+        const float p_in = sh.mass[slot.at][0], rest = rest_of(sh.mass[slot.at][1], r);
+        const float k_out = outside_factor(p_in + rest, rest, r) * up;
+        if (nothing_taught(p_in, rest)) {
+          zero_slice<T, kSumThreads>(st, d, same_phase, rs);
+        } else if (fabsf(m) <= kOrdinaryLogit && p.ordinary != 0) {
           const float M = m * p.c;
           const float k = k_out * exp2_fast(-fmaf(m, p.c, -M));
           const uint64_t c2 = pair(p.c, p.c), minus_m = pair(-M, -M), k2 = pair(k, k), zero = pair(0.f, 0.f);

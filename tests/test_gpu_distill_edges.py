@@ -157,3 +157,21 @@ def test_the_smallest_temperatures(mode, temperature):
         loss, grad = cwl.cwl_distill_topk(z, ids, vals, teacher=mode, temperature=temperature)
         alone, _ = cwl.cwl_distill_topk(z, ids, vals, teacher=mode, temperature=temperature, want_grad=False)
         assert bool((loss == 0).all()) and bool((alone == 0).all()) and bool((grad == 0).all())
+
+
+def test_rows_without_entries_teach_nothing_whatever_they_hold():
+    """Teacher logits, every entry padding: loss and gradient are 0, of a row with NaN or +inf logits or none allowed too."""
+    for T, V in FORMS:
+        z = torch.randn(T, V, device="cuda")
+        z[0, 5], z[1, 7], z[2] = float("nan"), float("inf"), float("-inf")
+        ids = torch.full((T, 6), -1, dtype=torch.int32, device="cuda")
+        vals = torch.full((T, 6), float("nan"), device="cuda")
+        if T > 5:
+            ids[5:, 2] = 11
+            vals[5:, 2] = 1.0
+        for dlogits in (None, z.clone()):
+            loss, grad = cwl.cwl_distill_topk(z, ids, vals, dlogits=dlogits)
+            alone, _ = cwl.cwl_distill_topk(z, ids, vals, want_grad=False)
+            n = min(T, 5)
+            assert bool((loss[:n] == 0).all()) and bool((alone[:n] == 0).all()) and bool((grad[:n] == 0).all())
+            assert bool(torch.isfinite(loss).all()) and bool((loss[n:] > 0).all()) and torch.allclose(loss, alone, rtol=1e-5, atol=0)
