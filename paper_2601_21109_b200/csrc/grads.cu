@@ -23,6 +23,7 @@
 // B K-major, as they lie in memory.  FOLD reads X / dY M-major (their columns are the output rows) and G / H' N-major.
 // Every wait is bounded: when one runs out the CTA raises CWL_ERR_TIMEOUT, stores nothing and still meets its cluster (whose
 // other CTAs may store what lacks its part).
+#include "cluster.cuh"
 #include "cwl_common.cuh"
 #include "gate.cuh"
 #include "tcgen05_common.cuh"
@@ -92,27 +93,6 @@ __device__ __forceinline__ uint32_t grad_idesc(int n, int a_mn, int b_mn) {
   return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) |
          ((uint32_t)(kGM >> 4) << 24);
 }
-__device__ __forceinline__ uint32_t grad_cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void grad_cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void grad_cluster_barrier_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void grad_cluster_barrier_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ uint32_t grad_peer(uint32_t addr, uint32_t cta) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
-  return r;
-}
-__device__ __forceinline__ void st_peer_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
-__device__ __forceinline__ void st_peer_b32(uint32_t addr, uint32_t v) {
-  asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
-}
 __device__ __forceinline__ void store8(void* out, int64_t at, int f32, const float4& a, const float4& b) {
   if (f32) {
     float4* o = reinterpret_cast<float4*>(reinterpret_cast<float*>(out) + at);
@@ -164,7 +144,7 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
 
   // which tile, which share of its K loop
   const int split = p.split;
-  const int cta = split > 1 ? (int)grad_cluster_rank() : 0;
+  const int cta = split > 1 ? (int)cluster_rank() : 0;
   int tile = blockIdx.x / split;
   int side = p.first;
   if (tile >= p.n_tiles[side]) { tile -= p.n_tiles[side]; side ^= 1; }
@@ -193,7 +173,7 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  if (split > 1 && !p.meet_in_ring) grad_cluster_barrier_arrive();
+  if (split > 1 && !p.meet_in_ring) cluster_barrier_arrive();
   // SHRINK waits here for the launch ahead, and only then lets FOLD be placed: a FOLD that runs therefore knows that what
   // came before SHRINK is complete.  It reads X and dY at once; all that SHRINK writes, and its own outputs, wait below.
   if (kPhase == PHASE_SHRINK) {
@@ -348,10 +328,10 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
     // the CTAs.  Layouts are such that a warp's stores are contiguous: [column group of 4][rows][4] and [column][128 rows].
     if (p.meet_in_ring) {                                // over the ring, once it is idle in the whole cluster
       tc_fence_before();
-      grad_cluster_barrier();
+      cluster_barrier();
       tc_fence_after();
     } else {
-      grad_cluster_barrier_wait();                       // the peers run (they arrived at their start)
+      cluster_barrier_wait();                       // the peers run (they arrived at their start)
     }
     const int tile_m = kGM * n_acc;
     const int share = (by_rows ? tile_m : p.R) / split;
@@ -362,7 +342,7 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
         const int at_row = acc * kGM + row;
         if (by_rows) {
           const int owner = at_row / share;
-          const uint32_t to = grad_peer(meet, owner) + (uint32_t)(cta * part + (at_row - owner * share) * 4) * 4u;
+          const uint32_t to = peer_shared(meet, owner) + (uint32_t)(cta * part + (at_row - owner * share) * 4) * 4u;
           for (int c = 0; c < p.R; c += 32) {
             uint32_t v[32];
             columns(acc, c, v);
@@ -377,13 +357,13 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
             columns(acc, c, v);
             const int n = min(32, p.R - c);
             int owner = c / share, left = share - (c - owner * share);
-            uint32_t to = grad_peer(meet, owner) + (uint32_t)(cta * part + (share - left) * tile_m + at_row) * 4u;
+            uint32_t to = peer_shared(meet, owner) + (uint32_t)(cta * part + (share - left) * tile_m + at_row) * 4u;
 #pragma unroll
             for (int j = 0; j < 32; ++j) {
               if (j < n) {
                 if (left == 0) {
                   left = share;
-                  to = grad_peer(meet, ++owner) + (uint32_t)(cta * part + at_row) * 4u;
+                  to = peer_shared(meet, ++owner) + (uint32_t)(cta * part + at_row) * 4u;
                 }
                 st_peer_b32(to, v[j]);
                 to += (uint32_t)tile_m * 4u;
@@ -395,7 +375,7 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
       }
       tc_fence_before();
     }
-    grad_cluster_barrier();                              // this CTA's shares have arrived, and it may leave when it is done
+    cluster_barrier();                              // this CTA's shares have arrived, and it may leave when it is done
     if (*abort_flag == 0) {
       const float* in = reinterpret_cast<const float*>(base_ptr + p.meet_off);
       // eight numbers of an output row a thread

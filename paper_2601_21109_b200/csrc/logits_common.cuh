@@ -6,6 +6,7 @@
 #include <cuda_fp16.h>
 #include <math_constants.h>
 
+#include "cluster.cuh"
 #include "cwl_common.cuh"
 
 namespace cwl {
@@ -370,29 +371,6 @@ __device__ __forceinline__ RowSlice row_slice(const T* z, int V, int cta, int lo
   s.e0 = cta == 0 ? 0 : s.head + s.v0 * Elem<T>::kVec;
   s.e1 = cta == n_cta - 1 ? V : s.head + s.v1 * Elem<T>::kVec;
   return s;
-}
-
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_barrier() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_barrier_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_barrier_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// address of this shared-memory object in another CTA of the cluster
-__device__ __forceinline__ uint32_t peer_shared(const void* p, uint32_t cta) {
-  uint32_t r;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(cta));
-  return r;
-}
-__device__ __forceinline__ void st_peer_u64(uint32_t addr, unsigned long long v) {
-  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
-}
-__device__ __forceinline__ void st_peer_f32(uint32_t addr, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
 }
 
 // Launch in clusters of `cluster` CTAs, chained to the launch ahead like launch_chained.  A kernel that executes cluster
