@@ -7,23 +7,11 @@ namespace cwl {
 
 struct RowGate { float w_in, w_out; int r_in, r_out; };  // g[j] = w_in [j < r_in] + w_out [j < r_out]
 
-// `Params` has T, R, window, window_mode, table and row_gates (null unless every row brings its own descriptor).
-// Per-row gate from the chunk table (Sec. III-C rank mask and scale, Sec. III-D cross-fade weight).
+// Gate of row t from the chunk table (Sec. III-C rank mask and scale, Sec. III-D cross-fade weight).  `Params` has T, R, window,
+// window_mode and table.
 template <typename Params>
-__device__ __forceinline__ RowGate row_gate(int t, const Params& p) {
+__device__ __forceinline__ RowGate table_gate(int t, const Params& p) {
   RowGate g{0.f, 0.f, 0, 0};
-  if (p.row_gates != nullptr) {
-    if (t < p.T) {
-      const cwl_row_gate d = p.row_gates[t];
-      g.r_in = min(max(d.rank_in, 0), p.R);
-      g.w_in = d.lambda * d.scale_in;
-      if (d.lambda < 1.f) {
-        g.r_out = min(max(d.rank_out, 0), p.R);
-        g.w_out = (1.f - d.lambda) * d.scale_out;
-      }
-    }
-    return g;
-  }
   const cwl_chunk_table& tb = p.table;
   const int C = min(*tb.n_chunks, tb.capacity);
   if (t < p.T && C > 0 && t >= tb.offsets[0] && t < tb.offsets[C]) {
@@ -56,6 +44,22 @@ __device__ __forceinline__ RowGate row_gate(int t, const Params& p) {
     if (lam < 1.f) {
       g.r_out = min(max(tb.rank[c_out], 0), p.R);
       g.w_out = (1.f - lam) * tb.scale[c_out];
+    }
+  }
+  return g;
+}
+// The same where rows may bring their own descriptors: `Params` also has row_gates, null unless every row does.
+template <typename Params>
+__device__ __forceinline__ RowGate row_gate(int t, const Params& p) {
+  if (p.row_gates == nullptr) return table_gate(t, p);
+  RowGate g{0.f, 0.f, 0, 0};
+  if (t < p.T) {
+    const cwl_row_gate d = p.row_gates[t];
+    g.r_in = min(max(d.rank_in, 0), p.R);
+    g.w_in = d.lambda * d.scale_in;
+    if (d.lambda < 1.f) {
+      g.r_out = min(max(d.rank_out, 0), p.R);
+      g.w_out = (1.f - d.lambda) * d.scale_out;
     }
   }
   return g;

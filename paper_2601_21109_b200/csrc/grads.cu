@@ -48,7 +48,6 @@ struct GradParams {
   int d[2];                    // d_in, d_out
   int window, window_mode;
   cwl_chunk_table table;
-  const cwl_row_gate* row_gates;
   int n_tiles[2], first;       // output tiles per side; the side whose tiles come first (the one with the longer K loop)
   int n_kb[2];                 // 64-deep K blocks per side
   int split;                   // CTAs of the cluster that share a tile's K loop
@@ -260,7 +259,7 @@ grad_kernel(const __grid_constant__ GradMaps maps, const __grid_constant__ GradP
     }
   } else if (kPhase == PHASE_SHRINK) {
     const int mine = (warp & 3) * 32 + lane;             // the row this thread drains
-    gates[mine] = row_gate(m0 + mine, p);                // while the main loop runs (a chain of dependent loads)
+    gates[mine] = table_gate(m0 + mine, p);                // while the main loop runs (a chain of dependent loads)
   }
 
   if (kPhase == PHASE_FOLD) pdl_wait();                  // every thread, before it writes an output
@@ -557,7 +556,7 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
   __nv_bfloat16* G = reinterpret_cast<__nv_bfloat16*>(static_cast<uint8_t*>(workspace) + gated_bytes(T, R));
   GradParams p = {};
   p.T = T; p.R = R; p.d[0] = d_in; p.d[1] = d_out;
-  p.window = window; p.window_mode = window_mode; p.table = table; p.row_gates = nullptr;
+  p.window = window; p.window_mode = window_mode; p.table = table;
   p.gated[0] = H; p.gated[1] = G;
   p.lo_col = lo_column(R);
   p.gated_ld = p.lo_col + R;
@@ -593,5 +592,5 @@ extern "C" cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY
   CWL_CUDA_TRY(launch_phase<PHASE_FOLD>(fold, p, l, chained, st));
   return CWL_OK;
 } catch (...) {
-  return CWL_ERR_CUDA;                                   // the cache of tensor maps allocates; nothing may leave a C entry
+  return CWL_ERR_CUDA;                                   // nothing may leave a C entry
 }

@@ -11,7 +11,6 @@
 
 namespace cwl {
 
-constexpr float kRowLog2e = 1.4426950408889634f;
 constexpr float kRowLn2 = 0.6931471805599453f;
 constexpr float kMaskedLogit = -1.0e30f;
 constexpr float kMaskedExponent = -1.0e30f;   // stands for -inf where a weight of 0 is multiplied with its exponent
@@ -227,16 +226,6 @@ __device__ __forceinline__ void absorb(RowStat& a, float z, float c) {
   a.S += e;
   a.U = fmaf(t, e, a.U);
 }
-__device__ __forceinline__ RowStat merge(RowStat a, RowStat b, float c) {
-  const float m = max_nan(a.m, b.m);
-  if (m == -CUDART_INF_F) return a;       // both empty
-  rebase(a, m, c);
-  rebase(b, m, c);
-  a.S += b.S;
-  a.U += b.U;
-  return a;
-}
-
 __device__ __forceinline__ void absorb_scalar(RowStat& a, float v, float c) {
   const float m_new = max_nan(a.m, v);
   if (m_new == -CUDART_INF_F) return;
