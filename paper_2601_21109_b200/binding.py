@@ -219,9 +219,9 @@ def _declare(L):
     return L
 
 
-def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
+def _stream_ptr(stream: Optional[torch.cuda.Stream], device: Optional[int] = None) -> int:
     if stream is None:      # the current stream's handle without a stream object around it (3 us less per call)
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice() if device is None else device)
     return int(stream.cuda_stream)
 
 
@@ -269,18 +269,23 @@ class DeviceChunkTable:
         t.n_chunks.fill_(n)
         return t
 
-    _c = None                                    # (addresses, marshalled struct) of the last call; not part of the state
+    _c = None                                    # addresses, marshalled struct and device of the last call; not part of the state
 
     def __getstate__(self):
         return {k: v for k, v in self.__dict__.items() if k != "_c"}
 
-    def c_struct(self) -> CChunkTable:
+    def _marshalled(self):
+        """The arrays' addresses, the struct for a call, and the CUDA device that holds all arrays (-1: there is none)."""
         at = (self.offsets.data_ptr(), self.rank.data_ptr(), self.scale.data_ptr(), self.rung.data_ptr(), self.flags.data_ptr(),
               self.n_chunks.data_ptr(), self.capacity)
         c = self._c
         if c is None or c[0] != at:              # arrays may be replaced, resized or given other storage at any time
-            c = self._c = (at, CChunkTable(*at))
-        return c[1]
+            here = {t.get_device() for t in (self.offsets, self.rank, self.scale, self.rung, self.flags, self.n_chunks)}
+            c = self._c = (at, CChunkTable(*at), here.pop() if len(here) == 1 else -1)
+        return c
+
+    def c_struct(self) -> CChunkTable:
+        return self._marshalled()[1]
 
     def to_host(self) -> dict:
         n = int(self.n_chunks.item())
@@ -608,22 +613,21 @@ def cwl_apply_noalloc(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor
     return Y
 
 
-def _on_current_device(*tensors: Optional[torch.Tensor]) -> None:
-    """Launches go to the current device: every tensor that a kernel is given has to be there."""
-    here = torch._C._cuda_getDevice()
-    for t in tensors:
-        assert t is None or t.get_device() == here, f"a tensor on {t.device}, the current device is cuda:{here}"
-
-
-def _check_status_word(status_word: Optional[torch.Tensor]) -> None:
-    assert status_word is None or (status_word.dtype == torch.int32 and status_word.numel() >= 1)
-
-
-def _row_stride(t: torch.Tensor) -> int:
-    """Distance of the rows of a matrix whose rows are contiguous; the stride of a dimension of one element says nothing."""
-    (rows, cols), (ld, unit) = t.shape, t.stride()
+def _row_stride(t: torch.Tensor, rows: int, cols: int) -> int:
+    """Distance of the rows of a [rows, cols] matrix whose rows are contiguous; the stride of a dimension of one element says
+    nothing."""
+    ld, unit = t.stride()
     assert unit == 1 or cols == 1
     return ld if rows > 1 else cols
+
+
+def _optional_on(device: int, t: Optional[torch.Tensor], dtype: torch.dtype, n: int) -> bool:
+    """None, or `n` contiguous elements of `dtype` on the device that the launch goes to."""
+    return t is None or (t.dtype == dtype and t.is_contiguous() and t.numel() == n and t.get_device() == device)
+
+
+def _status_on(device: int, t: Optional[torch.Tensor]) -> bool:
+    return t is None or (t.dtype == torch.int32 and t.numel() >= 1 and t.get_device() == device)
 
 
 class TokenLogprobs:
@@ -648,19 +652,18 @@ def cwl_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = N
     likely tokens of softmax(logits / temperature); logits fp32, bf16 or fp16 [T, V] on the device."""
     assert logits.dtype in _DTYPES
     T, V = logits.shape
-    ld = _row_stride(logits)
+    ld = _row_stride(logits, T, V)
     assert logits.is_cuda
+    here = torch._C._cuda_getDevice()            # launches go to the current device: everything has to be there
     if out is None:
         out = TokenLogprobs(T, top_k, targets is not None, logits.device)
     else:
         assert out.T == T and out.top_k == top_k and (out.logprob is None) == (targets is None)
-    if targets is not None:
-        assert targets.is_cuda and targets.dtype == torch.int32 and targets.is_contiguous() and targets.numel() == T
-    _check_status_word(status_word)
-    _on_current_device(logits, targets, out.lse, status_word)
+    assert logits.get_device() == out.lse.get_device() == here
+    assert _optional_on(here, targets, torch.int32, T) and _status_on(here, status_word)
     _check("cwl_token_logprobs", lib().cwl_token_logprobs(
         logits.data_ptr(), _DTYPES[logits.dtype], ld, T, V, _p(targets), temperature, top_k, *out._ptrs,
-        _p(status_word), _stream_ptr(stream)))
+        _p(status_word), _stream_ptr(stream, here)))
     return out
 
 
@@ -676,31 +679,28 @@ def cwl_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_va
     itself."""
     assert logits.dtype in _DTYPES
     T, V = logits.shape
-    K = teacher_ids.shape[1]
-    ld, ld_teacher = _row_stride(logits), _row_stride(teacher_ids)
+    rows, K = teacher_ids.shape
+    ld, ld_teacher = _row_stride(logits, T, V), _row_stride(teacher_ids, T, K)
     assert logits.is_cuda
-    assert teacher_ids.is_cuda and teacher_ids.dtype == torch.int32 and teacher_ids.shape[0] == T
-    assert teacher_values.is_cuda and teacher_values.dtype == torch.float32 and teacher_values.shape == teacher_ids.shape
-    assert _row_stride(teacher_values) == ld_teacher
-    assert weight is None or (weight.is_cuda and weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == T)
-    assert dloss is None or (dloss.is_cuda and dloss.dtype == torch.float32 and dloss.is_contiguous() and dloss.numel() == T)
-    if loss is not None:
-        assert loss.is_cuda and loss.dtype == torch.float32 and loss.is_contiguous() and loss.numel() == T
-    elif want_loss:
+    here = torch._C._cuda_getDevice()            # launches go to the current device: everything has to be there
+    assert rows == T and teacher_values.shape == teacher_ids.shape and _row_stride(teacher_values, T, K) == ld_teacher
+    assert teacher_ids.dtype == torch.int32 and teacher_values.dtype == torch.float32
+    assert logits.get_device() == teacher_ids.get_device() == teacher_values.get_device() == here
+    assert _optional_on(here, weight, torch.float32, T) and _optional_on(here, dloss, torch.float32, T)
+    assert _optional_on(here, loss, torch.float32, T) and _status_on(here, status_word)
+    if loss is None and want_loss:
         loss = teacher_values.new_empty(T)
     ld_d = 0
     if dlogits is not None:
-        ld_d = _row_stride(dlogits)
-        assert dlogits.is_cuda and dlogits.dtype == logits.dtype and dlogits.shape == (T, V)
+        ld_d = _row_stride(dlogits, T, V)
+        assert dlogits.dtype == logits.dtype and dlogits.shape == (T, V) and dlogits.get_device() == here
     elif want_grad:
         # rows as far apart as the logits': they then start at the same offset from a 16-byte boundary
         dlogits, ld_d = torch.empty_like(logits) if ld == V else logits.new_empty_strided((T, V), (ld, 1)), ld
-    _check_status_word(status_word)
-    _on_current_device(logits, teacher_ids, teacher_values, weight, dloss, loss, dlogits, status_word)
     _check("cwl_distill_topk", lib().cwl_distill_topk(
         logits.data_ptr(), _DTYPES[logits.dtype], ld, T, V, teacher_ids.data_ptr(), teacher_values.data_ptr(), ld_teacher, K,
         TEACHER_MODES[teacher], temperature, _p(weight), _p(dloss), _p(loss), _p(dlogits), ld_d, _p(status_word),
-        _stream_ptr(stream)))
+        _stream_ptr(stream, here)))
     return loss, dlogits
 
 
@@ -717,30 +717,33 @@ def cwl_apply_grads(X: torch.Tensor, dY: torch.Tensor, A: torch.Tensor, B: torch
     and the output's gradient dY (bf16); fp32 or bf16, of the type of ``dA`` and ``dB`` where they are given."""
     (T, d_in), (rows, d_out), (a_rows, R) = X.shape, dY.shape, A.shape
     assert rows == T and a_rows == d_in and B.shape == (R, d_out)
-    ldx, lddy, lda, ldb = _row_stride(X), _row_stride(dY), _row_stride(A), _row_stride(B)
-    assert X.is_cuda and dY.is_cuda and A.is_cuda and B.is_cuda
-    assert X.dtype == dY.dtype == A.dtype == B.dtype == torch.bfloat16
+    (ldx, ux), (lddy, uy), (lda, ua), (ldb, ub) = X.stride(), dY.stride(), A.stride(), B.stride()
+    assert ux == uy == ua == ub == 1 and X.dtype == dY.dtype == A.dtype == B.dtype == torch.bfloat16
+    if T == 1:                                   # a single row's stride says nothing
+        ldx, lddy = d_in, d_out
+    here = torch._C._cuda_getDevice()            # launches go to the current device: everything has to be there
+    _, c_table, table_on = table._marshalled()
+    assert X.get_device() == dY.get_device() == A.get_device() == B.get_device() == table_on == here
     if dA is None:
         dtype = grad_dtype if dB is None else dB.dtype
         dA, ldda = torch.empty_like(A, dtype=dtype) if lda == R else A.new_empty((d_in, R), dtype=dtype), R
     else:
-        ldda = _row_stride(dA)
-        assert dA.is_cuda and dA.dtype in _DTYPES and dA.shape == (d_in, R)
+        ldda, u = dA.stride()
+        assert u == 1 and dA.dtype in _DTYPES and dA.shape == (d_in, R) and dA.get_device() == here
     if dB is None:
         dB, lddb = torch.empty_like(B, dtype=dA.dtype) if ldb == d_out else B.new_empty((R, d_out), dtype=dA.dtype), d_out
     else:
-        lddb = _row_stride(dB)
-        assert dB.is_cuda and dB.dtype == dA.dtype and dB.shape == (R, d_out)
+        lddb, u = dB.stride()
+        assert u == 1 and dB.dtype == dA.dtype and dB.shape == (R, d_out) and dB.get_device() == here
     if workspace is None:
         workspace = torch.empty(cwl_apply_grads_workspace_bytes(T, d_in, d_out, R), dtype=torch.uint8, device=X.device)
     else:
-        assert workspace.dtype == torch.uint8 and workspace.is_contiguous()
-    _check_status_word(status_word)
-    _on_current_device(X, dY, A, B, dA, dB, workspace, status_word, table.offsets, table.rank, table.scale, table.flags, table.n_chunks)
+        assert workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.get_device() == here
+    assert _status_on(here, status_word)
     _check("cwl_apply_grads", lib().cwl_apply_grads(
-        X.data_ptr(), ldx, dY.data_ptr(), lddy, A.data_ptr(), lda, B.data_ptr(), ldb, T, d_in, d_out, R, table.c_struct(),
+        X.data_ptr(), ldx, dY.data_ptr(), lddy, A.data_ptr(), lda, B.data_ptr(), ldb, T, d_in, d_out, R, c_table,
         int(window), WINDOW_CENTRED if centred else WINDOW_CAUSAL, dA.data_ptr(), ldda, dB.data_ptr(), lddb, _DTYPES[dA.dtype],
-        workspace.data_ptr(), workspace.numel(), _p(status_word), _stream_ptr(stream)))
+        workspace.data_ptr(), workspace.numel(), _p(status_word), _stream_ptr(stream, here)))
     return dA, dB
 
 
