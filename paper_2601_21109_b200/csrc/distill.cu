@@ -177,26 +177,28 @@ __device__ __forceinline__ float inverse(float x) {
   return y;
 }
 // What a row's logits come to: its maximum m and S = sum 2^((z - m) c) over all of it, and the same of what lies outside the
-// entries, relative to the largest logit there: however far that lies below the row's maximum, the mass outside has its logarithm
-// and its elements their shares of it.
+// entries, relative to an m_out.  That is m itself where the mass outside shows beside it; where it does not (kNear) it is the
+// largest logit outside: however far that lies below the row's maximum, the mass outside then has its logarithm and its elements
+// their shares of it.
 struct RowMass {
   float m, s_row;
   float m_out, s_out;     // m and 0 where nothing lies outside
   float scale;            // 2^((m_out - m) c)
 };
-// From the parts outside the entries and of the entries, each relative to its own maximum; a bad row gives m = 0 and NaN masses.
+constexpr float kNear = 0x1p-40f;      // 2^-126, below which an exponential is 0, is nothing beside it
+__device__ __forceinline__ RowMass bad_mass() { return RowMass{0.f, CUDART_NAN_F, 0.f, CUDART_NAN_F, 1.f}; }
+__device__ __forceinline__ RowMass near_mass(float m, float s_out, float s_in) { return RowMass{m, s_out + s_in, m, s_out, 1.f}; }
 // An outside that lies below the maximum by more than kMaskedExponent is masked (with the type's lowest value), like -inf.
-__device__ __forceinline__ RowMass row_mass(float m_out, float s_out, float m_in, float s_in, float c) {
-  RowMass r;
-  r.m = max_nan(m_out, m_in);
-  if (bad_max(r.m)) return RowMass{0.f, CUDART_NAN_F, 0.f, CUDART_NAN_F, 1.f};
-  const float below = (m_out - r.m) * c;
+__device__ __forceinline__ RowMass far_mass(float m, float s_in, float m_out, float s_out, float c) {
+  const float below = (m_out - m) * c;
   const bool none = !(below > kMaskedExponent);
-  r.m_out = none ? r.m : m_out;
-  r.s_out = none ? 0.f : s_out;
-  r.scale = none ? 0.f : exp2_fast(below);
-  r.s_row = r.s_out * r.scale + (m_in == -CUDART_INF_F ? 0.f : s_in * exp2_fast((m_in - r.m) * c));
+  RowMass r{m, 0.f, none ? m : m_out, none ? 0.f : s_out, none ? 0.f : exp2_fast(below)};
+  r.s_row = s_in + r.s_out * r.scale;
   return r;
+}
+// a part's sum relative to m
+__device__ __forceinline__ float part_sum(float2 part, float m, float c) {
+  return part.x == -CUDART_INF_F ? 0.f : part.y * exp2_fast((part.x - m) * c);
 }
 // What the teacher leaves to the rest.  1 - sum p of a record that holds everything is not 0 but its rounding: an fp32 log-
 // probability u of a few operations is off by a few 2^-24 (1 + |u|), and sum p (1 + |u|) is at most 1 + ln 128 < 6.  A remainder
@@ -216,9 +218,7 @@ __device__ __forceinline__ double loss_term(const DistillParams& p, int id, floa
   const double ln_s = log((double)r.s_row);
   if (id >= 0 && !(prob == 0.f)) term = (double)prob * (lp - (((double)z - (double)r.m) * p.inv_temp_d - ln_s));
   if (tid == 0 && !(p_rest == 0.f)) {
-    // the scale as S_row has it while it counts there: its rounding then falls out between the entries' terms and this one
-    const double ln_out = r.scale > 0x1p-60f ? log((double)r.s_out * (double)r.scale)
-                                             : log((double)r.s_out) + ((double)r.m_out - (double)r.m) * p.inv_temp_d;
+    const double ln_out = log((double)r.s_out) + ((double)r.m_out - (double)r.m) * p.inv_temp_d;
     term += (double)p_rest * (log((double)p_rest) - (ln_out - ln_s));
   }
   if (tid == 0 && !(r.s_row == r.s_row) && !nothing_taught(p_in, p_rest)) term = (double)CUDART_NAN_F;
@@ -286,12 +286,6 @@ distill_small_kernel(const DistillParams p) {
     if (tid < p.K) sh.p[tid] = en.p;
     cp_async_wait_all();
     __syncthreads();                               // row and entries are in shared memory
-    if (nothing_taught(en.p_in, en.p_rest)) {
-      if (d != nullptr) zero_slice<T, kDsThreads>(tid, d, same_phase, rs);
-      if (p.loss != nullptr && tid == 0) p.loss[row] = 0.f;
-      continue;
-    }
-
     // lift the entries out of the row
     if (en.id >= 0) {
       en.z = Elem<T>::to_float(sm[lead + en.id]);
@@ -301,46 +295,58 @@ distill_small_kernel(const DistillParams p) {
     if (en.id >= 0) sm[lead + en.id] = Elem<T>::from_float(-CUDART_INF_F);
     __syncthreads();
 
-    // maximum outside the entries and of the entries, then the sums relative to each
-    float m_out = -CUDART_INF_F;
+    // maximum over the row and its entries, then the sums relative to it
     const uint4* sv = reinterpret_cast<const uint4*>(sm + rs.head + lead);
-    for (int i = tid; i < rs.v1; i += kDsThreads) {
-      const uint4 q = sv[i];
-      const uint32_t words[4] = {q.x, q.y, q.z, q.w};
-      m_out = max_nan(m_out, Elem<T>::max_of(words));
-    }
-    if (tid < rs.own_head) m_out = max_nan(m_out, Elem<T>::to_float(sm[lead + tid]));
-    if (tid < rs.own_tail) m_out = max_nan(m_out, Elem<T>::to_float(sm[lead + rs.tail_start + tid]));
-    m_out = key_value(__reduce_max_sync(0xffffffffu, order_key(m_out)));
-    float m_in = key_value(__reduce_max_sync(0xffffffffu, order_key(en.id >= 0 ? en.z : -CUDART_INF_F)));
-    if (lane == 0) { sh.red[wid] = m_out; sh.red2[wid] = m_in; }
-    __syncthreads();
-    m_out = sh.red[0];
-    m_in = sh.red2[0];
-    for (int i = 1; i < kDsWarps; ++i) {
-      m_out = max_nan(m_out, sh.red[i]);
-      m_in = max_nan(m_in, sh.red2[i]);
-    }
-    __syncthreads();
-    const float from = bad_max(m_out) ? 0.f : m_out;
-    float s_out = 0.f;
-    for (int i = tid; i < rs.v1; i += kDsThreads) {
-      float f[kVec];
-      Elem<T>::unpack(sv[i], f);
+    auto row_max = [&](float m) {
+      for (int i = tid; i < rs.v1; i += kDsThreads) {
+        const uint4 q = sv[i];
+        const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+        m = max_nan(m, Elem<T>::max_of(words));
+      }
+      if (tid < rs.own_head) m = max_nan(m, Elem<T>::to_float(sm[lead + tid]));
+      if (tid < rs.own_tail) m = max_nan(m, Elem<T>::to_float(sm[lead + rs.tail_start + tid]));
+      m = key_value(__reduce_max_sync(0xffffffffu, order_key(m)));
+      if (lane == 0) sh.red[wid] = m;
+      __syncthreads();
+      m = sh.red[0];
+      for (int i = 1; i < kDsWarps; ++i) m = max_nan(m, sh.red[i]);
+      __syncthreads();
+      return m;
+    };
+    auto sum_outside = [&](float m) {              // this warp's
+      float s = 0.f;
+      for (int i = tid; i < rs.v1; i += kDsThreads) {
+        float f[kVec];
+        Elem<T>::unpack(sv[i], f);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) s_out += exp2_fast((f[e] - from) * p.c);
-    }
-    if (tid < rs.own_head) s_out += exp2_fast((Elem<T>::to_float(sm[lead + tid]) - from) * p.c);
-    if (tid < rs.own_tail) s_out += exp2_fast((Elem<T>::to_float(sm[lead + rs.tail_start + tid]) - from) * p.c);
-    s_out = warp_sum(s_out);
-    float s_in = warp_sum(en.p_id >= 0.f && !bad_max(m_in) ? exp2_fast((en.z - m_in) * p.c) : 0.f);   // once per distinct id
-    if (lane == 0) { sh.red[wid] = s_out; sh.red2[wid] = s_in; }
+        for (int e = 0; e < kVec; ++e) s += exp2_fast((f[e] - m) * p.c);
+      }
+      if (tid < rs.own_head) s += exp2_fast((Elem<T>::to_float(sm[lead + tid]) - m) * p.c);
+      if (tid < rs.own_tail) s += exp2_fast((Elem<T>::to_float(sm[lead + rs.tail_start + tid]) - m) * p.c);
+      return warp_sum(s);
+    };
+    float m = row_max(en.id >= 0 ? en.z : -CUDART_INF_F);
+    const bool bad = bad_max(m);
+    if (bad) m = 0.f;
+    const float s_warp = sum_outside(m);
+    const float s_in_warp = warp_sum(en.p_id >= 0.f ? exp2_fast((en.z - m) * p.c) : 0.f);   // once per distinct id
+    if (lane == 0) { sh.red[wid] = s_warp; sh.red2[wid] = s_in_warp; }
     __syncthreads();
-    s_out = 0.f;
-    s_in = 0.f;
+    float s_out = 0.f, s_in = 0.f;
     for (int i = 0; i < kDsWarps; ++i) { s_out += sh.red[i]; s_in += sh.red2[i]; }
-    const RowMass r = row_mass(m_out, s_out, m_in, s_in, p.c);
+    RowMass r = bad ? bad_mass() : near_mass(m, s_out, s_in);
+    if (!bad && s_out < kNear) {
+      __syncthreads();                             // sh.red was read
+      const float m_out = row_max(-CUDART_INF_F);
+      const float s_far = sum_outside(m_out == -CUDART_INF_F ? 0.f : m_out);
+      if (lane == 0) sh.red[wid] = s_far;
+      __syncthreads();
+      s_out = 0.f;
+      for (int i = 0; i < kDsWarps; ++i) s_out += sh.red[i];
+      r = far_mass(m, s_in, m_out, s_out, p.c);
+    }
     const float rest = rest_of(en.p_rest, r);
+    const float k = outside_factor(en.p_in + rest, rest, r);
 
     if (p.loss != nullptr) {
       const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_in, rest, r, tid));
@@ -354,12 +360,16 @@ distill_small_kernel(const DistillParams p) {
     }
     if (d != nullptr) {
       const float up = w * p.temperature * (p.dloss != nullptr ? p.dloss[row] : 1.f);
-      const float k_out = outside_factor(en.p_in + rest, rest, r) * up;
-      store_slice<T, kDsThreads>(tid, d, same_phase, rs, [&](int i, float (&f)[kVec]) {
-        Elem<T>::unpack(sv[i], f);
+      const float k_out = k * up;
+      if (nothing_taught(en.p_in, rest)) {
+        zero_slice<T, kDsThreads>(tid, d, same_phase, rs);
+      } else {
+        store_slice<T, kDsThreads>(tid, d, same_phase, rs, [&](int i, float (&f)[kVec]) {
+          Elem<T>::unpack(sv[i], f);
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) f[e] = exp2_fast((f[e] - r.m_out) * p.c) * k_out;
-      }, [&](int i) { return exp2_fast((Elem<T>::to_float(sm[lead + i]) - r.m_out) * p.c) * k_out; });
+          for (int e = 0; e < kVec; ++e) f[e] = exp2_fast((f[e] - r.m_out) * p.c) * k_out;
+        }, [&](int i) { return exp2_fast((Elem<T>::to_float(sm[lead + i]) - r.m_out) * p.c) * k_out; });
+      }
       __syncthreads();                             // the entries' places now hold 0: put their own values there
       if (en.p_id >= 0.f) d[en.id] = Elem<T>::from_float(entry_gradient(p, en.z, en.p_id, en.p_in + rest, r.m, r.s_row) * up);
     }
@@ -507,13 +517,15 @@ distill_loss_kernel(const DistillParams p, const int mark_words) {
     // all parts together: lanes 0..3 outside the entries, 4..7 the entries
     const int k = lane & (2 * kLossWarps - 1);
     const bool outside = k < kLossWarps;
-    RowStat part{outside ? sh.part[k].x : sh.m_in[k - kLossWarps], outside ? sh.part[k].y : sh.s_in[k - kLossWarps], 0.f};
-    const float m_out = key_value(__reduce_max_sync(0xffffffffu, order_key(outside ? part.m : -CUDART_INF_F)));
-    const float m_in = key_value(__reduce_max_sync(0xffffffffu, order_key(outside ? -CUDART_INF_F : part.m)));
-    rescale(part, outside ? m_out : m_in, p.c);
-    const float s_out = warp_sum(lane < kLossWarps ? part.S : 0.f);
-    const float s_in = warp_sum(lane >= kLossWarps && lane < 2 * kLossWarps ? part.S : 0.f);
-    const RowMass r = row_mass(m_out, s_out, m_in, s_in, p.c);
+    const float2 part = outside ? sh.part[k] : make_float2(sh.m_in[k - kLossWarps], sh.s_in[k - kLossWarps]);
+    const float m = key_value(__reduce_max_sync(0xffffffffu, order_key(part.x)));
+    const float mine = lane < 2 * kLossWarps ? part_sum(part, m, p.c) : 0.f;
+    const float s_out = warp_sum(outside ? mine : 0.f), s_in = warp_sum(outside ? 0.f : mine);
+    RowMass r = bad_max(m) ? bad_mass() : near_mass(m, s_out, s_in);
+    if (!bad_max(m) && s_out < kNear) {
+      const float m_out = key_value(__reduce_max_sync(0xffffffffu, order_key(outside ? part.x : -CUDART_INF_F)));
+      r = far_mass(m, s_in, m_out, warp_sum(lane < kLossWarps ? part_sum(part, m_out, p.c) : 0.f), p.c);
+    }
     const double term = warp_sum(loss_term(p, en.id, en.p, en.lp, en.z, en.p_in, rest_of(en.p_rest, r), r, tid));
     __syncthreads();                           // red_d was read
     if (lane == 0) sh.red_d[wid] = term;
@@ -559,32 +571,37 @@ struct PipePlan {
 };
 
 // A row's masses from the parts of its slices, a part a lane of the warp (of eight slices, up to three).  Every sum warp waits
-// for it: a block that has the row to itself reads its entries' part as it stands (2048 rows of 32000 bf16: 48.3 -> 46.4 us).
+// for it: a block that has the row to itself reads its entries' part as it stands (2048 rows of 32000 bf16: 47.5 -> 46.5 us).
 __device__ __forceinline__ RowMass row_statistics(const float2* part, int n_cta, float c) {
   const int lane = threadIdx.x & 31;
+  float m = -CUDART_INF_F, s_out = 0.f, s_in = 0.f;
   if (n_cta == 1) {
     const float2 q = part[lane % kSumWarps], e = part[kSumWarps];
-    const float m_out = key_value(__reduce_max_sync(0xffffffffu, order_key(q.x)));
-    float s = q.x == -CUDART_INF_F ? 0.f : q.y * exp2_fast((q.x - m_out) * c);
+    m = max_nan(key_value(__reduce_max_sync(0xffffffffu, order_key(q.x))), e.x);
+    s_out = part_sum(q, m, c);
+    s_in = part_sum(e, m, c);
 #pragma unroll
-    for (int off = kSumWarps / 2; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    return row_mass(m_out, s, e.x, e.y, c);
+    for (int off = kSumWarps / 2; off > 0; off >>= 1) s_out += __shfl_xor_sync(0xffffffffu, s_out, off);
+  } else {
+    for (int i = lane; i < n_cta * kParts; i += 32) m = max_nan(m, part[i].x);
+    m = key_value(__reduce_max_sync(0xffffffffu, order_key(m)));
+    for (int i = lane; i < n_cta * kParts; i += 32) {
+      const float v = part_sum(part[i], m, c);
+      if (i % kParts == kSumWarps) s_in += v; else s_out += v;
+    }
+    s_out = warp_sum(s_out);
+    s_in = warp_sum(s_in);
   }
-  float m_out = -CUDART_INF_F, m_in = -CUDART_INF_F;
-  for (int i = lane; i < n_cta * kParts; i += 32) {
-    const float x = part[i].x;
-    if (i % kParts == kSumWarps) m_in = max_nan(m_in, x); else m_out = max_nan(m_out, x);
-  }
+  if (bad_max(m)) return bad_mass();
+  if (s_out >= kNear) return near_mass(m, s_out, s_in);
+  float m_out = -CUDART_INF_F;
+  for (int i = lane; i < n_cta * kParts; i += 32)
+    if (i % kParts != kSumWarps) m_out = max_nan(m_out, part[i].x);
   m_out = key_value(__reduce_max_sync(0xffffffffu, order_key(m_out)));
-  m_in = key_value(__reduce_max_sync(0xffffffffu, order_key(m_in)));
-  float s_out = 0.f, s_in = 0.f;
-  for (int i = lane; i < n_cta * kParts; i += 32) {
-    const bool entries = i % kParts == kSumWarps;
-    const float2 q = part[i];
-    const float v = q.x == -CUDART_INF_F ? 0.f : q.y * exp2_fast((q.x - (entries ? m_in : m_out)) * c);
-    if (entries) s_in += v; else s_out += v;
-  }
-  return row_mass(m_out, warp_sum(s_out), m_in, warp_sum(s_in), c);
+  s_out = 0.f;
+  for (int i = lane; i < n_cta * kParts; i += 32)
+    if (i % kParts != kSumWarps) s_out += part_sum(part[i], m_out, c);
+  return far_mass(m, s_in, m_out, warp_sum(s_out), c);
 }
 
 __device__ __forceinline__ void prepare_barrier() { __syncwarp(); asm volatile("bar.sync 1, 128;" ::: "memory"); }

@@ -46,6 +46,19 @@ def eps_of(V):
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("gap,tau", [(60.0, 1.0), (87.0, 1.0), (88.5, 1.0), (104.0, 1.0), (130.0, 2.0), (700.0, 1.0), (10000.0, 1.0), (12.0, 0.1)])
 def test_outside_mass_far_below_the_entries(gap, tau, dtype, mode):
+    outside_below(gap, tau, dtype, mode)
+
+
+@pytest.mark.parametrize("mode", ["logits", "logprobs"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("gap", [15.0, 24.0, 31.0, 34.0, 37.0, 45.0])
+def test_outside_mass_where_it_stops_showing_beside_the_entries(gap, dtype, mode):
+    """2^-40 of the row is 27.7 nats below it; the mass of thousands of tokens reaches it with the tokens further down.  Nearer, an
+    element's exponent counts from the row's maximum."""
+    outside_below(gap, 1.0, dtype, mode, from_row_maximum=True)
+
+
+def outside_below(gap, tau, dtype, mode, from_row_maximum=False):
     K = 8
     tau = float(np.float32(tau))
     for T, V in FORMS:
@@ -69,6 +82,8 @@ def test_outside_mass_far_below_the_entries(gap, tau, dtype, mode):
             assert float(((got.double() - rl).abs() - tol).max()) <= 0
         held = share == 0
         top = zt.double().masked_fill(torch.zeros_like(held).scatter_(1, ids.long(), True), float("-inf")).amax(1, keepdim=True)
+        if from_row_maximum:
+            top = zt.double().amax(1, keepdim=True)
         far = ((zt.double() - top).abs() / tau * 1.4427).clamp(max=200.0)
         tol = rg.abs() * (2 * eps + U * (30 + 3 * far) + torch.where(rest > 0, 20 * U / rest, 0.0)[:, None])
         tol += rg.abs() * HALF_ULP[dtype] * 1.01 + TINY[dtype] * 1.01
