@@ -14,10 +14,11 @@
 // each row and exchange (m, S) through distributed shared memory.
 //
 // What bounds them: HBM, with the logits read once and the gradient written once.  16384 rows of 32000 fp32, gradient
-// (clusters of two): 660 us, 6.4 TB/s; 2048 rows of 32000 bf16, loss and gradient, a quarter of weight 0 (a block a row):
-// 48 us, 4.8 TB/s -- ten rows a block, of which the first has no other to hide behind; 16384 rows of 32 KB (short rows):
-// 181 us, 5.9 TB/s; the loss alone of 1000 rows of 131072 fp16: 52 us, 5.0 TB/s -- one wave of blocks, whose ends nothing
-// fills -- and of 16384 rows of 32000 fp32: 310 us, 6.8 TB/s.  Seven rows of 32003 fp32 (eight blocks a row): 6.4 us.
+// (clusters of two): 660 to 710 us, by GPU and how long it has been under load, 6.3 to 5.9 TB/s; 2048 rows of 32000 bf16, loss and
+// gradient, a quarter of weight 0 (a block a row): 46.5 us, 4.9 TB/s -- ten rows a block, of which the first has no other to hide
+// behind; 16384 short rows of 32 KB: fp32 164 us, 6.6 TB/s, bf16 209 us, 5.1 TB/s; the loss alone of 1000 rows of 131072 fp16: 52
+// to 56 us, 5.0 to 4.7 TB/s -- one wave of blocks, all of which start and end together, on SMs of six or seven -- and of 16384 rows
+// of 32000 fp32: 310 us, 6.8 TB/s.  Seven rows of 32003 fp32 (eight blocks a row): 7 us on the device.
 #include <atomic>
 #include <cmath>
 
@@ -30,8 +31,10 @@ namespace {
 constexpr int kDsThreads = 128;           // of the kernel for short rows; at least CWL_MAX_TOP_K
 constexpr int kDsWarps = kDsThreads / 32;
 constexpr int kMaxDsCluster = 8;
-// Rows for one small block each: up to 16 KB always, up to 44 KB when there are four blocks an SM of them (16384 rows of
-// 32 KB: 181 us against 247 us of the pipelined kernel; 48 KB: 279 against 286; 400 rows of 32 KB: 13 against 12).
+// Rows for one small block each: up to 16 KB always, up to 44 KB when there are four blocks an SM of them.  Small blocks against
+// the pipelined kernel, us: 16384 rows of 32 KB 181 : 247, of 48 KB 279 : 286; at 300, 592, 900, 2000 rows of 17 KB 8.0 : 9.6, 8.9 :
+// 15.3, 14.6 : 22.1, 19.6 : 40.9; of 32 KB (bf16) 14.1 : 13.0, 16.9 : 17.2, 20.0 : 24.3, 33.4 : 46.0; of 44 KB 13.1 : 13.0, 15.6 :
+// 17.6, 20.5 : 24.3, 34.6 : 46.8.  (Rows of 17 and 22 KB would gain from 400 rows on.)
 constexpr int kSmallRowBytes = 16 * 1024;
 constexpr int kSmallManyRowBytes = 44 * 1024;
 constexpr int kSmallManyRows = 592;
@@ -382,12 +385,16 @@ distill_small_kernel(const DistillParams p) {
 // seven or eight blocks an SM.  A bit per element in shared memory marks the entries; a vector that holds one (64 of 4000, say) has
 // it replaced by -inf before it is summed, so that the mass outside the entries is again a sum of its own.
 // Eight blocks against seven: 16384 rows of 32000 fp16 213 -> 200 us, 4000 rows 61 -> 59; but rows that seven an SM hold at
-// once are spread more evenly that way: 1000 rows of 131072 fp16, back to back, 55 us, with eight 58.
+// once are spread more evenly that way: 1000 rows of 131072 fp16, back to back, 55 us (52 to 56 by GPU), with eight 58.
 constexpr int kLossThreads = 128;
 constexpr int kLossWarps = kLossThreads / 32;
 constexpr int kLossBatch = 4;
-constexpr int kLossMinRows = 740;              // five blocks an SM; with fewer the pipelined kernel, which cuts rows up, is faster
-                                               // (256 KB rows: 23 us against 50 us at 200 rows, 76 against 52 us at 1000)
+// From five blocks an SM on; with fewer rows the pipelined kernel, which cuts rows up.  Stream against pipeline, us, at 200, 400,
+// 600, 740, 1200 rows: 32 KB (fp32) 7.4 : 7.9, 9.2 : 11.7, 11.2 : 15.4, 11.8 : 16.8, 16.7 : 24.1; 64 KB (bf16) 11.7 : 9.2, 16.3 : 13.3,
+// 17.4 : 17.1, 17.7 : 18.5, 24.3 : 26.9; 256 KB (fp16) 34.9 : 21.6, 45.3 : 35.7, 48.0 : 49.5, 48.6 : 58.1, 67.7 : 89.3; 512 KB (fp32)
+// 42.0 : 35.9, 52.4 : 62.4, 61.2 : 90.9, 65.5 : 111.5, 119.7 : 175.0.  One bound for all sizes and types: fp32 rows, whose sums cost
+// half as much a byte, would gain from the stream from 300 rows on.
+constexpr int kLossMinRows = 740;
 
 struct LossShared {
   double red_d[kLossWarps];

@@ -11,10 +11,13 @@
 //           over X and dY: [G_hi G_lo] is one operand of 2 R columns, and the halves of the product meet in the epilogue.
 // X and dY are read by both: no output of FOLD can be summed before all of d_in / d_out went through SHRINK for its rows.
 //
-// What bounds it: those two passes (R = 64: T = 16384, 4096 -> 11008: 170 us for twice 495 MB, 5.8 TB/s; T = 4096, 57 us).
-// Short ones are bound by the two launches, each with its ramp and its meeting of partial sums (T = 2048, 4096 -> 4096: 24.6
-// us; T = 256, 1024 -> 1024, R = 16: 10 to 12 us on the device), the tensor pipe never (14 % and 30 % of its cycles).  Reading the rows that SHRINK
-// read last first, or SHRINK in waves of rows so that they could still be in L2: 169 -> 169 to 189 us.
+// What bounds it (R = 64, T = 16384, 4096 -> 11008: 173 us in bursts, 188 to 203 under lasting load, twice 495 MB at 5.7 to 4.9
+// TB/s; T = 4096: 56 us, 4.4 TB/s): no unit as a whole, most likely what the busiest SMs take in.  At T = 4096 SHRINK takes 32.6 us and FOLD 33.4, with DRAM at 49 and
+// 47 %, L2 at 28 %, the tensor pipe at 14 and 30 % of their cycles.  [G_hi G_lo] comes into every CTA beside X and dY (in FOLD half of
+// 251 MB), and the tiles deal unevenly: 236 CTAs of FOLD on 148 SMs, of which the busiest take in 2.13 MB and the idlest 1.06; the
+// busiest of SHRINK 1.50 MB where the mean is 1.30.  Reading the rows that SHRINK read last first, or SHRINK in waves of rows so that
+// they could still be in L2, therefore changed nothing: 169 -> 169 to 189 us.  Short ones are bound by the two launches, each with its
+// ramp and its meeting of partial sums (T = 2048, 4096 -> 4096: 24.6 us; T = 256, 1024 -> 1024, R = 16: 12 us on the device).
 // The K loop of a tile is split over the CTAs of a cluster where the tiles alone do not fill the GPU; the partial
 // accumulators meet in distributed shared memory in a fixed order, so results do not depend on timing.
 //

@@ -9,12 +9,12 @@
 // even and odd cells is a lower bound of the row's K-th largest logit, and only cells whose maximum reaches it can hold one of the
 // top K: a few per cent of the row are read a second time (from L2), and what reaches the bound is sorted in shared memory.
 //
-// What bounds it: without alternatives the one pass over the logits (2048 rows of 32000 fp32: 43 us, 6.1 TB/s; 16384 rows
-// of 32000 bf16: 162 us, 6.5 TB/s); with K = 64 the issue slots (16384 rows of 32000 bf16: 266 us, 4.0 TB/s; 12300 warp
-// instructions a row, of which 6950 are the pass itself, 2100 the cells and the fixed part of the selection and 3200 the
-// second reads, the 64 places and their sort).  Rows of 500 elements with K = 64: 16384 of them in 193 us.  Few rows are
-// cut up over a cluster: one row of 32000 fp32 with K = 20 in 7.1 us (launch, one pass of 16 KB a block, selection, the
-// leader's merge), 64 bf16 rows in 10 us.
+// What bounds it: without alternatives the one pass over the logits (2048 rows of 32000 fp32: 42 to 45 us, 6.2 to 5.9 TB/s; 16384
+// rows of 32000 bf16: 163 us, 6.4 TB/s); with K = 64 the instructions of a row and its serial phases (16384 rows of 32000 bf16: 265
+// to 276 us, 3.9 TB/s, issue slots 63 % active; 12300 warp instructions a row, of which 6950 are the pass itself, 2100 the cells and
+// the fixed part of the selection and 3200 the second reads, the 64 places and their sort).  16384 rows of 500 fp32 with K = 64: 132
+// us.  Few rows are cut up over a cluster: one row of 32000 fp32 with K = 20 in 7.5 us (launch, one pass of 16 KB a block, selection,
+// the leader's merge), 64 bf16 rows in 10.4 us.
 // A warp a row instead of four (24 rows an SM): 263 -> 350 us; the serial parts of a row then take four times as long.  Eight
 // blocks an SM instead of seven: 266 -> 271.  Rows cut in two where they do not fill the GPU (777 of 50021 fp32): 32 -> 40.
 #include <cmath>
@@ -567,7 +567,12 @@ token_logprobs_kernel(const LogprobParams p, const int log2_cta) {
 }
 
 // CTAs that share a row (as a power of two).  One per row once the rows fill the GPU; with fewer rows the row is cut so
-// that more SMs pull on it, down to slices of 2048 elements.
+// that more SMs pull on it, down to slices of 2048 elements, while no more than 592 blocks come of it.  us with 1 : 2 : 4 : 8 blocks a
+// row, 50000 fp32 without alternatives: 100 rows 16.0 : 11.4 : 9.2 : 8.0, 148 16.4 : 12.8 : 10.4 : 11.5, 296 20.2 : 15.0 : 17.3 : 17.9,
+// 400 21.7 : 17.0 : 19.3 : 22.7, 500 21.8 : 19.4 : 24.8 : 27.4, 600 24.3 : 27.6 : 27.6 : 31.3, 777 27.8 : 30.6 : 34.9 : 39.4; 32000 bf16,
+// K = 20: 100 rows 9.0 : 10.9 : 10.7 : 10.4, 296 16.7 : 14.6 : 18.3 : 25.8, 600 19.4 : 21.5 : 29.1 : 47.3; 131072 bf16, K = 20: 148 26.6 :
+// 27.2 : 20.2 : 22.1, 296 43.9 : 30.7 : 30.2 : 34.7, 600 49.2 : 45.5 : 47.7 : 61.4.  One bound for all of them: between 297 and some 500
+// rows two blocks a row would be 10 to 45 % faster than the one they get, at 222 rows four than two.
 int logprob_cluster(int T, int V) {
   int l = 0;
   while ((1 << l) < kMaxLpCluster && ((int64_t)T << (l + 1)) <= 592 && (V >> (l + 1)) >= 2048) ++l;
