@@ -422,11 +422,12 @@ cwl_status cwl_token_logprobs(const void* logits, cwl_dtype dtype, int64_t ld_lo
  *   dlogits[t,v] = dloss[t] d loss[t] / d z_v
  *                = dloss[t] weight[t] tau ( q_v (sum_j p_j + p_rest) - p_v - [v not among the entries] p_rest q_v / q_rest )
  * An entry with a negative id is padding.  Rows of weight 0 give loss 0 and gradient 0 and are not read; rows without
- * entries under CWL_TEACHER_LOGITS give the same, whatever their logits are.  -inf student logits have q = 0 (loss +inf if the teacher wants one).  q_rest
- * is kept by its logarithm, however small; it is 0 where every logit outside the entries is -inf, or lies 1e30 tau ln 2 or more
- * below the row's maximum (masks of the type's lowest value): +inf loss then, if p_rest is not 0, and no gradient there.  A row
- * with NaN or +inf logits, or of -inf only, gives NaN.  An id that occurs twice counts with the sum of its p.  An id >= V
- * counts as padding and flags CWL_ERR_INVALID_ARG in *status_word.  A temperature below 2^-127 counts as 2^-127.
+ * entries under CWL_TEACHER_LOGITS give the same, whatever their logits are.  -inf student logits have q = 0 (loss +inf if
+ * the teacher wants one).  q_rest is kept by its logarithm, however small; it is 0 where every logit outside the entries is
+ * -inf, or lies 1e30 tau ln 2 or more below the row's maximum (masks of fp32's or bf16's lowest value): +inf loss then, if
+ * p_rest is not 0, and no gradient there.  A row with NaN or +inf logits, or of -inf only, gives NaN.  An id that occurs
+ * twice counts with each of its entries in the loss and with the sum of their p in the gradient.  An id >= V counts as
+ * padding and flags CWL_ERR_INVALID_ARG in *status_word.  A temperature below 2^-127 counts as 2^-127.
  *   logits          DEV [T, V] of `dtype`, row stride ld_logits >= V; rows may start at any element
  *   teacher_ids     DEV int32 [T, K], teacher_values DEV fp32 [T, K], both with row stride ld_teacher >= K
  *   weight          DEV fp32 [T] or NULL (all 1);  dloss  DEV fp32 [T] or NULL (all 1): the upstream gradient of loss[t]

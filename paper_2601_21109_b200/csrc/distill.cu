@@ -191,7 +191,7 @@ struct RowMass {
 constexpr float kNear = 0x1p-40f;      // 2^-126, below which an exponential is 0, is nothing beside it
 __device__ __forceinline__ RowMass bad_mass() { return RowMass{0.f, CUDART_NAN_F, 0.f, CUDART_NAN_F, 1.f}; }
 __device__ __forceinline__ RowMass near_mass(float m, float s_out, float s_in) { return RowMass{m, s_out + s_in, m, s_out, 1.f}; }
-// An outside that lies below the maximum by more than kMaskedExponent is masked (with the type's lowest value), like -inf.
+// An outside that lies below the maximum by more than kMaskedExponent is masked (with fp32's or bf16's lowest value), like -inf.
 __device__ __forceinline__ RowMass far_mass(float m, float s_in, float m_out, float s_out, float c) {
   const float below = (m_out - m) * c;
   const bool none = !(below > kMaskedExponent);
