@@ -466,6 +466,32 @@ cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY, int64_t l
                            void* dA, int64_t ldda, void* dB, int64_t lddb, cwl_dtype grad_dtype,
                            void* workspace, size_t workspace_bytes, int32_t* status_word, void* stream);
 
+/* Softmax cross entropy of a head's projection over a large vocabulary, and its gradients; the logits are not kept.  With
+ * z_t = x_t W and lse[t] = ln sum_v exp(z_tv),
+ *   loss[t] = weight[t] (lse[t] - z_t,y),  y = targets[t]
+ *   dZ = dloss o weight o (softmax(z) - onehot(y)),   dX = dZ W^T,   dW = X^T dZ
+ * A row counts if it has a target and a weight other than 0; every other row has loss 0, lse 0 and gradient 0, whatever its
+ * activations hold, and costs no arithmetic.  A negative target means none; one >= V gives loss NaN, lse NaN and no
+ * gradient, and flags CWL_ERR_INVALID_ARG in *status_word.
+ *   X       DEV bf16 [T, d];  W  DEV bf16 [d, V]: 16-byte aligned, rows a multiple of 16 bytes apart, any d and V
+ *   targets DEV int32 [T];  weight  DEV fp32 [T] or NULL (all 1)
+ *   loss    DEV fp32 [T] or NULL.  With it, one call gives the loss and, where dX or dW are given, the gradients of its sum;
+ *           lse (DEV fp32 [T], may be NULL) is an output and dloss has to be NULL
+ *           NULL: a backward call.  lse is an input, from the forward call, and dloss (DEV fp32 [T] or NULL, all 1) the
+ *           upstream gradient of loss[t]; rows where it is 0 do not count either
+ *   dX      DEV [T, d] or NULL;  dW  DEV [d, V] or NULL; of grad_dtype (CWL_F32 or CWL_BF16), aligned to their type, any
+ *           row stride; overwritten; not overlapping an input
+ *   workspace   DEV, at least cwl_head_loss_workspace_bytes(T, d, V, dX given, dW given) bytes, 256-byte aligned
+ * Logits and all sums are fp32; dZ is rounded to bf16 for the products with W and X.  X of rows that count and W finite.
+ * T == 0 writes zeros to dW.  Results do not depend on timing.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (T or V > 2^24, d > 2^20), WORKSPACE, CUDA; TIMEOUT through *status_word. */
+size_t     cwl_head_loss_workspace_bytes(int32_t T, int32_t d, int32_t V, int32_t want_dx, int32_t want_dw);
+cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw, int32_t T, int32_t d, int32_t V,
+                         const int32_t* targets, const float* weight, const float* dloss,
+                         float* loss, float* lse, void* dX, int64_t lddx, void* dW, int64_t lddw,
+                         cwl_dtype grad_dtype, void* workspace, size_t workspace_bytes,
+                         int32_t* status_word, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,7 +9,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import torch
 
@@ -27,7 +27,7 @@ EXPORTS = ["cwl_status_string", "cwl_version", "cwl_score_tokens", "cwl_score_to
            "cwl_apply_noalloc_scratch_need", "cwl_apply_noalloc", "cwl_prefetch_next", "cwl_apply_mode",
            "cwl_batch_align_workspace_bytes", "cwl_batch_align", "cwl_set_pair_budget",
            "cwl_apply_batch_workspace_bytes", "cwl_apply_batch", "cwl_token_logprobs", "cwl_distill_topk",
-           "cwl_apply_grads_workspace_bytes", "cwl_apply_grads"]
+           "cwl_apply_grads_workspace_bytes", "cwl_apply_grads", "cwl_head_loss_workspace_bytes", "cwl_head_loss"]
 NOALLOC_SCRATCH_BYTES = 8 << 20
 WINDOW_CAUSAL, WINDOW_CENTRED = 0, 1
 MAX_BATCH = 4
@@ -216,6 +216,12 @@ def _declare(L):
                                       C.c_int32, C.c_int32, C.c_int32, C.c_int32, CChunkTable, C.c_int32, C.c_int32,
                                       C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_size_t,
                                       C.c_void_p, C.c_void_p]
+        L.cwl_head_loss_workspace_bytes.restype = C.c_size_t
+        L.cwl_head_loss_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+        L.cwl_head_loss.restype = C.c_int
+        L.cwl_head_loss.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
+                                    C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                                    C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
     return L
 
 
@@ -745,6 +751,65 @@ def cwl_apply_grads(X: torch.Tensor, dY: torch.Tensor, A: torch.Tensor, B: torch
         int(window), WINDOW_CENTRED if centred else WINDOW_CAUSAL, dA.data_ptr(), ldda, dB.data_ptr(), lddb, _DTYPES[dA.dtype],
         workspace.data_ptr(), workspace.numel(), _p(status_word), _stream_ptr(stream, here)))
     return dA, dB
+
+
+def cwl_head_loss_workspace_bytes(T: int, d: int, V: int, want_dx: bool = False, want_dw: bool = False) -> int:
+    return int(lib().cwl_head_loss_workspace_bytes(T, d, V, int(want_dx), int(want_dw)))
+
+
+class HeadLoss(NamedTuple):
+    """What cwl_head_loss gives: ``loss`` and ``lse`` fp32 [T] (a backward call: None, and the lse it was given), ``dX`` [T, d]
+    and ``dW`` [d, V] or None."""
+    loss: Optional[torch.Tensor]
+    lse: Optional[torch.Tensor]
+    dX: Optional[torch.Tensor]
+    dW: Optional[torch.Tensor]
+
+
+def cwl_head_loss(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                  dloss: Optional[torch.Tensor] = None, want_loss: bool = True, want_dx: bool = False, want_dw: bool = False,
+                  loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None,
+                  dW: Optional[torch.Tensor] = None, grad_dtype: torch.dtype = torch.bfloat16,
+                  workspace: Optional[torch.Tensor] = None, status_word: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None) -> HeadLoss:
+    """Cross entropy of softmax(X W) against ``targets`` (negative: none) row by row, times ``weight``, and the gradients of
+    its sum, without keeping the logits; X [T, d] and W [d, V] bf16.  ``want_loss=False`` is a backward call: it takes the
+    forward call's ``lse`` and the upstream gradient ``dloss``.  Gradients are fp32 or bf16, of the type of ``dX`` and ``dW``
+    where they are given."""
+    (T, d), (rows, V) = X.shape, W.shape
+    assert rows == d and X.dtype == W.dtype == torch.bfloat16
+    ldx, ldw = _row_stride(X, T, d), _row_stride(W, d, V)
+    here = torch._C._cuda_getDevice()            # launches go to the current device: everything has to be there
+    assert X.is_cuda and X.get_device() == W.get_device() == here
+    assert targets is not None and _optional_on(here, targets, torch.int32, T) and _status_on(here, status_word)
+    assert _optional_on(here, weight, torch.float32, T) and _optional_on(here, dloss, torch.float32, T)
+    assert _optional_on(here, loss, torch.float32, T) and _optional_on(here, lse, torch.float32, T)
+    if want_loss or loss is not None:
+        assert dloss is None, "an upstream gradient belongs to a backward call (want_loss=False)"
+        loss = X.new_empty(T, dtype=torch.float32) if loss is None else loss
+        lse = X.new_empty(T, dtype=torch.float32) if lse is None else lse
+    else:
+        assert lse is not None, "a backward call needs the forward call's lse"
+    given = dX if dX is not None else dW
+    dtype = grad_dtype if given is None else given.dtype
+    ldd = ldw_out = 0
+    if dX is not None or want_dx:
+        dX = X.new_empty((T, d), dtype=dtype) if dX is None else dX
+        assert dX.shape == (T, d) and dX.dtype == dtype and dX.get_device() == here
+        ldd = _row_stride(dX, T, d)
+    if dW is not None or want_dw:
+        # rows as far apart as W's: they then start on 16-byte boundaries whatever V is
+        dW = W.new_empty_strided((d, V), (max(ldw, V), 1), dtype=dtype) if dW is None else dW
+        assert dW.shape == (d, V) and dW.dtype == dtype and dW.get_device() == here
+        ldw_out = _row_stride(dW, d, V)
+    if workspace is None:
+        workspace = torch.empty(cwl_head_loss_workspace_bytes(T, d, V, dX is not None, dW is not None), dtype=torch.uint8, device=X.device)
+    else:
+        assert workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.get_device() == here
+    _check("cwl_head_loss", lib().cwl_head_loss(
+        X.data_ptr(), ldx, W.data_ptr(), ldw, T, d, V, targets.data_ptr(), _p(weight), _p(dloss), _p(loss), _p(lse), _p(dX), ldd,
+        _p(dW), ldw_out, _DTYPES.get(dtype, -1), workspace.data_ptr(), workspace.numel(), _p(status_word), _stream_ptr(stream, here)))
+    return HeadLoss(loss, lse, dX, dW)
 
 
 def bf16_from_bits(bits, device="cuda") -> torch.Tensor:

@@ -1,0 +1,136 @@
+"""cwl_head_loss against its definition in 64 bits and against differences.
+
+Tolerances, entry by entry, from the arithmetic.  A logit is an fp32 sum of d products (2^-23 d of the sum of their magnitudes,
+however they cancel): ez.  An exponential's argument is rounded at the size of the logits and the function itself is good to
+2^-22; at most 1024 of them are added up one after the other: el.  So lse is within ez + el, a probability within twice that of
+itself, dZ is rounded to bf16 (2^-8 of a number), and the products with W and X sum V or T terms in fp32 (2^-23 of their
+magnitudes each) and are rounded to their own type (2^-8 or 2^-24)."""
+import pytest
+import torch
+
+from paper_2601_21109_b200 import binding as cwl
+
+pytestmark = pytest.mark.gpu
+
+
+def operands(seed, T, d, V, pad=0, spread=3.0):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+
+    def m(r, c, std):
+        buf = torch.full((r, (c + pad + 7) // 8 * 8), 9.0, dtype=torch.bfloat16, device="cuda")
+        buf[:, :c].copy_(torch.randn(r, c, device="cuda", generator=gen) * std)
+        return buf[:, :c]
+    X, W = m(T, d, 1.0), m(d, V, spread * d ** -0.5)
+    y = torch.randint(0, V, (T,), device="cuda", generator=gen, dtype=torch.int32)
+    w = torch.rand(T, device="cuda", generator=gen) + 0.5
+    return X, W, y, w
+
+
+def reference(X, W, y, w, dloss=None, lse=None):
+    """Everything in 64 bits, with the tolerances of loss, lse and dZ."""
+    V, d = W.shape[1], W.shape[0]
+    x, wt = X.double(), W.double()
+    on = (y >= 0) & (y < V) & (w != 0)
+    if dloss is not None:
+        on &= dloss != 0
+    x = torch.where(on[:, None], x, 0.0)
+    z = x @ wt
+    ez = (d * 2.0 ** -23 * (x.abs() @ wt.abs())).amax(1)
+    el = (2 * z.abs().amax(1) + 4) * 2.0 ** -22 + 1024 * 2.0 ** -24
+    own = torch.logsumexp(z, 1)
+    norm = own if lse is None else lse.double()
+    zy = z.gather(1, y.clamp(0, V - 1).long()[:, None])[:, 0]
+    up = torch.where(on, w.double() * (1 if dloss is None else dloss.double()), 0.0)
+    q = (z - norm[:, None]).exp()
+    dz = q.clone()
+    dz.scatter_add_(1, y.clamp(0, V - 1).long()[:, None], torch.full((len(y), 1), -1.0, dtype=torch.float64, device=z.device))
+    dz = dz * up[:, None]
+    tz = q * (up.abs() * 2.02 * (ez + el))[:, None] + dz.abs() * 2.0 ** -8
+    loss = torch.where(on, w.double() * (own - zy), 0.0)
+    tl = torch.where(on, ez + el + own.abs() * 2.0 ** -23, 0.0)
+    return dict(on=on, x=x, W=wt, lse=torch.where(on, own, 0.0), tl=tl, loss=loss, tloss=w.double().abs() * (2 * tl) + loss.abs() * 2.0 ** -22,
+                dz=dz, tz=tz)
+
+
+def within(got, ref, tol, what):
+    over = (got.double() - ref).abs() - tol * 1.01 - 1e-30
+    assert bool(torch.isfinite(got).all()), f"{what}: not finite"
+    assert float(over.max()) <= 0, f"{what}: over tolerance by {float(over.max()):.3e}"
+
+
+def check_gradients(r, dX, dW, T, V):
+    u = 2.0 ** -23
+    if dX is not None:
+        out = 2.0 ** -8 if dX.dtype == torch.bfloat16 else 2.0 ** -24
+        ref = r["dz"] @ r["W"].T
+        within(dX, ref, (r["tz"] + V * u * r["dz"].abs()) @ r["W"].abs().T + ref.abs() * out, "dX")
+        if float(ref.norm()) > 0:       # what 2^-8 of every dZ, of either sign, comes to in a norm, and the rounding of dX
+            assert float((dX.double() - ref).norm() / ref.norm()) <= 2.0 ** -8 + out
+    if dW is not None:
+        out = 2.0 ** -8 if dW.dtype == torch.bfloat16 else 2.0 ** -24
+        ref = r["x"].T @ r["dz"]
+        within(dW, ref, r["x"].abs().T @ (r["tz"] + T * u * r["dz"].abs()) + ref.abs() * out, "dW")
+
+
+def check(X, W, y, w, **kw):
+    T, V = X.shape[0], W.shape[1]
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    o = cwl.cwl_head_loss(X, W, y, weight=w, status_word=status, **kw)
+    assert int(status.item()) == 0
+    r = reference(X, W, y, torch.ones_like(y, dtype=torch.float32) if w is None else w)
+    within(o.lse, r["lse"], r["tl"], "lse")
+    within(o.loss, r["loss"], r["tloss"], "loss")
+    check_gradients(r, o.dX, o.dW, T, V)
+    return o
+
+
+SIZES = [(1, 64, 500), (1, 4096, 32000), (2, 16, 8), (7, 8, 1), (3, 1, 17), (5, 33, 31), (48, 512, 3001), (127, 200, 1000), (128, 64, 512), (129, 1000, 2049),
+         (255, 136, 777), (256, 256, 256), (257, 72, 4097), (300, 1024, 5003), (777, 2048, 1234), (1000, 24, 20011), (1536, 640, 8192)]
+
+
+@pytest.mark.parametrize("T,d,V", SIZES)
+def test_loss_alone(T, d, V):
+    check(*operands(T + d, T, d, V))
+
+
+@pytest.mark.parametrize("T,d,V", SIZES)
+def test_loss_and_gradients(T, d, V):
+    X, W, y, w = operands(T + d, T, d, V, pad=3)
+    check(X, W, y, w, want_dx=True, want_dw=True)
+    check(X, W, y, w, want_dx=True, grad_dtype=torch.float32)
+    check(X, W, y, None, want_dw=True, grad_dtype=torch.float32)
+
+
+@pytest.mark.parametrize("T,d,V", SIZES)
+def test_backward_call(T, d, V):
+    X, W, y, w = operands(T + d, T, d, V)
+    f = cwl.cwl_head_loss(X, W, y, weight=w)
+    g = torch.rand(T, device="cuda") - 0.5
+    g[::5] = 0.0
+    o = cwl.cwl_head_loss(X, W, y, weight=w, dloss=g, lse=f.lse, want_loss=False, want_dx=True, want_dw=True, grad_dtype=torch.float32)
+    assert o.loss is None and o.lse is f.lse
+    check_gradients(reference(X, W, y, w, dloss=g, lse=f.lse), o.dX, o.dW, T, V)
+
+
+@pytest.mark.parametrize("T,d,V", [(9, 64, 700), (300, 136, 2049), (600, 512, 1000)])
+@pytest.mark.parametrize("share", [0.0, 0.02, 0.5, 1.0])
+def test_rows_that_do_not_count(T, d, V, share):
+    """Rows without a target or of weight 0 have zeros everywhere, whatever their activations hold."""
+    X, W, y, w = operands(T, T, d, V)
+    off = torch.rand(T, device="cuda") < share
+    half = torch.rand(T, device="cuda") < 0.5
+    y = torch.where(off & half, -1, y)
+    w = torch.where(off & ~half, 0.0, w)
+    X[off] = float("nan")
+    o = check(X, W, y, w, want_dx=True, want_dw=True)
+    for t in (o.loss, o.lse, o.dX):
+        assert not bool(t[off].any())
+    check(X, W, y, w, want_dx=True, want_dw=True, grad_dtype=torch.float32)
+
+
+def test_a_vocabulary_in_pieces():
+    X, W, y, w = operands(1, 16384, 64, 20000)
+    y[::7] = -1
+    check(X, W, y, w, want_dx=True, want_dw=True)
+    check(X, W, y, w, want_dx=True, grad_dtype=torch.float32)
