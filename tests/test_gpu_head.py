@@ -134,3 +134,17 @@ def test_a_vocabulary_in_pieces():
     y[::7] = -1
     check(X, W, y, w, want_dx=True, want_dw=True)
     check(X, W, y, w, want_dx=True, grad_dtype=torch.float32)
+
+
+@pytest.mark.parametrize("grad", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,d,V,spread", [(60, 64, 3000, 60.0), (700, 136, 4504, 40.0), (16384, 16, 20000, 100.0)])
+def test_logits_far_apart(T, d, V, spread, grad):
+    """Logits hundreds above the row's reference, more so from piece to piece: columns that outgrow it take another one."""
+    X, W, y, w = operands(7, T, d, V)
+    W.copy_(W * torch.linspace(0.1, spread / 3.0, V, device="cuda"))
+    check(X, W, y, w, want_dx=True, grad_dtype=grad)
+    check(X, W.flip(1).contiguous(), y, w, want_dx=True, grad_dtype=grad)
+    W[:, 0] = 0                                                     # the reference itself far above all others
+    W[0, 0] = 100.0
+    X[:, 0] = X[:, 0].abs() + 1
+    check(X, W, y, w, want_dx=True, grad_dtype=grad)
