@@ -492,6 +492,41 @@ cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw,
                          cwl_dtype grad_dtype, void* workspace, size_t workspace_bytes,
                          int32_t* status_word, void* stream);
 
+/* Newton-Schulz orthogonalisation of adapter factors, alone and as the update of a ladder's factors.  For a factor U with its
+ * short side first (transposed where it has more rows than columns),
+ *   X_0 = U / (|U|_F + eps),   X_(k+1) = a X_k + b (X_k X_k^T) X_k + c (X_k X_k^T)^2 X_k,   O = X_steps
+ * brings all singular values near 1 and leaves the singular vectors as they are (a = 3.4445, b = -4.775, c = 2.0315 with 5 steps are
+ * customary).  Computed with 64-bit Gram matrices; O carries the rounding of fp32 products, then that of its own type.
+ *   cwl_orthogonalize  out = O                             of `out_dtype` (CWL_F32 or CWL_BF16)
+ *   cwl_factor_step    momentum = beta momentum + grad;    U = grad + beta momentum (nesterov != 0) or momentum
+ *                      out = (1 - lr weight_decay) out - lr scale O;    low = bf16(out)
+ * A factor of zeros gives zeros (momentum and weight decay apply all the same); one with NaN or infinities gives NaN everywhere.
+ *   factors    HOST array of n, copied at call time; pointers inside are DEV; different factors must not overlap
+ *   iteration  HOST
+ *   workspace  DEV, at least cwl_orthogonalize_workspace_bytes(factors, n) bytes (which reads rows and cols only), 256-byte
+ *              aligned; both calls
+ * Any number of factors, rows and cols from 1, the smaller of them at most CWL_MAX_RANK, the larger at most 2^22; any row
+ * stride, elements aligned to their type.  out must not overlap grad.
+ * Results do not depend on timing, nor on which other factors share the call but for the order of sums over the longer side.
+ * Errors: INVALID_ARG (NULLs, sizes below 1, steps outside 1..CWL_MAX_NS_STEPS, eps negative, momentum outside [0, 1), values
+ * that are not finite, unknown types), SHAPE (strides, alignment), UNSUPPORTED (sizes), WORKSPACE, CUDA.  n == 0 is a no-op. */
+#define CWL_MAX_NS_STEPS 16
+typedef struct {
+  int32_t rows, cols;
+  const void* grad; int64_t ld_grad;        /* DEV [rows, cols] of the call's type: the gradient, or the matrix to orthogonalise */
+  void* momentum; int64_t ld_momentum;      /* DEV fp32 [rows, cols], read and written; cwl_factor_step only */
+  void* out; int64_t ld_out;                /* DEV [rows, cols]: O, or the fp32 master, read and written */
+  void* low; int64_t ld_low;                /* DEV bf16 [rows, cols] or NULL: the master's copy; cwl_factor_step only */
+  float scale;                              /* of the update; cwl_factor_step only */
+} cwl_factor;
+typedef struct { int32_t steps; double a, b, c, eps; } cwl_newton_schulz;
+size_t     cwl_orthogonalize_workspace_bytes(const cwl_factor* factors, int32_t n);
+cwl_status cwl_orthogonalize(const cwl_factor* factors, int32_t n, cwl_dtype in_dtype, cwl_dtype out_dtype,
+                             const cwl_newton_schulz* iteration, void* workspace, size_t workspace_bytes, void* stream);
+cwl_status cwl_factor_step(const cwl_factor* factors, int32_t n, cwl_dtype grad_dtype, const cwl_newton_schulz* iteration,
+                           float lr, float momentum, float weight_decay, int32_t nesterov,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,7 +27,8 @@ EXPORTS = ["cwl_status_string", "cwl_version", "cwl_score_tokens", "cwl_score_to
            "cwl_apply_noalloc_scratch_need", "cwl_apply_noalloc", "cwl_prefetch_next", "cwl_apply_mode",
            "cwl_batch_align_workspace_bytes", "cwl_batch_align", "cwl_set_pair_budget",
            "cwl_apply_batch_workspace_bytes", "cwl_apply_batch", "cwl_token_logprobs", "cwl_distill_topk",
-           "cwl_apply_grads_workspace_bytes", "cwl_apply_grads", "cwl_head_loss_workspace_bytes", "cwl_head_loss"]
+           "cwl_apply_grads_workspace_bytes", "cwl_apply_grads", "cwl_head_loss_workspace_bytes", "cwl_head_loss",
+           "cwl_orthogonalize_workspace_bytes", "cwl_orthogonalize", "cwl_factor_step"]
 NOALLOC_SCRATCH_BYTES = 8 << 20
 WINDOW_CAUSAL, WINDOW_CENTRED = 0, 1
 MAX_BATCH = 4
@@ -83,6 +84,16 @@ class CBatchItem(C.Structure):
 class CSignalMix(C.Structure):
     _fields_ = [("w_entropy", C.c_float), ("w_novelty", C.c_float), ("w_prior", C.c_float),
                 ("ngram", C.c_int32), ("context", C.c_int32), ("prior_span", C.c_int32)]
+
+
+class CFactor(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("cols", C.c_int32), ("grad", C.c_void_p), ("ld_grad", C.c_int64),
+                ("momentum", C.c_void_p), ("ld_momentum", C.c_int64), ("out", C.c_void_p), ("ld_out", C.c_int64),
+                ("low", C.c_void_p), ("ld_low", C.c_int64), ("scale", C.c_float)]
+
+
+class CNewtonSchulz(C.Structure):
+    _fields_ = [("steps", C.c_int32), ("a", C.c_double), ("b", C.c_double), ("c", C.c_double), ("eps", C.c_double)]
 
 
 class CApplyPlanInfo(C.Structure):
@@ -222,6 +233,14 @@ def _declare(L):
         L.cwl_head_loss.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int32, C.c_int32, C.c_int32,
                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
                                     C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
+        L.cwl_orthogonalize_workspace_bytes.restype = C.c_size_t
+        L.cwl_orthogonalize_workspace_bytes.argtypes = [C.POINTER(CFactor), C.c_int32]
+        L.cwl_orthogonalize.restype = C.c_int
+        L.cwl_orthogonalize.argtypes = [C.POINTER(CFactor), C.c_int32, C.c_int, C.c_int, C.POINTER(CNewtonSchulz), C.c_void_p,
+                                        C.c_size_t, C.c_void_p]
+        L.cwl_factor_step.restype = C.c_int
+        L.cwl_factor_step.argtypes = [C.POINTER(CFactor), C.c_int32, C.c_int, C.POINTER(CNewtonSchulz), C.c_float, C.c_float,
+                                      C.c_float, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
     return L
 
 
@@ -810,6 +829,110 @@ def cwl_head_loss(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, weigh
         X.data_ptr(), ldx, W.data_ptr(), ldw, T, d, V, targets.data_ptr(), _p(weight), _p(dloss), _p(loss), _p(lse), _p(dX), ldd,
         _p(dW), ldw_out, _DTYPES.get(dtype, -1), workspace.data_ptr(), workspace.numel(), _p(status_word), _stream_ptr(stream, here)))
     return HeadLoss(loss, lse, dX, dW)
+
+
+NS_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+class _FactorCall:
+    """Factors with everything marshalled once, for calls that come every step: descriptors, iteration, workspace.  The tensors
+    are kept; they are read and written where they lie at every call."""
+
+    def __init__(self, n: int, device: int, steps: int, coefficients: Sequence[float], eps: float, workspace: Optional[torch.Tensor],
+                 fill, keep):
+        self.n, self.device, self.keep = n, device, keep
+        self.factors = (CFactor * max(n, 1))()
+        for i in range(n):
+            fill(i, self.factors[i])
+        a, b, c = coefficients
+        self.iteration = CNewtonSchulz(int(steps), float(a), float(b), float(c), float(eps))
+        need = int(lib().cwl_orthogonalize_workspace_bytes(self.factors, n))
+        if workspace is None:
+            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=f"cuda:{device}")
+        assert workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.get_device() == device
+        self.workspace = workspace
+
+    def _stream(self, stream):
+        assert torch._C._cuda_getDevice() == self.device      # launches go to the current device: everything has to be there
+        return _stream_ptr(stream, self.device)
+
+
+def _one_device(tensors: Sequence[torch.Tensor]) -> int:
+    here = torch._C._cuda_getDevice()
+    assert all(t.dim() == 2 and t.is_cuda and t.get_device() == here for t in tensors)
+    return here
+
+
+class OrthogonalizeCall(_FactorCall):
+    """cwl_orthogonalize of a list of factors: ``outs[i]`` (fp32 or bf16) = Newton-Schulz of ``factors[i]`` (fp32, bf16 or
+    fp16), every call anew from what the factors hold then."""
+
+    def __init__(self, factors: Sequence[torch.Tensor], outs: Sequence[torch.Tensor], steps: int = 5,
+                 coefficients: Sequence[float] = NS_COEFFICIENTS, eps: float = 1e-7, workspace: Optional[torch.Tensor] = None):
+        factors, outs = list(factors), list(outs)
+        assert len(factors) == len(outs) and all(u.shape == o.shape for u, o in zip(factors, outs))
+        here = _one_device(factors + outs)
+        types, out_types = {u.dtype for u in factors} or {torch.float32}, {o.dtype for o in outs} or {torch.float32}
+        assert len(types) == len(out_types) == 1 and types <= set(_DTYPES) and out_types <= set(_DTYPES)
+        self.in_type, self.out_type = _DTYPES[types.pop()], _DTYPES[out_types.pop()]
+
+        def fill(i, f):
+            u, o = factors[i], outs[i]
+            f.rows, f.cols = u.shape
+            f.grad, f.ld_grad, f.out, f.ld_out = _p(u), _row_stride(u, *u.shape), _p(o), _row_stride(o, *o.shape)
+        super().__init__(len(factors), here, steps, coefficients, eps, workspace, fill, (factors, outs))
+
+    def __call__(self, stream: Optional[torch.cuda.Stream] = None) -> Sequence[torch.Tensor]:
+        _check("cwl_orthogonalize", lib().cwl_orthogonalize(self.factors, self.n, self.in_type, self.out_type, C.byref(self.iteration),
+                                                            _p(self.workspace), self.workspace.numel(), self._stream(stream)))
+        return self.keep[1]
+
+
+def cwl_orthogonalize(factors: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None, steps: int = 5,
+                      coefficients: Sequence[float] = NS_COEFFICIENTS, eps: float = 1e-7, out_dtype: torch.dtype = torch.float32,
+                      workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> Sequence[torch.Tensor]:
+    """The factors orthogonalised by ``steps`` Newton-Schulz products; see OrthogonalizeCall for a call made every step."""
+    if outs is None:
+        outs = [torch.empty(u.shape, dtype=out_dtype, device=u.device) for u in factors]
+    return OrthogonalizeCall(factors, outs, steps, coefficients, eps, workspace)(stream)
+
+
+class FactorStep(_FactorCall):
+    """cwl_factor_step of a ladder's factors: the momentum takes the gradient in, the fp32 ``masters`` move by the
+    orthogonalised momentum, and the bf16 copies ``lows`` (None: there are none) follow.  ``scales`` multiply each factor's update; by
+    default sqrt(max(1, rows / cols))."""
+
+    def __init__(self, masters: Sequence[torch.Tensor], lows: Optional[Sequence[torch.Tensor]], grads: Sequence[torch.Tensor],
+                 momenta: Sequence[torch.Tensor], steps: int = 5, coefficients: Sequence[float] = NS_COEFFICIENTS, eps: float = 1e-7,
+                 scales: Optional[Sequence[float]] = None, workspace: Optional[torch.Tensor] = None):
+        masters, grads, momenta = list(masters), list(grads), list(momenta)
+        lows = [None] * len(masters) if lows is None else list(lows)
+        assert len(masters) == len(lows) == len(grads) == len(momenta)
+        here = _one_device(masters + grads + momenta + [t for t in lows if t is not None])
+        types = {g.dtype for g in grads} or {torch.float32}
+        assert len(types) == 1 and types <= set(_DTYPES)
+        for p, low, g, m in zip(masters, lows, grads, momenta):
+            assert p.dtype == m.dtype == torch.float32 and p.shape == g.shape == m.shape
+            assert low is None or (low.dtype == torch.bfloat16 and low.shape == p.shape)
+        if scales is None:
+            scales = [max(1.0, p.shape[0] / p.shape[1]) ** 0.5 for p in masters]
+        assert len(scales) == len(masters)
+        self.in_type = _DTYPES[types.pop()]
+
+        def fill(i, f):
+            p, low, g, m = masters[i], lows[i], grads[i], momenta[i]
+            f.rows, f.cols = p.shape
+            f.grad, f.ld_grad, f.momentum, f.ld_momentum = _p(g), _row_stride(g, *g.shape), _p(m), _row_stride(m, *m.shape)
+            f.out, f.ld_out, f.scale = _p(p), _row_stride(p, *p.shape), float(scales[i])
+            if low is not None:
+                f.low, f.ld_low = _p(low), _row_stride(low, *low.shape)
+        super().__init__(len(masters), here, steps, coefficients, eps, workspace, fill, (masters, lows, grads, momenta))
+
+    def __call__(self, lr: float, momentum: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
+                 stream: Optional[torch.cuda.Stream] = None) -> None:
+        _check("cwl_factor_step", lib().cwl_factor_step(self.factors, self.n, self.in_type, C.byref(self.iteration), lr, momentum,
+                                                        weight_decay, int(nesterov), _p(self.workspace), self.workspace.numel(),
+                                                        self._stream(stream)))
 
 
 def bf16_from_bits(bits, device="cuda") -> torch.Tensor:

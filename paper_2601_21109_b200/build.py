@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcwl.so")
 LIB_HOOKS = os.path.join(HERE, "libcwl_hooks.so")
 SOURCES = ["api.cu", "score.cu", "partition.cu", "align.cu", "stream.cu", "ladder.cu", "apply.cu", "logprobs.cu", "distill.cu",
-           "grads.cu", "head.cu"]
+           "grads.cu", "head.cu", "factors.cu"]
 HOOKED = ["apply.cu", "distill.cu", "grads.cu", "head.cu"]     # sources whose test build differs
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v", "--expt-relaxed-constexpr"]

@@ -1,0 +1,885 @@
+// cwl_orthogonalize and cwl_factor_step: Newton-Schulz orthogonalisation of adapter factors, alone and as a factor's update.
+//
+//   X_0 = U / (|U|_F + eps),   X_(k+1) = a X_k + b (X_k X_k^T) X_k + c (X_k X_k^T)^2 X_k      (X with its short side first)
+//
+// Every X_k is a polynomial in G_0 = X_0 X_0^T times X_0, so the iteration is done on R x R matrices, R the short side:
+//   P_k = a I + b G_k + c G_k^2,   G_(k+1) = P_k G_k P_k,   Q_(k+1) = P_k Q_k,   O = Q_steps X_0
+// U is read twice instead of 2 steps times, and the products over its long side shrink from 2 steps to 1.5 (G_0 is symmetric).
+// The price is precision: directions of singular value s enter G_0 as s^2 and are amplified a^(2 steps) times, so G_0 and the
+// iteration are in 64 bits (on the tensor cores' 64-bit products; in 32 bits, directions of s = 2e-3 would be off by a
+// per cent).  All matrices of the iteration are symmetric and commute: only tiles of the lower triangle are computed.
+//
+//   GRAM     a block per (factor, pair of 64-row blocks, slice of the long side): partial products in 64 bits
+//   ITERATE  R <= 64: a block a factor, all in shared memory.  R > 64: launches of 32 x 32 tiles over L2-resident matrices
+//   APPLY    a block per (factor, 128 columns of the long side, 64 rows): Q U in 32 bits, and the update
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <math.h>
+
+#include "cwl_common.cuh"
+
+namespace cwl {
+namespace {
+
+constexpr int kFewFactors = 16, kMostFactors = 496;   // of a launch: their descriptors are kernel parameters (1 KB, 31 KB)
+constexpr int kShort = 64;                         // R up to which the iteration stays in one block
+
+struct Factor {
+  const void* u;                                   // gradient, or the matrix to orthogonalise
+  float* m;                                        // momentum (step)
+  void* out;                                       // fp32 master (step), or the orthogonalised matrix
+  __nv_bfloat16* low;                              // bf16 copy of the master, or null
+  int ldu, ldm, ldo, ldl;
+  int rows, cols;
+  float scale;                                     // of the update
+  int first;                                       // first block of the launch at hand
+};
+static_assert(sizeof(Factor) == 64, "descriptors in kernel parameters");
+
+struct FactorCommon {
+  int n;
+  int step, nesterov, in_type, out_type;
+  float beta, keep, lr;                            // step: momentum, 1 - lr weight_decay, learning rate
+  int slice;                                       // GRAM: long-side elements a block
+  int steps;
+  double a, b, c, eps;
+  double* partial;                                 // GRAM: [block][64][64]
+  float* q;                                        // [factor] R x R, each `q_stride` apart
+  int64_t q_stride;
+};
+template <int kMost>
+struct FactorArgs {
+  FactorCommon c;
+  Factor f[kMost];
+};
+static_assert(sizeof(FactorArgs<kMostFactors>) <= 32 * 1024 - 256, "kernel parameters");
+
+__host__ __device__ __forceinline__ int short_side(const Factor& f) { return f.rows < f.cols ? f.rows : f.cols; }
+__host__ __device__ __forceinline__ int long_side(const Factor& f) { return f.rows < f.cols ? f.cols : f.rows; }
+__host__ __device__ __forceinline__ int block_pairs(int R) { const int b = (R + 63) / 64; return b * (b + 1) / 2; }
+// blocks of APPLY: 128 elements of the long side, 64 of the short one
+constexpr int kApplyLong = 128, kApplyShort = 64;
+__host__ __device__ __forceinline__ int apply_blocks(const Factor& f) {
+  return ((long_side(f) + kApplyLong - 1) / kApplyLong) * ((short_side(f) + kApplyShort - 1) / kApplyShort);
+}
+
+// The factor that a block of GRAM works on.
+__device__ __forceinline__ int find_factor(const Factor* f, int n, int block) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (f[mid].first <= block) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ float load_typed(const void* p, int64_t at, int type) {
+  if (type == CWL_F32) return static_cast<const float*>(p)[at];
+  if (type == CWL_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]);
+  return __half2float(static_cast<const __half*>(p)[at]);
+}
+// four consecutive elements; `vec`: they lie on a boundary of four
+__device__ __forceinline__ float4 load4(const void* p, int64_t at, int type, bool vec, int left) {
+  if (vec && left >= 4) {
+    if (type == CWL_F32) return *reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+    const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + at);
+    if (type == CWL_BF16)
+      return make_float4(__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xFFFF0000u), __uint_as_float(q.y << 16), __uint_as_float(q.y & 0xFFFF0000u));
+    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&q.x)), y = __half22float2(*reinterpret_cast<const __half2*>(&q.y));
+    return make_float4(x.x, x.y, y.x, y.y);
+  }
+  return make_float4(left > 0 ? load_typed(p, at, type) : 0.f, left > 1 ? load_typed(p, at + 1, type) : 0.f,
+                     left > 2 ? load_typed(p, at + 2, type) : 0.f, left > 3 ? load_typed(p, at + 3, type) : 0.f);
+}
+__device__ __forceinline__ void store4_f32(float* p, const float4& v, bool vec, int left) {
+  if (vec && left >= 4) {
+    *reinterpret_cast<float4*>(p) = v;
+  } else {
+    if (left > 0) p[0] = v.x;
+    if (left > 1) p[1] = v.y;
+    if (left > 2) p[2] = v.z;
+    if (left > 3) p[3] = v.w;
+  }
+}
+__device__ __forceinline__ void store4_bf16(__nv_bfloat16* p, const float4& v, bool vec, int left) {
+  const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+  if (vec && left >= 4) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+  } else {
+    if (left > 0) p[0] = a.x;
+    if (left > 1) p[1] = a.y;
+    if (left > 2) p[2] = b.x;
+    if (left > 3) p[3] = b.y;
+  }
+}
+__device__ __forceinline__ bool vec_rows(const void* p, int ld, int elem) {
+  return (reinterpret_cast<uintptr_t>(p) & (4 * elem - 1)) == 0 && (ld & 3) == 0;
+}
+__device__ __forceinline__ int elem_size(int type) { return type == CWL_F32 ? 4 : 2; }
+
+// Four consecutive elements of U (row r, columns c...), `left` of which exist.  A step's U is the gradient plus the momentum
+// after it took the gradient in; with kUpdate the momentum is brought up to date here.
+template <bool kUpdate>
+__device__ __forceinline__ float4 load_u(const FactorCommon& a, const Factor& f, int r, int c, int left, bool vec_u, bool vec_m) {
+  if (left <= 0) return make_float4(0.f, 0.f, 0.f, 0.f);
+  const float4 g = load4(f.u, (int64_t)r * f.ldu + c, a.in_type, vec_u, left);
+  if (!a.step) return g;
+  float* at = f.m + (int64_t)r * f.ldm + c;
+  float4 m = load4(at, 0, CWL_F32, vec_m, left);
+  if (kUpdate) {
+    m = make_float4(fmaf(a.beta, m.x, g.x), fmaf(a.beta, m.y, g.y), fmaf(a.beta, m.z, g.z), fmaf(a.beta, m.w, g.w));
+    store4_f32(at, m, vec_m, left);
+  }
+  if (!a.nesterov) return m;
+  return make_float4(fmaf(a.beta, m.x, g.x), fmaf(a.beta, m.y, g.y), fmaf(a.beta, m.z, g.z), fmaf(a.beta, m.w, g.w));
+}
+
+// D += A B, 8 x 8 x 4 in 64 bits.  Lane l holds A[l / 4][l % 4], B[l % 4][l / 4] and D[l / 4][2 (l % 4) + {0, 1}]: with B's
+// columns as rows of a symmetric product both operands are read the same way.
+__device__ __forceinline__ void mma_f64(double (&d)[2], double a, double b) {
+  asm("mma.sync.aligned.m8n8k4.row.col.f64.f64.f64.f64 {%0, %1}, {%2}, {%3}, {%0, %1};" : "+d"(d[0]), "+d"(d[1]) : "d"(a), "d"(b));
+}
+
+// ------------------------------------------------------------------------------------------------------------- GRAM
+constexpr int kGramThreads = 128;
+constexpr int kGramK = 32;                         // long-side elements staged at a time
+constexpr int kGramLd = kGramK + 4;                // doubles a row: lanes of a fragment hit different banks
+
+// A 64-row block of U (rows first of the short side, elements k0... of the long side) on its way to shared memory.
+struct GramPiece { float4 v[4]; };
+template <bool kUpdate>
+__device__ __forceinline__ void gram_load(const FactorCommon& a, const Factor& f, bool tall, int first, int k0, int k_end, bool vec_u, bool vec_m, GramPiece& q) {
+  const int R = short_side(f), tid = threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (tall) {                                    // U [long][short]: 16 threads a row of 64
+      const int k = k0 + i * 8 + (tid >> 4), s = first + (tid & 15) * 4;
+      q.v[i] = load_u<kUpdate>(a, f, k, s, k < k_end ? R - s : 0, vec_u, vec_m);
+    } else {                                       // U [short][long]: 8 threads a row of 32
+      const int s = first + i * 16 + (tid >> 3), k = k0 + (tid & 7) * 4;
+      q.v[i] = load_u<kUpdate>(a, f, s, k, s < R ? k_end - k : 0, vec_u, vec_m);
+    }
+  }
+}
+__device__ __forceinline__ void gram_put(double* to, bool tall, const GramPiece& q) {
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float v[4] = {q.v[i].x, q.v[i].y, q.v[i].z, q.v[i].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (tall) to[((tid & 15) * 4 + j) * kGramLd + i * 8 + (tid >> 4)] = (double)v[j];
+      else to[(i * 16 + (tid >> 3)) * kGramLd + (tid & 7) * 4 + j] = (double)v[j];
+    }
+  }
+}
+
+template <int kMost>
+__global__ void __launch_bounds__(kGramThreads, 2) gram_kernel(const __grid_constant__ FactorArgs<kMost> args) {
+  const FactorCommon& a = args.c;
+  __shared__ __align__(16) double rows_i[64 * kGramLd], rows_j[64 * kGramLd];
+  double* sums = rows_j;                           // 36 tiles of 64, where one block of rows is all there is
+  static_assert(64 * kGramLd >= 36 * 64, "room for the tiles");
+  pdl_launch_dependents();
+  pdl_wait();
+  const Factor& f = args.f[find_factor(args.f, a.n, blockIdx.x)];
+  const int R = short_side(f), n = long_side(f), pairs = block_pairs(R);
+  const bool tall = f.rows > f.cols;
+  int unit = blockIdx.x - f.first;
+  const int slice = unit / pairs;
+  int bi = 0, bj = unit % pairs;
+  while (bj > bi) { bj -= bi + 1; ++bi; }          // bj <= bi
+  const int k_begin = slice * a.slice, k_end = min(n, k_begin + a.slice);
+  const bool vec_u = vec_rows(f.u, f.ldu, elem_size(a.in_type)), vec_m = a.step && vec_rows(f.m, f.ldm, 4);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, fr = lane >> 2, fc = lane & 3;
+  double* out = a.partial + (int64_t)blockIdx.x * 64 * 64;
+
+  if (bi == bj) {
+    // 36 tiles of the lower triangle in every warp, which takes a quarter of the K steps: eight fragments serve 36 products
+    const int tiles = min(8, (R - bi * 64 + 7) / 8);
+    double acc[36][2];
+#pragma unroll
+    for (int i = 0; i < 36; ++i) acc[i][0] = acc[i][1] = 0.0;
+    GramPiece q;
+    const bool update = a.step != 0 && R <= kShort;  // each element is read by one block only
+    if (update) gram_load<true>(a, f, tall, bi * 64, k_begin, k_end, vec_u, vec_m, q);
+    else gram_load<false>(a, f, tall, bi * 64, k_begin, k_end, vec_u, vec_m, q);
+    for (int k0 = k_begin; k0 < k_end; k0 += kGramK) {
+      __syncthreads();
+      gram_put(rows_i, tall, q);
+      __syncthreads();
+      if (k0 + kGramK < k_end) {
+        if (update) gram_load<true>(a, f, tall, bi * 64, k0 + kGramK, k_end, vec_u, vec_m, q);
+        else gram_load<false>(a, f, tall, bi * 64, k0 + kGramK, k_end, vec_u, vec_m, q);
+      }
+#pragma unroll 1
+      for (int s = warp; s < kGramK / 4; s += 4) {
+        double x[8];
+#pragma unroll
+        for (int t = 0; t < 8; ++t) x[t] = rows_i[(t * 8 + fr) * kGramLd + s * 4 + fc];
+#pragma unroll
+        for (int ti = 0; ti < 8; ++ti) {
+          if (ti < tiles) {
+#pragma unroll
+            for (int tj = 0; tj <= ti; ++tj) mma_f64(acc[ti * (ti + 1) / 2 + tj], x[ti], x[tj]);
+          }
+        }
+      }
+    }
+    // the warps' sums, in their order
+    for (int w = 0; w < 4; ++w) {
+      __syncthreads();
+      if (warp == w) {
+#pragma unroll
+        for (int i = 0; i < 36; ++i) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            double* s = sums + i * 64 + fr * 8 + fc * 2 + j;
+            *s = w == 0 ? acc[i][j] : *s + acc[i][j];
+          }
+        }
+      }
+    }
+    __syncthreads();
+    for (int at = threadIdx.x; at < 64 * 64; at += kGramThreads) {
+      const int r = at >> 6, c = at & 63;
+      const int hi = max(r, c), lo = min(r, c);    // of tiles on the diagonal both halves are there
+      const int ti = hi >> 3, tj = lo >> 3;
+      out[at] = sums[(ti * (ti + 1) / 2 + tj) * 64 + (hi & 7) * 8 + (lo & 7)];
+    }
+  } else {
+    // a warp a quadrant of 32 x 32
+    const int qi = (warp >> 1) * 32, qj = (warp & 1) * 32;
+    double acc[4][4][2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j][0] = acc[i][j][1] = 0.0;
+    GramPiece q, r;
+    gram_load<false>(a, f, tall, bi * 64, k_begin, k_end, vec_u, vec_m, q);
+    gram_load<false>(a, f, tall, bj * 64, k_begin, k_end, vec_u, vec_m, r);
+    for (int k0 = k_begin; k0 < k_end; k0 += kGramK) {
+      __syncthreads();
+      gram_put(rows_i, tall, q);
+      gram_put(rows_j, tall, r);
+      __syncthreads();
+      if (k0 + kGramK < k_end) {
+        gram_load<false>(a, f, tall, bi * 64, k0 + kGramK, k_end, vec_u, vec_m, q);
+        gram_load<false>(a, f, tall, bj * 64, k0 + kGramK, k_end, vec_u, vec_m, r);
+      }
+#pragma unroll
+      for (int s = 0; s < kGramK / 4; ++s) {
+        double x[4], y[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          x[t] = rows_i[(qi + t * 8 + fr) * kGramLd + s * 4 + fc];
+          y[t] = rows_j[(qj + t * 8 + fr) * kGramLd + s * 4 + fc];
+        }
+#pragma unroll
+        for (int ti = 0; ti < 4; ++ti)
+#pragma unroll
+          for (int tj = 0; tj < 4; ++tj) mma_f64(acc[ti][tj], x[ti], y[tj]);
+      }
+    }
+#pragma unroll
+    for (int ti = 0; ti < 4; ++ti)
+#pragma unroll
+      for (int tj = 0; tj < 4; ++tj)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) out[(qi + ti * 8 + fr) * 64 + qj + tj * 8 + fc * 2 + j] = acc[ti][tj][j];
+  }
+}
+
+// Momentum of the factors whose elements GRAM reads more than once (R > 64).
+constexpr int kMomentumThreads = 256;
+template <int kMost>
+__global__ void __launch_bounds__(kMomentumThreads) momentum_kernel(const __grid_constant__ FactorArgs<kMost> args) {
+  pdl_launch_dependents();
+  pdl_wait();
+  const FactorCommon& a = args.c;
+  const Factor& f = args.f[blockIdx.y];
+  if (short_side(f) <= kShort) return;
+  const bool vec_u = vec_rows(f.u, f.ldu, elem_size(a.in_type)), vec_m = vec_rows(f.m, f.ldm, 4);
+  const int per_row = (f.cols + 3) / 4;
+  const int64_t total = (int64_t)f.rows * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * kMomentumThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kMomentumThreads) {
+    const int r = (int)(i / per_row), c = (int)(i % per_row) * 4;
+    load_u<true>(a, f, r, c, f.cols - c, vec_u, vec_m);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------- ITERATE, R <= 64
+constexpr int kIterThreads = 256;
+constexpr int kIterLd = 68;                        // doubles a row
+constexpr size_t kIterSmem = ((size_t)4 * 64 * kIterLd + 1) * 8;
+
+__device__ __forceinline__ void lower_tile(int i, int& ti, int& tj) {
+  ti = 0;
+  while (i > ti) { i -= ti + 1; ++ti; }
+  tj = i;
+}
+
+// Tiles of this warp of the product of two symmetric, commuting matrices in shared memory.
+struct IterTiles { double d[5][2]; };
+__device__ __forceinline__ void iter_product(const double* x, const double* y, int n_tiles, int k_steps, int warp, int fr, int fc, IterTiles& t) {
+#pragma unroll
+  for (int i = 0; i < 5; ++i) {
+    t.d[i][0] = t.d[i][1] = 0.0;
+    const int tile = warp + 8 * i;
+    if (tile < n_tiles) {
+      int ti, tj;
+      lower_tile(tile, ti, tj);
+      const double* p = x + (ti * 8 + fr) * kIterLd + fc;
+      const double* q = y + (tj * 8 + fr) * kIterLd + fc;
+      double odd[2] = {0.0, 0.0};
+#pragma unroll 4
+      for (int k = 0; k < k_steps; k += 2) {
+        mma_f64(t.d[i], p[k * 4], q[k * 4]);
+        mma_f64(odd, p[k * 4 + 4], q[k * 4 + 4]);
+      }
+      t.d[i][0] += odd[0];
+      t.d[i][1] += odd[1];
+    }
+  }
+}
+template <typename F>
+__device__ __forceinline__ void iter_store(double* to, int n_tiles, int warp, int fr, int fc, const IterTiles& t, F value) {
+#pragma unroll
+  for (int i = 0; i < 5; ++i) {
+    const int tile = warp + 8 * i;
+    if (tile < n_tiles) {
+      int ti, tj;
+      lower_tile(tile, ti, tj);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = ti * 8 + fr, c = tj * 8 + fc * 2 + j;
+        const double v = value(r, c, t.d[i][j]);
+        if (ti != tj || c <= r) {                  // one value for both halves
+          to[r * kIterLd + c] = v;
+          to[c * kIterLd + r] = v;
+        }
+      }
+    }
+  }
+}
+
+template <int kMost>
+__global__ void __launch_bounds__(kIterThreads) iterate_kernel(const __grid_constant__ FactorArgs<kMost> args) {
+  const FactorCommon& a = args.c;
+  extern __shared__ __align__(16) double iter_raw[];
+  double* G = iter_raw;
+  double* P = G + 64 * kIterLd;
+  double* S = P + 64 * kIterLd;
+  double* Q = S + 64 * kIterLd;
+  double& size_slot = Q[64 * kIterLd];
+  pdl_launch_dependents();
+  pdl_wait();
+  const Factor& f = args.f[blockIdx.x];
+  const int R = short_side(f);
+  if (R > kShort) return;
+  const int n = long_side(f), slices = (n + a.slice - 1) / a.slice;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, fr = lane >> 2, fc = lane & 3;
+  const double* part = a.partial + (int64_t)f.first * 64 * 64;
+  for (int at = tid; at < 64 * 64; at += kIterThreads) {
+    double s = 0.0;
+#pragma unroll 4
+    for (int k = 0; k < slices; ++k) s += part[(int64_t)k * 64 * 64 + at];
+    G[(at >> 6) * kIterLd + (at & 63)] = s;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    double s = 0.0;
+    for (int i = 0; i < R; ++i) s += G[i * kIterLd + i];
+    size_slot = s;
+  }
+  __syncthreads();
+  const double trace = size_slot, size = sqrt(trace) + a.eps;
+  const double unit = trace == 0.0 ? 0.0 : 1.0 / size;        // a factor of zeros stays one
+  for (int at = tid; at < 64 * 64; at += kIterThreads) G[(at >> 6) * kIterLd + (at & 63)] *= unit * unit;
+  const int t8 = (R + 7) / 8, n_tiles = t8 * (t8 + 1) / 2, k_steps = (t8 * 2);
+  IterTiles t, u;
+  for (int step = 0; step < a.steps; ++step) {
+    const bool first = step == 0, last = step + 1 == a.steps;
+    __syncthreads();
+    iter_product(G, G, n_tiles, k_steps, warp, fr, fc, t);
+    iter_store(P, n_tiles, warp, fr, fc, t, [&](int r, int c, double v) { return (r == c ? a.a : 0.0) + a.b * G[r * kIterLd + c] + a.c * v; });
+    __syncthreads();
+    if (!first) iter_product(P, Q, n_tiles, k_steps, warp, fr, fc, u);
+    if (!last) iter_product(P, G, n_tiles, k_steps, warp, fr, fc, t);
+    __syncthreads();
+    if (first) {
+      for (int at = tid; at < 64 * 64; at += kIterThreads) Q[(at >> 6) * kIterLd + (at & 63)] = P[(at >> 6) * kIterLd + (at & 63)];
+    } else {
+      iter_store(Q, n_tiles, warp, fr, fc, u, [](int, int, double v) { return v; });
+    }
+    if (last) break;
+    iter_store(S, n_tiles, warp, fr, fc, t, [](int, int, double v) { return v; });
+    __syncthreads();
+    iter_product(P, S, n_tiles, k_steps, warp, fr, fc, t);
+    iter_store(G, n_tiles, warp, fr, fc, t, [](int, int, double v) { return v; });
+  }
+  __syncthreads();
+  float* q = a.q + blockIdx.x * a.q_stride;
+  for (int at = tid; at < R * R; at += kIterThreads) q[at] = (float)(Q[(at / R) * kIterLd + at % R] * unit);
+}
+
+// ------------------------------------------------------------------------------------------------- ITERATE, R > 64
+// Matrices of padded size Rp (a multiple of 32) in the workspace, of which lower tiles of 32 x 32 are computed, and mirrored.
+struct BigArgs {
+  int n, steps, slice;
+  double a, b, c, eps;
+  const double* partial;
+  double* big;                                     // [factor of this list][G, P, S, Q, Q of the next step][stride]
+  int64_t stride;
+  double* unit;                                    // [factor of this list] 1 / (norm + eps)
+  float* q; int64_t q_stride;
+  uint16_t which[kMostFactors], R[kMostFactors];   // place in the call's list, short side
+  int first[kMostFactors], slices[kMostFactors];   // GRAM's blocks
+};
+static_assert(sizeof(BigArgs) <= 8 * 1024, "kernel parameters");
+__host__ __device__ __forceinline__ int padded(int R) { return (R + 31) / 32 * 32; }
+
+// Sums of GRAM's partial products, scaled: G_0.  A block a 64 x 64 pair.
+__global__ void __launch_bounds__(kIterThreads) big_gram_kernel(const __grid_constant__ BigArgs a) {
+  __shared__ double met[kIterThreads / 32];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int R = a.R[blockIdx.y], pairs = block_pairs(R), slices = a.slices[blockIdx.y];
+  if ((int)blockIdx.x >= pairs) return;
+  const int Rp = padded(R), tid = threadIdx.x;
+  int bi = 0, bj = blockIdx.x;
+  while (bj > bi) { bj -= bi + 1; ++bi; }
+  const double* part = a.partial + (int64_t)a.first[blockIdx.y] * 64 * 64;
+  // the trace: every block adds it up in the same order
+  double s = 0.0;
+  for (int i = tid; i < R; i += kIterThreads) {
+    const int b = i >> 6, pair = b * (b + 1) / 2 + b;
+#pragma unroll 4
+    for (int k = 0; k < slices; ++k) s += part[((int64_t)k * pairs + pair) * 64 * 64 + (i & 63) * 65];
+  }
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((tid & 31) == 0) met[tid >> 5] = s;
+  __syncthreads();
+  double trace = 0.0;
+  for (int w = 0; w < kIterThreads / 32; ++w) trace += met[w];
+  const double unit = trace == 0.0 ? 0.0 : 1.0 / (sqrt(trace) + a.eps);
+  double* G = a.big + (int64_t)blockIdx.y * 5 * a.stride;
+  for (int at = tid; at < 64 * 64; at += kIterThreads) {
+    const int r = bi * 64 + (at >> 6), c = bj * 64 + (at & 63);
+    if (r >= Rp || c >= Rp) continue;
+    double v = 0.0;
+#pragma unroll 4
+    for (int k = 0; k < slices; ++k) v += part[((int64_t)k * pairs + blockIdx.x) * 64 * 64 + at];
+    v *= unit * unit;
+    G[(int64_t)r * Rp + c] = v;
+    if (bi != bj) G[(int64_t)c * Rp + r] = v;
+  }
+  if (blockIdx.x == 0 && tid == 0) a.unit[blockIdx.y] = unit;
+}
+
+// One product a launch (two where they do not depend on one another):
+//   POLY    P = a I + b G + c G G; in the first step this is Q too
+//   SPREAD  S = P G, and Q' = P Q (z = 1, or alone in the last step, where it leaves as fp32, times 1 / (norm + eps))
+//   GRAM    G = P S
+enum : int { BIG_POLY = 0, BIG_SPREAD = 1, BIG_GRAM = 2 };
+constexpr int kBigThreads = 128;
+constexpr int kBigLd = CWL_MAX_RANK + 4;
+constexpr size_t kBigSmem = (size_t)2 * 32 * kBigLd * 8;
+__global__ void __launch_bounds__(kBigThreads) big_product_kernel(const __grid_constant__ BigArgs a, int what, int step) {
+  extern __shared__ __align__(16) double big_raw[];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int R = a.R[blockIdx.y], Rp = padded(R);
+  int ti = 0, tj = blockIdx.x;
+  while (tj > ti) { tj -= ti + 1; ++ti; }
+  if (ti >= Rp / 32) return;
+  const bool last = step + 1 == a.steps;
+  double* G = a.big + (int64_t)blockIdx.y * 5 * a.stride;
+  double* P = G + a.stride;
+  double* S = P + a.stride;
+  double* Q = S + a.stride + (step & 1) * a.stride;
+  double* Q_next = S + a.stride + ((step + 1) & 1) * a.stride;
+  const bool of_q = what == BIG_SPREAD && (last || blockIdx.z == 1);
+  const double* x = what == BIG_POLY ? G : P;
+  const double* y = what == BIG_GRAM ? S : of_q ? Q : G;
+  double* to = what == BIG_POLY ? P : what == BIG_GRAM ? G : of_q ? Q_next : S;
+  double* rows_x = big_raw;
+  double* rows_y = big_raw + 32 * kBigLd;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, fr = lane >> 2, fc = lane & 3;
+#pragma unroll 8
+  for (int i = tid; i < 32 * (Rp / 2); i += kBigThreads) {
+    const int r = i / (Rp / 2), c = (i % (Rp / 2)) * 2;
+    *reinterpret_cast<double2*>(rows_x + r * kBigLd + c) = *reinterpret_cast<const double2*>(x + (int64_t)(ti * 32 + r) * Rp + c);
+    *reinterpret_cast<double2*>(rows_y + r * kBigLd + c) = *reinterpret_cast<const double2*>(y + (int64_t)(tj * 32 + r) * Rp + c);
+  }
+  __syncthreads();
+  const int qi = (warp >> 1) * 16, qj = (warp & 1) * 16;
+  double acc[2][2][2] = {};
+#pragma unroll 4
+  for (int k = 0; k < Rp / 4; ++k) {
+    double u[2], v[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      u[t] = rows_x[(qi + t * 8 + fr) * kBigLd + k * 4 + fc];
+      v[t] = rows_y[(qj + t * 8 + fr) * kBigLd + k * 4 + fc];
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) mma_f64(acc[i][j], u[i], v[j]);
+  }
+  float* q = a.q + a.which[blockIdx.y] * a.q_stride;
+  const double unit = of_q || (what == BIG_POLY && a.steps == 1) ? a.unit[blockIdx.y] : 0.0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int r = ti * 32 + qi + i * 8 + fr, c = tj * 32 + qj + j * 8 + fc * 2 + k;
+        if (ti == tj && c > r) continue;           // one value for both halves
+        double v = acc[i][j][k];
+        if (what == BIG_POLY) v = (r == c ? a.a : 0.0) + a.b * G[(int64_t)r * Rp + c] + a.c * v;
+        if (last && (of_q || what == BIG_POLY && step == 0)) {
+          if (r < R && c < R) q[(int64_t)r * R + c] = q[(int64_t)c * R + r] = (float)(v * unit);
+          if (of_q) continue;
+        }
+        to[(int64_t)r * Rp + c] = v;
+        to[(int64_t)c * Rp + r] = v;
+        if (what == BIG_POLY && step == 0) {
+          Q_next[(int64_t)r * Rp + c] = v;
+          Q_next[(int64_t)c * Rp + r] = v;
+        }
+      }
+}
+
+// ------------------------------------------------------------------------------------------------------------ APPLY
+// O = Q U over 64 short-side rows and 128 long-side elements.  Outputs of a thread: 8 x 4 with the lanes along the rows of the
+// factor as they lie in memory, whichever side that is.
+constexpr int kApplyThreads = 256;
+constexpr int kApplyK = 32;
+constexpr int kApplyLdX = kApplyLong + 4, kApplyLdQ = kApplyShort + 4;
+
+template <bool kTall>
+__device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& f, const float* q, int long0, int short0, float* xs, float* qs) {
+  const int R = short_side(f), n = long_side(f), tid = threadIdx.x;
+  const bool vec_u = vec_rows(f.u, f.ldu, elem_size(a.in_type)), vec_m = a.step && vec_rows(f.m, f.ldm, 4);
+  const bool vec_q = (R & 3) == 0;
+  // this thread's outputs: short side s0.., long side l0..
+  constexpr int kS = kTall ? 4 : 8, kL = kTall ? 8 : 4;
+  const int s0 = kTall ? (tid & 15) * 4 : (tid >> 5) * 8, l0 = kTall ? (tid >> 4) * 8 : (tid & 31) * 4;
+  float acc[kS][kL];
+#pragma unroll
+  for (int i = 0; i < kS; ++i)
+#pragma unroll
+    for (int j = 0; j < kL; ++j) acc[i][j] = 0.f;
+
+  float4 x[4], y[2];
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (kTall) {                                 // U [long][short]: eight threads 32 of a row
+        const int l = long0 + i * 32 + (tid >> 3), k = k0 + (tid & 7) * 4;
+        x[i] = load_u<false>(a, f, l, k, l < n ? R - k : 0, vec_u, vec_m);
+      } else {                                     // U [short][long]: a warp 128 of a row
+        const int k = k0 + i * 8 + (tid >> 5), l = long0 + (tid & 31) * 4;
+        x[i] = load_u<false>(a, f, k, l, k < R ? n - l : 0, vec_u, vec_m);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {                  // Q is symmetric: its row k is the column wanted
+      const int k = k0 + i * 16 + (tid >> 4), s = short0 + (tid & 15) * 4, left = k < R ? R - s : 0;
+      y[i] = load4(q, (int64_t)k * R + s, CWL_F32, vec_q, left);
+    }
+  };
+  fetch(0);
+  for (int k0 = 0; k0 < R; k0 += kApplyK) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (kTall) {
+        const int l = i * 32 + (tid >> 3), k = (tid & 7) * 4;
+        xs[k * kApplyLdX + l] = x[i].x; xs[(k + 1) * kApplyLdX + l] = x[i].y;
+        xs[(k + 2) * kApplyLdX + l] = x[i].z; xs[(k + 3) * kApplyLdX + l] = x[i].w;
+      } else {
+        *reinterpret_cast<float4*>(xs + (i * 8 + (tid >> 5)) * kApplyLdX + (tid & 31) * 4) = x[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<float4*>(qs + (i * 16 + (tid >> 4)) * kApplyLdQ + (tid & 15) * 4) = y[i];
+    __syncthreads();
+    if (k0 + kApplyK < R) fetch(k0 + kApplyK);
+#pragma unroll 8
+    for (int k = 0; k < kApplyK; ++k) {
+      float sv[kS], lv[kL];
+#pragma unroll
+      for (int i = 0; i < kS; i += 4) *reinterpret_cast<float4*>(sv + i) = *reinterpret_cast<const float4*>(qs + k * kApplyLdQ + s0 + i);
+#pragma unroll
+      for (int j = 0; j < kL; j += 4) *reinterpret_cast<float4*>(lv + j) = *reinterpret_cast<const float4*>(xs + k * kApplyLdX + l0 + j);
+#pragma unroll
+      for (int i = 0; i < kS; ++i)
+#pragma unroll
+        for (int j = 0; j < kL; ++j) acc[i][j] = fmaf(sv[i], lv[j], acc[i][j]);
+    }
+  }
+
+  const int out_type = a.step ? CWL_F32 : a.out_type;
+  const bool vec_o = vec_rows(f.out, f.ldo, elem_size(out_type)), vec_l = f.low != nullptr && vec_rows(f.low, f.ldl, 2);
+  const float by = a.step ? -a.lr * f.scale : 1.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    // four neighbours of a row of the factor
+    const int r = kTall ? long0 + l0 + i : short0 + s0 + i, c = kTall ? short0 + s0 : long0 + l0;
+    const int left = r < f.rows ? f.cols - c : 0;
+    if (left <= 0) continue;
+    float4 v = kTall ? make_float4(acc[0][i % kL], acc[1 % kS][i % kL], acc[2 % kS][i % kL], acc[3 % kS][i % kL])
+                     : make_float4(acc[i % kS][0], acc[i % kS][1 % kL], acc[i % kS][2 % kL], acc[i % kS][3 % kL]);
+    if (a.step) {
+      float* at = static_cast<float*>(f.out) + (int64_t)r * f.ldo + c;
+      const float4 p = load4(at, 0, CWL_F32, vec_o, left);
+      v = make_float4(fmaf(by, v.x, a.keep * p.x), fmaf(by, v.y, a.keep * p.y), fmaf(by, v.z, a.keep * p.z), fmaf(by, v.w, a.keep * p.w));
+      store4_f32(at, v, vec_o, left);
+      if (f.low != nullptr) store4_bf16(f.low + (int64_t)r * f.ldl + c, v, vec_l, left);
+    } else if (out_type == CWL_F32) {
+      store4_f32(static_cast<float*>(f.out) + (int64_t)r * f.ldo + c, v, vec_o, left);
+    } else {
+      store4_bf16(static_cast<__nv_bfloat16*>(f.out) + (int64_t)r * f.ldo + c, v, vec_o, left);
+    }
+  }
+}
+
+template <int kMost>
+__global__ void __launch_bounds__(kApplyThreads, 2) apply_factors_kernel(const __grid_constant__ FactorArgs<kMost> args) {
+  __shared__ __align__(16) float xs[kApplyK * kApplyLdX], qs[kApplyK * kApplyLdQ];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int at = find_factor(args.f, args.c.n, blockIdx.x);
+  const Factor& f = args.f[at];
+  const int unit = blockIdx.x - f.first, row_tiles = (short_side(f) + kApplyShort - 1) / kApplyShort;
+  const int long0 = unit / row_tiles * kApplyLong, short0 = unit % row_tiles * kApplyShort;
+  const float* q = args.c.q + at * args.c.q_stride;
+  if (f.rows > f.cols) apply_tile<true>(args.c, f, q, long0, short0, xs, qs);
+  else apply_tile<false>(args.c, f, q, long0, short0, xs, qs);
+}
+
+// ------------------------------------------------------------------------------------------------------------- host
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+// Long-side elements a block of GRAM: short enough that the blocks fill the GPU evenly, long enough that their sums
+// (32 KB a block) stay a small part of what is read.
+constexpr int64_t kGramBlocks = 2400;
+constexpr int kGramLeast = 256;
+struct FactorPlan { int slice, n_big, most_R; int64_t blocks; size_t partial, q, big, unit, total; int64_t q_stride, stride; };
+template <typename Item>
+FactorPlan factor_plan(const Item* items, int n) {
+  FactorPlan p = {};
+  int64_t work = 0;
+  int big = 0;
+  for (int i = 0; i < n; ++i) {
+    const int R = items[i].rows < items[i].cols ? items[i].rows : items[i].cols, len = items[i].rows < items[i].cols ? items[i].cols : items[i].rows;
+    work += (int64_t)block_pairs(R) * len;
+    if (R > p.most_R) p.most_R = R;
+    if (R > kShort) { ++p.n_big; if (R > big) big = R; }
+  }
+  int64_t slice = (work + kGramBlocks - 1) / kGramBlocks;
+  slice = (slice + kGramK - 1) / kGramK * kGramK;
+  if (slice < kGramLeast) slice = kGramLeast;
+  if (slice > 1 << 20) slice = 1 << 20;
+  p.slice = (int)slice;
+  for (int i = 0; i < n; ++i) {
+    const int R = items[i].rows < items[i].cols ? items[i].rows : items[i].cols, len = items[i].rows < items[i].cols ? items[i].cols : items[i].rows;
+    p.blocks += (int64_t)block_pairs(R) * ceil_div(len, p.slice);
+  }
+  p.q_stride = ((int64_t)p.most_R * p.most_R + 3) / 4 * 4;
+  p.stride = (int64_t)padded(big) * padded(big);
+  p.q = align256((size_t)p.blocks * 64 * 64 * 8);
+  p.big = p.q + align256((size_t)p.q_stride * n * 4);
+  p.unit = p.big + align256((size_t)p.stride * 5 * p.n_big * 8);
+  p.total = p.unit + align256((size_t)p.n_big * 8);
+  return p;
+}
+
+// Items are worked on in groups whose descriptors fit a launch; the groups follow one another and share the workspace.
+template <typename Item>
+size_t factor_bytes(const Item* items, int n) {
+  size_t most = 0;
+  for (int i = 0; i < n; i += kMostFactors) {
+    const size_t b = factor_plan(items + i, n - i < kMostFactors ? n - i : kMostFactors).total;
+    if (b > most) most = b;
+  }
+  return most;
+}
+
+template <int kMost, typename Item, typename Fill>
+cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, void* workspace, bool chained, cudaStream_t st) {
+  const FactorPlan plan = factor_plan(items, n);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  FactorArgs<kMost> args;
+  args.c = common;
+  args.c.n = n;
+  args.c.slice = plan.slice;
+  args.c.partial = reinterpret_cast<double*>(ws);
+  args.c.q = reinterpret_cast<float*>(ws + plan.q);
+  args.c.q_stride = plan.q_stride;
+  BigArgs big;
+  big.n = 0; big.steps = common.steps; big.slice = plan.slice;
+  big.a = common.a; big.b = common.b; big.c = common.c; big.eps = common.eps;
+  big.partial = args.c.partial;
+  big.big = reinterpret_cast<double*>(ws + plan.big); big.stride = plan.stride;
+  big.unit = reinterpret_cast<double*>(ws + plan.unit);
+  big.q = args.c.q; big.q_stride = plan.q_stride;
+  int64_t gram_blocks = 0, blocks = 0;
+  bool any_small = false;
+  int most_R = 0;
+  int64_t most_elements = 0;
+  for (int i = 0; i < n; ++i) {
+    Factor& f = args.f[i];
+    f = Factor{};
+    f.rows = items[i].rows; f.cols = items[i].cols;
+    fill(items[i], f);
+    f.first = (int)gram_blocks;
+    const int R = short_side(f), slices = ceil_div(long_side(f), plan.slice);
+    if (R > kShort) {
+      big.which[big.n] = (uint16_t)i; big.R[big.n] = (uint16_t)R; big.first[big.n] = f.first; big.slices[big.n] = slices;
+      ++big.n;
+      if (R > most_R) most_R = R;
+      const int64_t e = (int64_t)f.rows * f.cols;
+      if (e > most_elements) most_elements = e;
+    } else {
+      any_small = true;
+    }
+    gram_blocks += (int64_t)block_pairs(R) * slices;
+  }
+  if (common.step && big.n > 0) {
+    const int64_t x = (most_elements / 4 + kMomentumThreads * 4 - 1) / (kMomentumThreads * 4);
+    CWL_CUDA_TRY(launch_chained(chained, momentum_kernel<kMost>, dim3((unsigned)(x < 592 ? x + 1 : 592), (unsigned)n), dim3(kMomentumThreads), 0, st, args));
+  }
+  CWL_CUDA_TRY(launch_chained(chained, gram_kernel<kMost>, dim3((unsigned)gram_blocks), dim3(kGramThreads), 0, st, args));
+  if (any_small) {
+    static SharedMemoryGrant grant;
+    CWL_CUDA_TRY(grant(iterate_kernel<kMost>));
+    CWL_CUDA_TRY(launch_chained(chained, iterate_kernel<kMost>, dim3((unsigned)n), dim3(kIterThreads), kIterSmem, st, args));
+  }
+  if (big.n > 0) {
+    static SharedMemoryGrant grant;
+    CWL_CUDA_TRY(grant(big_product_kernel));
+    CWL_CUDA_TRY(launch_chained(chained, big_gram_kernel, dim3((unsigned)block_pairs(most_R), (unsigned)big.n), dim3(kIterThreads), 0, st, big));
+    const int t = padded(most_R) / 32, tiles = t * (t + 1) / 2;
+    for (int step = 0; step < common.steps; ++step) {
+      const bool last = step + 1 == common.steps;
+      auto product = [&](int what, int z) {
+        return launch_chained(chained, big_product_kernel, dim3((unsigned)tiles, (unsigned)big.n, (unsigned)z), dim3(kBigThreads), kBigSmem, st, big, what, step);
+      };
+      CWL_CUDA_TRY(product(BIG_POLY, 1));
+      if (last && step == 0) break;
+      CWL_CUDA_TRY(product(BIG_SPREAD, step == 0 || last ? 1 : 2));
+      if (!last) CWL_CUDA_TRY(product(BIG_GRAM, 1));
+    }
+  }
+  for (int i = 0; i < n; ++i) {
+    args.f[i].first = (int)blocks;
+    blocks += apply_blocks(args.f[i]);
+  }
+  CWL_CUDA_TRY(launch_chained(chained, apply_factors_kernel<kMost>, dim3((unsigned)blocks), dim3(kApplyThreads), 0, st, args));
+  return CWL_OK;
+}
+
+template <typename Item, typename Fill>
+cwl_status run_factors(const Item* items, int n, const FactorCommon& common, Fill fill, void* workspace, size_t workspace_bytes, void* stream) {
+  if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < factor_bytes(items, n)) return CWL_ERR_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool chained = !stream_is_capturing(st);
+  for (int i = 0; i < n; i += kMostFactors) {
+    const int m = n - i < kMostFactors ? n - i : kMostFactors;
+    const cwl_status s = m <= kFewFactors ? run_group<kFewFactors>(items + i, m, common, fill, workspace, chained, st)
+                                          : run_group<kMostFactors>(items + i, m, common, fill, workspace, chained, st);
+    if (s != CWL_OK) return s;
+  }
+  return CWL_OK;
+}
+
+bool bad_type(cwl_dtype t) { return t != CWL_F32 && t != CWL_BF16 && t != CWL_F16; }
+cwl_status check_iteration(const cwl_newton_schulz* ns) {
+  if (ns == nullptr || ns->steps < 1 || ns->steps > CWL_MAX_NS_STEPS) return CWL_ERR_INVALID_ARG;
+  if (!isfinite(ns->a) || !isfinite(ns->b) || !isfinite(ns->c) || !(ns->eps >= 0.0) || !isfinite(ns->eps)) return CWL_ERR_INVALID_ARG;
+  return CWL_OK;
+}
+constexpr int kMostLong = 1 << 22;
+cwl_status check_size(int rows, int cols) {
+  if (rows < 1 || cols < 1) return CWL_ERR_INVALID_ARG;
+  const int R = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+  return R > CWL_MAX_RANK || n > kMostLong ? CWL_ERR_UNSUPPORTED : CWL_OK;
+}
+// element alignment, and rows that do not run into one another
+bool bad_rows(const void* p, int64_t ld, int rows, int cols, int elem) {
+  return (reinterpret_cast<uintptr_t>(p) % elem) != 0 || (rows > 1 && ld < cols) || ld > INT32_MAX || ld < 0;
+}
+int row_step(int64_t ld, int rows, int cols) { return rows > 1 ? (int)ld : cols; }
+int type_bytes(cwl_dtype t) { return t == CWL_F32 ? 4 : 2; }
+
+}  // namespace
+}  // namespace cwl
+
+extern "C" size_t cwl_orthogonalize_workspace_bytes(const cwl_factor* factors, int32_t n) {
+  if (factors == nullptr || n <= 0) return 0;
+  for (int i = 0; i < n; ++i)
+    if (cwl::check_size(factors[i].rows, factors[i].cols) != CWL_OK) return 0;
+  return cwl::factor_bytes(factors, n);
+}
+
+extern "C" cwl_status cwl_orthogonalize(const cwl_factor* factors, int32_t n, cwl_dtype in_dtype, cwl_dtype out_dtype,
+                                        const cwl_newton_schulz* iteration, void* workspace, size_t workspace_bytes, void* stream) try {
+  using namespace cwl;
+  if (n < 0 || (n > 0 && factors == nullptr)) return CWL_ERR_INVALID_ARG;
+  if (bad_type(in_dtype) || (out_dtype != CWL_F32 && out_dtype != CWL_BF16)) return CWL_ERR_INVALID_ARG;
+  cwl_status s = check_iteration(iteration);
+  if (s != CWL_OK) return s;
+  for (int i = 0; i < n; ++i) {
+    const cwl_factor& f = factors[i];
+    if ((s = check_size(f.rows, f.cols)) != CWL_OK) return s;
+    if (f.grad == nullptr || f.out == nullptr) return CWL_ERR_INVALID_ARG;
+    if (bad_rows(f.grad, f.ld_grad, f.rows, f.cols, type_bytes(in_dtype)) || bad_rows(f.out, f.ld_out, f.rows, f.cols, type_bytes(out_dtype))) return CWL_ERR_SHAPE;
+  }
+  if (n == 0) return CWL_OK;
+  FactorCommon c = {};
+  c.in_type = in_dtype; c.out_type = out_dtype;
+  c.steps = iteration->steps; c.a = iteration->a; c.b = iteration->b; c.c = iteration->c; c.eps = iteration->eps;
+  return run_factors(factors, n, c, [](const cwl_factor& i, Factor& f) {
+    f.u = i.grad; f.out = i.out;
+    f.ldu = row_step(i.ld_grad, i.rows, i.cols); f.ldo = row_step(i.ld_out, i.rows, i.cols);
+  }, workspace, workspace_bytes, stream);
+} catch (...) {
+  return CWL_ERR_CUDA;                                   // nothing may leave a C entry
+}
+
+extern "C" cwl_status cwl_factor_step(const cwl_factor* factors, int32_t n, cwl_dtype grad_dtype, const cwl_newton_schulz* iteration,
+                                      float lr, float momentum, float weight_decay, int32_t nesterov,
+                                      void* workspace, size_t workspace_bytes, void* stream) try {
+  using namespace cwl;
+  if (n < 0 || (n > 0 && factors == nullptr) || bad_type(grad_dtype)) return CWL_ERR_INVALID_ARG;
+  if (!isfinite(lr) || !isfinite(weight_decay) || !(momentum >= 0.f) || !(momentum < 1.f)) return CWL_ERR_INVALID_ARG;
+  cwl_status s = check_iteration(iteration);
+  if (s != CWL_OK) return s;
+  for (int i = 0; i < n; ++i) {
+    const cwl_factor& f = factors[i];
+    if ((s = check_size(f.rows, f.cols)) != CWL_OK) return s;
+    if (f.grad == nullptr || f.momentum == nullptr || f.out == nullptr || !isfinite(f.scale)) return CWL_ERR_INVALID_ARG;
+    if (bad_rows(f.grad, f.ld_grad, f.rows, f.cols, type_bytes(grad_dtype)) || bad_rows(f.momentum, f.ld_momentum, f.rows, f.cols, 4) ||
+        bad_rows(f.out, f.ld_out, f.rows, f.cols, 4) || (f.low != nullptr && bad_rows(f.low, f.ld_low, f.rows, f.cols, 2)))
+      return CWL_ERR_SHAPE;
+  }
+  if (n == 0) return CWL_OK;
+  FactorCommon c = {};
+  c.step = 1; c.nesterov = nesterov != 0; c.in_type = grad_dtype; c.out_type = CWL_F32;
+  c.beta = momentum; c.keep = (float)(1.0 - (double)lr * weight_decay); c.lr = lr;
+  c.steps = iteration->steps; c.a = iteration->a; c.b = iteration->b; c.c = iteration->c; c.eps = iteration->eps;
+  return run_factors(factors, n, c, [](const cwl_factor& i, Factor& f) {
+    f.u = i.grad; f.m = static_cast<float*>(i.momentum); f.out = i.out; f.low = static_cast<__nv_bfloat16*>(i.low);
+    f.ldu = row_step(i.ld_grad, i.rows, i.cols); f.ldm = row_step(i.ld_momentum, i.rows, i.cols);
+    f.ldo = row_step(i.ld_out, i.rows, i.cols); f.ldl = row_step(i.ld_low, i.rows, i.cols);
+    f.scale = i.scale;
+  }, workspace, workspace_bytes, stream);
+} catch (...) {
+  return CWL_ERR_CUDA;                                   // nothing may leave a C entry
+}
