@@ -135,63 +135,135 @@ __device__ __forceinline__ float4 load_u(const FactorCommon& a, const Factor& f,
   return make_float4(fmaf(a.beta, m.x, g.x), fmaf(a.beta, m.y, g.y), fmaf(a.beta, m.z, g.z), fmaf(a.beta, m.w, g.w));
 }
 
+// 16 bytes from global to shared memory, of which `bytes` are read and the rest filled with zeros
+__device__ __forceinline__ void copy16(void* to, const void* from, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kPending>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
+
+// Rows of this matrix can be copied 16 bytes at a time.
+__device__ __forceinline__ bool wide_rows(const void* p, int ld, int elem) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ((int64_t)ld * elem & 15) == 0;
+}
+// four elements as they lie in shared memory
+__device__ __forceinline__ float4 four_of(const void* at, int type) {
+  if (type == CWL_F32) return *static_cast<const float4*>(at);
+  const uint2 q = *static_cast<const uint2*>(at);
+  if (type == CWL_BF16)
+    return make_float4(__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xFFFF0000u), __uint_as_float(q.y << 16), __uint_as_float(q.y & 0xFFFF0000u));
+  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&q.x)), y = __half22float2(*reinterpret_cast<const __half2*>(&q.y));
+  return make_float4(x.x, x.y, y.x, y.y);
+}
+
 // D += A B, 8 x 8 x 4 in 64 bits.  Lane l holds A[l / 4][l % 4], B[l % 4][l / 4] and D[l / 4][2 (l % 4) + {0, 1}]: with B's
 // columns as rows of a symmetric product both operands are read the same way.
 __device__ __forceinline__ void mma_f64(double (&d)[2], double a, double b) {
   asm("mma.sync.aligned.m8n8k4.row.col.f64.f64.f64.f64 {%0, %1}, {%2}, {%3}, {%0, %1};" : "+d"(d[0]), "+d"(d[1]) : "d"(a), "d"(b));
 }
 
+__device__ __forceinline__ void lower_tile(int i, int& ti, int& tj) {
+  ti = 0;
+  while (i > ti) { i -= ti + 1; ++ti; }
+  tj = i;
+}
+
 // ------------------------------------------------------------------------------------------------------------- GRAM
 constexpr int kGramThreads = 128;
 constexpr int kGramK = 32;                         // long-side elements staged at a time
-constexpr int kGramLd = kGramK + 4;                // doubles a row: lanes of a fragment hit different banks
+constexpr int kGramLd = kGramK + 4;                // doubles a row
+// Place of element k of row r.  Lanes of a fragment (four rows by four k) and lanes that store one k of sixteen rows hit
+// sixteen different banks of 8 bytes.
+__device__ __forceinline__ int gram_at(int r, int k) { return r * kGramLd + (k ^ (r >> 2 & 3)); }
 
-// A 64-row block of U (rows first of the short side, elements k0... of the long side) on its way to shared memory.
-struct GramPiece { float4 v[4]; };
-template <bool kUpdate>
-__device__ __forceinline__ void gram_load(const FactorCommon& a, const Factor& f, bool tall, int first, int k0, int k_end, bool vec_u, bool vec_m, GramPiece& q) {
-  const int R = short_side(f), tid = threadIdx.x;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (tall) {                                    // U [long][short]: 16 threads a row of 64
-      const int k = k0 + i * 8 + (tid >> 4), s = first + (tid & 15) * 4;
-      q.v[i] = load_u<kUpdate>(a, f, k, s, k < k_end ? R - s : 0, vec_u, vec_m);
-    } else {                                       // U [short][long]: 8 threads a row of 32
-      const int s = first + i * 16 + (tid >> 3), k = k0 + (tid & 7) * 4;
-      q.v[i] = load_u<kUpdate>(a, f, s, k, s < R ? k_end - k : 0, vec_u, vec_m);
+// A block of 64 of the short side (from `first` on) by kGramK of the long side, on its way to shared memory in 64 bits.  Where rows
+// allow it the raw elements of the next chunks are already on their way to a ring in shared memory; else they are read
+// when they are wanted.
+constexpr int kGramRing = 3;
+constexpr int kGramRaw = 64 * kGramK * 4;          // bytes of a chunk, 4 an element at most
+struct GramSide {
+  const FactorCommon& a;
+  const Factor& f;
+  bool tall, wide, vec_u, vec_m, update;
+  int first, k_end;
+  uint8_t* raw;                                    // [kGramRing][gradient, momentum][kGramRaw]
+  __device__ __forceinline__ uint8_t* piece(int slot, int which) const { return raw + (slot * (a.step ? 2 : 1) + which) * kGramRaw; }
+  // rows of a chunk as they lie in memory: 64 of 32 elements, or (tall) 32 of 64
+  __device__ __forceinline__ void copy_rows(uint8_t* to, const void* from, int ld, int elem, int k0) const {
+    const int R = short_side(f), run = tall ? 64 : kGramK, per_row = run * elem / 16, per = 16 / elem;
+    for (int i = threadIdx.x; i < 64 * kGramK * elem / 16; i += kGramThreads) {
+      const int row = i / per_row, at = (i % per_row) * per;
+      const int r = tall ? k0 + row : first + row, c = tall ? first + at : k0 + at;
+      const int left = r < (tall ? k_end : R) ? (tall ? R : k_end) - c : 0;
+      const int bytes = min(max(left, 0) * elem, 16);
+      // (tall: lanes read one 16-byte piece of many rows, so its place depends on the row)
+      const int piece16 = i % per_row;
+      copy16(to + (i - piece16 + (tall ? piece16 ^ (row & 7) : piece16)) * 16, static_cast<const uint8_t*>(from) + (bytes > 0 ? ((int64_t)r * ld + c) * elem : 0), bytes);
     }
   }
-}
-__device__ __forceinline__ void gram_put(double* to, bool tall, const GramPiece& q) {
-  const int tid = threadIdx.x;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float v[4] = {q.v[i].x, q.v[i].y, q.v[i].z, q.v[i].w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (tall) to[((tid & 15) * 4 + j) * kGramLd + i * 8 + (tid >> 4)] = (double)v[j];
-      else to[(i * 16 + (tid >> 3)) * kGramLd + (tid & 7) * 4 + j] = (double)v[j];
+  __device__ __forceinline__ void start(int k0, int slot) const {
+    if (wide && k0 < k_end) {
+      copy_rows(piece(slot, 0), f.u, f.ldu, elem_size(a.in_type), k0);
+      if (a.step) copy_rows(piece(slot, 1), f.m, f.ldm, 4, k0);
     }
   }
-}
+  __device__ __forceinline__ void put(double* to, int k0, int slot) const {
+    const int R = short_side(f), tid = threadIdx.x, elem = elem_size(a.in_type);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      // four neighbours: lanes of a warp take the four-groups of neighbouring rows, so that their stores meet few banks
+      const int row = tall ? tid & 31 : i * 16 + (tid & 15), at = tall ? i * 16 + (tid >> 5) * 4 : (tid >> 4) * 4;
+      const int r = tall ? k0 + row : first + row, c = tall ? first + at : k0 + at;
+      const int left = r < (tall ? k_end : R) ? (tall ? R : k_end) - c : 0;
+      float4 u;
+      if (wide) {
+        const int run = tall ? 64 : kGramK, turn = tall ? (row & 7) << 4 : 0;
+        const float4 g = four_of(piece(slot, 0) + (((row * run + at) * elem) ^ turn), a.in_type);
+        u = g;
+        if (a.step) {
+          float4 m = four_of(piece(slot, 1) + (((row * run + at) * 4) ^ turn), CWL_F32);
+          if (update) {
+            m = make_float4(fmaf(a.beta, m.x, g.x), fmaf(a.beta, m.y, g.y), fmaf(a.beta, m.z, g.z), fmaf(a.beta, m.w, g.w));
+            store4_f32(f.m + (int64_t)r * f.ldm + c, m, vec_m, left);
+          }
+          u = a.nesterov ? make_float4(fmaf(a.beta, m.x, g.x), fmaf(a.beta, m.y, g.y), fmaf(a.beta, m.z, g.z), fmaf(a.beta, m.w, g.w)) : m;
+        }
+      } else {
+        u = update ? load_u<true>(a, f, r, c, left, vec_u, vec_m) : load_u<false>(a, f, r, c, left, vec_u, vec_m);
+      }
+      const float v[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        to[tall ? gram_at(at + j, row) : gram_at(row, at + j)] = (double)v[j];
+      }
+    }
+  }
+};
 
 template <int kMost>
 __global__ void __launch_bounds__(kGramThreads, 2) gram_kernel(const __grid_constant__ FactorArgs<kMost> args) {
   const FactorCommon& a = args.c;
-  __shared__ __align__(16) double rows_i[64 * kGramLd], rows_j[64 * kGramLd];
+  extern __shared__ __align__(16) uint8_t gram_raw[];
+  double* rows_i = reinterpret_cast<double*>(gram_raw);
+  double* rows_j = rows_i + 64 * kGramLd;
   double* sums = rows_j;                           // 36 tiles of 64, where one block of rows is all there is
   static_assert(64 * kGramLd >= 36 * 64, "room for the tiles");
+  uint8_t* ring = gram_raw + 2 * 64 * kGramLd * 8;
   pdl_launch_dependents();
   pdl_wait();
   const Factor& f = args.f[find_factor(args.f, a.n, blockIdx.x)];
   const int R = short_side(f), n = long_side(f), pairs = block_pairs(R);
-  const bool tall = f.rows > f.cols;
   int unit = blockIdx.x - f.first;
   const int slice = unit / pairs;
   int bi = 0, bj = unit % pairs;
   while (bj > bi) { bj -= bi + 1; ++bi; }          // bj <= bi
   const int k_begin = slice * a.slice, k_end = min(n, k_begin + a.slice);
-  const bool vec_u = vec_rows(f.u, f.ldu, elem_size(a.in_type)), vec_m = a.step && vec_rows(f.m, f.ldm, 4);
+  const int elem = elem_size(a.in_type);
+  const bool wide = wide_rows(f.u, f.ldu, elem) && (!a.step || wide_rows(f.m, f.ldm, 4));
+  const bool vec_u = vec_rows(f.u, f.ldu, elem), vec_m = a.step && vec_rows(f.m, f.ldm, 4);
+  // each element is read by one block only where R <= 64: the momentum is brought up to date there
+  const GramSide si{a, f, f.rows > f.cols, wide, vec_u, vec_m, a.step != 0 && R <= kShort, bi * 64, k_end, ring};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, fr = lane >> 2, fc = lane & 3;
   double* out = a.partial + (int64_t)blockIdx.x * 64 * 64;
 
@@ -201,23 +273,23 @@ __global__ void __launch_bounds__(kGramThreads, 2) gram_kernel(const __grid_cons
     double acc[36][2];
 #pragma unroll
     for (int i = 0; i < 36; ++i) acc[i][0] = acc[i][1] = 0.0;
-    GramPiece q;
-    const bool update = a.step != 0 && R <= kShort;  // each element is read by one block only
-    if (update) gram_load<true>(a, f, tall, bi * 64, k_begin, k_end, vec_u, vec_m, q);
-    else gram_load<false>(a, f, tall, bi * 64, k_begin, k_end, vec_u, vec_m, q);
+#pragma unroll
+    for (int i = 0; i < kGramRing - 1; ++i) { si.start(k_begin + i * kGramK, i); copies_commit(); }
+    int slot = 0;
     for (int k0 = k_begin; k0 < k_end; k0 += kGramK) {
+      copies_wait<kGramRing - 2>();
+      __syncthreads();                             // the chunk has arrived; the one before is done with
+      si.put(rows_i, k0, slot);
+      const int next = slot == 0 ? kGramRing - 1 : slot - 1;
+      si.start(k0 + (kGramRing - 1) * kGramK, next);
+      copies_commit();
+      if (++slot == kGramRing) slot = 0;
       __syncthreads();
-      gram_put(rows_i, tall, q);
-      __syncthreads();
-      if (k0 + kGramK < k_end) {
-        if (update) gram_load<true>(a, f, tall, bi * 64, k0 + kGramK, k_end, vec_u, vec_m, q);
-        else gram_load<false>(a, f, tall, bi * 64, k0 + kGramK, k_end, vec_u, vec_m, q);
-      }
 #pragma unroll 1
       for (int s = warp; s < kGramK / 4; s += 4) {
         double x[8];
 #pragma unroll
-        for (int t = 0; t < 8; ++t) x[t] = rows_i[(t * 8 + fr) * kGramLd + s * 4 + fc];
+        for (int t = 0; t < 8; ++t) x[t] = rows_i[gram_at(t * 8 + fr, s * 4 + fc)];
 #pragma unroll
         for (int ti = 0; ti < 8; ++ti) {
           if (ti < tiles) {
@@ -242,39 +314,42 @@ __global__ void __launch_bounds__(kGramThreads, 2) gram_kernel(const __grid_cons
       }
     }
     __syncthreads();
-    for (int at = threadIdx.x; at < 64 * 64; at += kGramThreads) {
-      const int r = at >> 6, c = at & 63;
-      const int hi = max(r, c), lo = min(r, c);    // of tiles on the diagonal both halves are there
-      const int ti = hi >> 3, tj = lo >> 3;
-      out[at] = sums[(ti * (ti + 1) / 2 + tj) * 64 + (hi & 7) * 8 + (lo & 7)];
-    }
+    // as tiles of the lower triangle
+    for (int at = threadIdx.x; at < 36 * 32; at += kGramThreads) reinterpret_cast<double2*>(out)[at] = reinterpret_cast<const double2*>(sums)[at];
   } else {
     // a warp a quadrant of 32 x 32
+    const GramSide sj{a, f, f.rows > f.cols, wide, vec_u, vec_m, false, bj * 64, k_end, ring + kGramRing * (a.step ? 2 : 1) * kGramRaw};
     const int qi = (warp >> 1) * 32, qj = (warp & 1) * 32;
     double acc[4][4][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[i][j][0] = acc[i][j][1] = 0.0;
-    GramPiece q, r;
-    gram_load<false>(a, f, tall, bi * 64, k_begin, k_end, vec_u, vec_m, q);
-    gram_load<false>(a, f, tall, bj * 64, k_begin, k_end, vec_u, vec_m, r);
+#pragma unroll
+    for (int i = 0; i < kGramRing - 1; ++i) {
+      si.start(k_begin + i * kGramK, i);
+      sj.start(k_begin + i * kGramK, i);
+      copies_commit();
+    }
+    int slot = 0;
     for (int k0 = k_begin; k0 < k_end; k0 += kGramK) {
+      copies_wait<kGramRing - 2>();
       __syncthreads();
-      gram_put(rows_i, tall, q);
-      gram_put(rows_j, tall, r);
+      si.put(rows_i, k0, slot);
+      sj.put(rows_j, k0, slot);
+      const int next = slot == 0 ? kGramRing - 1 : slot - 1;
+      si.start(k0 + (kGramRing - 1) * kGramK, next);
+      sj.start(k0 + (kGramRing - 1) * kGramK, next);
+      copies_commit();
+      if (++slot == kGramRing) slot = 0;
       __syncthreads();
-      if (k0 + kGramK < k_end) {
-        gram_load<false>(a, f, tall, bi * 64, k0 + kGramK, k_end, vec_u, vec_m, q);
-        gram_load<false>(a, f, tall, bj * 64, k0 + kGramK, k_end, vec_u, vec_m, r);
-      }
 #pragma unroll
       for (int s = 0; s < kGramK / 4; ++s) {
         double x[4], y[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          x[t] = rows_i[(qi + t * 8 + fr) * kGramLd + s * 4 + fc];
-          y[t] = rows_j[(qj + t * 8 + fr) * kGramLd + s * 4 + fc];
+          x[t] = rows_i[gram_at(qi + t * 8 + fr, s * 4 + fc)];
+          y[t] = rows_j[gram_at(qj + t * 8 + fr, s * 4 + fc)];
         }
 #pragma unroll
         for (int ti = 0; ti < 4; ++ti)
@@ -286,9 +361,16 @@ __global__ void __launch_bounds__(kGramThreads, 2) gram_kernel(const __grid_cons
     for (int ti = 0; ti < 4; ++ti)
 #pragma unroll
       for (int tj = 0; tj < 4; ++tj)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) out[(qi + ti * 8 + fr) * 64 + qj + tj * 8 + fc * 2 + j] = acc[ti][tj][j];
+        *reinterpret_cast<double2*>(out + (qi + ti * 8 + fr) * 64 + qj + tj * 8 + fc * 2) = make_double2(acc[ti][tj][0], acc[ti][tj][1]);
   }
+  copies_wait<0>();
+}
+// shared memory of GRAM: two blocks of rows in 64 bits, and the ring (twice, where a pair has two of them)
+size_t gram_smem(bool step, bool pairs) { return (size_t)2 * 64 * kGramLd * 8 + (size_t)kGramRing * (step ? 2 : 1) * (pairs ? 2 : 1) * kGramRaw; }
+// where entry (r, c), r >= c, of a 64 x 64 block on the diagonal lies among its tiles
+__device__ __forceinline__ int lower_at(int r, int c) {
+  const int ti = r >> 3, tj = c >> 3;
+  return (ti * (ti + 1) / 2 + tj) * 64 + (r & 7) * 8 + (c & 7);
 }
 
 // Momentum of the factors whose elements GRAM reads more than once (R > 64).
@@ -314,11 +396,6 @@ constexpr int kIterThreads = 256;
 constexpr int kIterLd = 68;                        // doubles a row
 constexpr size_t kIterSmem = ((size_t)4 * 64 * kIterLd + 1) * 8;
 
-__device__ __forceinline__ void lower_tile(int i, int& ti, int& tj) {
-  ti = 0;
-  while (i > ti) { i -= ti + 1; ++ti; }
-  tj = i;
-}
 
 // Tiles of this warp of the product of two symmetric, commuting matrices in shared memory.
 struct IterTiles { double d[5][2]; };
@@ -381,11 +458,28 @@ __global__ void __launch_bounds__(kIterThreads) iterate_kernel(const __grid_cons
   const int n = long_side(f), slices = (n + a.slice - 1) / a.slice;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, fr = lane >> 2, fc = lane & 3;
   const double* part = a.partial + (int64_t)f.first * 64 * 64;
-  for (int at = tid; at < 64 * 64; at += kIterThreads) {
-    double s = 0.0;
-#pragma unroll 4
-    for (int k = 0; k < slices; ++k) s += part[(int64_t)k * 64 * 64 + at];
-    G[(at >> 6) * kIterLd + (at & 63)] = s;
+  const int t8 = (R + 7) / 8, n_tiles = t8 * (t8 + 1) / 2, k_steps = (t8 * 2);
+  {
+    // tiles of the lower triangle, summed over the slices; all loads of two slices go out at once
+    constexpr int kEach = 36 * 64 / kIterThreads;
+    double s[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) s[e] = 0.0;
+#pragma unroll 2
+    for (int k = 0; k < slices; ++k) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (e * kIterThreads + tid < n_tiles * 64) s[e] += part[(int64_t)k * 64 * 64 + e * kIterThreads + tid];
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int at = e * kIterThreads + tid;
+      if (at >= n_tiles * 64) continue;
+      int ti, tj;
+      lower_tile(at >> 6, ti, tj);
+      const int r = ti * 8 + (at >> 3 & 7), c = tj * 8 + (at & 7);
+      if (r >= c) G[r * kIterLd + c] = G[c * kIterLd + r] = s[e];
+    }
   }
   __syncthreads();
   if (tid == 0) {
@@ -397,7 +491,6 @@ __global__ void __launch_bounds__(kIterThreads) iterate_kernel(const __grid_cons
   const double trace = size_slot, size = sqrt(trace) + a.eps;
   const double unit = trace == 0.0 ? 0.0 : 1.0 / size;        // a factor of zeros stays one
   for (int at = tid; at < 64 * 64; at += kIterThreads) G[(at >> 6) * kIterLd + (at & 63)] *= unit * unit;
-  const int t8 = (R + 7) / 8, n_tiles = t8 * (t8 + 1) / 2, k_steps = (t8 * 2);
   IterTiles t, u;
   for (int step = 0; step < a.steps; ++step) {
     const bool first = step == 0, last = step + 1 == a.steps;
@@ -456,7 +549,7 @@ __global__ void __launch_bounds__(kIterThreads) big_gram_kernel(const __grid_con
   for (int i = tid; i < R; i += kIterThreads) {
     const int b = i >> 6, pair = b * (b + 1) / 2 + b;
 #pragma unroll 4
-    for (int k = 0; k < slices; ++k) s += part[((int64_t)k * pairs + pair) * 64 * 64 + (i & 63) * 65];
+    for (int k = 0; k < slices; ++k) s += part[((int64_t)k * pairs + pair) * 64 * 64 + lower_at(i & 63, i & 63)];
   }
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((tid & 31) == 0) met[tid >> 5] = s;
@@ -465,15 +558,33 @@ __global__ void __launch_bounds__(kIterThreads) big_gram_kernel(const __grid_con
   for (int w = 0; w < kIterThreads / 32; ++w) trace += met[w];
   const double unit = trace == 0.0 ? 0.0 : 1.0 / (sqrt(trace) + a.eps);
   double* G = a.big + (int64_t)blockIdx.y * 5 * a.stride;
-  for (int at = tid; at < 64 * 64; at += kIterThreads) {
-    const int r = bi * 64 + (at >> 6), c = bj * 64 + (at & 63);
+  constexpr int kEach = 64 * 64 / kIterThreads;
+  double v[kEach];
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) v[e] = 0.0;
+  // of a block on the diagonal its tiles of the lower triangle are there, all of the others
+  const int entries = bi == bj ? 36 * 64 : 64 * 64;
+  for (int k = 0; k < slices; ++k) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e)
+      if (e * kIterThreads + tid < entries) v[e] += part[((int64_t)k * pairs + blockIdx.x) * 64 * 64 + e * kIterThreads + tid];
+  }
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int at = e * kIterThreads + tid;
+    if (at >= entries) continue;
+    int r = at >> 6, c = at & 63;
+    if (bi == bj) {
+      int ti, tj;
+      lower_tile(at >> 6, ti, tj);
+      r = ti * 8 + (at >> 3 & 7);
+      c = tj * 8 + (at & 7);
+      if (c > r) continue;
+    }
+    r += bi * 64;
+    c += bj * 64;
     if (r >= Rp || c >= Rp) continue;
-    double v = 0.0;
-#pragma unroll 4
-    for (int k = 0; k < slices; ++k) v += part[((int64_t)k * pairs + blockIdx.x) * 64 * 64 + at];
-    v *= unit * unit;
-    G[(int64_t)r * Rp + c] = v;
-    if (bi != bj) G[(int64_t)c * Rp + r] = v;
+    G[(int64_t)r * Rp + c] = G[(int64_t)c * Rp + r] = v[e] * unit * unit;
   }
   if (blockIdx.x == 0 && tid == 0) a.unit[blockIdx.y] = unit;
 }
@@ -507,12 +618,14 @@ __global__ void __launch_bounds__(kBigThreads) big_product_kernel(const __grid_c
   double* rows_x = big_raw;
   double* rows_y = big_raw + 32 * kBigLd;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, fr = lane >> 2, fc = lane & 3;
-#pragma unroll 8
-  for (int i = tid; i < 32 * (Rp / 2); i += kBigThreads) {
-    const int r = i / (Rp / 2), c = (i % (Rp / 2)) * 2;
-    *reinterpret_cast<double2*>(rows_x + r * kBigLd + c) = *reinterpret_cast<const double2*>(x + (int64_t)(ti * 32 + r) * Rp + c);
-    *reinterpret_cast<double2*>(rows_y + r * kBigLd + c) = *reinterpret_cast<const double2*>(y + (int64_t)(tj * 32 + r) * Rp + c);
+  for (int r = warp; r < 32; r += kBigThreads / 32) {
+    for (int c = lane * 2; c < Rp; c += 64) {
+      copy16(rows_x + r * kBigLd + c, x + (int64_t)(ti * 32 + r) * Rp + c, 16);
+      copy16(rows_y + r * kBigLd + c, y + (int64_t)(tj * 32 + r) * Rp + c, 16);
+    }
   }
+  copies_commit();
+  copies_wait<0>();
   __syncthreads();
   const int qi = (warp >> 1) * 16, qj = (warp & 1) * 16;
   double acc[2][2][2] = {};
@@ -575,16 +688,35 @@ __device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& 
 #pragma unroll
     for (int j = 0; j < kL; ++j) acc[i][j] = 0.f;
 
-  float4 x[4], y[2];
+  // What comes next is loaded raw, all loads together, and becomes U when it is put into shared memory.
+  float4 x[4], mom[4], y[2];
+  const bool inside = vec_u && (!a.step || vec_m) && (kTall ? (R & 3) == 0 : (n & 3) == 0);
+  auto place = [&](int k0, int i, int& r, int& c) {
+    if (kTall) { r = long0 + i * 32 + (tid >> 3); c = k0 + (tid & 7) * 4; }      // U [long][short]: eight threads 32 of a row
+    else { r = k0 + i * 8 + (tid >> 5); c = long0 + (tid & 31) * 4; }            // U [short][long]: a warp 128 of a row
+    return r < f.rows ? f.cols - c : 0;
+  };
   auto fetch = [&](int k0) {
+    int r, c;
+    if (inside) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (kTall) {                                 // U [long][short]: eight threads 32 of a row
-        const int l = long0 + i * 32 + (tid >> 3), k = k0 + (tid & 7) * 4;
-        x[i] = load_u<false>(a, f, l, k, l < n ? R - k : 0, vec_u, vec_m);
-      } else {                                     // U [short][long]: a warp 128 of a row
-        const int k = k0 + i * 8 + (tid >> 5), l = long0 + (tid & 31) * 4;
-        x[i] = load_u<false>(a, f, k, l, k < R ? n - l : 0, vec_u, vec_m);
+      for (int i = 0; i < 4; ++i) {
+        const bool there = place(k0, i, r, c) > 0;
+        const int64_t at = (int64_t)r * f.ldu + c;
+        if (a.in_type == CWL_F32) {
+          x[i] = there ? *reinterpret_cast<const float4*>(static_cast<const float*>(f.u) + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+        } else {
+          const float2 q = there ? *reinterpret_cast<const float2*>(static_cast<const uint16_t*>(f.u) + at) : make_float2(0.f, 0.f);
+          x[i].x = q.x;
+          x[i].y = q.y;
+        }
+        if (a.step) mom[i] = there ? *reinterpret_cast<const float4*>(f.m + (int64_t)r * f.ldm + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int left = place(k0, i, r, c);
+        x[i] = load_u<false>(a, f, r, c, left, vec_u, vec_m);
       }
     }
 #pragma unroll
@@ -593,17 +725,25 @@ __device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& 
       y[i] = load4(q, (int64_t)k * R + s, CWL_F32, vec_q, left);
     }
   };
+  auto made = [&](int i) {                         // U from what was loaded
+    if (!inside) return x[i];
+    const float4 g = four_of(&x[i], a.in_type);
+    if (!a.step) return g;
+    const float4 m = mom[i];
+    return a.nesterov ? make_float4(fmaf(a.beta, m.x, g.x), fmaf(a.beta, m.y, g.y), fmaf(a.beta, m.z, g.z), fmaf(a.beta, m.w, g.w)) : m;
+  };
   fetch(0);
   for (int k0 = 0; k0 < R; k0 += kApplyK) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      const float4 u = made(i);
       if (kTall) {
         const int l = i * 32 + (tid >> 3), k = (tid & 7) * 4;
-        xs[k * kApplyLdX + l] = x[i].x; xs[(k + 1) * kApplyLdX + l] = x[i].y;
-        xs[(k + 2) * kApplyLdX + l] = x[i].z; xs[(k + 3) * kApplyLdX + l] = x[i].w;
+        xs[k * kApplyLdX + l] = u.x; xs[(k + 1) * kApplyLdX + l] = u.y;
+        xs[(k + 2) * kApplyLdX + l] = u.z; xs[(k + 3) * kApplyLdX + l] = u.w;
       } else {
-        *reinterpret_cast<float4*>(xs + (i * 8 + (tid >> 5)) * kApplyLdX + (tid & 31) * 4) = x[i];
+        *reinterpret_cast<float4*>(xs + (i * 8 + (tid >> 5)) * kApplyLdX + (tid & 31) * 4) = u;
       }
     }
 #pragma unroll
@@ -627,19 +767,33 @@ __device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& 
   const int out_type = a.step ? CWL_F32 : a.out_type;
   const bool vec_o = vec_rows(f.out, f.ldo, elem_size(out_type)), vec_l = f.low != nullptr && vec_rows(f.low, f.ldl, 2);
   const float by = a.step ? -a.lr * f.scale : 1.f;
+  // four neighbours of a row of the factor at a time; a step's masters all come in before the first is written back
+  auto at_output = [&](int i, int& r, int& c) {
+    r = kTall ? long0 + l0 + i : short0 + s0 + i;
+    c = kTall ? short0 + s0 : long0 + l0;
+    return r < f.rows ? f.cols - c : 0;
+  };
+  int r, c;
+  float4 p[8];
+  if (a.step) {
+    const bool whole = vec_o && (f.cols & 3) == 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int left = at_output(i, r, c);
+      const float* at = static_cast<const float*>(f.out) + (int64_t)r * f.ldo + c;
+      if (whole) p[i] = left > 0 ? *reinterpret_cast<const float4*>(at) : make_float4(0.f, 0.f, 0.f, 0.f);
+      else p[i] = load4(at, 0, CWL_F32, vec_o, left);
+    }
+  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    // four neighbours of a row of the factor
-    const int r = kTall ? long0 + l0 + i : short0 + s0 + i, c = kTall ? short0 + s0 : long0 + l0;
-    const int left = r < f.rows ? f.cols - c : 0;
+    const int left = at_output(i, r, c);
     if (left <= 0) continue;
     float4 v = kTall ? make_float4(acc[0][i % kL], acc[1 % kS][i % kL], acc[2 % kS][i % kL], acc[3 % kS][i % kL])
                      : make_float4(acc[i % kS][0], acc[i % kS][1 % kL], acc[i % kS][2 % kL], acc[i % kS][3 % kL]);
     if (a.step) {
-      float* at = static_cast<float*>(f.out) + (int64_t)r * f.ldo + c;
-      const float4 p = load4(at, 0, CWL_F32, vec_o, left);
-      v = make_float4(fmaf(by, v.x, a.keep * p.x), fmaf(by, v.y, a.keep * p.y), fmaf(by, v.z, a.keep * p.z), fmaf(by, v.w, a.keep * p.w));
-      store4_f32(at, v, vec_o, left);
+      v = make_float4(fmaf(by, v.x, a.keep * p[i].x), fmaf(by, v.y, a.keep * p[i].y), fmaf(by, v.z, a.keep * p[i].z), fmaf(by, v.w, a.keep * p[i].w));
+      store4_f32(static_cast<float*>(f.out) + (int64_t)r * f.ldo + c, v, vec_o, left);
       if (f.low != nullptr) store4_bf16(f.low + (int64_t)r * f.ldl + c, v, vec_l, left);
     } else if (out_type == CWL_F32) {
       store4_f32(static_cast<float*>(f.out) + (int64_t)r * f.ldo + c, v, vec_o, left);
@@ -755,7 +909,9 @@ cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, v
     const int64_t x = (most_elements / 4 + kMomentumThreads * 4 - 1) / (kMomentumThreads * 4);
     CWL_CUDA_TRY(launch_chained(chained, momentum_kernel<kMost>, dim3((unsigned)(x < 592 ? x + 1 : 592), (unsigned)n), dim3(kMomentumThreads), 0, st, args));
   }
-  CWL_CUDA_TRY(launch_chained(chained, gram_kernel<kMost>, dim3((unsigned)gram_blocks), dim3(kGramThreads), 0, st, args));
+  static SharedMemoryGrant gram_grant;
+  CWL_CUDA_TRY(gram_grant(gram_kernel<kMost>));
+  CWL_CUDA_TRY(launch_chained(chained, gram_kernel<kMost>, dim3((unsigned)gram_blocks), dim3(kGramThreads), gram_smem(common.step != 0, big.n > 0), st, args));
   if (any_small) {
     static SharedMemoryGrant grant;
     CWL_CUDA_TRY(grant(iterate_kernel<kMost>));
