@@ -67,9 +67,9 @@ struct HeadRows {                                 // the packed rows, written by
   float* sum;                                     // ... their sum over the pieces so far
   float* alpha;                                   // ... what the sums of the pieces before this one are multiplied with
   float* scale;                                   // DX: up / sum (a backward call: up)
-  unsigned* above;                                // EXP: bit per 64 columns of the piece that took their own reference
+  unsigned* above;                                // EXP: bit per chunk of columns of the piece that took their own reference
   float* above_ref;                               // ... and that reference
-  int above_words, chunks;                        // words and 64-column chunks a row
+  int above_words, chunks;                        // words and chunks a row (64 columns; in head_few_kernel a block's)
 };
 
 struct HeadMaps { CUtensorMap a, a_packed, b; };  // a: of X itself (every row counts), a_packed: of the packed rows
@@ -607,6 +607,8 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
   }
 }
 
+#include "head_few.cuh"
+
 // ------------------------------------------------------------------------------------------------ rows that count
 struct RowsParams {
   const __nv_bfloat16* X; int64_t ldx;
@@ -759,6 +761,7 @@ head_finish_kernel(HeadRows rows, const float2* part, int n_part, int rows_alloc
   if ((int64_t)blockIdx.x * 32 >= n) return;
   float m = -INFINITY, s = 0.f;
   if (row < n) {
+#pragma unroll 8
     for (int c = slice; c < n_part; c += kFinishThreads / 32) {
       const float2 x = part[(int64_t)c * rows_alloc + row];
       const float top = fmaxf(m, x.x), ref = top == -INFINITY ? 0.f : top;
@@ -792,6 +795,7 @@ struct MergeParams {
   int n_part, rows_alloc, last;
   __nv_bfloat16* dz; int64_t dz_ld;
   int width, halves, half_at;
+  int chunk_cols;                                 // columns that share a reference
   const float* weight; float* loss; float* lse;
 };
 __global__ void __launch_bounds__(kFinishThreads) head_merge_kernel(const MergeParams p) {
@@ -806,6 +810,7 @@ __global__ void __launch_bounds__(kFinishThreads) head_merge_kernel(const MergeP
   const float ref = row < n ? rows.ref[row] : 0.f;
   float m = ref, s = 0.f;
   if (row < n) {
+#pragma unroll 8
     for (int c = slice; c < p.n_part; c += kFinishThreads / 32) {
       const float2 x = p.part[(int64_t)c * p.rows_alloc + row];
       if (x.x > m) { s *= exp2_fast((m - x.x) * kLog2e); m = x.x; }
@@ -842,7 +847,7 @@ __global__ void __launch_bounds__(kFinishThreads) head_merge_kernel(const MergeP
     if (!(new_ref[r] > old_ref[r])) continue;            // as good as always
     const int64_t at = row0 + r;
     for (int c = threadIdx.x; c < p.width; c += kFinishThreads) {
-      const int chunk = c >> 6;
+      const int chunk = c / p.chunk_cols;
       const bool above = rows.above[at * rows.above_words + (chunk >> 5)] >> (chunk & 31) & 1u;
       const float f = exp2_fast(((above ? rows.above_ref[at * rows.chunks + chunk] : old_ref[r]) - new_ref[r]) * kLog2e);
       __nv_bfloat16* e = p.dz + at * p.dz_ld + c;
@@ -1018,12 +1023,13 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 // workspace is that of the larger of both.
 struct HeadLayout {
   int rows_alloc, piece, pieces, halves;
+  int few;                                              // logits by head_few_kernel
   int stats_pass;                                       // a product for lse alone comes first
   int logit_chunk;                                      // K blocks of the logits' products that are summed in the tensor memory, 0 = all
   int from_e;                                           // dX comes from E and the gathered columns of W, without dZ
   HeadPlan stats, dz, dx, dw;
   int64_t packed_ld;
-  int dx_groups, dw_groups, above_words;
+  int dx_groups, dw_groups, above_words, chunks;
   size_t list, part, packed, above, above_ref, wy, dz_at, acc_x, acc_w, total;
 };
 constexpr int kLists = 9;
@@ -1038,6 +1044,7 @@ HeadLayout head_layout(int T, int d, int V, bool forward, bool want_dx, bool wan
   const int most_tn = l.logit_chunk > 0 ? 256 : kHMaxTile;
   const int k_d = ceil_div(d, kHK), k_t = ceil_div(T, kHK);
   l.packed_ld = (d + 7) / 8 * 8;
+  l.few = T <= kFewRows;
   l.piece = grads ? head_piece(l.rows_alloc, V, halves) : 0;
   l.pieces = grads ? ceil_div(V, l.piece) : 0;
   size_t at = 0;
@@ -1046,11 +1053,12 @@ HeadLayout head_layout(int T, int d, int V, bool forward, bool want_dx, bool wan
   take(256 + kLists * l.list);
   size_t parts = 0;
   if (l.stats_pass) {
-    l.stats = head_plan(T, V, k_d, false, most_tn, 32);
+    l.stats = l.few ? HeadPlan{few_columns(V), ceil_div(V, few_columns(V)), 1} : head_plan(T, V, k_d, false, most_tn, 32);
     parts = l.stats.n_cols;
   }
   if (grads) {
-    l.dz = head_plan(T, l.piece, k_d, false, most_tn, 64);
+    l.dz = l.few && l.from_e ? HeadPlan{few_columns(l.piece), ceil_div(l.piece, few_columns(l.piece)), 1}
+                             : head_plan(T, l.piece, k_d, false, most_tn, 64);
     if (l.from_e && forward) parts = l.dz.n_cols;
   }
   l.part = take(parts * 2 * l.rows_alloc * 8);
@@ -1070,9 +1078,10 @@ HeadLayout head_layout(int T, int d, int V, bool forward, bool want_dx, bool wan
     }
     if (l.from_e) {
       l.wy = take((size_t)l.rows_alloc * l.dx_groups * 8);
-      l.above_words = ceil_div(l.piece / 64, 32);
+      l.chunks = l.few ? l.dz.n_cols : l.piece / 64;
+      l.above_words = ceil_div(l.chunks, 32);
       l.above = take((size_t)l.rows_alloc * l.above_words * 4);
-      l.above_ref = take((size_t)l.rows_alloc * (l.piece / 64) * 4);
+      l.above_ref = take((size_t)l.rows_alloc * l.chunks * 4);
     }
   }
   l.total = at;
@@ -1167,7 +1176,7 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
   rows.above = reinterpret_cast<unsigned*>(ws + l.above);
   rows.above_ref = reinterpret_cast<float*>(ws + l.above_ref);
   rows.above_words = l.above_words;
-  rows.chunks = l.piece / 64;
+  rows.chunks = l.chunks;
   __nv_bfloat16* packed = reinterpret_cast<__nv_bfloat16*>(ws + l.packed);
   __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + l.dz_at);
   float2* part = reinterpret_cast<float2*>(ws + l.part);
@@ -1212,13 +1221,16 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
   if (!encode_map(&logits.a, X, d, T, ux, kHK, kHM) || !encode_map(&logits.a_packed, packed, d, l.rows_alloc, l.packed_ld, kHK, kHM) ||
       !encode_map(&logits.b, W, V, d, uw, 64, kHK))
     return CWL_ERR_CUDA;
+  HeadMaps few = logits;
+  if (l.few && (!encode_map(&few.a, X, d, T, ux, kHK, few_box(T)) || !encode_map(&few.a_packed, packed, d, l.rows_alloc, l.packed_ld, kHK, few_box(T))))
+    return CWL_ERR_CUDA;
 
   if (l.stats_pass) {
     HeadParams q = p;
     q.n_extent = V; q.k_extent = d; q.tn = l.stats.tn; q.n_cols = l.stats.n_cols; q.kb_per_split = ceil_div(d, kHK); q.chunk_kb = l.logit_chunk;
-    CWL_CUDA_TRY(launch_logits<HEAD_STATS>(logits, q, T, chained, st));
+    CWL_CUDA_TRY(l.few ? launch_few<HEAD_STATS>(few, q, T, chained, st) : launch_logits<HEAD_STATS>(logits, q, T, chained, st));
     CWL_CUDA_TRY(launch_chained(chained, head_finish_kernel, dim3((unsigned)ceil_div(T, 32)), dim3(kFinishThreads), 0, st, rows,
-                                static_cast<const float2*>(part), 2 * l.stats.n_cols, l.rows_alloc, weight, loss, lse));
+                                static_cast<const float2*>(part), (l.few ? 1 : 2) * l.stats.n_cols, l.rows_alloc, weight, loss, lse));
   }
   for (int piece = 0; piece < l.pieces; ++piece) {
     const int first = piece * l.piece, width = V - first < l.piece ? V - first : l.piece;
@@ -1228,10 +1240,10 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
     q.tn = l.dz.tn; q.n_cols = ceil_div(width, q.tn);
     q.dz = dz; q.dz_ld = dz_ld; q.halves = l.halves; q.half_at = l.piece; q.online = online;
     if (l.from_e) {
-      CWL_CUDA_TRY(launch_logits<HEAD_EXP>(logits, q, T, chained, st));
+      CWL_CUDA_TRY(l.few ? launch_few<HEAD_EXP>(few, q, T, chained, st) : launch_logits<HEAD_EXP>(logits, q, T, chained, st));
       if (online) {
         MergeParams m = {};
-        m.rows = rows; m.part = part; m.n_part = 2 * q.n_cols; m.rows_alloc = l.rows_alloc; m.last = last;
+        m.rows = rows; m.part = part; m.n_part = l.few ? q.n_cols : 2 * q.n_cols; m.chunk_cols = l.few ? q.tn : 64; m.rows_alloc = l.rows_alloc; m.last = last;
         m.dz = dz; m.dz_ld = dz_ld; m.width = width; m.halves = l.halves; m.half_at = l.piece;
         m.weight = weight; m.loss = loss; m.lse = lse;
         CWL_CUDA_TRY(launch_chained(chained, head_merge_kernel, dim3((unsigned)ceil_div(T, 32)), dim3(kFinishThreads), 0, st, m));

@@ -7,9 +7,10 @@ the factors are then trained under a chunk table that mixes the ladder's ranks.
 
     teacher   cwl_apply at full rank -> cwl_token_logprobs: top K of the tempered teacher
     step      cwl_apply under the table -> cwl_distill_topk: loss, and its gradient in the place of the logits
-              -> cwl_apply_grads: dA, dB -> Adam on fp32 copies of the factors (a few torch calls)
+              -> cwl_apply_grads: dA, dB -> Adam on fp32 copies of the factors (a few torch calls), or
+                 cwl_factor_step: orthogonalised momentum
 
-    python -m paper_2601_21109_b200.distill_ladder [--steps N] [--tokens T] [--width D] [--vocab V]
+    python -m paper_2601_21109_b200.distill_ladder [--steps N] [--tokens T] [--width D] [--vocab V] [--optimizer adam|muon]
 """
 from __future__ import annotations
 
@@ -27,7 +28,8 @@ class LadderDistiller:
 
     def __init__(self, X: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.Tensor, teacher_table: cwl.DeviceChunkTable,
                  table: cwl.DeviceChunkTable, window: int, top_k: int = 64, temperature: float = 1.0, lr: float = 1e-3,
-                 weight: Optional[torch.Tensor] = None):
+                 weight: Optional[torch.Tensor] = None, optimizer: str = "adam"):
+        assert optimizer in ("adam", "muon")
         T, d_in, d_out, R = X.shape[0], X.shape[1], W.shape[1], A.shape[1]
         self.X, self.W, self.table, self.window, self.temperature, self.lr = X, W, table, int(window), float(temperature), float(lr)
         self.status = torch.zeros(1, dtype=torch.int32, device=X.device)
@@ -43,6 +45,8 @@ class LadderDistiller:
         self.loss = torch.empty(T, dtype=torch.float32, device=X.device)
         self.dA, self.dB = torch.empty_like(self.master[0]), torch.empty_like(self.master[1])
         self.steps = 0
+        self.update = None if optimizer == "adam" else cwl.FactorStep(self.master, [self.A, self.B], [self.dA, self.dB],
+                                                                      [m for m, _ in self.moments])
 
     def forward(self) -> torch.Tensor:
         """The student's logits under the chunk table."""
@@ -62,6 +66,9 @@ class LadderDistiller:
         """One training step on the current stream; no host synchronisation."""
         self.gradients()
         self.steps += 1
+        if self.update is not None:
+            self.update(self.lr)
+            return
         b1, b2 = 0.9, 0.999
         scale = self.lr * (1 - b2 ** self.steps) ** 0.5 / (1 - b1 ** self.steps)
         for p, (m, v), g, low in zip(self.master, self.moments, (self.dA, self.dB), (self.A, self.B)):
@@ -100,8 +107,9 @@ def main() -> None:
     ap.add_argument("--tokens", type=int, default=2048)
     ap.add_argument("--width", type=int, default=4096)
     ap.add_argument("--vocab", type=int, default=32000)
+    ap.add_argument("--optimizer", choices=("adam", "muon"), default="adam")
     a = ap.parse_args()
-    d = synthetic(a.tokens, a.width, a.vocab)
+    d = synthetic(a.tokens, a.width, a.vocab, optimizer=a.optimizer)
     d.gradients()
     print(f"before: loss {float(d.loss.sum()):.4f}, top-1 agreement {d.agreement():.3f}")
     start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
