@@ -177,52 +177,65 @@ constexpr int kGramLd = kGramK + 4;                // doubles a row
 // sixteen different banks of 8 bytes.
 __device__ __forceinline__ int gram_at(int r, int k) { return r * kGramLd + (k ^ (r >> 2 & 3)); }
 
+// Raw rows in shared memory, kRun elements each, in pieces of 16 bytes.  The place of a piece depends on its row, so that lanes
+// that read the same piece of neighbouring rows hit different banks.
+template <int kRun>
+__device__ __forceinline__ int raw_turn(int row, int elem) {
+  const int pitch = kRun * elem;                   // bytes: 64 or more
+  return (pitch < 128 ? row >> 1 : row) & 7 & (pitch / 16 - 1);
+}
+// byte offset of element `at` (a multiple of 4) of a row
+template <int kRun>
+__device__ __forceinline__ int raw_at(int row, int at, int elem) {
+  return row * kRun * elem + ((at * elem) ^ (raw_turn<kRun>(row, elem) << 4));
+}
+// Starts copies of rows [r0, r0 + kRows) x columns [c0, c0 + kRun) of a matrix, zeros outside [.., r_end) x [.., c_end).
+template <int kRows, int kRun, int kThreads>
+__device__ __forceinline__ void raw_copy(uint8_t* to, const void* from, int ld, int elem, int r0, int r_end, int c0, int c_end) {
+  const int shift = (elem == 4 ? 2 : 1) + (kRun == 128 ? 7 : kRun == 64 ? 6 : 5) - 4;      // pieces a row
+  const int piece = threadIdx.x & ((1 << shift) - 1), c = c0 + (piece << (elem == 4 ? 2 : 3));
+  const int bytes = min(max(c_end - c, 0) * elem, 16);
+  const uint8_t* src = static_cast<const uint8_t*>(from) + (int64_t)c * elem;
+  for (int row = threadIdx.x >> shift; row < kRows; row += kThreads >> shift) {
+    const bool there = r0 + row < r_end && bytes > 0;
+    copy16(to + row * kRun * elem + ((piece ^ raw_turn<kRun>(row, elem)) << 4), there ? src + (int64_t)(r0 + row) * ld * elem : from, there ? bytes : 0);
+  }
+}
+
 // A block of 64 of the short side (from `first` on) by kGramK of the long side, on its way to shared memory in 64 bits.  Where rows
 // allow it the raw elements of the next chunks are already on their way to a ring in shared memory; else they are read
 // when they are wanted.
 constexpr int kGramRing = 3;
 constexpr int kGramRaw = 64 * kGramK * 4;          // bytes of a chunk, 4 an element at most
+template <bool kTall>
 struct GramSide {
   const FactorCommon& a;
   const Factor& f;
-  bool tall, wide, vec_u, vec_m, update;
+  bool wide, vec_u, vec_m, update;
   int first, k_end;
   uint8_t* raw;                                    // [kGramRing][gradient, momentum][kGramRaw]
+  static constexpr int kRows = kTall ? kGramK : 64, kRun = kTall ? 64 : kGramK;   // of a chunk as it lies in memory
   __device__ __forceinline__ uint8_t* piece(int slot, int which) const { return raw + (slot * (a.step ? 2 : 1) + which) * kGramRaw; }
-  // rows of a chunk as they lie in memory: 64 of 32 elements, or (tall) 32 of 64
-  __device__ __forceinline__ void copy_rows(uint8_t* to, const void* from, int ld, int elem, int k0) const {
-    const int R = short_side(f), run = tall ? 64 : kGramK, per_row = run * elem / 16, per = 16 / elem;
-    for (int i = threadIdx.x; i < 64 * kGramK * elem / 16; i += kGramThreads) {
-      const int row = i / per_row, at = (i % per_row) * per;
-      const int r = tall ? k0 + row : first + row, c = tall ? first + at : k0 + at;
-      const int left = r < (tall ? k_end : R) ? (tall ? R : k_end) - c : 0;
-      const int bytes = min(max(left, 0) * elem, 16);
-      // (tall: lanes read one 16-byte piece of many rows, so its place depends on the row)
-      const int piece16 = i % per_row;
-      copy16(to + (i - piece16 + (tall ? piece16 ^ (row & 7) : piece16)) * 16, static_cast<const uint8_t*>(from) + (bytes > 0 ? ((int64_t)r * ld + c) * elem : 0), bytes);
-    }
-  }
   __device__ __forceinline__ void start(int k0, int slot) const {
-    if (wide && k0 < k_end) {
-      copy_rows(piece(slot, 0), f.u, f.ldu, elem_size(a.in_type), k0);
-      if (a.step) copy_rows(piece(slot, 1), f.m, f.ldm, 4, k0);
-    }
+    if (!wide || k0 >= k_end) return;
+    const int R = short_side(f), r0 = kTall ? k0 : first, r_end = kTall ? k_end : R, c0 = kTall ? first : k0, c_end = kTall ? R : k_end;
+    raw_copy<kRows, kRun, kGramThreads>(piece(slot, 0), f.u, f.ldu, elem_size(a.in_type), r0, r_end, c0, c_end);
+    if (a.step) raw_copy<kRows, kRun, kGramThreads>(piece(slot, 1), f.m, f.ldm, 4, r0, r_end, c0, c_end);
   }
   __device__ __forceinline__ void put(double* to, int k0, int slot) const {
     const int R = short_side(f), tid = threadIdx.x, elem = elem_size(a.in_type);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      // four neighbours: lanes of a warp take the four-groups of neighbouring rows, so that their stores meet few banks
-      const int row = tall ? tid & 31 : i * 16 + (tid & 15), at = tall ? i * 16 + (tid >> 5) * 4 : (tid >> 4) * 4;
-      const int r = tall ? k0 + row : first + row, c = tall ? first + at : k0 + at;
-      const int left = r < (tall ? k_end : R) ? (tall ? R : k_end) - c : 0;
+      // four neighbours of a row; lanes take neighbouring rows
+      const int row = kTall ? tid & 31 : i * 16 + (tid & 15), at = kTall ? i * 16 + (tid >> 5) * 4 : (tid >> 4) * 4;
+      const int r = kTall ? k0 + row : first + row, c = kTall ? first + at : k0 + at;
+      const int left = r < (kTall ? k_end : R) ? (kTall ? R : k_end) - c : 0;
       float4 u;
       if (wide) {
-        const int run = tall ? 64 : kGramK, turn = tall ? (row & 7) << 4 : 0;
-        const float4 g = four_of(piece(slot, 0) + (((row * run + at) * elem) ^ turn), a.in_type);
+        const float4 g = four_of(piece(slot, 0) + raw_at<kRun>(row, at, elem), a.in_type);
         u = g;
         if (a.step) {
-          float4 m = four_of(piece(slot, 1) + (((row * run + at) * 4) ^ turn), CWL_F32);
+          float4 m = four_of(piece(slot, 1) + raw_at<kRun>(row, at, 4), CWL_F32);
           if (update) {
             m = make_float4(fmaf(a.beta, m.x, g.x), fmaf(a.beta, m.y, g.y), fmaf(a.beta, m.z, g.z), fmaf(a.beta, m.w, g.w));
             store4_f32(f.m + (int64_t)r * f.ldm + c, m, vec_m, left);
@@ -234,27 +247,20 @@ struct GramSide {
       }
       const float v[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        to[tall ? gram_at(at + j, row) : gram_at(row, at + j)] = (double)v[j];
-      }
+      for (int j = 0; j < 4; ++j) to[kTall ? gram_at(at + j, row) : gram_at(row, at + j)] = (double)v[j];
     }
   }
 };
 
-template <int kMost>
-__global__ void __launch_bounds__(kGramThreads, 2) gram_kernel(const __grid_constant__ FactorArgs<kMost> args) {
-  const FactorCommon& a = args.c;
-  extern __shared__ __align__(16) uint8_t gram_raw[];
+template <bool kTall>
+__device__ __forceinline__ void gram_block(const FactorCommon& a, const Factor& f, uint8_t* gram_raw, double* out) {
   double* rows_i = reinterpret_cast<double*>(gram_raw);
   double* rows_j = rows_i + 64 * kGramLd;
   double* sums = rows_j;                           // 36 tiles of 64, where one block of rows is all there is
   static_assert(64 * kGramLd >= 36 * 64, "room for the tiles");
   uint8_t* ring = gram_raw + 2 * 64 * kGramLd * 8;
-  pdl_launch_dependents();
-  pdl_wait();
-  const Factor& f = args.f[find_factor(args.f, a.n, blockIdx.x)];
   const int R = short_side(f), n = long_side(f), pairs = block_pairs(R);
-  int unit = blockIdx.x - f.first;
+  const int unit = blockIdx.x - f.first;
   const int slice = unit / pairs;
   int bi = 0, bj = unit % pairs;
   while (bj > bi) { bj -= bi + 1; ++bi; }          // bj <= bi
@@ -263,9 +269,8 @@ __global__ void __launch_bounds__(kGramThreads, 2) gram_kernel(const __grid_cons
   const bool wide = wide_rows(f.u, f.ldu, elem) && (!a.step || wide_rows(f.m, f.ldm, 4));
   const bool vec_u = vec_rows(f.u, f.ldu, elem), vec_m = a.step && vec_rows(f.m, f.ldm, 4);
   // each element is read by one block only where R <= 64: the momentum is brought up to date there
-  const GramSide si{a, f, f.rows > f.cols, wide, vec_u, vec_m, a.step != 0 && R <= kShort, bi * 64, k_end, ring};
+  const GramSide<kTall> si{a, f, wide, vec_u, vec_m, a.step != 0 && R <= kShort, bi * 64, k_end, ring};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, fr = lane >> 2, fc = lane & 3;
-  double* out = a.partial + (int64_t)blockIdx.x * 64 * 64;
 
   if (bi == bj) {
     // 36 tiles of the lower triangle in every warp, which takes a quarter of the K steps: eight fragments serve 36 products
@@ -318,7 +323,7 @@ __global__ void __launch_bounds__(kGramThreads, 2) gram_kernel(const __grid_cons
     for (int at = threadIdx.x; at < 36 * 32; at += kGramThreads) reinterpret_cast<double2*>(out)[at] = reinterpret_cast<const double2*>(sums)[at];
   } else {
     // a warp a quadrant of 32 x 32
-    const GramSide sj{a, f, f.rows > f.cols, wide, vec_u, vec_m, false, bj * 64, k_end, ring + kGramRing * (a.step ? 2 : 1) * kGramRaw};
+    const GramSide<kTall> sj{a, f, wide, vec_u, vec_m, false, bj * 64, k_end, ring + kGramRing * (a.step ? 2 : 1) * kGramRaw};
     const int qi = (warp >> 1) * 32, qj = (warp & 1) * 32;
     double acc[4][4][2];
 #pragma unroll
@@ -365,6 +370,16 @@ __global__ void __launch_bounds__(kGramThreads, 2) gram_kernel(const __grid_cons
   }
   copies_wait<0>();
 }
+template <int kMost>
+__global__ void __launch_bounds__(kGramThreads, 2) gram_kernel(const __grid_constant__ FactorArgs<kMost> args) {
+  extern __shared__ __align__(16) uint8_t gram_raw[];
+  pdl_launch_dependents();
+  pdl_wait();
+  const Factor& f = args.f[find_factor(args.f, args.c.n, blockIdx.x)];
+  double* out = args.c.partial + (int64_t)blockIdx.x * 64 * 64;
+  if (f.rows > f.cols) gram_block<true>(args.c, f, gram_raw, out);
+  else gram_block<false>(args.c, f, gram_raw, out);
+}
 // shared memory of GRAM: two blocks of rows in 64 bits, and the ring (twice, where a pair has two of them)
 size_t gram_smem(bool step, bool pairs) { return (size_t)2 * 64 * kGramLd * 8 + (size_t)kGramRing * (step ? 2 : 1) * (pairs ? 2 : 1) * kGramRaw; }
 // where entry (r, c), r >= c, of a 64 x 64 block on the diagonal lies among its tiles
@@ -391,51 +406,78 @@ __global__ void __launch_bounds__(kMomentumThreads) momentum_kernel(const __grid
   }
 }
 
+// Sums of the slices' partial products of factors of R <= 64, into the first slice's place: 64 entries a block, four groups of
+// slices, so that one block does not read them all in a row.
+constexpr int kSlicesThreads = 256;
+template <int kMost>
+__global__ void __launch_bounds__(kSlicesThreads) slices_kernel(const __grid_constant__ FactorArgs<kMost> args) {
+  __shared__ double met[kSlicesThreads];
+  pdl_launch_dependents();
+  pdl_wait();
+  const Factor& f = args.f[blockIdx.y];
+  const int R = short_side(f), t8 = (R + 7) / 8, slices = (long_side(f) + args.c.slice - 1) / args.c.slice;
+  if (R > kShort || (int)blockIdx.x >= t8 * (t8 + 1) / 2) return;
+  double* part = args.c.partial + (int64_t)f.first * 64 * 64 + blockIdx.x * 64 + (threadIdx.x & 63);
+  double s = 0.0;
+#pragma unroll 8
+  for (int k = threadIdx.x >> 6; k < slices; k += kSlicesThreads / 64) s += part[(int64_t)k * 64 * 64];
+  met[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x < 64) part[0] = met[threadIdx.x] + met[threadIdx.x + 64] + met[threadIdx.x + 128] + met[threadIdx.x + 192];
+}
+
 // ---------------------------------------------------------------------------------------------------- ITERATE, R <= 64
-constexpr int kIterThreads = 256;
+constexpr int kIterThreads = 384;                  // 12 warps of three tiles: 36, the lower triangle of 8 x 8
+constexpr int kIterTiles = 3;
 constexpr int kIterLd = 68;                        // doubles a row
 constexpr size_t kIterSmem = ((size_t)4 * 64 * kIterLd + 1) * 8;
 
-
-// Tiles of this warp of the product of two symmetric, commuting matrices in shared memory.
-struct IterTiles { double d[5][2]; };
-__device__ __forceinline__ void iter_product(const double* x, const double* y, int n_tiles, int k_steps, int warp, int fr, int fc, IterTiles& t) {
+// This warp's tiles of the lower triangle, neighbours in the order of rows.  Where the triangle is smaller, the last ones stand
+// for the missing; they are not stored.
+struct IterMine {
+  int count, left[kIterTiles], right[kIterTiles], row[kIterTiles], col[kIterTiles];
+  __device__ __forceinline__ IterMine(int n_tiles, int warp, int fr, int fc) {
+    const int first = warp * kIterTiles;
+    count = min(max(n_tiles - first, 0), kIterTiles);
 #pragma unroll
-  for (int i = 0; i < 5; ++i) {
-    t.d[i][0] = t.d[i][1] = 0.0;
-    const int tile = warp + 8 * i;
-    if (tile < n_tiles) {
+    for (int i = 0; i < kIterTiles; ++i) {
       int ti, tj;
-      lower_tile(tile, ti, tj);
-      const double* p = x + (ti * 8 + fr) * kIterLd + fc;
-      const double* q = y + (tj * 8 + fr) * kIterLd + fc;
-      double odd[2] = {0.0, 0.0};
-#pragma unroll 4
-      for (int k = 0; k < k_steps; k += 2) {
-        mma_f64(t.d[i], p[k * 4], q[k * 4]);
-        mma_f64(odd, p[k * 4 + 4], q[k * 4 + 4]);
-      }
-      t.d[i][0] += odd[0];
-      t.d[i][1] += odd[1];
+      lower_tile(min(first + i, n_tiles - 1), ti, tj);
+      left[i] = (ti * 8 + fr) * kIterLd + fc;
+      right[i] = (tj * 8 + fr) * kIterLd + fc;
+      row[i] = ti * 8 + fr;
+      col[i] = tj * 8 + fc * 2;
     }
+  }
+};
+struct IterSums { double d[kIterTiles][2]; };
+// Product of two symmetric, commuting matrices in shared memory.  The tiles advance together and the fragments of several K steps
+// are on their way at once, without a branch in between.
+__device__ __forceinline__ void iter_product(const double* x, const double* y, const IterMine& w, int k_steps, IterSums& t) {
+#pragma unroll
+  for (int i = 0; i < kIterTiles; ++i) t.d[i][0] = t.d[i][1] = 0.0;
+  if (w.count == 0) return;
+#pragma unroll 4
+  for (int k = 0; k < k_steps; ++k) {
+    double l[kIterTiles], r[kIterTiles];
+#pragma unroll
+    for (int i = 0; i < kIterTiles; ++i) { l[i] = x[w.left[i] + k * 4]; r[i] = y[w.right[i] + k * 4]; }
+#pragma unroll
+    for (int i = 0; i < kIterTiles; ++i) mma_f64(t.d[i], l[i], r[i]);
   }
 }
 template <typename F>
-__device__ __forceinline__ void iter_store(double* to, int n_tiles, int warp, int fr, int fc, const IterTiles& t, F value) {
+__device__ __forceinline__ void iter_store(double* to, const IterMine& w, const IterSums& t, F value) {
 #pragma unroll
-  for (int i = 0; i < 5; ++i) {
-    const int tile = warp + 8 * i;
-    if (tile < n_tiles) {
-      int ti, tj;
-      lower_tile(tile, ti, tj);
+  for (int i = 0; i < kIterTiles; ++i) {
+    if (i >= w.count) break;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int r = ti * 8 + fr, c = tj * 8 + fc * 2 + j;
-        const double v = value(r, c, t.d[i][j]);
-        if (ti != tj || c <= r) {                  // one value for both halves
-          to[r * kIterLd + c] = v;
-          to[c * kIterLd + r] = v;
-        }
+    for (int j = 0; j < 2; ++j) {
+      const int r = w.row[i], c = w.col[i] + j;
+      const double v = value(r, c, t.d[i][j]);
+      if (c <= r) {                                // one value for both halves
+        to[r * kIterLd + c] = v;
+        to[c * kIterLd + r] = v;
       }
     }
   }
@@ -455,62 +497,51 @@ __global__ void __launch_bounds__(kIterThreads) iterate_kernel(const __grid_cons
   const Factor& f = args.f[blockIdx.x];
   const int R = short_side(f);
   if (R > kShort) return;
-  const int n = long_side(f), slices = (n + a.slice - 1) / a.slice;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, fr = lane >> 2, fc = lane & 3;
   const double* part = a.partial + (int64_t)f.first * 64 * 64;
-  const int t8 = (R + 7) / 8, n_tiles = t8 * (t8 + 1) / 2, k_steps = (t8 * 2);
-  {
-    // tiles of the lower triangle, summed over the slices; all loads of two slices go out at once
-    constexpr int kEach = 36 * 64 / kIterThreads;
-    double s[kEach];
+  const int t8 = (R + 7) / 8, n_tiles = t8 * (t8 + 1) / 2, k_steps = t8 * 2, used = t8 * 8;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) s[e] = 0.0;
-#pragma unroll 2
-    for (int k = 0; k < slices; ++k) {
-#pragma unroll
-      for (int e = 0; e < kEach; ++e)
-        if (e * kIterThreads + tid < n_tiles * 64) s[e] += part[(int64_t)k * 64 * 64 + e * kIterThreads + tid];
-    }
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int at = e * kIterThreads + tid;
-      if (at >= n_tiles * 64) continue;
-      int ti, tj;
-      lower_tile(at >> 6, ti, tj);
-      const int r = ti * 8 + (at >> 3 & 7), c = tj * 8 + (at & 7);
-      if (r >= c) G[r * kIterLd + c] = G[c * kIterLd + r] = s[e];
-    }
+  for (int e = 0; e < 36 * 64 / kIterThreads; ++e) {
+    const int at = e * kIterThreads + tid;
+    if (at >= n_tiles * 64) continue;
+    const double v = part[at];
+    int ti, tj;
+    lower_tile(at >> 6, ti, tj);
+    const int r = ti * 8 + (at >> 3 & 7), c = tj * 8 + (at & 7);
+    if (r >= c) G[r * kIterLd + c] = G[c * kIterLd + r] = v;
   }
   __syncthreads();
-  if (tid == 0) {
-    double s = 0.0;
-    for (int i = 0; i < R; ++i) s += G[i * kIterLd + i];
-    size_slot = s;
+  if (tid < 32) {
+    double s = tid < R ? G[tid * kIterLd + tid] : 0.0;
+    if (tid + 32 < R) s += G[(tid + 32) * kIterLd + tid + 32];
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if (tid == 0) size_slot = s;
   }
   __syncthreads();
   const double trace = size_slot, size = sqrt(trace) + a.eps;
   const double unit = trace == 0.0 ? 0.0 : 1.0 / size;        // a factor of zeros stays one
-  for (int at = tid; at < 64 * 64; at += kIterThreads) G[(at >> 6) * kIterLd + (at & 63)] *= unit * unit;
-  IterTiles t, u;
+  for (int at = tid; at < used * 64; at += kIterThreads) G[(at >> 6) * kIterLd + (at & 63)] *= unit * unit;
+  const IterMine mine(n_tiles, warp, fr, fc);
+  IterSums t, u;
   for (int step = 0; step < a.steps; ++step) {
     const bool first = step == 0, last = step + 1 == a.steps;
     __syncthreads();
-    iter_product(G, G, n_tiles, k_steps, warp, fr, fc, t);
-    iter_store(P, n_tiles, warp, fr, fc, t, [&](int r, int c, double v) { return (r == c ? a.a : 0.0) + a.b * G[r * kIterLd + c] + a.c * v; });
+    iter_product(G, G, mine, k_steps, t);
+    iter_store(P, mine, t, [&](int r, int c, double v) { return (r == c ? a.a : 0.0) + a.b * G[r * kIterLd + c] + a.c * v; });
     __syncthreads();
-    if (!first) iter_product(P, Q, n_tiles, k_steps, warp, fr, fc, u);
-    if (!last) iter_product(P, G, n_tiles, k_steps, warp, fr, fc, t);
+    if (!first) iter_product(P, Q, mine, k_steps, u);
+    if (!last) iter_product(P, G, mine, k_steps, t);
     __syncthreads();
     if (first) {
-      for (int at = tid; at < 64 * 64; at += kIterThreads) Q[(at >> 6) * kIterLd + (at & 63)] = P[(at >> 6) * kIterLd + (at & 63)];
+      for (int at = tid; at < used * 64; at += kIterThreads) Q[(at >> 6) * kIterLd + (at & 63)] = P[(at >> 6) * kIterLd + (at & 63)];
     } else {
-      iter_store(Q, n_tiles, warp, fr, fc, u, [](int, int, double v) { return v; });
+      iter_store(Q, mine, u, [](int, int, double v) { return v; });
     }
     if (last) break;
-    iter_store(S, n_tiles, warp, fr, fc, t, [](int, int, double v) { return v; });
+    iter_store(S, mine, t, [](int, int, double v) { return v; });
     __syncthreads();
-    iter_product(P, S, n_tiles, k_steps, warp, fr, fc, t);
-    iter_store(G, n_tiles, warp, fr, fc, t, [](int, int, double v) { return v; });
+    iter_product(P, S, mine, k_steps, t);
+    iter_store(G, mine, t, [](int, int, double v) { return v; });
   }
   __syncthreads();
   float* q = a.q + blockIdx.x * a.q_stride;
@@ -534,8 +565,9 @@ static_assert(sizeof(BigArgs) <= 8 * 1024, "kernel parameters");
 __host__ __device__ __forceinline__ int padded(int R) { return (R + 31) / 32 * 32; }
 
 // Sums of GRAM's partial products, scaled: G_0.  A block a 64 x 64 pair.
-__global__ void __launch_bounds__(kIterThreads) big_gram_kernel(const __grid_constant__ BigArgs a) {
-  __shared__ double met[kIterThreads / 32];
+constexpr int kBigGramThreads = 256;
+__global__ void __launch_bounds__(kBigGramThreads) big_gram_kernel(const __grid_constant__ BigArgs a) {
+  __shared__ double met[kBigGramThreads / 32];
   pdl_launch_dependents();
   pdl_wait();
   const int R = a.R[blockIdx.y], pairs = block_pairs(R), slices = a.slices[blockIdx.y];
@@ -546,7 +578,7 @@ __global__ void __launch_bounds__(kIterThreads) big_gram_kernel(const __grid_con
   const double* part = a.partial + (int64_t)a.first[blockIdx.y] * 64 * 64;
   // the trace: every block adds it up in the same order
   double s = 0.0;
-  for (int i = tid; i < R; i += kIterThreads) {
+  for (int i = tid; i < R; i += kBigGramThreads) {
     const int b = i >> 6, pair = b * (b + 1) / 2 + b;
 #pragma unroll 4
     for (int k = 0; k < slices; ++k) s += part[((int64_t)k * pairs + pair) * 64 * 64 + lower_at(i & 63, i & 63)];
@@ -555,10 +587,10 @@ __global__ void __launch_bounds__(kIterThreads) big_gram_kernel(const __grid_con
   if ((tid & 31) == 0) met[tid >> 5] = s;
   __syncthreads();
   double trace = 0.0;
-  for (int w = 0; w < kIterThreads / 32; ++w) trace += met[w];
+  for (int w = 0; w < kBigGramThreads / 32; ++w) trace += met[w];
   const double unit = trace == 0.0 ? 0.0 : 1.0 / (sqrt(trace) + a.eps);
   double* G = a.big + (int64_t)blockIdx.y * 5 * a.stride;
-  constexpr int kEach = 64 * 64 / kIterThreads;
+  constexpr int kEach = 64 * 64 / kBigGramThreads;
   double v[kEach];
 #pragma unroll
   for (int e = 0; e < kEach; ++e) v[e] = 0.0;
@@ -567,11 +599,11 @@ __global__ void __launch_bounds__(kIterThreads) big_gram_kernel(const __grid_con
   for (int k = 0; k < slices; ++k) {
 #pragma unroll
     for (int e = 0; e < kEach; ++e)
-      if (e * kIterThreads + tid < entries) v[e] += part[((int64_t)k * pairs + blockIdx.x) * 64 * 64 + e * kIterThreads + tid];
+      if (e * kBigGramThreads + tid < entries) v[e] += part[((int64_t)k * pairs + blockIdx.x) * 64 * 64 + e * kBigGramThreads + tid];
   }
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
-    const int at = e * kIterThreads + tid;
+    const int at = e * kBigGramThreads + tid;
     if (at >= entries) continue;
     int r = at >> 6, c = at & 63;
     if (bi == bj) {
@@ -823,7 +855,7 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 // Long-side elements a block of GRAM: short enough that the blocks fill the GPU evenly, long enough that their sums
 // (32 KB a block) stay a small part of what is read.
 constexpr int64_t kGramBlocks = 2400;
-constexpr int kGramLeast = 256;
+constexpr int kGramLeast = 128;
 struct FactorPlan { int slice, n_big, most_R; int64_t blocks; size_t partial, q, big, unit, total; int64_t q_stride, stride; };
 template <typename Item>
 FactorPlan factor_plan(const Item* items, int n) {
@@ -885,7 +917,7 @@ cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, v
   big.q = args.c.q; big.q_stride = plan.q_stride;
   int64_t gram_blocks = 0, blocks = 0;
   bool any_small = false;
-  int most_R = 0;
+  int most_R = 0, most_slices = 0;
   int64_t most_elements = 0;
   for (int i = 0; i < n; ++i) {
     Factor& f = args.f[i];
@@ -902,6 +934,7 @@ cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, v
       if (e > most_elements) most_elements = e;
     } else {
       any_small = true;
+      if (slices > most_slices) most_slices = slices;
     }
     gram_blocks += (int64_t)block_pairs(R) * slices;
   }
@@ -913,6 +946,8 @@ cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, v
   CWL_CUDA_TRY(gram_grant(gram_kernel<kMost>));
   CWL_CUDA_TRY(launch_chained(chained, gram_kernel<kMost>, dim3((unsigned)gram_blocks), dim3(kGramThreads), gram_smem(common.step != 0, big.n > 0), st, args));
   if (any_small) {
+    if (most_slices > 1)
+      CWL_CUDA_TRY(launch_chained(chained, slices_kernel<kMost>, dim3(36, (unsigned)n), dim3(kSlicesThreads), 0, st, args));
     static SharedMemoryGrant grant;
     CWL_CUDA_TRY(grant(iterate_kernel<kMost>));
     CWL_CUDA_TRY(launch_chained(chained, iterate_kernel<kMost>, dim3((unsigned)n), dim3(kIterThreads), kIterSmem, st, args));
@@ -920,7 +955,7 @@ cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, v
   if (big.n > 0) {
     static SharedMemoryGrant grant;
     CWL_CUDA_TRY(grant(big_product_kernel));
-    CWL_CUDA_TRY(launch_chained(chained, big_gram_kernel, dim3((unsigned)block_pairs(most_R), (unsigned)big.n), dim3(kIterThreads), 0, st, big));
+    CWL_CUDA_TRY(launch_chained(chained, big_gram_kernel, dim3((unsigned)block_pairs(most_R), (unsigned)big.n), dim3(kBigGramThreads), 0, st, big));
     const int t = padded(most_R) / 32, tiles = t * (t + 1) / 2;
     for (int step = 0; step < common.steps; ++step) {
       const bool last = step + 1 == common.steps;

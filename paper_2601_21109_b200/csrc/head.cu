@@ -749,36 +749,51 @@ __global__ void __launch_bounds__(kRowsThreads) head_rows_kernel(const RowsParam
   }
 }
 
-// Log-sum-exp and loss of every row that counts, from the tiles' maxima and sums.  32 rows a block, eight threads a row.
+// (max, sum) of a row over the tiles, relative to a reference that is at least `m`: kRowsEach rows a block (32, or one where
+// there are few), 256 / kRowsEach threads a row, met in a fixed order.  The first thread of a row gets the result.
 constexpr int kFinishThreads = 256;
+__device__ __forceinline__ float2 join_sums(const float2& a, const float2& b) {
+  const float top = fmaxf(a.x, b.x), ref = top == -INFINITY ? 0.f : top;
+  // a NaN in a sum stays one; a maximum is NaN only where all logits were
+  return make_float2(top, a.y * exp2_fast((a.x - ref) * kLog2e) + b.y * exp2_fast((b.x - ref) * kLog2e));
+}
+template <int kRowsEach>
+__device__ __forceinline__ float2 row_sums(const float2* part, int n_part, int rows_alloc, int64_t row, bool there, float m, float2* met) {
+  constexpr int kSlices = kFinishThreads / kRowsEach;
+  const int slice = threadIdx.x / kRowsEach;
+  float2 all = make_float2(m, 0.f);
+  if (there) {
+    // eight loads at a time
+    for (int c0 = slice; c0 < n_part; c0 += kSlices * 8) {
+      float2 x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = c0 + k * kSlices < n_part ? part[(int64_t)(c0 + k * kSlices) * rows_alloc + row] : make_float2(m, 0.f);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) all = join_sums(all, x[k]);
+    }
+  }
+  met[threadIdx.x] = all;
+#pragma unroll
+  for (int k = kSlices / 2; k >= 1; k /= 2) {
+    __syncthreads();
+    if (slice < k) met[threadIdx.x] = all = join_sums(all, met[threadIdx.x + k * kRowsEach]);
+  }
+  return all;
+}
+
+// Log-sum-exp and loss of every row that counts, from the tiles' maxima and sums.
+template <int kRowsEach>
 __global__ void __launch_bounds__(kFinishThreads)
 head_finish_kernel(HeadRows rows, const float2* part, int n_part, int rows_alloc, const float* weight, float* loss, float* lse) {
   __shared__ float2 met[kFinishThreads];
   pdl_launch_dependents();
   pdl_wait();
-  const int n = *rows.n, lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
-  const int64_t row = (int64_t)blockIdx.x * 32 + lane;
-  if ((int64_t)blockIdx.x * 32 >= n) return;
-  float m = -INFINITY, s = 0.f;
-  if (row < n) {
-#pragma unroll 8
-    for (int c = slice; c < n_part; c += kFinishThreads / 32) {
-      const float2 x = part[(int64_t)c * rows_alloc + row];
-      const float top = fmaxf(m, x.x), ref = top == -INFINITY ? 0.f : top;
-      s = s * exp2_fast((m - ref) * kLog2e) + x.y * exp2_fast((x.x - ref) * kLog2e);
-      m = top;
-    }
-  }
-  met[threadIdx.x] = make_float2(m, s);
-  __syncthreads();
-  if (slice == 0 && row < n) {
-    for (int k = 1; k < kFinishThreads / 32; ++k) {
-      const float2 x = met[k * 32 + lane];
-      const float top = fmaxf(m, x.x), ref = top == -INFINITY ? 0.f : top;
-      s = s * exp2_fast((m - ref) * kLog2e) + x.y * exp2_fast((x.x - ref) * kLog2e);
-      m = top;
-    }
-    const float l = m + logf(s);
+  const int n = *rows.n;
+  if ((int64_t)blockIdx.x * kRowsEach >= n) return;
+  const int64_t row = (int64_t)blockIdx.x * kRowsEach + threadIdx.x % kRowsEach;
+  const float2 all = row_sums<kRowsEach>(part, n_part, rows_alloc, row, row < n, -INFINITY, met);
+  if (threadIdx.x < kRowsEach && row < n) {
+    const float l = all.x + logf(all.y);
     const int t = rows.row[row];
     rows.lse[row] = l;
     if (lse != nullptr) lse[t] = l;
@@ -798,38 +813,25 @@ struct MergeParams {
   int chunk_cols;                                 // columns that share a reference
   const float* weight; float* loss; float* lse;
 };
+template <int kRowsEach>
 __global__ void __launch_bounds__(kFinishThreads) head_merge_kernel(const MergeParams p) {
   __shared__ float2 met[kFinishThreads];
-  __shared__ float old_ref[32], new_ref[32];
+  __shared__ float old_ref[kRowsEach], new_ref[kRowsEach];
   pdl_launch_dependents();
   pdl_wait();
   const HeadRows& rows = p.rows;
-  const int n = *rows.n, lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
-  const int row0 = blockIdx.x * 32, row = row0 + lane;
+  const int n = *rows.n, r = threadIdx.x % kRowsEach;
+  const int row0 = blockIdx.x * kRowsEach, row = row0 + r;
   if (row0 >= n) return;
   const float ref = row < n ? rows.ref[row] : 0.f;
-  float m = ref, s = 0.f;
-  if (row < n) {
-#pragma unroll 8
-    for (int c = slice; c < p.n_part; c += kFinishThreads / 32) {
-      const float2 x = p.part[(int64_t)c * p.rows_alloc + row];
-      if (x.x > m) { s *= exp2_fast((m - x.x) * kLog2e); m = x.x; }
-      s += m > x.x ? x.y * exp2_fast((x.x - m) * kLog2e) : x.y;
-    }
-  }
-  met[threadIdx.x] = make_float2(m, s);
-  __syncthreads();
-  if (slice == 0) {
-    for (int k = 1; k < kFinishThreads / 32; ++k) {
-      const float2 x = met[k * 32 + lane];
-      if (x.x > m) { s *= exp2_fast((m - x.x) * kLog2e); m = x.x; }
-      s += m > x.x ? x.y * exp2_fast((x.x - m) * kLog2e) : x.y;
-    }
-    old_ref[lane] = ref;
-    new_ref[lane] = m;
+  const float2 all = row_sums<kRowsEach>(p.part, p.n_part, p.rows_alloc, row, row < n, ref, met);
+  if (threadIdx.x < kRowsEach) {
+    const float m = all.x;
+    old_ref[r] = ref;
+    new_ref[r] = m;
     if (row < n) {
       const float alpha = m > ref ? exp2_fast((ref - m) * kLog2e) : 1.f;
-      const float sum = rows.sum[row] * alpha + s;
+      const float sum = rows.sum[row] * alpha + all.y;
       rows.alpha[row] = alpha;
       rows.ref[row] = m;
       rows.sum[row] = sum;
@@ -843,7 +845,7 @@ __global__ void __launch_bounds__(kFinishThreads) head_merge_kernel(const MergeP
     }
   }
   __syncthreads();
-  for (int r = 0; r < 32 && row0 + r < n; ++r) {
+  for (int r = 0; r < kRowsEach && row0 + r < n; ++r) {
     if (!(new_ref[r] > old_ref[r])) continue;            // as good as always
     const int64_t at = row0 + r;
     for (int c = threadIdx.x; c < p.width; c += kFinishThreads) {
@@ -950,14 +952,26 @@ head_sum_kernel(HeadRows rows, int T, int m_extent, int cols, const float* acc, 
   if ((int64_t)m_tile * kHM >= m_rows) return;
   const int64_t tiles = (int64_t)((m_rows + 2 * kHM - 1) / (2 * kHM)) * 2;
   const float unit = wy == nullptr && n > 0 ? dz_unit(rows) : 1.f;
-  for (int i = threadIdx.x; i < 8 * kHM; i += kSumThreads) {
-    const int g = i / kHM, r = i % kHM, row = m_tile * kHM + r;
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (col0 + g * 4 < cols && row < m_rows) {
-      for (int k = 0; k < split; ++k) {
+  constexpr int kEach = 8 * kHM / kSumThreads;
+  float4 sums[kEach];
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) sums[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+  for (int k = 0; k < split; ++k) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const int i = e * kSumThreads + threadIdx.x, g = i / kHM, r = i % kHM;
+      if (col0 + g * 4 < cols && m_tile * kHM + r < m_rows) {
         const float4 x = *reinterpret_cast<const float4*>(acc + (((k * tiles + m_tile) * groups + col0 / 4 + g) * kHM + r) * 4);
-        s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+        sums[e].x += x.x; sums[e].y += x.y; sums[e].z += x.z; sums[e].w += x.w;
       }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const int i = e * kSumThreads + threadIdx.x, g = i / kHM, r = i % kHM, row = m_tile * kHM + r;
+    float4 s = sums[e];
+    if (col0 + g * 4 < cols && row < m_rows) {
       if (wy != nullptr) {
         const float f = rows.scale[row], up = rows.up[row];
         const uint32_t* w = wy + ((int64_t)m_tile * groups * 2 + col0 / 2 + g * 2) * kHM + r;
@@ -1008,6 +1022,7 @@ HeadPlan head_plan(int m_rows, int cols, int n_kb, bool may_split, int most_tn, 
   return best;
 }
 
+constexpr int kOneRowEach = 592;                        // rows up to which finishing takes a block a row: four blocks an SM
 constexpr size_t kPieceBytes = (size_t)256 << 20;       // E or dZ of a piece of the vocabulary
 constexpr int kPieceMin = 2048;
 int head_piece(int rows_alloc, int V, int halves) {
@@ -1229,8 +1244,12 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
     HeadParams q = p;
     q.n_extent = V; q.k_extent = d; q.tn = l.stats.tn; q.n_cols = l.stats.n_cols; q.kb_per_split = ceil_div(d, kHK); q.chunk_kb = l.logit_chunk;
     CWL_CUDA_TRY(l.few ? launch_few<HEAD_STATS>(few, q, T, chained, st) : launch_logits<HEAD_STATS>(logits, q, T, chained, st));
-    CWL_CUDA_TRY(launch_chained(chained, head_finish_kernel, dim3((unsigned)ceil_div(T, 32)), dim3(kFinishThreads), 0, st, rows,
-                                static_cast<const float2*>(part), (l.few ? 1 : 2) * l.stats.n_cols, l.rows_alloc, weight, loss, lse));
+    const float2* parts = part;
+    const int n_part = (l.few ? 1 : 2) * l.stats.n_cols;
+    CWL_CUDA_TRY(T <= kOneRowEach ? launch_chained(chained, head_finish_kernel<1>, dim3((unsigned)T), dim3(kFinishThreads), 0, st, rows, parts, n_part,
+                                                   l.rows_alloc, weight, loss, lse)
+                                  : launch_chained(chained, head_finish_kernel<32>, dim3((unsigned)ceil_div(T, 32)), dim3(kFinishThreads), 0, st, rows,
+                                                   parts, n_part, l.rows_alloc, weight, loss, lse));
   }
   for (int piece = 0; piece < l.pieces; ++piece) {
     const int first = piece * l.piece, width = V - first < l.piece ? V - first : l.piece;
@@ -1246,7 +1265,8 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
         m.rows = rows; m.part = part; m.n_part = l.few ? q.n_cols : 2 * q.n_cols; m.chunk_cols = l.few ? q.tn : 64; m.rows_alloc = l.rows_alloc; m.last = last;
         m.dz = dz; m.dz_ld = dz_ld; m.width = width; m.halves = l.halves; m.half_at = l.piece;
         m.weight = weight; m.loss = loss; m.lse = lse;
-        CWL_CUDA_TRY(launch_chained(chained, head_merge_kernel, dim3((unsigned)ceil_div(T, 32)), dim3(kFinishThreads), 0, st, m));
+        CWL_CUDA_TRY(T <= kOneRowEach ? launch_chained(chained, head_merge_kernel<1>, dim3((unsigned)T), dim3(kFinishThreads), 0, st, m)
+                                      : launch_chained(chained, head_merge_kernel<32>, dim3((unsigned)ceil_div(T, 32)), dim3(kFinishThreads), 0, st, m));
       }
     } else {
       CWL_CUDA_TRY(launch_logits<HEAD_DZ>(logits, q, T, chained, st));

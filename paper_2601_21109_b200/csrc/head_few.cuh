@@ -41,8 +41,8 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
       : "r"(taddr) : "memory");
 }
 
-// kN numbers a lane, reduced over the lanes: lane l ends with number(s) l mod 32 (kN = 64: l and l + 32; kN = 16: lanes l and
-// l + 16 have the same).  Each step halves what a lane still has to pass on.
+// kN (16 or 32) numbers a lane, reduced over the lanes: lane l ends with number l mod kN in its first place.  Each step halves
+// what a lane still has to pass on.
 template <int kN, typename Op>
 __device__ __forceinline__ void reduce_lanes(float (&v)[kN], int lane, Op op) {
   constexpr unsigned all = 0xffffffffu;
@@ -51,15 +51,12 @@ __device__ __forceinline__ void reduce_lanes(float (&v)[kN], int lane, Op op) {
     for (int j = 0; j < kN; ++j) v[j] = op(v[j], __shfl_xor_sync(all, v[j], 16));
   }
 #pragma unroll
-  for (int w = (kN < 32 ? kN : 32) / 2; w >= 1; w /= 2) {
+  for (int w = kN / 2; w >= 1; w /= 2) {
     const bool upper = (lane & w) != 0;
 #pragma unroll
-    for (int b = 0; b < (kN + 31) / 32; ++b) {           // groups of 32 numbers
-#pragma unroll
-      for (int j = 0; j < w; ++j) {
-        const float give = upper ? v[b * 32 + j] : v[b * 32 + j + w], keep = upper ? v[b * 32 + j + w] : v[b * 32 + j];
-        v[b * 32 + j] = op(keep, __shfl_xor_sync(all, give, w));
-      }
+    for (int j = 0; j < w; ++j) {
+      const float give = upper ? v[j] : v[j + w], keep = upper ? v[j + w] : v[j];
+      v[j] = op(keep, __shfl_xor_sync(all, give, w));
     }
   }
 }
@@ -181,6 +178,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
     if (epi < kRows) targets[epi] = epi < n ? p.rows.target[epi] - p.n_first : -1;
     asm volatile("bar.sync 1, 256;" ::: "memory");
     const bool mine = m < m_tiles;
+    constexpr int kPart = kRows < 32 ? kRows : 32;
     uint32_t local = 0;
     bool ok = true;
     for (int tile = blockIdx.x; ok && tile < n_tiles; tile += gridDim.x) {
@@ -194,7 +192,6 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
         tc_fence_after();
         if (mine) {
           const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + (slot * 2 + m) * kRows;
-          constexpr int kPart = kRows < 32 ? kRows : 32;
 #pragma unroll
           for (int j0 = 0; j0 < kRows; j0 += kPart) {
             uint32_t r[kPart];
@@ -220,15 +217,14 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
         for (int j = 0; j < kRows; ++j)
           if (targets[j] == col) p.rows.z_target[j] = z[j];
       }
-      // the rows' maxima over the block's columns
-      float v[kRows];
+      // the rows' maxima over the block's columns, 32 rows at a time
 #pragma unroll
-      for (int j = 0; j < kRows; ++j) v[j] = there ? z[j] : -INFINITY;
-      reduce_lanes<kRows>(v, lane, [](float x, float y) { return fmaxf(x, y); });
-      constexpr int kEach = kRows < 32 ? kRows : 32;
-      if (lane < kEach) {
+      for (int b = 0; b < kRows; b += kPart) {
+        float v[kPart];
 #pragma unroll
-        for (int b = 0; b < (kRows + 31) / 32; ++b) meet[w8 * kRows + b * 32 + lane] = v[b * 32];
+        for (int j = 0; j < kPart; ++j) v[j] = there ? z[b + j] : -INFINITY;
+        reduce_lanes<kPart>(v, lane, [](float x, float y) { return fmaxf(x, y); });
+        if (lane < kPart) meet[w8 * kRows + b + lane] = v[0];
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");
       float* common = meet + 8 * kRows;                          // [kRows]: the rows' references
@@ -248,16 +244,16 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll
-      for (int j = 0; j < kRows; ++j) v[j] = there && j < n ? exp2_fast(fmaf(z[j], kLog2e, -common[j] * kLog2e)) : 0.f;
+      for (int j = 0; j < kRows; ++j) z[j] = there && j < n ? exp2_fast(fmaf(z[j], kLog2e, -common[j] * kLog2e)) : 0.f;
       if (kMode == HEAD_EXP) {
         if (there) {
           __nv_bfloat16* e = p.dz + col;
 #pragma unroll
           for (int j = 0; j < kRows; ++j) {
             if (j < n) {
-              const __nv_bfloat16 hi = __float2bfloat16_rn(v[j]);
+              const __nv_bfloat16 hi = __float2bfloat16_rn(z[j]);
               *e = hi;
-              if (p.halves == 2) e[p.half_at] = __float2bfloat16_rn(v[j] - __bfloat162float(hi));
+              if (p.halves == 2) e[p.half_at] = __float2bfloat16_rn(z[j] - __bfloat162float(hi));
               e += p.dz_ld;
             }
           }
@@ -272,10 +268,13 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
           continue;
         }
       }
-      reduce_lanes<kRows>(v, lane, [](float x, float y) { return x + y; });
-      if (lane < kEach) {
 #pragma unroll
-        for (int b = 0; b < (kRows + 31) / 32; ++b) meet[w8 * kRows + b * 32 + lane] = v[b * 32];
+      for (int b = 0; b < kRows; b += kPart) {
+        float v[kPart];
+#pragma unroll
+        for (int j = 0; j < kPart; ++j) v[j] = z[b + j];
+        reduce_lanes<kPart>(v, lane, [](float x, float y) { return x + y; });
+        if (lane < kPart) meet[w8 * kRows + b + lane] = v[0];
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");
       if (epi < n) {
