@@ -147,16 +147,6 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 __device__ __forceinline__ bool wide_rows(const void* p, int ld, int elem) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ((int64_t)ld * elem & 15) == 0;
 }
-// four elements as they lie in shared memory
-__device__ __forceinline__ float4 four_of(const void* at, int type) {
-  if (type == CWL_F32) return *static_cast<const float4*>(at);
-  const uint2 q = *static_cast<const uint2*>(at);
-  if (type == CWL_BF16)
-    return make_float4(__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xFFFF0000u), __uint_as_float(q.y << 16), __uint_as_float(q.y & 0xFFFF0000u));
-  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&q.x)), y = __half22float2(*reinterpret_cast<const __half2*>(&q.y));
-  return make_float4(x.x, x.y, y.x, y.y);
-}
-
 // D += A B, 8 x 8 x 4 in 64 bits.  Lane l holds A[l / 4][l % 4], B[l % 4][l / 4] and D[l / 4][2 (l % 4) + {0, 1}]: with B's
 // columns as rows of a symmetric product both operands are read the same way.
 __device__ __forceinline__ void mma_f64(double (&d)[2], double a, double b) {
@@ -170,7 +160,7 @@ __device__ __forceinline__ void lower_tile(int i, int& ti, int& tj) {
 }
 
 // ------------------------------------------------------------------------------------------------------------- GRAM
-constexpr int kGramThreads = 128;
+constexpr int kGramThreads = 256;
 constexpr int kGramK = 32;                         // long-side elements staged at a time
 constexpr int kGramLd = kGramK + 4;                // doubles a row
 // Place of element k of row r.  Lanes of a fragment (four rows by four k) and lanes that store one k of sixteen rows hit
@@ -179,27 +169,57 @@ __device__ __forceinline__ int gram_at(int r, int k) { return r * kGramLd + (k ^
 
 // Raw rows in shared memory, kRun elements each, in pieces of 16 bytes.  The place of a piece depends on its row, so that lanes
 // that read the same piece of neighbouring rows hit different banks.
-template <int kRun>
-__device__ __forceinline__ int raw_turn(int row, int elem) {
-  const int pitch = kRun * elem;                   // bytes: 64 or more
-  return (pitch < 128 ? row >> 1 : row) & 7 & (pitch / 16 - 1);
+template <int kRun, int kElem>
+__device__ __forceinline__ int raw_turn(int row) {
+  constexpr int kPitch = kRun * kElem;             // bytes: 64 or more
+  return (kPitch < 128 ? row >> 1 : row) & 7 & (kPitch / 16 - 1);
 }
 // byte offset of element `at` (a multiple of 4) of a row
-template <int kRun>
-__device__ __forceinline__ int raw_at(int row, int at, int elem) {
-  return row * kRun * elem + ((at * elem) ^ (raw_turn<kRun>(row, elem) << 4));
+template <int kRun, int kElem>
+__device__ __forceinline__ int raw_at(int row, int at) {
+  return row * kRun * kElem + ((at * kElem) ^ (raw_turn<kRun, kElem>(row) << 4));
 }
-// Starts copies of rows [r0, r0 + kRows) x columns [c0, c0 + kRun) of a matrix, zeros outside [.., r_end) x [.., c_end).
-template <int kRows, int kRun, int kThreads>
-__device__ __forceinline__ void raw_copy(uint8_t* to, const void* from, int ld, int elem, int r0, int r_end, int c0, int c_end) {
-  const int shift = (elem == 4 ? 2 : 1) + (kRun == 128 ? 7 : kRun == 64 ? 6 : 5) - 4;      // pieces a row
-  const int piece = threadIdx.x & ((1 << shift) - 1), c = c0 + (piece << (elem == 4 ? 2 : 3));
-  const int bytes = min(max(c_end - c, 0) * elem, 16);
-  const uint8_t* src = static_cast<const uint8_t*>(from) + (int64_t)c * elem;
-  for (int row = threadIdx.x >> shift; row < kRows; row += kThreads >> shift) {
-    const bool there = r0 + row < r_end && bytes > 0;
-    copy16(to + row * kRun * elem + ((piece ^ raw_turn<kRun>(row, elem)) << 4), there ? src + (int64_t)(r0 + row) * ld * elem : from, there ? bytes : 0);
+// What one thread copies of every chunk of kRows x kRun elements of a matrix: the same piece of rows some way apart.  Chunks follow
+// one another along the rows or along the columns; places outside [.., r_end) x [.., c_end) read as zeros.
+template <int kRows, int kRun, int kElem, int kThreads>
+struct RawCopy {
+  static constexpr int kPieces = kRun * kElem / 16, kStep = kThreads / kPieces, kEach = kRows / kStep;
+  static_assert(kThreads % kPieces == 0 && kRows % kStep == 0 && kStep % 8 == 0, "every thread the same piece, at the same turn");
+  const uint8_t* src;
+  int64_t pitch;
+  int to, row, col;
+  __device__ __forceinline__ RawCopy(const void* from, int ld, int r0, int c0) {
+    const int piece = threadIdx.x & (kPieces - 1);
+    row = threadIdx.x / kPieces;
+    col = c0 + piece * (16 / kElem);
+    pitch = (int64_t)ld * kElem;
+    src = static_cast<const uint8_t*>(from) + (r0 + row) * pitch + (int64_t)col * kElem;
+    to = row * kRun * kElem + ((piece ^ raw_turn<kRun, kElem>(row)) << 4);
+    row += r0;
   }
+  // the chunk at (rows, columns) further on from the first one
+  __device__ __forceinline__ void start(uint8_t* at, int rows, int cols, int r_end, int c_end) const {
+    const int bytes = min(max(c_end - col - cols, 0) * kElem, 16);
+    const uint8_t* p = src + rows * pitch + (int64_t)cols * kElem;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const bool there = row + rows + i * kStep < r_end && bytes > 0;
+      copy16(at + to + i * kStep * kRun * kElem, there ? p + i * kStep * pitch : src, there ? bytes : 0);
+    }
+  }
+};
+template <int kElem>
+__device__ __forceinline__ float4 raw_four(const uint8_t* at, bool bf16) {
+  if (kElem == 4) return *reinterpret_cast<const float4*>(at);
+  const uint2 q = *reinterpret_cast<const uint2*>(at);
+  if (bf16)
+    return make_float4(__uint_as_float(q.x << 16), __uint_as_float(q.x & 0xFFFF0000u), __uint_as_float(q.y << 16), __uint_as_float(q.y & 0xFFFF0000u));
+  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&q.x)), y = __half22float2(*reinterpret_cast<const __half2*>(&q.y));
+  return make_float4(x.x, x.y, y.x, y.y);
+}
+// U of a step from gradient and momentum, both as they are now
+__device__ __forceinline__ float4 step_u(const FactorCommon& a, const float4& g, const float4& m) {
+  return a.nesterov ? make_float4(fmaf(a.beta, m.x, g.x), fmaf(a.beta, m.y, g.y), fmaf(a.beta, m.z, g.z), fmaf(a.beta, m.w, g.w)) : m;
 }
 
 // A block of 64 of the short side (from `first` on) by kGramK of the long side, on its way to shared memory in 64 bits.  Where rows
@@ -207,42 +227,49 @@ __device__ __forceinline__ void raw_copy(uint8_t* to, const void* from, int ld, 
 // when they are wanted.
 constexpr int kGramRing = 3;
 constexpr int kGramRaw = 64 * kGramK * 4;          // bytes of a chunk, 4 an element at most
-template <bool kTall>
+template <bool kTall, bool kStep, int kElem>
 struct GramSide {
+  static constexpr int kRows = kTall ? kGramK : 64, kRun = kTall ? 64 : kGramK;   // of a chunk as it lies in memory
   const FactorCommon& a;
   const Factor& f;
   bool wide, vec_u, vec_m, update;
-  int first, k_end;
+  int first, k_begin, k_end;
   uint8_t* raw;                                    // [kGramRing][gradient, momentum][kGramRaw]
-  static constexpr int kRows = kTall ? kGramK : 64, kRun = kTall ? 64 : kGramK;   // of a chunk as it lies in memory
-  __device__ __forceinline__ uint8_t* piece(int slot, int which) const { return raw + (slot * (a.step ? 2 : 1) + which) * kGramRaw; }
+  RawCopy<kRows, kRun, kElem, kGramThreads> copy_u;
+  RawCopy<kRows, kRun, 4, kGramThreads> copy_m;
+  __device__ __forceinline__ GramSide(const FactorCommon& a_, const Factor& f_, bool wide_, bool vec_u_, bool vec_m_, bool update_, int first_, int k_begin_, int k_end_, uint8_t* raw_)
+      : a(a_), f(f_), wide(wide_), vec_u(vec_u_), vec_m(vec_m_), update(update_), first(first_), k_begin(k_begin_), k_end(k_end_), raw(raw_),
+        copy_u(f_.u, f_.ldu, kTall ? k_begin_ : first_, kTall ? first_ : k_begin_), copy_m(f_.m, f_.ldm, kTall ? k_begin_ : first_, kTall ? first_ : k_begin_) {}
+  __device__ __forceinline__ uint8_t* piece(int slot, int which) const { return raw + (slot * (kStep ? 2 : 1) + which) * kGramRaw; }
   __device__ __forceinline__ void start(int k0, int slot) const {
     if (!wide || k0 >= k_end) return;
-    const int R = short_side(f), r0 = kTall ? k0 : first, r_end = kTall ? k_end : R, c0 = kTall ? first : k0, c_end = kTall ? R : k_end;
-    raw_copy<kRows, kRun, kGramThreads>(piece(slot, 0), f.u, f.ldu, elem_size(a.in_type), r0, r_end, c0, c_end);
-    if (a.step) raw_copy<kRows, kRun, kGramThreads>(piece(slot, 1), f.m, f.ldm, 4, r0, r_end, c0, c_end);
+    const int R = short_side(f), on = k0 - k_begin, r_end = kTall ? k_end : R, c_end = kTall ? R : k_end;
+    copy_u.start(piece(slot, 0), kTall ? on : 0, kTall ? 0 : on, r_end, c_end);
+    if (kStep) copy_m.start(piece(slot, 1), kTall ? on : 0, kTall ? 0 : on, r_end, c_end);
   }
   __device__ __forceinline__ void put(double* to, int k0, int slot) const {
-    const int R = short_side(f), tid = threadIdx.x, elem = elem_size(a.in_type);
+    const int R = short_side(f), tid = threadIdx.x;
+    const bool bf16 = a.in_type == CWL_BF16;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       // four neighbours of a row; lanes take neighbouring rows
-      const int row = kTall ? tid & 31 : i * 16 + (tid & 15), at = kTall ? i * 16 + (tid >> 5) * 4 : (tid >> 4) * 4;
+      const int row = kTall ? tid & 31 : i * 32 + (tid & 15) + (tid >> 7) * 16, at = kTall ? i * 32 + (tid >> 5) * 4 : (tid >> 4 & 7) * 4;
       const int r = kTall ? k0 + row : first + row, c = kTall ? first + at : k0 + at;
-      const int left = r < (kTall ? k_end : R) ? (kTall ? R : k_end) - c : 0;
       float4 u;
       if (wide) {
-        const float4 g = four_of(piece(slot, 0) + raw_at<kRun>(row, at, elem), a.in_type);
+        const float4 g = raw_four<kElem>(piece(slot, 0) + raw_at<kRun, kElem>(row, at), bf16);
         u = g;
-        if (a.step) {
-          float4 m = four_of(piece(slot, 1) + raw_at<kRun>(row, at, 4), CWL_F32);
+        if (kStep) {
+          float4 m = *reinterpret_cast<const float4*>(piece(slot, 1) + raw_at<kRun, 4>(row, at));
           if (update) {
             m = make_float4(fmaf(a.beta, m.x, g.x), fmaf(a.beta, m.y, g.y), fmaf(a.beta, m.z, g.z), fmaf(a.beta, m.w, g.w));
-            store4_f32(f.m + (int64_t)r * f.ldm + c, m, vec_m, left);
+            const int left = r < (kTall ? k_end : R) ? (kTall ? R : k_end) - c : 0;
+            store4_f32(f.m + (int64_t)r * f.ldm + c, m, true, left);
           }
-          u = a.nesterov ? make_float4(fmaf(a.beta, m.x, g.x), fmaf(a.beta, m.y, g.y), fmaf(a.beta, m.z, g.z), fmaf(a.beta, m.w, g.w)) : m;
+          u = step_u(a, g, m);
         }
       } else {
+        const int left = r < (kTall ? k_end : R) ? (kTall ? R : k_end) - c : 0;
         u = update ? load_u<true>(a, f, r, c, left, vec_u, vec_m) : load_u<false>(a, f, r, c, left, vec_u, vec_m);
       }
       const float v[4] = {u.x, u.y, u.z, u.w};
@@ -252,7 +279,7 @@ struct GramSide {
   }
 };
 
-template <bool kTall>
+template <bool kTall, bool kStep, int kElem>
 __device__ __forceinline__ void gram_block(const FactorCommon& a, const Factor& f, uint8_t* gram_raw, double* out) {
   double* rows_i = reinterpret_cast<double*>(gram_raw);
   double* rows_j = rows_i + 64 * kGramLd;
@@ -265,120 +292,135 @@ __device__ __forceinline__ void gram_block(const FactorCommon& a, const Factor& 
   int bi = 0, bj = unit % pairs;
   while (bj > bi) { bj -= bi + 1; ++bi; }          // bj <= bi
   const int k_begin = slice * a.slice, k_end = min(n, k_begin + a.slice);
-  const int elem = elem_size(a.in_type);
-  const bool wide = wide_rows(f.u, f.ldu, elem) && (!a.step || wide_rows(f.m, f.ldm, 4));
-  const bool vec_u = vec_rows(f.u, f.ldu, elem), vec_m = a.step && vec_rows(f.m, f.ldm, 4);
+  const bool wide = wide_rows(f.u, f.ldu, kElem) && (!kStep || wide_rows(f.m, f.ldm, 4));
+  const bool vec_u = vec_rows(f.u, f.ldu, kElem), vec_m = kStep && vec_rows(f.m, f.ldm, 4);
   // each element is read by one block only where R <= 64: the momentum is brought up to date there
-  const GramSide<kTall> si{a, f, wide, vec_u, vec_m, a.step != 0 && R <= kShort, bi * 64, k_end, ring};
+  const GramSide<kTall, kStep, kElem> si(a, f, wide, vec_u, vec_m, kStep && R <= kShort, bi * 64, k_begin, k_end, ring);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, fr = lane >> 2, fc = lane & 3;
 
-  if (bi == bj) {
-    // 36 tiles of the lower triangle in every warp, which takes a quarter of the K steps: eight fragments serve 36 products
-    const int tiles = min(8, (R - bi * 64 + 7) / 8);
-    double acc[36][2];
+  auto pipeline = [&](auto start, auto put, auto multiply) {
 #pragma unroll
-    for (int i = 0; i < 36; ++i) acc[i][0] = acc[i][1] = 0.0;
-#pragma unroll
-    for (int i = 0; i < kGramRing - 1; ++i) { si.start(k_begin + i * kGramK, i); copies_commit(); }
+    for (int i = 0; i < kGramRing - 1; ++i) { start(k_begin + i * kGramK, i); copies_commit(); }
     int slot = 0;
     for (int k0 = k_begin; k0 < k_end; k0 += kGramK) {
       copies_wait<kGramRing - 2>();
       __syncthreads();                             // the chunk has arrived; the one before is done with
-      si.put(rows_i, k0, slot);
-      const int next = slot == 0 ? kGramRing - 1 : slot - 1;
-      si.start(k0 + (kGramRing - 1) * kGramK, next);
+      put(k0, slot);
+      start(k0 + (kGramRing - 1) * kGramK, slot == 0 ? kGramRing - 1 : slot - 1);
       copies_commit();
       if (++slot == kGramRing) slot = 0;
       __syncthreads();
-#pragma unroll 1
-      for (int s = warp; s < kGramK / 4; s += 4) {
-        double x[8];
-#pragma unroll
-        for (int t = 0; t < 8; ++t) x[t] = rows_i[gram_at(t * 8 + fr, s * 4 + fc)];
-#pragma unroll
-        for (int ti = 0; ti < 8; ++ti) {
-          if (ti < tiles) {
-#pragma unroll
-            for (int tj = 0; tj <= ti; ++tj) mma_f64(acc[ti * (ti + 1) / 2 + tj], x[ti], x[tj]);
-          }
-        }
-      }
+      multiply();
     }
-    // the warps' sums, in their order
-    for (int w = 0; w < 4; ++w) {
-      __syncthreads();
-      if (warp == w) {
-#pragma unroll
-        for (int i = 0; i < 36; ++i) {
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            double* s = sums + i * 64 + fr * 8 + fc * 2 + j;
-            *s = w == 0 ? acc[i][j] : *s + acc[i][j];
-          }
-        }
-      }
-    }
+    copies_wait<0>();
     __syncthreads();
+  };
+  if (bi == bj) {
+    // 36 tiles of the lower triangle, 18 a warp; four warps take a quarter of the K steps each: eight fragments serve 18 products
+    const int half = warp >> 2, quarter = warp & 3;
+    double acc[18][2];
+#pragma unroll
+    for (int i = 0; i < 18; ++i) acc[i][0] = acc[i][1] = 0.0;
+    pipeline([&](int k0, int slot) { si.start(k0, slot); }, [&](int k0, int slot) { si.put(rows_i, k0, slot); },
+             [&]() {
+#pragma unroll 1
+               for (int s = quarter; s < kGramK / 4; s += 4) {
+                 double x[8];
+#pragma unroll
+                 for (int t = 0; t < 8; ++t) x[t] = rows_i[gram_at(t * 8 + fr, s * 4 + fc)];
+                 // in the order of rows: rows 0 to 4 and half of row 5, or the rest (a branch around each half: predicated
+                 // products of the other half would take the unit's time all the same)
+                 if (half == 0) {
+#pragma unroll
+                   for (int ti = 0; ti < 8; ++ti)
+#pragma unroll
+                     for (int tj = 0; tj <= ti; ++tj) {
+                       const int at = ti * (ti + 1) / 2 + tj;
+                       if (at < 18) mma_f64(acc[at < 18 ? at : 0], x[ti], x[tj]);
+                     }
+                 } else {
+#pragma unroll
+                   for (int ti = 0; ti < 8; ++ti)
+#pragma unroll
+                     for (int tj = 0; tj <= ti; ++tj) {
+                       const int at = ti * (ti + 1) / 2 + tj;
+                       if (at >= 18) mma_f64(acc[at < 18 ? 0 : at - 18], x[ti], x[tj]);
+                     }
+                 }
+               }
+             });
+    // the quarters' sums, in their order
+    for (int w = 0; w < 4; ++w) {
+      if (quarter == w) {
+#pragma unroll
+        for (int i = 0; i < 18; ++i) {
+          double2* to = reinterpret_cast<double2*>(sums + (half * 18 + i) * 64 + fr * 8 + fc * 2);
+          double2 v = w == 0 ? make_double2(0.0, 0.0) : *to;
+          v.x += acc[i][0];
+          v.y += acc[i][1];
+          *to = v;
+        }
+      }
+      __syncthreads();
+    }
     // as tiles of the lower triangle
     for (int at = threadIdx.x; at < 36 * 32; at += kGramThreads) reinterpret_cast<double2*>(out)[at] = reinterpret_cast<const double2*>(sums)[at];
   } else {
-    // a warp a quadrant of 32 x 32
-    const GramSide<kTall> sj{a, f, wide, vec_u, vec_m, false, bj * 64, k_end, ring + kGramRing * (a.step ? 2 : 1) * kGramRaw};
-    const int qi = (warp >> 1) * 32, qj = (warp & 1) * 32;
+    // a warp a quadrant of 32 x 32 and half of the K steps
+    const GramSide<kTall, kStep, kElem> sj(a, f, wide, vec_u, vec_m, false, bj * 64, k_begin, k_end, ring + kGramRing * (kStep ? 2 : 1) * kGramRaw);
+    const int qi = (warp >> 1 & 1) * 32, qj = (warp & 1) * 32, half = warp >> 2;
     double acc[4][4][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) acc[i][j][0] = acc[i][j][1] = 0.0;
+    pipeline([&](int k0, int slot) { si.start(k0, slot); sj.start(k0, slot); },
+             [&](int k0, int slot) { si.put(rows_i, k0, slot); sj.put(rows_j, k0, slot); },
+             [&]() {
 #pragma unroll
-    for (int i = 0; i < kGramRing - 1; ++i) {
-      si.start(k_begin + i * kGramK, i);
-      sj.start(k_begin + i * kGramK, i);
-      copies_commit();
+               for (int s = 0; s < kGramK / 8; ++s) {
+                 double x[4], y[4];
+#pragma unroll
+                 for (int t = 0; t < 4; ++t) {
+                   x[t] = rows_i[gram_at(qi + t * 8 + fr, (s * 2 + half) * 4 + fc)];
+                   y[t] = rows_j[gram_at(qj + t * 8 + fr, (s * 2 + half) * 4 + fc)];
+                 }
+#pragma unroll
+                 for (int ti = 0; ti < 4; ++ti)
+#pragma unroll
+                   for (int tj = 0; tj < 4; ++tj) mma_f64(acc[ti][tj], x[ti], y[tj]);
+               }
+             });
+    static_assert(2 * 64 * kGramLd >= 64 * 64, "room for one half's sums");
+    double2* met = reinterpret_cast<double2*>(rows_i);
+    auto place = [&](int ti, int tj) { return ((qi + ti * 8 + fr) * 64 + qj + tj * 8 + fc * 2) / 2; };
+    if (half == 1) {
+#pragma unroll
+      for (int ti = 0; ti < 4; ++ti)
+#pragma unroll
+        for (int tj = 0; tj < 4; ++tj) met[place(ti, tj)] = make_double2(acc[ti][tj][0], acc[ti][tj][1]);
     }
-    int slot = 0;
-    for (int k0 = k_begin; k0 < k_end; k0 += kGramK) {
-      copies_wait<kGramRing - 2>();
-      __syncthreads();
-      si.put(rows_i, k0, slot);
-      sj.put(rows_j, k0, slot);
-      const int next = slot == 0 ? kGramRing - 1 : slot - 1;
-      si.start(k0 + (kGramRing - 1) * kGramK, next);
-      sj.start(k0 + (kGramRing - 1) * kGramK, next);
-      copies_commit();
-      if (++slot == kGramRing) slot = 0;
-      __syncthreads();
+    __syncthreads();
+    if (half == 0) {
 #pragma unroll
-      for (int s = 0; s < kGramK / 4; ++s) {
-        double x[4], y[4];
+      for (int ti = 0; ti < 4; ++ti)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          x[t] = rows_i[gram_at(qi + t * 8 + fr, s * 4 + fc)];
-          y[t] = rows_j[gram_at(qj + t * 8 + fr, s * 4 + fc)];
+        for (int tj = 0; tj < 4; ++tj) {
+          const double2 v = met[place(ti, tj)];
+          reinterpret_cast<double2*>(out)[place(ti, tj)] = make_double2(acc[ti][tj][0] + v.x, acc[ti][tj][1] + v.y);
         }
-#pragma unroll
-        for (int ti = 0; ti < 4; ++ti)
-#pragma unroll
-          for (int tj = 0; tj < 4; ++tj) mma_f64(acc[ti][tj], x[ti], y[tj]);
-      }
     }
-#pragma unroll
-    for (int ti = 0; ti < 4; ++ti)
-#pragma unroll
-      for (int tj = 0; tj < 4; ++tj)
-        *reinterpret_cast<double2*>(out + (qi + ti * 8 + fr) * 64 + qj + tj * 8 + fc * 2) = make_double2(acc[ti][tj][0], acc[ti][tj][1]);
   }
-  copies_wait<0>();
 }
-template <int kMost>
+template <int kMost, bool kStep, int kElem>
 __global__ void __launch_bounds__(kGramThreads, 2) gram_kernel(const __grid_constant__ FactorArgs<kMost> args) {
   extern __shared__ __align__(16) uint8_t gram_raw[];
   pdl_launch_dependents();
   pdl_wait();
   const Factor& f = args.f[find_factor(args.f, args.c.n, blockIdx.x)];
   double* out = args.c.partial + (int64_t)blockIdx.x * 64 * 64;
-  if (f.rows > f.cols) gram_block<true>(args.c, f, gram_raw, out);
-  else gram_block<false>(args.c, f, gram_raw, out);
+  if (f.rows > f.cols) gram_block<true, kStep, kElem>(args.c, f, gram_raw, out);
+  else gram_block<false, kStep, kElem>(args.c, f, gram_raw, out);
 }
 // shared memory of GRAM: two blocks of rows in 64 bits, and the ring (twice, where a pair has two of them)
 size_t gram_smem(bool step, bool pairs) { return (size_t)2 * 64 * kGramLd * 8 + (size_t)kGramRing * (step ? 2 : 1) * (pairs ? 2 : 1) * kGramRaw; }
@@ -564,24 +606,24 @@ struct BigArgs {
 static_assert(sizeof(BigArgs) <= 8 * 1024, "kernel parameters");
 __host__ __device__ __forceinline__ int padded(int R) { return (R + 31) / 32 * 32; }
 
-// Sums of GRAM's partial products, scaled: G_0.  A block a 64 x 64 pair.
-constexpr int kBigGramThreads = 256;
+// Sums of GRAM's partial products, scaled: G_0.  Eight blocks a 64 x 64 pair, two entries a thread.
+constexpr int kBigGramThreads = 256, kBigGramShare = 8;
 __global__ void __launch_bounds__(kBigGramThreads) big_gram_kernel(const __grid_constant__ BigArgs a) {
   __shared__ double met[kBigGramThreads / 32];
   pdl_launch_dependents();
   pdl_wait();
-  const int R = a.R[blockIdx.y], pairs = block_pairs(R), slices = a.slices[blockIdx.y];
-  if ((int)blockIdx.x >= pairs) return;
+  const int R = a.R[blockIdx.y], pairs = block_pairs(R), slices = a.slices[blockIdx.y], pair = blockIdx.x / kBigGramShare;
+  if (pair >= pairs) return;
   const int Rp = padded(R), tid = threadIdx.x;
-  int bi = 0, bj = blockIdx.x;
+  int bi = 0, bj = pair;
   while (bj > bi) { bj -= bi + 1; ++bi; }
   const double* part = a.partial + (int64_t)a.first[blockIdx.y] * 64 * 64;
   // the trace: every block adds it up in the same order
   double s = 0.0;
   for (int i = tid; i < R; i += kBigGramThreads) {
-    const int b = i >> 6, pair = b * (b + 1) / 2 + b;
-#pragma unroll 4
-    for (int k = 0; k < slices; ++k) s += part[((int64_t)k * pairs + pair) * 64 * 64 + lower_at(i & 63, i & 63)];
+    const int b = i >> 6, p = b * (b + 1) / 2 + b;
+#pragma unroll 16
+    for (int k = 0; k < slices; ++k) s += part[((int64_t)k * pairs + p) * 64 * 64 + lower_at(i & 63, i & 63)];
   }
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((tid & 31) == 0) met[tid >> 5] = s;
@@ -590,21 +632,13 @@ __global__ void __launch_bounds__(kBigGramThreads) big_gram_kernel(const __grid_
   for (int w = 0; w < kBigGramThreads / 32; ++w) trace += met[w];
   const double unit = trace == 0.0 ? 0.0 : 1.0 / (sqrt(trace) + a.eps);
   double* G = a.big + (int64_t)blockIdx.y * 5 * a.stride;
-  constexpr int kEach = 64 * 64 / kBigGramThreads;
-  double v[kEach];
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) v[e] = 0.0;
   // of a block on the diagonal its tiles of the lower triangle are there, all of the others
-  const int entries = bi == bj ? 36 * 64 : 64 * 64;
-  for (int k = 0; k < slices; ++k) {
-#pragma unroll
-    for (int e = 0; e < kEach; ++e)
-      if (e * kBigGramThreads + tid < entries) v[e] += part[((int64_t)k * pairs + blockIdx.x) * 64 * 64 + e * kBigGramThreads + tid];
-  }
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const int at = e * kBigGramThreads + tid;
-    if (at >= entries) continue;
+  const int entries = (bi == bj ? 36 * 64 : 64 * 64) / kBigGramShare;
+  for (int e = tid; e < entries; e += kBigGramThreads) {
+    const int at = (blockIdx.x % kBigGramShare) * entries + e;
+    double v = 0.0;
+#pragma unroll 16
+    for (int k = 0; k < slices; ++k) v += part[((int64_t)k * pairs + pair) * 64 * 64 + at];
     int r = at >> 6, c = at & 63;
     if (bi == bj) {
       int ti, tj;
@@ -616,7 +650,7 @@ __global__ void __launch_bounds__(kBigGramThreads) big_gram_kernel(const __grid_
     r += bi * 64;
     c += bj * 64;
     if (r >= Rp || c >= Rp) continue;
-    G[(int64_t)r * Rp + c] = G[(int64_t)c * Rp + r] = v[e] * unit * unit;
+    G[(int64_t)r * Rp + c] = G[(int64_t)c * Rp + r] = v * unit * unit;
   }
   if (blockIdx.x == 0 && tid == 0) a.unit[blockIdx.y] = unit;
 }
@@ -701,113 +735,56 @@ __global__ void __launch_bounds__(kBigThreads) big_product_kernel(const __grid_c
 
 // ------------------------------------------------------------------------------------------------------------ APPLY
 // O = Q U over 64 short-side rows and 128 long-side elements.  Outputs of a thread: 8 x 4 with the lanes along the rows of the
-// factor as they lie in memory, whichever side that is.
+// factor as they lie in memory, whichever side that is; two neighbours of the long side advance in one instruction, with each
+// number of Q twice in shared memory.
 constexpr int kApplyThreads = 256;
 constexpr int kApplyK = 32;
-constexpr int kApplyLdX = kApplyLong + 4, kApplyLdQ = kApplyShort + 4;
+constexpr int kApplyRing = 2;
+constexpr int kApplyLdX = kApplyLong + 4, kApplyLdQ = 2 * kApplyShort + 4;
+constexpr int kApplyRaw = kApplyK * kApplyLong;    // elements of a chunk
 
-template <bool kTall>
-__device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& f, const float* q, int long0, int short0, float* xs, float* qs) {
+__device__ __forceinline__ void fma_two(float2& d, const float2& a, const float2& b) {
+  unsigned long long x = *reinterpret_cast<const unsigned long long*>(&d);
+  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(x) : "l"(*reinterpret_cast<const unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&b)));
+  d = *reinterpret_cast<float2*>(&x);
+}
+
+template <bool kTall, bool kStep, int kElem>
+__device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& f, const float* q, int long0, int short0, uint8_t* raw) {
   const int R = short_side(f), n = long_side(f), tid = threadIdx.x;
-  const bool vec_u = vec_rows(f.u, f.ldu, elem_size(a.in_type)), vec_m = a.step && vec_rows(f.m, f.ldm, 4);
-  const bool vec_q = (R & 3) == 0;
-  // this thread's outputs: short side s0.., long side l0..
+  const bool wide = wide_rows(f.u, f.ldu, kElem) && (!kStep || wide_rows(f.m, f.ldm, 4));
+  const bool vec_u = vec_rows(f.u, f.ldu, kElem), vec_m = kStep && vec_rows(f.m, f.ldm, 4), vec_q = (R & 3) == 0, bf16 = a.in_type == CWL_BF16;
+  float* xs = reinterpret_cast<float*>(raw);
+  float* qs = xs + kApplyK * kApplyLdX;
+  uint8_t* ring = raw + (kApplyK * kApplyLdX + kApplyK * kApplyLdQ) * 4;
+  constexpr int kSlot = kApplyRaw * (kElem + (kStep ? 4 : 0));
+  // a chunk as it lies in memory
+  constexpr int kRows = kTall ? kApplyLong : kApplyK, kRun = kTall ? kApplyK : kApplyLong;
+  const RawCopy<kRows, kRun, kElem, kApplyThreads> copy_u(f.u, f.ldu, kTall ? long0 : 0, kTall ? 0 : long0);
+  const RawCopy<kRows, kRun, 4, kApplyThreads> copy_m(f.m, f.ldm, kTall ? long0 : 0, kTall ? 0 : long0);
+  auto start = [&](int k0, int slot) {
+    if (wide && k0 < R) {
+      copy_u.start(ring + slot * kSlot, kTall ? 0 : k0, kTall ? k0 : 0, f.rows, f.cols);
+      if (kStep) copy_m.start(ring + slot * kSlot + kApplyRaw * kElem, kTall ? 0 : k0, kTall ? k0 : 0, f.rows, f.cols);
+    }
+    copies_commit();
+  };
+#pragma unroll
+  for (int i = 0; i < kApplyRing; ++i) start(i * kApplyK, i);
+
+  // this thread's outputs: short side s0.., long side l0..; at_output(i): its i-th four neighbours of a row of the factor
   constexpr int kS = kTall ? 4 : 8, kL = kTall ? 8 : 4;
   const int s0 = kTall ? (tid & 15) * 4 : (tid >> 5) * 8, l0 = kTall ? (tid >> 4) * 8 : (tid & 31) * 4;
-  float acc[kS][kL];
-#pragma unroll
-  for (int i = 0; i < kS; ++i)
-#pragma unroll
-    for (int j = 0; j < kL; ++j) acc[i][j] = 0.f;
-
-  // What comes next is loaded raw, all loads together, and becomes U when it is put into shared memory.
-  float4 x[4], mom[4], y[2];
-  const bool inside = vec_u && (!a.step || vec_m) && (kTall ? (R & 3) == 0 : (n & 3) == 0);
-  auto place = [&](int k0, int i, int& r, int& c) {
-    if (kTall) { r = long0 + i * 32 + (tid >> 3); c = k0 + (tid & 7) * 4; }      // U [long][short]: eight threads 32 of a row
-    else { r = k0 + i * 8 + (tid >> 5); c = long0 + (tid & 31) * 4; }            // U [short][long]: a warp 128 of a row
-    return r < f.rows ? f.cols - c : 0;
-  };
-  auto fetch = [&](int k0) {
-    int r, c;
-    if (inside) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool there = place(k0, i, r, c) > 0;
-        const int64_t at = (int64_t)r * f.ldu + c;
-        if (a.in_type == CWL_F32) {
-          x[i] = there ? *reinterpret_cast<const float4*>(static_cast<const float*>(f.u) + at) : make_float4(0.f, 0.f, 0.f, 0.f);
-        } else {
-          const float2 q = there ? *reinterpret_cast<const float2*>(static_cast<const uint16_t*>(f.u) + at) : make_float2(0.f, 0.f);
-          x[i].x = q.x;
-          x[i].y = q.y;
-        }
-        if (a.step) mom[i] = there ? *reinterpret_cast<const float4*>(f.m + (int64_t)r * f.ldm + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int left = place(k0, i, r, c);
-        x[i] = load_u<false>(a, f, r, c, left, vec_u, vec_m);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {                  // Q is symmetric: its row k is the column wanted
-      const int k = k0 + i * 16 + (tid >> 4), s = short0 + (tid & 15) * 4, left = k < R ? R - s : 0;
-      y[i] = load4(q, (int64_t)k * R + s, CWL_F32, vec_q, left);
-    }
-  };
-  auto made = [&](int i) {                         // U from what was loaded
-    if (!inside) return x[i];
-    const float4 g = four_of(&x[i], a.in_type);
-    if (!a.step) return g;
-    const float4 m = mom[i];
-    return a.nesterov ? make_float4(fmaf(a.beta, m.x, g.x), fmaf(a.beta, m.y, g.y), fmaf(a.beta, m.z, g.z), fmaf(a.beta, m.w, g.w)) : m;
-  };
-  fetch(0);
-  for (int k0 = 0; k0 < R; k0 += kApplyK) {
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 u = made(i);
-      if (kTall) {
-        const int l = i * 32 + (tid >> 3), k = (tid & 7) * 4;
-        xs[k * kApplyLdX + l] = u.x; xs[(k + 1) * kApplyLdX + l] = u.y;
-        xs[(k + 2) * kApplyLdX + l] = u.z; xs[(k + 3) * kApplyLdX + l] = u.w;
-      } else {
-        *reinterpret_cast<float4*>(xs + (i * 8 + (tid >> 5)) * kApplyLdX + (tid & 31) * 4) = u;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) *reinterpret_cast<float4*>(qs + (i * 16 + (tid >> 4)) * kApplyLdQ + (tid & 15) * 4) = y[i];
-    __syncthreads();
-    if (k0 + kApplyK < R) fetch(k0 + kApplyK);
-#pragma unroll 8
-    for (int k = 0; k < kApplyK; ++k) {
-      float sv[kS], lv[kL];
-#pragma unroll
-      for (int i = 0; i < kS; i += 4) *reinterpret_cast<float4*>(sv + i) = *reinterpret_cast<const float4*>(qs + k * kApplyLdQ + s0 + i);
-#pragma unroll
-      for (int j = 0; j < kL; j += 4) *reinterpret_cast<float4*>(lv + j) = *reinterpret_cast<const float4*>(xs + k * kApplyLdX + l0 + j);
-#pragma unroll
-      for (int i = 0; i < kS; ++i)
-#pragma unroll
-        for (int j = 0; j < kL; ++j) acc[i][j] = fmaf(sv[i], lv[j], acc[i][j]);
-    }
-  }
-
-  const int out_type = a.step ? CWL_F32 : a.out_type;
+  const int out_type = kStep ? CWL_F32 : a.out_type;
   const bool vec_o = vec_rows(f.out, f.ldo, elem_size(out_type)), vec_l = f.low != nullptr && vec_rows(f.low, f.ldl, 2);
-  const float by = a.step ? -a.lr * f.scale : 1.f;
-  // four neighbours of a row of the factor at a time; a step's masters all come in before the first is written back
   auto at_output = [&](int i, int& r, int& c) {
     r = kTall ? long0 + l0 + i : short0 + s0 + i;
     c = kTall ? short0 + s0 : long0 + l0;
     return r < f.rows ? f.cols - c : 0;
   };
   int r, c;
-  float4 p[8];
-  if (a.step) {
+  float4 p[kStep ? 8 : 1];
+  if (kStep) {                                     // a step's masters, on their way meanwhile
     const bool whole = vec_o && (f.cols & 3) == 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -817,14 +794,76 @@ __device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& 
       else p[i] = load4(at, 0, CWL_F32, vec_o, left);
     }
   }
+  float2 acc[kS][kL / 2];
+#pragma unroll
+  for (int i = 0; i < kS; ++i)
+#pragma unroll
+    for (int j = 0; j < kL / 2; ++j) acc[i][j] = make_float2(0.f, 0.f);
+
+  int slot = 0;
+  for (int k0 = 0; k0 < R; k0 += kApplyK) {
+    float4 y[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {                  // Q is symmetric: its row k is the column wanted
+      const int k = k0 + i * 16 + (tid >> 4), s = short0 + (tid & 15) * 4, left = k < R ? R - s : 0;
+      y[i] = load4(q, (int64_t)k * R + s, CWL_F32, vec_q, left);
+    }
+    copies_wait<kApplyRing - 1>();
+    __syncthreads();                               // the chunk has arrived; the one before is done with
+    const uint8_t* u_raw = ring + slot * kSlot;
+    const uint8_t* m_raw = u_raw + kApplyRaw * kElem;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = kTall ? i * 32 + (tid & 31) : i * 8 + (tid >> 5), at = kTall ? (tid >> 5) * 4 : (tid & 31) * 4;
+      float4 u;
+      if (wide) {
+        u = raw_four<kElem>(u_raw + raw_at<kRun, kElem>(row, at), bf16);
+        if (kStep) u = step_u(a, u, *reinterpret_cast<const float4*>(m_raw + raw_at<kRun, 4>(row, at)));
+      } else {
+        const int ur = kTall ? long0 + row : k0 + row, uc = kTall ? k0 + at : long0 + at;
+        u = load_u<false>(a, f, ur, uc, ur < f.rows ? f.cols - uc : 0, vec_u, vec_m);
+      }
+      if (kTall) {
+        xs[at * kApplyLdX + row] = u.x; xs[(at + 1) * kApplyLdX + row] = u.y;
+        xs[(at + 2) * kApplyLdX + row] = u.z; xs[(at + 3) * kApplyLdX + row] = u.w;
+      } else {
+        *reinterpret_cast<float4*>(xs + row * kApplyLdX + at) = u;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float4* to = reinterpret_cast<float4*>(qs + (i * 16 + (tid >> 4)) * kApplyLdQ + (tid & 15) * 8);
+      to[0] = make_float4(y[i].x, y[i].x, y[i].y, y[i].y);
+      to[1] = make_float4(y[i].z, y[i].z, y[i].w, y[i].w);
+    }
+    __syncthreads();
+    start(k0 + kApplyRing * kApplyK, slot);
+    slot ^= 1;
+#pragma unroll 4
+    for (int k = 0; k < kApplyK; ++k) {
+      float2 sv[kS], lv[kL / 2];
+#pragma unroll
+      for (int i = 0; i < kS; i += 2) *reinterpret_cast<float4*>(sv + i) = *reinterpret_cast<const float4*>(qs + k * kApplyLdQ + (s0 + i) * 2);
+#pragma unroll
+      for (int j = 0; j < kL / 2; j += 2) *reinterpret_cast<float4*>(lv + j) = *reinterpret_cast<const float4*>(xs + k * kApplyLdX + l0 + j * 2);
+#pragma unroll
+      for (int i = 0; i < kS; ++i)
+#pragma unroll
+        for (int j = 0; j < kL / 2; ++j) fma_two(acc[i][j], sv[i], lv[j]);
+    }
+  }
+  copies_wait<0>();
+
+  const float by = kStep ? -a.lr * f.scale : 1.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int left = at_output(i, r, c);
     if (left <= 0) continue;
-    float4 v = kTall ? make_float4(acc[0][i % kL], acc[1 % kS][i % kL], acc[2 % kS][i % kL], acc[3 % kS][i % kL])
-                     : make_float4(acc[i % kS][0], acc[i % kS][1 % kL], acc[i % kS][2 % kL], acc[i % kS][3 % kL]);
-    if (a.step) {
-      v = make_float4(fmaf(by, v.x, a.keep * p[i].x), fmaf(by, v.y, a.keep * p[i].y), fmaf(by, v.z, a.keep * p[i].z), fmaf(by, v.w, a.keep * p[i].w));
+    auto out = [&](int s, int l) { return l & 1 ? acc[s % kS][l / 2 % (kL / 2)].y : acc[s % kS][l / 2 % (kL / 2)].x; };
+    float4 v = kTall ? make_float4(out(0, i), out(1, i), out(2, i), out(3, i)) : make_float4(out(i, 0), out(i, 1), out(i, 2), out(i, 3));
+    if (kStep) {
+      const float4 m = p[kStep ? i : 0];
+      v = make_float4(fmaf(by, v.x, a.keep * m.x), fmaf(by, v.y, a.keep * m.y), fmaf(by, v.z, a.keep * m.z), fmaf(by, v.w, a.keep * m.w));
       store4_f32(static_cast<float*>(f.out) + (int64_t)r * f.ldo + c, v, vec_o, left);
       if (f.low != nullptr) store4_bf16(f.low + (int64_t)r * f.ldl + c, v, vec_l, left);
     } else if (out_type == CWL_F32) {
@@ -835,9 +874,9 @@ __device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& 
   }
 }
 
-template <int kMost>
+template <int kMost, bool kStep, int kElem>
 __global__ void __launch_bounds__(kApplyThreads, 2) apply_factors_kernel(const __grid_constant__ FactorArgs<kMost> args) {
-  __shared__ __align__(16) float xs[kApplyK * kApplyLdX], qs[kApplyK * kApplyLdQ];
+  extern __shared__ __align__(16) uint8_t apply_raw[];
   pdl_launch_dependents();
   pdl_wait();
   const int at = find_factor(args.f, args.c.n, blockIdx.x);
@@ -845,8 +884,11 @@ __global__ void __launch_bounds__(kApplyThreads, 2) apply_factors_kernel(const _
   const int unit = blockIdx.x - f.first, row_tiles = (short_side(f) + kApplyShort - 1) / kApplyShort;
   const int long0 = unit / row_tiles * kApplyLong, short0 = unit % row_tiles * kApplyShort;
   const float* q = args.c.q + at * args.c.q_stride;
-  if (f.rows > f.cols) apply_tile<true>(args.c, f, q, long0, short0, xs, qs);
-  else apply_tile<false>(args.c, f, q, long0, short0, xs, qs);
+  if (f.rows > f.cols) apply_tile<true, kStep, kElem>(args.c, f, q, long0, short0, apply_raw);
+  else apply_tile<false, kStep, kElem>(args.c, f, q, long0, short0, apply_raw);
+}
+constexpr size_t apply_smem(bool step, int elem) {
+  return (size_t)(kApplyK * kApplyLdX + kApplyK * kApplyLdQ) * 4 + (size_t)kApplyRing * kApplyRaw * (elem + (step ? 4 : 0));
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -897,7 +939,22 @@ size_t factor_bytes(const Item* items, int n) {
   return most;
 }
 
-template <int kMost, typename Item, typename Fill>
+template <int kMost, bool kStep, int kElem>
+cudaError_t launch_gram(const FactorArgs<kMost>& args, int64_t blocks, bool pairs, bool chained, cudaStream_t st) {
+  static SharedMemoryGrant grant;
+  const cudaError_t e = grant(gram_kernel<kMost, kStep, kElem>);
+  if (e != cudaSuccess) return e;
+  return launch_chained(chained, gram_kernel<kMost, kStep, kElem>, dim3((unsigned)blocks), dim3(kGramThreads), gram_smem(kStep, pairs), st, args);
+}
+template <int kMost, bool kStep, int kElem>
+cudaError_t launch_apply(const FactorArgs<kMost>& args, int64_t blocks, bool chained, cudaStream_t st) {
+  static SharedMemoryGrant grant;
+  const cudaError_t e = grant(apply_factors_kernel<kMost, kStep, kElem>);
+  if (e != cudaSuccess) return e;
+  return launch_chained(chained, apply_factors_kernel<kMost, kStep, kElem>, dim3((unsigned)blocks), dim3(kApplyThreads), apply_smem(kStep, kElem), st, args);
+}
+
+template <int kMost, bool kStep, int kElem, typename Item, typename Fill>
 cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, void* workspace, bool chained, cudaStream_t st) {
   const FactorPlan plan = factor_plan(items, n);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
@@ -942,9 +999,7 @@ cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, v
     const int64_t x = (most_elements / 4 + kMomentumThreads * 4 - 1) / (kMomentumThreads * 4);
     CWL_CUDA_TRY(launch_chained(chained, momentum_kernel<kMost>, dim3((unsigned)(x < 592 ? x + 1 : 592), (unsigned)n), dim3(kMomentumThreads), 0, st, args));
   }
-  static SharedMemoryGrant gram_grant;
-  CWL_CUDA_TRY(gram_grant(gram_kernel<kMost>));
-  CWL_CUDA_TRY(launch_chained(chained, gram_kernel<kMost>, dim3((unsigned)gram_blocks), dim3(kGramThreads), gram_smem(common.step != 0, big.n > 0), st, args));
+  CWL_CUDA_TRY((launch_gram<kMost, kStep, kElem>(args, gram_blocks, big.n > 0, chained, st)));
   if (any_small) {
     if (most_slices > 1)
       CWL_CUDA_TRY(launch_chained(chained, slices_kernel<kMost>, dim3(36, (unsigned)n), dim3(kSlicesThreads), 0, st, args));
@@ -955,7 +1010,7 @@ cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, v
   if (big.n > 0) {
     static SharedMemoryGrant grant;
     CWL_CUDA_TRY(grant(big_product_kernel));
-    CWL_CUDA_TRY(launch_chained(chained, big_gram_kernel, dim3((unsigned)block_pairs(most_R), (unsigned)big.n), dim3(kBigGramThreads), 0, st, big));
+    CWL_CUDA_TRY(launch_chained(chained, big_gram_kernel, dim3((unsigned)(block_pairs(most_R) * kBigGramShare), (unsigned)big.n), dim3(kBigGramThreads), 0, st, big));
     const int t = padded(most_R) / 32, tiles = t * (t + 1) / 2;
     for (int step = 0; step < common.steps; ++step) {
       const bool last = step + 1 == common.steps;
@@ -972,19 +1027,22 @@ cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, v
     args.f[i].first = (int)blocks;
     blocks += apply_blocks(args.f[i]);
   }
-  CWL_CUDA_TRY(launch_chained(chained, apply_factors_kernel<kMost>, dim3((unsigned)blocks), dim3(kApplyThreads), 0, st, args));
+  CWL_CUDA_TRY((launch_apply<kMost, kStep, kElem>(args, blocks, chained, st)));
   return CWL_OK;
 }
 
-template <typename Item, typename Fill>
+template <bool kStep, typename Item, typename Fill>
 cwl_status run_factors(const Item* items, int n, const FactorCommon& common, Fill fill, void* workspace, size_t workspace_bytes, void* stream) {
   if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < factor_bytes(items, n)) return CWL_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool chained = !stream_is_capturing(st);
   for (int i = 0; i < n; i += kMostFactors) {
     const int m = n - i < kMostFactors ? n - i : kMostFactors;
-    const cwl_status s = m <= kFewFactors ? run_group<kFewFactors>(items + i, m, common, fill, workspace, chained, st)
-                                          : run_group<kMostFactors>(items + i, m, common, fill, workspace, chained, st);
+    const bool f32 = common.in_type == CWL_F32;
+    const cwl_status s = m <= kFewFactors ? (f32 ? run_group<kFewFactors, kStep, 4>(items + i, m, common, fill, workspace, chained, st)
+                                                 : run_group<kFewFactors, kStep, 2>(items + i, m, common, fill, workspace, chained, st))
+                                          : (f32 ? run_group<kMostFactors, kStep, 4>(items + i, m, common, fill, workspace, chained, st)
+                                                 : run_group<kMostFactors, kStep, 2>(items + i, m, common, fill, workspace, chained, st));
     if (s != CWL_OK) return s;
   }
   return CWL_OK;
@@ -1036,7 +1094,7 @@ extern "C" cwl_status cwl_orthogonalize(const cwl_factor* factors, int32_t n, cw
   FactorCommon c = {};
   c.in_type = in_dtype; c.out_type = out_dtype;
   c.steps = iteration->steps; c.a = iteration->a; c.b = iteration->b; c.c = iteration->c; c.eps = iteration->eps;
-  return run_factors(factors, n, c, [](const cwl_factor& i, Factor& f) {
+  return run_factors<false>(factors, n, c, [](const cwl_factor& i, Factor& f) {
     f.u = i.grad; f.out = i.out;
     f.ldu = row_step(i.ld_grad, i.rows, i.cols); f.ldo = row_step(i.ld_out, i.rows, i.cols);
   }, workspace, workspace_bytes, stream);
@@ -1065,7 +1123,7 @@ extern "C" cwl_status cwl_factor_step(const cwl_factor* factors, int32_t n, cwl_
   c.step = 1; c.nesterov = nesterov != 0; c.in_type = grad_dtype; c.out_type = CWL_F32;
   c.beta = momentum; c.keep = (float)(1.0 - (double)lr * weight_decay); c.lr = lr;
   c.steps = iteration->steps; c.a = iteration->a; c.b = iteration->b; c.c = iteration->c; c.eps = iteration->eps;
-  return run_factors(factors, n, c, [](const cwl_factor& i, Factor& f) {
+  return run_factors<true>(factors, n, c, [](const cwl_factor& i, Factor& f) {
     f.u = i.grad; f.m = static_cast<float*>(i.momentum); f.out = i.out; f.low = static_cast<__nv_bfloat16*>(i.low);
     f.ldu = row_step(i.ld_grad, i.rows, i.cols); f.ldm = row_step(i.ld_momentum, i.rows, i.cols);
     f.ldo = row_step(i.ld_out, i.rows, i.cols); f.ldl = row_step(i.ld_low, i.rows, i.cols);
