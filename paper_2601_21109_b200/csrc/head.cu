@@ -12,17 +12,18 @@
 //   DX     piece of E or dZ times W^T; the sums over the pieces are kept in fp32
 //   DW     X^T times piece of dZ: whole columns of dW
 //
-// Loss and dX in one call take two products, not three: dX = up (sum_v E_tv W_v / sum_v E_tv - W_y) needs the row's sum at the
-// end only.  bf16 has the exponents of fp32, so that any logit of the row will do as the reference r_t as long as no other
+// Loss and dX in one call take two products, not three: dX = up (sum_(v != y) E_tv W_v - W_y sum_(v != y) E_tv) / sum_v E_tv needs
+// the row's sums at the end only.  bf16 has the exponents of fp32, so that any logit of the row will do as the reference r_t as long as no other
 // lies 60 above it: the target's, or (many rows) that of column 0.  Where one does, its 64 columns take a reference of their own,
 // and head_merge_kernel puts the row's piece on a common one before DX reads it.  The target's column W_y is gathered from W
 // and subtracted in fp32, so that it is not among what is rounded to bf16: a token of which the model knows little has
-// dX near -up W_y.
+// dX near -up W_y, and where the model is sure of it E_y W_y and W_y would cancel.
 //
 // Roundings to fewer bits: E and dZ to bf16 (2^-9 of a number on the average row: dX's own rounding to bf16 is as large).
-// For fp32 gradients they are kept as the sum of two bf16 numbers (2^-17), each multiplied on its own, and the tensor cores'
-// sums, which are truncated at every step of 16 (2.4e-6 of a sum of 256 steps, measured on the logits of d = 4096), are added
-// up in fp32 after every kChunkBlocks K blocks.  dZ is relative to the first row's up: rows of one weight are then not rounded twice.
+// For fp32 gradients they are kept as the sum of two bf16 numbers (2^-17), of up to kThreeTermRows rows, where one number's error
+// shows in a whole column of dW, of three (2^-25), each multiplied on its own; and the tensor cores' sums, which are
+// truncated at every step of 16 (2.4e-6 of a sum of 256 steps, measured on the logits of d = 4096), are added up in fp32 after
+// every kChunkBlocks K blocks, over the terms.  dZ is relative to the first row's up: rows of one weight are then not rounded twice.
 #include "cluster.cuh"
 #include "cwl_common.cuh"
 #include "pair_mma.cuh"
@@ -45,7 +46,8 @@ constexpr size_t kHSmem = 1024 + kHRing + kHEpiWarps * kHOutBuf + kHBars + 32;
 constexpr int kHPairs = 74;                       // CTA pairs that schedules are made for (a B200 holds 74)
 constexpr int kHRaster = 16;                      // row tiles whose columns are walked together, so that they share W in L2
 constexpr int kHeadMaxRows = 1 << 24, kHeadMaxWidth = 1 << 20;   // T and V, d
-constexpr int kChunkBlocks = 32;                  // K blocks after which the sums of an fp32 gradient leave the tensor memory
+constexpr int kChunkBlocks = 64;                  // K blocks, times terms, after which the sums of an fp32 gradient leave the tensor memory
+constexpr int kThreeTermRows = 512;
 // Logits of up to kExactRows rows, or of more than kExactWidth activations, are added up in fp32 after every kLogitChunk K
 // blocks: the truncation of the tensor cores' own sums would show in the loss of a single token that the model is sure of (1.6e-5
 // of one of 0.9, d = 4096), and would grow with d.  It takes tiles of 256 columns, whose operands come in no faster than they
@@ -64,9 +66,10 @@ struct HeadRows {                                 // the packed rows, written by
   float* lse;                                     // known from the start in a backward call
   float* z_target;
   float* ref;                                     // EXP: reference of the row's exponentials (a backward call: lse)
-  float* sum;                                     // ... their sum over the pieces so far
+  float* sum;                                     // ... their sum over the pieces so far, without the target's
   float* alpha;                                   // ... what the sums of the pieces before this one are multiplied with
-  float* scale;                                   // DX: up / sum (a backward call: up)
+  float* scale;                                   // DX: up / sum of all (a backward call: up)
+  float* of_target;                               // DX: up times what the other tokens' probabilities add up to
   unsigned* above;                                // EXP: bit per chunk of columns of the piece that took their own reference
   float* above_ref;                               // ... and that reference
   int above_words, chunks;                        // words and chunks a row (64 columns; in head_few_kernel a block's)
@@ -84,7 +87,7 @@ struct HeadParams {
   int stages, stage_bytes;                        // of the ring
   int split, kb_per_split;                        // shares of the K loop
   int chunk_kb;                                   // K blocks after which sums leave the tensor memory (0: at the end)
-  int halves, half_at;                            // E / dZ is one bf16 number or two, whose second lies half_at columns on
+  int terms, term_at;                             // E / dZ is the sum of so many bf16 numbers, each term_at columns after the one before
   int rows_alloc;                                 // rows of the workspace arrays
   float2* part;                                   // STATS, EXP: [2 n_cols][rows_alloc] (max, sum)
   int online;                                     // EXP: statistics wanted, references may be outgrown
@@ -98,6 +101,11 @@ struct HeadParams {
   int32_t* status_word;
 };
 
+// What W's column of the target is taken away with: up (1 - q_y).  A call that gives the loss has it from the sum without the
+// target, however near to 1 the target's probability is; a backward call has lse.
+__device__ __forceinline__ float target_factor(const HeadRows& rows, int row, int online) {
+  return online ? rows.of_target[row] : -rows.up[row] * expm1f(rows.z_target[row] - rows.lse[row]);
+}
 // The unit of dZ: the first row's up, unless it is out of the ordinary.
 __device__ __forceinline__ float dz_unit(const HeadRows& rows) {
   const float u = rows.up[0];
@@ -244,12 +252,12 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
   const int m_rows = p.m_extent > 0 ? p.m_extent : n;
   HeadWork work;
   work.n_m_pairs = (m_rows + 2 * kHM - 1) / (2 * kHM);
-  // a K block of two halves is worked on twice, right after one another
+  // a K block is worked on once for each term, right after one another
   work.n_kb = ((p.k_extent > 0 ? p.k_extent : n) + kHK - 1) / kHK;
   work.kb_per_split = p.k_extent > 0 ? p.kb_per_split : (work.n_kb + p.split - 1) / p.split;
   work.chunk_kb = p.chunk_kb > 0 ? p.chunk_kb : max(work.kb_per_split, 1);
   work.n_chunks = max((min(work.kb_per_split, work.n_kb) + work.chunk_kb - 1) / work.chunk_kb, 1);
-  const int halves = kMode == HEAD_DX || kMode == HEAD_DW ? p.halves : 1;     // ... as the operand of this product
+  const int terms = kMode == HEAD_DX || kMode == HEAD_DW ? p.terms : 1;     // ... as the operand of this product
   const bool wide = p.tn > 256;
   const int n_stages = p.stages, stage_bytes = p.stage_bytes;
   const CUtensorMap* map_a = kMode != HEAD_DX && n < p.T ? &maps.a_packed : &maps.a;
@@ -270,13 +278,13 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
       const bool has_box = bi >= 0 && bi < boxes;
       const int at = p.n_first + n0 + (bi < boxes_a ? (int)rank * ca + bi * 64 : wa + (int)rank * cb + (bi - boxes_a) * 64);
       const int m0 = (t.m_pair * 2 + (int)rank) * kHM;
-      const int n_blk = t.n_blk * halves;
+      const int n_blk = t.n_blk * terms;
       for (int b = 0; b < n_blk; ++b) {
         if (CWL_WITHHELD(p) && i == 0 && b == n_blk - 1) { ok = false; break; }
         const bool step_ok = mbar_wait(empty_bar(s), ph ^ 1u, abort_flag);
         if (!__all_sync(0xffffffffu, step_ok)) { ok = false; break; }
-        const int k = (t.kb0 + (halves == 2 ? b >> 1 : b)) * kHK;
-        const int second = halves == 2 && (b & 1) ? p.half_at : 0;
+        const int block = terms == 1 ? b : b / terms;
+        const int k = (t.kb0 + block) * kHK, second = (b - block * terms) * p.term_at;
         const uint32_t sa = base + s * stage_bytes, sb = sa + kHLeft, full = leader_full0 + 8u * s;
         if (lane == 0) {
           if (rank == 0) mbar_expect_tx(full_bar(s), tx);
@@ -317,7 +325,7 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
         const int wa = min(wt, 256), wb = wt - wa;
         const uint32_t idesc_a = pair_idesc(wa, kLeftMn, kRightMn), idesc_b = pair_idesc(wb > 0 ? wb : 32, kLeftMn, kRightMn);
         const uint64_t second = (uint64_t)((((wa >> 1) + 63) >> 6) * kHBox) >> 4;
-        const int n_blk = t.n_blk * halves;
+        const int n_blk = t.n_blk * terms;
         if (n_blk <= 0) continue;                 // nothing to add up: the epilogue takes zeros
         const int slot = wide ? 0 : (int)(local & 1u);
         const uint32_t use = wide ? local : local >> 1;
@@ -446,7 +454,7 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
         float m = ref, sum = 0.f;                 // STATS, EXP: the sum so far, relative to m
         auto take = [&](int c, float (&v)[64]) {  // columns [c, c + 64) of the tile
           const int left = live ? cols - c : 0;
-          if ((kMode == HEAD_STATS || (kMode == HEAD_EXP && p.online)) && (unsigned)(y - c) < 64u) {
+          if ((kMode == HEAD_STATS || kMode == HEAD_EXP) && (unsigned)(y - c) < 64u) {
 #pragma unroll
             for (int j = 0; j < 64; ++j)
               if (j == y - c) p.rows.z_target[row] = v[j];
@@ -465,6 +473,10 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
               atomicOr(p.rows.above + (int64_t)row * p.rows.above_words + (chunk >> 5), 1u << (chunk & 31));
               p.rows.above_ref[(int64_t)row * p.rows.chunks + chunk] = top;
             }
+          }
+          if (kMode == HEAD_EXP && (unsigned)(y - c) < 64u) {      // the target stays out of E and of the sum
+#pragma unroll
+            for (int j = 0; j < 64; ++j) v[j] = j == y - c ? -INFINITY : v[j];
           }
           const float shift = own * kLog2e;
           float part = 0.f;
@@ -487,15 +499,15 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
             for (int j = 0; j < 64; ++j) v[j] = j < left ? v[j] * up : 0.f;
           }
 #pragma unroll 1
-          for (int part_of = 0; part_of < p.halves; ++part_of) {
+          for (int term = 0; term < p.terms; ++term) {
             __syncwarp();                         // every lane has read what was staged before
             stage_bf16_row(buf, lane, v);
-            if (p.halves == 2) {
+            if (p.terms > 1) {
 #pragma unroll
               for (int j = 0; j < 64; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
             }
             __syncwarp();
-            uint8_t* first = reinterpret_cast<uint8_t*>(p.dz + (int64_t)row0 * p.dz_ld + n0 + c + part_of * p.half_at);
+            uint8_t* first = reinterpret_cast<uint8_t*>(p.dz + (int64_t)row0 * p.dz_ld + n0 + c + term * p.term_at);
             store_staged(buf, lane, 128, 1, 2, [&](int r) { return first + (int64_t)r * p.dz_ld * 2; });
           }
         };
@@ -524,8 +536,8 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
         const int mine = !live ? -1 : kMode == HEAD_DX && n < p.T ? p.rows.row[row] : row;
         const bool from_e = kMode == HEAD_DX && p.wy != nullptr;
         const float alpha = from_e && p.acc_in && t.chunk == 0 && live ? p.rows.alpha[row] : 1.f;
-        const float up = from_e && live ? p.rows.up[row] : 0.f;
-        const float scale = from_e ? (live ? p.rows.scale[row] : 0.f) : n > 0 ? dz_unit(p.rows) : 1.f;
+        const float up = from_e && live && !keep ? target_factor(p.rows, row, p.online) : 0.f;
+        const float scale = from_e ? (live && !keep ? p.rows.scale[row] : 0.f) : n > 0 ? dz_unit(p.rows) : 1.f;
         const uint32_t* wy = p.wy + ((int64_t)m_tile * p.acc_groups * 2 + n0 / 2) * kHM + quad * 32 + lane;
         const int chunk = keep || p.out_f32 ? 32 : 64;
 #pragma unroll 1
@@ -809,7 +821,7 @@ struct MergeParams {
   const float2* part;
   int n_part, rows_alloc, last;
   __nv_bfloat16* dz; int64_t dz_ld;
-  int width, halves, half_at;
+  int width, terms, term_at;
   int chunk_cols;                                 // columns that share a reference
   const float* weight; float* loss; float* lse;
 };
@@ -836,11 +848,13 @@ __global__ void __launch_bounds__(kFinishThreads) head_merge_kernel(const MergeP
       rows.ref[row] = m;
       rows.sum[row] = sum;
       if (p.last) {
-        const float l = m + logf(sum);
+        const float z = rows.z_target[row], total = sum + exp2_fast((z - m) * kLog2e), up = rows.up[row];
+        const float l = m + logf(total);
         const int t = rows.row[row];
         if (p.lse != nullptr) p.lse[t] = l;
-        p.loss[t] = (p.weight != nullptr ? p.weight[t] : 1.f) * (l - rows.z_target[row]);
-        rows.scale[row] = rows.up[row] / sum;
+        p.loss[t] = (p.weight != nullptr ? p.weight[t] : 1.f) * (l - z);
+        rows.scale[row] = up / total;
+        rows.of_target[row] = up * (sum / total);
       }
     }
   }
@@ -853,11 +867,13 @@ __global__ void __launch_bounds__(kFinishThreads) head_merge_kernel(const MergeP
       const bool above = rows.above[at * rows.above_words + (chunk >> 5)] >> (chunk & 31) & 1u;
       const float f = exp2_fast(((above ? rows.above_ref[at * rows.chunks + chunk] : old_ref[r]) - new_ref[r]) * kLog2e);
       __nv_bfloat16* e = p.dz + at * p.dz_ld + c;
-      float x = __bfloat162float(e[0]);
-      if (p.halves == 2) x += __bfloat162float(e[p.half_at]);
+      float x = 0.f;
+      for (int k = p.terms - 1; k >= 0; --k) x += __bfloat162float(e[k * p.term_at]);
       x *= f;
-      e[0] = __float2bfloat16_rn(x);
-      if (p.halves == 2) e[p.half_at] = __float2bfloat16_rn(x - __bfloat162float(e[0]));
+      for (int k = 0; k < p.terms; ++k) {
+        e[k * p.term_at] = __float2bfloat16_rn(x);
+        x -= __bfloat162float(e[k * p.term_at]);
+      }
     }
     __syncthreads();
     for (int w = threadIdx.x; w < rows.above_words; w += kFinishThreads) rows.above[at * rows.above_words + w] = 0u;
@@ -942,7 +958,7 @@ head_gather_ordered_kernel(HeadRows rows, const __nv_bfloat16* W, int64_t ldw, i
 // A block takes 32 columns of a 128-row tile.
 constexpr int kSumThreads = 256;
 __global__ void __launch_bounds__(kSumThreads)
-head_sum_kernel(HeadRows rows, int T, int m_extent, int cols, const float* acc, int groups, int split, const uint32_t* wy,
+head_sum_kernel(HeadRows rows, int T, int online, int m_extent, int cols, const float* acc, int groups, int split, const uint32_t* wy,
                 void* out, int64_t ld, int f32) {
   __shared__ float tile[kHM][33];
   pdl_launch_dependents();
@@ -973,7 +989,7 @@ head_sum_kernel(HeadRows rows, int T, int m_extent, int cols, const float* acc, 
     float4 s = sums[e];
     if (col0 + g * 4 < cols && row < m_rows) {
       if (wy != nullptr) {
-        const float f = rows.scale[row], up = rows.up[row];
+        const float f = rows.scale[row], up = target_factor(rows, row, online);
         const uint32_t* w = wy + ((int64_t)m_tile * groups * 2 + col0 / 2 + g * 2) * kHM + r;
         const uint32_t x = w[0], y = w[kHM];
         s.x = s.x * f - up * __uint_as_float(x << 16); s.y = s.y * f - up * __uint_as_float(x & 0xFFFF0000u);
@@ -1025,8 +1041,8 @@ HeadPlan head_plan(int m_rows, int cols, int n_kb, bool may_split, int most_tn, 
 constexpr int kOneRowEach = 592;                        // rows up to which finishing takes a block a row: four blocks an SM
 constexpr size_t kPieceBytes = (size_t)256 << 20;       // E or dZ of a piece of the vocabulary
 constexpr int kPieceMin = 2048;
-int head_piece(int rows_alloc, int V, int halves) {
-  int64_t most = (int64_t)(kPieceBytes / 2 / halves) / rows_alloc / 512 * 512;
+int head_piece(int rows_alloc, int V, int terms) {
+  int64_t most = (int64_t)(kPieceBytes / 2 / terms) / rows_alloc / 512 * 512;
   if (most < kPieceMin) most = kPieceMin;
   const int pieces = (int)((V + most - 1) / most);
   return ceil_div(ceil_div(V, pieces), 512) * 512;
@@ -1034,10 +1050,9 @@ int head_piece(int rows_alloc, int V, int halves) {
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-// How a call is carried out, and where its arrays lie in the workspace.  `halves` is 2 for fp32 gradients; the size of the
-// workspace is that of the larger of both.
+// How a call is carried out, and where its arrays lie in the workspace, whose size is that of the largest way.
 struct HeadLayout {
-  int rows_alloc, piece, pieces, halves;
+  int rows_alloc, piece, pieces, terms;
   int few;                                              // logits by head_few_kernel
   int stats_pass;                                       // a product for lse alone comes first
   int logit_chunk;                                      // K blocks of the logits' products that are summed in the tensor memory, 0 = all
@@ -1047,11 +1062,12 @@ struct HeadLayout {
   int dx_groups, dw_groups, above_words, chunks;
   size_t list, part, packed, above, above_ref, wy, dz_at, acc_x, acc_w, total;
 };
-constexpr int kLists = 9;
-HeadLayout head_layout(int T, int d, int V, bool forward, bool want_dx, bool want_dw, int halves) {
+constexpr int kLists = 10;
+HeadLayout head_layout(int T, int d, int V, bool forward, bool want_dx, bool want_dw, bool f32) {
   HeadLayout l = {};
   l.rows_alloc = (int)(((int64_t)T + 255) / 256 * 256);
-  l.halves = halves;
+  const int terms = !f32 ? 1 : T <= kThreeTermRows ? 3 : 2;
+  l.terms = terms;
   const bool grads = want_dx || want_dw;
   l.from_e = want_dx && !want_dw;
   l.stats_pass = forward && !l.from_e;
@@ -1060,7 +1076,7 @@ HeadLayout head_layout(int T, int d, int V, bool forward, bool want_dx, bool wan
   const int k_d = ceil_div(d, kHK), k_t = ceil_div(T, kHK);
   l.packed_ld = (d + 7) / 8 * 8;
   l.few = T <= kFewRows;
-  l.piece = grads ? head_piece(l.rows_alloc, V, halves) : 0;
+  l.piece = grads ? head_piece(l.rows_alloc, V, terms) : 0;
   l.pieces = grads ? ceil_div(V, l.piece) : 0;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += align256(bytes); return here; };
@@ -1079,17 +1095,17 @@ HeadLayout head_layout(int T, int d, int V, bool forward, bool want_dx, bool wan
   l.part = take(parts * 2 * l.rows_alloc * 8);
   l.packed = take((size_t)l.rows_alloc * l.packed_ld * 2);
   if (grads) {
-    l.dz_at = take((size_t)l.rows_alloc * l.piece * halves * 2);
+    l.dz_at = take((size_t)l.rows_alloc * l.piece * terms * 2);
     if (want_dx) {
-      l.dx = head_plan(T, d, l.piece / kHK * halves, true, kHMaxTile, 32);
+      l.dx = head_plan(T, d, l.piece / kHK * terms, true, kHMaxTile, 32);
       l.dx_groups = ceil_div(d, 4);
       // fp32 gradients pass through the sums at every chunk
-      if (l.pieces > 1 || l.dx.split > 1 || halves == 2) l.acc_x = take((size_t)l.dx.split * l.rows_alloc * l.dx_groups * 16);
+      if (l.pieces > 1 || l.dx.split > 1 || terms > 1) l.acc_x = take((size_t)l.dx.split * l.rows_alloc * l.dx_groups * 16);
     }
     if (want_dw) {
-      l.dw = head_plan(d, l.piece, k_t * halves, true, kHMaxTile, 32);
+      l.dw = head_plan(d, l.piece, k_t * terms, true, kHMaxTile, 32);
       l.dw_groups = l.piece / 4;
-      if (l.dw.split > 1 || halves == 2) l.acc_w = take((size_t)l.dw.split * ceil_div(d, 2 * kHM) * 2 * kHM * l.dw_groups * 16);
+      if (l.dw.split > 1 || terms > 1) l.acc_w = take((size_t)l.dw.split * ceil_div(d, 2 * kHM) * 2 * kHM * l.dw_groups * 16);
     }
     if (l.from_e) {
       l.wy = take((size_t)l.rows_alloc * l.dx_groups * 8);
@@ -1137,9 +1153,9 @@ extern "C" size_t cwl_head_loss_workspace_bytes(int32_t T, int32_t d, int32_t V,
   using namespace cwl;
   if (T <= 0 || d <= 0 || V <= 0 || T > kHeadMaxRows || V > kHeadMaxRows || d > kHeadMaxWidth) return 0;
   size_t most = 0;
-  for (int halves = 1; halves <= 2; ++halves) {
+  for (int f32 = 0; f32 <= 1; ++f32) {
     for (int forward = 0; forward <= 1; ++forward) {
-      const size_t n = head_layout(T, d, V, forward != 0, want_dx != 0, want_dw != 0, halves).total;
+      const size_t n = head_layout(T, d, V, forward != 0, want_dx != 0, want_dw != 0, f32 != 0).total;
       if (n > most) most = n;
     }
   }
@@ -1174,7 +1190,7 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
   if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
       workspace_bytes < cwl_head_loss_workspace_bytes(T, d, V, dX != nullptr, dW != nullptr))
     return CWL_ERR_WORKSPACE;
-  const HeadLayout l = head_layout(T, d, V, forward, dX != nullptr, dW != nullptr, es == 4 ? 2 : 1);
+  const HeadLayout l = head_layout(T, d, V, forward, dX != nullptr, dW != nullptr, es == 4);
   const bool online = l.from_e && forward;
   // a sector of 32 bytes for each number of the targets' columns, or all of W
   const bool in_order = (int64_t)T * 32 > (int64_t)V * 2;
@@ -1186,8 +1202,8 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
   rows.row = reinterpret_cast<int*>(list(0));
   rows.target = reinterpret_cast<int*>(list(1));
   rows.up = list(2); rows.lse = list(3); rows.z_target = list(4);
-  rows.ref = list(5); rows.sum = list(6); rows.alpha = list(7); rows.scale = list(8);
-  static_assert(kLists == 9, "arrays of a number a row");
+  rows.ref = list(5); rows.sum = list(6); rows.alpha = list(7); rows.scale = list(8); rows.of_target = list(9);
+  static_assert(kLists == 10, "arrays of a number a row");
   rows.above = reinterpret_cast<unsigned*>(ws + l.above);
   rows.above_ref = reinterpret_cast<float*>(ws + l.above_ref);
   rows.above_words = l.above_words;
@@ -1196,7 +1212,7 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
   __nv_bfloat16* dz = reinterpret_cast<__nv_bfloat16*>(ws + l.dz_at);
   float2* part = reinterpret_cast<float2*>(ws + l.part);
   uint32_t* wy = l.from_e ? reinterpret_cast<uint32_t*>(ws + l.wy) : nullptr;
-  const int64_t dz_ld = (int64_t)l.piece * l.halves;
+  const int64_t dz_ld = (int64_t)l.piece * l.terms;
   const bool chained = !stream_is_capturing(st);
 
   RowsParams r = {};
@@ -1226,7 +1242,7 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
   }
 
   HeadParams p = {};
-  p.rows = rows; p.T = T; p.rows_alloc = l.rows_alloc; p.split = 1; p.halves = 1;
+  p.rows = rows; p.T = T; p.rows_alloc = l.rows_alloc; p.split = 1; p.terms = 1;
   p.part = part;
   p.wait_limit_ns = training_wait_limit();
   p.withhold = training_withhold();
@@ -1257,13 +1273,13 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
     HeadParams q = p;
     q.n_extent = width; q.n_first = first; q.k_extent = d; q.kb_per_split = ceil_div(d, kHK); q.chunk_kb = l.logit_chunk;
     q.tn = l.dz.tn; q.n_cols = ceil_div(width, q.tn);
-    q.dz = dz; q.dz_ld = dz_ld; q.halves = l.halves; q.half_at = l.piece; q.online = online;
+    q.dz = dz; q.dz_ld = dz_ld; q.terms = l.terms; q.term_at = l.piece; q.online = online;
     if (l.from_e) {
       CWL_CUDA_TRY(l.few ? launch_few<HEAD_EXP>(few, q, T, chained, st) : launch_logits<HEAD_EXP>(logits, q, T, chained, st));
       if (online) {
         MergeParams m = {};
         m.rows = rows; m.part = part; m.n_part = l.few ? q.n_cols : 2 * q.n_cols; m.chunk_cols = l.few ? q.tn : 64; m.rows_alloc = l.rows_alloc; m.last = last;
-        m.dz = dz; m.dz_ld = dz_ld; m.width = width; m.halves = l.halves; m.half_at = l.piece;
+        m.dz = dz; m.dz_ld = dz_ld; m.width = width; m.terms = l.terms; m.term_at = l.piece;
         m.weight = weight; m.loss = loss; m.lse = lse;
         CWL_CUDA_TRY(T <= kOneRowEach ? launch_chained(chained, head_merge_kernel<1>, dim3((unsigned)T), dim3(kFinishThreads), 0, st, m)
                                       : launch_chained(chained, head_merge_kernel<32>, dim3((unsigned)ceil_div(T, 32)), dim3(kFinishThreads), 0, st, m));
@@ -1271,16 +1287,16 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
     } else {
       CWL_CUDA_TRY(launch_logits<HEAD_DZ>(logits, q, T, chained, st));
     }
-    // where E / dZ is two numbers, columns [width, piece) of the first are never read: its last block is stored whole
-    const int64_t stored = l.halves == 2 ? l.piece + width : width;
+    // where E / dZ is several numbers, the last block of each is stored whole, and DX reads no further
+    const int64_t stored = (int64_t)(l.terms - 1) * l.piece + width;
     if (dX != nullptr) {
       q = p;
-      q.n_extent = d; q.k_extent = width; q.k_first = first; q.halves = l.halves; q.half_at = l.piece;
-      q.chunk_kb = l.halves == 2 ? kChunkBlocks : 0;
+      q.n_extent = d; q.k_extent = width; q.k_first = first; q.terms = l.terms; q.term_at = l.piece;
+      q.chunk_kb = l.terms > 1 ? kChunkBlocks / l.terms : 0;
       q.tn = l.dx.tn; q.n_cols = l.dx.n_cols; q.split = l.dx.split; q.kb_per_split = ceil_div(ceil_div(width, kHK), q.split);
       q.acc = reinterpret_cast<float*>(ws + l.acc_x); q.acc_groups = l.dx_groups;
       q.acc_in = piece > 0; q.acc_out = q.split > 1 || !last;
-      q.wy = wy;
+      q.wy = wy; q.online = online;
       q.out = dX; q.out_ld = lddx; q.out_f32 = es == 4;
       q.out_vec = aligned16(dX) && (T == 1 || lddx * es % 16 == 0);
       if (!encode_map(&maps.a, dz, stored, l.rows_alloc, dz_ld, kHK, kHM) || !encode_map(&maps.b, W, V, d, uw, kHK, 64)) return CWL_ERR_CUDA;
@@ -1288,13 +1304,13 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
       CWL_CUDA_TRY((launch_head<HEAD_DX, false>(maps, q, T, chained, st)));
       if (last && q.split > 1)
         CWL_CUDA_TRY(launch_chained(chained, head_sum_kernel, dim3((unsigned)ceil_div(T, kHM), (unsigned)ceil_div(d, 32)), dim3(kSumThreads), 0, st,
-                                    rows, T, 0, d, static_cast<const float*>(q.acc), q.acc_groups, q.split, static_cast<const uint32_t*>(wy), dX, lddx,
+                                    rows, T, online ? 1 : 0, 0, d, static_cast<const float*>(q.acc), q.acc_groups, q.split, static_cast<const uint32_t*>(wy), dX, lddx,
                                     q.out_f32));
     }
     if (dW != nullptr) {
       q = p;
-      q.m_extent = d; q.n_extent = width; q.halves = l.halves; q.half_at = l.piece;
-      q.chunk_kb = l.halves == 2 ? kChunkBlocks : 0;
+      q.m_extent = d; q.n_extent = width; q.terms = l.terms; q.term_at = l.piece;
+      q.chunk_kb = l.terms > 1 ? kChunkBlocks / l.terms : 0;
       q.tn = l.dw.tn; q.n_cols = ceil_div(width, q.tn); q.split = l.dw.split;
       q.acc = reinterpret_cast<float*>(ws + l.acc_w); q.acc_groups = l.dw_groups; q.acc_out = q.split > 1;
       q.out = static_cast<uint8_t*>(dW) + (size_t)first * es; q.out_ld = lddw; q.out_f32 = es == 4;
@@ -1305,7 +1321,7 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
       CWL_CUDA_TRY((launch_head<HEAD_DW, false>(maps, q, d, chained, st)));
       if (q.split > 1)
         CWL_CUDA_TRY(launch_chained(chained, head_sum_kernel, dim3((unsigned)ceil_div(d, kHM), (unsigned)ceil_div(width, 32)), dim3(kSumThreads), 0, st,
-                                    rows, T, d, width, static_cast<const float*>(q.acc), q.acc_groups, q.split, static_cast<const uint32_t*>(nullptr), q.out,
+                                    rows, T, 0, d, width, static_cast<const float*>(q.acc), q.acc_groups, q.split, static_cast<const uint32_t*>(nullptr), q.out,
                                     lddw, q.out_f32));
     }
   }

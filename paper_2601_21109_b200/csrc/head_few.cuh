@@ -244,24 +244,33 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll
-      for (int j = 0; j < kRows; ++j) z[j] = there && j < n ? exp2_fast(fmaf(z[j], kLog2e, -common[j] * kLog2e)) : 0.f;
+      for (int j = 0; j < kRows; ++j) {
+        // EXP: the target stays out of E and of the sum
+        const bool in = there && j < n && (kMode != HEAD_EXP || targets[j] != col);
+        z[j] = in ? exp2_fast(fmaf(z[j], kLog2e, -common[j] * kLog2e)) : 0.f;
+      }
       if (kMode == HEAD_EXP) {
         if (there) {
           __nv_bfloat16* e = p.dz + col;
 #pragma unroll
           for (int j = 0; j < kRows; ++j) {
             if (j < n) {
-              const __nv_bfloat16 hi = __float2bfloat16_rn(z[j]);
-              *e = hi;
-              if (p.halves == 2) e[p.half_at] = __float2bfloat16_rn(z[j] - __bfloat162float(hi));
+              float left = z[j];
+              for (int term = 0; term < p.terms; ++term) {
+                const __nv_bfloat16 part = __float2bfloat16_rn(left);
+                e[term * p.term_at] = part;
+                left -= __bfloat162float(part);
+              }
               e += p.dz_ld;
             }
           }
         }
-        if (p.halves == 2 && tile == n_tiles - 1) {
+        if (p.terms > 1 && tile == n_tiles - 1) {
           // columns up to the end of the last K block of DX, which reads on there
           const int pad = -p.n_extent & (kHK - 1);
-          for (int i = epi; i < n * pad; i += 256) p.dz[(int64_t)(i / pad) * p.dz_ld + p.n_extent + i % pad] = __float2bfloat16_rn(0.f);
+          for (int i = epi; i < n * pad; i += 256)
+            for (int term = 0; term < p.terms; ++term)
+              p.dz[(int64_t)(i / pad) * p.dz_ld + term * p.term_at + p.n_extent + i % pad] = __float2bfloat16_rn(0.f);
         }
         if (!p.online) {
           asm volatile("bar.sync 1, 256;" ::: "memory");         // before the next tile's maxima

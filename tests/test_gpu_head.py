@@ -43,8 +43,12 @@ def reference(X, W, y, w, dloss=None, lse=None):
     zy = z.gather(1, y.clamp(0, V - 1).long()[:, None])[:, 0]
     up = torch.where(on, w.double() * (1 if dloss is None else dloss.double()), 0.0)
     q = (z - norm[:, None]).exp()
-    dz = q.clone()
-    dz.scatter_add_(1, y.clamp(0, V - 1).long()[:, None], torch.full((len(y), 1), -1.0, dtype=torch.float64, device=z.device))
+    at = y.clamp(0, V - 1).long()[:, None]
+    if lse is None:                                     # 1 - q_y is what the others add up to (64 bits do not hold 1 - 1e-17)
+        dz = q.scatter(1, at, 0.0)
+        dz.scatter_(1, at, -dz.sum(1, keepdim=True))
+    else:
+        dz = q.scatter_add(1, at, torch.full((len(y), 1), -1.0, dtype=torch.float64, device=z.device))
     dz = dz * up[:, None]
     tz = q * (up.abs() * 2.02 * (ez + el))[:, None] + dz.abs() * 2.0 ** -8
     loss = torch.where(on, w.double() * (own - zy), 0.0)
@@ -148,3 +152,34 @@ def test_logits_far_apart(T, d, V, spread, grad):
     W[0, 0] = 100.0
     X[:, 0] = X[:, 0].abs() + 1
     check(X, W, y, w, want_dx=True, grad_dtype=grad)
+
+
+@pytest.mark.parametrize("T,d,V", [(20, 64, 3000), (300, 256, 5000)])
+def test_gradients_of_tokens_that_the_model_is_sure_of(T, d, V):
+    """Where the target's probability is near 1 what is left of dX is small, and its error is relative to that: in one call
+    1 - q_y is a sum of the others, not a difference."""
+    X, W, y, w = operands(11, T, d, V)
+    col = W[:, y.long()].T.float()
+    X.copy_(X * 0.2 + 1.6 * col / col.norm(dim=1, keepdim=True) * torch.linspace(2, 9, T, device="cuda")[:, None])
+    r = reference(X, W, y, w)
+    rest = 1 - torch.exp(-r["loss"] / w.double())
+    assert float(rest.min()) < 1e-3
+    ez = d * 2.0 ** -23 * (X.double().abs() @ W.double().abs()).amax(1)     # of a logit: a relative error of a probability
+    for grad in (torch.bfloat16, torch.float32):
+        o = cwl.cwl_head_loss(X, W, y, weight=w, want_dx=True, grad_dtype=grad)
+        ref = r["dz"] @ r["W"].T
+        size = (r["dz"].abs() @ r["W"].abs().T)
+        # every term of the sum: its rounding, twice the logits' errors, the fp32 sums; nothing of the size of W_y alone
+        share = 2.0 ** -8 if grad == torch.bfloat16 else 2.0 ** -16
+        tol = size * (share + V * 2.0 ** -23 + 4 * ez[:, None] + 2.0 ** -19) + ref.abs() * (2.0 ** -8 if grad == torch.bfloat16 else 2.0 ** -24)
+        within(o.dX, ref, tol, "dX")
+
+
+@pytest.mark.parametrize("T", [1, 2, 40, 500])
+def test_fp32_gradients_of_few_rows_carry_fp32(T):
+    """One row's dZ rounded to 16 bits would show in a whole column of dW: three numbers keep it to 2^-24."""
+    X, W, y, w = operands(T, T, 320, 2000)
+    o = cwl.cwl_head_loss(X, W, y, weight=w, want_dx=True, want_dw=True, grad_dtype=torch.float32)
+    r = reference(X, W, y, w)
+    for got, ref in ((o.dX, r["dz"] @ r["W"].T), (o.dW, r["x"].T @ r["dz"])):
+        assert float((got.double() - ref).norm() / ref.norm()) <= 4e-6
