@@ -667,6 +667,7 @@ __global__ void __launch_bounds__(kRowsThreads) head_rows_kernel(const RowsParam
   const int first = (int)(first64 < p.T ? first64 : p.T);
   const int last = (int)(first64 + p.per_block < p.T ? first64 + p.per_block : p.T);
   int before = 0, total = 0;
+#pragma unroll 8
   for (int64_t t = tid; t < p.T; t += kRowsThreads) {
     const int c = row_counts(p, (int)t) ? 1 : 0;
     total += c;
@@ -720,30 +721,34 @@ __global__ void __launch_bounds__(kRowsThreads) head_rows_kernel(const RowsParam
     const int rows_here = (int)(last - t0 < kRowsThreads ? last - t0 : kRowsThreads);
     for (int r = warp; r < rows_here; r += kRowsThreads / 32) {
       const int to = counts[r];
-      if (to >= 0 && p.online && p.reference) {
+      const bool pack = total < p.T, refer = p.online && p.reference;
+      if (to >= 0 && (pack || refer)) {
         const __nv_bfloat16* x = p.X + (t0 + r) * p.ldx;
+        __nv_bfloat16* out = p.packed + (int64_t)to * p.packed_ld;
         float z = 0.f;
-        const int vectors = min(p.d, kRowsColumn) / 8;
-#pragma unroll 4
-        for (int j = lane; j < vectors; j += 32) {
-          const uint4 q = reinterpret_cast<const uint4*>(x)[j], c = reinterpret_cast<const uint4*>(column)[j];
-          const uint32_t a[4] = {q.x, q.y, q.z, q.w}, b[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll 8
+        for (int j = lane; j < p.d / 8; j += 32) {
+          const uint4 q = __ldg(reinterpret_cast<const uint4*>(x) + j);
+          if (pack) reinterpret_cast<uint4*>(out)[j] = q;
+          if (refer && j < kRowsColumn / 8) {
+            const uint4 c = reinterpret_cast<const uint4*>(column)[j];
+            const uint32_t a[4] = {q.x, q.y, q.z, q.w}, b[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            z = fmaf(__uint_as_float(a[k] << 16), __uint_as_float(b[k] << 16), z);
-            z = fmaf(__uint_as_float(a[k] & 0xFFFF0000u), __uint_as_float(b[k] & 0xFFFF0000u), z);
+            for (int k = 0; k < 4; ++k) {
+              z = fmaf(__uint_as_float(a[k] << 16), __uint_as_float(b[k] << 16), z);
+              z = fmaf(__uint_as_float(a[k] & 0xFFFF0000u), __uint_as_float(b[k] & 0xFFFF0000u), z);
+            }
           }
         }
-        for (int j = vectors * 8 + lane; j < p.d; j += 32) z = fmaf(__bfloat162float(x[j]), __bfloat162float(p.W[(int64_t)j * p.ldw]), z);
-        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-        if (lane == 0) p.rows.ref[to] = fabsf(z) < 1e30f ? z : 0.f;
-      }
-      if (to >= 0 && total < p.T) {
-        const __nv_bfloat16* from = p.X + (t0 + r) * p.ldx;
-        __nv_bfloat16* out = p.packed + (int64_t)to * p.packed_ld;
-#pragma unroll 8
-        for (int j = lane; j < p.d / 8; j += 32) reinterpret_cast<uint4*>(out)[j] = reinterpret_cast<const uint4*>(from)[j];
-        for (int j = p.d / 8 * 8 + lane; j < p.d; j += 32) out[j] = from[j];
+        if (pack)
+          for (int j = p.d / 8 * 8 + lane; j < p.d; j += 32) out[j] = x[j];
+        if (refer) {
+          // what the column in shared memory does not hold, and the elements after the last eight
+          for (int j = min(p.d / 8 * 8, kRowsColumn) + lane; j < p.d; j += 32)
+            z = fmaf(__bfloat162float(x[j]), __bfloat162float(p.W[(int64_t)j * p.ldw]), z);
+          for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+          if (lane == 0) p.rows.ref[to] = fabsf(z) < 1e30f ? z : 0.f;
+        }
       } else if (to == -1 && p.dX != nullptr) {
         uint8_t* out = reinterpret_cast<uint8_t*>(p.dX) + (t0 + r) * p.lddx * p.dx_elem;
         for (int j = lane; j < p.d; j += 32) {
@@ -1223,7 +1228,7 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
   r.dX = dX; r.lddx = lddx; r.dx_elem = es;
   r.packed = packed; r.packed_ld = l.packed_ld; r.rows = rows; r.backward = !forward; r.online = online; r.reference = in_order;
   r.status_word = status_word;
-  int blocks = ceil_div(T, 16);
+  int blocks = ceil_div(T, 8);
   if (blocks > 592) blocks = 592;
   r.per_block = ceil_div(T, blocks);
   CWL_CUDA_TRY(launch_chained(chained, head_rows_kernel, dim3((unsigned)blocks), dim3(kRowsThreads), 0, st, r));
