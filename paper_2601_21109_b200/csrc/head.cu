@@ -431,6 +431,11 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
                 }
               }
             }
+          } else if (kMode == HEAD_DZ) {          // rows that are not there are written as zeros all the same
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int j = 0; j < 64; ++j) held[k][j] = 0.f;
           }
           if (t.chunk + 1 < work.n_chunks) {
             tc_fence_before();
@@ -439,7 +444,7 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
             continue;
           }
         }
-        float up = 1.f, ref = -INFINITY;
+        float up = 0.f, ref = kMode == HEAD_STATS ? -INFINITY : 0.f;
         int y = -1;
         if (live) {
           y = p.rows.target[row] - (p.n_first + n0);
@@ -452,51 +457,56 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
           }
         }
         float m = ref, sum = 0.f;                 // STATS, EXP: the sum so far, relative to m
-        auto take = [&](int c, float (&v)[64]) {  // columns [c, c + 64) of the tile
-          const int left = live ? cols - c : 0;
-          if ((kMode == HEAD_STATS || kMode == HEAD_EXP) && (unsigned)(y - c) < 64u) {
+        auto take = [&](int c, float (&v)[64]) {  // columns [c, c + 64) of the tile; sums and maxima in four chains
+          if (cols - c < 64) {
+#pragma unroll
+            for (int j = 0; j < 64; ++j) v[j] = j < cols - c ? v[j] : -INFINITY;
+          }
+          const bool mine = (unsigned)(y - c) < 64u;
+          if ((kMode == HEAD_STATS || kMode == HEAD_EXP) && mine) {
 #pragma unroll
             for (int j = 0; j < 64; ++j)
               if (j == y - c) p.rows.z_target[row] = v[j];
           }
           float own = ref;                        // reference of these columns
           if (kMode == HEAD_STATS || (kMode == HEAD_EXP && p.online)) {
-            float top = -INFINITY;
+            float t4[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-            for (int j = 0; j < 64; ++j) top = j < left ? fmaxf(top, v[j]) : top;
+            for (int j = 4; j < 64; ++j) t4[j & 3] = fmaxf(t4[j & 3], v[j]);
+            const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
             if (kMode == HEAD_STATS) {
               own = top > m ? top : m;
               if (own == -INFINITY) own = 0.f;
-            } else if (top > ref + kAbove) {
+            } else if (live && top > ref + kAbove) {
               own = top;
               const int chunk = (n0 + c) >> 6;    // tiles start at multiples of 64 here
               atomicOr(p.rows.above + (int64_t)row * p.rows.above_words + (chunk >> 5), 1u << (chunk & 31));
               p.rows.above_ref[(int64_t)row * p.rows.chunks + chunk] = top;
             }
           }
-          if (kMode == HEAD_EXP && (unsigned)(y - c) < 64u) {      // the target stays out of E and of the sum
+          if (kMode == HEAD_EXP && mine) {        // the target stays out of E and of the sum
 #pragma unroll
             for (int j = 0; j < 64; ++j) v[j] = j == y - c ? -INFINITY : v[j];
           }
           const float shift = own * kLog2e;
-          float part = 0.f;
+          float p4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int j = 0; j < 64; ++j) {
-            const float e = j < left ? exp2_fast(fmaf(v[j], kLog2e, -shift)) : 0.f;
-            v[j] = e;
-            if (kMode != HEAD_DZ) part += e;
+            v[j] = exp2_fast(fmaf(v[j], kLog2e, -shift));
+            if (kMode != HEAD_DZ) p4[j & 3] += v[j];
           }
           if (kMode != HEAD_DZ) {
+            const float part = (p4[0] + p4[1]) + (p4[2] + p4[3]);
             if (own > m) { sum *= exp2_fast((m - own) * kLog2e); m = own; }
             sum += m > own ? part * exp2_fast((own - m) * kLog2e) : part;
             if (kMode == HEAD_STATS) return;
           } else {
-            if ((unsigned)(y - c) < 64u) {
+            if (mine) {
 #pragma unroll
               for (int j = 0; j < 64; ++j) v[j] -= j == y - c ? 1.f : 0.f;
             }
 #pragma unroll
-            for (int j = 0; j < 64; ++j) v[j] = j < left ? v[j] * up : 0.f;
+            for (int j = 0; j < 64; ++j) v[j] *= up;         // rows that are not there: 0
           }
 #pragma unroll 1
           for (int term = 0; term < p.terms; ++term) {
@@ -512,7 +522,7 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
           }
         };
         if (kSums) {
-          if (row0 < m_rows || kMode != HEAD_STATS) {
+          if (row0 < m_rows || kMode == HEAD_DZ) {
 #pragma unroll
             for (int k = 0; k < 2; ++k)
               if ((2 * k + chalf) * 64 < cols) take((2 * k + chalf) * 64, held[k]);
