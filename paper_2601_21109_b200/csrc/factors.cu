@@ -735,48 +735,105 @@ __global__ void __launch_bounds__(kBigThreads) big_product_kernel(const __grid_c
 
 // ------------------------------------------------------------------------------------------------------------ APPLY
 // O = Q U over 64 short-side rows and 128 long-side elements.  Outputs of a thread: 8 x 4 with the lanes along the rows of the
-// factor as they lie in memory, whichever side that is; two neighbours of the long side advance in one instruction, with each
-// number of Q twice in shared memory.
+// factor as they lie in memory, whichever side that is.
 constexpr int kApplyThreads = 256;
 constexpr int kApplyK = 32;
-constexpr int kApplyRing = 2;
-constexpr int kApplyLdX = kApplyLong + 4, kApplyLdQ = 2 * kApplyShort + 4;
-constexpr int kApplyRaw = kApplyK * kApplyLong;    // elements of a chunk
-
-__device__ __forceinline__ void fma_two(float2& d, const float2& a, const float2& b) {
-  unsigned long long x = *reinterpret_cast<const unsigned long long*>(&d);
-  asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(x) : "l"(*reinterpret_cast<const unsigned long long*>(&a)), "l"(*reinterpret_cast<const unsigned long long*>(&b)));
-  d = *reinterpret_cast<float2*>(&x);
-}
+constexpr int kApplyLdX = kApplyLong + 4, kApplyLdQ = kApplyShort + 4;
 
 template <bool kTall, bool kStep, int kElem>
-__device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& f, const float* q, int long0, int short0, uint8_t* raw) {
+__device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& f, const float* q, int long0, int short0, float* xs, float* qs) {
   const int R = short_side(f), n = long_side(f), tid = threadIdx.x;
-  const bool wide = wide_rows(f.u, f.ldu, kElem) && (!kStep || wide_rows(f.m, f.ldm, 4));
-  const bool vec_u = vec_rows(f.u, f.ldu, kElem), vec_m = kStep && vec_rows(f.m, f.ldm, 4), vec_q = (R & 3) == 0, bf16 = a.in_type == CWL_BF16;
-  float* xs = reinterpret_cast<float*>(raw);
-  float* qs = xs + kApplyK * kApplyLdX;
-  uint8_t* ring = raw + (kApplyK * kApplyLdX + kApplyK * kApplyLdQ) * 4;
-  constexpr int kSlot = kApplyRaw * (kElem + (kStep ? 4 : 0));
-  // a chunk as it lies in memory
-  constexpr int kRows = kTall ? kApplyLong : kApplyK, kRun = kTall ? kApplyK : kApplyLong;
-  const RawCopy<kRows, kRun, kElem, kApplyThreads> copy_u(f.u, f.ldu, kTall ? long0 : 0, kTall ? 0 : long0);
-  const RawCopy<kRows, kRun, 4, kApplyThreads> copy_m(f.m, f.ldm, kTall ? long0 : 0, kTall ? 0 : long0);
-  auto start = [&](int k0, int slot) {
-    if (wide && k0 < R) {
-      copy_u.start(ring + slot * kSlot, kTall ? 0 : k0, kTall ? k0 : 0, f.rows, f.cols);
-      if (kStep) copy_m.start(ring + slot * kSlot + kApplyRaw * kElem, kTall ? 0 : k0, kTall ? k0 : 0, f.rows, f.cols);
-    }
-    copies_commit();
-  };
-#pragma unroll
-  for (int i = 0; i < kApplyRing; ++i) start(i * kApplyK, i);
-
-  // this thread's outputs: short side s0.., long side l0..; at_output(i): its i-th four neighbours of a row of the factor
+  const bool vec_u = vec_rows(f.u, f.ldu, kElem), vec_m = kStep && vec_rows(f.m, f.ldm, 4);
+  const bool vec_q = (R & 3) == 0;
+  // this thread's outputs: short side s0.., long side l0..
   constexpr int kS = kTall ? 4 : 8, kL = kTall ? 8 : 4;
   const int s0 = kTall ? (tid & 15) * 4 : (tid >> 5) * 8, l0 = kTall ? (tid >> 4) * 8 : (tid & 31) * 4;
+  float acc[kS][kL];
+#pragma unroll
+  for (int i = 0; i < kS; ++i)
+#pragma unroll
+    for (int j = 0; j < kL; ++j) acc[i][j] = 0.f;
+
+  // What comes next is loaded raw, all loads together, and becomes U when it is put into shared memory.
+  float4 x[4], mom[kStep ? 4 : 1], y[2];
+  const bool inside = vec_u && (!kStep || vec_m) && (kTall ? (R & 3) == 0 : (n & 3) == 0);
+  auto place = [&](int k0, int i, int& r, int& c) {
+    if (kTall) { r = long0 + i * 32 + (tid >> 3); c = k0 + (tid & 7) * 4; }      // U [long][short]: eight threads 32 of a row
+    else { r = k0 + i * 8 + (tid >> 5); c = long0 + (tid & 31) * 4; }            // U [short][long]: a warp 128 of a row
+    return r < f.rows ? f.cols - c : 0;
+  };
+  auto fetch = [&](int k0) {
+    int r, c;
+    if (inside) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool there = place(k0, i, r, c) > 0;
+        const int64_t at = (int64_t)r * f.ldu + c;
+        if (kElem == 4) {
+          x[i] = there ? *reinterpret_cast<const float4*>(static_cast<const float*>(f.u) + at) : make_float4(0.f, 0.f, 0.f, 0.f);
+        } else {
+          const float2 q = there ? *reinterpret_cast<const float2*>(static_cast<const uint16_t*>(f.u) + at) : make_float2(0.f, 0.f);
+          x[i].x = q.x;
+          x[i].y = q.y;
+        }
+        if (kStep) mom[kStep ? i : 0] = there ? *reinterpret_cast<const float4*>(f.m + (int64_t)r * f.ldm + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int left = place(k0, i, r, c);
+        x[i] = load_u<false>(a, f, r, c, left, vec_u, vec_m);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {                  // Q is symmetric: its row k is the column wanted
+      const int k = k0 + i * 16 + (tid >> 4), s = short0 + (tid & 15) * 4, left = k < R ? R - s : 0;
+      y[i] = load4(q, (int64_t)k * R + s, CWL_F32, vec_q, left);
+    }
+  };
+  auto made = [&](int i) {                         // U from what was loaded
+    if (!inside) return x[i];
+    const float4 g = raw_four<kElem>(reinterpret_cast<const uint8_t*>(&x[i]), a.in_type == CWL_BF16);
+    if (!kStep) return g;
+    const float4 m = mom[kStep ? i : 0];
+    return step_u(a, g, m);
+  };
+  fetch(0);
+  for (int k0 = 0; k0 < R; k0 += kApplyK) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 u = made(i);
+      if (kTall) {
+        const int l = i * 32 + (tid >> 3), k = (tid & 7) * 4;
+        xs[k * kApplyLdX + l] = u.x; xs[(k + 1) * kApplyLdX + l] = u.y;
+        xs[(k + 2) * kApplyLdX + l] = u.z; xs[(k + 3) * kApplyLdX + l] = u.w;
+      } else {
+        *reinterpret_cast<float4*>(xs + (i * 8 + (tid >> 5)) * kApplyLdX + (tid & 31) * 4) = u;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<float4*>(qs + (i * 16 + (tid >> 4)) * kApplyLdQ + (tid & 15) * 4) = y[i];
+    __syncthreads();
+    if (k0 + kApplyK < R) fetch(k0 + kApplyK);
+#pragma unroll 8
+    for (int k = 0; k < kApplyK; ++k) {
+      float sv[kS], lv[kL];
+#pragma unroll
+      for (int i = 0; i < kS; i += 4) *reinterpret_cast<float4*>(sv + i) = *reinterpret_cast<const float4*>(qs + k * kApplyLdQ + s0 + i);
+#pragma unroll
+      for (int j = 0; j < kL; j += 4) *reinterpret_cast<float4*>(lv + j) = *reinterpret_cast<const float4*>(xs + k * kApplyLdX + l0 + j);
+#pragma unroll
+      for (int i = 0; i < kS; ++i)
+#pragma unroll
+        for (int j = 0; j < kL; ++j) acc[i][j] = fmaf(sv[i], lv[j], acc[i][j]);
+    }
+  }
+
   const int out_type = kStep ? CWL_F32 : a.out_type;
   const bool vec_o = vec_rows(f.out, f.ldo, elem_size(out_type)), vec_l = f.low != nullptr && vec_rows(f.low, f.ldl, 2);
+  const float by = kStep ? -a.lr * f.scale : 1.f;
+  // four neighbours of a row of the factor at a time; a step's masters all come in before the first is written back
   auto at_output = [&](int i, int& r, int& c) {
     r = kTall ? long0 + l0 + i : short0 + s0 + i;
     c = kTall ? short0 + s0 : long0 + l0;
@@ -784,86 +841,25 @@ __device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& 
   };
   int r, c;
   float4 p[kStep ? 8 : 1];
-  if (kStep) {                                     // a step's masters, on their way meanwhile
+  if (kStep) {
     const bool whole = vec_o && (f.cols & 3) == 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int left = at_output(i, r, c);
       const float* at = static_cast<const float*>(f.out) + (int64_t)r * f.ldo + c;
-      if (whole) p[i] = left > 0 ? *reinterpret_cast<const float4*>(at) : make_float4(0.f, 0.f, 0.f, 0.f);
-      else p[i] = load4(at, 0, CWL_F32, vec_o, left);
+      if (whole) p[kStep ? i : 0] = left > 0 ? *reinterpret_cast<const float4*>(at) : make_float4(0.f, 0.f, 0.f, 0.f);
+      else p[kStep ? i : 0] = load4(at, 0, CWL_F32, vec_o, left);
     }
   }
-  float2 acc[kS][kL / 2];
-#pragma unroll
-  for (int i = 0; i < kS; ++i)
-#pragma unroll
-    for (int j = 0; j < kL / 2; ++j) acc[i][j] = make_float2(0.f, 0.f);
-
-  int slot = 0;
-  for (int k0 = 0; k0 < R; k0 += kApplyK) {
-    float4 y[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {                  // Q is symmetric: its row k is the column wanted
-      const int k = k0 + i * 16 + (tid >> 4), s = short0 + (tid & 15) * 4, left = k < R ? R - s : 0;
-      y[i] = load4(q, (int64_t)k * R + s, CWL_F32, vec_q, left);
-    }
-    copies_wait<kApplyRing - 1>();
-    __syncthreads();                               // the chunk has arrived; the one before is done with
-    const uint8_t* u_raw = ring + slot * kSlot;
-    const uint8_t* m_raw = u_raw + kApplyRaw * kElem;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = kTall ? i * 32 + (tid & 31) : i * 8 + (tid >> 5), at = kTall ? (tid >> 5) * 4 : (tid & 31) * 4;
-      float4 u;
-      if (wide) {
-        u = raw_four<kElem>(u_raw + raw_at<kRun, kElem>(row, at), bf16);
-        if (kStep) u = step_u(a, u, *reinterpret_cast<const float4*>(m_raw + raw_at<kRun, 4>(row, at)));
-      } else {
-        const int ur = kTall ? long0 + row : k0 + row, uc = kTall ? k0 + at : long0 + at;
-        u = load_u<false>(a, f, ur, uc, ur < f.rows ? f.cols - uc : 0, vec_u, vec_m);
-      }
-      if (kTall) {
-        xs[at * kApplyLdX + row] = u.x; xs[(at + 1) * kApplyLdX + row] = u.y;
-        xs[(at + 2) * kApplyLdX + row] = u.z; xs[(at + 3) * kApplyLdX + row] = u.w;
-      } else {
-        *reinterpret_cast<float4*>(xs + row * kApplyLdX + at) = u;
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      float4* to = reinterpret_cast<float4*>(qs + (i * 16 + (tid >> 4)) * kApplyLdQ + (tid & 15) * 8);
-      to[0] = make_float4(y[i].x, y[i].x, y[i].y, y[i].y);
-      to[1] = make_float4(y[i].z, y[i].z, y[i].w, y[i].w);
-    }
-    __syncthreads();
-    start(k0 + kApplyRing * kApplyK, slot);
-    slot ^= 1;
-#pragma unroll 4
-    for (int k = 0; k < kApplyK; ++k) {
-      float2 sv[kS], lv[kL / 2];
-#pragma unroll
-      for (int i = 0; i < kS; i += 2) *reinterpret_cast<float4*>(sv + i) = *reinterpret_cast<const float4*>(qs + k * kApplyLdQ + (s0 + i) * 2);
-#pragma unroll
-      for (int j = 0; j < kL / 2; j += 2) *reinterpret_cast<float4*>(lv + j) = *reinterpret_cast<const float4*>(xs + k * kApplyLdX + l0 + j * 2);
-#pragma unroll
-      for (int i = 0; i < kS; ++i)
-#pragma unroll
-        for (int j = 0; j < kL / 2; ++j) fma_two(acc[i][j], sv[i], lv[j]);
-    }
-  }
-  copies_wait<0>();
-
-  const float by = kStep ? -a.lr * f.scale : 1.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int left = at_output(i, r, c);
     if (left <= 0) continue;
-    auto out = [&](int s, int l) { return l & 1 ? acc[s % kS][l / 2 % (kL / 2)].y : acc[s % kS][l / 2 % (kL / 2)].x; };
-    float4 v = kTall ? make_float4(out(0, i), out(1, i), out(2, i), out(3, i)) : make_float4(out(i, 0), out(i, 1), out(i, 2), out(i, 3));
+    float4 v = kTall ? make_float4(acc[0][i % kL], acc[1 % kS][i % kL], acc[2 % kS][i % kL], acc[3 % kS][i % kL])
+                     : make_float4(acc[i % kS][0], acc[i % kS][1 % kL], acc[i % kS][2 % kL], acc[i % kS][3 % kL]);
     if (kStep) {
-      const float4 m = p[kStep ? i : 0];
-      v = make_float4(fmaf(by, v.x, a.keep * m.x), fmaf(by, v.y, a.keep * m.y), fmaf(by, v.z, a.keep * m.z), fmaf(by, v.w, a.keep * m.w));
+      const float4 was = p[kStep ? i : 0];
+      v = make_float4(fmaf(by, v.x, a.keep * was.x), fmaf(by, v.y, a.keep * was.y), fmaf(by, v.z, a.keep * was.z), fmaf(by, v.w, a.keep * was.w));
       store4_f32(static_cast<float*>(f.out) + (int64_t)r * f.ldo + c, v, vec_o, left);
       if (f.low != nullptr) store4_bf16(f.low + (int64_t)r * f.ldl + c, v, vec_l, left);
     } else if (out_type == CWL_F32) {
@@ -876,7 +872,7 @@ __device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& 
 
 template <int kMost, bool kStep, int kElem>
 __global__ void __launch_bounds__(kApplyThreads, 2) apply_factors_kernel(const __grid_constant__ FactorArgs<kMost> args) {
-  extern __shared__ __align__(16) uint8_t apply_raw[];
+  __shared__ __align__(16) float xs[kApplyK * kApplyLdX], qs[kApplyK * kApplyLdQ];
   pdl_launch_dependents();
   pdl_wait();
   const int at = find_factor(args.f, args.c.n, blockIdx.x);
@@ -884,11 +880,8 @@ __global__ void __launch_bounds__(kApplyThreads, 2) apply_factors_kernel(const _
   const int unit = blockIdx.x - f.first, row_tiles = (short_side(f) + kApplyShort - 1) / kApplyShort;
   const int long0 = unit / row_tiles * kApplyLong, short0 = unit % row_tiles * kApplyShort;
   const float* q = args.c.q + at * args.c.q_stride;
-  if (f.rows > f.cols) apply_tile<true, kStep, kElem>(args.c, f, q, long0, short0, apply_raw);
-  else apply_tile<false, kStep, kElem>(args.c, f, q, long0, short0, apply_raw);
-}
-constexpr size_t apply_smem(bool step, int elem) {
-  return (size_t)(kApplyK * kApplyLdX + kApplyK * kApplyLdQ) * 4 + (size_t)kApplyRing * kApplyRaw * (elem + (step ? 4 : 0));
+  if (f.rows > f.cols) apply_tile<true, kStep, kElem>(args.c, f, q, long0, short0, xs, qs);
+  else apply_tile<false, kStep, kElem>(args.c, f, q, long0, short0, xs, qs);
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -948,10 +941,7 @@ cudaError_t launch_gram(const FactorArgs<kMost>& args, int64_t blocks, bool pair
 }
 template <int kMost, bool kStep, int kElem>
 cudaError_t launch_apply(const FactorArgs<kMost>& args, int64_t blocks, bool chained, cudaStream_t st) {
-  static SharedMemoryGrant grant;
-  const cudaError_t e = grant(apply_factors_kernel<kMost, kStep, kElem>);
-  if (e != cudaSuccess) return e;
-  return launch_chained(chained, apply_factors_kernel<kMost, kStep, kElem>, dim3((unsigned)blocks), dim3(kApplyThreads), apply_smem(kStep, kElem), st, args);
+  return launch_chained(chained, apply_factors_kernel<kMost, kStep, kElem>, dim3((unsigned)blocks), dim3(kApplyThreads), 0, st, args);
 }
 
 template <int kMost, bool kStep, int kElem, typename Item, typename Fill>
