@@ -52,7 +52,7 @@ constexpr int kThreeTermRows = 512;
 // blocks: the truncation of the tensor cores' own sums would show in the loss of a single token that the model is sure of (1.6e-5
 // of one of 0.9, d = 4096), and would grow with d.  It takes tiles of 256 columns, whose operands come in no faster than they
 // are worked on; with one row tile, where W's rate in HBM is the bound, that costs nothing.
-constexpr int kExactRows = 256, kExactWidth = 8192, kLogitChunk = 8;
+constexpr int kExactRows = 256, kExactWidth = 8192, kLogitChunk = 16;
 constexpr float kAbove = 60.f;                    // a logit this far above the reference takes another one
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -952,10 +952,15 @@ head_gather_ordered_kernel(HeadRows rows, const __nv_bfloat16* W, int64_t ldw, i
   const int width = min(columns, V - first);
   const bool two = pair * 2 + 1 < d;
   const uint16_t* from = reinterpret_cast<const uint16_t*>(W) + (int64_t)pair * 2 * ldw + first;
+  // all copies of the block on their way at once
+  auto copy = [](void* to, const void* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(src), "r"(bytes) : "memory");
+  };
   for (int j = threadIdx.x; j < width / 8; j += kOrderedThreads) {
-    reinterpret_cast<uint4*>(first_row)[j] = __ldcs(reinterpret_cast<const uint4*>(from) + j);
-    reinterpret_cast<uint4*>(second_row)[j] = two ? __ldcs(reinterpret_cast<const uint4*>(from + ldw) + j) : make_uint4(0, 0, 0, 0);
+    copy(first_row + j * 8, from + j * 8, 16);
+    copy(second_row + j * 8, two ? from + ldw + j * 8 : from, two ? 16 : 0);
   }
+  asm volatile("cp.async.commit_group;\n\tcp.async.wait_group 0;" ::: "memory");
   for (int j = width / 8 * 8 + threadIdx.x; j < width; j += kOrderedThreads) {
     first_row[j] = from[j];
     second_row[j] = two ? from[ldw + j] : (uint16_t)0;
@@ -1068,7 +1073,7 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 // How a call is carried out, and where its arrays lie in the workspace, whose size is that of the largest way.
 struct HeadLayout {
   int rows_alloc, piece, pieces, terms;
-  int few;                                              // logits by head_few_kernel
+  int few;                                              // logits (of STATS, or of EXP) by head_few_kernel
   int stats_pass;                                       // a product for lse alone comes first
   int logit_chunk;                                      // K blocks of the logits' products that are summed in the tensor memory, 0 = all
   int from_e;                                           // dX comes from E and the gathered columns of W, without dZ
@@ -1086,11 +1091,11 @@ HeadLayout head_layout(int T, int d, int V, bool forward, bool want_dx, bool wan
   const bool grads = want_dx || want_dw;
   l.from_e = want_dx && !want_dw;
   l.stats_pass = forward && !l.from_e;
+  l.few = T <= (l.from_e ? kFewExpRows : kFewRows);
   l.logit_chunk = T <= kExactRows || d > kExactWidth ? kLogitChunk : 0;
   const int most_tn = l.logit_chunk > 0 ? 256 : kHMaxTile;
   const int k_d = ceil_div(d, kHK), k_t = ceil_div(T, kHK);
   l.packed_ld = (d + 7) / 8 * 8;
-  l.few = T <= kFewRows;
   l.piece = grads ? head_piece(l.rows_alloc, V, terms) : 0;
   l.pieces = grads ? ceil_div(V, l.piece) : 0;
   size_t at = 0;

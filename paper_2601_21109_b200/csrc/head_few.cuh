@@ -1,13 +1,16 @@
-// Logits of up to 64 rows (included by head.cu): STATS and EXP with the operands' places exchanged, Z^T = W^T X^T.
+// Logits of up to 64 rows, 128 where the loss alone is wanted (included by head.cu): STATS and EXP with the operands' places exchanged, Z^T = W^T X^T.
 //
 // Few rows are bound by the bytes of W.  head_kernel would fill 256 rows of tensor memory with them and spend half of what it
 // brings into shared memory on X; here the vocabulary is the M dimension (W's columns are contiguous: an M-major operand),
 // the rows are the N dimension, and a stage is W but for a few KB.  A block takes up to 256 columns of the vocabulary: two
-// tiles of 128 x kRows, drained every kLogitChunk K blocks into fp32 sums of the epilogue's threads, one column of the
+// tiles of 128 x kRows, drained every kFewChunk K blocks into fp32 sums of the epilogue's threads, one column of the
 // vocabulary and all rows a thread.  Single blocks, no pairs: columns are dealt evenly over the SMs, to eight.
 #pragma once
 
-constexpr int kFewRows = 64;
+constexpr int kFewRows = 128;                             // of STATS
+// EXP keeps a register a row beside E's stores: with 128 rows it spills (100 rows: 157 us against head_kernel's 90)
+constexpr int kFewExpRows = 64;
+constexpr int kFewChunk = 8;                               // K blocks
 constexpr int kFewMaxStages = 8;
 constexpr int kFewRing = 200 * 1024;
 constexpr int kFewThreads = 64 + 32 * 8;
@@ -105,7 +108,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
   const int n = *p.rows.n;
   const int n_tiles = n > 0 ? p.n_cols : 0;              // nothing to do without rows
   const int n_kb = (p.k_extent + kHK - 1) / kHK;
-  const int n_chunks = (n_kb + kLogitChunk - 1) / kLogitChunk;
+  const int n_chunks = (n_kb + kFewChunk - 1) / kFewChunk;
   const int boxes = (p.tn + 63) / 64, m_tiles = (boxes + 1) / 2;
   const int stage_bytes = p.stage_bytes, n_stages = p.stages, x_at = boxes * kHBox;
   const CUtensorMap* map_x = n < p.T ? &maps.a_packed : &maps.a;
@@ -150,7 +153,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
           const int slot = local & 1u;
           if (!mbar_wait(acc_empty(slot), ((local >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
           tc_fence_after();
-          const int n_blk = min(kLogitChunk, n_kb - chunk * kLogitChunk);
+          const int n_blk = min(kFewChunk, n_kb - chunk * kFewChunk);
           for (int b = 0; b < n_blk; ++b) {
             if (!mbar_wait(full_bar(s), ph, abort_flag)) { ok = false; break; }
             tc_fence_after();
@@ -322,12 +325,13 @@ cudaError_t launch_few_rows(const HeadMaps& maps, HeadParams p, bool chained, cu
   const int blocks = p.n_cols < kFewBlocks ? p.n_cols : kFewBlocks;
   return launch_chained(chained, head_few_kernel<kMode, kRows>, dim3((unsigned)blocks), dim3(kFewThreads), kFewSmem, st, maps, p);
 }
-inline int few_box(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : 64; }
+inline int few_box(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
 template <int kMode>
 cudaError_t launch_few(const HeadMaps& maps, const HeadParams& p, int T, bool chained, cudaStream_t st) {
   switch (few_box(T)) {
     case 16: return launch_few_rows<kMode, 16>(maps, p, chained, st);
     case 32: return launch_few_rows<kMode, 32>(maps, p, chained, st);
-    default: return launch_few_rows<kMode, 64>(maps, p, chained, st);
+    case 64: return launch_few_rows<kMode, 64>(maps, p, chained, st);
+    default: return launch_few_rows<HEAD_STATS, 128>(maps, p, chained, st);      // EXP has 64 at most
   }
 }
