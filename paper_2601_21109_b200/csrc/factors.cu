@@ -890,7 +890,7 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 // Long-side elements a block of GRAM: short enough that the blocks fill the GPU evenly, long enough that their sums
 // (32 KB a block) stay a small part of what is read.
 constexpr int64_t kGramBlocks = 2400;
-constexpr int kGramLeast = 128;
+constexpr int kGramLeast = 128, kGramLeastBig = 256;
 struct FactorPlan { int slice, n_big, most_R; int64_t blocks; size_t partial, q, big, unit, total; int64_t q_stride, stride; };
 template <typename Item>
 FactorPlan factor_plan(const Item* items, int n) {
@@ -905,7 +905,8 @@ FactorPlan factor_plan(const Item* items, int n) {
   }
   int64_t slice = (work + kGramBlocks - 1) / kGramBlocks;
   slice = (slice + kGramK - 1) / kGramK * kGramK;
-  if (slice < kGramLeast) slice = kGramLeast;
+  const int least = p.n_big > 0 ? kGramLeastBig : kGramLeast;
+  if (slice < least) slice = least;
   if (slice > 1 << 20) slice = 1 << 20;
   p.slice = (int)slice;
   for (int i = 0; i < n; ++i) {

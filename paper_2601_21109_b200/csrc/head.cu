@@ -1191,7 +1191,6 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
   if (T < 0 || d <= 0 || V <= 0) return CWL_ERR_INVALID_ARG;
   if (grad_dtype != CWL_F32 && grad_dtype != CWL_BF16) return CWL_ERR_INVALID_ARG;
   if (T > kHeadMaxRows || V > kHeadMaxRows || d > kHeadMaxWidth) return CWL_ERR_UNSUPPORTED;
-  if (loss == nullptr && dX == nullptr && dW == nullptr) return CWL_ERR_INVALID_ARG;
   const int es = grad_dtype == CWL_F32 ? 4 : 2;
   auto bad_grad = [&](const void* ptr, int64_t ld, int64_t cols, int64_t rows) {
     return ptr != nullptr && ((reinterpret_cast<uintptr_t>(ptr) % es) != 0 || (rows > 1 && ld < cols));
@@ -1203,6 +1202,7 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
     return CWL_OK;
   }
   if (X == nullptr || W == nullptr || targets == nullptr) return CWL_ERR_INVALID_ARG;
+  if (loss == nullptr && dX == nullptr && dW == nullptr) return CWL_ERR_INVALID_ARG;
   if (loss == nullptr && lse == nullptr) return CWL_ERR_INVALID_ARG;      // a backward call reads it
   if (loss != nullptr && dloss != nullptr) return CWL_ERR_INVALID_ARG;    // an upstream gradient belongs to a backward call
   if (bad_operand(X, ldx, d, T) || bad_operand(W, ldw, V, d)) return CWL_ERR_SHAPE;

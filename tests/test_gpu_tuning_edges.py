@@ -62,6 +62,8 @@ def test_no_rows():
     X, W, y, w = operands(1, 4, 64, 100)
     o = cwl.cwl_head_loss(X[:0], W, y[:0], weight=w[:0], want_dx=True, want_dw=True)
     assert o.loss.shape == (0,) and o.dX.shape == (0, 64) and not bool(o.dW.any())
+    o = cwl.cwl_head_loss(X[:0], W, y[:0])                    # tensors of no rows have no address
+    assert o.loss.shape == (0,) and o.dX is None
     for T in (1, 70, 600):
         X, W, y, w = operands(T, T, 64, 1000)
         for yy, ww in ((torch.full_like(y, -1), w), (y, torch.zeros_like(w))):

@@ -24,7 +24,7 @@ def head(L, X=P, ldx=64, W=P, ldw=96, T=8, d=64, V=96, targets=P, weight=None, d
 
 
 def test_head_loss_refusals(L):
-    assert head(L, T=0) == 0 and head(L, T=0, dX=P) == 0
+    assert head(L, T=0) == 0 and head(L, T=0, dX=P) == 0 and head(L, T=0, X=None, targets=None, loss=None, lse=None) == 0
     assert head(L, T=-1) == 1 and head(L, d=0) == 1 and head(L, V=0) == 1 and head(L, dtype=2) == 1 and head(L, dtype=7) == 1
     assert head(L, T=(1 << 24) + 1) == 3 and head(L, V=(1 << 24) + 1) == 3 and head(L, d=(1 << 20) + 1) == 3
     assert head(L, X=None) == 1 and head(L, W=None) == 1 and head(L, targets=None) == 1
