@@ -645,7 +645,7 @@ struct RowsParams {
   int32_t* status_word;
 };
 
-constexpr int kRowsThreads = 256;
+constexpr int kRowsThreads = 1024;
 constexpr int kRowsColumn = 8192;                 // of W's column 0 kept in shared memory
 
 __device__ __forceinline__ float row_up(const RowsParams& p, int t) {
@@ -655,9 +655,11 @@ __device__ __forceinline__ float row_up(const RowsParams& p, int t) {
 }
 // a row counts if it has a target and its loss or, in a backward call, its gradient is not 0 whatever the logits are
 __device__ __forceinline__ bool row_counts(const RowsParams& p, int t) {
-  const int y = p.targets[t];
-  if (y < 0 || y >= p.V) return false;
-  return (p.backward ? row_up(p, t) : p.weight != nullptr ? p.weight[t] : 1.f) != 0.f;
+  // no branch between the loads: those of many rows go out together
+  const unsigned y = (unsigned)__ldg(p.targets + t);
+  float up = p.weight != nullptr ? __ldg(p.weight + t) : 1.f;
+  if (p.backward && p.dloss != nullptr) up *= __ldg(p.dloss + t);
+  return (y < (unsigned)p.V) & (up != 0.f);
 }
 
 // Lists the rows that count, packs their activations where some do not, works out their references (of many rows: the logit of column 0),
@@ -1244,7 +1246,7 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
   r.packed = packed; r.packed_ld = l.packed_ld; r.rows = rows; r.backward = !forward; r.online = online; r.reference = in_order;
   r.status_word = status_word;
   int blocks = ceil_div(T, 8);
-  if (blocks > 592) blocks = 592;
+  if (blocks > 148) blocks = 148;
   r.per_block = ceil_div(T, blocks);
   CWL_CUDA_TRY(launch_chained(chained, head_rows_kernel, dim3((unsigned)blocks), dim3(kRowsThreads), 0, st, r));
   if (l.from_e) {
