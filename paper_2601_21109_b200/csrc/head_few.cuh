@@ -215,7 +215,12 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       asm volatile("bar.sync 1, 256;" ::: "memory");
       if (*epi_go == 0) break;
 
-      if (there) {
+      // is any row's target among this warp's columns?
+      bool held = false;
+#pragma unroll
+      for (int j = 0; j < kRows; j += 32) held |= (unsigned)(targets[j + (lane & (kPart - 1))] - (col - lane)) < 32u;
+      held = __any_sync(0xffffffffu, held);
+      if (held && there) {
 #pragma unroll
         for (int j = 0; j < kRows; ++j)
           if (targets[j] == col) p.rows.z_target[j] = z[j];
@@ -247,19 +252,25 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll
-      for (int j = 0; j < kRows; ++j) {
-        // EXP: the target stays out of E and of the sum
-        const bool in = there && j < n && (kMode != HEAD_EXP || targets[j] != col);
-        z[j] = in ? exp2_fast(fmaf(z[j], kLog2e, -common[j] * kLog2e)) : 0.f;
+      for (int j = 0; j < kRows; ++j) z[j] = there && j < n ? exp2_fast(fmaf(z[j], kLog2e, -common[j] * kLog2e)) : 0.f;
+      if (kMode == HEAD_EXP && held) {                           // the target stays out of E and of the sum
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) z[j] = targets[j] == col ? 0.f : z[j];
       }
       if (kMode == HEAD_EXP) {
         if (there) {
           __nv_bfloat16* e = p.dz + col;
+          if (p.terms == 1) {
 #pragma unroll
-          for (int j = 0; j < kRows; ++j) {
-            if (j < n) {
+            for (int j = 0; j < kRows; ++j) {
+              if (j < n) *e = __float2bfloat16_rn(z[j]);
+              e += p.dz_ld;
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < kRows; ++j) {
               float left = z[j];
-              for (int term = 0; term < p.terms; ++term) {
+              for (int term = 0; term < p.terms && j < n; ++term) {
                 const __nv_bfloat16 part = __float2bfloat16_rn(left);
                 e[term * p.term_at] = part;
                 left -= __bfloat162float(part);
