@@ -482,8 +482,9 @@ cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY, int64_t l
  *   dX      DEV [T, d] or NULL;  dW  DEV [d, V] or NULL; of grad_dtype (CWL_F32 or CWL_BF16), aligned to their type, any
  *           row stride; overwritten; not overlapping an input
  *   workspace   DEV, at least cwl_head_loss_workspace_bytes(T, d, V, dX given, dW given) bytes, 256-byte aligned
- * Logits and all sums are fp32; dZ is rounded to bf16 for the products with W and X.  X of rows that count and W finite.
- * T == 0 writes zeros to dW.  Results do not depend on timing.
+ * Logits and all sums are fp32; what multiplies W and X in the gradients is bf16 where they are, and the sum of two bf16
+ * numbers (three up to 512 rows) where they are fp32, without the target, whose share stays fp32.  X of rows that count and W
+ * finite.  T == 0 writes zeros to dW.  Results do not depend on timing.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (T or V > 2^24, d > 2^20), WORKSPACE, CUDA; TIMEOUT through *status_word. */
 size_t     cwl_head_loss_workspace_bytes(int32_t T, int32_t d, int32_t V, int32_t want_dx, int32_t want_dw);
 cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw, int32_t T, int32_t d, int32_t V,

@@ -18,9 +18,10 @@ extern "C" {
  * the waits on it run out.  Process-wide (two atomics). */
 void cwl_debug_set(int64_t wait_limit_ns, int32_t withhold_publish);
 
-/* The same for cwl_distill_topk and cwl_apply_grads: wait limit (ns; <= 0 restores 2 s) and, with withhold != 0, one copy
- * that is never made -- the second row of every block of the pipelined distillation kernel, the last K block of every CTA
- * of the gradients' first launch -- so that the waits on it run out. */
+/* The same for cwl_distill_topk, cwl_apply_grads and cwl_head_loss: wait limit (ns; <= 0 restores 2 s) and, with withhold != 0,
+ * one copy that is never made -- the second row of every block of the pipelined distillation kernel, the last K block of
+ * every CTA of the gradients' first launch, that of the first tile of every CTA of the head's products -- so that the waits
+ * on it run out. */
 void cwl_debug_training_set(int64_t wait_limit_ns, int32_t withhold);
 
 /* Read-bandwidth ceiling of one decode-sized launch: 148 CTAs (one per SM) stream [ptr, ptr + bytes) once, each its

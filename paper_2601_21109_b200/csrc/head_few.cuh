@@ -5,6 +5,9 @@
 // the rows are the N dimension, and a stage is W but for a few KB.  A block takes up to 256 columns of the vocabulary: two
 // tiles of 128 x kRows, drained every kFewChunk K blocks into fp32 sums of the epilogue's threads, one column of the
 // vocabulary and all rows a thread.  Single blocks, no pairs: columns are dealt evenly over the SMs, to eight.
+//
+// Bound by HBM: one row, 4096 -> 32000: 43.5 us, 262 MB at 6.0 TB/s (head_kernel: 57 with tiles of 448 columns, 84 with sums in
+// fp32); 48 rows, EXP: 54 us (88); 128 rows, STATS: 61 us (66).
 #pragma once
 
 constexpr int kFewRows = 128;                             // of STATS
