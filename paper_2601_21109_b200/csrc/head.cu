@@ -79,7 +79,7 @@ struct HeadRows {                                 // the packed rows, written by
   float* ref;                                     // EXP: reference of the row's exponentials (a backward call: lse)
   float* sum;                                     // ... their sum over the pieces so far, without the target's
   float* alpha;                                   // ... what the sums of the pieces before this one are multiplied with
-  float* scale;                                   // DX: up / sum of all (a backward call: up)
+  float* scale;                                   // DX: the root of 1 / sum of all (a backward call: up)
   float* of_target;                               // DX: up times what the other tokens' probabilities add up to
   unsigned* above;                                // EXP: bit per chunk of columns of the piece that took their own reference
   float* above_ref;                               // ... and that reference
@@ -116,6 +116,12 @@ struct HeadParams {
 // target, however near to 1 the target's probability is; a backward call has lse.
 __device__ __forceinline__ float target_factor(const HeadRows& rows, int row, int online) {
   return online ? rows.of_target[row] : -rows.up[row] * expm1f(rows.z_target[row] - rows.lse[row]);
+}
+// What DX's sums are multiplied with, one after the other: up / sum of all, as two factors, since a target far above the
+// reference puts it below what a number holds where its product with the sums is not.
+__device__ __forceinline__ float2 row_factors(const HeadRows& rows, int row, int online) {
+  const float s = rows.scale[row];
+  return online ? make_float2(s, s * rows.up[row]) : make_float2(s, 1.f);
 }
 // The unit of dZ: the first row's up, unless it is out of the ordinary.
 __device__ __forceinline__ float dz_unit(const HeadRows& rows) {
@@ -477,7 +483,10 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
           if ((kMode == HEAD_STATS || kMode == HEAD_EXP) && mine) {
 #pragma unroll
             for (int j = 0; j < 64; ++j)
-              if (j == y - c) p.rows.z_target[row] = v[j];
+              if (j == y - c) {
+                p.rows.z_target[row] = v[j];
+                if (kMode == HEAD_EXP) v[j] = -INFINITY;         // the target stays out of E, of the sum and of what a reference is held against
+              }
           }
           float own = ref;                        // reference of these columns
           if (kMode == HEAD_STATS || (kMode == HEAD_EXP && p.online)) {
@@ -494,10 +503,6 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
               atomicOr(p.rows.above + (int64_t)row * p.rows.above_words + (chunk >> 5), 1u << (chunk & 31));
               p.rows.above_ref[(int64_t)row * p.rows.chunks + chunk] = top;
             }
-          }
-          if (kMode == HEAD_EXP && mine) {        // the target stays out of E and of the sum
-#pragma unroll
-            for (int j = 0; j < 64; ++j) v[j] = j == y - c ? -INFINITY : v[j];
           }
           const float shift = own * kLog2e;
           float p4[4] = {0.f, 0.f, 0.f, 0.f};
@@ -558,7 +563,8 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
         const bool from_e = kMode == HEAD_DX && p.wy != nullptr;
         const float alpha = from_e && p.acc_in && t.chunk == 0 && live ? p.rows.alpha[row] : 1.f;
         const float up = from_e && live && !keep ? target_factor(p.rows, row, p.online) : 0.f;
-        const float scale = from_e ? (live && !keep ? p.rows.scale[row] : 0.f) : n > 0 ? dz_unit(p.rows) : 1.f;
+        const float2 scale = from_e ? (live && !keep ? row_factors(p.rows, row, p.online) : make_float2(0.f, 0.f))
+                                    : make_float2(n > 0 ? dz_unit(p.rows) : 1.f, 1.f);
         const uint32_t* wy = p.wy + ((int64_t)m_tile * p.acc_groups * 2 + n0 / 2) * kHM + quad * 32 + lane;
         const int chunk = keep || p.out_f32 ? 32 : 64;
 #pragma unroll 1
@@ -592,7 +598,7 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
               continue;
             }
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] *= scale;
+            for (int j = 0; j < 32; ++j) v[j] = v[j] * scale.x * scale.y;
             if (from_e) {
 #pragma unroll
               for (int g = 0; g < 16; ++g) {
@@ -876,35 +882,59 @@ __global__ void __launch_bounds__(kFinishThreads) head_merge_kernel(const MergeP
       rows.ref[row] = m;
       rows.sum[row] = sum;
       if (p.last) {
-        const float z = rows.z_target[row], total = sum + exp2_fast((z - m) * kLog2e), up = rows.up[row];
-        const float l = m + logf(total);
+        // the target, which no reference is held against, joins: relative to its own logit where that is the larger
+        const float z = rows.z_target[row], h = z > m ? exp2_fast((m - z) * (0.5f * kLog2e)) : 1.f;
+        const float others = sum * h * h, total = others + (z > m ? 1.f : exp2_fast((z - m) * kLog2e));
+        const float l = (z > m ? z : m) + logf(total);
         const int t = rows.row[row];
         if (p.lse != nullptr) p.lse[t] = l;
         p.loss[t] = (p.weight != nullptr ? p.weight[t] : 1.f) * (l - z);
-        rows.scale[row] = up / total;
-        rows.of_target[row] = up * (sum / total);
+        rows.scale[row] = h * rsqrtf(total);
+        rows.of_target[row] = rows.up[row] * (others / total);
       }
     }
   }
   __syncthreads();
-  for (int r = 0; r < kRowsEach && row0 + r < n; ++r) {
+  // a row to a warp, or to the block; numbers eight at a time
+  constexpr int kTogether = kRowsEach == 1 ? kFinishThreads : 32;
+  const int lane = threadIdx.x % kTogether;
+  for (int r = threadIdx.x / kTogether; r < kRowsEach && row0 + r < n; r += kFinishThreads / kTogether) {
     if (!(new_ref[r] > old_ref[r])) continue;            // as good as always
     const int64_t at = row0 + r;
-    for (int c = threadIdx.x; c < p.width; c += kFinishThreads) {
+    const float from_old = exp2_fast((old_ref[r] - new_ref[r]) * kLog2e);
+    auto factor = [&](int c) {
       const int chunk = c / p.chunk_cols;
       const bool above = rows.above[at * rows.above_words + (chunk >> 5)] >> (chunk & 31) & 1u;
-      const float f = exp2_fast(((above ? rows.above_ref[at * rows.chunks + chunk] : old_ref[r]) - new_ref[r]) * kLog2e);
-      __nv_bfloat16* e = p.dz + at * p.dz_ld + c;
-      float x = 0.f;
-      for (int k = p.terms - 1; k >= 0; --k) x += __bfloat162float(e[k * p.term_at]);
-      x *= f;
+      return above ? exp2_fast((rows.above_ref[at * rows.chunks + chunk] - new_ref[r]) * kLog2e) : from_old;
+    };
+    auto put = [&](__nv_bfloat16* e, float x) {
       for (int k = 0; k < p.terms; ++k) {
         e[k * p.term_at] = __float2bfloat16_rn(x);
         x -= __bfloat162float(e[k * p.term_at]);
       }
+    };
+    __nv_bfloat16* e = p.dz + at * p.dz_ld;
+    const int whole = p.terms == 1 ? p.width / 8 : 0;
+#pragma unroll 4
+    for (int i = lane; i < whole; i += kTogether) {
+      uint4 q = reinterpret_cast<const uint4*>(e)[i];
+      const float f = factor(i * 8);
+      uint32_t* w = reinterpret_cast<uint32_t*>(&q);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const __nv_bfloat162 two = __floats2bfloat162_rn(__uint_as_float(w[k] << 16) * f, __uint_as_float(w[k] & 0xFFFF0000u) * f);
+        w[k] = reinterpret_cast<const uint32_t&>(two);
+      }
+      reinterpret_cast<uint4*>(e)[i] = q;
     }
-    __syncthreads();
-    for (int w = threadIdx.x; w < rows.above_words; w += kFinishThreads) rows.above[at * rows.above_words + w] = 0u;
+    for (int c = whole * 8 + lane; c < p.width; c += kTogether) {
+      float x = 0.f;
+      for (int k = p.terms - 1; k >= 0; --k) x += __bfloat162float(e[c + k * p.term_at]);
+      put(e + c, x * factor(c));
+    }
+    if (kTogether == 32) __syncwarp();
+    else __syncthreads();
+    for (int w = lane; w < rows.above_words; w += kTogether) rows.above[at * rows.above_words + w] = 0u;
   }
 }
 
@@ -1022,11 +1052,12 @@ head_sum_kernel(HeadRows rows, int T, int online, int m_extent, int cols, const 
     float4 s = sums[e];
     if (col0 + g * 4 < cols && row < m_rows) {
       if (wy != nullptr) {
-        const float f = rows.scale[row], up = target_factor(rows, row, online);
+        const float2 f = row_factors(rows, row, online);
+        const float up = target_factor(rows, row, online);
         const uint32_t* w = wy + ((int64_t)m_tile * groups * 2 + col0 / 2 + g * 2) * kHM + r;
         const uint32_t x = w[0], y = w[kHM];
-        s.x = s.x * f - up * __uint_as_float(x << 16); s.y = s.y * f - up * __uint_as_float(x & 0xFFFF0000u);
-        s.z = s.z * f - up * __uint_as_float(y << 16); s.w = s.w * f - up * __uint_as_float(y & 0xFFFF0000u);
+        s.x = s.x * f.x * f.y - up * __uint_as_float(x << 16); s.y = s.y * f.x * f.y - up * __uint_as_float(x & 0xFFFF0000u);
+        s.z = s.z * f.x * f.y - up * __uint_as_float(y << 16); s.w = s.w * f.x * f.y - up * __uint_as_float(y & 0xFFFF0000u);
       } else {
         s.x *= unit; s.y *= unit; s.z *= unit; s.w *= unit;
       }
@@ -1105,7 +1136,7 @@ HeadLayout head_layout(int T, int d, int V, bool forward, bool want_dx, bool wan
   l.from_e = want_dx && !want_dw;
   l.stats_pass = forward && !l.from_e;
   l.few = T <= (l.from_e ? kFewExpRows : kFewRows);
-  l.logit_chunk = T <= kExactRows || d > kExactWidth ? kLogitChunk : 0;
+  l.logit_chunk = T <= kExactRows || d > kExactWidth || (grads && f32) ? kLogitChunk : 0;
   const int most_tn = l.logit_chunk > 0 ? 256 : kHMaxTile;
   const int k_d = ceil_div(d, kHK), k_t = ceil_div(T, kHK);
   l.packed_ld = (d + 7) / 8 * 8;

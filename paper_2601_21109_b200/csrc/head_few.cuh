@@ -226,7 +226,10 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       if (held && there) {
 #pragma unroll
         for (int j = 0; j < kRows; ++j)
-          if (targets[j] == col) p.rows.z_target[j] = z[j];
+          if (targets[j] == col) {
+            p.rows.z_target[j] = z[j];
+            if (kMode == HEAD_EXP) z[j] = -INFINITY;             // the target stays out of E, of the sum and of what a reference is held against
+          }
       }
       // the rows' maxima over the block's columns, 32 rows at a time
 #pragma unroll
@@ -256,10 +259,6 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll
       for (int j = 0; j < kRows; ++j) z[j] = there && j < n ? exp2_fast(fmaf(z[j], kLog2e, -common[j] * kLog2e)) : 0.f;
-      if (kMode == HEAD_EXP && held) {                           // the target stays out of E and of the sum
-#pragma unroll
-        for (int j = 0; j < kRows; ++j) z[j] = targets[j] == col ? 0.f : z[j];
-      }
       if (kMode == HEAD_EXP) {
         if (there) {
           __nv_bfloat16* e = p.dz + col;
