@@ -59,10 +59,12 @@ constexpr int kHRaster = 16;                      // row tiles whose columns are
 constexpr int kHeadMaxRows = 1 << 24, kHeadMaxWidth = 1 << 20;   // T and V, d
 constexpr int kChunkBlocks = 64;                  // K blocks, times terms, after which the sums of an fp32 gradient leave the tensor memory
 constexpr int kThreeTermRows = 512;
-// Logits of up to kExactRows rows, or of more than kExactWidth activations, are added up in fp32 after every kLogitChunk K
-// blocks: the truncation of the tensor cores' own sums would show in the loss of a single token that the model is sure of (1.6e-5
-// of one of 0.9, d = 4096), and would grow with d.  It takes tiles of 256 columns, whose operands come in no faster than they
-// are worked on; with one row tile, where W's rate in HBM is the bound, that costs nothing.
+// Logits of up to kExactRows rows, of more than kExactWidth activations, or behind fp32 gradients, are added up in fp32 after every
+// kLogitChunk K blocks: the truncation of the tensor cores' own sums would show in the loss of a single token that the model is
+// sure of (1.6e-5 of one of 0.9, d = 4096), would grow with d, and would be most of what fp32 gradients lose (d = 8192, lse given: 4e-5
+// without, 7e-6 with).  It takes tiles of 256 columns, whose operands come in no faster than they are worked on; with one row tile,
+// where W's rate in HBM is the bound, that costs nothing.  Elsewhere it costs 7 to 8 % of a call (16384 rows 7.1 -> 7.7 ms, 4096
+// rows backward 1.74 -> 1.89; 24 K blocks 5 %, 8 K blocks 17 %) and would bring lse from 2.4e-6 to 6e-7: not worth it beside bf16 gradients.
 constexpr int kExactRows = 256, kExactWidth = 8192, kLogitChunk = 16;
 constexpr float kAbove = 60.f;                    // a logit this far above the reference takes another one
 constexpr float kLog2e = 1.4426950408889634f;
@@ -1136,9 +1138,9 @@ HeadLayout head_layout(int T, int d, int V, bool forward, bool want_dx, bool wan
   l.from_e = want_dx && !want_dw;
   l.stats_pass = forward && !l.from_e;
   l.few = T <= (l.from_e ? kFewExpRows : kFewRows);
-  l.logit_chunk = T <= kExactRows || d > kExactWidth || (grads && f32) ? kLogitChunk : 0;
-  const int most_tn = l.logit_chunk > 0 ? 256 : kHMaxTile;
   const int k_d = ceil_div(d, kHK), k_t = ceil_div(T, kHK);
+  l.logit_chunk = (T <= kExactRows || d > kExactWidth || (grads && f32)) && k_d > kLogitChunk ? kLogitChunk : 0;
+  const int most_tn = l.logit_chunk > 0 ? 256 : kHMaxTile;
   l.packed_ld = (d + 7) / 8 * 8;
   l.piece = grads ? head_piece(l.rows_alloc, V, terms) : 0;
   l.pieces = grads ? ceil_div(V, l.piece) : 0;
