@@ -669,9 +669,13 @@ __global__ void __launch_bounds__(kBigGramThreads) big_gram_kernel(const __grid_
 //   SPREAD  S = P G, and Q' = P Q (z = 1, or alone in the last step, where it leaves as fp32, times 1 / (norm + eps))
 //   GRAM    G = P S
 enum : int { BIG_POLY = 0, BIG_SPREAD = 1, BIG_GRAM = 2 };
+// A block takes 16 x 16 entries, each of its warps a quarter of the sums, which it brings in itself and waits for alone: at R = 256
+// that is 136 blocks a factor (32 x 32 entries: 36, each with all of 2.2 us of products in one SM, twice that where P G and P Q go
+// together).
 constexpr int kBigThreads = 128;
+constexpr int kBigTile = 16;
 constexpr int kBigLd = CWL_MAX_RANK + 4;
-constexpr size_t kBigSmem = (size_t)2 * 32 * kBigLd * 8;
+constexpr size_t kBigSmem = (size_t)(2 * kBigTile * kBigLd + 4 * kBigTile * kBigTile) * 8;
 __global__ void __launch_bounds__(kBigThreads) big_product_kernel(const __grid_constant__ BigArgs a, int what, int step) {
   extern __shared__ __align__(16) double big_raw[];
   pdl_launch_dependents();
@@ -679,7 +683,7 @@ __global__ void __launch_bounds__(kBigThreads) big_product_kernel(const __grid_c
   const int R = a.R[blockIdx.y], Rp = padded(R);
   int ti = 0, tj = blockIdx.x;
   while (tj > ti) { tj -= ti + 1; ++ti; }
-  if (ti >= Rp / 32) return;
+  if (ti >= Rp / kBigTile) return;
   const bool last = step + 1 == a.steps;
   double* G = a.big + (int64_t)blockIdx.y * 5 * a.stride;
   double* P = G + a.stride;
@@ -691,55 +695,70 @@ __global__ void __launch_bounds__(kBigThreads) big_product_kernel(const __grid_c
   const double* y = what == BIG_GRAM ? S : of_q ? Q : G;
   double* to = what == BIG_POLY ? P : what == BIG_GRAM ? G : of_q ? Q_next : S;
   double* rows_x = big_raw;
-  double* rows_y = big_raw + 32 * kBigLd;
+  double* rows_y = rows_x + kBigTile * kBigLd;
+  double* sums = rows_y + kBigTile * kBigLd;       // [warp][16][16]
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, fr = lane >> 2, fc = lane & 3;
-  for (int r = warp; r < 32; r += kBigThreads / 32) {
-    for (int c = lane * 2; c < Rp; c += 64) {
-      copy16(rows_x + r * kBigLd + c, x + (int64_t)(ti * 32 + r) * Rp + c, 16);
-      copy16(rows_y + r * kBigLd + c, y + (int64_t)(tj * 32 + r) * Rp + c, 16);
+  const int share = Rp / 4, k_first = warp * share;        // Rp is a multiple of 32
+  for (int r = 0; r < kBigTile; ++r) {
+    for (int c = k_first + lane * 2; c < k_first + share; c += 64) {
+      copy16(rows_x + r * kBigLd + c, x + (int64_t)(ti * kBigTile + r) * Rp + c, 16);
+      copy16(rows_y + r * kBigLd + c, y + (int64_t)(tj * kBigTile + r) * Rp + c, 16);
     }
   }
   copies_commit();
+  // what else this thread's entries are made of, on its way too
+  constexpr int kOne = kBigTile * kBigTile, kMine = kOne / kBigThreads;
+  double g[kMine] = {};
+  if (what == BIG_POLY) {
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+      const int e = tid + i * kBigThreads;
+      g[i] = G[(int64_t)(ti * kBigTile + e / kBigTile) * Rp + tj * kBigTile + e % kBigTile];
+    }
+  }
+  const double unit = of_q || (what == BIG_POLY && a.steps == 1) ? a.unit[blockIdx.y] : 0.0;
   copies_wait<0>();
-  __syncthreads();
-  const int qi = (warp >> 1) * 16, qj = (warp & 1) * 16;
+  __syncwarp();
   double acc[2][2][2] = {};
 #pragma unroll 4
-  for (int k = 0; k < Rp / 4; ++k) {
+  for (int k = k_first; k < k_first + share; k += 4) {
     double u[2], v[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      u[t] = rows_x[(qi + t * 8 + fr) * kBigLd + k * 4 + fc];
-      v[t] = rows_y[(qj + t * 8 + fr) * kBigLd + k * 4 + fc];
+      u[t] = rows_x[(t * 8 + fr) * kBigLd + k + fc];
+      v[t] = rows_y[(t * 8 + fr) * kBigLd + k + fc];
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int j = 0; j < 2; ++j) mma_f64(acc[i][j], u[i], v[j]);
   }
-  float* q = a.q + a.which[blockIdx.y] * a.q_stride;
-  const double unit = of_q || (what == BIG_POLY && a.steps == 1) ? a.unit[blockIdx.y] : 0.0;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int r = ti * 32 + qi + i * 8 + fr, c = tj * 32 + qj + j * 8 + fc * 2 + k;
-        if (ti == tj && c > r) continue;           // one value for both halves
-        double v = acc[i][j][k];
-        if (what == BIG_POLY) v = (r == c ? a.a : 0.0) + a.b * G[(int64_t)r * Rp + c] + a.c * v;
-        if (last && (of_q || what == BIG_POLY && step == 0)) {
-          if (r < R && c < R) q[(int64_t)r * R + c] = q[(int64_t)c * R + r] = (float)(v * unit);
-          if (of_q) continue;
-        }
-        to[(int64_t)r * Rp + c] = v;
-        to[(int64_t)c * Rp + r] = v;
-        if (what == BIG_POLY && step == 0) {
-          Q_next[(int64_t)r * Rp + c] = v;
-          Q_next[(int64_t)c * Rp + r] = v;
-        }
-      }
+      for (int k = 0; k < 2; ++k) sums[warp * kBigTile * kBigTile + (i * 8 + fr) * kBigTile + j * 8 + fc * 2 + k] = acc[i][j][k];
+  __syncthreads();
+  float* q = a.q + a.which[blockIdx.y] * a.q_stride;
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) {
+    const int e = tid + i * kBigThreads;
+    const int r = ti * kBigTile + e / kBigTile, c = tj * kBigTile + e % kBigTile;
+    if (c > r) continue;                           // one value for both halves
+    double v = (sums[e] + sums[e + kOne]) + (sums[e + 2 * kOne] + sums[e + 3 * kOne]);
+    if (what == BIG_POLY) v = (r == c ? a.a : 0.0) + a.b * g[i] + a.c * v;
+    if (last && (of_q || what == BIG_POLY && step == 0)) {
+      if (r < R && c < R) q[(int64_t)r * R + c] = q[(int64_t)c * R + r] = (float)(v * unit);
+      if (of_q) continue;
+    }
+    to[(int64_t)r * Rp + c] = v;
+    to[(int64_t)c * Rp + r] = v;
+    if (what == BIG_POLY && step == 0) {
+      Q_next[(int64_t)r * Rp + c] = v;
+      Q_next[(int64_t)c * Rp + r] = v;
+    }
+  }
 }
 
 // ------------------------------------------------------------------------------------------------------------ APPLY
@@ -1011,7 +1030,7 @@ cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, v
     static SharedMemoryGrant grant;
     CWL_CUDA_TRY(grant(big_product_kernel));
     CWL_CUDA_TRY(launch_chained(chained, big_gram_kernel, dim3((unsigned)(block_pairs(most_R) * kBigGramShare), (unsigned)big.n), dim3(kBigGramThreads), 0, st, big));
-    const int t = padded(most_R) / 32, tiles = t * (t + 1) / 2;
+    const int t = padded(most_R) / kBigTile, tiles = t * (t + 1) / 2;
     for (int step = 0; step < common.steps; ++step) {
       const bool last = step + 1 == common.steps;
       auto product = [&](int what, int z) {
