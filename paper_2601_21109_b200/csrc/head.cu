@@ -32,9 +32,8 @@
 // pipe active 79 % in EXP and 84 % in DX.  Tiles of 256 x 512 a pair of CTAs, because with 256 x 256 operands reach shared
 // memory no faster than they are used; what the epilogue of a tile leaves uncovered is 2 % of it at d = 4096 and 15 % at d = 1024
 // (4000 rows of 131072: 0.89 ms, 1.2 PFLOP/s; pipe 66 %): it hands the first 256 columns back before the others, and the
-// next tile's products of as many K blocks as the ring holds start there.  fp32 gradients: two products for one, 2.35 to 2.5 ms for 2047
+// next tile's products of as many K blocks as the ring holds start there.  fp32 gradients: two products for one, 2.6 ms for 2047
 // rows, 2048 -> 50021, dX and dW.
-
 #include "cluster.cuh"
 #include "cwl_common.cuh"
 #include "pair_mma.cuh"
