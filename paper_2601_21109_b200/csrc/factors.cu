@@ -614,8 +614,10 @@ struct BigArgs {
 static_assert(sizeof(BigArgs) <= 8 * 1024, "kernel parameters");
 __host__ __device__ __forceinline__ int padded(int R) { return (R + 31) / 32 * 32; }
 
-// Sums of GRAM's partial products, scaled: G_0.  Eight blocks a 64 x 64 pair, two entries a thread.
-constexpr int kBigGramThreads = 256, kBigGramShare = 8;
+// Sums of GRAM's partial products, scaled: G_0.  Sixteen blocks a 64 x 64 pair, an entry a thread, whose slices are on their way
+// before the trace's.
+constexpr int kBigGramThreads = 256, kBigGramShare = 16;
+static_assert(64 * 64 == kBigGramThreads * kBigGramShare, "an entry a thread");
 __global__ void __launch_bounds__(kBigGramThreads) big_gram_kernel(const __grid_constant__ BigArgs a) {
   __shared__ double met[kBigGramThreads / 32];
   pdl_launch_dependents();
@@ -626,6 +628,13 @@ __global__ void __launch_bounds__(kBigGramThreads) big_gram_kernel(const __grid_
   int bi = 0, bj = pair;
   while (bj > bi) { bj -= bi + 1; ++bi; }
   const double* part = a.partial + (int64_t)a.first[blockIdx.y] * 64 * 64;
+  // of a block on the diagonal its tiles of the lower triangle are there, all of the others
+  const int entries = (bi == bj ? 36 * 64 : 64 * 64) / kBigGramShare, at = (blockIdx.x % kBigGramShare) * entries + tid;
+  double v = 0.0;
+  if (tid < entries) {
+#pragma unroll 16
+    for (int k = 0; k < slices; ++k) v += part[((int64_t)k * pairs + pair) * 64 * 64 + at];
+  }
   // the trace: every block adds it up in the same order
   double s = 0.0;
   for (int i = tid; i < R; i += kBigGramThreads) {
@@ -640,25 +649,18 @@ __global__ void __launch_bounds__(kBigGramThreads) big_gram_kernel(const __grid_
   for (int w = 0; w < kBigGramThreads / 32; ++w) trace += met[w];
   const double unit = trace == 0.0 ? 0.0 : 1.0 / (sqrt(trace) + a.eps);
   double* G = a.big + (int64_t)blockIdx.y * 5 * a.stride;
-  // of a block on the diagonal its tiles of the lower triangle are there, all of the others
-  const int entries = (bi == bj ? 36 * 64 : 64 * 64) / kBigGramShare;
-  for (int e = tid; e < entries; e += kBigGramThreads) {
-    const int at = (blockIdx.x % kBigGramShare) * entries + e;
-    double v = 0.0;
-#pragma unroll 16
-    for (int k = 0; k < slices; ++k) v += part[((int64_t)k * pairs + pair) * 64 * 64 + at];
+  if (tid < entries) {
     int r = at >> 6, c = at & 63;
     if (bi == bj) {
       int ti, tj;
       lower_tile(at >> 6, ti, tj);
       r = ti * 8 + (at >> 3 & 7);
       c = tj * 8 + (at & 7);
-      if (c > r) continue;
     }
+    const bool other_half = bi == bj && c > r;     // of a tile on the diagonal
     r += bi * 64;
     c += bj * 64;
-    if (r >= Rp || c >= Rp) continue;
-    G[(int64_t)r * Rp + c] = G[(int64_t)c * Rp + r] = v * unit * unit;
+    if (!other_half && r < Rp && c < Rp) G[(int64_t)r * Rp + c] = G[(int64_t)c * Rp + r] = v * unit * unit;
   }
   if (blockIdx.x == 0 && tid == 0) a.unit[blockIdx.y] = unit;
 }
