@@ -840,11 +840,12 @@ head_finish_kernel(HeadRows rows, const float2* part, int n_part, int rows_alloc
   const int64_t row = (int64_t)blockIdx.x * kRowsEach + threadIdx.x % kRowsEach;
   const float2 all = row_sums<kRowsEach>(part, n_part, rows_alloc, row, row < n, -INFINITY, met);
   if (threadIdx.x < kRowsEach && row < n) {
-    const float l = all.x + logf(all.y);
+    const float over = logf(all.y), l = all.x + over;
     const int t = rows.row[row];
     rows.lse[row] = l;
     if (lse != nullptr) lse[t] = l;
-    if (loss != nullptr) loss[t] = (weight != nullptr ? weight[t] : 1.f) * (l - rows.z_target[row]);
+    // not l - z, which has been rounded at the size of the logits
+    if (loss != nullptr) loss[t] = (weight != nullptr ? weight[t] : 1.f) * (all.x - rows.z_target[row] + over);
   }
 }
 
@@ -886,10 +887,10 @@ __global__ void __launch_bounds__(kFinishThreads) head_merge_kernel(const MergeP
         // the target, which no reference is held against, joins: relative to its own logit where that is the larger
         const float z = rows.z_target[row], h = z > m ? exp2_fast((m - z) * (0.5f * kLog2e)) : 1.f;
         const float others = sum * h * h, total = others + (z > m ? 1.f : exp2_fast((z - m) * kLog2e));
-        const float l = (z > m ? z : m) + logf(total);
+        const float over = z > m ? log1pf(others) : logf(total);
         const int t = rows.row[row];
-        if (p.lse != nullptr) p.lse[t] = l;
-        p.loss[t] = (p.weight != nullptr ? p.weight[t] : 1.f) * (l - z);
+        if (p.lse != nullptr) p.lse[t] = (z > m ? z : m) + over;
+        p.loss[t] = (p.weight != nullptr ? p.weight[t] : 1.f) * (z > m ? over : m - z + over);
         rows.scale[row] = h * rsqrtf(total);
         rows.of_target[row] = rows.up[row] * (others / total);
       }

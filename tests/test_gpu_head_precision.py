@@ -21,16 +21,17 @@ def exact(X, W, y, w, lse=None):
     return dz @ wt.T, x.T @ dz, z
 
 
-@pytest.mark.parametrize("T", [20, 100, 300, 1500])
+@pytest.mark.parametrize("T,V", [(20, 3000), (100, 3000), (300, 3000), (1500, 3000), (1500, 100001)])
 @pytest.mark.parametrize("grad", [torch.bfloat16, torch.float32])
-def test_rows_of_sure_tokens(T, grad):
+def test_rows_of_sure_tokens(T, V, grad):
     """Targets up to 140 above the others: every row's gradient that fp32 can hold has the relative precision of the rest.  Row by
     row: E's rounding and dX's (2^-9 each at most in a norm, taken whole), and twice what a logit of up to 200 loses in 16
     truncated steps (2^-23 of it each: 2^-11.3)."""
-    d, V = 256, 3000
+    d = 256
     gen = torch.Generator(device="cuda")
     gen.manual_seed(T)
-    W = (torch.randn(d, V, device="cuda", generator=gen) * d ** -0.5).bfloat16()
+    buf = torch.zeros(d, (V + 7) // 8 * 8, dtype=torch.bfloat16, device="cuda")
+    W = buf[:, :V].copy_(torch.randn(d, V, device="cuda", generator=gen) * d ** -0.5)
     y = torch.randint(0, V, (T,), device="cuda", generator=gen, dtype=torch.int32)
     y[::7] = 0                                          # the column that rows take their reference from
     gap = torch.linspace(0, 140, T, device="cuda")[torch.randperm(T, device="cuda", generator=gen)]
@@ -75,3 +76,22 @@ def test_gradients_of_32_bits_of_a_wide_head(T, want_dw, backward):
     assert float((o.dX.double() - dx).norm() / dx.norm()) <= bound
     if want_dw:
         assert float((o.dW.double() - dw).norm() / dw.norm()) <= bound
+
+
+@pytest.mark.parametrize("T", [3, 100, 400])
+@pytest.mark.parametrize("want_dx", [False, True])
+def test_loss_of_sure_tokens(T, want_dx):
+    """The loss of a token whose target stands out is as exact as its logits are apart, not as they are large: the differences of exact
+    logits (small multiples of powers of two, 16 products) are exact, and what the others add up to has 2^-22 of itself per
+    exponential and 2^-24 per sum of at most 1024."""
+    d, V = 16, 600
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(T)
+    W = (torch.randint(-4, 5, (d, V), device="cuda", generator=gen) / 4.0).bfloat16()
+    X = (torch.randint(-8, 9, (T, d), device="cuda", generator=gen) / 4.0).bfloat16()
+    z = X.double() @ W.double()
+    y = z.argmax(1).int()
+    o = cwl.cwl_head_loss(X, W, y, want_dx=want_dx)
+    apart = z - z.gather(1, y.long()[:, None])
+    ref = torch.log1p(apart.exp().scatter(1, y.long()[:, None], 0.0).sum(1))
+    assert float((o.loss.double() - ref).abs().max()) <= (2 * float(apart.abs().max()) + 4) * 2.0 ** -22 + 1024 * 2.0 ** -24
