@@ -686,8 +686,8 @@ __global__ void __launch_bounds__(kRowsThreads) head_rows_kernel(const RowsParam
   __shared__ int sums[2][kRowsThreads / 32];
   __shared__ int counts[kRowsThreads];
   __shared__ __align__(16) __nv_bfloat16 column[kRowsColumn];
-  pdl_launch_dependents();
   pdl_wait();
+  pdl_launch_dependents();                        // after the wait: head_few_kernel fetches W by that
   if (p.online && p.reference) {
 #pragma unroll 8
     for (int j = threadIdx.x; j < kRowsColumn; j += kRowsThreads) column[j] = j < p.d ? p.W[(int64_t)j * p.ldw] : __float2bfloat16_rn(0.f);
