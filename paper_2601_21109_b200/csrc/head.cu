@@ -79,7 +79,7 @@ struct HeadRows {                                 // the packed rows, written by
   float* z_target;
   float* ref;                                     // EXP: reference of the row's exponentials (a backward call: lse)
   float* sum;                                     // ... their sum over the pieces so far, without the target's
-  float* alpha;                                   // ... what the sums of the pieces before this one are multiplied with
+  float* alpha;                                   // ... what the sums of the pieces before this one are multiplied with (not in a backward call)
   float* scale;                                   // DX: the root of 1 / sum of all (a backward call: up)
   float* of_target;                               // DX: up times what the other tokens' probabilities add up to
   unsigned* above;                                // EXP: bit per chunk of columns of the piece that took their own reference
@@ -562,7 +562,8 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
         // where this warp's rows go: rows of the call for DX, columns of X for DW
         const int mine = !live ? -1 : kMode == HEAD_DX && n < p.T ? p.rows.row[row] : row;
         const bool from_e = kMode == HEAD_DX && p.wy != nullptr;
-        const float alpha = from_e && p.acc_in && t.chunk == 0 && live ? p.rows.alpha[row] : 1.f;
+        // a backward call's reference is lse from the first piece on: nobody writes alpha
+        const float alpha = from_e && p.online && p.acc_in && t.chunk == 0 && live ? p.rows.alpha[row] : 1.f;
         const float up = from_e && live && !keep ? target_factor(p.rows, row, p.online) : 0.f;
         const float2 scale = from_e ? (live && !keep ? row_factors(p.rows, row, p.online) : make_float2(0.f, 0.f))
                                     : make_float2(n > 0 ? dz_unit(p.rows) : 1.f, 1.f);
