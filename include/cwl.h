@@ -483,8 +483,9 @@ cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY, int64_t l
  *           row stride; overwritten; not overlapping an input
  *   workspace   DEV, at least cwl_head_loss_workspace_bytes(T, d, V, dX given, dW given) bytes, 256-byte aligned
  * Logits and all sums are fp32; what multiplies W and X in the gradients is bf16 where they are, and the sum of two bf16
- * numbers (three up to 512 rows) where they are fp32, without the target, whose share stays fp32.  X of rows that count and W
- * finite.  T == 0 writes zeros to dW.  Results do not depend on timing.
+ * numbers (three up to 512 rows) where they are fp32.  In a call for dX alone the target is not among it: its share stays fp32;
+ * where dW is wanted it is rounded like the others.  Either way 1 - softmax(z)_y has the relative precision of the others'
+ * probabilities (a backward call: of expm1(z_y - lse[t])), however sure a token is.  X of rows that count and W finite.  T == 0 writes zeros to dW.  Results do not depend on timing.
  * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (T or V > 2^24, d > 2^20), WORKSPACE, CUDA; TIMEOUT through *status_word. */
 size_t     cwl_head_loss_workspace_bytes(int32_t T, int32_t d, int32_t V, int32_t want_dx, int32_t want_dw);
 cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw, int32_t T, int32_t d, int32_t V,

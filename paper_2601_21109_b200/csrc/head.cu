@@ -6,7 +6,7 @@
 // Rows without a target or of weight 0 cost nothing: the first kernel lists the others and packs their activations
 // together (or, where every row counts, leaves X as it is), and all products run over the packed rows.  These are
 // tensor-core products of one persistent kernel, which differ in the way their operands lie and in what becomes of a tile:
-//   STATS  z tile -> (max, sum of exponentials) of its columns per row, and the target's logit
+//   STATS  z tile -> (max, sum of exponentials) of its columns per row without the target's, and the target's logit
 //   EXP    z tile of a piece of the vocabulary -> E = e^(z - r_t) in bf16, to a workspace, with the same statistics
 //   DZ     z tile of a piece again, once lse is known -> dZ in bf16, to a workspace (where dW is wanted)
 //   DX     piece of E or dZ times W^T; the sums over the pieces are kept in fp32
@@ -18,7 +18,9 @@
 // but the target's, which joins at the end, lies 60 above it: the target's, or (many rows) that of column 0.  Where one does, its 64 columns take a reference of their own,
 // and head_merge_kernel puts the row's piece on a common one before DX reads it.  The target's column W_y is gathered from W
 // and subtracted in fp32, so that it is not among what is rounded to bf16: a token of which the model knows little has
-// dX near -up W_y, and where the model is sure of it E_y W_y and W_y would cancel.
+// dX near -up W_y, and where the model is sure of it E_y W_y and W_y would cancel.  Where dW is wanted, the target is an entry
+// of dZ like the others, rounded like them, but not as e^(z_y - lse) - 1, of which little would be left where the model is sure:
+// -up (1 - q_y) is what the others add up to (head_finish_kernel), or up expm1(z_y - lse) where lse is given.
 //
 // Roundings to fewer bits: E and dZ to bf16 (2^-9 of a number on the average row: dX's own rounding to bf16 is as large).
 // For fp32 gradients they are kept as the sum of two bf16 numbers (2^-17), of up to kThreeTermRows rows, where one number's error
@@ -81,7 +83,7 @@ struct HeadRows {                                 // the packed rows, written by
   float* sum;                                     // ... their sum over the pieces so far, without the target's
   float* alpha;                                   // ... what the sums of the pieces before this one are multiplied with (not in a backward call)
   float* scale;                                   // DX: the root of 1 / sum of all (a backward call: up)
-  float* of_target;                               // DX: up times what the other tokens' probabilities add up to
+  float* of_target;                               // DX, DZ: up times what the other tokens' probabilities add up to (a call that gives the loss)
   unsigned* above;                                // EXP: bit per chunk of columns of the piece that took their own reference
   float* above_ref;                               // ... and that reference
   int above_words, chunks;                        // words and chunks a row (64 columns; in head_few_kernel a block's)
@@ -102,7 +104,7 @@ struct HeadParams {
   int terms, term_at;                             // E / dZ is the sum of so many bf16 numbers, each term_at columns after the one before
   int rows_alloc;                                 // rows of the workspace arrays
   float2* part;                                   // STATS, EXP: [2 n_cols][rows_alloc] (max, sum)
-  int online;                                     // EXP: statistics wanted, references may be outgrown
+  int online;                                     // a call that gives the loss.  EXP: statistics wanted, references may be outgrown
   __nv_bfloat16* dz; int64_t dz_ld;               // EXP, DZ
   float* acc; int acc_groups;                     // fp32 sums [split][128-row tile][group of 4 columns][128 rows][4]
   int acc_in, acc_out;                            // DX, DW: add what is there; leave the sum there instead of in `out`
@@ -481,12 +483,17 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
             for (int j = 0; j < 64; ++j) v[j] = j < cols - c ? v[j] : -INFINITY;
           }
           const bool mine = (unsigned)(y - c) < 64u;
-          if ((kMode == HEAD_STATS || kMode == HEAD_EXP) && mine) {
+          float z_y = 0.f;                        // DZ: the target's logit
+          if (mine) {
 #pragma unroll
             for (int j = 0; j < 64; ++j)
               if (j == y - c) {
-                p.rows.z_target[row] = v[j];
-                if (kMode == HEAD_EXP) v[j] = -INFINITY;         // the target stays out of E, of the sum and of what a reference is held against
+                if (kMode == HEAD_DZ) {
+                  z_y = v[j];
+                } else {
+                  p.rows.z_target[row] = v[j];
+                  v[j] = -INFINITY;               // the target stays out of E, of the sum and of what a reference is held against
+                }
               }
           }
           float own = ref;                        // reference of these columns
@@ -496,8 +503,7 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
             for (int j = 4; j < 64; ++j) t4[j & 3] = fmaxf(t4[j & 3], v[j]);
             const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
             if (kMode == HEAD_STATS) {
-              own = top > m ? top : m;
-              if (own == -INFINITY) own = 0.f;
+              own = top > m ? top : m;            // -inf as long as there was nothing but the target
             } else if (live && top > ref + kAbove) {
               own = top;
               const int chunk = (n0 + c) >> 6;    // tiles start at multiples of 64 here
@@ -505,7 +511,7 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
               p.rows.above_ref[(int64_t)row * p.rows.chunks + chunk] = top;
             }
           }
-          const float shift = own * kLog2e;
+          const float shift = kMode == HEAD_STATS && own == -INFINITY ? 0.f : own * kLog2e;
           float p4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int j = 0; j < 64; ++j) {
@@ -518,12 +524,13 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
             sum += m > own ? part * exp2_fast((own - m) * kLog2e) : part;
             if (kMode == HEAD_STATS) return;
           } else {
-            if (mine) {
-#pragma unroll
-              for (int j = 0; j < 64; ++j) v[j] -= j == y - c ? 1.f : 0.f;
-            }
 #pragma unroll
             for (int j = 0; j < 64; ++j) v[j] *= up;         // rows that are not there: 0
+            if (mine) {
+              const float of_target = p.online ? -p.rows.of_target[row] / dz_unit(p.rows) : up * expm1f(z_y - ref);
+#pragma unroll
+              for (int j = 0; j < 64; ++j) v[j] = j == y - c ? of_target : v[j];
+            }
           }
 #pragma unroll 1
           for (int term = 0; term < p.terms; ++term) {
@@ -829,7 +836,25 @@ __device__ __forceinline__ float2 row_sums(const float2* part, int n_part, int r
   return all;
 }
 
-// Log-sum-exp and loss of every row that counts, from the tiles' maxima and sums.
+// The target joins the others, whose exponentials add up to `sum` relative to m: relative to its own logit z where that is the larger.
+struct JoinedTarget {
+  float top, over;                                // log-sum-exp = top + over
+  float loss, others;                             // lse - z; what the others' probabilities add up to
+  float scale;                                    // root of 1 / the sum of all
+};
+__device__ __forceinline__ JoinedTarget join_target(float m, float sum, float z) {
+  JoinedTarget t;
+  const float h = z > m ? exp2_fast((m - z) * (0.5f * kLog2e)) : 1.f;
+  const float others = sum * h * h, total = others + (z > m ? 1.f : exp2_fast((z - m) * kLog2e));
+  t.top = z > m ? z : m;
+  t.over = z > m ? log1pf(others) : logf(total);
+  t.loss = z > m ? t.over : m - z + t.over;       // not lse - z, which has been rounded at the size of the logits
+  t.others = others / total;
+  t.scale = h * rsqrtf(total);
+  return t;
+}
+
+// Log-sum-exp, loss and the target's share of dZ of every row that counts, from the tiles' maxima and sums.
 template <int kRowsEach>
 __global__ void __launch_bounds__(kFinishThreads)
 head_finish_kernel(HeadRows rows, const float2* part, int n_part, int rows_alloc, const float* weight, float* loss, float* lse) {
@@ -841,12 +866,13 @@ head_finish_kernel(HeadRows rows, const float2* part, int n_part, int rows_alloc
   const int64_t row = (int64_t)blockIdx.x * kRowsEach + threadIdx.x % kRowsEach;
   const float2 all = row_sums<kRowsEach>(part, n_part, rows_alloc, row, row < n, -INFINITY, met);
   if (threadIdx.x < kRowsEach && row < n) {
-    const float over = logf(all.y), l = all.x + over;
+    const JoinedTarget j = join_target(all.x, all.y, rows.z_target[row]);
+    const float l = j.top + j.over;
     const int t = rows.row[row];
     rows.lse[row] = l;
+    rows.of_target[row] = rows.up[row] * j.others;
     if (lse != nullptr) lse[t] = l;
-    // not l - z, which has been rounded at the size of the logits
-    if (loss != nullptr) loss[t] = (weight != nullptr ? weight[t] : 1.f) * (all.x - rows.z_target[row] + over);
+    if (loss != nullptr) loss[t] = (weight != nullptr ? weight[t] : 1.f) * j.loss;
   }
 }
 
@@ -885,15 +911,12 @@ __global__ void __launch_bounds__(kFinishThreads) head_merge_kernel(const MergeP
       rows.ref[row] = m;
       rows.sum[row] = sum;
       if (p.last) {
-        // the target, which no reference is held against, joins: relative to its own logit where that is the larger
-        const float z = rows.z_target[row], h = z > m ? exp2_fast((m - z) * (0.5f * kLog2e)) : 1.f;
-        const float others = sum * h * h, total = others + (z > m ? 1.f : exp2_fast((z - m) * kLog2e));
-        const float over = z > m ? log1pf(others) : logf(total);
+        const JoinedTarget j = join_target(m, sum, rows.z_target[row]);
         const int t = rows.row[row];
-        if (p.lse != nullptr) p.lse[t] = (z > m ? z : m) + over;
-        p.loss[t] = (p.weight != nullptr ? p.weight[t] : 1.f) * (z > m ? over : m - z + over);
-        rows.scale[row] = h * rsqrtf(total);
-        rows.of_target[row] = rows.up[row] * (others / total);
+        if (p.lse != nullptr) p.lse[t] = j.top + j.over;
+        p.loss[t] = (p.weight != nullptr ? p.weight[t] : 1.f) * j.loss;
+        rows.scale[row] = j.scale;
+        rows.of_target[row] = rows.up[row] * j.others;
       }
     }
   }
@@ -1352,6 +1375,7 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
                                       : launch_chained(chained, head_merge_kernel<32>, dim3((unsigned)ceil_div(T, 32)), dim3(kFinishThreads), 0, st, m));
       }
     } else {
+      q.online = forward;
       CWL_CUDA_TRY(launch_logits<HEAD_DZ>(logits, q, T, chained, st));
     }
     // where E / dZ is several numbers, the last block of each is stored whole, and DX reads no further

@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
         for (int j = 0; j < kRows; ++j)
           if (targets[j] == col) {
             p.rows.z_target[j] = z[j];
-            if (kMode == HEAD_EXP) z[j] = -INFINITY;             // the target stays out of E, of the sum and of what a reference is held against
+            z[j] = -INFINITY;                                    // the target stays out of E, of the sum and of what a reference is held against
           }
       }
       // the rows' maxima over the block's columns, 32 rows at a time
@@ -321,7 +321,8 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
       if (epi < n) {
         float sum = 0.f;
         for (int w = 0; w < 8; ++w) sum += meet[w * kRows + epi];
-        p.part[(int64_t)tile * p.rows_alloc + epi] = make_float2(common[epi], sum);
+        // the maximum of nothing but the target is -inf
+        p.part[(int64_t)tile * p.rows_alloc + epi] = make_float2(kMode == HEAD_STATS && sum == 0.f ? -INFINITY : common[epi], sum);
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");             // before the next tile's maxima
     }
