@@ -836,23 +836,32 @@ NS_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 class _FactorCall:
     """Factors with everything marshalled once, for calls that come every step: descriptors, iteration, workspace.  The tensors
-    are kept; they are read and written where they lie at every call."""
+    are kept; they are read and written where they lie at every call, and looked at anew where one has got other storage."""
 
-    def __init__(self, n: int, device: int, steps: int, coefficients: Sequence[float], eps: float, workspace: Optional[torch.Tensor],
-                 fill, keep):
-        self.n, self.device, self.keep = n, device, keep
-        self.factors = (CFactor * max(n, 1))()
-        for i in range(n):
-            fill(i, self.factors[i])
+    def __init__(self, keep, steps: int, coefficients: Sequence[float], eps: float, workspace: Optional[torch.Tensor]):
+        self.keep, self.n = keep, len(keep[0])
+        self._tensors = [t for tensors in keep for t in tensors if t is not None]
         a, b, c = coefficients
         self.iteration = CNewtonSchulz(int(steps), float(a), float(b), float(c), float(eps))
-        need = int(lib().cwl_orthogonalize_workspace_bytes(self.factors, n))
-        if workspace is None:
-            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=f"cuda:{device}")
-        assert workspace.dtype == torch.uint8 and workspace.is_contiguous() and workspace.get_device() == device
-        self.workspace = workspace
+        self._given, self.workspace = workspace, workspace
+        self._marshal()
 
-    def _stream(self, stream):
+    def _marshal(self) -> None:
+        at = list(map(torch.Tensor.data_ptr, self._tensors))
+        self.device = self._checked()
+        self.factors = (CFactor * max(self.n, 1))()
+        for i in range(self.n):
+            self._fill(i, self.factors[i])
+        need = max(int(lib().cwl_orthogonalize_workspace_bytes(self.factors, self.n)), 1)
+        if self._given is None and (self.workspace is None or self.workspace.numel() < need):
+            self.workspace = torch.empty(need, dtype=torch.uint8, device=f"cuda:{self.device}")
+        assert self.workspace.dtype == torch.uint8 and self.workspace.is_contiguous() and self.workspace.get_device() == self.device
+        self._at = at                            # last: a call whose tensors were refused looks at them again
+
+    def _ready(self, stream) -> int:
+        """The stream's handle, with descriptors of the tensors as they are now."""
+        if list(map(torch.Tensor.data_ptr, self._tensors)) != self._at:
+            self._marshal()
         assert torch._C._cuda_getDevice() == self.device      # launches go to the current device: everything has to be there
         return _stream_ptr(stream, self.device)
 
@@ -869,22 +878,26 @@ class OrthogonalizeCall(_FactorCall):
 
     def __init__(self, factors: Sequence[torch.Tensor], outs: Sequence[torch.Tensor], steps: int = 5,
                  coefficients: Sequence[float] = NS_COEFFICIENTS, eps: float = 1e-7, workspace: Optional[torch.Tensor] = None):
-        factors, outs = list(factors), list(outs)
+        super().__init__((list(factors), list(outs)), steps, coefficients, eps, workspace)
+
+    def _checked(self) -> int:
+        factors, outs = self.keep
         assert len(factors) == len(outs) and all(u.shape == o.shape for u, o in zip(factors, outs))
         here = _one_device(factors + outs)
         types, out_types = {u.dtype for u in factors} or {torch.float32}, {o.dtype for o in outs} or {torch.float32}
         assert len(types) == len(out_types) == 1 and types <= set(_DTYPES) and out_types <= set(_DTYPES)
         self.in_type, self.out_type = _DTYPES[types.pop()], _DTYPES[out_types.pop()]
+        return here
 
-        def fill(i, f):
-            u, o = factors[i], outs[i]
-            f.rows, f.cols = u.shape
-            f.grad, f.ld_grad, f.out, f.ld_out = _p(u), _row_stride(u, *u.shape), _p(o), _row_stride(o, *o.shape)
-        super().__init__(len(factors), here, steps, coefficients, eps, workspace, fill, (factors, outs))
+    def _fill(self, i: int, f: CFactor) -> None:
+        u, o = self.keep[0][i], self.keep[1][i]
+        f.rows, f.cols = u.shape
+        f.grad, f.ld_grad, f.out, f.ld_out = _p(u), _row_stride(u, *u.shape), _p(o), _row_stride(o, *o.shape)
 
     def __call__(self, stream: Optional[torch.cuda.Stream] = None) -> Sequence[torch.Tensor]:
+        st = self._ready(stream)
         _check("cwl_orthogonalize", lib().cwl_orthogonalize(self.factors, self.n, self.in_type, self.out_type, C.byref(self.iteration),
-                                                            _p(self.workspace), self.workspace.numel(), self._stream(stream)))
+                                                            _p(self.workspace), self.workspace.numel(), st))
         return self.keep[1]
 
 
@@ -905,8 +918,22 @@ class FactorStep(_FactorCall):
     def __init__(self, masters: Sequence[torch.Tensor], lows: Optional[Sequence[torch.Tensor]], grads: Sequence[torch.Tensor],
                  momenta: Sequence[torch.Tensor], steps: int = 5, coefficients: Sequence[float] = NS_COEFFICIENTS, eps: float = 1e-7,
                  scales: Optional[Sequence[float]] = None, workspace: Optional[torch.Tensor] = None):
-        masters, grads, momenta = list(masters), list(grads), list(momenta)
+        masters = list(masters)
         lows = [None] * len(masters) if lows is None else list(lows)
+        self._scales = scales
+        super().__init__((masters, lows, list(grads), list(momenta)), steps, coefficients, eps, workspace)
+
+    def of(self, masters: Sequence[torch.Tensor], lows: Optional[Sequence[torch.Tensor]], grads: Sequence[torch.Tensor],
+           momenta: Sequence[torch.Tensor]) -> "FactorStep":
+        """This call where these are its tensors, otherwise one like it of them."""
+        now = (masters, [None] * len(masters) if lows is None else lows, grads, momenta)
+        if all(len(a) == len(b) and all(x is y for x, y in zip(a, b)) for a, b in zip(self.keep, now)):
+            return self
+        it = self.iteration
+        return FactorStep(*now, it.steps, (it.a, it.b, it.c), it.eps, self._scales, self._given)
+
+    def _checked(self) -> int:
+        masters, lows, grads, momenta = self.keep
         assert len(masters) == len(lows) == len(grads) == len(momenta)
         here = _one_device(masters + grads + momenta + [t for t in lows if t is not None])
         types = {g.dtype for g in grads} or {torch.float32}
@@ -914,25 +941,24 @@ class FactorStep(_FactorCall):
         for p, low, g, m in zip(masters, lows, grads, momenta):
             assert p.dtype == m.dtype == torch.float32 and p.shape == g.shape == m.shape
             assert low is None or (low.dtype == torch.bfloat16 and low.shape == p.shape)
-        if scales is None:
-            scales = [max(1.0, p.shape[0] / p.shape[1]) ** 0.5 for p in masters]
-        assert len(scales) == len(masters)
+        assert self._scales is None or len(self._scales) == len(masters)
         self.in_type = _DTYPES[types.pop()]
+        return here
 
-        def fill(i, f):
-            p, low, g, m = masters[i], lows[i], grads[i], momenta[i]
-            f.rows, f.cols = p.shape
-            f.grad, f.ld_grad, f.momentum, f.ld_momentum = _p(g), _row_stride(g, *g.shape), _p(m), _row_stride(m, *m.shape)
-            f.out, f.ld_out, f.scale = _p(p), _row_stride(p, *p.shape), float(scales[i])
-            if low is not None:
-                f.low, f.ld_low = _p(low), _row_stride(low, *low.shape)
-        super().__init__(len(masters), here, steps, coefficients, eps, workspace, fill, (masters, lows, grads, momenta))
+    def _fill(self, i: int, f: CFactor) -> None:
+        p, low, g, m = (tensors[i] for tensors in self.keep)
+        f.rows, f.cols = p.shape
+        f.grad, f.ld_grad, f.momentum, f.ld_momentum = _p(g), _row_stride(g, *g.shape), _p(m), _row_stride(m, *m.shape)
+        f.out, f.ld_out = _p(p), _row_stride(p, *p.shape)
+        f.scale = max(1.0, f.rows / f.cols) ** 0.5 if self._scales is None else float(self._scales[i])
+        if low is not None:
+            f.low, f.ld_low = _p(low), _row_stride(low, *low.shape)
 
     def __call__(self, lr: float, momentum: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
                  stream: Optional[torch.cuda.Stream] = None) -> None:
+        st = self._ready(stream)
         _check("cwl_factor_step", lib().cwl_factor_step(self.factors, self.n, self.in_type, C.byref(self.iteration), lr, momentum,
-                                                        weight_decay, int(nesterov), _p(self.workspace), self.workspace.numel(),
-                                                        self._stream(stream)))
+                                                        weight_decay, int(nesterov), _p(self.workspace), self.workspace.numel(), st))
 
 
 def bf16_from_bits(bits, device="cuda") -> torch.Tensor:

@@ -67,6 +67,7 @@ class LadderDistiller:
         self.gradients()
         self.steps += 1
         if self.update is not None:
+            self.update = self.update.of(self.master, [self.A, self.B], [self.dA, self.dB], [m for m, _ in self.moments])
             self.update(self.lr)
             return
         b1, b2 = 0.9, 0.999

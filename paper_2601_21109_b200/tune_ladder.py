@@ -64,6 +64,7 @@ class LadderTuner:
     def step(self) -> None:
         """One training step on the current stream; no host synchronisation."""
         self.gradients()
+        self.update = self.update.of(self.master, [self.A, self.B], [self.dA, self.dB], self.moments)
         self.update(self.lr, self.momentum, self.weight_decay)
 
     def capture(self) -> "torch.cuda.CUDAGraph":
