@@ -480,13 +480,14 @@ cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY, int64_t l
  *           NULL: a backward call.  lse is an input, from the forward call, and dloss (DEV fp32 [T] or NULL, all 1) the
  *           upstream gradient of loss[t]; rows where it is 0 do not count either
  *   dX      DEV [T, d] or NULL;  dW  DEV [d, V] or NULL; of grad_dtype (CWL_F32 or CWL_BF16), aligned to their type, any
- *           row stride; overwritten; not overlapping an input
+ *           row stride; overwritten; overlapping neither X, W nor one another (lying between their rows is fine)
  *   workspace   DEV, at least cwl_head_loss_workspace_bytes(T, d, V, dX given, dW given) bytes, 256-byte aligned
  * Logits and all sums are fp32; what multiplies W and X in the gradients is bf16 where they are, and the sum of two bf16
  * numbers (three up to 512 rows) where they are fp32.  In a call for dX alone the target is not among it: its share stays fp32;
  * where dW is wanted it is rounded like the others.  Either way 1 - softmax(z)_y has the relative precision of the others'
  * probabilities (a backward call: of expm1(z_y - lse[t])), however sure a token is.  X of rows that count and W finite.  T == 0 writes zeros to dW.  Results do not depend on timing.
- * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (T or V > 2^24, d > 2^20), WORKSPACE, CUDA; TIMEOUT through *status_word. */
+ * Errors: INVALID_ARG (overlaps among them), SHAPE, UNSUPPORTED (T or V > 2^24, d > 2^20), WORKSPACE, CUDA; TIMEOUT through
+ * *status_word. */
 size_t     cwl_head_loss_workspace_bytes(int32_t T, int32_t d, int32_t V, int32_t want_dx, int32_t want_dw);
 cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw, int32_t T, int32_t d, int32_t V,
                          const int32_t* targets, const float* weight, const float* dloss,
@@ -508,10 +509,11 @@ cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw,
  *   workspace  DEV, at least cwl_orthogonalize_workspace_bytes(factors, n) bytes (which reads rows and cols only), 256-byte
  *              aligned; both calls
  * Any number of factors, rows and cols from 1, the smaller of them at most CWL_MAX_RANK, the larger at most 2^22; any row
- * stride, elements aligned to their type.  out must not overlap grad.
+ * stride, elements aligned to their type.  grad, momentum, out and low of a factor must not overlap (they may lie between one
+ * another's rows).
  * Results do not depend on timing, nor on which other factors share the call but for the order of sums over the longer side.
  * Errors: INVALID_ARG (NULLs, sizes below 1, steps outside 1..CWL_MAX_NS_STEPS, eps negative, momentum outside [0, 1), values
- * that are not finite, unknown types), SHAPE (strides, alignment), UNSUPPORTED (sizes), WORKSPACE, CUDA.  n == 0 is a no-op. */
+ * that are not finite, unknown types, overlaps), SHAPE (strides, alignment), UNSUPPORTED (sizes), WORKSPACE, CUDA.  n == 0 is a no-op. */
 #define CWL_MAX_NS_STEPS 16
 typedef struct {
   int32_t rows, cols;

@@ -57,6 +57,11 @@ cwl_status cwl_probe_read_mix(const void* ptr, size_t bytes, const void* hot, si
  * Errors: CUDA. */
 cwl_status cwl_trace_set(long long* slots, int32_t pair);
 
+/* The test of outputs against inputs that the tuning calls make: 1 where two matrices of `rows` rows of `width` bytes, `pitch` bytes
+ * apart, have a byte in common.  Nothing is read at the addresses. */
+int32_t cwl_debug_overlap(const void* a, int64_t rows_a, int64_t width_a, int64_t pitch_a,
+                          const void* b, int64_t rows_b, int64_t width_b, int64_t pitch_b);
+
 #ifdef __cplusplus
 }
 #endif

@@ -841,6 +841,7 @@ class _FactorCall:
     def __init__(self, keep, steps: int, coefficients: Sequence[float], eps: float, workspace: Optional[torch.Tensor]):
         self.keep, self.n = keep, len(keep[0])
         self._tensors = [t for tensors in keep for t in tensors if t is not None]
+        self._written = [t for k in self._WRITTEN for t in keep[k] if t is not None]
         a, b, c = coefficients
         self.iteration = CNewtonSchulz(int(steps), float(a), float(b), float(c), float(eps))
         self._given, self.workspace = workspace, workspace
@@ -849,6 +850,8 @@ class _FactorCall:
     def _marshal(self) -> None:
         at = list(map(torch.Tensor.data_ptr, self._tensors))
         self.device = self._checked()
+        written = [t.data_ptr() for t in self._written if t.numel()]
+        assert len(set(written)) == len(written), "a tensor would be written twice"
         self.factors = (CFactor * max(self.n, 1))()
         for i in range(self.n):
             self._fill(i, self.factors[i])
@@ -875,6 +878,7 @@ def _one_device(tensors: Sequence[torch.Tensor]) -> int:
 class OrthogonalizeCall(_FactorCall):
     """cwl_orthogonalize of a list of factors: ``outs[i]`` (fp32 or bf16) = Newton-Schulz of ``factors[i]`` (fp32, bf16 or
     fp16), every call anew from what the factors hold then."""
+    _WRITTEN = (1,)
 
     def __init__(self, factors: Sequence[torch.Tensor], outs: Sequence[torch.Tensor], steps: int = 5,
                  coefficients: Sequence[float] = NS_COEFFICIENTS, eps: float = 1e-7, workspace: Optional[torch.Tensor] = None):
@@ -914,6 +918,7 @@ class FactorStep(_FactorCall):
     """cwl_factor_step of a ladder's factors: the momentum takes the gradient in, the fp32 ``masters`` move by the
     orthogonalised momentum, and the bf16 copies ``lows`` (None: there are none) follow.  ``scales`` multiply each factor's update; by
     default sqrt(max(1, rows / cols))."""
+    _WRITTEN = (0, 1, 3)
 
     def __init__(self, masters: Sequence[torch.Tensor], lows: Optional[Sequence[torch.Tensor]], grads: Sequence[torch.Tensor],
                  momenta: Sequence[torch.Tensor], steps: int = 5, coefficients: Sequence[float] = NS_COEFFICIENTS, eps: float = 1e-7,

@@ -28,6 +28,29 @@ __host__ __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b -
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// A matrix in memory: `rows` of `width` bytes, `pitch` apart (at least their width, where there are several).
+struct MatrixSpan { uintptr_t at; int64_t rows, width, pitch; };
+inline MatrixSpan matrix_span(const void* at, int64_t ld, int64_t rows, int64_t cols, int elem) {
+  return MatrixSpan{reinterpret_cast<uintptr_t>(at), rows, cols * elem, (rows > 1 ? ld : cols) * elem};
+}
+// Do two matrices have a byte in common?  Rows that lie between the other's rows (columns of one buffer) do not count.
+inline bool overlap(const MatrixSpan& a, const MatrixSpan& b) {
+  if (a.at == 0 || b.at == 0 || a.rows <= 0 || b.rows <= 0 || a.width <= 0 || b.width <= 0) return false;
+  if (a.at > b.at) return overlap(b, a);
+  const int64_t off = (int64_t)(b.at - a.at);      // a begins first
+  if (off >= (a.rows - 1) * a.pitch + a.width) return false;
+  if (a.pitch == b.pitch) {
+    const int64_t within = off % a.pitch;          // where b's rows lie in a's
+    return within < a.width || within + b.width > a.pitch;
+  }
+  for (int64_t i = 0; i < b.rows; ++i) {           // the last of a's rows that begins before a row of b ends
+    const int64_t begin = off + i * b.pitch, end = begin + b.width;
+    const int64_t k = (end - 1) / a.pitch < a.rows - 1 ? (end - 1) / a.pitch : a.rows - 1;
+    if (k * a.pitch + a.width > begin) return true;
+  }
+  return false;
+}
+
 // Programmatic dependent launch.  A kernel launched with launch_chained() may have its CTAs placed while the kernel
 // before it in the stream is still running; it must call pdl_wait() before its first access to global memory, which
 // returns once that kernel has completed and its writes are visible.  pdl_launch_dependents() lets the NEXT chained

@@ -1052,9 +1052,21 @@ cwl_status run_group(const Item* items, int n, FactorCommon common, Fill fill, v
   return CWL_OK;
 }
 
+// A factor's matrices read and written by the same call, by different blocks: none may lie in another's place.
+bool shares_memory(const cwl_factor& f, bool step, int in_bytes, int out_bytes) {
+  const MatrixSpan at[4] = {matrix_span(f.grad, f.ld_grad, f.rows, f.cols, in_bytes), matrix_span(f.out, f.ld_out, f.rows, f.cols, out_bytes),
+                            matrix_span(f.momentum, f.ld_momentum, f.rows, f.cols, 4), matrix_span(f.low, f.ld_low, f.rows, f.cols, 2)};
+  for (int i = 0; i < (step ? 4 : 2); ++i)
+    for (int j = 0; j < i; ++j)
+      if (overlap(at[i], at[j])) return true;
+  return false;
+}
+
 template <bool kStep, typename Item, typename Fill>
 cwl_status run_factors(const Item* items, int n, const FactorCommon& common, Fill fill, void* workspace, size_t workspace_bytes, void* stream) {
   if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < factor_bytes(items, n)) return CWL_ERR_WORKSPACE;
+  for (int i = 0; i < n; ++i)
+    if (shares_memory(items[i], kStep, common.in_type == CWL_F32 ? 4 : 2, common.out_type == CWL_F32 ? 4 : 2)) return CWL_ERR_INVALID_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const bool chained = !stream_is_capturing(st);
   for (int i = 0; i < n; i += kMostFactors) {

@@ -1280,6 +1280,10 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
   if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
       workspace_bytes < cwl_head_loss_workspace_bytes(T, d, V, dX != nullptr, dW != nullptr))
     return CWL_ERR_WORKSPACE;
+  // gradients are written while X and W are still being read
+  const MatrixSpan x_at = matrix_span(X, ldx, T, d, 2), w_at = matrix_span(W, ldw, d, V, 2), dx_at = matrix_span(dX, lddx, T, d, es),
+                   dw_at = matrix_span(dW, lddw, d, V, es);
+  if (overlap(dx_at, x_at) || overlap(dx_at, w_at) || overlap(dw_at, x_at) || overlap(dw_at, w_at) || overlap(dx_at, dw_at)) return CWL_ERR_INVALID_ARG;
   const HeadLayout l = head_layout(T, d, V, forward, dX != nullptr, dW != nullptr, es == 4);
   const bool online = l.from_e && forward;
   // a sector of 32 bytes for each number of the targets' columns, or all of W

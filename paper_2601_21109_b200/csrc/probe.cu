@@ -162,4 +162,8 @@ extern "C" cwl_status cwl_probe_read(const void* ptr, size_t bytes, int32_t* sta
                               static_cast<const unsigned char*>(ptr), (unsigned long long)bytes, status_word));
   return CWL_OK;
 }
+extern "C" int32_t cwl_debug_overlap(const void* a, int64_t rows_a, int64_t width_a, int64_t pitch_a, const void* b, int64_t rows_b, int64_t width_b,
+                                     int64_t pitch_b) {
+  return cwl::overlap(cwl::matrix_span(a, pitch_a, rows_a, width_a, 1), cwl::matrix_span(b, pitch_b, rows_b, width_b, 1)) ? 1 : 0;
+}
 #endif  // CWL_TEST_HOOKS
