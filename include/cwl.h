@@ -503,7 +503,8 @@ cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, int64_t ldw,
  *   cwl_orthogonalize  out = O                             of `out_dtype` (CWL_F32 or CWL_BF16)
  *   cwl_factor_step    momentum = beta momentum + grad;    U = grad + beta momentum (nesterov != 0) or momentum
  *                      out = (1 - lr weight_decay) out - lr scale O;    low = bf16(out)
- * A factor of zeros gives zeros (momentum and weight decay apply all the same); one with NaN or infinities gives NaN everywhere.
+ * A factor of zeros gives zeros (momentum and weight decay apply all the same); one with NaN or infinities gives NaN everywhere;
+ * with eps = 0 any other gives what its multiples would, to the ends of its type's range.
  *   factors    HOST array of n, copied at call time; pointers inside are DEV; different factors must not overlap
  *   iteration  HOST
  *   workspace  DEV, at least cwl_orthogonalize_workspace_bytes(factors, n) bytes (which reads rows and cols only), 256-byte

@@ -54,7 +54,7 @@ struct FactorCommon {
   int steps;
   double a, b, c, eps;
   double* partial;                                 // GRAM: [block][64][64]
-  float* q;                                        // [factor] R x R, each `q_stride` apart
+  float* q;                                        // [factor] R x R, each `q_stride` apart, and at the end of each what U is lifted by
   int64_t q_stride;
 };
 template <int kMost>
@@ -167,6 +167,20 @@ __device__ __forceinline__ void lower_tile(int i, int& ti, int& tj) {
   while (i > ti) { i -= ti + 1; ++ti; }
   tj = i;
 }
+
+// 1 / (norm + eps) as Q and APPLY take it: what Q is multiplied with, and, where fp32 would not hold that times Q (norms near either
+// end of its range), the powers of two, one after the other, that APPLY lifts U by instead.  Within 2^32 of 1 the latter are 1.
+constexpr int kLiftFrom = 32;
+struct SplitUnit { double of_q; float2 lift; };
+__device__ __forceinline__ SplitUnit split_unit(double unit) {
+  SplitUnit s{unit, make_float2(1.f, 1.f)};
+  if (isfinite(unit) && unit != 0.0) {             // a factor that is not finite, or zeros
+    const int e = ilogb(unit);
+    if (e > kLiftFrom || e < -kLiftFrom) s = SplitUnit{scalbn(unit, -e), make_float2(scalbnf(1.f, e / 2), scalbnf(1.f, e - e / 2))};
+  }
+  return s;
+}
+__host__ __device__ __forceinline__ float2* lift_at(float* q, int64_t q_stride) { return reinterpret_cast<float2*>(q + q_stride) - 1; }
 
 // ------------------------------------------------------------------------------------------------------------- GRAM
 constexpr int kGramThreads = 256;
@@ -596,7 +610,9 @@ __global__ void __launch_bounds__(kIterThreads) iterate_kernel(const __grid_cons
   }
   __syncthreads();
   float* q = a.q + blockIdx.x * a.q_stride;
-  for (int at = tid; at < R * R; at += kIterThreads) q[at] = (float)(Q[(at / R) * kIterLd + at % R] * unit);
+  const SplitUnit split = split_unit(unit);
+  for (int at = tid; at < R * R; at += kIterThreads) q[at] = (float)(Q[(at / R) * kIterLd + at % R] * split.of_q);
+  if (tid == 0) *lift_at(q, a.q_stride) = split.lift;
 }
 
 // ------------------------------------------------------------------------------------------------- ITERATE, R > 64
@@ -607,7 +623,7 @@ struct BigArgs {
   const double* partial;
   double* big;                                     // [factor of this list][G, P, S, Q, Q of the next step][stride]
   int64_t stride;
-  double* unit;                                    // [factor of this list] 1 / (norm + eps)
+  double* unit;                                    // [factor of this list] what Q is multiplied with at the end
   float* q; int64_t q_stride;
   uint16_t which[kMostFactors], R[kMostFactors];   // place in the call's list, short side
   int first[kMostFactors], slices[kMostFactors];   // GRAM's blocks
@@ -663,12 +679,16 @@ __global__ void __launch_bounds__(kBigGramThreads) big_gram_kernel(const __grid_
     c += bj * 64;
     if (!other_half && r < Rp && c < Rp) G[(int64_t)r * Rp + c] = G[(int64_t)c * Rp + r] = v * unit * unit;
   }
-  if (blockIdx.x == 0 && tid == 0) a.unit[blockIdx.y] = unit;
+  if (blockIdx.x == 0 && tid == 0) {
+    const SplitUnit split = split_unit(unit);
+    a.unit[blockIdx.y] = split.of_q;
+    *lift_at(a.q + a.which[blockIdx.y] * a.q_stride, a.q_stride) = split.lift;
+  }
 }
 
 // One product a launch (two where they do not depend on one another):
 //   POLY    P = a I + b G + c G G; in the first step this is Q too
-//   SPREAD  S = P G, and Q' = P Q (z = 1, or alone in the last step, where it leaves as fp32, times 1 / (norm + eps))
+//   SPREAD  S = P G, and Q' = P Q (z = 1, or alone in the last step, where it leaves as fp32, times its unit)
 //   GRAM    G = P S
 enum : int { BIG_POLY = 0, BIG_SPREAD = 1, BIG_GRAM = 2 };
 // A block takes 16 x 16 entries, each of its warps a quarter of the sums, which it brings in itself and waits for alone: at R = 256
@@ -771,7 +791,7 @@ constexpr int kApplyK = 32;
 constexpr int kApplyLdX = kApplyLong + 4, kApplyLdQ = kApplyShort + 4;
 
 template <bool kTall, bool kStep, int kElem>
-__device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& f, const float* q, int long0, int short0, float* xs, float* qs) {
+__device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& f, const float* q, float2 lift, int long0, int short0, float* xs, float* qs) {
   const int R = short_side(f), n = long_side(f), tid = threadIdx.x;
   const bool vec_u = vec_rows(f.u, f.ldu, kElem), vec_m = kStep && vec_rows(f.m, f.ldm, 4);
   const bool vec_q = (R & 3) == 0;
@@ -821,12 +841,15 @@ __device__ __forceinline__ void apply_tile(const FactorCommon& a, const Factor& 
       y[i] = load4(q, (int64_t)k * R + s, CWL_F32, vec_q, left);
     }
   };
+  const bool lifted = lift.x != 1.f || lift.y != 1.f;
   auto made = [&](int i) {                         // U from what was loaded
-    if (!inside) return x[i];
-    const float4 g = raw_four<kElem>(reinterpret_cast<const uint8_t*>(&x[i]), a.in_type == CWL_BF16);
-    if (!kStep) return g;
-    const float4 m = mom[kStep ? i : 0];
-    return step_u(a, g, m);
+    float4 u = x[i];
+    if (inside) {
+      u = raw_four<kElem>(reinterpret_cast<const uint8_t*>(&x[i]), a.in_type == CWL_BF16);
+      if (kStep) u = step_u(a, u, mom[kStep ? i : 0]);
+    }
+    if (lifted) u = make_float4(u.x * lift.x * lift.y, u.y * lift.x * lift.y, u.z * lift.x * lift.y, u.w * lift.x * lift.y);
+    return u;
   };
   fetch(0);
   for (int k0 = 0; k0 < R; k0 += kApplyK) {
@@ -909,9 +932,10 @@ __global__ void __launch_bounds__(kApplyThreads, 2) apply_factors_kernel(const _
   const Factor& f = args.f[at];
   const int unit = blockIdx.x - f.first, row_tiles = (short_side(f) + kApplyShort - 1) / kApplyShort;
   const int long0 = unit / row_tiles * kApplyLong, short0 = unit % row_tiles * kApplyShort;
-  const float* q = args.c.q + at * args.c.q_stride;
-  if (f.rows > f.cols) apply_tile<true, kStep, kElem>(args.c, f, q, long0, short0, xs, qs);
-  else apply_tile<false, kStep, kElem>(args.c, f, q, long0, short0, xs, qs);
+  float* q = args.c.q + at * args.c.q_stride;
+  const float2 lift = *lift_at(q, args.c.q_stride);
+  if (f.rows > f.cols) apply_tile<true, kStep, kElem>(args.c, f, q, lift, long0, short0, xs, qs);
+  else apply_tile<false, kStep, kElem>(args.c, f, q, lift, long0, short0, xs, qs);
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -943,7 +967,7 @@ FactorPlan factor_plan(const Item* items, int n) {
     const int R = items[i].rows < items[i].cols ? items[i].rows : items[i].cols, len = items[i].rows < items[i].cols ? items[i].cols : items[i].rows;
     p.blocks += (int64_t)block_pairs(R) * ceil_div(len, p.slice);
   }
-  p.q_stride = ((int64_t)p.most_R * p.most_R + 3) / 4 * 4;
+  p.q_stride = ((int64_t)p.most_R * p.most_R + 3) / 4 * 4 + 4;
   p.stride = (int64_t)padded(big) * padded(big);
   p.q = align256((size_t)p.blocks * 64 * 64 * 8);
   p.big = p.q + align256((size_t)p.q_stride * n * 4);
