@@ -8,6 +8,8 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import functools
+import inspect
 import os
 from typing import NamedTuple, Optional, Sequence
 
@@ -324,6 +326,37 @@ def _check(call: str, status: int) -> None:
         raise CwlError(call, status)
 
 
+def _tensors_in(x):
+    if torch.is_tensor(x):
+        yield x
+    elif isinstance(x, (list, tuple)):
+        for y in x:
+            yield from _tensors_in(y)
+    elif isinstance(x, dict) or hasattr(x, "__dict__"):
+        yield from _tensors_in(list((x if isinstance(x, dict) else vars(x)).values()))
+
+
+def _on_its_stream(call):
+    """For calls that may be given a ``stream``: workspaces and outputs that they allocate belong to it.  A workspace is free again
+    as soon as the call returns, for what is queued behind it on that stream and for nothing else; outputs are known to be used
+    on the caller's stream, too."""
+    at = list(inspect.signature(call).parameters).index("stream")
+
+    @functools.wraps(call)
+    def on(*args, **kw):
+        stream = args[at] if len(args) > at else kw.get("stream")
+        if stream is None:
+            return call(*args, **kw)
+        callers = torch.cuda.current_stream()
+        with torch.cuda.stream(stream):
+            out = call(*args, **kw)
+        for t in _tensors_in(out):
+            t.record_stream(callers)
+        return out
+    return on
+
+
+@_on_its_stream
 def cwl_score_tokens(logits: torch.Tensor, score: Optional[torch.Tensor] = None,
                      stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
     """score[t] = normalised softmax entropy of logits[t, :] (fp32 [T, V] on the device)."""
@@ -336,6 +369,7 @@ def cwl_score_tokens(logits: torch.Tensor, score: Optional[torch.Tensor] = None,
     return score
 
 
+@_on_its_stream
 def cwl_score_tokens_mixed(logits: torch.Tensor, token_ids: torch.Tensor, cu_seqlens: torch.Tensor,
                            w_entropy: float, w_novelty: float, w_prior: float, ngram: int, context: int,
                            prior_span: int, score: Optional[torch.Tensor] = None,
@@ -358,6 +392,7 @@ def cwl_partition_workspace_bytes(T: int, n_seq: int) -> int:
     return int(lib().cwl_partition_workspace_bytes(T, n_seq))
 
 
+@_on_its_stream
 def cwl_partition(score: torch.Tensor, cu_seqlens: torch.Tensor, policy: CPolicy,
                   table: Optional[DeviceChunkTable] = None, workspace: Optional[torch.Tensor] = None,
                   status_word: Optional[torch.Tensor] = None,
@@ -377,6 +412,7 @@ def cwl_partition(score: torch.Tensor, cu_seqlens: torch.Tensor, policy: CPolicy
     return table
 
 
+@_on_its_stream
 def cwl_batch_align(score: torch.Tensor, cu_seqlens: torch.Tensor, policy: CPolicy, n_buckets: int,
                     table: Optional[DeviceChunkTable] = None, workspace: Optional[torch.Tensor] = None,
                     status_word: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
@@ -413,6 +449,7 @@ def cwl_apply_noalloc_scratch_need(T: int, d_in: int, d_out: int, R: int) -> int
     return int(lib().cwl_apply_noalloc_scratch_need(T, d_in, d_out, R))
 
 
+@_on_its_stream
 def cwl_apply(X: torch.Tensor, W: torch.Tensor, A: Optional[torch.Tensor], B: Optional[torch.Tensor],
               table: Optional[DeviceChunkTable], window: int, Y: Optional[torch.Tensor] = None,
               workspace: Optional[torch.Tensor] = None, status_word: Optional[torch.Tensor] = None,
@@ -450,6 +487,7 @@ def cwl_apply_grouped_workspace_bytes(T: int, d_in: int, d_outs: Sequence[int], 
     return int(lib().cwl_apply_grouped_workspace_bytes(T, d_in, len(d_outs), arr, R))
 
 
+@_on_its_stream
 def cwl_apply_grouped(X: torch.Tensor, Ws: Sequence[torch.Tensor], As: Optional[Sequence[torch.Tensor]],
                       Bs: Optional[Sequence[torch.Tensor]], table: Optional[DeviceChunkTable], window: int,
                       Ys: Optional[Sequence[torch.Tensor]] = None, workspace: Optional[torch.Tensor] = None,
@@ -511,6 +549,7 @@ class DeviceStream:
         return self.gates[:self.n_seq].cpu().numpy().view(dt).reshape(self.n_seq)
 
 
+@_on_its_stream
 def cwl_apply_rows(X: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.Tensor, gates: torch.Tensor,
                    Y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                    status_word: Optional[torch.Tensor] = None,
@@ -529,6 +568,7 @@ def cwl_apply_rows(X: torch.Tensor, W: torch.Tensor, A: torch.Tensor, B: torch.T
     return Y
 
 
+@_on_its_stream
 def cwl_ladder_build(A: torch.Tensor, B: torch.Tensor, want_f32: bool = True,
                      stream: Optional[torch.cuda.Stream] = None) -> dict:
     """SVD-ordered adapter factors of a trained (A [d_in, R], B [R, d_out]) pair, bf16 on the device (offline).
@@ -670,6 +710,7 @@ class TokenLogprobs:
         self._ptrs = (_p(self.logprob), _p(self.lse), _p(self.entropy), _p(self.top_ids), _p(self.top_logprobs))
 
 
+@_on_its_stream
 def cwl_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top_k: int = 0, temperature: float = 1.0,
                        out: Optional[TokenLogprobs] = None, status_word: Optional[torch.Tensor] = None,
                        stream: Optional[torch.cuda.Stream] = None) -> TokenLogprobs:
@@ -692,6 +733,7 @@ def cwl_token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = N
     return out
 
 
+@_on_its_stream
 def cwl_distill_topk(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_values: torch.Tensor, teacher: str = "logits",
                      temperature: float = 1.0, weight: Optional[torch.Tensor] = None, dloss: Optional[torch.Tensor] = None,
                      want_loss: bool = True, want_grad: bool = True, loss: Optional[torch.Tensor] = None,
@@ -733,6 +775,7 @@ def cwl_apply_grads_workspace_bytes(T: int, d_in: int, d_out: int, R: int) -> in
     return int(lib().cwl_apply_grads_workspace_bytes(T, d_in, d_out, R))
 
 
+@_on_its_stream
 def cwl_apply_grads(X: torch.Tensor, dY: torch.Tensor, A: torch.Tensor, B: torch.Tensor, table: DeviceChunkTable, window: int,
                     dA: Optional[torch.Tensor] = None, dB: Optional[torch.Tensor] = None,
                     grad_dtype: torch.dtype = torch.bfloat16, workspace: Optional[torch.Tensor] = None,
@@ -785,6 +828,7 @@ class HeadLoss(NamedTuple):
     dW: Optional[torch.Tensor]
 
 
+@_on_its_stream
 def cwl_head_loss(X: torch.Tensor, W: torch.Tensor, targets: torch.Tensor, weight: Optional[torch.Tensor] = None,
                   dloss: Optional[torch.Tensor] = None, want_loss: bool = True, want_dx: bool = False, want_dw: bool = False,
                   loss: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, dX: Optional[torch.Tensor] = None,
@@ -866,6 +910,8 @@ class _FactorCall:
         if list(map(torch.Tensor.data_ptr, self._tensors)) != self._at:
             self._marshal()
         assert torch._C._cuda_getDevice() == self.device      # launches go to the current device: everything has to be there
+        if stream is not None:
+            self.workspace.record_stream(stream)              # this call may be dropped before it has run
         return _stream_ptr(stream, self.device)
 
 
@@ -905,6 +951,7 @@ class OrthogonalizeCall(_FactorCall):
         return self.keep[1]
 
 
+@_on_its_stream
 def cwl_orthogonalize(factors: Sequence[torch.Tensor], outs: Optional[Sequence[torch.Tensor]] = None, steps: int = 5,
                       coefficients: Sequence[float] = NS_COEFFICIENTS, eps: float = 1e-7, out_dtype: torch.dtype = torch.float32,
                       workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> Sequence[torch.Tensor]:
