@@ -1242,8 +1242,9 @@ bool bad_operand(const void* ptr, int64_t ld, int64_t cols, int64_t rows) {
 extern "C" size_t cwl_head_loss_workspace_bytes(int32_t T, int32_t d, int32_t V, int32_t want_dx, int32_t want_dw) {
   using namespace cwl;
   if (T <= 0 || d <= 0 || V <= 0 || T > kHeadMaxRows || V > kHeadMaxRows || d > kHeadMaxWidth) return 0;
-  size_t most = 0;
-  for (int f32 = 0; f32 <= 1; ++f32) {
+  // of the loss alone, too: a training loop's evaluation runs in the workspace of its steps
+  size_t most = head_layout(T, d, V, true, false, false, false).total;
+  for (int f32 = 0; f32 <= 1 && (want_dx != 0 || want_dw != 0); ++f32) {
     for (int forward = 0; forward <= 1; ++forward) {
       const size_t n = head_layout(T, d, V, forward != 0, want_dx != 0, want_dw != 0, f32 != 0).total;
       if (n > most) most = n;
