@@ -55,6 +55,8 @@ inline bool overlap(const MatrixSpan& a, const MatrixSpan& b) {
 // before it in the stream is still running; it must call pdl_wait() before its first access to global memory, which
 // returns once that kernel has completed and its writes are visible.  pdl_launch_dependents() lets the NEXT chained
 // launch do the same with respect to this kernel.  Both do nothing in a kernel launched the ordinary way.
+// A kernel may read before pdl_wait() what no kernel since a COMPLETED one has written: the first kernel of its call has to wait
+// before it lets others begin, and every launch of the call up to the reader must leave that memory alone (head_few_kernel and W).
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

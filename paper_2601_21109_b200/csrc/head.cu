@@ -695,7 +695,7 @@ __global__ void __launch_bounds__(kRowsThreads) head_rows_kernel(const RowsParam
   __shared__ int counts[kRowsThreads];
   __shared__ __align__(16) __nv_bfloat16 column[kRowsColumn];
   pdl_wait();
-  pdl_launch_dependents();                        // after the wait: head_few_kernel fetches W by that
+  pdl_launch_dependents();                        // after the wait and never before it: head_few_kernel fetches W by that
   if (p.online && p.reference) {
 #pragma unroll 8
     for (int j = threadIdx.x; j < kRowsColumn; j += kRowsThreads) column[j] = j < p.d ? p.W[(int64_t)j * p.ldw] : __float2bfloat16_rn(0.f);
@@ -1321,6 +1321,7 @@ extern "C" cwl_status cwl_head_loss(const void* X, int64_t ldx, const void* W, i
   int blocks = ceil_div(T, 8);
   if (blocks > 148) blocks = 148;
   r.per_block = ceil_div(T, blocks);
+  // first of the call's launches: head_few_kernel reads W before its own wait on the strength of this one's
   CWL_CUDA_TRY(launch_chained(chained, head_rows_kernel, dim3((unsigned)blocks), dim3(kRowsThreads), 0, st, r));
   if (l.from_e) {
     const __nv_bfloat16* w = static_cast<const __nv_bfloat16*>(W);

@@ -109,8 +109,11 @@ __global__ void __launch_bounds__(kFewThreads, 1) head_few_kernel(const __grid_c
   const int n_chunks = (n_kb + kFewChunk - 1) / kFewChunk;
   const int boxes = (p.tn + 63) / 64, m_tiles = (boxes + 1) / 2;
   const int stage_bytes = p.stage_bytes, n_stages = p.stages, x_at = boxes * kHBox;
-  // W is there once head_rows_kernel is past its own wait, after which it lets this kernel begin: as much of it as the ring
-  // holds is fetched beside the kernels ahead (a tenth of it for 4096 -> 32000; one row 53.8 -> 52.1 us, 48 rows 143 -> 139)
+  // Before pdl_wait().  W is there once head_rows_kernel is past its own wait, after which it lets the next kernel begin: all that was
+  // launched before this call has completed then, and nothing of this call writes W (outputs that overlap it are refused).
+  // head_rows_kernel has to stay the first launch of the call and to let others begin only after its wait; what is launched
+  // between the two (head_gather_kernel, DX, sums) may let the next one begin whenever it likes.  As much of W as the ring holds
+  // is fetched beside the kernels ahead (a tenth of it for 4096 -> 32000; one row 53.8 -> 52.1 us, 48 rows 143 -> 139)
   const int ahead = min(n_stages, n_kb - (CWL_WITHHELD(p) ? 1 : 0));
   if (warp == 0 && lane >= 1 && lane <= boxes) {
     for (int b = 0; b < ahead; ++b)
