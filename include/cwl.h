@@ -482,7 +482,7 @@ cwl_status cwl_apply_grads(const void* X, int64_t ldx, const void* dY, int64_t l
  *   dX      DEV [T, d] or NULL;  dW  DEV [d, V] or NULL; of grad_dtype (CWL_F32 or CWL_BF16), aligned to their type, any
  *           row stride; overwritten; overlapping neither X, W nor one another (lying between their rows is fine)
  *   workspace   DEV, at least cwl_head_loss_workspace_bytes(T, d, V, dX given, dW given) bytes, 256-byte aligned; one made for
- *               gradients does for the loss alone, too
+ *               gradients does for the loss alone, too, not always one made for more rows for fewer
  * Logits and all sums are fp32; what multiplies W and X in the gradients is bf16 where they are, and the sum of two bf16
  * numbers (three up to 512 rows) where they are fp32.  In a call for dX alone the target is not among it: its share stays fp32;
  * where dW is wanted it is rounded like the others.  Either way 1 - softmax(z)_y has the relative precision of the others'

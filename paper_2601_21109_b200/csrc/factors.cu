@@ -13,12 +13,12 @@
 //   ITERATE  R <= 64: a block a factor, all in shared memory.  R > 64: launches of 16 x 16 tiles over L2-resident matrices
 //   APPLY    a block per (factor, 128 columns of the long side, 64 rows): Q U in 32 bits, and the update
 //
-// What bounds it (one B200).  Many factors (448 of R = 64, bf16 gradients, the update: 1.44 ms; floor 0.49, 3.2 GB): GRAM 0.55 ms, 64-bit
+// What bounds it (one B200).  Many factors (448 of R = 64, bf16 gradients, the update: 1.45 ms; floor 0.49, 3.2 GB): GRAM 0.55 ms, 64-bit
 // products at 58 % of the 18.5 T/s that a loop of nothing else reaches (0.32 ms), beside 10 bytes an element; iteration 0.13,
-// at 90 % of that rate; APPLY 0.74, 10.2 G multiply-adds at 38 % of the units' rate beside 16 bytes an element: 16 warps an SM wait for
+// at 90 % of that rate; APPLY 0.75, 10.2 G multiply-adds at 38 % of the units' rate beside 16 bytes an element: 16 warps an SM wait for
 // shared memory and for one another's phases (4 x 8 outputs a thread two to an instruction, 8 x 8 outputs, copies ahead through shared
 // memory, several tiles a block: 0.79 to 1.01; pairs of tf32 on the tensor cores: 0.675, and O 1.7 times as far
-// off).  Few factors: four launches that wait for one another (a pair of 4096 x 64: 55 us, of which the iteration's 17 products in one SM
+// off).  Few factors: four launches that wait for one another (a pair of 4096 x 64: 56 us, of which the iteration's 17 products in one SM
 // 34, 20 of them the SM's 64-bit rate; four SMs a factor with stores to one another took 68 when one took 62).  R > 64: a launch a product of the iteration, 6.6 us each at R = 256 (256 x 11008 and two more: 230 to 250 us, 92 of them
 // these; one cooperative launch with a barrier between products: 118).
 #include <cuda_bf16.h>

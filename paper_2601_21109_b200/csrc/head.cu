@@ -28,13 +28,15 @@
 // truncated at every step of 16 (2.4e-6 of a sum of 256 steps, measured on the logits of d = 4096), are added up in fp32 after
 // every kChunkBlocks K blocks, over the terms.  dZ is relative to the first row's up: rows of one weight are then not rounded twice.
 //
+// bf16 rows that outgrow their reference are rounded a second time when head_merge_kernel puts them on the new one (2^-9 again).
+//
 // What bounds it (one B200): the tensor cores, under the power cap once a call lasts.  16384 rows, 4096 -> 32000, loss and dX: 6.9 to
-// 7.2 ms, of which the two products take 3.0 + 3.1 (1.39 PFLOP/s where a library's product keeps up 1.41, 1.68 in bursts), the gather
-// 0.15, listing rows and references 0.05, the merges 0.04; 1536 of 2048 rows: 0.70 to 0.80 ms, 0.30 + 0.33 + 0.053 + 0.017.  Tensor
+// 7.3 ms, of which the two products take 3.0 + 3.1 (1.39 PFLOP/s where a library's product keeps up 1.41, 1.68 in bursts), the gather
+// 0.15, listing rows and references 0.05, the merges 0.04; 1536 of 2048 rows: 0.70 to 0.81 ms, 0.30 + 0.33 + 0.053 + 0.017.  Tensor
 // pipe active 79 % in EXP and 84 % in DX.  Tiles of 256 x 512 a pair of CTAs, because with 256 x 256 operands reach shared
 // memory no faster than they are used; what the epilogue of a tile leaves uncovered is 2 % of it at d = 4096 and 15 % at d = 1024
-// (4000 rows of 131072: 0.89 ms, 1.2 PFLOP/s; pipe 66 %): it hands the first 256 columns back before the others, and the
-// next tile's products of as many K blocks as the ring holds start there.  fp32 gradients: two products for one, 2.6 ms for 2047
+// (4000 rows of 131072: 0.89 to 0.94 ms, 1.2 PFLOP/s; pipe 66 %): it hands the first 256 columns back before the others, and the
+// next tile's products of as many K blocks as the ring holds start there.  fp32 gradients: two products for one, 2.7 ms for 2047
 // rows, 2048 -> 50021, dX and dW.
 #include "cluster.cuh"
 #include "cwl_common.cuh"
@@ -401,7 +403,9 @@ head_kernel(const __grid_constant__ HeadMaps maps, const __grid_constant__ HeadP
     const int quad = warp & 3;                    // tensor-memory lanes this warp may read
     const int chalf = (warp - 2) >> 2;            // the two warps of a quadrant take alternate chunks of columns
     const uint32_t buf = out_bufs + (uint32_t)(warp - 2) * kHOutBuf;
-    float held[2][64];                            // kSums: the chunks' sums of this warp's columns
+    // kSums: the chunks' sums of this warp's columns.  Beside the 64 numbers at work they do not fit 168 registers (320 threads are
+    // given them as 384 would be): STATS spills 0.5 KB a thread, EXP 0.7, DZ 0.7, which is in what these sums are said to cost above.
+    float held[2][64];
     uint32_t local = 0;
     HeadItem t;
     for (int i = 0; head_item(i, work, p, t); ++i) {

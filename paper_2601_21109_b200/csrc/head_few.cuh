@@ -7,7 +7,7 @@
 // vocabulary and all rows a thread.  Single blocks, no pairs: columns are dealt evenly over the SMs, to eight.
 //
 // Bound by HBM: one row, 4096 -> 32000: 43.5 us, 262 MB at 6.0 TB/s (head_kernel: 57 with tiles of 448 columns, 84 with sums in
-// fp32); 48 rows, EXP: 54 us (88); 128 rows, STATS: 61 us (66).
+// fp32); 48 rows, EXP: 54 us (88); 128 rows, STATS: 61 to 64 us (66), spills of 0.5 KB a thread among them.
 #pragma once
 
 constexpr int kFewRows = 128;                             // of STATS
